@@ -1,10 +1,10 @@
 """Serving operators over a rotated, pruned cache: the 8-bit cache and the attention of drafted tokens.
 
 Five operators on one attention layer, each as a user calls it through the binding and in its plain form:
-  write    a prompt's Keys and Values into the 8-bit caches, and these read back   rk_compress_q8, rk_unpack_cache_q8
-  append   one token a sequence into the 8-bit caches, and these read back          rk_append_q8, rk_unpack_cache_q8
-  decode   one token's attention over the 8-bit caches (and a text segment)         rk_decode_attn_q8
-  tree     the attention of a tree of drafted tokens over cache, text and drafts    rk_decode_attn_tree, rk_decode_attn_tree_q8
+  write    a prompt's Keys and Values into the 8-bit caches, and these read back   rk_compress_quant, rk_unpack_cache_quant
+  append   one token a sequence into the 8-bit caches, and these read back          rk_append_quant, rk_unpack_cache_quant
+  decode   one token's attention over the 8-bit caches (and a text segment)         rk_decode_attn_quant
+  tree     the attention of a tree of drafted tokens over cache, text and drafts    rk_decode_attn_tree, rk_decode_attn_tree_quant
   commit   the accepted drafts go behind the text segment                           rk_append_text_path
 
 A row x of a head (the rotated Key k R_r, or a Value) is held in 8 bits as whole numbers c = round(x / s), |c| <= 127, and one bfloat16
@@ -240,7 +240,7 @@ def _hold(s):
     s.ctx = ctx
     s.lay = rk.Layout(B, Hq, H, r, kind, getattr(s, "cap", 32), L if c["op"] != "write" else 0, seq_len=getattr(s, "len", None))
     if c["op"] != "commit":
-        kb, vb = rk.rk_cache_bytes_q8(s.lay) if c["q8"] else rk.rk_cache_bytes(s.lay)
+        kb, vb = rk.rk_cache_bytes_quant(s.lay) if c["q8"] else rk.rk_cache_bytes(s.lay)
         s.kc = torch.zeros(kb, dtype=torch.uint8, device=DEV)
         s.vc = torch.zeros(vb, dtype=torch.uint8, device=DEV)
     if c["op"] in ("append", "decode", "tree"):
@@ -250,7 +250,7 @@ def _hold(s):
         wide[..., :r] = s.Kt
         n = L if c["op"] == "append" else s.Kt.shape[2]
         keys, values = rk.Rows(wide, n, n_tokens_dev=s.len), rk.Rows(s.Vt, n, n_tokens_dev=s.len)
-        put = rk.rk_compress_q8 if c["q8"] else rk.rk_compress
+        put = rk.rk_compress_quant if c["q8"] else rk.rk_compress
         put(ctx, s.lay, keys, pick, s.kc, values=values, v_cache=s.vc)
         torch.cuda.synchronize()
     if c["op"] in ("write", "append"):
@@ -282,7 +282,7 @@ def run(s):
 def _read_back(s):
     """Values that are held in 8 bits, as bfloat16."""
     if own:
-        _rk().rk_unpack_cache_q8(s.ctx, s.held, s.kc, s.vc, s.k_rows, s.v_rows)
+        _rk().rk_unpack_cache_quant(s.ctx, s.held, s.kc, s.vc, s.k_rows, s.v_rows)
         return s.k_rows.to(torch.bfloat16), s.v_rows.to(torch.bfloat16)
 
 
@@ -296,7 +296,7 @@ def _in_8_bits(x):
 def _write(s):
     c = s.c
     if own:
-        _rk().rk_compress_q8(s.ctx, s.lay, s.keys, s.Rr, s.kc, values=s.values, v_cache=s.vc, seq_len_out=s.len_out)
+        _rk().rk_compress_quant(s.ctx, s.lay, s.keys, s.Rr, s.kc, values=s.values, v_cache=s.vc, seq_len_out=s.len_out)
         k, v = _read_back(s)
         return k, v, s.len_out
     K, V = s.K.float(), s.V.float()
@@ -314,7 +314,7 @@ def _write(s):
 
 def _append(s):
     if own:
-        _rk().rk_append_q8(s.ctx, s.lay, s.k_new, s.v_new, s.Rr, s.kc, s.vc, s.len_out)
+        _rk().rk_append_quant(s.ctx, s.lay, s.k_new, s.v_new, s.Rr, s.kc, s.vc, s.len_out)
         k, v = _read_back(s)
         return k, v, s.len_out
     k = _in_8_bits(torch.matmul(s.k_new.float()[:, :, None], s.Rr))
@@ -328,9 +328,9 @@ def _attend(s):
     if own:
         rk = _rk()
         if c["op"] == "decode":
-            rk.rk_decode_attn_q8(s.ctx, s.lay, s.q, s.kc, s.vc, s.Rr, s.dmu, s.text, s.scale, s.out, s.ws)
+            rk.rk_decode_attn_quant(s.ctx, s.lay, s.q, s.kc, s.vc, s.Rr, s.dmu, s.text, s.scale, s.out, s.ws)
         else:
-            call = rk.rk_decode_attn_tree_q8 if c["q8"] else rk.rk_decode_attn_tree
+            call = rk.rk_decode_attn_tree_quant if c["q8"] else rk.rk_decode_attn_tree
             call(s.ctx, s.lay, s.q, s.kc, s.vc, s.Rr, s.dmu, s.text, s.drafts, s.scale, s.out, s.ws)
         return s.out
     B, T, Hq, _ = s.q.shape
