@@ -135,6 +135,21 @@ typedef struct {
     int32_t* len;
 } rk_text;
 
+/* Drafted tokens, not yet accepted: n_tokens of them a sequence (the first n_tokens_dev[b] of sequence b, NULL = all; the count is
+ * held within 0..n_tokens), whose full-width Keys and Values are k and v as in rk_text: element (b, h, t, c) at data[b*stride_b +
+ * h*stride_h + t*stride_t + c], L->dtype, 16-byte aligned, strides multiples of 8 elements.  mask[b*n_tokens + i], 8-byte aligned: bit j
+ * says that draft i attends draft j (a tree: its ancestors and itself; any mask is served, an empty one too); bits from the sequence's
+ * count on are ignored.  mask NULL: a chain, draft i attends drafts 0..i.                                                        */
+#define RK_MAX_DRAFTS 64
+typedef struct {
+    const void* k;
+    const void* v;
+    int64_t stride_b, stride_h, stride_t;
+    int32_t n_tokens;              /* 1..RK_MAX_DRAFTS      */
+    const int32_t* n_tokens_dev;   /* device [B] or NULL    */
+    const uint64_t* mask;          /* device [B, n_tokens] or NULL */
+} rk_drafts;
+
 /* Outputs of rk_fit_rotation (all device, fp32 unless noted). */
 typedef struct {
     float* R;            /* [B,H_kv,d,d]  column c = eigenvector of eigvals[c] (solver order) */
@@ -382,6 +397,78 @@ rk_status rk_append_text_decode_attn_dual(rk_ctx* ctx, const rk_layout* L, const
                                           const float* R_r, const float* delta_mu, const rk_text* text,
                                           float scale, void* out, void* workspace, size_t workspace_bytes,
                                           void* stream);
+
+/* ---- the caches in 8 bits -------------------------------------------------------
+ * Half the bytes of a bf16 cache: a row x of a head (the rotated Key k R_r, in fp32, or a Value) is held as
+ * whole numbers c = round(x / s), ties to even, |c| <= 127, and one step s for the row, max |x| / 127 rounded up
+ * to a bfloat16; what is read back is c s.  (Quotients and k R_r are rounded as fp32 arithmetic does, k R_r with bf16
+ * products to 2^-16 of |k| |R_r|, so that a value within that of the middle between two codes may take either.)
+ * A row with an infinity or a NaN reads back as NaN; one whose largest magnitude is below 2^-100 as zeros.
+ * L->dtype is the type of Keys, Values, q, out and rows read back; the caches are byte buffers of
+ * rk_cache_bytes_quant() bytes, 16-byte aligned, in a layout of their own (blocks of 32 tokens; slabs spaced as in the
+ * other caches): keep padded to 16, plus 4 bytes of steps, and d bytes a token and head.  The
+ * entry points of the other caches do not read them.  The plain kernels (RK_OPT_FORCE_GENERIC) do not
+ * exist for these entry points and those of drafted tokens: the option changes nothing there.               */
+rk_status rk_cache_bytes_quant(const rk_layout* L, size_t* k_q8_bytes, size_t* v_q8_bytes);
+
+/* rk_compress into 8-bit caches.  `values` is required and uses the row selection of `keys`.  Rows from n_b on
+ * stay as they were.  The caches may not lie over keys, values or R_r.
+ * Errors: INVALID_ARG, UNSUPPORTED, CAPACITY, HIP.                                                            */
+rk_status rk_compress_quant(rk_ctx* ctx, const rk_layout* L, const rk_rows* keys, const float* R_r, void* k_q8,
+                         const rk_rows* values, void* v_q8, int32_t* seq_len_out, void* stream);
+
+/* One token per sequence into 8-bit caches: row L->seq_len[b] (required) of every KV head, then seq_len_out[b] =
+ * L->seq_len[b] + 1; seq_len_out may be L->seq_len itself, which then grows as under rk_append, or another
+ * array.  k_new, v_new: [B,H_kv,d] in L->dtype.  RK_ERR_CAPACITY if L->max_seq_len + 1 > capacity (nothing is
+ * launched); on the device a sequence at capacity is left untouched, and its length copied.  Calls on one
+ * context must not overlap.  Errors: INVALID_ARG, UNSUPPORTED, CAPACITY, HIP.                                  */
+rk_status rk_append_quant(rk_ctx* ctx, const rk_layout* L, const void* k_new, const void* v_new, const float* R_r,
+                       void* k_q8, void* v_q8, int32_t* seq_len_out, void* stream);
+
+/* 8-bit caches -> row-major k_rows [B,H_kv,capacity,keep] and/or v_rows [B,H_kv,capacity,d] in L->dtype (either may
+ * be NULL).  With L->seq_len only rows below min(seq_len[b], capacity) are written, without it all.
+ * Errors: INVALID_ARG, UNSUPPORTED, HIP.                                                                       */
+rk_status rk_unpack_cache_quant(rk_ctx* ctx, const rk_layout* L, const void* k_q8, const void* v_q8, void* k_rows,
+                             void* v_rows, void* stream);
+
+/* ---- attention of drafted tokens, and over 8-bit caches ------------------------------
+ * Bytes of workspace for n_tokens query tokens a sequence (rk_decode_attn_quant: 1), 0 for an invalid layout or n_tokens
+ * outside 1..RK_MAX_DRAFTS.  It does not depend on lengths: what serves one max_seq_len serves every other.   */
+size_t rk_tree_workspace_size(const rk_ctx* ctx, const rk_layout* L, int32_t n_tokens);
+
+/* rk_decode_attn_dual over 8-bit caches; text may be NULL (rk_decode_attn over them).  q and out: [B,H_q,d].
+ * 16-byte aligned: q, both caches, workspace.  Calls with workspaces of their own may overlap, on one context too.
+ * A sequence with nothing to attend yields zeros.
+ * Errors: INVALID_ARG, UNSUPPORTED, CAPACITY (max_seq_len > capacity), WORKSPACE, HIP.                         */
+rk_status rk_decode_attn_quant(rk_ctx* ctx, const rk_layout* L, const void* q, const void* k_q8, const void* v_q8,
+                            const float* R_r, const float* delta_mu, const rk_text* text, float scale, void* out,
+                            void* workspace, size_t workspace_bytes, void* stream);
+
+/* The attention of T = drafts->n_tokens drafted tokens per sequence in one pass over the cache.  q, out: [B,T,H_q,d] in
+ * L->dtype.  Draft i of sequence b attends all seq_len[b] cached tokens (scores (q R_r . k~ + q . delta_mu) * scale, as
+ * rk_decode_attn), all len[b] rows of `text` (or NULL) and the drafts that mask[b,i] names (q . k * scale, as the
+ * text rows of rk_decode_attn_dual), under ONE softmax; a row that sees nothing is zeros.  What a row does not
+ * see does not touch it, also where it is an infinity or a NaN.  Rows of out from the sequence's count of drafts on
+ * stay as they were.  Nothing is appended: rk_append_text_path takes the accepted drafts into the text segment.
+ * B T H_q at most 2^31 - 1.  Workspace: rk_tree_workspace_size(ctx, L, T), 16-byte aligned, as q and the caches are; calls with
+ * workspaces of their own may overlap.  The cache is the one of rk_compress, or of rk_compress_quant for the second.
+ * Errors: INVALID_ARG (a malformed text or drafts too), UNSUPPORTED, CAPACITY (max_seq_len > capacity), WORKSPACE, HIP. */
+rk_status rk_decode_attn_tree(rk_ctx* ctx, const rk_layout* L, const void* q, const void* k_packed, const void* v_cache,
+                              const float* R_r, const float* delta_mu, const rk_text* text, const rk_drafts* drafts,
+                              float scale, void* out, void* workspace, size_t workspace_bytes, void* stream);
+rk_status rk_decode_attn_tree_quant(rk_ctx* ctx, const rk_layout* L, const void* q, const void* k_q8, const void* v_q8,
+                                 const float* R_r, const float* delta_mu, const rk_text* text, const rk_drafts* drafts,
+                                 float scale, void* out, void* workspace, size_t workspace_bytes, void* stream);
+
+/* The accepted drafts join the text segment: row len[b] + i of text->k / text->v receives draft path[b*path_len + i] for i <
+ * n_path[b] and every KV head; len_out[b] = len[b] + the rows copied.  len_out may be text->len or another array.
+ * path [B, path_len], n_path [B]: device; path_len 1..RK_MAX_DRAFTS.  A path ends before its first entry that is not one of the
+ * sequence's drafts, and where the segment is full; the same draft may stand in it twice.  The segment and the
+ * drafts may not overlap in memory.  RK_ERR_CAPACITY if text->max_len + path_len > text->capacity.  Calls on one
+ * context must not overlap.  Errors: INVALID_ARG, UNSUPPORTED, CAPACITY, HIP.                                 */
+rk_status rk_append_text_path(rk_ctx* ctx, const rk_layout* L, const rk_text* text, const rk_drafts* drafts,
+                              const int32_t* path, int32_t path_len, const int32_t* n_path, int32_t* len_out,
+                              void* stream);
 
 #ifdef __cplusplus
 }

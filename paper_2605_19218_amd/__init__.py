@@ -29,8 +29,11 @@ EXPORTS = [
     "rk_fit_workspace_size", "rk_decode_workspace_size", "rk_decode_plan", "rk_fit_rotation",
     "rk_gather_rotation", "rk_compress", "rk_append", "rk_decode_attn", "rk_cache_bytes", "rk_unpack_cache",
     "rk_decode_attn_dual", "rk_append_text", "rk_fit_subspace", "rk_query_sigma", "rk_append_decode_attn",
-    "rk_append_text_decode_attn_dual", "rk_decode_attn_static", "rk_stream_read",
+    "rk_append_text_decode_attn_dual", "rk_decode_attn_static", "rk_stream_read", "rk_cache_bytes_quant", "rk_compress_quant",
+    "rk_append_quant", "rk_unpack_cache_quant", "rk_tree_workspace_size", "rk_decode_attn_quant", "rk_decode_attn_tree",
+    "rk_decode_attn_tree_quant", "rk_append_text_path",
 ]
+RK_MAX_DRAFTS = 64
 RK_STATIC_SCRATCH_BYTES = 8 << 20
 
 
@@ -61,6 +64,11 @@ class rk_subspace(C.Structure):
     _fields_ = [("v0", C.c_void_p), ("iterations", C.c_int32), ("ridge", C.c_double)]
 
 
+class rk_drafts(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("stride_b", C.c_int64), ("stride_h", C.c_int64),
+                ("stride_t", C.c_int64), ("n_tokens", C.c_int32), ("n_tokens_dev", C.c_void_p), ("mask", C.c_void_p)]
+
+
 class RotateKError(RuntimeError):
     def __init__(self, status: int, text: str):
         super().__init__(f"rotatek status {status}: {text}")
@@ -81,7 +89,7 @@ def lib():
         L = C.CDLL(LIB_PATH)
         vp, i32, i64, u32, f32, sz = C.c_void_p, C.c_int32, C.c_int64, C.c_uint32, C.c_float, C.c_size_t
         PL, PR, PF = C.POINTER(rk_layout), C.POINTER(rk_rows), C.POINTER(rk_fit_out)
-        PT = C.POINTER(rk_text)
+        PT, PD = C.POINTER(rk_text), C.POINTER(rk_drafts)
         L.rk_create.argtypes = [C.POINTER(vp), C.c_int]
         L.rk_destroy.argtypes = [vp]
         L.rk_status_str.argtypes = [C.c_int]
@@ -110,8 +118,19 @@ def lib():
         L.rk_append_decode_attn.argtypes = [vp, PL, vp, vp, vp, vp, vp, vp, vp, vp, f32, vp, vp, sz, vp]
         L.rk_fit_subspace.argtypes = [vp, PL, PR, vp, u32, C.POINTER(rk_subspace), vp, vp, vp, vp, vp, vp, sz, vp]
         L.rk_query_sigma.argtypes = [vp, PL, vp, i64, i64, i64, i32, vp, vp]
+        L.rk_cache_bytes_quant.argtypes = [PL, C.POINTER(sz), C.POINTER(sz)]
+        L.rk_compress_quant.argtypes = [vp, PL, PR, vp, vp, PR, vp, vp, vp]
+        L.rk_append_quant.argtypes = [vp, PL, vp, vp, vp, vp, vp, vp, vp]
+        L.rk_unpack_cache_quant.argtypes = [vp, PL, vp, vp, vp, vp, vp]
+        L.rk_tree_workspace_size.argtypes = [vp, PL, i32]
+        L.rk_tree_workspace_size.restype = sz
+        L.rk_decode_attn_quant.argtypes = [vp, PL, vp, vp, vp, vp, vp, PT, f32, vp, vp, sz, vp]
+        L.rk_decode_attn_tree.argtypes = [vp, PL, vp, vp, vp, vp, vp, PT, PD, f32, vp, vp, sz, vp]
+        L.rk_decode_attn_tree_quant.argtypes = [vp, PL, vp, vp, vp, vp, vp, PT, PD, f32, vp, vp, sz, vp]
+        L.rk_append_text_path.argtypes = [vp, PL, PT, PD, vp, i32, vp, vp, vp]
         for name in EXPORTS:
-            if name not in ("rk_status_str", "rk_last_error", "rk_fit_workspace_size", "rk_decode_workspace_size"):
+            if name not in ("rk_status_str", "rk_last_error", "rk_fit_workspace_size", "rk_decode_workspace_size",
+                            "rk_tree_workspace_size"):
                 getattr(L, name).restype = C.c_int
         try:
             from . import _rkbind
@@ -225,6 +244,22 @@ class Text:
         st = self.strides if self.strides is not None else tuple(self.k.stride()[:3])
         cap = self.capacity if self.capacity is not None else int(self.k.shape[2])
         return rk_text(_ptr(self.k), _ptr(self.v), st[0], st[1], st[2], cap, self.max_len, _ptr(self.len))
+
+
+@dataclass
+class Drafts:
+    """Drafted tokens: k, v tensor-likes [B, H_kv, n_tokens, d] sharing one set of strides; mask int64 [B, n_tokens], bit j of
+    mask[b, i]: draft i attends draft j (None: drafts 0..i)."""
+    k: Any
+    v: Any
+    n_tokens: int
+    mask: Any = None                     # device int64 [B, n_tokens], contiguous
+    n_tokens_dev: Any = None             # device int32 [B]
+    strides: Optional[tuple] = None      # (stride_b, stride_h, stride_t) in elements
+
+    def c(self) -> rk_drafts:
+        st = self.strides if self.strides is not None else tuple(self.k.stride()[:3])
+        return rk_drafts(_ptr(self.k), _ptr(self.v), st[0], st[1], st[2], self.n_tokens, _ptr(self.n_tokens_dev), _ptr(self.mask))
 
 
 # ---- the ABI, same names -----------------------------------------------------
@@ -382,3 +417,75 @@ def rk_query_sigma(ctx, layout: Layout, q_window, window: int, sigma, strides: O
     st = strides if strides is not None else tuple(q_window.stride()[:3])
     _check(ctx, lib().rk_query_sigma(ctx, C.byref(layout.c()), _ptr(q_window), st[0], st[1], st[2], int(window),
                                      _ptr(sigma), _stream(stream)))
+
+
+def rk_cache_bytes_quant(layout: Layout):
+    """(bytes of the 8-bit Key cache, bytes of the 8-bit Value cache)."""
+    k, v = C.c_size_t(), C.c_size_t()
+    st = lib().rk_cache_bytes_quant(C.byref(layout.c()), C.byref(k), C.byref(v))
+    if st != RK_OK:
+        raise RotateKError(st, lib().rk_status_str(st).decode())
+    return k.value, v.value
+
+
+def rk_compress_quant(ctx, layout: Layout, keys: Rows, R_r, k_q8, values: Rows, v_cache, seq_len_out=None, stream=None) -> None:
+    """rk_compress into 8-bit caches (`v_cache` is the 8-bit Value cache)."""
+    kref = C.byref(keys.c()) if keys is not None else None
+    vref = C.byref(values.c()) if values is not None else None
+    _check(ctx, lib().rk_compress_quant(ctx, C.byref(layout.c()), kref, _ptr(R_r), _ptr(k_q8), vref, _ptr(v_cache),
+                                     _ptr(seq_len_out), _stream(stream)))
+
+
+def rk_append_quant(ctx, layout: Layout, k_new, v_new, R_r, k_q8, v_q8, seq_len_out, stream=None) -> None:
+    """One token at row layout.seq_len[b]; seq_len_out[b] = layout.seq_len[b] + 1 (may be the same tensor)."""
+    _check(ctx, lib().rk_append_quant(ctx, C.byref(layout.c()), _ptr(k_new), _ptr(v_new), _ptr(R_r), _ptr(k_q8), _ptr(v_q8),
+                                   _ptr(seq_len_out), _stream(stream)))
+
+
+def rk_unpack_cache_quant(ctx, layout: Layout, k_q8, v_q8, k_rows, v_rows, stream=None) -> None:
+    _check(ctx, lib().rk_unpack_cache_quant(ctx, C.byref(layout.c()), _ptr(k_q8), _ptr(v_q8), _ptr(k_rows), _ptr(v_rows),
+                                         _stream(stream)))
+
+
+def rk_tree_workspace_size(ctx, layout: Layout, n_tokens: int) -> int:
+    return int(lib().rk_tree_workspace_size(ctx, C.byref(layout.c()), int(n_tokens)))
+
+
+def rk_decode_attn_quant(ctx, layout: Layout, q, k_q8, v_q8, R_r, delta_mu, text: Optional[Text], scale: float, out, workspace,
+                      stream=None, workspace_bytes: Optional[int] = None) -> None:
+    wb = workspace_bytes if workspace_bytes is not None else (_nbytes(workspace) if workspace is not None else 0)
+    tref = C.byref(text.c()) if text is not None else None
+    _check(ctx, lib().rk_decode_attn_quant(ctx, C.byref(layout.c()), _ptr(q), _ptr(k_q8), _ptr(v_q8), _ptr(R_r), _ptr(delta_mu),
+                                        tref, float(scale), _ptr(out), _ptr(workspace), wb, _stream(stream)))
+
+
+def rk_decode_attn_tree(ctx, layout: Layout, q, k_packed, v_cache, R_r, delta_mu, text: Optional[Text], drafts: Drafts,
+                        scale: float, out, workspace, stream=None, workspace_bytes: Optional[int] = None) -> None:
+    """q, out: [B, drafts.n_tokens, H_q, d]."""
+    wb = workspace_bytes if workspace_bytes is not None else (_nbytes(workspace) if workspace is not None else 0)
+    tref = C.byref(text.c()) if text is not None else None
+    dref = C.byref(drafts.c()) if drafts is not None else None
+    _check(ctx, lib().rk_decode_attn_tree(ctx, C.byref(layout.c()), _ptr(q), _ptr(k_packed), _ptr(v_cache), _ptr(R_r),
+                                          _ptr(delta_mu), tref, dref, float(scale), _ptr(out), _ptr(workspace), wb,
+                                          _stream(stream)))
+
+
+def rk_decode_attn_tree_quant(ctx, layout: Layout, q, k_q8, v_q8, R_r, delta_mu, text: Optional[Text], drafts: Drafts,
+                           scale: float, out, workspace, stream=None, workspace_bytes: Optional[int] = None) -> None:
+    """rk_decode_attn_tree over 8-bit caches."""
+    wb = workspace_bytes if workspace_bytes is not None else (_nbytes(workspace) if workspace is not None else 0)
+    tref = C.byref(text.c()) if text is not None else None
+    dref = C.byref(drafts.c()) if drafts is not None else None
+    _check(ctx, lib().rk_decode_attn_tree_quant(ctx, C.byref(layout.c()), _ptr(q), _ptr(k_q8), _ptr(v_q8), _ptr(R_r),
+                                             _ptr(delta_mu), tref, dref, float(scale), _ptr(out), _ptr(workspace), wb,
+                                             _stream(stream)))
+
+
+def rk_append_text_path(ctx, layout: Layout, text: Text, drafts: Drafts, path, n_path, len_out, path_len: Optional[int] = None,
+                        stream=None) -> None:
+    """path: device int32 [B, path_len] (contiguous); n_path, len_out: device int32 [B]; len_out may be text.len."""
+    tref = C.byref(text.c()) if text is not None else None
+    dref = C.byref(drafts.c()) if drafts is not None else None
+    n = path_len if path_len is not None else int(path.shape[1])
+    _check(ctx, lib().rk_append_text_path(ctx, C.byref(layout.c()), tref, dref, _ptr(path), n, _ptr(n_path), _ptr(len_out),
+                                          _stream(stream)))

@@ -292,6 +292,58 @@ DecodePlan decode_plan(const rk_ctx* ctx, const rk_layout* L, int text_rows = 0)
     return p;
 }
 
+// Attention of T query tokens a sequence: row blocks of a KV head, splits of the cache and of the full-width rows.
+struct RowsPlan { int nrb16, nrb, Sv, Sr; };
+int rows_per_block(const rk_layout* L, int T)       // in sixteens; fp32 rows take twice the registers
+{
+    const int64_t rows = (int64_t)T * (L->n_q_heads / L->n_kv_heads);
+    return rows <= 16 ? 1 : rows <= 32 || L->dtype == RK_F32 ? 2 : 4;
+}
+int64_t row_blocks(const rk_layout* L, int T)
+{
+    const int64_t rows = (int64_t)T * (L->n_q_heads / L->n_kv_heads), per = 16 * rows_per_block(L, T);
+    return (rows + per - 1) / per;
+}
+// partial slots of a row: what any length may take
+int rows_slots(const rk_ctx* ctx, const rk_layout* L, int T)
+{
+    const int64_t groups = row_blocks(L, T) * L->batch * L->n_kv_heads, n_cu = ctx ? ctx->n_cu : 256;
+    int64_t s = 2 * n_cu / groups;
+    s = s < 10 ? 10 : s > 64 ? 64 : s;
+    if (ctx && ctx->decode_splits > 0 && s < ctx->decode_splits + 8) s = ctx->decode_splits + 8;
+    return (int)s;
+}
+size_t rows_ws(const rk_ctx* ctx, const rk_layout* L, int T)
+{
+    return align_up((size_t)L->batch * T * L->n_q_heads * rows_slots(ctx, L, T) * (D + 2) * sizeof(float), 256);
+}
+RowsPlan rows_plan(const rk_ctx* ctx, const rk_layout* L, int T, int text_rows, bool drafts, bool q8)
+{
+    RowsPlan p;
+    p.nrb16 = rows_per_block(L, T);
+    p.nrb = (int)row_blocks(L, T);
+    const int64_t groups = (int64_t)p.nrb * L->batch * L->n_kv_heads;
+    const int n_cu = ctx ? ctx->n_cu : 256, slots = rows_slots(ctx, L, T);
+    const int tiles = (L->max_seq_len + 31) / 32, plain = (text_rows + 31) / 32 + (drafts ? (T + 31) / 32 : 0);
+    const int most_v = tiles > 8 ? (tiles + 7) / 8 : 1, most_r = (plain + 3) / 4;
+    const double es = (double)elem_size(L->dtype), cv = tiles * (q8 ? 1.0 : es) * (keep_padded(L->keep) + D), cr = plain * es * 2 * D;
+    int total = (int)(n_cu / groups);
+    if (total < 1) total = 1;
+    p.Sr = 0;
+    if (plain) {
+        p.Sr = (int)(total * cr / (cv + cr) + 0.5);
+        if (p.Sr > most_r) p.Sr = most_r;
+        if (p.Sr > slots / 2) p.Sr = slots / 2;
+        if (p.Sr < 1) p.Sr = 1;
+    }
+    p.Sv = total - p.Sr;
+    if (ctx && ctx->decode_splits > 0) p.Sv = ctx->decode_splits;
+    else if (p.Sv > most_v) p.Sv = most_v;
+    if (p.Sv > slots - p.Sr) p.Sv = slots - p.Sr;
+    if (p.Sv < 1) p.Sv = 1;
+    return p;
+}
+
 hipStream_t as_stream(void* s) { return (hipStream_t)s; }
 
 // Makes `device` current for the duration of a call and puts the caller's device back
@@ -828,6 +880,221 @@ rk_status rk_append_text(rk_ctx* ctx, const rk_layout* L, const rk_text* text, c
                            text->stride_b, text->stride_h, text->stride_t, text->len, as_stream(stream));
     if (e != hipSuccess) return hip_fail(ctx, e, "append_text launch");
     return RK_OK;
+}
+
+rk_status rk_cache_bytes_quant(const rk_layout* L, size_t* k_q8_bytes, size_t* v_q8_bytes)
+{
+    rk_status s = check_layout(nullptr, L);
+    if (s != RK_OK) return s;
+    const size_t slabs = (size_t)L->batch * L->n_kv_heads * slab_tokens(L->capacity);
+    if (k_q8_bytes) *k_q8_bytes = slabs / 32 * q8_kblock(keep_padded(L->keep));
+    if (v_q8_bytes) *v_q8_bytes = slabs * D;
+    return RK_OK;
+}
+
+rk_status rk_compress_quant(rk_ctx* ctx, const rk_layout* L, const rk_rows* keys, const float* R_r, void* k_q8,
+                         const rk_rows* values, void* v_q8, int32_t* seq_len_out, void* stream)
+{
+    if (!ctx) return RK_ERR_INVALID_ARG;
+    rk_status s = check_layout(ctx, L);
+    if (s != RK_OK) return s;
+    s = check_rows(ctx, L, keys, "keys");
+    if (s != RK_OK) return s;
+    s = check_rows(ctx, L, values, "values");
+    if (s != RK_OK) return s;
+    if (!R_r || !k_q8 || !v_q8) return fail(ctx, RK_ERR_INVALID_ARG, "compress_q8: R_r, k_q8 or v_q8 is NULL");
+    if (((uintptr_t)k_q8 & 15) || ((uintptr_t)v_q8 & 15))
+        return fail(ctx, RK_ERR_INVALID_ARG, "compress_q8: the caches must be 16-byte aligned");
+    if (values->n_tokens != keys->n_tokens || values->tok_idx != keys->tok_idx || values->tok_off != keys->tok_off ||
+        values->n_tokens_dev != keys->n_tokens_dev)
+        return fail(ctx, RK_ERR_INVALID_ARG, "compress_q8: values must use the same row selection as keys");
+    if (keys->n_tokens > L->capacity)
+        return fail(ctx, RK_ERR_CAPACITY, "compress_q8: %d rows exceed capacity %d", keys->n_tokens, L->capacity);
+    if (ctx->device == RK_DEVICE_NONE) return fail(ctx, RK_ERR_NO_DEVICE, "valid arguments, but the context has no device");
+    DeviceGuard dev(ctx->device);
+    hipError_t e = dev.status;
+    if (e != hipSuccess) return hip_fail(ctx, e, "hipSetDevice");
+    e = launch_compress_q8(L->dtype, to_dev(keys), to_dev(values), L->batch, L->n_kv_heads, L->capacity, L->keep, R_r, k_q8, v_q8,
+                           seq_len_out, ctx->n_cu, as_stream(stream));
+    return e == hipSuccess ? RK_OK : hip_fail(ctx, e, "compress_q8 launch");
+}
+
+rk_status rk_append_quant(rk_ctx* ctx, const rk_layout* L, const void* k_new, const void* v_new, const float* R_r, void* k_q8,
+                       void* v_q8, int32_t* seq_len_out, void* stream)
+{
+    if (!ctx) return RK_ERR_INVALID_ARG;
+    rk_status s = check_layout(ctx, L);
+    if (s != RK_OK) return s;
+    if (!k_new || !v_new || !R_r || !k_q8 || !v_q8 || !L->seq_len || !seq_len_out)
+        return fail(ctx, RK_ERR_INVALID_ARG, "append_q8: NULL pointer");
+    if (((uintptr_t)k_q8 & 15) || ((uintptr_t)v_q8 & 15))
+        return fail(ctx, RK_ERR_INVALID_ARG, "append_q8: the caches must be 16-byte aligned");
+    if (L->max_seq_len + 1 > L->capacity)
+        return fail(ctx, RK_ERR_CAPACITY, "append_q8: %d + 1 rows exceed capacity %d", L->max_seq_len, L->capacity);
+    if (ctx->device == RK_DEVICE_NONE) return fail(ctx, RK_ERR_NO_DEVICE, "valid arguments, but the context has no device");
+    DeviceGuard dev(ctx->device);
+    hipError_t e = dev.status;
+    if (e != hipSuccess) return hip_fail(ctx, e, "hipSetDevice");
+    e = launch_append_q8(L->dtype, L->batch, L->n_kv_heads, L->capacity, L->keep, k_new, v_new, R_r, k_q8, v_q8, L->seq_len,
+                         seq_len_out, ctx->tickets, as_stream(stream));
+    return e == hipSuccess ? RK_OK : hip_fail(ctx, e, "append_q8 launch");
+}
+
+rk_status rk_unpack_cache_quant(rk_ctx* ctx, const rk_layout* L, const void* k_q8, const void* v_q8, void* k_rows, void* v_rows,
+                             void* stream)
+{
+    if (!ctx) return RK_ERR_INVALID_ARG;
+    rk_status s = check_layout(ctx, L);
+    if (s != RK_OK) return s;
+    if (!k_q8 || (v_rows && !v_q8) || (!k_rows && !v_rows))       // (the steps of the Values lie beside the Keys')
+        return fail(ctx, RK_ERR_INVALID_ARG, "unpack_q8: nothing to do or source missing");
+    if (((uintptr_t)k_q8 & 15) || ((uintptr_t)v_q8 & 15))
+        return fail(ctx, RK_ERR_INVALID_ARG, "unpack_q8: the caches must be 16-byte aligned");
+    if (ctx->device == RK_DEVICE_NONE) return fail(ctx, RK_ERR_NO_DEVICE, "valid arguments, but the context has no device");
+    DeviceGuard dev(ctx->device);
+    hipError_t e = dev.status;
+    if (e != hipSuccess) return hip_fail(ctx, e, "hipSetDevice");
+    e = launch_unpack_q8(L->dtype, L->batch, L->n_kv_heads, L->capacity, L->keep, k_q8, v_q8, L->seq_len, k_rows, v_rows,
+                         as_stream(stream));
+    return e == hipSuccess ? RK_OK : hip_fail(ctx, e, "unpack_q8 launch");
+}
+
+size_t rk_tree_workspace_size(const rk_ctx* ctx, const rk_layout* L, int32_t n_tokens)
+{
+    if (check_layout(nullptr, L) != RK_OK || n_tokens < 1 || n_tokens > RK_MAX_DRAFTS) return 0;
+    return rows_ws(ctx, L, n_tokens);
+}
+
+static rk_status check_drafts(rk_ctx* ctx, const rk_drafts* d)
+{
+    if (!d || !d->k || !d->v) return fail(ctx, RK_ERR_INVALID_ARG, "drafts: NULL, or NULL k or v");
+    if (((uintptr_t)d->k & 15) || ((uintptr_t)d->v & 15))
+        return fail(ctx, RK_ERR_INVALID_ARG, "drafts: k and v must be 16-byte aligned");
+    if (d->n_tokens < 1 || d->n_tokens > RK_MAX_DRAFTS)
+        return fail(ctx, RK_ERR_INVALID_ARG, "drafts: n_tokens %d outside 1..%d", d->n_tokens, RK_MAX_DRAFTS);
+    if (d->stride_b < 0 || d->stride_h < 0 || d->stride_t < D || (d->stride_b % 8) || (d->stride_h % 8) || (d->stride_t % 8))
+        return fail(ctx, RK_ERR_INVALID_ARG, "drafts: strides must be non-negative multiples of 8 elements, stride_t >= %d", D);
+    if ((uintptr_t)d->mask & 7) return fail(ctx, RK_ERR_INVALID_ARG, "drafts: mask must be 8-byte aligned");
+    return RK_OK;
+}
+
+static rk_status rows_common(rk_ctx* ctx, const rk_layout* L, const void* q, const void* k_cache, const void* v_cache,
+                             const float* R_r, const float* delta_mu, const rk_text* text, const rk_drafts* drafts, bool q8,
+                             float scale, void* out, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!ctx) return RK_ERR_INVALID_ARG;
+    rk_status s = check_layout(ctx, L);
+    if (s != RK_OK) return s;
+    if (!q || !k_cache || !v_cache || !R_r || !out || !L->seq_len)
+        return fail(ctx, RK_ERR_INVALID_ARG, "attention: NULL pointer (q, caches, R_r, out, seq_len)");
+    if (((uintptr_t)k_cache & 15) || ((uintptr_t)v_cache & 15) || ((uintptr_t)q & 15))
+        return fail(ctx, RK_ERR_INVALID_ARG, "attention: q and the caches must be 16-byte aligned");
+    if (L->max_seq_len > L->capacity)
+        return fail(ctx, RK_ERR_CAPACITY, "attention: max_seq_len %d exceeds capacity %d", L->max_seq_len, L->capacity);
+    if (text && (s = check_text(ctx, text, false)) != RK_OK) return s;
+    const int T = drafts ? drafts->n_tokens : 1;
+    if ((int64_t)L->batch * T * L->n_q_heads > INT32_MAX)
+        return fail(ctx, RK_ERR_UNSUPPORTED, "attention: more than %d query rows", INT32_MAX);
+    const size_t need = rows_ws(ctx, L, T);
+    if (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 15))
+        return fail(ctx, RK_ERR_WORKSPACE, "attention workspace: need %zu bytes, 16-byte aligned", need);
+    if (ctx->device == RK_DEVICE_NONE) return fail(ctx, RK_ERR_NO_DEVICE, "valid arguments, but the context has no device");
+
+    DeviceGuard dev(ctx->device);
+    hipError_t e = dev.status;
+    if (e != hipSuccess) return hip_fail(ctx, e, "hipSetDevice");
+    const RowsPlan p = rows_plan(ctx, L, T, text ? text->max_len : 0, drafts != nullptr, q8);
+    RowsArgs a{};
+    a.q = q; a.Kc = k_cache; a.Vc = v_cache; a.Rr = R_r; a.dmu = delta_mu; a.seq_len = L->seq_len; a.out = out;
+    a.B = L->batch; a.T = T; a.Hq = L->n_q_heads; a.Hkv = L->n_kv_heads; a.G = a.Hq / a.Hkv;
+    a.cap = L->capacity; a.r = L->keep; a.rp = keep_padded(L->keep);
+    a.Sv = p.Sv; a.Sr = p.Sr; a.nrb = p.nrb;
+    const float sc = scale > 0.f ? scale : 1.0f / sqrtf((float)L->head_dim);
+    a.scale_log2 = sc * 1.44269504088896340736f;
+    if (text) {
+        a.text_k = text->k; a.text_v = text->v; a.text_len = text->len; a.text_max = text->max_len;
+        a.text_sb = text->stride_b; a.text_sh = text->stride_h; a.text_st = text->stride_t;
+    }
+    if (drafts) {
+        a.draft_k = drafts->k; a.draft_v = drafts->v; a.n_drafts = drafts->n_tokens_dev; a.mask = drafts->mask;
+        a.draft_sb = drafts->stride_b; a.draft_sh = drafts->stride_h; a.draft_st = drafts->stride_t;
+    }
+    const size_t slots = (size_t)a.B * T * a.Hq * (p.Sv + p.Sr);
+    a.ws_acc = (float*)workspace; a.ws_m = a.ws_acc + slots * D; a.ws_l = a.ws_m + slots;
+    hipStream_t st = as_stream(stream);
+    e = L->dtype == RK_F32 ? (q8 ? launch_rows_q8_f32(a, p.nrb16, st) : launch_rows_f32(a, p.nrb16, st))
+                           : (q8 ? launch_rows_q8_bf16(a, p.nrb16, st) : launch_rows_bf16(a, p.nrb16, st));
+    if (e != hipSuccess) return hip_fail(ctx, e, "attention launch");
+    if (p.Sv + p.Sr > 1) {
+        e = launch_rows_merge(L->dtype, a, st);
+        if (e != hipSuccess) return hip_fail(ctx, e, "attention merge launch");
+    }
+    return RK_OK;
+}
+
+rk_status rk_decode_attn_quant(rk_ctx* ctx, const rk_layout* L, const void* q, const void* k_q8, const void* v_q8,
+                            const float* R_r, const float* delta_mu, const rk_text* text, float scale, void* out,
+                            void* workspace, size_t workspace_bytes, void* stream)
+{
+    return rows_common(ctx, L, q, k_q8, v_q8, R_r, delta_mu, text, nullptr, true, scale, out, workspace, workspace_bytes, stream);
+}
+
+static rk_status tree_common(rk_ctx* ctx, const rk_layout* L, const void* q, const void* k_cache, const void* v_cache,
+                             const float* R_r, const float* delta_mu, const rk_text* text, const rk_drafts* drafts, bool q8,
+                             float scale, void* out, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!ctx) return RK_ERR_INVALID_ARG;
+    const rk_status s = check_drafts(ctx, drafts);
+    return s != RK_OK ? s : rows_common(ctx, L, q, k_cache, v_cache, R_r, delta_mu, text, drafts, q8, scale, out, workspace,
+                                        workspace_bytes, stream);
+}
+
+rk_status rk_decode_attn_tree(rk_ctx* ctx, const rk_layout* L, const void* q, const void* k_packed, const void* v_cache,
+                              const float* R_r, const float* delta_mu, const rk_text* text, const rk_drafts* drafts,
+                              float scale, void* out, void* workspace, size_t workspace_bytes, void* stream)
+{
+    return tree_common(ctx, L, q, k_packed, v_cache, R_r, delta_mu, text, drafts, false, scale, out, workspace, workspace_bytes, stream);
+}
+
+rk_status rk_decode_attn_tree_quant(rk_ctx* ctx, const rk_layout* L, const void* q, const void* k_q8, const void* v_q8,
+                                 const float* R_r, const float* delta_mu, const rk_text* text, const rk_drafts* drafts,
+                                 float scale, void* out, void* workspace, size_t workspace_bytes, void* stream)
+{
+    return tree_common(ctx, L, q, k_q8, v_q8, R_r, delta_mu, text, drafts, true, scale, out, workspace, workspace_bytes, stream);
+}
+
+rk_status rk_append_text_path(rk_ctx* ctx, const rk_layout* L, const rk_text* text, const rk_drafts* drafts,
+                              const int32_t* path, int32_t path_len, const int32_t* n_path, int32_t* len_out, void* stream)
+{
+    if (!ctx) return RK_ERR_INVALID_ARG;
+    rk_status s = check_layout(ctx, L);
+    if (s != RK_OK) return s;
+    if (!text) return fail(ctx, RK_ERR_INVALID_ARG, "append_text_path: text is NULL");
+    if ((s = check_text(ctx, text, true)) != RK_OK || (s = check_drafts(ctx, drafts)) != RK_OK) return s;
+    if (!path || !n_path || !len_out) return fail(ctx, RK_ERR_INVALID_ARG, "append_text_path: NULL pointer (path, n_path, len_out)");
+    if (path_len < 1 || path_len > RK_MAX_DRAFTS)
+        return fail(ctx, RK_ERR_INVALID_ARG, "append_text_path: path_len %d outside 1..%d", path_len, RK_MAX_DRAFTS);
+    if (text->max_len + path_len > text->capacity)
+        return fail(ctx, RK_ERR_CAPACITY, "append_text_path: %d + %d rows exceed capacity %d", text->max_len, path_len, text->capacity);
+    // rows copied by one work-group may be read by another: the drafts' rows and the segment's lie apart
+    const size_t es = elem_size(L->dtype);
+    auto span = [&](int64_t sb, int64_t sh, int64_t st, int rows) {
+        return (size_t)((L->batch - 1) * sb + (L->n_kv_heads - 1) * sh + (int64_t)(rows - 1) * st + D) * es;
+    };
+    const size_t tb = span(text->stride_b, text->stride_h, text->stride_t, text->capacity);
+    const size_t db = span(drafts->stride_b, drafts->stride_h, drafts->stride_t, drafts->n_tokens);
+    if (ranges_meet(text->k, tb, drafts->k, db) || ranges_meet(text->k, tb, drafts->v, db) || ranges_meet(text->v, tb, drafts->k, db) ||
+        ranges_meet(text->v, tb, drafts->v, db))
+        return fail(ctx, RK_ERR_INVALID_ARG, "append_text_path: text segment and drafts overlap in memory");
+    if (ctx->device == RK_DEVICE_NONE) return fail(ctx, RK_ERR_NO_DEVICE, "valid arguments, but the context has no device");
+    DeviceGuard dev(ctx->device);
+    hipError_t e = dev.status;
+    if (e != hipSuccess) return hip_fail(ctx, e, "hipSetDevice");
+    const PathArgs a{text->k, text->v, text->stride_b, text->stride_h, text->stride_t, text->len, text->capacity,
+                     drafts->k, drafts->v, drafts->stride_b, drafts->stride_h, drafts->stride_t, drafts->n_tokens_dev,
+                     path, n_path, len_out, L->batch, L->n_kv_heads, drafts->n_tokens, path_len};
+    e = launch_append_path(L->dtype, a, ctx->tickets, as_stream(stream));
+    return e == hipSuccess ? RK_OK : hip_fail(ctx, e, "append_text_path launch");
 }
 
 }  // extern "C"

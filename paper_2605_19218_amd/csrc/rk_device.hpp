@@ -161,6 +161,19 @@ __host__ __device__ __forceinline__ size_t vidx(int t, int c) {
     return (size_t)(t >> 5) * 4096 + (size_t)(c >> 4) * 512 + (size_t)g * 128 + (size_t)(c & 15) * 8 + jj;
 }
 
+//  The 8-bit caches: blocks of 32 tokens in both.
+//  Keys:   [t / 32]{ codes [c / 8][t % 16][(t / 16) % 2][c % 8], then 32 words (step of the Key, step of the Value), bf16 each }
+//          lane (g, n) reads octet 4 i + g of tokens n and 16 + n as one 16-byte piece: the A operand of both 16-token halves.
+//  Values: [t / 32][c / 32][g][c % 16][(c / 16) % 2][jj], (g, jj) as above: 16 bytes are the A operands of two channel blocks.
+__host__ __device__ __forceinline__ size_t q8_kblock(int rp) { return (size_t)32 * (rp + 4); }
+__host__ __device__ __forceinline__ size_t q8_kplace(int t, int c) {      // within its block
+    return (size_t)(c >> 3) * 256 + (size_t)(t & 15) * 16 + (size_t)((t >> 4) & 1) * 8 + (c & 7);
+}
+__host__ __device__ __forceinline__ size_t q8_vidx(int t, int c) {
+    const int tl = t & 31, g = (tl & 15) >> 2, jj = ((tl >> 4) << 2) | (tl & 3);
+    return (size_t)(t >> 5) * 4096 + (size_t)(c >> 5) * 1024 + (size_t)g * 256 + (size_t)(c & 15) * 16 + (size_t)((c >> 4) & 1) * 8 + jj;
+}
+
 // 16-byte non-temporal (streaming) accesses: data that is written once and read once by a later
 // kernel, or read exactly once, should not displace anything in the caches
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));

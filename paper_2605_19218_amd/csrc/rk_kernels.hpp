@@ -50,6 +50,57 @@ hipError_t launch_append(int dtype, int B, int Hkv, int cap, int r, const void* 
 hipError_t launch_unpack(int dtype, int U, int cap, int r, const void* Kp, const void* Vc, void* k_rows,
                          void* v_rows, hipStream_t st);
 
+// ---- rk_q8.hip: the 8-bit caches ---------------------------------------------
+hipError_t launch_compress_q8(int dtype, const RowsDev& keys, const RowsDev& vals, int B, int Hkv, int cap, int r, const float* Rr, void* Kq,
+                              void* Vq, int32_t* seq_len_out, int n_cu, hipStream_t st);
+// writes row seq_len[b]; seq_len_out[b] = seq_len[b] + 1 (may be the same array); tickets as launch_append
+hipError_t launch_append_q8(int dtype, int B, int Hkv, int cap, int r, const void* k_new, const void* v_new, const float* Rr, void* Kq, void* Vq,
+                            const int32_t* seq_len, int32_t* seq_len_out, int32_t* tickets, hipStream_t st);
+// rows below seq_len[b] (null: all) of both caches
+hipError_t launch_unpack_q8(int dtype, int B, int Hkv, int cap, int r, const void* Kq, const void* Vq, const int32_t* seq_len, void* k_rows,
+                            void* v_rows, hipStream_t st);
+
+// ---- rk_attn_rows.hpp, rk_tree*.hip: several query rows a KV head ---------------
+struct RowsArgs {
+    const void* q;               // [B, T, Hq, d]
+    const void *Kc, *Vc;
+    const float *Rr, *dmu;       // dmu: or null
+    const int32_t* seq_len;
+    int32_t B, T, Hq, Hkv, G, cap, r, rp;
+    int32_t Sv, Sr, nrb;         // splits of the cache, of the full-width rows behind them; row blocks of a KV head
+    float scale_log2;
+    const void *text_k, *text_v; // or null; strides in elements
+    int64_t text_sb, text_sh, text_st;
+    const int32_t* text_len;     // or null: text_max
+    int32_t text_max;
+    const void *draft_k, *draft_v;                // or null: one row of the cache and the text alone (T = 1)
+    int64_t draft_sb, draft_sh, draft_st;
+    const int32_t* n_drafts;     // or null: T
+    const uint64_t* mask;        // [B, T] or null: row t sees drafts 0 ..t
+    void* out;
+    float *ws_m, *ws_l, *ws_acc; // [B, T, Hq, S] and [B, T, Hq, S, d]
+};
+// fmt: ROWS_BF16, ROWS_F32, ROWS_Q8_BF16, ROWS_Q8_F32; nrb16: blocks of 16 rows a work-group takes (1, 2; 4 with bf16 rows)
+hipError_t launch_rows_bf16(const RowsArgs& a, int nrb16, hipStream_t st);
+hipError_t launch_rows_f32(const RowsArgs& a, int nrb16, hipStream_t st);
+hipError_t launch_rows_q8_bf16(const RowsArgs& a, int nrb16, hipStream_t st);
+hipError_t launch_rows_q8_f32(const RowsArgs& a, int nrb16, hipStream_t st);
+hipError_t launch_rows_merge(int dtype, const RowsArgs& a, hipStream_t st);
+// row text_len[b] + i of the text segment receives draft path[b][i], i < n_path[b]; len_out[b] counts them
+struct PathArgs {
+    void *text_k, *text_v;
+    int64_t text_sb, text_sh, text_st;
+    const int32_t* text_len;
+    int32_t text_cap;
+    const void *draft_k, *draft_v;
+    int64_t draft_sb, draft_sh, draft_st;
+    const int32_t* n_drafts;     // or null: T
+    const int32_t *path, *n_path;
+    int32_t* len_out;            // may be text_len
+    int32_t B, Hkv, T, P;
+};
+hipError_t launch_append_path(int dtype, const PathArgs& a, int32_t* tickets, hipStream_t st);
+
 // ---- rk_decode.hip ---------------------------------------------------------
 // Partials: m [B,Hq,S], l [B,Hq,S], acc [B,Hq,S,d]; m is in the log2 domain.
 bool decode_mfma_supported(int dtype, int r);

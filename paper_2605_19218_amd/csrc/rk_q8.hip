@@ -1,0 +1,443 @@
+// The 8-bit caches: written for a prompt (compress_q8), for one token (append_q8), and read back (unpack_q8).
+//
+// A row x of a head, the rotated Key k R_r (in fp32) or a Value, is held as whole numbers c = round(x / s), |c| <= 127, and ONE step s for
+// the row, the bfloat16 next above or at max |x| / 127.  Upwards, so that no element passes 127; sixteen bits are enough for a step, since
+// the codes are made with the rounded one (it costs at most 2^-7 of the step itself, and halves what the steps take).  A row with an infinity or
+// a NaN has s = NaN: all of it reads back as NaN.  A row whose largest element is below 2^-100 has s = 0 (1 / s stays finite).
+// What bounds these kernels is memory; the layout (rk_device.hpp) is made for the attention that reads it.
+#include "rk_kernels.hpp"
+
+namespace rk {
+
+// The step of a row from the bits of its largest magnitude, as bf16 bits, and 1 / s (0 where every code is 0).
+__device__ __forceinline__ uint32_t row_step(uint32_t top, float& inv)
+{
+    const uint32_t up = (__float_as_uint(__uint_as_float(top) / 127.f) + 0xffffu) & 0xffff0000u;
+    const bool finite = top < 0x7f800000u, tiny = top < 0x0d800000u;        // 2^-100
+    inv = finite && !tiny ? 1.f / __uint_as_float(up) : 0.f;
+    return !finite ? 0x7fc0u : tiny ? 0u : up >> 16;
+}
+// the code in the low byte: 1.5 2^23 + c is c's two's complement there, and the sum is rounded once, to the nearest even
+__device__ __forceinline__ uint32_t code_of(float x, float inv) { return __float_as_uint(fmaf(x, inv, 12582912.f)); }
+__device__ __forceinline__ uint32_t low_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d)
+{
+    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0c0c0400u), __builtin_amdgcn_perm(b, a, 0x0c0c0400u), 0x05040100u);
+}
+__device__ __forceinline__ uint32_t mag(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+
+// maximum over the lanes l % 16 + 16 g, and over an aligned group of 16 lanes (as whole numbers: a NaN is the largest)
+__device__ __forceinline__ uint32_t groups_umax(uint32_t v)
+{
+    const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    v = max((uint32_t)a[0], (uint32_t)a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return max((uint32_t)b[0], (uint32_t)b[1]);
+}
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp_u32(uint32_t v)
+{
+    return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, CTRL, 0xf, 0xf, true);
+}
+__device__ __forceinline__ uint32_t row16_umax(uint32_t v)
+{
+    v = max(v, dpp_u32<0xB1>(v));
+    v = max(v, dpp_u32<0x4E>(v));
+    v = max(v, dpp_u32<0x141>(v));
+    return max(v, dpp_u32<0x140>(v));
+}
+
+// eight channels of a row
+__device__ __forceinline__ void load8(const bf16_t* p, float (&x)[8])
+{
+    const uint4 v = *(const uint4*)p;
+    const uint32_t d[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[2 * i] = __uint_as_float(d[i] << 16);
+        x[2 * i + 1] = __uint_as_float(d[i] & 0xffff0000u);
+    }
+}
+__device__ __forceinline__ void load8(const float* p, float (&x)[8])
+{
+    const f32x4 a = *(const f32x4*)p, b = *(const f32x4*)(p + 4);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[i] = a[i];
+        x[4 + i] = b[i];
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Prompt rows.  A wave takes blocks of 32 tokens.  Keys: D^T[channel j][token] = R_r^T . K^T on v_mfma_f32_16x16x32_bf16, R_r as bf16 head
+// and remainder in LDS (made once a work-group), an fp32 Key likewise, without the product of the two remainders: 2^-16 of |k| |R_r|, a
+// five-hundredth of a step.  Lane (g, n) then holds channels 16 jb + 4 g ..+3 of tokens n and 16 + n: the row's maximum is two lane swaps, and
+// a swap of halves between two jb makes the 16 bytes of the layout (one octet of both tokens).
+// Values: lane (g, n) takes channels 8 n ..+7 of the eight tokens whose codes the layout puts side by side, and the bytes are transposed in
+// the lane; pairs of lanes two apart exchange halves, again for whole 16-byte pieces.
+// Grid: (blocks of `each` tokens, h_kv, b).
+template <typename T, int R>
+__global__ __launch_bounds__(256) void compress_q8(RowsDev keys, RowsDev vals, int Hkv, int cap, int r, int each, const float* __restrict__ Rr,
+                                                   uint8_t* __restrict__ Kq, uint8_t* __restrict__ Vq, int32_t* __restrict__ seq_len_out)
+{
+    constexpr int JB = R / 16;
+    constexpr bool F32 = sizeof(T) == 4;
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    bf16x8* frag = (bf16x8*)smem;               // [jb][i][part][lane]
+    const int h = blockIdx.y, b = blockIdx.z, u = b * Hkv + h;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, n = lane & 15;
+    const int n_b = min(rows_count(keys, b), cap);
+    if (blockIdx.x == 0 && h == 0 && tid == 0 && seq_len_out) seq_len_out[b] = n_b;
+    const int64_t first = (int64_t)blockIdx.x * each;
+    if (first >= n_b) return;
+    const int blk0 = (int)first, blk1 = (int)min(first + each, (int64_t)n_b);
+
+    const float* Ru = Rr + (size_t)u * D * r;
+    for (int f = wave; f < JB * 4; f += 4) {
+        const int j = 16 * (f >> 2) + n, c0 = 32 * (f & 3) + 8 * g;
+        float x[8];
+#pragma unroll
+        for (int jj = 0; jj < 8; ++jj) {
+            const float v = Ru[(c0 + jj) * r + min(j, r - 1)];
+            x[jj] = j < r ? v : 0.f;
+        }
+        bf16x8 hi, lo;
+        split_bf16x8(x, hi, lo);
+        frag[(2 * f) * 64 + lane] = hi;
+        frag[(2 * f + 1) * 64 + lane] = lo;
+    }
+    __syncthreads();
+
+    const int rp = keep_padded(r);
+    const size_t blocks = slab_tokens(cap) / 32, kblk = q8_kblock(rp);
+    uint8_t* Ku = Kq + (size_t)u * blocks * kblk;
+    uint8_t* Vu = Vq + (size_t)u * blocks * (32 * D);
+    const T* kdata = (const T*)keys.data + (int64_t)b * keys.sb + (int64_t)h * keys.sh;
+    const T* vdata = (const T*)vals.data + (int64_t)b * vals.sb + (int64_t)h * vals.sh;
+    const int32_t* list = keys.tok_idx ? keys.tok_idx + keys.tok_off[b] : nullptr;
+    auto row_of = [&](int t) {                  // rows behind the last are clamped to it and not stored
+        t = min(t, n_b - 1);
+        return list ? (int64_t)list[t] : (int64_t)t;
+    };
+
+#pragma unroll 1
+    for (int t0 = blk0 + 32 * wave; t0 < blk1; t0 += 128) {
+        const bool full = t0 + 32 <= n_b;
+        uint8_t* kb = Ku + (size_t)(t0 >> 5) * kblk;
+        uint8_t* vb = Vu + (size_t)(t0 >> 5) * (32 * D);
+        uint16_t* steps = (uint16_t*)(kb + 32 * rp);         // (Key, Value) of a token side by side
+
+        // ---- Values: requested first, they are used last
+        float xv[8][8];
+#pragma unroll
+        for (int jj = 0; jj < 8; ++jj) {
+            const int tl = jj < 4 ? 4 * g + jj : 12 + 4 * g + jj;
+            load8(vdata + row_of(t0 + tl) * vals.st + 8 * n, xv[jj]);
+        }
+        // ---- Keys
+        f32x4 acc[2][JB];
+        {
+            bf16x8 kh[2][4], kl[2][F32 ? 4 : 1];
+#pragma unroll
+            for (int tb = 0; tb < 2; ++tb) {
+                const T* kr = kdata + row_of(t0 + 16 * tb + n) * keys.st + 8 * g;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if constexpr (F32) {
+                        float x[8];
+                        load8(kr + 32 * i, x);
+                        split_bf16x8(x, kh[tb][i], kl[tb][i]);
+                    } else {
+                        kh[tb][i] = *(const bf16x8*)(kr + 32 * i);
+                    }
+                }
+            }
+#pragma unroll
+            for (int jb = 0; jb < JB; ++jb) {
+                acc[0][jb] = acc[1][jb] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const bf16x8 hi = frag[((jb * 4 + i) * 2) * 64 + lane], lo = frag[((jb * 4 + i) * 2 + 1) * 64 + lane];
+#pragma unroll
+                    for (int tb = 0; tb < 2; ++tb) {
+                        acc[tb][jb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lo, kh[tb][i], acc[tb][jb], 0, 0, 0);
+                        if constexpr (F32) acc[tb][jb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(hi, kl[tb][i], acc[tb][jb], 0, 0, 0);
+                        acc[tb][jb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(hi, kh[tb][i], acc[tb][jb], 0, 0, 0);
+                    }
+                }
+            }
+        }
+        float inv[2];
+        uint32_t ks[2];
+#pragma unroll
+        for (int tb = 0; tb < 2; ++tb) {
+            uint32_t top = 0;
+#pragma unroll
+            for (int jb = 0; jb < JB; ++jb)
+#pragma unroll
+                for (int ii = 0; ii < 4; ++ii) top = max(top, mag(acc[tb][jb][ii]));
+            ks[tb] = row_step(groups_umax(top), inv[tb]);
+        }
+#pragma unroll
+        for (int jb = 0; jb < JB; jb += 2) {
+            uint32_t piece[4];
+#pragma unroll
+            for (int tb = 0; tb < 2; ++tb) {
+                uint32_t w[2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const f32x4 a = acc[tb][jb + e];
+                    w[e] = low_bytes(code_of(a[0], inv[tb]), code_of(a[1], inv[tb]), code_of(a[2], inv[tb]), code_of(a[3], inv[tb]));
+                }
+                // odd lane groups give their half of jb and get the even ones' half of jb + 1
+                const auto x = __builtin_amdgcn_permlane16_swap(w[0], w[1], false, false);
+                piece[2 * tb] = x[0];
+                piece[2 * tb + 1] = x[1];
+            }
+            const int oct = 2 * (jb + (g & 1)) + (g >> 1);
+            if (8 * oct < rp) {
+                uint8_t* to = kb + oct * 256 + n * 16;
+                if (full || t0 + 16 + n < n_b) *(uint4*)to = make_uint4(piece[0], piece[1], piece[2], piece[3]);
+                else if (t0 + n < n_b) *(uint2*)to = make_uint2(piece[0], piece[1]);
+            }
+        }
+        {
+            const int tl = 16 * (g & 1) + n;
+            if (g < 2 && t0 + tl < n_b) steps[2 * tl] = (uint16_t)(g ? ks[1] : ks[0]);
+        }
+
+        // ---- Values
+        uint32_t lo4[8], hi4[8], vs[8];
+        float vinv[8];
+#pragma unroll
+        for (int jj = 0; jj < 8; ++jj) {
+            uint32_t top = 0;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) top = max(top, mag(xv[jj][k]));
+            vs[jj] = row_step(row16_umax(top), vinv[jj]);
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            lo4[k] = low_bytes(code_of(xv[0][k], vinv[0]), code_of(xv[1][k], vinv[1]), code_of(xv[2][k], vinv[2]), code_of(xv[3][k], vinv[3]));
+            hi4[k] = low_bytes(code_of(xv[4][k], vinv[4]), code_of(xv[5][k], vinv[5]), code_of(xv[6][k], vinv[6]), code_of(xv[7][k], vinv[7]));
+        }
+        uint32_t mine = 0;
+#pragma unroll
+        for (int jj = 0; jj < 8; ++jj) mine = n == jj ? vs[jj] : mine;
+        {
+            const int tl = (n & 7) < 4 ? 4 * g + (n & 7) : 12 + 4 * g + (n & 7);
+            if (n < 8 && t0 + tl < n_b) steps[2 * tl + 1] = (uint16_t)mine;
+        }
+        // channel 8 n + k is place 8 (n % 2) + k of channel block n / 2; blocks lie in pairs
+        uint8_t* to = vb + (n >> 2) * 1024 + g * 256 + (n & 1) * 128;
+        if (full) {
+            const bool odd = n & 2;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const uint32_t a = dpp_u32<0x4E>(odd ? lo4[k] : lo4[k + 4]), c = dpp_u32<0x4E>(odd ? hi4[k] : hi4[k + 4]);
+                *(uint4*)(to + (odd ? 64 : 0) + 16 * k) = odd ? make_uint4(a, c, lo4[k + 4], hi4[k + 4]) : make_uint4(lo4[k], hi4[k], a, c);
+            }
+        } else {
+            to += (n & 2) * 4;
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+#pragma unroll
+                for (int jj = 0; jj < 8; ++jj) {
+                    const int tl = jj < 4 ? 4 * g + jj : 12 + 4 * g + jj;
+                    if (t0 + tl < n_b) to[16 * k + jj] = (uint8_t)((jj < 4 ? lo4[k] : hi4[k]) >> (8 * (jj & 3)));
+                }
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// One token a sequence: k~ = k R_r in fp32, thread (half, j) of 2 x 128 sums 64 channels of column j.  Bound by two round trips: the
+// length and the inputs, then R_r (32 KB at r = 64, all loads of a thread independent).  The last work-group of a sequence writes the new
+// length: seq_len_out may be seq_len itself, which all of them read.
+template <typename T>
+__global__ __launch_bounds__(256) void append_q8(int Hkv, int cap, int r, const T* __restrict__ k_new, const T* __restrict__ v_new,
+                                                 const float* __restrict__ Rr, uint8_t* __restrict__ Kq, uint8_t* __restrict__ Vq,
+                                                 const int32_t* seq_len, int32_t* seq_len_out, int32_t* __restrict__ tickets)
+{
+    __shared__ float ks[D], part[D];
+    __shared__ uint32_t tops[4];
+    const int h = blockIdx.x, b = blockIdx.y, u = b * Hkv + h;
+    const int tid = threadIdx.x, wave = tid >> 6, j = tid & 127, half = tid >> 7;
+    const int len = seq_len[b];
+    const bool room = len >= 0 && len < cap;
+    float x = 0.f;
+    if (half) x = ld_elem(v_new + (size_t)u * D + j);
+    else ks[j] = ld_elem(k_new + (size_t)u * D + j);
+    __syncthreads();
+    float a = 0.f;
+    if (j < r) {
+        const float* Rc = Rr + (size_t)u * D * r + (size_t)(64 * half) * r + j;
+#pragma unroll 16
+        for (int c = 0; c < 64; ++c) a = fmaf(ks[64 * half + c], Rc[c * r], a);
+    }
+    if (half) part[j] = a;
+    __syncthreads();
+    if (!half) x = j < r ? a + part[j] : 0.f;       // waves 0 and 1: the rotated Key; 2 and 3: the Value
+    uint32_t top = mag(x);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
+    if ((tid & 63) == 0) tops[wave] = top;
+    __syncthreads();
+    float inv;
+    const uint32_t step = row_step(max(tops[2 * half], tops[2 * half + 1]), inv);
+    if (room) {
+        const int rp = keep_padded(r);
+        const size_t blocks = slab_tokens(cap) / 32;
+        uint8_t* kb = Kq + ((size_t)u * blocks + (len >> 5)) * q8_kblock(rp);
+        const uint8_t code = (uint8_t)code_of(x, inv);
+        if (half) Vq[(size_t)u * blocks * (32 * D) + q8_vidx(len, j)] = code;
+        else if (j < rp) kb[q8_kplace(len, j)] = code;
+        if (j == 0) ((uint16_t*)(kb + 32 * rp))[2 * (len & 31) + half] = (uint16_t)step;
+    }
+    if (tid == 0 && atomicAdd(tickets + b, 1) == Hkv - 1) {
+        tickets[b] = 0;
+        seq_len_out[b] = room ? len + 1 : len;
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Both caches back to rows, a wave a block of 32 tokens: what was read 16 bytes a lane is written as whole rows, the Values by the same
+// transpose of bytes as above.  Bound by memory (5 of 7 bytes are written at r = 64 in bf16).
+__device__ __forceinline__ float code_at(uint32_t w, int i) { return (float)((int32_t)(w << (24 - 8 * i)) >> 24); }
+__device__ __forceinline__ void store8(bf16_t* p, const float (&x)[8])
+{
+    uint32_t d[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) d[i] = __builtin_bit_cast(uint32_t, (bf16x2){(__bf16)x[2 * i], (__bf16)x[2 * i + 1]});
+    nt_store16(p, make_uint4(d[0], d[1], d[2], d[3]));
+}
+__device__ __forceinline__ void store8(float* p, const float (&x)[8])
+{
+    nt_store16(p, make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])));
+    nt_store16(p + 4, make_uint4(__float_as_uint(x[4]), __float_as_uint(x[5]), __float_as_uint(x[6]), __float_as_uint(x[7])));
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void unpack_q8(int Hkv, int cap, int r, const uint8_t* __restrict__ Kq, const uint8_t* __restrict__ Vq,
+                                                 const int32_t* __restrict__ seq_len, T* __restrict__ k_rows, T* __restrict__ v_rows)
+{
+    const int h = blockIdx.y, b = blockIdx.z;
+    const size_t u = (size_t)b * Hkv + h;
+    const int lane = threadIdx.x & 63, g = lane >> 4, n = lane & 15;
+    const int t0 = (blockIdx.x * 4 + (threadIdx.x >> 6)) * 32;
+    const int len = seq_len ? min(max(seq_len[b], 0), cap) : cap;
+    if (t0 >= len) return;
+    const int rp = keep_padded(r);
+    const size_t blocks = slab_tokens(cap) / 32;
+    const uint8_t* kb = Kq + (u * blocks + (t0 >> 5)) * q8_kblock(rp);
+    const uint16_t* steps = (const uint16_t*)(kb + 32 * rp);
+    auto step = [&](int tl, int which) { return __uint_as_float((uint32_t)steps[2 * tl + which] << 16); };
+    if (k_rows) {
+        // consecutive lanes take consecutive octets of a token: whole rows are written
+        const int octs = (r + 7) / 8;
+        const bool wide = r % 8 == 0 && ((uintptr_t)k_rows & 15) == 0;
+        T* to = k_rows + (u * cap + t0) * (size_t)r;
+        for (int p = lane; p < 16 * octs; p += 64) {
+            const int tn = p / octs, oct = p - tn * octs;
+            const uint4 raw = *(const uint4*)(kb + oct * 256 + tn * 16);
+#pragma unroll
+            for (int tb = 0; tb < 2; ++tb) {
+                const int tl = 16 * tb + tn;
+                if (t0 + tl >= len) continue;
+                const float s = step(tl, 0);
+                float x[8];
+#pragma unroll
+                for (int c = 0; c < 8; ++c) {
+                    const uint32_t w = tb ? (c < 4 ? raw.z : raw.w) : (c < 4 ? raw.x : raw.y);
+                    x[c] = code_at(w, c & 3) * s;
+                }
+                T* at = to + (size_t)tl * r + 8 * oct;
+                if (wide) store8(at, x);
+                else
+#pragma unroll
+                    for (int c = 0; c < 8; ++c)
+                        if (8 * oct + c < r) st_elem(at + c, x[c]);
+            }
+        }
+    }
+    if (v_rows) {
+        const bool wide = ((uintptr_t)v_rows & 15) == 0;
+        const uint8_t* from = Vq + (u * blocks + (t0 >> 5)) * (size_t)(32 * D) + (n >> 2) * 1024 + g * 256 + (n & 1) * 128 + (n & 2) * 4;
+        T* to = v_rows + (u * cap + t0) * (size_t)D;
+        uint2 raw[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) raw[k] = *(const uint2*)(from + 16 * k);
+#pragma unroll
+        for (int jj = 0; jj < 8; ++jj) {
+            const int tl = jj < 4 ? 4 * g + jj : 12 + 4 * g + jj;
+            if (t0 + tl >= len) continue;
+            const float s = step(tl, 1);
+            float x[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) x[k] = code_at(jj < 4 ? raw[k].x : raw[k].y, jj & 3) * s;
+            T* at = to + (size_t)tl * D + 8 * n;
+            if (wide) store8(at, x);
+            else
+#pragma unroll
+                for (int k = 0; k < 8; ++k) st_elem(at + k, x[k]);
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+template <typename T, int R>
+static hipError_t compress_q8_r(const RowsDev& keys, const RowsDev& vals, int B, int Hkv, int cap, int r, int each, const float* Rr, uint8_t* Kq,
+                                uint8_t* Vq, int32_t* seq_len_out, hipStream_t st)
+{
+    const size_t lds = (size_t)R * D * 4;
+    const hipError_t e = allow_dynamic_lds((const void*)compress_q8<T, R>, lds);
+    if (e != hipSuccess) return e;
+    const int nb = keys.n_tokens > 0 ? (int)(((int64_t)keys.n_tokens + each - 1) / each) : 1;
+    compress_q8<T, R><<<dim3(nb, Hkv, B), 256, lds, st>>>(keys, vals, Hkv, cap, r, each, Rr, Kq, Vq, seq_len_out);
+    return hipGetLastError();
+}
+
+hipError_t launch_compress_q8(int dtype, const RowsDev& keys, const RowsDev& vals, int B, int Hkv, int cap, int r, const float* Rr, void* Kq,
+                              void* Vq, int32_t* seq_len_out, int n_cu, hipStream_t st)
+{
+    // 128 tokens a work-group, a block a wave, while that gives no more than eight work-groups a compute unit; then longer pieces, so that R_r
+    // is made ready less often
+    const int64_t total = (int64_t)B * Hkv * keys.n_tokens;
+    int each = 128;
+    while (each < 1024 && total > (int64_t)each * 8 * n_cu) each *= 2;
+    auto go = [&](auto t) {
+        typedef decltype(t) T;
+        uint8_t *kq = (uint8_t*)Kq, *vq = (uint8_t*)Vq;
+        const int w = (r + 31) / 32;
+        if (w == 1) return compress_q8_r<T, 32>(keys, vals, B, Hkv, cap, r, each, Rr, kq, vq, seq_len_out, st);
+        if (w == 2) return compress_q8_r<T, 64>(keys, vals, B, Hkv, cap, r, each, Rr, kq, vq, seq_len_out, st);
+        if (w == 3) return compress_q8_r<T, 96>(keys, vals, B, Hkv, cap, r, each, Rr, kq, vq, seq_len_out, st);
+        return compress_q8_r<T, 128>(keys, vals, B, Hkv, cap, r, each, Rr, kq, vq, seq_len_out, st);
+    };
+    return dtype == 0 ? go(0.f) : go(bf16_t{});
+}
+
+hipError_t launch_append_q8(int dtype, int B, int Hkv, int cap, int r, const void* k_new, const void* v_new, const float* Rr, void* Kq, void* Vq,
+                            const int32_t* seq_len, int32_t* seq_len_out, int32_t* tickets, hipStream_t st)
+{
+    const dim3 grid(Hkv, B);
+    if (dtype == 0)
+        append_q8<float><<<grid, 256, 0, st>>>(Hkv, cap, r, (const float*)k_new, (const float*)v_new, Rr, (uint8_t*)Kq, (uint8_t*)Vq, seq_len,
+                                               seq_len_out, tickets);
+    else
+        append_q8<bf16_t><<<grid, 256, 0, st>>>(Hkv, cap, r, (const bf16_t*)k_new, (const bf16_t*)v_new, Rr, (uint8_t*)Kq, (uint8_t*)Vq, seq_len,
+                                                seq_len_out, tickets);
+    return hipGetLastError();
+}
+
+hipError_t launch_unpack_q8(int dtype, int B, int Hkv, int cap, int r, const void* Kq, const void* Vq, const int32_t* seq_len, void* k_rows,
+                            void* v_rows, hipStream_t st)
+{
+    const dim3 grid((cap + 127) / 128, Hkv, B);
+    if (dtype == 0)
+        unpack_q8<float><<<grid, 256, 0, st>>>(Hkv, cap, r, (const uint8_t*)Kq, (const uint8_t*)Vq, seq_len, (float*)k_rows, (float*)v_rows);
+    else
+        unpack_q8<bf16_t><<<grid, 256, 0, st>>>(Hkv, cap, r, (const uint8_t*)Kq, (const uint8_t*)Vq, seq_len, (bf16_t*)k_rows, (bf16_t*)v_rows);
+    return hipGetLastError();
+}
+
+}  // namespace rk

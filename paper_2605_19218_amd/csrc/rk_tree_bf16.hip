@@ -1,0 +1,7 @@
+// Attention of several query rows a KV head (rk_attn_rows.hpp), packed bf16 cache, bf16 rows.
+#include <type_traits>
+#include "rk_attn_rows.hpp"
+
+namespace rk {
+hipError_t launch_rows_bf16(const RowsArgs& a, int nrb16, hipStream_t st) { return launch_rows_fmt<ROWS_BF16>(a, nrb16, st); }
+}  // namespace rk

@@ -1,0 +1,308 @@
+"""The attention of drafted tokens, and the way of accepted ones into the text segment, against plain forms in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2605_19218_amd as rk
+from rows_util import D, DEV, attend, f64, kind, normal, rotation, tolerance, up32
+
+pytestmark = pytest.mark.gpu
+BF, F32 = torch.bfloat16, torch.float32
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = rk.rk_create(0)
+    yield c
+    rk.rk_destroy(c)
+
+
+def tree_mask(g, T):
+    seen = []
+    for i in range(T):
+        p = int(g.integers(-1, i)) if i else -1
+        seen.append((seen[p] if p >= 0 else 0) | 1 << i)
+    return seen
+
+
+def words(mask):
+    return torch.tensor([[x - (1 << 64) if x >> 63 else x for x in row] for row in mask], dtype=torch.int64, device=DEV)
+
+
+class Layer:
+    """Caches (bf16 / fp32 packed, or 8 bits) with known values, text and drafts whose rows behind their end hold NaN and infinities."""
+
+    def __init__(self, ctx, g, dt, q8, B, Hq, Hkv, r, lens, tl, T, nd, mask="tree", poison=True):
+        self.ctx, self.dt, self.q8, self.lens, self.tl, self.T, self.nd = ctx, dt, q8, lens, tl, T, nd
+        N, M = max(lens), max(tl) if tl else 0
+        self.N, self.M, cap = N, M, up32(N)
+        self.Rr = rotation(g, B, Hkv, r)
+        self.dmu = torch.from_numpy(g.standard_normal((B, Hkv, D)).astype(np.float32) * 0.2).to(DEV)
+        self.len = torch.tensor(lens, dtype=torch.int32, device=DEV)
+        self.lay = rk.Layout(B, Hq, Hkv, r, kind(dt), cap, N, seq_len=self.len)
+        kb, vb = (rk.rk_cache_bytes_quant if q8 else rk.rk_cache_bytes)(self.lay)
+        self.k = torch.full((kb,), 0xff if poison else 0, dtype=torch.uint8, device=DEV)
+        self.v = torch.full((vb,), 0xff if poison else 0, dtype=torch.uint8, device=DEV)
+        K, V = normal(g, (B, Hkv, max(N, 1), D), dt, 1.5), normal(g, (B, Hkv, max(N, 1), D), dt)
+        put = rk.rk_compress_quant if q8 else rk.rk_compress
+        put(ctx, self.lay, rk.Rows(K, N, n_tokens_dev=self.len), self.Rr, self.k, values=rk.Rows(V, N, n_tokens_dev=self.len), v_cache=self.v)
+        self.q = normal(g, (B, T, Hq, D), dt)
+        self.text = None
+        if tl:
+            self.tk, self.tv = normal(g, (B, M + T + 1, Hkv, D), dt).transpose(1, 2), normal(g, (B, M + T + 1, Hkv, D), dt).transpose(1, 2)
+            for b in range(B):
+                if poison:
+                    self.tk[b, :, tl[b]:], self.tv[b, :, tl[b]:] = float("inf"), float("nan")
+            self.text_len = torch.tensor(tl, dtype=torch.int32, device=DEV)
+            self.text = rk.Text(self.tk, self.tv, M, len=self.text_len)
+        self.kd, self.vd = normal(g, (B, T, Hkv, D), dt).transpose(1, 2), normal(g, (B, T, Hkv, D), dt).transpose(1, 2)
+        for b in range(B):
+            if poison:
+                self.kd[b, :, nd[b]:], self.vd[b, :, nd[b]:] = float("nan"), float("-inf")
+        self.n_drafts = torch.tensor(nd, dtype=torch.int32, device=DEV)
+        self.mask = None
+        if mask == "tree":
+            self.mask = [tree_mask(g, T) for _ in range(B)]
+        elif mask == "odd":                 # anything: empty rows, rows without themselves, bits behind the end
+            self.mask = [[int(x) for x in g.integers(0, 2 ** 63, T)] for _ in range(B)]
+            for b in range(B):
+                self.mask[b][int(g.integers(T))] = 0
+                self.mask[b][0] |= 1 << 63
+        self.drafts = rk.Drafts(self.kd, self.vd, T, mask=None if self.mask is None else words(self.mask), n_tokens_dev=self.n_drafts)
+        self.out = torch.full((B, T, Hq, D), 5.0, dtype=dt, device=DEV)
+        self.ws = torch.full((rk.rk_tree_workspace_size(ctx, self.lay, T),), 0xff, dtype=torch.uint8, device=DEV)
+
+    def call(self, stream=None, out=None):
+        f = rk.rk_decode_attn_tree_quant if self.q8 else rk.rk_decode_attn_tree
+        f(self.ctx, self.lay, self.q, self.k, self.v, self.Rr, self.dmu, self.text, self.drafts, 0.0, self.out if out is None else out, self.ws,
+          stream=stream)
+
+    def stored(self):
+        L = self.lay
+        k = torch.zeros(L.batch, L.n_kv_heads, L.capacity, L.keep, dtype=F32, device=DEV)
+        v = torch.zeros(L.batch, L.n_kv_heads, L.capacity, D, dtype=F32, device=DEV)
+        if self.q8:
+            rk.rk_unpack_cache_quant(self.ctx, rk.Layout(L.batch, L.n_kv_heads, L.n_kv_heads, L.keep, rk.RK_F32, L.capacity, 0, seq_len=self.len),
+                                  self.k, self.v, k, v)
+        else:
+            k, v = k.to(self.dt), v.to(self.dt)
+            rk.rk_unpack_cache(self.ctx, L, self.k, self.v, k, v)
+        return f64(k), f64(v)
+
+    def check(self):
+        got = f64(self.out)
+        ref, size, top = attend(f64(self.q), *self.stored(), self.lens, f64(self.Rr), f64(self.dmu),
+                                (f64(self.tk), f64(self.tv)) if self.text else None, self.tl, (f64(self.kd), f64(self.vd)), self.nd, self.mask)
+        tol = tolerance(ref, size, top, self.N + self.M + self.T, self.dt)
+        for b, n in enumerate(self.nd):
+            e, lim = np.abs(got[b, :n] - ref[b, :n]), tol[b, :n]
+            assert np.isfinite(got[b, :n]).all() and (e <= lim).all(), (b, (e / np.maximum(lim, 1e-30)).max())
+            assert (got[b, n:] == 5.0).all()
+        return got, ref
+
+
+SHAPES = [
+    # B, Hq, Hkv, r, lens, text, T, drafts
+    (1, 2, 2, 32, [70], [9], 1, [1]),
+    (2, 8, 2, 64, [300, 33], [40, 0], 4, [4, 3]),
+    (3, 28, 4, 64, [1000, 0, 1], [70, 33, 0], 16, [16, 5, 0]),
+    (1, 7, 1, 37, [257], None, 9, [9]),
+    (2, 8, 8, 128, [513, 100], [1, 64], 33, [33, 32]),
+    (1, 16, 1, 96, [650], [130], 64, [64]),
+    (2, 3, 3, 16, [31, 2], [3, 31], 64, [40, 64]),
+    (1, 24, 1, 80, [0], None, 7, [7]),
+    (1, 32, 8, 1, [129], [300], 8, [8]),
+    (2, 48, 1, 112, [400, 90], None, 3, [2, 3]),
+]
+
+
+@pytest.mark.parametrize("dt,q8", [(BF, False), (F32, False), (BF, True), (F32, True)])
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "%dx%d-%d-r%d-T%d" % (s[0], s[1], s[2], s[3], s[6]))
+@pytest.mark.parametrize("mask", ["tree", "chain", "odd"])
+def test_tree(ctx, dt, q8, shape, mask):
+    B, Hq, Hkv, r, lens, tl, T, nd = shape
+    x = Layer(ctx, np.random.default_rng(B + Hq + r + T), dt, q8, B, Hq, Hkv, r, lens, tl, T, nd, mask)
+    x.call()
+    x.check()
+
+
+@pytest.mark.parametrize("dt,q8", [(BF, False), (F32, False), (BF, True), (F32, True)])
+@pytest.mark.parametrize("splits", [1, 2, 5, 40])
+def test_splits(ctx, dt, q8, splits):
+    x = None
+    rk.rk_set_option(ctx, rk.RK_OPT_DECODE_SPLITS, splits)
+    try:
+        x = Layer(ctx, np.random.default_rng(splits), dt, q8, 2, 12, 4, 64, [900, 200], [100, 7], 10, [10, 6])
+        x.call()
+    finally:
+        rk.rk_set_option(ctx, rk.RK_OPT_DECODE_SPLITS, 0)
+    x.check()
+
+
+@pytest.mark.parametrize("dt,q8", [(BF, False), (F32, False), (BF, True)])
+def test_nothing_but_masks(ctx, dt, q8):
+    """No cache, no text: a row whose mask is empty is zeros, one that sees itself alone is its Value."""
+    x = Layer(ctx, np.random.default_rng(3), dt, q8, 1, 4, 2, 32, [0], None, 6, [6])
+    x.mask = [[0, 2, 0, 4 + 8, 1 << 40, 32]]
+    x.drafts.mask = words(x.mask)
+    x.call()
+    got, _ = x.check()
+    assert (got[0, [0, 2, 4]] == 0).all()
+    for i, j in ((1, 1), (5, 5)):
+        assert np.array_equal(got[0, i], f64(x.vd)[0, [0, 0, 1, 1], j])
+
+
+@pytest.mark.parametrize("dt,q8", [(BF, False), (F32, False), (BF, True), (F32, True)])
+@pytest.mark.parametrize("T", [5, 40])
+def test_masked_drafts_that_are_no_numbers(ctx, dt, q8, T):
+    """NaN and infinities in Keys and Values of a draft reach the rows that see it, and no other."""
+    x = Layer(ctx, np.random.default_rng(T), dt, q8, 1, 6, 2, 64, [150], [20], T, [T])
+    x.call()
+    clean = f64(x.out)
+    nan, inf = float("nan"), float("inf")
+    bad = {1: nan, 2: inf, 3: -inf, T - 1: nan}
+    for j, w in bad.items():
+        x.vd[0, :, j, 5], x.vd[0, :, j, 77] = w, w
+    x.kd[0, :, T - 1, 9] = nan
+    x.mask = [[m & ~sum(1 << j for j in bad) for m in x.mask[0]]]
+    see = {0: [1], 1: [2], 2: [3], 3: [2, 3], 4: [T - 1]}
+    for i, js in see.items():
+        x.mask[0][i] |= sum(1 << j for j in js)
+    x.drafts.mask = words(x.mask)
+    x.call()
+    got = f64(x.out)
+    hit = [5, 77]
+    rest = [c for c in range(D) if c not in hit]
+    assert np.isnan(got[0, 0][:, hit]).all() and (got[0, 1][:, hit] == inf).all() and (got[0, 2][:, hit] == -inf).all()
+    assert np.isnan(got[0, 3][:, hit]).all() and np.isnan(got[0, 4]).all()
+    assert np.isfinite(got[0, :4][..., rest]).all() and np.isfinite(got[0, 5:]).all()
+    for j in bad:                                  # the other rows: as with numbers in those places
+        x.vd[0, :, j, hit] = 0.0
+    x.kd[0, :, T - 1, 9] = 0.0
+    x.call()
+    same = f64(x.out)
+    assert np.array_equal(got[0, 5:], same[0, 5:]) and np.array_equal(got[0, :4][..., rest], same[0, :4][..., rest])
+    assert not np.array_equal(same, clean)
+
+
+def test_minus_infinity_scores_weigh_nothing(ctx):
+    x = Layer(ctx, np.random.default_rng(1), BF, False, 1, 4, 2, 32, [0], [40], 3, [3])
+    x.q.abs_()
+    x.tk[0, :, :40] = float("-inf")                # every text score is minus infinity
+    x.call()
+    x.tl, x.text = None, None
+    x.check()
+
+
+def test_far_scores_do_not_lose_the_weights(ctx):
+    """Scores that rise by hundreds along the cache: the running maximum moves in every tile."""
+    for dt in (BF, F32):
+        x = Layer(ctx, np.random.default_rng(4), dt, False, 1, 2, 1, 32, [640], [32], 20, [20])
+        K = torch.zeros(1, 1, 640, D, dtype=dt, device=DEV)
+        K[..., :32] = torch.from_numpy(f64(x.Rr)[0, 0].T @ f64(x.q)[0, 0, 0])[None, None, None].to(dt).to(DEV) * \
+            torch.arange(640, device=DEV)[None, None, :, None].to(dt) / 16
+        eye = torch.eye(D, device=DEV)[:, :32].expand(1, 1, D, 32).contiguous()
+        rk.rk_compress(ctx, x.lay, rk.Rows(K, 640), eye, x.k)
+        x.call()
+        x.check()
+
+
+def test_streams_and_graph_replay(ctx):
+    x = Layer(ctx, np.random.default_rng(8), BF, True, 2, 8, 2, 64, [500, 77], [40, 3], 12, [12, 7])
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    x.call(stream=s)
+    s.synchronize()
+    want = x.out.clone()
+    x.check()
+    x.out.fill_(5.0)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(s):
+        x.call(stream=s)                          # (warm)
+        s.synchronize()
+        with torch.cuda.graph(graph, stream=s):
+            x.call(stream=s)
+    for i in range(4):
+        x.out.fill_(5.0)
+        eager = torch.randn(64, device=DEV).sum().item()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(x.out, want) and np.isfinite(eager)
+
+
+def test_two_calls_at_once(ctx):
+    """Calls with workspaces of their own may overlap on one context."""
+    a = Layer(ctx, np.random.default_rng(21), BF, False, 2, 8, 2, 64, [3000, 2000], [40, 3], 16, [16, 7])
+    b = Layer(ctx, np.random.default_rng(22), BF, True, 2, 8, 2, 64, [3000, 2000], [40, 3], 16, [16, 7])
+    s = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        a.call(stream=s[0])
+        b.call(stream=s[1])
+    torch.cuda.synchronize()
+    a.check()
+    b.check()
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("Hkv,T,P", [(1, 1, 1), (8, 8, 8), (3, 64, 64), (2, 20, 9)])
+def test_append_path(ctx, dt, Hkv, T, P):
+    B, M = 5, 30
+    g = np.random.default_rng(T + P)
+    tk, tv = normal(g, (B, M + P, Hkv, D), dt).transpose(1, 2), normal(g, (B, Hkv, M + P, D), dt)
+    tv = tv.clone().transpose(1, 2).contiguous().transpose(1, 2)
+    kd, vd = normal(g, (B, Hkv, T, D), dt), normal(g, (B, Hkv, T, D), dt)
+    nd = [T, T, max(T // 2, 1), 0, T]
+    lens = [0, M, 7, 3, M + P]                     # the last has no room
+    path = g.integers(0, T, (B, P)).astype(np.int32)
+    path[1] = np.minimum(path[1], T - 1)
+    npath = [P, max(P - 1, 0), P, P, P]
+    if P > 2:
+        path[0, 2] = -1                            # ends there
+    lay = rk.Layout(B, Hkv, Hkv, 32, kind(dt), 32, 0)
+    text = rk.Text(tk, tv, M, len=torch.tensor(lens, dtype=torch.int32, device=DEV))
+    drafts = rk.Drafts(kd, vd, T, n_tokens_dev=torch.tensor(nd, dtype=torch.int32, device=DEV))
+    wk, wv, n = f64(tk), f64(tv), list(lens)
+    for b in range(B):
+        for j in range(npath[b]):
+            p = int(path[b, j])
+            if not 0 <= p < nd[b] or n[b] >= M + P:
+                break
+            wk[b, :, n[b]], wv[b, :, n[b]] = f64(kd)[b, :, p], f64(vd)[b, :, p]
+            n[b] += 1
+    out = torch.full((B,), -1, dtype=torch.int32, device=DEV)
+    dev = [torch.from_numpy(path).to(DEV), torch.tensor(npath, dtype=torch.int32, device=DEV)]
+    for to in (out, text.len):                     # twice: the second writes the same rows and the length itself
+        rk.rk_append_text_path(ctx, lay, text, drafts, *dev, to)
+        assert to.tolist() == n
+        assert np.array_equal(f64(tk), wk) and np.array_equal(f64(tv), wv)
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+def test_speculative_steps_together(ctx, dt):
+    """As a server uses them: a prompt into 8 bits, a tree over it, its accepted path into the text, the next token over cache and text, a
+    token into the 8-bit cache, and the next tree."""
+    B, Hq, Hkv, r, N, T = 2, 8, 2, 64, 200, 12
+    g = np.random.default_rng(77)
+    x = Layer(ctx, g, dt, True, B, Hq, Hkv, r, [N, 150], [20, 5], T, [12, 8], poison=False)
+    x.lay.capacity = up32(N)
+    x.call()
+    x.check()
+    path = torch.tensor([[0, 3, 4, 9], [1, 2, 0, 0]], dtype=torch.int32, device=DEV)
+    rk.rk_append_text_path(ctx, x.lay, x.text, x.drafts, path, torch.tensor([4, 2], dtype=torch.int32, device=DEV), x.text_len)
+    assert x.text_len.tolist() == [24, 7]
+    for b, p in ((0, [0, 3, 4, 9]), (1, [1, 2])):
+        for i, j in enumerate(p):
+            assert torch.equal(x.tk[b, :, x.tl[b] + i], x.kd[b, :, j]) and torch.equal(x.tv[b, :, x.tl[b] + i], x.vd[b, :, j])
+    x.tl, x.text.max_len = [24, 7], 24
+    q1, o1 = x.q[:, 0].contiguous(), torch.zeros(B, Hq, D, dtype=dt, device=DEV)
+    rk.rk_decode_attn_quant(ctx, x.lay, q1, x.k, x.v, x.Rr, x.dmu, x.text, 0.0, o1, x.ws)
+    ref, size, top = attend(f64(q1)[:, None], *x.stored(), x.lens, f64(x.Rr), f64(x.dmu), (f64(x.tk), f64(x.tv)), x.tl)
+    assert (np.abs(f64(o1)[:, None] - ref) <= tolerance(ref, size, top, N + 24, dt)).all()
+    rk.rk_append_quant(ctx, x.lay, normal(g, (B, Hkv, D), dt), normal(g, (B, Hkv, D), dt), x.Rr, x.k, x.v, x.len)
+    x.lens = [N + 1, 151]
+    assert x.len.tolist() == x.lens
+    x.lay.max_seq_len = N + 1
+    x.call()
+    x.check()
