@@ -266,7 +266,7 @@ def _hold(s):
     if c["text"]:
         s.text = rk.Text(s.kt, s.vt, c["text"], len=s.text_len)
     if T:
-        s.drafts = rk.Drafts(s.kd, s.vd, T, mask=s.bits, n_tokens_dev=s.n_drafts)
+        s.drafts = rk.Drafts(s.kd, s.vd, T, mask=s.bits, n_tokens_dev=s.n_drafts if c["op"] == "tree" else None)
     if c["op"] in ("decode", "tree"):
         s.out = torch.zeros(B, max(T, 1), Hq, D, device=DEV, dtype=dt)
         s.ws = torch.empty(rk.rk_tree_workspace_size(ctx, s.lay, max(T, 1)), dtype=torch.uint8, device=DEV)
