@@ -297,7 +297,7 @@ struct RowsPlan { int nrb16, nrb, Sv, Sr; };
 int rows_per_block(const rk_layout* L, int T)       // in sixteens; fp32 rows take twice the registers
 {
     const int64_t rows = (int64_t)T * (L->n_q_heads / L->n_kv_heads);
-    return rows <= 16 ? 1 : rows <= 32 || L->dtype == RK_F32 ? 2 : 4;
+    return rows <= 16 ? 1 : rows <= 32 || L->dtype == RK_F32 ? 2 : rows <= 64 ? 4 : 8;
 }
 int64_t row_blocks(const rk_layout* L, int T)
 {
@@ -327,7 +327,8 @@ RowsPlan rows_plan(const rk_ctx* ctx, const rk_layout* L, int T, int text_rows, 
     const int tiles = (L->max_seq_len + 31) / 32, plain = (text_rows + 31) / 32 + (drafts ? (T + 31) / 32 : 0);
     const int most_v = tiles > 8 ? (tiles + 7) / 8 : 1, most_r = (plain + 3) / 4;
     const double es = (double)elem_size(L->dtype), cv = tiles * (q8 ? 1.0 : es) * (keep_padded(L->keep) + D), cr = plain * es * 2 * D;
-    int total = (int)(n_cu / groups);
+    // (the kernels of four and eight sixteens: two work-groups a compute unit)
+    int total = (int)((p.nrb16 >= 4 ? 2 : 1) * n_cu / groups);
     if (total < 1) total = 1;
     p.Sr = 0;
     if (plain) {

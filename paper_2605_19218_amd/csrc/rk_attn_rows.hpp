@@ -698,7 +698,7 @@ __device__ __forceinline__ float partial_weight(float m, float l, float M)
 }
 
 template <int FMT, int R, int NRB>
-__global__ __launch_bounds__(256, NRB == 1 ? 2 : 1) void attn_rows(RowsArgs A)
+__global__ __launch_bounds__(256, NRB == 1 && FMT != ROWS_F32 ? 2 : 1) void attn_rows(RowsArgs A)
 {
     constexpr bool F32IO = FMT == ROWS_F32 || FMT == ROWS_Q8_F32;
     typedef typename std::conditional<F32IO, float, bf16_t>::type T;
@@ -860,8 +860,7 @@ template <int FMT, int R>
 static void launch_rows_r(int nrb16, dim3 grid, const RowsArgs& a, hipStream_t st)
 {
     if (nrb16 == 1) attn_rows<FMT, R, 1><<<grid, 256, 0, st>>>(a);
-    else if (nrb16 == 2) attn_rows<FMT, R, 2><<<grid, 256, 0, st>>>(a);
-    else if constexpr (FMT == ROWS_BF16 || FMT == ROWS_Q8_BF16) attn_rows<FMT, R, 4><<<grid, 256, 0, st>>>(a);
+    else attn_rows<FMT, R, 2><<<grid, 256, 0, st>>>(a);
 }
 template <int FMT>
 static hipError_t launch_rows_fmt(const RowsArgs& a, int nrb16, hipStream_t st)

@@ -80,7 +80,7 @@ struct RowsArgs {
     void* out;
     float *ws_m, *ws_l, *ws_acc; // [B, T, Hq, S] and [B, T, Hq, S, d]
 };
-// fmt: ROWS_BF16, ROWS_F32, ROWS_Q8_BF16, ROWS_Q8_F32; nrb16: blocks of 16 rows a work-group takes (1, 2; 4 with bf16 rows)
+// fmt: ROWS_BF16, ROWS_F32, ROWS_Q8_BF16, ROWS_Q8_F32; nrb16: blocks of 16 rows a work-group takes (1, 2; with bf16 rows 4, 8 too)
 hipError_t launch_rows_bf16(const RowsArgs& a, int nrb16, hipStream_t st);
 hipError_t launch_rows_f32(const RowsArgs& a, int nrb16, hipStream_t st);
 hipError_t launch_rows_q8_bf16(const RowsArgs& a, int nrb16, hipStream_t st);

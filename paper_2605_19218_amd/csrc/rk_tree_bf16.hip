@@ -1,7 +1,10 @@
-// Attention of several query rows a KV head (rk_attn_rows.hpp), packed bf16 cache, bf16 rows.
+// Attention of several query rows a KV head (rk_attn_rows.hpp, rk_attn_block.hpp), packed bf16 cache, bf16 rows.
 #include <type_traits>
-#include "rk_attn_rows.hpp"
+#include "rk_attn_block.hpp"
 
 namespace rk {
-hipError_t launch_rows_bf16(const RowsArgs& a, int nrb16, hipStream_t st) { return launch_rows_fmt<ROWS_BF16>(a, nrb16, st); }
+hipError_t launch_rows_bf16(const RowsArgs& a, int nrb16, hipStream_t st) 
+{
+    return nrb16 <= 2 ? launch_rows_fmt<ROWS_BF16>(a, nrb16, st) : launch_block_fmt<ROWS_BF16>(a, nrb16, st);
+}
 }  // namespace rk
