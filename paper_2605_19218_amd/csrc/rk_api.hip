@@ -48,7 +48,7 @@ rk_status hip_fail(rk_ctx* ctx, hipError_t e, const char* what)
     return fail(ctx, RK_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
 }
 
-constexpr int APP_TICKETS = 1 << 16;   // >= batch
+constexpr int APP_TICKETS = CONTEXT_TICKETS;   // >= batch
 constexpr int DEC_COUNTERS = 1 << 16;  // units (b, h_kv, head group) whose split-K merge can ride in the split launch
 
 size_t elem_size(int dtype) { return dtype == RK_F32 ? 4 : 2; }
@@ -324,23 +324,38 @@ RowsPlan rows_plan(const rk_ctx* ctx, const rk_layout* L, int T, int text_rows, 
     p.nrb = (int)row_blocks(L, T);
     const int64_t groups = (int64_t)p.nrb * L->batch * L->n_kv_heads;
     const int n_cu = ctx ? ctx->n_cu : 256, slots = rows_slots(ctx, L, T);
-    const int tiles = (L->max_seq_len + 31) / 32, plain = (text_rows + 31) / 32 + (drafts ? (T + 31) / 32 : 0);
-    const int most_v = tiles > 8 ? (tiles + 7) / 8 : 1, most_r = (plain + 3) / 4;
-    const double es = (double)elem_size(L->dtype), cv = tiles * (q8 ? 1.0 : es) * (keep_padded(L->keep) + D), cr = plain * es * 2 * D;
-    // (the kernels of four and eight sixteens: two work-groups a compute unit)
-    int total = (int)((p.nrb16 >= 4 ? 2 : 1) * n_cu / groups);
-    if (total < 1) total = 1;
-    p.Sr = 0;
-    if (plain) {
-        p.Sr = (int)(total * cr / (cv + cr) + 0.5);
-        if (p.Sr > most_r) p.Sr = most_r;
-        if (p.Sr > slots / 2) p.Sr = slots / 2;
-        if (p.Sr < 1) p.Sr = 1;
+    const bool block = p.nrb16 >= 4;
+    // steps of a work-group: tokens of the cache, and full-width rows, that all of its waves take at once
+    const int step_v = p.nrb16 == 8 ? 64 : 128, step_r = 128;
+    const int nv = (L->max_seq_len + step_v - 1) / step_v, nr = block ? (text_rows + 127) / 128 + (drafts ? 1 : 0) : ((text_rows + 31) / 32 + (drafts ? (T + 31) / 32 : 0) + 3) / 4;
+    const double tv = 1.2, tr = 4.0, begin = 8.0;
+    (void)step_r; (void)q8;
+    const int most_v = nv < 1 ? 1 : nv, most_r = nr;
+    const int total = (int)(n_cu / groups) < 1 ? 1 : (int)(n_cu / groups);
+    p.Sv = 1;
+    p.Sr = nr ? 1 : 0;
+    double best = 1e30;
+    const int r0 = nr ? 1 : 0, r1 = nr < slots / 2 ? nr : slots / 2;
+    for (int r = r0; r <= r1; ++r) {
+        const int lo = total > r + 1 ? total - r : 1, hi = total > r + 1 ? total - r : 8;
+        for (int v = lo; v <= hi; ++v) {
+            const int sv = v > most_v ? most_v : v > slots - r ? slots - r : v;
+            const double wv = begin + (nv + sv - 1) / sv * tv, wr = r ? begin + (nr + r - 1) / r * tr : 0.0;
+            const double work = groups * (sv * wv + r * wr) / n_cu;
+            double cost = wv > wr ? wv : wr;
+            if (groups * (sv + r) > n_cu) {
+                const double rounds = (double)((groups * sv + n_cu - 1) / n_cu) * wv;
+                cost = rounds > work ? rounds : work;
+            }
+            cost += (double)L->batch * T * L->n_q_heads * (sv + r) * 520.0 * 2 / 4e6;
+            if (cost < best) { best = cost; p.Sv = sv; p.Sr = r; }
+        }
     }
-    p.Sv = total - p.Sr;
-    if (ctx && ctx->decode_splits > 0) p.Sv = ctx->decode_splits;
-    else if (p.Sv > most_v) p.Sv = most_v;
-    if (p.Sv > slots - p.Sr) p.Sv = slots - p.Sr;
+    (void)most_r;
+    if (ctx && ctx->decode_splits > 0) {
+        p.Sv = ctx->decode_splits;
+        if (p.Sv > slots - p.Sr) p.Sv = slots - p.Sr;
+    }
     if (p.Sv < 1) p.Sv = 1;
     return p;
 }

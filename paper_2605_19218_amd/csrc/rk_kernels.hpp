@@ -50,6 +50,11 @@ hipError_t launch_append(int dtype, int B, int Hkv, int cap, int r, const void* 
 hipError_t launch_unpack(int dtype, int U, int cap, int r, const void* Kp, const void* Vc, void* k_rows,
                          void* v_rows, hipStream_t st);
 
+// A context's counters, one a sequence: from one to the next, so that the atomics of different sequences meet on lines of their own while there is
+// room (64 x 32 work-groups of a few rows each, four counters' atomics on a line: 51 us, APART_US).
+constexpr int CONTEXT_TICKETS = 1 << 16;
+inline int tickets_apart(int B) { return B <= CONTEXT_TICKETS / 32 ? 32 : 1; }
+
 // ---- rk_q8.hip: the 8-bit caches ---------------------------------------------
 hipError_t launch_compress_q8(int dtype, const RowsDev& keys, const RowsDev& vals, int B, int Hkv, int cap, int r, const float* Rr, void* Kq,
                               void* Vq, int32_t* seq_len_out, int n_cu, hipStream_t st);

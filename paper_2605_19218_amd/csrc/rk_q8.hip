@@ -256,7 +256,7 @@ __global__ __launch_bounds__(256) void compress_q8(RowsDev keys, RowsDev vals, i
 template <typename T>
 __global__ __launch_bounds__(256) void append_q8(int Hkv, int cap, int r, const T* __restrict__ k_new, const T* __restrict__ v_new,
                                                  const float* __restrict__ Rr, uint8_t* __restrict__ Kq, uint8_t* __restrict__ Vq,
-                                                 const int32_t* seq_len, int32_t* seq_len_out, int32_t* __restrict__ tickets)
+                                                 const int32_t* seq_len, int32_t* seq_len_out, int32_t* __restrict__ tickets, int apart)
 {
     __shared__ float ks[D], part[D];
     __shared__ uint32_t tops[4];
@@ -293,8 +293,8 @@ __global__ __launch_bounds__(256) void append_q8(int Hkv, int cap, int r, const 
         else if (j < rp) kb[q8_kplace(len, j)] = code;
         if (j == 0) ((uint16_t*)(kb + 32 * rp))[2 * (len & 31) + half] = (uint16_t)step;
     }
-    if (tid == 0 && atomicAdd(tickets + b, 1) == Hkv - 1) {
-        tickets[b] = 0;
+    if (tid == 0 && atomicAdd(tickets + (size_t)b * apart, 1) == Hkv - 1) {
+        tickets[(size_t)b * apart] = 0;
         seq_len_out[b] = room ? len + 1 : len;
     }
 }
@@ -422,10 +422,10 @@ hipError_t launch_append_q8(int dtype, int B, int Hkv, int cap, int r, const voi
     const dim3 grid(Hkv, B);
     if (dtype == 0)
         append_q8<float><<<grid, 256, 0, st>>>(Hkv, cap, r, (const float*)k_new, (const float*)v_new, Rr, (uint8_t*)Kq, (uint8_t*)Vq, seq_len,
-                                               seq_len_out, tickets);
+                                               seq_len_out, tickets, tickets_apart(B));
     else
         append_q8<bf16_t><<<grid, 256, 0, st>>>(Hkv, cap, r, (const bf16_t*)k_new, (const bf16_t*)v_new, Rr, (uint8_t*)Kq, (uint8_t*)Vq, seq_len,
-                                                seq_len_out, tickets);
+                                                seq_len_out, tickets, tickets_apart(B));
     return hipGetLastError();
 }
 

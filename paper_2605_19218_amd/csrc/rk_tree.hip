@@ -81,7 +81,7 @@ hipError_t launch_rows_merge(int dtype, const RowsArgs& a, hipStream_t st)
 // bytes a lane.  The path ends at its first entry that is no draft, and where the segment is full.  The last work-group of a sequence writes the
 // length: len_out may be the length that all of them read.
 template <typename T>
-__global__ __launch_bounds__(256) void append_path(PathArgs A, int32_t* __restrict__ tickets)
+__global__ __launch_bounds__(256) void append_path(PathArgs A, int32_t* __restrict__ tickets, int apart)
 {
     constexpr int PR = D * (int)sizeof(T) / 16;          // 16-byte pieces of a row
     const int h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, lane = tid & 63;
@@ -103,8 +103,8 @@ __global__ __launch_bounds__(256) void append_path(PathArgs A, int32_t* __restri
         else ((uint4*)((T*)A.text_v + dst))[piece] = ((const uint4*)((const T*)A.draft_v + src))[piece];
     }
     __syncthreads();
-    if (tid == 0 && atomicAdd(tickets + b, 1) == (int)(gridDim.x * gridDim.y) - 1) {
-        tickets[b] = 0;
+    if (tid == 0 && atomicAdd(tickets + (size_t)b * apart, 1) == (int)(gridDim.x * gridDim.y) - 1) {
+        tickets[(size_t)b * apart] = 0;
         A.len_out[b] = len + n;
     }
 }
@@ -112,8 +112,8 @@ __global__ __launch_bounds__(256) void append_path(PathArgs A, int32_t* __restri
 hipError_t launch_append_path(int dtype, const PathArgs& a, int32_t* tickets, hipStream_t st)
 {
     const dim3 grid((a.P + 7) / 8, a.Hkv, a.B);
-    if (dtype == 0) append_path<float><<<grid, 256, 0, st>>>(a, tickets);
-    else append_path<bf16_t><<<grid, 256, 0, st>>>(a, tickets);
+    if (dtype == 0) append_path<float><<<grid, 256, 0, st>>>(a, tickets, tickets_apart(a.B));
+    else append_path<bf16_t><<<grid, 256, 0, st>>>(a, tickets, tickets_apart(a.B));
     return hipGetLastError();
 }
 
