@@ -326,12 +326,13 @@ RowsPlan rows_plan(const rk_ctx* ctx, const rk_layout* L, int T, int text_rows, 
     const int n_cu = ctx ? ctx->n_cu : 256, slots = rows_slots(ctx, L, T);
     const bool block = p.nrb16 >= 4;
     // steps of a work-group: tokens of the cache, and full-width rows, that all of its waves take at once
-    const int step_v = p.nrb16 == 8 ? 64 : 128, step_r = 128;
-    const int nv = (L->max_seq_len + step_v - 1) / step_v, nr = block ? (text_rows + 127) / 128 + (drafts ? 1 : 0) : ((text_rows + 31) / 32 + (drafts ? (T + 31) / 32 : 0) + 3) / 4;
+    const int step_v = p.nrb16 == 8 ? 32 : p.nrb16 == 4 ? 64 : 128, step_r = 128;
+    const int nv = (L->max_seq_len + step_v - 1) / step_v, nr = block ? (text_rows + 63) / 64 + (drafts ? 1 : 0) : ((text_rows + 31) / 32 + (drafts ? (T + 31) / 32 : 0) + 3) / 4;
     const double tv = 1.2, tr = 4.0, begin = 8.0;
+    const int n_wg = block ? 2 * n_cu : n_cu;        // work-groups at once
     (void)step_r; (void)q8;
     const int most_v = nv < 1 ? 1 : nv, most_r = nr;
-    const int total = (int)(n_cu / groups) < 1 ? 1 : (int)(n_cu / groups);
+    const int total = (int)(n_wg / groups) < 1 ? 1 : (int)(n_wg / groups);
     p.Sv = 1;
     p.Sr = nr ? 1 : 0;
     double best = 1e30;
@@ -341,10 +342,10 @@ RowsPlan rows_plan(const rk_ctx* ctx, const rk_layout* L, int T, int text_rows, 
         for (int v = lo; v <= hi; ++v) {
             const int sv = v > most_v ? most_v : v > slots - r ? slots - r : v;
             const double wv = begin + (nv + sv - 1) / sv * tv, wr = r ? begin + (nr + r - 1) / r * tr : 0.0;
-            const double work = groups * (sv * wv + r * wr) / n_cu;
+            const double work = groups * (sv * wv + r * wr) / n_wg;
             double cost = wv > wr ? wv : wr;
-            if (groups * (sv + r) > n_cu) {
-                const double rounds = (double)((groups * sv + n_cu - 1) / n_cu) * wv;
+            if (groups * (sv + r) > n_wg) {
+                const double rounds = (double)((groups * sv + n_wg - 1) / n_wg) * wv;
                 cost = rounds > work ? rounds : work;
             }
             cost += (double)L->batch * T * L->n_q_heads * (sv + r) * 520.0 * 2 / 4e6;

@@ -10,15 +10,15 @@
 //   S^T[token][row] = K . q~^T, O^T[channel][row] = V^T . P^T: lane (h, n) = (lane / 32, lane % 32) holds row n's scores of tokens 8 j + 4 h ..+3,
 //   j < 4.  Step s of the second product takes j = s and j = s + 2 of them as they are: tokens 4 g ..+3 and 16 + 4 g ..+3, g = 2 s + h, which is a
 //   16-byte piece of the Value cache; a Key operand is one of the Key cache.  So the stages are copied piece by piece.
-// RW: row groups of a work-group, 32 rows each; the 8 / RW waves of a group take a tile of a stage each.
+// RW: row groups of a work-group, 32 rows each; the 4 / RW waves of a group take a tile of a stage each.
 #pragma once
 #include "rk_attn_rows.hpp"
 
 namespace rk {
 
-constexpr int BLOCK_NT = 512;                            // eight waves: two a SIMD, one work-group a compute unit
-constexpr int BLOCK_V = 32768, BLOCK_BUF = 65536;       // in a buffer: Keys of up to 128 tokens and 128 channels, their Values behind them
-constexpr int BLOCK_LDS = 2 * BLOCK_BUF + 2 * 1024 + 64;// two buffers; steps of Keys and Values; flags
+constexpr int BLOCK_NT = 256;                            // four waves, a SIMD each; two work-groups a compute unit
+constexpr int BLOCK_V = 16384, BLOCK_BUF = 32768;       // in a buffer: Keys of up to 64 tokens and 128 channels, their Values behind them
+constexpr int BLOCK_LDS = 2 * BLOCK_BUF + 2 * 512 + 64; // two buffers; steps of Keys and Values; flags
 
 __device__ __forceinline__ float halves_sum(float v)
 {
@@ -132,8 +132,8 @@ struct BlockState {
 template <int FMT, int R, int TG> struct CacheStage;
 template <int R, int TG>
 struct CacheStage<ROWS_BF16, R, TG> {
-    static constexpr int KP = TG * 4 * R, NK = (KP + BLOCK_NT - 1) / BLOCK_NT, DEPTH = TG == 4 || R > 96 ? 2 : 3;
-    uint4 k[NK], v[TG];
+    static constexpr int KP = TG * 4 * R, NK = (KP + BLOCK_NT - 1) / BLOCK_NT, DEPTH = TG == 2 || R > 96 ? 2 : 3;
+    uint4 k[NK], v[2 * TG];
     // tiles TG s ..+TG-1 of the sequence (`last`: its last tile, taken instead of one behind it)
     __device__ __forceinline__ void load(const char* Ku, const char* Vu, int s, int last, int rp, int tid, int wave)
     {
@@ -143,7 +143,7 @@ struct CacheStage<ROWS_BF16, R, TG> {
             k[j] = *(const uint4*)(Ku + (size_t)min(TG * s + tile, last) * (64 * rp) + (uint32_t)((m >> 4) * (32 * rp) + (8 * o < rp ? o : 0) * 256 + (m & 15) * 16));
         }
 #pragma unroll
-        for (int j = 0; j < TG; ++j) v[j] = *(const uint4*)(Vu + (size_t)min(TG * s + j, last) * 8192 + (uint32_t)(tid * 16));
+        for (int j = 0; j < 2 * TG; ++j) v[j] = *(const uint4*)(Vu + (size_t)min(TG * s + (j >> 1), last) * 8192 + (uint32_t)((j & 1) * 4096 + tid * 16));
     }
     // `left`: tokens of the stage that exist; Values behind them may be anything
     __device__ __forceinline__ void store(char* buf, float*, int left, int tid)
@@ -154,24 +154,24 @@ struct CacheStage<ROWS_BF16, R, TG> {
         const int n = tid & 15, g = (tid >> 4) & 3;
         if (left < 32 * TG) {
 #pragma unroll
-            for (int j = 0; j < TG; ++j) {
+            for (int j = 0; j < 2 * TG; ++j) {
                 uint32_t x[4] = {v[j].x, v[j].y, v[j].z, v[j].w};
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const int t = 32 * j + 16 * (i >> 1) + 4 * g + 2 * (i & 1);
+                    const int t = 32 * (j >> 1) + 16 * (i >> 1) + 4 * g + 2 * (i & 1);
                     x[i] &= t + 1 < left ? ~0u : t < left ? 0xffffu : 0u;
                 }
                 v[j] = make_uint4(x[0], x[1], x[2], x[3]);
             }
         }
 #pragma unroll
-        for (int j = 0; j < TG; ++j) *(uint4*)(buf + BLOCK_V + j * 8192 + value_place(tid >> 6, g, n)) = v[j];
+        for (int j = 0; j < 2 * TG; ++j) *(uint4*)(buf + BLOCK_V + (j >> 1) * 8192 + value_place(4 * (j & 1) + (tid >> 6), g, n)) = v[j];
     }
 };
 template <int R, int TG>
 struct CacheStage<ROWS_Q8_BF16, R, TG> {
-    static constexpr int KP = TG * 2 * R, NK = (KP + BLOCK_NT - 1) / BLOCK_NT, DEPTH = TG == 4 && R > 64 ? 2 : 3;
-    uint4 k[NK], v[TG / 2];
+    static constexpr int KP = TG * 2 * R, NK = (KP + BLOCK_NT - 1) / BLOCK_NT, DEPTH = 3;
+    uint4 k[NK], v[TG];
     uint32_t step;
     __device__ __forceinline__ void load(const char* Ku, const char* Vu, int s, int last, int rp, int tid, int wave)
     {
@@ -182,8 +182,8 @@ struct CacheStage<ROWS_Q8_BF16, R, TG> {
             k[j] = *(const uint4*)(Ku + (size_t)min(TG * s + tile, last) * kblk + (uint32_t)((8 * o < rp ? o : 0) * 256 + n * 16));
         }
 #pragma unroll
-        for (int j = 0; j < TG / 2; ++j) v[j] = *(const uint4*)(Vu + (size_t)min(TG * s + 2 * j + (wave >> 2), last) * 4096 + (uint32_t)((tid & 255) * 16));
-        const int tile = min(wave, TG / 2 - 1) * 2, a = min(TG * s + tile, last), b = min(TG * s + tile + 1, last);
+        for (int j = 0; j < TG; ++j) v[j] = *(const uint4*)(Vu + (size_t)min(TG * s + j, last) * 4096 + (uint32_t)(tid * 16));
+        const int a = min(TG * s, last), b = min(TG * s + TG - 1, last);
         step = *(const uint32_t*)(Ku + (size_t)a * kblk + (uint32_t)(32 * rp + (tid & 32 ? (b - a) * (int)kblk : 0) + (tid & 31) * 4));
     }
     // `left`: tokens of the stage that exist
@@ -197,31 +197,31 @@ struct CacheStage<ROWS_Q8_BF16, R, TG> {
                 *(uint4*)(buf + key_place(o, 16 + n)) = __builtin_bit_cast(uint4, codes_bf16(k[j].z, k[j].w));
             }
         }
-        const int n = tid & 15, g = (tid >> 4) & 3, cp = (tid >> 6) & 3;
+        const int n = tid & 15, g = (tid >> 4) & 3, cp = tid >> 6;
 #pragma unroll
-        for (int j = 0; j < TG / 2; ++j) {
-            char* to = buf + BLOCK_V + (2 * j + (tid >> 8)) * 8192;
+        for (int j = 0; j < TG; ++j) {
+            char* to = buf + BLOCK_V + j * 8192;
             *(uint4*)(to + value_place(2 * cp, g, n)) = __builtin_bit_cast(uint4, codes_bf16(v[j].x, v[j].y));
             *(uint4*)(to + value_place(2 * cp + 1, g, n)) = __builtin_bit_cast(uint4, codes_bf16(v[j].z, v[j].w));
         }
         if (tid < 32 * TG) {
             steps[tid] = __uint_as_float(step << 16);
-            steps[128 + tid] = tid < left ? __uint_as_float(step & 0xffff0000u) : 0.f;
+            steps[64 + tid] = tid < left ? __uint_as_float(step & 0xffff0000u) : 0.f;
         }
     }
 };
 
-// 128 full-width rows: threads 0..255 take the Keys, the others the Values, eight tokens by eight channels each, transposed in registers.
+// 64 full-width rows: threads 0..127 take the Keys, the others the Values, eight tokens by eight channels each, transposed in registers.
 struct PlainStage {
     uint4 x[8];
-    // token (of 128) of Value x[j]: the eight slots of (tile, g)
-    static __device__ __forceinline__ int token(int tid, int j) { return 32 * ((tid >> 6) & 3) + 4 * ((tid >> 4) & 3) + (j < 4 ? j : 12 + j); }
+    // token (of 64) of Value x[j]: the eight slots of (tile, g)
+    static __device__ __forceinline__ int token(int tid, int j) { return 32 * ((tid >> 6) & 1) + 4 * ((tid >> 4) & 3) + (j < 4 ? j : 12 + j); }
     __device__ __forceinline__ void load(const bf16_t* kp, const bf16_t* vp, int64_t stride, int r0, int rows, int tid)
     {
-        if (tid < 256) {
+        if (tid < 128) {
 #pragma unroll
             for (int j = 0; j < 8; ++j)
-                x[j] = *(const uint4*)(kp + (int64_t)min(r0 + (tid >> 2) + 64 * (j >> 2), rows - 1) * stride + 8 * ((tid & 3) + 4 * (j & 3)));
+                x[j] = *(const uint4*)(kp + (int64_t)min(r0 + (tid >> 2) + 32 * (j >> 2), rows - 1) * stride + 8 * ((tid & 3) + 4 * (j & 3)));
         } else {
 #pragma unroll
             for (int j = 0; j < 8; ++j) x[j] = *(const uint4*)(vp + (int64_t)min(r0 + token(tid, j), rows - 1) * stride + 8 * (tid & 15));
@@ -230,10 +230,10 @@ struct PlainStage {
     // `odd` (drafts): a bit for each whose Value holds one that is no number; nothing of that goes into the product
     __device__ __forceinline__ void store(char* buf, uint32_t* odd, int r0, int rows, int tid)
     {
-        if (tid < 256) {
+        if (tid < 128) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const int t = (tid >> 2) + 64 * (j >> 2);
+                const int t = (tid >> 2) + 32 * (j >> 2);
                 *(uint4*)(buf + (t >> 5) * 8192 + key_place((tid & 3) + 4 * (j & 3), t & 31)) = x[j];
             }
         } else {
@@ -261,7 +261,7 @@ struct PlainStage {
                     }
                 }
             }
-            char* to = buf + BLOCK_V + ((tid >> 6) & 3) * 8192 + value_place(co >> 1, (tid >> 4) & 3, 8 * (co & 1));
+            char* to = buf + BLOCK_V + ((tid >> 6) & 1) * 8192 + value_place(co >> 1, (tid >> 4) & 3, 8 * (co & 1));
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 const uint32_t sel = (k & 1) ? 0x07060302u : 0x05040100u;
@@ -277,13 +277,13 @@ struct PlainStage {
 };
 
 template <int FMT, int R, int RW>
-__global__ __launch_bounds__(BLOCK_NT, 1) void attn_block(RowsArgs A)
+__global__ __launch_bounds__(BLOCK_NT, 2) void attn_block(RowsArgs A)
 {
     constexpr bool Q8 = FMT == ROWS_Q8_BF16;
-    constexpr int TG = 8 / RW;           // waves of a row group: each takes a tile of a stage
+    constexpr int TG = 4 / RW;           // waves of a row group: each takes a tile of a stage
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    float* steps = (float*)(lds + 2 * BLOCK_BUF);                  // [buffer][Keys 128, Values 128]
-    uint32_t* odd = (uint32_t*)(steps + 512);                      // a bit a draft
+    float* steps = (float*)(lds + 2 * BLOCK_BUF);                  // [buffer][Keys 64, Values 64]
+    uint32_t* odd = (uint32_t*)(steps + 256);                      // a bit a draft
 
     const uint32_t turn = blockIdx.x >> 3;                         // (the row blocks of a stretch follow each other on one XCD)
     const uint32_t pair = turn / A.nrb * 8 + (blockIdx.x & 7), block = turn % A.nrb;
@@ -306,11 +306,11 @@ __global__ __launch_bounds__(BLOCK_NT, 1) void attn_block(RowsArgs A)
     BlockState st;                       // (cleared only in front of the loops: its registers are the prologue's until then)
     if (split < A.Sv) {
         const float* Ru = A.Rr + (size_t)u * D * A.r;
-        constexpr int NF = (R / 4 + 7) / 8;      // fragments of R_r^T a wave makes ready: 32 columns, 16 channels each
+        constexpr int NF = R / 16;               // fragments of R_r^T a wave makes ready: 32 columns, 16 channels each
         float x[NF][8];
 #pragma unroll
         for (int w = 0; w < NF; ++w) {
-            const int f = min(8 * w + wave, R / 4 - 1), j = 32 * (f >> 3) + n;
+            const int f = 4 * w + wave, j = 32 * (f >> 3) + n;
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[w][e] = Ru[(16 * (f & 7) + 8 * h + e) * A.r + min(j, A.r - 1)];
         }
@@ -335,15 +335,13 @@ __global__ __launch_bounds__(BLOCK_NT, 1) void attn_block(RowsArgs A)
             // R_r^T as A operands, head and remainder, in LDS; then this wave's rows of q R_r
 #pragma unroll
             for (int w = 0; w < NF; ++w) {
-                const int f = 8 * w + wave, j = 32 * (f >> 3) + n;
-                if (f < R / 4) {
+                const int f = 4 * w + wave, j = 32 * (f >> 3) + n;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) x[w][e] = j < A.r ? x[w][e] : 0.f;
-                    bf16x8 hi, lo;
-                    split_bf16x8(x[w], hi, lo);
-                    *(bf16x8*)(lds + (2 * f) * 1024 + lane * 16) = hi;
-                    *(bf16x8*)(lds + (2 * f + 1) * 1024 + lane * 16) = lo;
-                }
+                for (int e = 0; e < 8; ++e) x[w][e] = j < A.r ? x[w][e] : 0.f;
+                bf16x8 hi, lo;
+                split_bf16x8(x[w], hi, lo);
+                *(bf16x8*)(lds + (2 * f) * 1024 + lane * 16) = hi;
+                *(bf16x8*)(lds + (2 * f + 1) * 1024 + lane * 16) = lo;
             }
             float bias = 0.f;
             if (A.dmu) {
@@ -407,7 +405,7 @@ __global__ __launch_bounds__(BLOCK_NT, 1) void attn_block(RowsArgs A)
                         p = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, qr[i][1], p, 0, 0, 0);
                         p = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, qr[i][0], p, 0, 0, 0);
                     }
-                    const float* ks = steps + buf * 256 + 32 * tile + 4 * h;
+                    const float* ks = steps + buf * 128 + 32 * tile + 4 * h;
                     if constexpr (Q8) {
 #pragma unroll
                         for (int q = 0; q < 4; ++q) {
@@ -424,7 +422,7 @@ __global__ __launch_bounds__(BLOCK_NT, 1) void attn_block(RowsArgs A)
                     if constexpr (Q8) {
 #pragma unroll
                         for (int q = 0; q < 4; ++q) {
-                            const f32x4 w = *(const f32x4*)(ks + 128 + 8 * q);
+                            const f32x4 w = *(const f32x4*)(ks + 64 + 8 * q);
 #pragma unroll
                             for (int i = 0; i < 4; ++i) p[4 * q + i] *= w[i];
                         }
@@ -432,7 +430,7 @@ __global__ __launch_bounds__(BLOCK_NT, 1) void attn_block(RowsArgs A)
                     st.accumulate(p, vt, lane);
                 }
                 buf ^= 1;
-                next.store(lds + buf * BLOCK_BUF, steps + buf * 256, len - 32 * TG * (s + 1), tid);
+                next.store(lds + buf * BLOCK_BUF, steps + buf * 128, len - 32 * TG * (s + 1), tid);
                 lds_barrier();
             };
 #pragma unroll 1
@@ -455,7 +453,7 @@ __global__ __launch_bounds__(BLOCK_NT, 1) void attn_block(RowsArgs A)
         const bool active = row0 < live * A.G;
         st.clear();
         const int text = A.text_k ? min(max(A.text_len ? A.text_len[b] : A.text_max, 0), A.text_max) : 0;
-        const int tt = (text + 127) / 128, stages = tt + (drafts > 0), k = split - A.Sv;
+        const int tt = (text + 63) / 64, stages = tt + (drafts > 0), k = split - A.Sv;
         const int s0 = (int)((int64_t)stages * k / A.Sr), s1 = (int)((int64_t)stages * (k + 1) / A.Sr);
         if (s0 < s1) {
             const bf16_t* tk = (const bf16_t*)A.text_k + (int64_t)b * A.text_sb + (int64_t)hk * A.text_sh;
@@ -465,10 +463,10 @@ __global__ __launch_bounds__(BLOCK_NT, 1) void attn_block(RowsArgs A)
             PlainStage X[2];
             auto load = [&](PlainStage& x, int s) {
                 const bool own = s >= tt;
-                x.load(own ? dk : tk, own ? dv : tv, own ? A.draft_st : A.text_st, own ? 0 : 128 * s, own ? drafts : text, tid);
+                x.load(own ? dk : tk, own ? dv : tv, own ? A.draft_st : A.text_st, own ? 0 : 64 * s, own ? drafts : text, tid);
             };
             auto store = [&](PlainStage& x, int s, int buf) {
-                x.store(lds + buf * BLOCK_BUF, s >= tt && s < s1 ? odd : nullptr, s >= tt ? 0 : 128 * s, s >= tt ? drafts : text, tid);
+                x.store(lds + buf * BLOCK_BUF, s >= tt && s < s1 ? odd : nullptr, s >= tt ? 0 : 64 * s, s >= tt ? drafts : text, tid);
             };
             load(X[0], s0);
             load(X[1], min(s0 + 1, s1 - 1));
@@ -484,10 +482,10 @@ __global__ __launch_bounds__(BLOCK_NT, 1) void attn_block(RowsArgs A)
                 load(mine, min(s + 2, s1 - 1));
                 if (active) {
 #pragma unroll 1
-                    for (int tile = wave / RW; tile < 4; tile += TG) {
+                    for (int tile = wave / RW; tile < 2; tile += TG) {
                         const char* kt = lds + buf * BLOCK_BUF + tile * 8192;
                         const char* vt = lds + buf * BLOCK_BUF + BLOCK_V + tile * 8192;
-                        const int left = (own ? drafts : text - 128 * s) - 32 * tile;
+                        const int left = (own ? drafts : text - 64 * s) - 32 * tile;
                         if (left <= 0) break;
                         f32x16 p;
 #pragma unroll
