@@ -293,7 +293,7 @@ DecodePlan decode_plan(const rk_ctx* ctx, const rk_layout* L, int text_rows = 0)
 }
 
 // Attention of T query tokens a sequence: row blocks of a KV head, splits of the cache and of the full-width rows.
-struct RowsPlan { int nrb16, nrb, Sv, Sr; };
+struct RowsPlan { int nrb16, nrb, Sv, Sr; bool fold; };
 int rows_per_block(const rk_layout* L, int T)       // in sixteens; fp32 rows take twice the registers
 {
     const int64_t rows = (int64_t)T * (L->n_q_heads / L->n_kv_heads);
@@ -315,7 +315,8 @@ int rows_slots(const rk_ctx* ctx, const rk_layout* L, int T)
 }
 size_t rows_ws(const rk_ctx* ctx, const rk_layout* L, int T)
 {
-    return align_up((size_t)L->batch * T * L->n_q_heads * rows_slots(ctx, L, T) * (D + 2) * sizeof(float), 256);
+    // (256 bytes more: the accumulators begin a cache line, whatever the workspace's address)
+    return align_up((size_t)L->batch * T * L->n_q_heads * rows_slots(ctx, L, T) * (D + 2) * sizeof(float), 256) + 256;
 }
 RowsPlan rows_plan(const rk_ctx* ctx, const rk_layout* L, int T, int text_rows, bool drafts, bool q8)
 {
@@ -358,6 +359,12 @@ RowsPlan rows_plan(const rk_ctx* ctx, const rk_layout* L, int T, int text_rows, 
         if (p.Sv > slots - p.Sr) p.Sv = slots - p.Sr;
     }
     if (p.Sv < 1) p.Sv = 1;
+    // The partials of a row block folded by its last work-group: where the units fill the XCDs evenly, and what one work-group then reads is
+    // little (the merge launch spreads it over the device).
+    const int64_t units = (int64_t)L->batch * L->n_kv_heads, rows = (int64_t)T * (L->n_q_heads / L->n_kv_heads);
+    const int S = p.Sv + p.Sr;
+    p.fold = !block && ctx && ctx->fuse_merge && ctx->xcd_deal_ok && S > 1 && units % 8 == 0 && groups <= DEC_COUNTERS &&
+             (rows < 16 * p.nrb16 ? rows : 16 * p.nrb16) * S <= 64;
     return p;
 }
 
@@ -1037,12 +1044,14 @@ static rk_status rows_common(rk_ctx* ctx, const rk_layout* L, const void* q, con
         a.draft_sb = drafts->stride_b; a.draft_sh = drafts->stride_h; a.draft_st = drafts->stride_t;
     }
     const size_t slots = (size_t)a.B * T * a.Hq * (p.Sv + p.Sr);
-    a.ws_acc = (float*)workspace; a.ws_m = a.ws_acc + slots * D; a.ws_l = a.ws_m + slots;
+    a.ws_acc = (float*)align_up((uintptr_t)workspace, 256); a.ws_m = a.ws_acc + slots * D; a.ws_l = a.ws_m + slots;
+    a.max_len = L->max_seq_len;
+    a.done = p.fold ? ctx->tickets + APP_TICKETS : nullptr;
     hipStream_t st = as_stream(stream);
     e = L->dtype == RK_F32 ? (q8 ? launch_rows_q8_f32(a, p.nrb16, st) : launch_rows_f32(a, p.nrb16, st))
                            : (q8 ? launch_rows_q8_bf16(a, p.nrb16, st) : launch_rows_bf16(a, p.nrb16, st));
     if (e != hipSuccess) return hip_fail(ctx, e, "attention launch");
-    if (p.Sv + p.Sr > 1) {
+    if (p.Sv + p.Sr > 1 && !p.fold) {
         e = launch_rows_merge(L->dtype, a, st);
         if (e != hipSuccess) return hip_fail(ctx, e, "attention merge launch");
     }

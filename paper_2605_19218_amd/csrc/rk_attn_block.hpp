@@ -285,14 +285,12 @@ __global__ __launch_bounds__(BLOCK_NT, 2) void attn_block(RowsArgs A)
     float* steps = (float*)(lds + 2 * BLOCK_BUF);                  // [buffer][Keys 64, Values 64]
     uint32_t* odd = (uint32_t*)(steps + 256);                      // a bit a draft
 
-    const uint32_t turn = blockIdx.x >> 3;                         // (the row blocks of a stretch follow each other on one XCD)
-    const uint32_t pair = turn / A.nrb * 8 + (blockIdx.x & 7), block = turn % A.nrb;
-    const uint32_t units = A.B * A.Hkv;
-    if (pair >= units * (A.Sv + A.Sr)) return;
-    const int split = pair / units, u = pair - split * units, b = u / A.Hkv, hk = u - b * A.Hkv;
+    int split, u, block;
+    if (!rows_place(A, split, u, block)) return;
+    const int b = u / A.Hkv, hk = u - b * A.Hkv;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, n = lane & 31;
     const int S = A.Sv + A.Sr;
-    if ((int)block * 32 * RW >= A.T * A.G) return;
+    if (block * 32 * RW >= A.T * A.G) return;
     const int row0 = (block * RW + wave % RW) * 32, row = row0 + n;
     const int rc = min(row, A.T * A.G - 1), tok = rc / A.G;
     const size_t at = (size_t)(b * A.T + tok) * A.Hq + hk * A.G + (rc - tok * A.G);
@@ -320,7 +318,7 @@ __global__ __launch_bounds__(BLOCK_NT, 2) void attn_block(RowsArgs A)
         for (int i = 0; i < 16; ++i) dm[i] = *(const f32x4_any*)(dp + 16 * (i >> 1) + 8 * h + 4 * (i & 1));
         __builtin_amdgcn_sched_barrier(0);
         if (A.draft_k) live = drafts_of();
-        if ((int)block * 32 * RW >= live * A.G) return;
+        if (block * 32 * RW >= live * A.G) return;
         const bool active = row0 < live * A.G;                     // (a wave without rows helps with the staging)
         constexpr int DEPTH = CacheStage<FMT, R, TG>::DEPTH;
         const int len = min(max(A.seq_len[b], 0), A.cap), stages = (len + 32 * TG - 1) / (32 * TG), last = (len + 31) / 32 - 1;
@@ -449,7 +447,7 @@ __global__ __launch_bounds__(BLOCK_NT, 2) void attn_block(RowsArgs A)
     } else {
         const int drafts = drafts_of();
         if (A.draft_k) live = drafts;
-        if ((int)block * 32 * RW >= live * A.G) return;
+        if (block * 32 * RW >= live * A.G) return;
         const bool active = row0 < live * A.G;
         st.clear();
         const int text = A.text_k ? min(max(A.text_len ? A.text_len[b] : A.text_max, 0), A.text_max) : 0;
@@ -590,9 +588,8 @@ static hipError_t launch_block_r(int nrb16, dim3 grid, const RowsArgs& a, hipStr
 template <int FMT>
 static hipError_t launch_block_fmt(const RowsArgs& a, int nrb16, hipStream_t st)
 {
-    const int64_t pairs = (int64_t)a.B * a.Hkv * (a.Sv + a.Sr), blocks = (pairs + 7) / 8 * 8 * a.nrb;
-    if (blocks > 0x7fffffff) return hipErrorInvalidValue;
-    const dim3 grid((uint32_t)blocks);
+    const dim3 grid = rows_grid(a);
+    if (!grid.x) return hipErrorInvalidValue;
     switch ((a.r + 31) / 32) {
         case 1: return launch_block_r<FMT, 32>(nrb16, grid, a, st);
         case 2: return launch_block_r<FMT, 64>(nrb16, grid, a, st);

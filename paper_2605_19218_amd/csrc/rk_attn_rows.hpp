@@ -590,34 +590,47 @@ struct PlainRowsF32 {
 };
 
 // q R_r of this work-group's rows into qt [16 NRB][R + 4], and q . delta_mu of row n of each block: D^T[j][row] = R_r^T . q^T, column blocks
-// of R_r shared by the waves.  q in bf16 is exact and R_r goes as head and remainder; in fp32 all of it is fp32.
+// of R_r shared by the waves.  q in bf16 is exact and R_r goes as head and remainder; in fp32 all of it is fp32.  load() asks for
+// everything, make() waits for it.
+template <typename T, int R, int NRB> struct Rotation;
 template <int R, int NRB>
-__device__ __forceinline__ void rotate_queries(const bf16_t* const (&qrow)[NRB], const float* Ru, const float* dm, int r, float* qt, float (&bias)[NRB],
-                                               int wave, int g, int n)
-{
+struct Rotation<bf16_t, R, NRB> {
+    static constexpr int NW = (R + 63) / 64;
     bf16x8 qf[NRB][4];
+    float x[NW][4][8];
+    f32x4 dm[8];
+    __device__ __forceinline__ void load(const bf16_t* const (&qrow)[NRB], const float* Ru, const float* dp, int r, int wave, int g, int n)
+    {
 #pragma unroll
-    for (int rb = 0; rb < NRB; ++rb)
+        for (int rb = 0; rb < NRB; ++rb)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) qf[rb][i] = *(const bf16x8*)(qrow[rb] + 32 * i + 8 * g);
+            for (int i = 0; i < 4; ++i) qf[rb][i] = *(const bf16x8*)(qrow[rb] + 32 * i + 8 * g);
 #pragma unroll
-    for (int w = 0; w < (R + 63) / 64; ++w) {
-        const int jb = wave + 4 * w, j = 16 * jb + n;
-        if (16 * jb < R) {
-            f32x4 acc[NRB];
-#pragma unroll
-            for (int rb = 0; rb < NRB; ++rb) acc[rb] = (f32x4){0.f, 0.f, 0.f, 0.f};
-            float x[4][8];
+        for (int w = 0; w < NW; ++w) {
+            const int j = min(16 * (wave + 4 * w) + n, r - 1);
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int jj = 0; jj < 8; ++jj) x[i][jj] = Ru[(32 * i + 8 * g + jj) * r + min(j, r - 1)];
+                for (int e = 0; e < 8; ++e) x[w][i][e] = Ru[(32 * i + 8 * g + e) * r + j];
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) dm[i] = *(const f32x4_any*)(dp + 32 * (i >> 1) + 8 * g + 4 * (i & 1));
+    }
+    __device__ __forceinline__ void make(float* qt, float (&bias)[NRB], bool biased, int r, int wave, int g, int n)
+    {
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            const int jb = wave + 4 * w;
+            if (16 * jb >= R) break;
+            f32x4 acc[NRB];
+#pragma unroll
+            for (int rb = 0; rb < NRB; ++rb) acc[rb] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
 #pragma unroll
-                for (int jj = 0; jj < 8; ++jj) x[i][jj] = j < r ? x[i][jj] : 0.f;
+                for (int e = 0; e < 8; ++e) x[w][i][e] = 16 * jb + n < r ? x[w][i][e] : 0.f;
                 bf16x8 hi, lo;
-                split_bf16x8(x[i], hi, lo);
+                split_bf16x8(x[w][i], hi, lo);
 #pragma unroll
                 for (int rb = 0; rb < NRB; ++rb) {
                     acc[rb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lo, qf[rb][i], acc[rb], 0, 0, 0);
@@ -627,74 +640,175 @@ __device__ __forceinline__ void rotate_queries(const bf16_t* const (&qrow)[NRB],
 #pragma unroll
             for (int rb = 0; rb < NRB; ++rb) *(f32x4*)(qt + (16 * rb + n) * (R + 4) + 16 * jb + 4 * g) = acc[rb];
         }
-    }
 #pragma unroll
-    for (int rb = 0; rb < NRB; ++rb) bias[rb] = 0.f;
-    if (dm) {
+        for (int rb = 0; rb < NRB; ++rb) {
+            bias[rb] = 0.f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const f32x4 a = *(const f32x4_any*)(dm + 32 * i + 8 * g), b = *(const f32x4_any*)(dm + 32 * i + 8 * g + 4);
+            for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int rb = 0; rb < NRB; ++rb)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) bias[rb] = fmaf((float)qf[rb][i][e], e < 4 ? a[e] : b[e - 4], bias[rb]);
+                for (int e = 0; e < 8; ++e) bias[rb] = fmaf((float)qf[rb][i][e], dm[2 * i + (e >> 2)][e & 3], bias[rb]);
+            bias[rb] = biased ? groups_sum(bias[rb]) : 0.f;
         }
-#pragma unroll
-        for (int rb = 0; rb < NRB; ++rb) bias[rb] = groups_sum(bias[rb]);
     }
-}
+};
 template <int R, int NRB>
-__device__ __forceinline__ void rotate_queries(const float* const (&qrow)[NRB], const float* Ru, const float* dm, int r, float* qt, float (&bias)[NRB],
-                                               int wave, int g, int n)
-{
+struct Rotation<float, R, NRB> {
+    static constexpr int NW = (R + 63) / 64;
     f32x4 qf[NRB][8];
+    float x[NW][8][4];
+    f32x4 dm[8];
+    __device__ __forceinline__ void load(const float* const (&qrow)[NRB], const float* Ru, const float* dp, int r, int wave, int g, int n)
+    {
 #pragma unroll
-    for (int rb = 0; rb < NRB; ++rb)
+        for (int rb = 0; rb < NRB; ++rb)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) qf[rb][i] = *(const f32x4*)(qrow[rb] + 16 * i + 4 * g);
+            for (int i = 0; i < 8; ++i) qf[rb][i] = *(const f32x4*)(qrow[rb] + 16 * i + 4 * g);
 #pragma unroll
-    for (int w = 0; w < (R + 63) / 64; ++w) {
-        const int jb = wave + 4 * w, j = 16 * jb + n;
-        if (16 * jb < R) {
-            f32x4 acc[NRB];
-#pragma unroll
-            for (int rb = 0; rb < NRB; ++rb) acc[rb] = (f32x4){0.f, 0.f, 0.f, 0.f};
-            float x[8][4];
+        for (int w = 0; w < NW; ++w) {
+            const int j = min(16 * (wave + 4 * w) + n, r - 1);
 #pragma unroll
             for (int i = 0; i < 8; ++i)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) x[i][e] = Ru[(16 * i + 4 * g + e) * r + min(j, r - 1)];
+                for (int e = 0; e < 4; ++e) x[w][i][e] = Ru[(16 * i + 4 * g + e) * r + j];
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) dm[i] = *(const f32x4_any*)(dp + 16 * i + 4 * g);
+    }
+    __device__ __forceinline__ void make(float* qt, float (&bias)[NRB], bool biased, int r, int wave, int g, int n)
+    {
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            const int jb = wave + 4 * w;
+            if (16 * jb >= R) break;
+            f32x4 acc[NRB];
+#pragma unroll
+            for (int rb = 0; rb < NRB; ++rb) acc[rb] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < 8; ++i)
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
 #pragma unroll
                     for (int rb = 0; rb < NRB; ++rb)
-                        acc[rb] = __builtin_amdgcn_mfma_f32_16x16x4f32(j < r ? x[i][e] : 0.f, qf[rb][i][e], acc[rb], 0, 0, 0);
+                        acc[rb] = __builtin_amdgcn_mfma_f32_16x16x4f32(16 * jb + n < r ? x[w][i][e] : 0.f, qf[rb][i][e], acc[rb], 0, 0, 0);
 #pragma unroll
             for (int rb = 0; rb < NRB; ++rb) *(f32x4*)(qt + (16 * rb + n) * (R + 4) + 16 * jb + 4 * g) = acc[rb];
         }
-    }
 #pragma unroll
-    for (int rb = 0; rb < NRB; ++rb) bias[rb] = 0.f;
-    if (dm) {
+        for (int rb = 0; rb < NRB; ++rb) {
+            bias[rb] = 0.f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const f32x4 a = *(const f32x4_any*)(dm + 16 * i + 4 * g);
+            for (int i = 0; i < 8; ++i)
 #pragma unroll
-            for (int rb = 0; rb < NRB; ++rb)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) bias[rb] = fmaf(qf[rb][i][e], a[e], bias[rb]);
+                for (int e = 0; e < 4; ++e) bias[rb] = fmaf(qf[rb][i][e], dm[i][e], bias[rb]);
+            bias[rb] = biased ? groups_sum(bias[rb]) : 0.f;
         }
-#pragma unroll
-        for (int rb = 0; rb < NRB; ++rb) bias[rb] = groups_sum(bias[rb]);
     }
-}
+};
 
 // The weight of a partial (m, l) under the maximum M of all: one that nothing weighs in has none, and a NaN stays one.
 __device__ __forceinline__ float partial_weight(float m, float l, float M)
 {
     return l == 0.f ? 0.f : rows_exp2(m - (M > ROWS_NEG_INF ? M : 0.f));
+}
+
+// What another work-group of the launch wrote, past this compute unit's L1 (whose lines may be older).
+__device__ __forceinline__ float past_l1(const float* p) { return __hip_atomic_load(const_cast<float*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+
+// Partials first, first + step, ... of the S of a row, by 32 lanes with four channels each: sum l_i w_i and sum acc_i w_i, w_i = 2^(m_i - M), M the maximum
+// of all S.  MC (up to eight) partials' loads at once.
+template <bool PAST_L1, int MC>
+__device__ __forceinline__ void merge_row(const float* m, const float* l, const float* acc, int S, int first, int step, int p, f32x4& num, float& sum)
+{
+    float M = ROWS_NEG_INF;
+    for (int i = p; i < S; i += 32) M = fmaxf(M, PAST_L1 ? past_l1(m + i) : m[i]);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o));
+    num = (f32x4){0.f, 0.f, 0.f, 0.f};
+    sum = 0.f;
+    for (int i0 = first; i0 < S; i0 += MC * step) {
+        f32x4 av[MC];
+#pragma unroll
+        for (int k = 0; k < MC; ++k) av[k] = *(const f32x4*)(acc + (size_t)min(i0 + k * step, S - 1) * D + 4 * p);
+        const int mine = i0 + (p & 7) * step, at = min(mine, S - 1);       // lane k of each eight: partial k's weight
+        const float mv = PAST_L1 ? past_l1(m + at) : m[at], lv = (p & 7) < MC && mine < S ? (PAST_L1 ? past_l1(l + at) : l[at]) : 0.f;
+        const float w = partial_weight(mv, lv, M), lw = lv * w;
+#pragma unroll
+        for (int k = 0; k < MC; ++k) {
+            sum += __shfl(lw, k, 8);
+            const float wk = __shfl(w, k, 8);
+            if (i0 + k * step < S) num += av[k] * wk;
+        }
+    }
+}
+
+// Which stretch and rows a work-group takes.  Work-groups go to the XCDs in turn by their index.  In both orders the row blocks of a
+// stretch follow each other on one XCD, and read it from its L2.  With counters (A.done) all splits of a unit are on the XCD u % 8, as the
+// fold inside the launch needs; else the stretches are dealt over all of them.
+__device__ __forceinline__ bool rows_place(const RowsArgs& A, int& split, int& u, int& block)
+{
+    const uint32_t units = A.B * A.Hkv, xcd = blockIdx.x & 7, turn = blockIdx.x >> 3;
+    if (A.done) {
+        block = turn % A.nrb;
+        u = turn / A.nrb * 8 + xcd;
+        split = blockIdx.y;
+        return u < (int)units;
+    }
+    block = turn % A.nrb;
+    const uint32_t pair = turn / A.nrb * 8 + xcd;
+    split = pair / units;
+    u = pair - split * units;
+    return pair < units * (A.Sv + A.Sr);
+}
+inline dim3 rows_grid(const RowsArgs& a)
+{
+    const int64_t units = (int64_t)a.B * a.Hkv, S = a.Sv + a.Sr;
+    const int64_t x = (a.done ? (units + 7) / 8 : (units * S + 7) / 8) * 8 * a.nrb;
+    return x > 0x7fffffff ? dim3(0) : dim3((uint32_t)x, a.done ? (uint32_t)S : 1);
+}
+
+// The fold inside the launch.  Vector stores are counted until the L2 has them, so after the wait and the barrier this work-group's partial is in
+// the XCD's L2, which all splits of the unit share; the one that counts S reads them there (the few bytes of m and l past its L1, whose
+// lines other units share; a partial's accumulators are lines of their own, which this compute unit has not read before: it may have
+// written them, and stores go through the L1).
+template <typename T, int ROWS>
+__device__ __forceinline__ void fold_rows(const RowsArgs& A, int group, int b, int hk, int row0, int live, float* pool)
+{
+    const int S = A.Sv + A.Sr, tid = threadIdx.x, p = tid & 31, grp = tid >> 5;
+    int* last = (int*)pool;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (tid == 0) *last = __hip_atomic_fetch_add(A.done + group, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == S - 1;
+    __syncthreads();
+    const bool mine = *last;
+    __syncthreads();
+    if (!mine) return;
+    if (tid == 0) A.done[group] = 0;                       // ready for the next launch on this context
+    const int rows = min(ROWS, live * A.G - row0), share = rows <= 1 ? 8 : rows <= 2 ? 4 : rows <= 4 ? 2 : 1;      // groups of 32 lanes a row
+    f32x4* part = (f32x4*)pool;                            // [group][32], and the sums behind
+    float* den = pool + 8 * 32 * 4;
+    for (int r0 = 0; r0 < rows; r0 += 8 / share) {
+        const int row = r0 + grp / share, r = row0 + min(row, rows - 1), tok = r / A.G;
+        const size_t to = (size_t)(b * A.T + tok) * A.Hq + hk * A.G + (r - tok * A.G);
+        f32x4 num;
+        float sum;
+        merge_row<true, 8>(A.ws_m + to * S, A.ws_l + to * S, A.ws_acc + to * S * D, S, grp % share, share, p, num, sum);
+        if (share > 1) {
+            part[grp * 32 + p] = num;
+            if (p == 0) den[grp] = sum;
+            __syncthreads();
+            if (grp % share == 0)
+                for (int k = 1; k < share; ++k) {
+                    num += part[(grp + k) * 32 + p];
+                    sum += den[grp + k];
+                }
+        }
+        if (grp % share == 0 && row < rows) {
+            const float inv = 1.f / sum;
+            T* o = (T*)A.out + to * D + 4 * p;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) st_elem(o + e, sum == 0.f ? 0.f : num[e] * inv);
+        }
+    }
 }
 
 template <int FMT, int R, int NRB>
@@ -707,49 +821,61 @@ __global__ __launch_bounds__(256, NRB == 1 && FMT != ROWS_F32 ? 2 : 1) void attn
     __shared__ __attribute__((aligned(16))) float pool[POOL];           // q R_r, and at the end the four waves' accumulators of 16 rows
     __shared__ float sm_m[4][16], sm_l[4][16];
 
-    // Work-groups go to the XCDs in turn by their index: the row blocks of a stretch follow each other on one XCD, and read it from its L2.
-    const uint32_t turn = blockIdx.x >> 3;
-    const uint32_t pair = turn / A.nrb * 8 + (blockIdx.x & 7), block = turn % A.nrb;
-    const uint32_t units = A.B * A.Hkv;
-    if (pair >= units * (A.Sv + A.Sr)) return;
-    const int split = pair / units, u = pair - split * units, b = u / A.Hkv, hk = u - b * A.Hkv;
+    int split, u, block;
+    if (!rows_place(A, split, u, block)) return;
+    const int b = u / A.Hkv, hk = u - b * A.Hkv;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, n = lane & 15;
     const int S = A.Sv + A.Sr;
-    const int drafts = A.draft_k ? min(max(A.n_drafts ? A.n_drafts[b] : A.T, 0), A.T) : 0;
-    const int live = A.draft_k ? drafts : A.T;             // tokens whose rows are asked for
     const int row0 = block * 16 * NRB;                     // rows of the KV head: token by token, its G heads
-    if (row0 >= live * A.G) return;
-    int tok[NRB], at[NRB];                                 // lane (., n): row n of block rb, its token and its place in q and out
+    if (row0 >= A.T * A.G) return;
+    int tok[NRB];                                          // lane (., n): the token of row n of block rb
     const T* qrow[NRB];
 #pragma unroll
     for (int rb = 0; rb < NRB; ++rb) {
         const int row = min(row0 + 16 * rb + n, A.T * A.G - 1);
         tok[rb] = row / A.G;
-        at[rb] = (b * A.T + tok[rb]) * A.Hq + hk * A.G + (row - tok[rb] * A.G);
-        qrow[rb] = (const T*)A.q + (size_t)at[rb] * D;
+        qrow[rb] = (const T*)A.q + ((size_t)(b * A.T + tok[rb]) * A.Hq + hk * A.G + (row - tok[rb] * A.G)) * D;
     }
+    auto drafts_of = [&]() { return A.draft_k ? min(max(A.n_drafts ? A.n_drafts[b] : A.T, 0), A.T) : 0; };
+    int live = A.T;                                        // tokens whose rows are asked for
 
-    RowState<NRB> st;
-    st.clear();
+    RowState<NRB> st;                                      // (cleared only in front of the loops: its registers are the prologue's until then)
     const bool cache = split < A.Sv;
     if (cache) {
         typedef typename TileOf<FMT, R>::type Tile;
         constexpr int ES = FMT == ROWS_F32 ? 4 : 2;
-        const int len = min(max(A.seq_len[b], 0), A.cap), tiles = (len + 31) / 32;
-        const int t0 = (int)((int64_t)tiles * split / A.Sv), t1 = (int)((int64_t)tiles * (split + 1) / A.Sv);
         const size_t slab = slab_tokens(A.cap);
         const bool q8 = FMT >= ROWS_Q8_BF16;
         const char* Ku = (const char*)A.Kc + (q8 ? (size_t)u * (slab / 32) * q8_kblock(A.rp) : (size_t)u * slab * A.rp * ES);
         const char* Vu = (const char*)A.Vc + (size_t)u * slab * D * (q8 ? 1 : ES);
+        auto share = [&](int len, int& t0, int& t1) {      // the split's tiles
+            const int tiles = (len + 31) / 32;
+            t0 = (int)((int64_t)tiles * split / A.Sv);
+            t1 = (int)((int64_t)tiles * (split + 1) / A.Sv);
+        };
+        // Everything is asked for before the length is known, which is a round trip of its own: the first tile where it lies if the
+        // sequence is as long as the host's bound (else it is asked for again).
+        int e0, e1, t0, t1;
+        share(min(A.max_len, A.cap), e0, e1);
+        Rotation<T, R, NRB> rot;
+        const float* Ru = A.Rr + (size_t)u * D * A.r;
+        rot.load(qrow, Ru, A.dmu ? A.dmu + (size_t)u * D : Ru, A.r, wave, g, n);      // (any address that can be read, without a bias)
+        Tile X, Y;
+        X.load(Ku, Vu, 32 * max(min(e0 + wave, e1 - 1), 0), A.rp, lane);
+        __builtin_amdgcn_sched_barrier(0);
+        const int len = min(max(A.seq_len[b], 0), A.cap);
+        if (A.draft_k) live = drafts_of();
+        if (row0 >= live * A.G) return;
+        share(len, t0, t1);
         if (t0 < t1) {
-            Tile X, Y;
-            int t = t0 + wave;
-            X.load(Ku, Vu, 32 * min(t, t1 - 1), A.rp, lane);           // (a wave without a tile reads the last one, and leaves it)
+            int t = t0 + wave;                             // (a wave without a tile reads the last one, and leaves it)
+            if (t0 != e0 || t1 != e1) X.load(Ku, Vu, 32 * min(t, t1 - 1), A.rp, lane);
             float bias[NRB];
-            rotate_queries<R, NRB>(qrow, A.Rr + (size_t)u * D * A.r, A.dmu ? A.dmu + (size_t)u * D : nullptr, A.r, pool, bias, wave, g, n);
-            __syncthreads();
+            rot.make(pool, bias, A.dmu != nullptr, A.r, wave, g, n);
+            lds_barrier();
             CacheRows<FMT, R, NRB> rows;
             rows.take(pool, A.scale_log2, g, n);
+            st.clear();
 #pragma unroll 1
             for (; t < t1; t += 8) {
                 Y.load(Ku, Vu, 32 * min(t + 4, t1 - 1), A.rp, lane);
@@ -763,9 +889,15 @@ __global__ __launch_bounds__(256, NRB == 1 && FMT != ROWS_F32 ? 2 : 1) void attn
             // the bias joins only now: it is the same for all of the cache, and would cost the scores bits
 #pragma unroll
             for (int rb = 0; rb < NRB; ++rb) st.m[rb] += bias[rb] * A.scale_log2;
+        } else {
+            st.clear();
         }
     } else {
         // tiles of 32 rows: first the text's, then the drafts'
+        const int drafts = drafts_of();
+        if (A.draft_k) live = drafts;
+        if (row0 >= live * A.G) return;
+        st.clear();
         const int text = A.text_k ? min(max(A.text_len ? A.text_len[b] : A.text_max, 0), A.text_max) : 0;
         const int tt = (text + 31) / 32, tiles = tt + (drafts + 31) / 32, k = split - A.Sv;
         const int t0 = (int)((int64_t)tiles * k / A.Sr), t1 = (int)((int64_t)tiles * (k + 1) / A.Sr);
@@ -854,6 +986,7 @@ __global__ __launch_bounds__(256, NRB == 1 && FMT != ROWS_F32 ? 2 : 1) void attn
             }
         }
     }
+    if (A.done) fold_rows<T, 16 * NRB>(A, u * A.nrb + block, b, hk, row0, live, pool);
 }
 
 template <int FMT, int R>
@@ -865,9 +998,8 @@ static void launch_rows_r(int nrb16, dim3 grid, const RowsArgs& a, hipStream_t s
 template <int FMT>
 static hipError_t launch_rows_fmt(const RowsArgs& a, int nrb16, hipStream_t st)
 {
-    const int64_t pairs = (int64_t)a.B * a.Hkv * (a.Sv + a.Sr), blocks = (pairs + 7) / 8 * 8 * a.nrb;
-    if (blocks > 0x7fffffff) return hipErrorInvalidValue;
-    const dim3 grid((uint32_t)blocks);
+    const dim3 grid = rows_grid(a);
+    if (!grid.x) return hipErrorInvalidValue;
     switch ((a.r + 31) / 32) {
         case 1: launch_rows_r<FMT, 32>(nrb16, grid, a, st); break;
         case 2: launch_rows_r<FMT, 64>(nrb16, grid, a, st); break;

@@ -84,6 +84,8 @@ struct RowsArgs {
     const uint64_t* mask;        // [B, T] or null: row t sees drafts 0 ..t
     void* out;
     float *ws_m, *ws_l, *ws_acc; // [B, T, Hq, S] and [B, T, Hq, S, d]
+    int32_t max_len;             // the host's bound of the lengths
+    int32_t* done;               // a counter a row block that is zero between launches: the partials are folded inside the launch; or null
 };
 // fmt: ROWS_BF16, ROWS_F32, ROWS_Q8_BF16, ROWS_Q8_F32; nrb16: blocks of 16 rows a work-group takes (1, 2; with bf16 rows 4, 8 too)
 hipError_t launch_rows_bf16(const RowsArgs& a, int nrb16, hipStream_t st);

@@ -9,12 +9,14 @@
 
 namespace rk {
 
-// The step of a row from the bits of its largest magnitude, as bf16 bits, and 1 / s (0 where every code is 0).
+// The step of a row from the bits of its largest magnitude, as bf16 bits, and 1 / s (0 where every code is 0).  By products with 1 / 127 (which falls
+// short of it by 4e-9 of itself: a quotient that is a bfloat16 comes out as that) and the reciprocal's 1 ulp: the two divisions, ten rows a lane and
+// block, were a third of the kernel's instructions.
 __device__ __forceinline__ uint32_t row_step(uint32_t top, float& inv)
 {
-    const uint32_t up = (__float_as_uint(__uint_as_float(top) / 127.f) + 0xffffu) & 0xffff0000u;
+    const uint32_t up = (__float_as_uint(__uint_as_float(top) * (1.f / 127.f)) + 0xffffu) & 0xffff0000u;
     const bool finite = top < 0x7f800000u, tiny = top < 0x0d800000u;        // 2^-100
-    inv = finite && !tiny ? 1.f / __uint_as_float(up) : 0.f;
+    inv = finite && !tiny ? __builtin_amdgcn_rcpf(__uint_as_float(up)) : 0.f;
     return !finite ? 0x7fc0u : tiny ? 0u : up >> 16;
 }
 // the code in the low byte: 1.5 2^23 + c is c's two's complement there, and the sum is rounded once, to the nearest even
@@ -72,8 +74,8 @@ __device__ __forceinline__ void load8(const float* p, float (&x)[8])
 // and remainder in LDS (made once a work-group), an fp32 Key likewise, without the product of the two remainders: 2^-16 of |k| |R_r|, a
 // five-hundredth of a step.  Lane (g, n) then holds channels 16 jb + 4 g ..+3 of tokens n and 16 + n: the row's maximum is two lane swaps, and
 // a swap of halves between two jb makes the 16 bytes of the layout (one octet of both tokens).
-// Values: lane (g, n) takes channels 8 n ..+7 of the eight tokens whose codes the layout puts side by side, and the bytes are transposed in
-// the lane; pairs of lanes two apart exchange halves, again for whole 16-byte pieces.
+// Values: lane (g, n) takes channels 8 n ..+7 of the eight tokens whose codes the layout puts side by side, the bytes are transposed in
+// the lane, and go through LDS into the layout.
 // Grid: (blocks of `each` tokens, h_kv, b).
 template <typename T, int R>
 __global__ __launch_bounds__(256) void compress_q8(RowsDev keys, RowsDev vals, int Hkv, int cap, int r, int each, const float* __restrict__ Rr,
@@ -83,6 +85,7 @@ __global__ __launch_bounds__(256) void compress_q8(RowsDev keys, RowsDev vals, i
     constexpr bool F32 = sizeof(T) == 4;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     bf16x8* frag = (bf16x8*)smem;               // [jb][i][part][lane]
+    unsigned char* vcodes = smem + R * D * 4 + (threadIdx.x >> 6) * 4096;      // this wave's block of Value codes
     const int h = blockIdx.y, b = blockIdx.z, u = b * Hkv + h;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, n = lane & 15;
     const int n_b = min(rows_count(keys, b), cap);
@@ -230,12 +233,15 @@ __global__ __launch_bounds__(256) void compress_q8(RowsDev keys, RowsDev vals, i
         // channel 8 n + k is place 8 (n % 2) + k of channel block n / 2; blocks lie in pairs
         uint8_t* to = vb + (n >> 2) * 1024 + g * 256 + (n & 1) * 128;
         if (full) {
-            const bool odd = n & 2;
+            // through LDS, so that a store is a kilobyte on end: from the lanes as they are, 64 bytes a lane in four stores, the
+            // stores of a block touched every line of it four times
+            unsigned char* at = vcodes + (to - vb) + (n & 2) * 4;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const uint32_t a = dpp_u32<0x4E>(odd ? lo4[k] : lo4[k + 4]), c = dpp_u32<0x4E>(odd ? hi4[k] : hi4[k + 4]);
-                *(uint4*)(to + (odd ? 64 : 0) + 16 * k) = odd ? make_uint4(a, c, lo4[k + 4], hi4[k + 4]) : make_uint4(lo4[k], hi4[k], a, c);
-            }
+            for (int k = 0; k < 8; ++k) *(uint2*)(at + 16 * k) = make_uint2(lo4[k], hi4[k]);
+            wave_lds_fence();
+#pragma unroll
+            for (int j = 0; j < 4; ++j) *(uint4*)(vb + 1024 * j + 16 * lane) = *(const uint4*)(vcodes + 1024 * j + 16 * lane);
+            wave_lds_fence();
         } else {
             to += (n & 2) * 4;
 #pragma unroll
@@ -388,7 +394,7 @@ template <typename T, int R>
 static hipError_t compress_q8_r(const RowsDev& keys, const RowsDev& vals, int B, int Hkv, int cap, int r, int each, const float* Rr, uint8_t* Kq,
                                 uint8_t* Vq, int32_t* seq_len_out, hipStream_t st)
 {
-    const size_t lds = (size_t)R * D * 4;
+    const size_t lds = (size_t)R * D * 4 + 4 * 4096;
     const hipError_t e = allow_dynamic_lds((const void*)compress_q8<T, R>, lds);
     if (e != hipSuccess) return e;
     const int nb = keys.n_tokens > 0 ? (int)(((int64_t)keys.n_tokens + each - 1) / each) : 1;

@@ -18,32 +18,9 @@ __global__ __launch_bounds__(256) void rows_merge(const float* __restrict__ ws_m
     if (row >= rows) return;
     const int bt = row / Hq, b = bt / n_tok;
     if (n_drafts && bt - b * n_tok >= n_drafts[b]) return;       // (rows behind the last draft stay as they were)
-    const float *m = ws_m + (size_t)row * S, *l = ws_l + (size_t)row * S;
-    const f32x4* a = (const f32x4*)(ws_acc + (size_t)row * S * D) + p;
-    float M = ROWS_NEG_INF;
-    for (int i = p; i < S; i += 32) M = fmaxf(M, m[i]);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o));
-    f32x4 num = (f32x4){0.f, 0.f, 0.f, 0.f};
-    float sum = 0.f;
-    constexpr int STEP = WIDE ? 8 : 1, MC = 4;
-    for (int i0 = WIDE ? grp : 0; i0 < S; i0 += MC * STEP) {
-        f32x4 av[MC];
-        float mv[MC], lv[MC];
-#pragma unroll
-        for (int k = 0; k < MC; ++k) {
-            const int i = i0 + k * STEP, at = min(i, S - 1);
-            av[k] = a[(size_t)at * 32];
-            mv[k] = m[at];
-            lv[k] = i < S ? l[at] : 0.f;
-        }
-#pragma unroll
-        for (int k = 0; k < MC; ++k) {
-            const float w = partial_weight(mv[k], lv[k], M);
-            sum = fmaf(lv[k], w, sum);
-            if (i0 + k * STEP < S) num += av[k] * w;
-        }
-    }
+    f32x4 num;
+    float sum;
+    merge_row<false, WIDE ? 2 : 4>(ws_m + (size_t)row * S, ws_l + (size_t)row * S, ws_acc + (size_t)row * S * D, S, WIDE ? grp : 0, WIDE ? 8 : 1, p, num, sum);
     if constexpr (WIDE) {
         part[grp][p] = num;
         if (p == 0) den[grp] = sum;

@@ -231,10 +231,12 @@ def test_streams_and_graph_replay(ctx):
         assert torch.equal(x.out, want) and np.isfinite(eager)
 
 
-def test_two_calls_at_once(ctx):
-    """Calls with workspaces of their own may overlap on one context."""
-    a = Layer(ctx, np.random.default_rng(21), BF, False, 2, 8, 2, 64, [3000, 2000], [40, 3], 16, [16, 7])
-    b = Layer(ctx, np.random.default_rng(22), BF, True, 2, 8, 2, 64, [3000, 2000], [40, 3], 16, [16, 7])
+@pytest.mark.parametrize("T", [3, 16])
+def test_two_calls_at_once(ctx, T):
+    """Calls on contexts of their own, with workspaces of their own, may overlap."""
+    other = rk.rk_create(0)
+    a = Layer(ctx, np.random.default_rng(21), BF, False, 2, 16, 4, 64, [3000, 2000], [40, 3], T, [T, T // 2])
+    b = Layer(other, np.random.default_rng(22), BF, True, 2, 16, 4, 64, [3000, 2000], [40, 3], T, [T, T // 2])
     s = [torch.cuda.Stream(), torch.cuda.Stream()]
     torch.cuda.synchronize()
     for _ in range(5):
@@ -243,6 +245,45 @@ def test_two_calls_at_once(ctx):
     torch.cuda.synchronize()
     a.check()
     b.check()
+    rk.rk_destroy(other)
+
+
+@pytest.mark.parametrize("dt,q8", [(BF, False), (F32, False), (BF, True), (F32, True)])
+@pytest.mark.parametrize("T,Hq", [(1, 8), (1, 16), (2, 16), (4, 32), (7, 16), (8, 32)])
+def test_fold_gives_what_the_merge_gives(ctx, dt, q8, T, Hq):
+    """8 units: the partials are folded inside the launch; the same by the second launch, again and again on one workspace and its counters."""
+    B, Hkv = 2, 4
+    x = Layer(ctx, np.random.default_rng(T + Hq), dt, q8, B, Hq, Hkv, 64, [1500, 700], [130, 20], T, [T, max(T - 1, 1)])
+    x.call()
+    x.check()
+    first = x.out.clone()
+    for _ in range(3):
+        x.out.fill_(5.0)
+        x.call()
+        assert torch.equal(x.out, first)
+    rk.rk_set_option(ctx, rk.RK_OPT_FUSE_MERGE, 0)
+    try:
+        x.out.fill_(5.0)
+        x.call()
+    finally:
+        rk.rk_set_option(ctx, rk.RK_OPT_FUSE_MERGE, 1)
+    x.check()
+    assert (x.out.float() - first.float()).abs().max() <= 4 * torch.finfo(dt).eps * first.float().abs().max()
+
+
+@pytest.mark.parametrize("q8", [False, True])
+@pytest.mark.parametrize("T", [2, 12, 40])
+@pytest.mark.parametrize("offset", [0, 16, 48])
+def test_bound_and_workspace_of_any_place(ctx, q8, T, offset):
+    """Lengths that are not the host's bound, above and below it, and a workspace that is aligned to 16 bytes only."""
+    x = Layer(ctx, np.random.default_rng(T), BF, q8, 2, 16, 4, 64, [640, 333], [30, 1], T, [T, T])
+    big = torch.full((rk.rk_tree_workspace_size(ctx, x.lay, T) + 64,), 0xff, dtype=torch.uint8, device=DEV)
+    x.ws = big[offset:offset + rk.rk_tree_workspace_size(ctx, x.lay, T)]
+    for bound in (640, 4, 0):
+        x.lay.max_seq_len = bound
+        x.out.fill_(5.0)
+        x.call()
+        x.check()
 
 
 @pytest.mark.parametrize("dt", [BF, F32])
