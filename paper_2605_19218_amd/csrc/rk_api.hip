@@ -318,53 +318,63 @@ size_t rows_ws(const rk_ctx* ctx, const rk_layout* L, int T)
     // (256 bytes more: the accumulators begin a cache line, whatever the workspace's address)
     return align_up((size_t)L->batch * T * L->n_q_heads * rows_slots(ctx, L, T) * (D + 2) * sizeof(float), 256) + 256;
 }
+// The split counts whose launch comes out cheapest, in microseconds as measured: a work-group begins with some 6; a step of its loop (four waves and 32
+// tokens each; of the kernels of many rows 32 tokens with 128 rows, 64 with 64) takes, at r = 64, with 16 rows bf16 0.37, fp32 1.8, 8 bits 0.67 (fp32
+// rows 0.9), with 32 rows two to three times that, with many 0.72 and 1.2; a step of full-width rows 2 to 3, which is their latency.  All
+// work-groups of few rows cannot be faster than the device streams; of many rows two share a compute unit and each takes half as long again.  A
+// split more is a partial a row, written and read.  Measured with each count (us): one token over 8 bits, 8 units x 30000 / 8 tokens, r = 64: 8 splits 31.0, 16
+// 20.0, 32 15.1, 48 13.9; 16 x 8 units x 600, r = 128: 1 12.1, 2 13.4, 4 15.6; 32 drafts, 8 units x 4000: 8 25.8, 16 21.6, 24 21.4, 32 24.7; 64 drafts, 8 x
+// 1000: 4 21.3, 8 18.8, 16 22.8.
 RowsPlan rows_plan(const rk_ctx* ctx, const rk_layout* L, int T, int text_rows, bool drafts, bool q8)
 {
     RowsPlan p;
     p.nrb16 = rows_per_block(L, T);
     p.nrb = (int)row_blocks(L, T);
-    const int64_t groups = (int64_t)p.nrb * L->batch * L->n_kv_heads;
-    const int n_cu = ctx ? ctx->n_cu : 256, slots = rows_slots(ctx, L, T);
-    const bool block = p.nrb16 >= 4;
-    // steps of a work-group: tokens of the cache, and full-width rows, that all of its waves take at once
-    const int step_v = p.nrb16 == 8 ? 32 : p.nrb16 == 4 ? 64 : 128, step_r = 128;
-    const int nv = (L->max_seq_len + step_v - 1) / step_v, nr = block ? (text_rows + 63) / 64 + (drafts ? 1 : 0) : ((text_rows + 31) / 32 + (drafts ? (T + 31) / 32 : 0) + 3) / 4;
-    const double tv = 1.2, tr = 4.0, begin = 8.0;
-    const int n_wg = block ? 2 * n_cu : n_cu;        // work-groups at once
-    (void)step_r; (void)q8;
-    const int most_v = nv < 1 ? 1 : nv, most_r = nr;
-    const int total = (int)(n_wg / groups) < 1 ? 1 : (int)(n_wg / groups);
-    p.Sv = 1;
-    p.Sr = nr ? 1 : 0;
+    const bool block = p.nrb16 >= 4, f32 = L->dtype == RK_F32;
+    const int64_t units = (int64_t)L->batch * L->n_kv_heads, groups = p.nrb * units;
+    const int64_t rows = (int64_t)T * (L->n_q_heads / L->n_kv_heads), in_block = rows < 16 * p.nrb16 ? rows : 16 * p.nrb16;
+    const int n_cu = ctx ? ctx->n_cu : 256, slots = rows_slots(ctx, L, T), n_wg = block ? 2 * n_cu : n_cu;
+    const int step = p.nrb16 == 8 ? 32 : p.nrb16 == 4 ? 64 : 128;
+    const int nv = (L->max_seq_len + step - 1) / step;
+    const int nr = block ? (text_rows + 63) / 64 + (drafts ? 1 : 0) : ((text_rows + 31) / 32 + (drafts ? (T + 31) / 32 : 0) + 3) / 4;
+    const double wide = (keep_padded(L->keep) + D) / 192.0, two = p.nrb16 == 2 ? (f32 ? 1.9 : q8 ? 1.7 : 3.0) : 1.0;
+    const double tv = wide * (p.nrb16 == 8 ? 0.72 : p.nrb16 == 4 ? 1.2 : two * (q8 ? (f32 ? 0.9 : 0.67) : f32 ? 1.8 : 0.37));
+    const double tr = block ? 3.0 : f32 ? 4.0 : 2.0;
+    const double token = q8 ? keep_padded(L->keep) + D + 4 : (double)elem_size(L->dtype) * (keep_padded(L->keep) + D);
+    const double stream = block ? 0.0 : (double)units * L->max_seq_len * token / 6.2e6;
+    auto folds = [&](int S) {
+        return !block && ctx && ctx->fuse_merge && ctx->xcd_deal_ok && S > 1 && units % 8 == 0 && groups <= DEC_COUNTERS && in_block * S <= 64;
+    };
+    auto cost = [&](int sv, int sr) {
+        const int S = sv + sr;
+        const int64_t W = groups * S;
+        const double v = (nv + sv - 1) / sv * tv, r = sr ? (nr + sr - 1) / sr * tr : 0.0;
+        double loop = v > r ? v : r;
+        if (block && W > n_cu) loop *= 1.5;
+        loop = loop > stream ? loop + 0.35 * stream : stream + 0.35 * loop;
+        const double rounds = (double)((groups * sv + n_wg - 1) / n_wg) + (W > n_wg ? 0.3 : 0.0);
+        const double merge = S == 1 ? 0.0 : folds(S) ? 1.5 : 2.5 + S / 32.0 + (double)rows * units * S * 1040 / 5e6;
+        return (6.0 + loop) * (W > n_wg ? rounds : 1.0) + merge;
+    };
+    const int most_v = nv < 1 ? 1 : nv < 48 ? nv : 48, r0 = nr ? 1 : 0, r1 = nr < slots / 2 ? nr : slots / 2;
+    static const int tries[] = {1, 2, 3, 4, 5, 6, 7, 8, 10, 12, 14, 16, 20, 24, 28, 32, 40, 48};
     double best = 1e30;
-    const int r0 = nr ? 1 : 0, r1 = nr < slots / 2 ? nr : slots / 2;
-    for (int r = r0; r <= r1; ++r) {
-        const int lo = total > r + 1 ? total - r : 1, hi = total > r + 1 ? total - r : 8;
-        for (int v = lo; v <= hi; ++v) {
-            const int sv = v > most_v ? most_v : v > slots - r ? slots - r : v;
-            const double wv = begin + (nv + sv - 1) / sv * tv, wr = r ? begin + (nr + r - 1) / r * tr : 0.0;
-            const double work = groups * (sv * wv + r * wr) / n_wg;
-            double cost = wv > wr ? wv : wr;
-            if (groups * (sv + r) > n_wg) {
-                const double rounds = (double)((groups * sv + n_wg - 1) / n_wg) * wv;
-                cost = rounds > work ? rounds : work;
-            }
-            cost += (double)L->batch * T * L->n_q_heads * (sv + r) * 520.0 * 2 / 4e6;
-            if (cost < best) { best = cost; p.Sv = sv; p.Sr = r; }
-        }
+    p.Sv = 1;
+    p.Sr = r0;
+    for (int r = r0; r <= r1 && r <= 8; r += r < 4 ? 1 : 2) {
+        const int64_t full = n_wg / groups - r;        // what fills the device
+        auto look = [&](int64_t v) {
+            if (v < 1 || v > most_v || v > slots - r) return;
+            const double c = cost((int)v, r);
+            if (c < best - 0.01) { best = c; p.Sv = (int)v; p.Sr = r; }
+        };
+        for (int v : tries) look(v);
+        look(full);
     }
-    (void)most_r;
-    if (ctx && ctx->decode_splits > 0) {
-        p.Sv = ctx->decode_splits;
-        if (p.Sv > slots - p.Sr) p.Sv = slots - p.Sr;
-    }
-    if (p.Sv < 1) p.Sv = 1;
+    if (ctx && ctx->decode_splits > 0) p.Sv = ctx->decode_splits < slots - p.Sr ? ctx->decode_splits : slots - p.Sr;
     // The partials of a row block folded by its last work-group: where the units fill the XCDs evenly, and what one work-group then reads is
     // little (the merge launch spreads it over the device).
-    const int64_t units = (int64_t)L->batch * L->n_kv_heads, rows = (int64_t)T * (L->n_q_heads / L->n_kv_heads);
-    const int S = p.Sv + p.Sr;
-    p.fold = !block && ctx && ctx->fuse_merge && ctx->xcd_deal_ok && S > 1 && units % 8 == 0 && groups <= DEC_COUNTERS &&
-             (rows < 16 * p.nrb16 ? rows : 16 * p.nrb16) * S <= 64;
+    p.fold = folds(p.Sv + p.Sr);
     return p;
 }
 

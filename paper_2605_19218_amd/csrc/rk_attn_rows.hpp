@@ -372,15 +372,17 @@ template <int R> struct TileOf<ROWS_Q8_F32, R> { typedef TileQ8<R> type; };
 // tokens of its group (bf16: the 8 x 8 transpose of a lane's own registers, at use).
 __device__ __forceinline__ uint32_t dword_of(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 
-// What a weight of 0 does not erase: a Value that is no number.  Where a tile of drafts holds one, it is taken out of the product, and
-// the rows that see its token get it added: sums of it are it (or NaN, of both infinities).
-struct Odd { float value; };
-__device__ __forceinline__ uint32_t pick_odd(uint32_t x, int kind)       // kind 0 NaN, 1 infinity, 2 minus infinity; x: fp32 bits
+// What a weight of 0 does not erase: a Value that is no number.  Where a draft holds one it is left out of the product (clean()), and behind the loop the
+// rows that see the draft get it added: a sum of it is it (or NaN, of both infinities).
+__device__ __forceinline__ bool no_number(uint32_t fp32_bits) { return (fp32_bits & 0x7f800000u) == 0x7f800000u; }
+// a bit a token of the tile, the same in all lanes, from a bit a token slot of this lane's group
+__device__ __forceinline__ uint32_t tokens_of(uint32_t slots, int g)
 {
-    const uint32_t a = x & 0x7fffffffu;
-    return kind == 0 ? a > 0x7f800000u : kind == 1 ? x == 0x7f800000u : x == 0xff800000u;
+    uint32_t t = (slots & 15) << (4 * g) | (slots >> 4) << (16 + 4 * g);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) t |= (uint32_t)__shfl_xor((int)t, o);
+    return __builtin_amdgcn_readfirstlane(t);
 }
-__device__ __forceinline__ float odd_value(int kind) { return __uint_as_float(kind == 0 ? 0x7fc00000u : kind == 1 ? 0x7f800000u : 0xff800000u); }
 
 template <int NRB>
 struct PlainRowsBf16 {
@@ -430,12 +432,36 @@ struct PlainRowsBf16 {
 #pragma unroll
         for (int jj = 0; jj < 8; ++jj)
 #pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                const uint32_t x = dword_of(v[jj], w);
-                any |= (x & 0x7f800000u) == 0x7f800000u || (x & 0x7f80u) == 0x7f80u;
-            }
+            for (int w = 0; w < 4; ++w) any |= no_number(dword_of(v[jj], w)) || no_number(dword_of(v[jj], w) << 16);
         return any;
     }
+    __device__ __forceinline__ uint32_t clean(int g)
+    {
+        uint32_t slots = 0;
+#pragma unroll
+        for (int jj = 0; jj < 8; ++jj) {
+            uint32_t w[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                w[i] = dword_of(v[jj], i);
+                const uint32_t keep = (no_number(w[i]) ? 0u : 0xffff0000u) | (no_number(w[i] << 16) ? 0u : 0xffffu);
+                slots |= keep == ~0u ? 0u : 1u << jj;
+                w[i] &= keep;
+            }
+            v[jj] = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+        return tokens_of(slots, g);
+    }
+    // channel e of eight of a draft, where it is no number
+    struct Eight {
+        uint4 d;
+        __device__ __forceinline__ explicit Eight(const bf16_t* p) : d(*(const uint4*)p) {}
+        __device__ __forceinline__ float odd(int e) const
+        {
+            const uint32_t w = e & 1 ? dword_of(d, e >> 1) & 0xffff0000u : dword_of(d, e >> 1) << 16;
+            return no_number(w) ? __uint_as_float(w) : 0.f;
+        }
+    };
     __device__ __forceinline__ uint4 column(int cb) const
     {
         const uint32_t sel = (cb & 1) ? 0x07060302u : 0x05040100u;
@@ -461,42 +487,6 @@ struct PlainRowsBf16 {
             for (int k2 = 1; k2 >= 0; --k2)
 #pragma unroll
                 for (int rb = 0; rb < NRB; ++rb) O[rb][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, p[rb][k2], O[rb][cb], 0, 0, 0);
-        }
-    }
-    // see: bit e of see[rb]: row n sees token slot e of this lane's group
-    __device__ __forceinline__ void add_odd(const uint32_t (&see)[NRB], f32x4 (&O)[NRB][8])
-    {
-        bf16x8 p[NRB];
-#pragma unroll
-        for (int rb = 0; rb < NRB; ++rb)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) p[rb][e] = (__bf16)((see[rb] >> e) & 1 ? 1.f : 0.f);
-#pragma unroll 1
-        for (int kind = 0; kind < 3; ++kind)
-#pragma unroll
-            for (int cb = 0; cb < 8; ++cb) {
-                const uint4 d = column(cb);
-                uint32_t x[4];
-#pragma unroll
-                for (int w = 0; w < 4; ++w)
-                    x[w] = (pick_odd(dword_of(d, w) << 16, kind) ? 0x3f80u : 0u) | (pick_odd(dword_of(d, w) & 0xffff0000u, kind) ? 0x3f800000u : 0u);
-                const bf16x8 vf = __builtin_bit_cast(bf16x8, make_uint4(x[0], x[1], x[2], x[3]));
-#pragma unroll
-                for (int rb = 0; rb < NRB; ++rb) {
-                    const f32x4 c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, p[rb], (f32x4){0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-#pragma unroll
-                    for (int ii = 0; ii < 4; ++ii) O[rb][cb][ii] += c[ii] > 0.f ? odd_value(kind) : 0.f;
-                }
-            }
-#pragma unroll
-        for (int jj = 0; jj < 8; ++jj) {
-            uint32_t w[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                w[i] = dword_of(v[jj], i);
-                w[i] &= ((w[i] & 0x7f800000u) == 0x7f800000u ? 0u : 0xffff0000u) | ((w[i] & 0x7f80u) == 0x7f80u ? 0u : 0xffffu);
-            }
-            v[jj] = make_uint4(w[0], w[1], w[2], w[3]);
         }
     }
 };
@@ -552,9 +542,31 @@ struct PlainRowsF32 {
 #pragma unroll
         for (int jj = 0; jj < 8; ++jj)
 #pragma unroll
-            for (int c = 0; c < 8; ++c) any |= (__float_as_uint(v[jj][c >> 2][c & 3]) & 0x7f800000u) == 0x7f800000u;
+            for (int c = 0; c < 8; ++c) any |= no_number(__float_as_uint(v[jj][c >> 2][c & 3]));
         return any;
     }
+    __device__ __forceinline__ uint32_t clean(int g)
+    {
+        uint32_t slots = 0;
+#pragma unroll
+        for (int jj = 0; jj < 8; ++jj)
+#pragma unroll
+            for (int c = 0; c < 8; ++c)
+                if (no_number(__float_as_uint(v[jj][c >> 2][c & 3]))) {
+                    slots |= 1u << jj;
+                    v[jj][c >> 2][c & 3] = 0.f;
+                }
+        return tokens_of(slots, g);
+    }
+    struct Eight {
+        f32x4 a, b;
+        __device__ __forceinline__ explicit Eight(const float* p) : a(*(const f32x4*)p), b(*(const f32x4*)(p + 4)) {}
+        __device__ __forceinline__ float odd(int e) const
+        {
+            const float x = e < 4 ? a[e & 3] : b[e & 3];
+            return no_number(__float_as_uint(x)) ? x : 0.f;
+        }
+    };
     __device__ __forceinline__ void accumulate(const f32x4 (&s)[NRB][2], f32x4 (&O)[NRB][8]) const
     {
 #pragma unroll
@@ -564,28 +576,6 @@ struct PlainRowsF32 {
 #pragma unroll
                 for (int rb = 0; rb < NRB; ++rb)
                     O[rb][cb] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[jj][cb >> 2][cb & 3], s[rb][jj >> 2][jj & 3], O[rb][cb], 0, 0, 0);
-    }
-    __device__ __forceinline__ void add_odd(const uint32_t (&see)[NRB], f32x4 (&O)[NRB][8])
-    {
-#pragma unroll 1
-        for (int kind = 0; kind < 3; ++kind)
-#pragma unroll
-            for (int cb = 0; cb < 8; ++cb)
-#pragma unroll
-                for (int rb = 0; rb < NRB; ++rb) {
-                    f32x4 c = (f32x4){0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                    for (int jj = 0; jj < 8; ++jj)
-                        c = __builtin_amdgcn_mfma_f32_16x16x4f32(pick_odd(__float_as_uint(v[jj][cb >> 2][cb & 3]), kind) ? 1.f : 0.f,
-                                                                 (see[rb] >> jj) & 1 ? 1.f : 0.f, c, 0, 0, 0);
-#pragma unroll
-                    for (int ii = 0; ii < 4; ++ii) O[rb][cb][ii] += c[ii] > 0.f ? odd_value(kind) : 0.f;
-                }
-#pragma unroll
-        for (int jj = 0; jj < 8; ++jj)
-#pragma unroll
-            for (int c = 0; c < 8; ++c)
-                if ((__float_as_uint(v[jj][c >> 2][c & 3]) & 0x7f800000u) == 0x7f800000u) v[jj][c >> 2][c & 3] = 0.f;
     }
 };
 
@@ -908,6 +898,7 @@ __global__ __launch_bounds__(256, NRB == 1 && FMT != ROWS_F32 ? 2 : 1) void attn
             const T* dv = (const T*)A.draft_v + (int64_t)b * A.draft_sb + (int64_t)hk * A.draft_sh;
             Plain X;
             X.take(qrow, g);
+            uint64_t odd = 0;                              // drafts whose Values hold one that is no number
 #pragma unroll 1
             for (int t = t0 + wave; t < t1; t += 4) {
                 const bool own = t >= tt;                  // drafts
@@ -935,8 +926,22 @@ __global__ __launch_bounds__(256, NRB == 1 && FMT != ROWS_F32 ? 2 : 1) void attn
                     if (r0 + (e < 4 ? 4 * g + e : 12 + 4 * g + e) >= rows) X.drop(e);
                 }
                 st.weigh(s);
-                if (own && __any(X.odd())) X.add_odd(see, st.O);
+                if (own && __any(X.odd())) odd |= (uint64_t)X.clean(g) << r0;
                 X.accumulate(s, st.O);
+            }
+#pragma unroll 1
+            for (; odd; odd &= odd - 1) {                  // (accumulator (cb, ii) is channel 32 g + 8 ii + cb)
+                const int j = __builtin_ctzll(odd);
+#pragma unroll
+                for (int ii = 0; ii < 4; ++ii) {
+                    const typename Plain::Eight x(dv + (int64_t)j * A.draft_st + 32 * g + 8 * ii);
+#pragma unroll
+                    for (int rb = 0; rb < NRB; ++rb) {
+                        const uint64_t mask = A.mask ? A.mask[(size_t)b * A.T + tok[rb]] : (2ull << tok[rb]) - 1;
+#pragma unroll
+                        for (int cb = 0; cb < 8; ++cb) st.O[rb][cb][ii] += (mask >> j) & 1 ? x.odd(cb) : 0.f;
+                    }
+                }
             }
         }
     }
