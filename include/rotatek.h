@@ -462,9 +462,9 @@ rk_status rk_decode_attn_tree_quant(rk_ctx* ctx, const rk_layout* L, const void*
 /* The accepted drafts join the text segment: row len[b] + i of text->k / text->v receives draft path[b*path_len + i] for i <
  * n_path[b] and every KV head; len_out[b] = len[b] + the rows copied.  len_out may be text->len or another array.
  * path [B, path_len], n_path [B]: device; path_len 1..RK_MAX_DRAFTS.  A path ends before its first entry that is not one of the
- * sequence's drafts, and where the segment is full; the same draft may stand in it twice.  The segment and the
- * drafts may not overlap in memory.  RK_ERR_CAPACITY if text->max_len + path_len > text->capacity.  Calls on one
- * context must not overlap.  Errors: INVALID_ARG, UNSUPPORTED, CAPACITY, HIP.                                 */
+ * sequence's drafts, and where the segment is full; the same draft may stand in it twice.  The stretch of memory from the
+ * segment's first row to its last and the drafts' may not meet.  RK_ERR_CAPACITY if text->max_len + path_len >
+ * text->capacity.  Calls on one context must not overlap.  Errors: INVALID_ARG, UNSUPPORTED, CAPACITY, HIP.                                 */
 rk_status rk_append_text_path(rk_ctx* ctx, const rk_layout* L, const rk_text* text, const rk_drafts* drafts,
                               const int32_t* path, int32_t path_len, const int32_t* n_path, int32_t* len_out,
                               void* stream);

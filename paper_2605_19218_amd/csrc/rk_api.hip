@@ -336,7 +336,8 @@ RowsPlan rows_plan(const rk_ctx* ctx, const rk_layout* L, int T, int text_rows, 
     const int n_cu = ctx ? ctx->n_cu : 256, slots = rows_slots(ctx, L, T), n_wg = block ? 2 * n_cu : n_cu;
     const int step = p.nrb16 == 8 ? 32 : p.nrb16 == 4 ? 64 : 128;
     const int nv = (L->max_seq_len + step - 1) / step;
-    const int nr = block ? (text_rows + 63) / 64 + (drafts ? 1 : 0) : ((text_rows + 31) / 32 + (drafts ? (T + 31) / 32 : 0) + 3) / 4;
+    const int64_t text = text_rows;        // (its bound is the caller's, up to the largest int)
+    const int nr = (int)(block ? (text + 63) / 64 + (drafts ? 1 : 0) : ((text + 31) / 32 + (drafts ? (T + 31) / 32 : 0) + 3) / 4);
     const double wide = (keep_padded(L->keep) + D) / 192.0, two = p.nrb16 == 2 ? (f32 ? 1.9 : q8 ? 1.7 : 3.0) : 1.0;
     const double tv = wide * (p.nrb16 == 8 ? 0.72 : p.nrb16 == 4 ? 1.2 : two * (q8 ? (f32 ? 0.9 : 0.67) : f32 ? 1.8 : 0.37));
     const double tr = block ? 3.0 : f32 ? 4.0 : 2.0;
@@ -1110,7 +1111,7 @@ rk_status rk_append_text_path(rk_ctx* ctx, const rk_layout* L, const rk_text* te
     if (!path || !n_path || !len_out) return fail(ctx, RK_ERR_INVALID_ARG, "append_text_path: NULL pointer (path, n_path, len_out)");
     if (path_len < 1 || path_len > RK_MAX_DRAFTS)
         return fail(ctx, RK_ERR_INVALID_ARG, "append_text_path: path_len %d outside 1..%d", path_len, RK_MAX_DRAFTS);
-    if (text->max_len + path_len > text->capacity)
+    if (text->max_len > text->capacity - path_len)
         return fail(ctx, RK_ERR_CAPACITY, "append_text_path: %d + %d rows exceed capacity %d", text->max_len, path_len, text->capacity);
     // rows copied by one work-group may be read by another: the drafts' rows and the segment's lie apart
     const size_t es = elem_size(L->dtype);

@@ -127,3 +127,10 @@ def test_null_context():
     L = rk.lib()
     assert L.rk_decode_attn_tree(None, C.byref(lay().c()), P, P, P, P, P, None, C.byref(drafts().c()), 0.0, P, P, 1, None) == rk.RK_ERR_INVALID_ARG
     assert L.rk_compress_quant(None, None, None, None, None, None, None, None, None) == rk.RK_ERR_INVALID_ARG
+
+
+def test_text_of_the_largest_bound(ctx):
+    """A bound next to the largest int does not pass for a small one."""
+    most = (1 << 31) - 1
+    t = text(max_len=most, capacity=most)
+    assert status(rk.rk_append_text_path, ctx, lay(), t, drafts(k=1 << 60, v=1 << 60), P, P, P, path_len=8) == rk.RK_ERR_CAPACITY
