@@ -140,6 +140,9 @@ def lib():
             _rkbind.bind(Layout, Text, *[C.cast(f, C.c_void_p).value for f in
                                          (L.rk_decode_attn, L.rk_append_decode_attn, L.rk_decode_attn_dual,
                                           L.rk_append_text_decode_attn_dual)])
+            _rkbind.bind_drafts(Drafts, *[C.cast(f, C.c_void_p).value for f in
+                                          (L.rk_append_quant, L.rk_decode_attn_quant, L.rk_decode_attn_tree,
+                                           L.rk_decode_attn_tree_quant, L.rk_append_text_path)])
             _bind = _rkbind
         _lib = L
     return _lib
@@ -438,6 +441,8 @@ def rk_compress_quant(ctx, layout: Layout, keys: Rows, R_r, k_q8, values: Rows, 
 
 def rk_append_quant(ctx, layout: Layout, k_new, v_new, R_r, k_q8, v_q8, seq_len_out, stream=None) -> None:
     """One token at row layout.seq_len[b]; seq_len_out[b] = layout.seq_len[b] + 1 (may be the same tensor)."""
+    if _bind is not None and _done(ctx, _bind.append_quant(ctx, layout, k_new, v_new, R_r, k_q8, v_q8, seq_len_out, stream)):
+        return
     _check(ctx, lib().rk_append_quant(ctx, C.byref(layout.c()), _ptr(k_new), _ptr(v_new), _ptr(R_r), _ptr(k_q8), _ptr(v_q8),
                                    _ptr(seq_len_out), _stream(stream)))
 
@@ -453,6 +458,9 @@ def rk_tree_workspace_size(ctx, layout: Layout, n_tokens: int) -> int:
 
 def rk_decode_attn_quant(ctx, layout: Layout, q, k_q8, v_q8, R_r, delta_mu, text: Optional[Text], scale: float, out, workspace,
                       stream=None, workspace_bytes: Optional[int] = None) -> None:
+    if _bind is not None and _done(ctx, _bind.decode_quant(ctx, layout, q, k_q8, v_q8, R_r, delta_mu, text, scale, out, workspace,
+                                                           stream, workspace_bytes)):
+        return
     wb = workspace_bytes if workspace_bytes is not None else (_nbytes(workspace) if workspace is not None else 0)
     tref = C.byref(text.c()) if text is not None else None
     _check(ctx, lib().rk_decode_attn_quant(ctx, C.byref(layout.c()), _ptr(q), _ptr(k_q8), _ptr(v_q8), _ptr(R_r), _ptr(delta_mu),
@@ -462,6 +470,9 @@ def rk_decode_attn_quant(ctx, layout: Layout, q, k_q8, v_q8, R_r, delta_mu, text
 def rk_decode_attn_tree(ctx, layout: Layout, q, k_packed, v_cache, R_r, delta_mu, text: Optional[Text], drafts: Drafts,
                         scale: float, out, workspace, stream=None, workspace_bytes: Optional[int] = None) -> None:
     """q, out: [B, drafts.n_tokens, H_q, d]."""
+    if _bind is not None and _done(ctx, _bind.tree(ctx, layout, q, k_packed, v_cache, R_r, delta_mu, text, drafts, scale, out,
+                                                   workspace, stream, workspace_bytes)):
+        return
     wb = workspace_bytes if workspace_bytes is not None else (_nbytes(workspace) if workspace is not None else 0)
     tref = C.byref(text.c()) if text is not None else None
     dref = C.byref(drafts.c()) if drafts is not None else None
@@ -473,6 +484,9 @@ def rk_decode_attn_tree(ctx, layout: Layout, q, k_packed, v_cache, R_r, delta_mu
 def rk_decode_attn_tree_quant(ctx, layout: Layout, q, k_q8, v_q8, R_r, delta_mu, text: Optional[Text], drafts: Drafts,
                            scale: float, out, workspace, stream=None, workspace_bytes: Optional[int] = None) -> None:
     """rk_decode_attn_tree over 8-bit caches."""
+    if _bind is not None and _done(ctx, _bind.tree_quant(ctx, layout, q, k_q8, v_q8, R_r, delta_mu, text, drafts, scale, out,
+                                                         workspace, stream, workspace_bytes)):
+        return
     wb = workspace_bytes if workspace_bytes is not None else (_nbytes(workspace) if workspace is not None else 0)
     tref = C.byref(text.c()) if text is not None else None
     dref = C.byref(drafts.c()) if drafts is not None else None
@@ -484,8 +498,10 @@ def rk_decode_attn_tree_quant(ctx, layout: Layout, q, k_q8, v_q8, R_r, delta_mu,
 def rk_append_text_path(ctx, layout: Layout, text: Text, drafts: Drafts, path, n_path, len_out, path_len: Optional[int] = None,
                         stream=None) -> None:
     """path: device int32 [B, path_len] (contiguous); n_path, len_out: device int32 [B]; len_out may be text.len."""
+    n = path_len if path_len is not None else int(path.shape[1])
+    if _bind is not None and _done(ctx, _bind.append_path(ctx, layout, text, drafts, path, n_path, len_out, n, stream)):
+        return
     tref = C.byref(text.c()) if text is not None else None
     dref = C.byref(drafts.c()) if drafts is not None else None
-    n = path_len if path_len is not None else int(path.shape[1])
     _check(ctx, lib().rk_append_text_path(ctx, C.byref(layout.c()), tref, dref, _ptr(path), n, _ptr(n_path), _ptr(len_out),
                                           _stream(stream)))

@@ -1,5 +1,6 @@
 // CPython side of the calls that a program makes once per generated token and layer: the arguments of rk_decode_attn,
-// rk_append_decode_attn, rk_decode_attn_dual and rk_append_text_decode_attn_dual, marshalled in C.  The same through ctypes costs some 5 us a
+// rk_append_decode_attn, rk_decode_attn_dual and rk_append_text_decode_attn_dual, of rk_append_quant and rk_decode_attn_quant, and, once per
+// round of drafts and layer, of rk_decode_attn_tree, rk_decode_attn_tree_quant and rk_append_text_path, marshalled in C.  The same through ctypes costs some 5 us a
 // call (structures built field by field, a converter per argument), which is as long as a short decode runs on the device: 8 KV heads x
 // 1024 tokens were called every 8.7 us, of which the device needed 5.8.
 //
@@ -23,14 +24,24 @@ typedef rk_status (*dual_fn)(rk_ctx*, const rk_layout*, const void*, const void*
 typedef rk_status (*append_dual_fn)(rk_ctx*, const rk_layout*, const void*, const void*, const void*, const void*, const void*,
                                     const float*, const float*, const rk_text*, float, void*, void*, size_t, void*);
 
+typedef rk_status (*append_quant_fn)(rk_ctx*, const rk_layout*, const void*, const void*, const float*, void*, void*, int32_t*, void*);
+typedef rk_status (*tree_fn)(rk_ctx*, const rk_layout*, const void*, const void*, const void*, const float*, const float*,
+                             const rk_text*, const rk_drafts*, float, void*, void*, size_t, void*);
+typedef rk_status (*path_fn)(rk_ctx*, const rk_layout*, const rk_text*, const rk_drafts*, const int32_t*, int32_t, const int32_t*,
+                             int32_t*, void*);
+
 decode_fn fn_decode;
 append_decode_fn fn_append_decode;
 dual_fn fn_dual;
 append_dual_fn fn_append_dual;
-PyTypeObject *layout_type, *text_type;      // the binding's classes (kept alive)
+append_quant_fn fn_append_quant;
+dual_fn fn_decode_quant;
+tree_fn fn_tree, fn_tree_quant;
+path_fn fn_path;
+PyTypeObject *layout_type, *text_type, *drafts_type;      // the binding's classes (kept alive)
 
 PyObject *s_batch, *s_nq, *s_nkv, *s_hd, *s_keep, *s_dtype, *s_cap, *s_max_seq, *s_seq, *s_data_ptr, *s_numel, *s_esize, *s_cuda_stream,
-    *s_k, *s_v, *s_max_len, *s_len, *s_strides, *s_stride, *s_shape;
+    *s_k, *s_v, *s_max_len, *s_len, *s_strides, *s_stride, *s_shape, *s_n_tokens, *s_n_tokens_dev, *s_mask;
 
 // All of these return false where the argument is not of the plain kind; an exception may then be set, and the caller clears it.
 bool integer(PyObject* o, long long* out)
@@ -100,6 +111,15 @@ bool three(PyObject* t, int64_t* out)       // the first three of a tuple
     }
     return true;
 }
+// strides of `given`, or those of the tensor `key`
+bool strides_of(PyObject* given, PyObject* key, int64_t* st)
+{
+    if (given != Py_None) return PyTuple_Check(given) && PyTuple_GET_SIZE(given) == 3 && three(given, st);
+    PyObject* s = PyObject_CallMethodNoArgs(key, s_stride);
+    const bool ok = s && three(s, st);
+    Py_XDECREF(s);
+    return ok;
+}
 bool text(PyObject* o, rk_text* T)
 {
     if (Py_TYPE(o) != text_type) return false;
@@ -109,14 +129,7 @@ bool text(PyObject* o, rk_text* T)
     PyObject* key = PyObject_GetAttr(o, s_k);
     PyObject* given = key ? PyObject_GetAttr(o, s_strides) : nullptr;
     PyObject* cap = given ? PyObject_GetAttr(o, s_cap) : nullptr;
-    bool ok = cap != nullptr;
-    if (ok && given == Py_None) {
-        PyObject* s = PyObject_CallMethodNoArgs(key, s_stride);
-        ok = s && three(s, st);
-        Py_XDECREF(s);
-    } else if (ok) {
-        ok = PyTuple_Check(given) && PyTuple_GET_SIZE(given) == 3 && three(given, st);
-    }
+    bool ok = cap && strides_of(given, key, st);
     long long rows = 0;
     if (ok && cap == Py_None) {
         PyObject* shape = PyObject_GetAttr(key, s_shape);
@@ -138,7 +151,34 @@ bool text(PyObject* o, rk_text* T)
     T->capacity = (int32_t)rows;
     return true;
 }
-// scale, out, workspace, stream, workspace_bytes: how every call ends
+bool drafts(PyObject* o, rk_drafts* d)
+{
+    if (!drafts_type || Py_TYPE(o) != drafts_type) return false;
+    void *k = nullptr, *v = nullptr, *n = nullptr, *mask = nullptr;
+    int64_t st[3];
+    if (!address_of(o, s_k, &k) || !address_of(o, s_v, &v) || !address_of(o, s_n_tokens_dev, &n) || !address_of(o, s_mask, &mask) ||
+        !int32_of(o, s_n_tokens, &d->n_tokens))
+        return false;
+    PyObject* key = PyObject_GetAttr(o, s_k);
+    PyObject* given = key ? PyObject_GetAttr(o, s_strides) : nullptr;
+    const bool ok = given && strides_of(given, key, st);
+    Py_XDECREF(given);
+    Py_XDECREF(key);
+    if (!ok) return false;
+    d->k = (decltype(d->k))k;
+    d->v = (decltype(d->v))v;
+    d->n_tokens_dev = (decltype(d->n_tokens_dev))n;
+    d->mask = (decltype(d->mask))mask;
+    d->stride_b = st[0];
+    d->stride_h = st[1];
+    d->stride_t = st[2];
+    return true;
+}
+bool stream_of(PyObject* o, void** out)
+{
+    return o == Py_None || PyLong_CheckExact(o) ? address(o, out) : address_of(o, s_cuda_stream, out);
+}
+// scale, out, workspace, stream, workspace_bytes: how every attention call ends
 struct Tail { float scale; void *out, *ws, *stream; size_t bytes; };
 bool tail(PyObject* const* a, Tail* t)
 {
@@ -147,11 +187,7 @@ bool tail(PyObject* const* a, Tail* t)
     if (s == -1.0 && PyErr_Occurred()) return false;
     t->scale = (float)s;
     if (!address(a[1], &t->out) || !address(a[2], &t->ws)) return false;
-    if (a[3] == Py_None || PyLong_CheckExact(a[3])) {
-        if (!address(a[3], &t->stream)) return false;
-    } else if (!address_of(a[3], s_cuda_stream, &t->stream)) {
-        return false;
-    }
+    if (!stream_of(a[3], &t->stream)) return false;
     long long n = 0, e = 1;
     if (a[4] != Py_None) {
         if (!integer(a[4], &n)) return false;
@@ -238,6 +274,74 @@ PyObject* py_append_dual(PyObject*, PyObject* const* a, Py_ssize_t n)
     return answer(s);
 }
 
+// (ctx, layout, k_new, v_new, R_r, k_q8, v_q8, seq_len_out, stream)
+PyObject* py_append_quant(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    void *ctx, *p[6], *stream;
+    rk_layout L;
+    if (n != 9 || !fn_append_quant || !address(a[0], &ctx) || !layout(a[1], &L) || !addresses(a + 2, 6, p) || !stream_of(a[8], &stream))
+        return other_path();
+    rk_status s;
+    Py_BEGIN_ALLOW_THREADS
+    s = fn_append_quant((rk_ctx*)ctx, &L, p[0], p[1], (const float*)p[2], p[3], p[4], (int32_t*)p[5], stream);
+    Py_END_ALLOW_THREADS
+    return answer(s);
+}
+// (ctx, layout, q, k_q8, v_q8, R_r, delta_mu, text or None, scale, out, workspace, stream, workspace_bytes)
+PyObject* py_decode_quant(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    void *ctx, *p[5];
+    rk_layout L;
+    rk_text T;
+    Tail t;
+    if (n != 13 || !fn_decode_quant || !address(a[0], &ctx) || !layout(a[1], &L) || !addresses(a + 2, 5, p) ||
+        (a[7] != Py_None && !text(a[7], &T)) || !tail(a + 8, &t))
+        return other_path();
+    rk_status s;
+    Py_BEGIN_ALLOW_THREADS
+    s = fn_decode_quant((rk_ctx*)ctx, &L, p[0], p[1], p[2], (const float*)p[3], (const float*)p[4], a[7] != Py_None ? &T : nullptr, t.scale,
+                        t.out, t.ws, t.bytes, t.stream);
+    Py_END_ALLOW_THREADS
+    return answer(s);
+}
+// (ctx, layout, q, k_packed, v_cache, R_r, delta_mu, text or None, drafts, scale, out, workspace, stream, workspace_bytes)
+PyObject* tree(tree_fn f, PyObject* const* a, Py_ssize_t n)
+{
+    void *ctx, *p[5];
+    rk_layout L;
+    rk_text T;
+    rk_drafts d;
+    Tail t;
+    if (n != 14 || !f || !address(a[0], &ctx) || !layout(a[1], &L) || !addresses(a + 2, 5, p) || (a[7] != Py_None && !text(a[7], &T)) ||
+        !drafts(a[8], &d) || !tail(a + 9, &t))
+        return other_path();
+    rk_status s;
+    Py_BEGIN_ALLOW_THREADS
+    s = f((rk_ctx*)ctx, &L, p[0], p[1], p[2], (const float*)p[3], (const float*)p[4], a[7] != Py_None ? &T : nullptr, &d, t.scale, t.out,
+          t.ws, t.bytes, t.stream);
+    Py_END_ALLOW_THREADS
+    return answer(s);
+}
+PyObject* py_tree(PyObject*, PyObject* const* a, Py_ssize_t n) { return tree(fn_tree, a, n); }
+PyObject* py_tree_quant(PyObject*, PyObject* const* a, Py_ssize_t n) { return tree(fn_tree_quant, a, n); }
+// (ctx, layout, text, drafts, path, n_path, len_out, path_len, stream)
+PyObject* py_append_path(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    void *ctx, *p[3], *stream;
+    rk_layout L;
+    rk_text T;
+    rk_drafts d;
+    long long len;
+    if (n != 9 || !fn_path || !address(a[0], &ctx) || !layout(a[1], &L) || !text(a[2], &T) || !drafts(a[3], &d) || !addresses(a + 4, 3, p) ||
+        !integer(a[7], &len) || len < INT32_MIN || len > INT32_MAX || !stream_of(a[8], &stream))
+        return other_path();
+    rk_status s;
+    Py_BEGIN_ALLOW_THREADS
+    s = fn_path((rk_ctx*)ctx, &L, &T, &d, (const int32_t*)p[0], (int32_t)len, (const int32_t*)p[1], (int32_t*)p[2], stream);
+    Py_END_ALLOW_THREADS
+    return answer(s);
+}
+
 // bind(Layout, Text, addresses of the four entry points)
 PyObject* py_bind(PyObject*, PyObject* args)
 {
@@ -257,7 +361,30 @@ PyObject* py_bind(PyObject*, PyObject* args)
     Py_RETURN_NONE;
 }
 
+// bind_drafts(Drafts, addresses of the five entry points)
+PyObject* py_bind_drafts(PyObject*, PyObject* args)
+{
+    PyObject* dt;
+    unsigned long long f[5];
+    if (!PyArg_ParseTuple(args, "O!KKKKK", &PyType_Type, &dt, f, f + 1, f + 2, f + 3, f + 4)) return nullptr;
+    Py_INCREF(dt);
+    Py_XDECREF((PyObject*)drafts_type);
+    drafts_type = (PyTypeObject*)dt;
+    fn_append_quant = (append_quant_fn)(uintptr_t)f[0];
+    fn_decode_quant = (dual_fn)(uintptr_t)f[1];
+    fn_tree = (tree_fn)(uintptr_t)f[2];
+    fn_tree_quant = (tree_fn)(uintptr_t)f[3];
+    fn_path = (path_fn)(uintptr_t)f[4];
+    Py_RETURN_NONE;
+}
+
 PyMethodDef methods[] = {
+    {"bind_drafts", py_bind_drafts, METH_VARARGS, "bind_drafts(Drafts, five entry point addresses)"},
+    {"append_quant", (PyCFunction)(void (*)(void))py_append_quant, METH_FASTCALL, "rk_append_quant; its status, or None for arguments not taken here"},
+    {"decode_quant", (PyCFunction)(void (*)(void))py_decode_quant, METH_FASTCALL, "rk_decode_attn_quant, likewise"},
+    {"tree", (PyCFunction)(void (*)(void))py_tree, METH_FASTCALL, "rk_decode_attn_tree, likewise"},
+    {"tree_quant", (PyCFunction)(void (*)(void))py_tree_quant, METH_FASTCALL, "rk_decode_attn_tree_quant, likewise"},
+    {"append_path", (PyCFunction)(void (*)(void))py_append_path, METH_FASTCALL, "rk_append_text_path, likewise"},
     {"bind", py_bind, METH_VARARGS, "bind(Layout, Text, four entry point addresses)"},
     {"decode", (PyCFunction)(void (*)(void))py_decode, METH_FASTCALL, "rk_decode_attn; its status, or None for arguments not taken here"},
     {"append_decode", (PyCFunction)(void (*)(void))py_append_decode, METH_FASTCALL, "rk_append_decode_attn, likewise"},
@@ -276,7 +403,8 @@ PyMODINIT_FUNC PyInit__rkbind(void)
         {&s_batch, "batch"}, {&s_nq, "n_q_heads"}, {&s_nkv, "n_kv_heads"}, {&s_hd, "head_dim"}, {&s_keep, "keep"}, {&s_dtype, "dtype"},
         {&s_cap, "capacity"}, {&s_max_seq, "max_seq_len"}, {&s_seq, "seq_len"}, {&s_data_ptr, "data_ptr"}, {&s_numel, "numel"},
         {&s_esize, "element_size"}, {&s_cuda_stream, "cuda_stream"}, {&s_k, "k"}, {&s_v, "v"}, {&s_max_len, "max_len"}, {&s_len, "len"},
-        {&s_strides, "strides"}, {&s_stride, "stride"}, {&s_shape, "shape"}};
+        {&s_strides, "strides"}, {&s_stride, "stride"}, {&s_shape, "shape"},
+        {&s_n_tokens, "n_tokens"}, {&s_n_tokens_dev, "n_tokens_dev"}, {&s_mask, "mask"}};
     for (auto& x : names)
         if (!(*x.at = PyUnicode_InternFromString(x.text))) return nullptr;
     return PyModule_Create(&module);
