@@ -129,6 +129,8 @@ struct BlockState {
 
 // TG tiles of the cache on their way into LDS: [tile][octet][token] and, BLOCK_V behind, [tile][channel block][step][lane].  A wave's pieces lie in
 // one tile each, so that an address is a uniform base and an offset that never changes.
+template <int TG>
+__device__ __forceinline__ int tile_of(int s, int t, int last) { return TG == 1 ? s : min(TG * s + t, last); }
 template <int FMT, int R, int TG> struct CacheStage;
 template <int R, int TG>
 struct CacheStage<ROWS_BF16, R, TG> {
@@ -140,10 +142,10 @@ struct CacheStage<ROWS_BF16, R, TG> {
 #pragma unroll
         for (int j = 0; j < NK; ++j) {           // piece: [tile][octet][token]
             const int tile = min((BLOCK_NT * j + 64 * wave) / (4 * R), TG - 1), p = (BLOCK_NT * j + tid) % (4 * R), m = p & 31, o = p >> 5;
-            k[j] = *(const uint4*)(Ku + (size_t)min(TG * s + tile, last) * (64 * rp) + (uint32_t)((m >> 4) * (32 * rp) + (8 * o < rp ? o : 0) * 256 + (m & 15) * 16));
+            k[j] = *(const uint4*)(Ku + (size_t)tile_of<TG>(s, tile, last) * (64 * rp) + (uint32_t)((m >> 4) * (32 * rp) + (8 * o < rp ? o : 0) * 256 + (m & 15) * 16));
         }
 #pragma unroll
-        for (int j = 0; j < 2 * TG; ++j) v[j] = *(const uint4*)(Vu + (size_t)min(TG * s + (j >> 1), last) * 8192 + (uint32_t)((j & 1) * 4096 + tid * 16));
+        for (int j = 0; j < 2 * TG; ++j) v[j] = *(const uint4*)(Vu + (size_t)tile_of<TG>(s, j >> 1, last) * 8192 + (uint32_t)((j & 1) * 4096 + tid * 16));
     }
     // `left`: tokens of the stage that exist; Values behind them may be anything
     __device__ __forceinline__ void store(char* buf, float*, int left, int tid)
@@ -179,11 +181,11 @@ struct CacheStage<ROWS_Q8_BF16, R, TG> {
 #pragma unroll
         for (int j = 0; j < NK; ++j) {           // piece: [tile][octet][token n, and 16 + n]
             const int tile = min((BLOCK_NT * j + 64 * wave) / (2 * R), TG - 1), p = (BLOCK_NT * j + tid) % (2 * R), n = p & 15, o = p >> 4;
-            k[j] = *(const uint4*)(Ku + (size_t)min(TG * s + tile, last) * kblk + (uint32_t)((8 * o < rp ? o : 0) * 256 + n * 16));
+            k[j] = *(const uint4*)(Ku + (size_t)tile_of<TG>(s, tile, last) * kblk + (uint32_t)((8 * o < rp ? o : 0) * 256 + n * 16));
         }
 #pragma unroll
-        for (int j = 0; j < TG; ++j) v[j] = *(const uint4*)(Vu + (size_t)min(TG * s + j, last) * 4096 + (uint32_t)(tid * 16));
-        const int a = min(TG * s, last), b = min(TG * s + TG - 1, last);
+        for (int j = 0; j < TG; ++j) v[j] = *(const uint4*)(Vu + (size_t)tile_of<TG>(s, j, last) * 4096 + (uint32_t)(tid * 16));
+        const int a = TG * s, b = tile_of<TG>(s, TG - 1, last);
         step = *(const uint32_t*)(Ku + (size_t)a * kblk + (uint32_t)(32 * rp + (tid & 32 ? (b - a) * (int)kblk : 0) + (tid & 31) * 4));
     }
     // `left`: tokens of the stage that exist
@@ -204,6 +206,7 @@ struct CacheStage<ROWS_Q8_BF16, R, TG> {
             *(uint4*)(to + value_place(2 * cp, g, n)) = __builtin_bit_cast(uint4, codes_bf16(v[j].x, v[j].y));
             *(uint4*)(to + value_place(2 * cp + 1, g, n)) = __builtin_bit_cast(uint4, codes_bf16(v[j].z, v[j].w));
         }
+        asm volatile("" : "+v"(step));             // (waited for by all: a load that only some wait for is waited for with all others, later)
         if (tid < 32 * TG) {
             steps[tid] = __uint_as_float(step << 16);
             steps[64 + tid] = tid < left ? __uint_as_float(step & 0xffff0000u) : 0.f;
@@ -321,7 +324,7 @@ __global__ __launch_bounds__(BLOCK_NT, 2) void attn_block(RowsArgs A)
         if (block * 32 * RW >= live * A.G) return;
         const bool active = row0 < live * A.G;                     // (a wave without rows helps with the staging)
         constexpr int DEPTH = CacheStage<FMT, R, TG>::DEPTH;
-        const int len = min(max(A.seq_len[b], 0), A.cap), stages = (len + 32 * TG - 1) / (32 * TG), last = (len + 31) / 32 - 1;
+        const int len = __builtin_amdgcn_readfirstlane(min(max(A.seq_len[b], 0), A.cap)), stages = (len + 32 * TG - 1) / (32 * TG), last = (len + 31) / 32 - 1;
         const int s0 = (int)((int64_t)stages * split / A.Sv), s1 = (int)((int64_t)stages * (split + 1) / A.Sv);
         const size_t slab = slab_tokens(A.cap);
         const char* Ku = (const char*)A.Kc + (Q8 ? (size_t)u * (slab / 32) * q8_kblock(A.rp) : (size_t)u * slab * A.rp * 2);
@@ -329,7 +332,10 @@ __global__ __launch_bounds__(BLOCK_NT, 2) void attn_block(RowsArgs A)
         if (s0 < s1) {
             CacheStage<FMT, R, TG> X[DEPTH];
 #pragma unroll
-            for (int k = 0; k < DEPTH; ++k) X[k].load(Ku, Vu, min(s0 + k, s1 - 1), last, A.rp, tid, wave);
+            for (int k = 0; k < DEPTH; ++k) {
+                X[k].load(Ku, Vu, min(s0 + k, s1 - 1), last, A.rp, tid, wave);
+                __builtin_amdgcn_sched_barrier(0);                 // (in this order, as the loop's waits count them)
+            }
             // R_r^T as A operands, head and remainder, in LDS; then this wave's rows of q R_r
 #pragma unroll
             for (int w = 0; w < NF; ++w) {
