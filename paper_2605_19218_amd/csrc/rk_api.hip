@@ -293,22 +293,26 @@ DecodePlan decode_plan(const rk_ctx* ctx, const rk_layout* L, int text_rows = 0)
 }
 
 // Attention of T query tokens a sequence: row blocks of a KV head, splits of the cache and of the full-width rows.
-struct RowsPlan { int nrb16, nrb, Sv, Sr; bool fold; };
-int rows_per_block(const rk_layout* L, int T)       // in sixteens; fp32 rows take twice the registers
+struct RowsPlan { int per, nrb, Sv, Sr; };
+// Rows of a work-group.  16 of them leave every wave to its own tokens (attn_rows), which reads the cache once for each 16; 128 (64) share what is staged in LDS
+// (attn_block; bf16 rows alone: fp32 rows would take twice the registers).  While the 16s fit beside each other on the device and the tokens are few, reading
+// again from the L2 costs less than staging, waves without rows and steps behind barriers.  us with 16 / 64 / 128 rows a work-group, r = 64, bf16: 8 units x 1000
+// tokens, 128 rows 13.2 / 17.3 / 17.8; 8 x 16000, 96 26.4 / 35.3 / 29.6, 128 32.7 / 37.0 / 32.2; 32 x 2000, 128 21.0 / 32.0 / 27.0; 32 x 8000, 32
+// 27.4 / 38.8 / 32.0, 96 56.0 / 54.0 / 43.7; 256 x 600, 32 25.2 / 35.6 / 29.2, 64 45.9 / 42.7 / 36.6; over 8 bits: 8 x 16000, 40 21.5 / 24.3 / 31.1, 96
+// 36.3 / 34.8 / 34.8; 32 x 8000, 32 24.2 / 29.0 / 33.5, 64 38.9 / 36.6 / 43.0, 128 66.4 / 55.3 / 53.2; 128 x 2000, 64 42.6 / 38.1 / 47.1, 448 - / 169.6 /
+// 148.0.  (fp32 rows, 16 against 32 a work-group while there were such kernels: 8 x 16000, 32 35.6 / 41.5; 256 x 600, 32 67 / 58.5.)
+int rows_per_group(const rk_ctx* ctx, const rk_layout* L, int T, bool q8)
 {
-    const int64_t rows = (int64_t)T * (L->n_q_heads / L->n_kv_heads);
-    return rows <= 16 ? 1 : rows <= 32 || L->dtype == RK_F32 ? 2 : rows <= 64 ? 4 : 8;
-}
-int64_t row_blocks(const rk_layout* L, int T)
-{
-    const int64_t rows = (int64_t)T * (L->n_q_heads / L->n_kv_heads), per = 16 * rows_per_block(L, T);
-    return (rows + per - 1) / per;
+    const int64_t rows = (int64_t)T * (L->n_q_heads / L->n_kv_heads), units = (int64_t)L->batch * L->n_kv_heads, n_cu = ctx ? ctx->n_cu : 256;
+    const int64_t blocks = (rows + 15) / 16 * units;
+    if (L->dtype == RK_F32 || rows <= 32 || (blocks <= 2 * n_cu && blocks * L->max_seq_len <= 2500 * n_cu)) return 16;
+    return q8 && rows <= 64 ? 64 : 128;
 }
 // partial slots of a row: what any length may take
 int rows_slots(const rk_ctx* ctx, const rk_layout* L, int T)
 {
-    const int64_t groups = row_blocks(L, T) * L->batch * L->n_kv_heads, n_cu = ctx ? ctx->n_cu : 256;
-    int64_t s = 2 * n_cu / groups;
+    const int64_t rows = (int64_t)T * (L->n_q_heads / L->n_kv_heads), n_cu = ctx ? ctx->n_cu : 256;
+    int64_t s = 2 * n_cu / ((rows + 127) / 128 * L->batch * L->n_kv_heads);
     s = s < 10 ? 10 : s > 64 ? 64 : s;
     if (ctx && ctx->decode_splits > 0 && s < ctx->decode_splits + 8) s = ctx->decode_splits + 8;
     return (int)s;
@@ -320,42 +324,41 @@ size_t rows_ws(const rk_ctx* ctx, const rk_layout* L, int T)
 }
 // The split counts whose launch comes out cheapest, in microseconds as measured: a work-group begins with some 6; a step of its loop (four waves and 32
 // tokens each; of the kernels of many rows 32 tokens with 128 rows, 64 with 64) takes, at r = 64, with 16 rows bf16 0.37, fp32 1.8, 8 bits 0.67 (fp32
-// rows 0.9), with 32 rows two to three times that, with many 0.72 and 1.2; a step of full-width rows 2 to 3, which is their latency.  All
-// work-groups of few rows cannot be faster than the device streams; of many rows two share a compute unit and each takes half as long again.  A
-// split more is a partial a row, written and read.  Measured with each count (us): one token over 8 bits, 8 units x 30000 / 8 tokens, r = 64: 8 splits 31.0, 16
-// 20.0, 32 15.1, 48 13.9; 16 x 8 units x 600, r = 128: 1 12.1, 2 13.4, 4 15.6; 32 drafts, 8 units x 4000: 8 25.8, 16 21.6, 24 21.4, 32 24.7; 64 drafts, 8 x
-// 1000: 4 21.3, 8 18.8, 16 22.8.
+// rows 0.9), with many 0.72 and 1.2; a step of full-width rows 2 to 3, which is their latency.  All work-groups of few rows cannot be faster than the
+// device streams; of many rows two share a compute unit and each takes half as long again.  A split more is a partial a row, written and read.  The
+// splits of full-width rows come last: they run beside the others while there is room for two work-groups a compute unit (of few rows), and behind them
+// otherwise.  Measured with each count (us): one token over 8 bits, 8 units x 30000 / 8 tokens, r = 64: 8 splits 31.0, 16 20.0, 32 15.1, 48 13.9; 16 x 8 units x
+// 600, r = 128: 1 12.1, 2 13.4, 4 15.6; 32 rows, 32 x 16000: 2 64.1, 3 50.4, 4 44.1, 6 52.9, 8 46.1; 8 x 16000: 8 18.0, 12 16.4, 16 16.4, 24 18.6; 448
+// rows over 8 bits, 32 x 16384: 2 291, 4 243, 6 264, 8 259.
 RowsPlan rows_plan(const rk_ctx* ctx, const rk_layout* L, int T, int text_rows, bool drafts, bool q8)
 {
     RowsPlan p;
-    p.nrb16 = rows_per_block(L, T);
-    p.nrb = (int)row_blocks(L, T);
-    const bool block = p.nrb16 >= 4, f32 = L->dtype == RK_F32;
-    const int64_t units = (int64_t)L->batch * L->n_kv_heads, groups = p.nrb * units;
-    const int64_t rows = (int64_t)T * (L->n_q_heads / L->n_kv_heads), in_block = rows < 16 * p.nrb16 ? rows : 16 * p.nrb16;
+    p.per = rows_per_group(ctx, L, T, q8);
+    const int64_t units = (int64_t)L->batch * L->n_kv_heads, rows = (int64_t)T * (L->n_q_heads / L->n_kv_heads);
+    p.nrb = (int)((rows + p.per - 1) / p.per);
+    const bool block = p.per > 16, f32 = L->dtype == RK_F32;
+    const int64_t groups = p.nrb * units;
     const int n_cu = ctx ? ctx->n_cu : 256, slots = rows_slots(ctx, L, T), n_wg = block ? 2 * n_cu : n_cu;
-    const int step = p.nrb16 == 8 ? 32 : p.nrb16 == 4 ? 64 : 128;
+    const int step = p.per == 128 ? 32 : p.per == 64 ? 64 : 128;
     const int nv = (L->max_seq_len + step - 1) / step;
     const int64_t text = text_rows;        // (its bound is the caller's, up to the largest int)
     const int nr = (int)(block ? (text + 63) / 64 + (drafts ? 1 : 0) : ((text + 31) / 32 + (drafts ? (T + 31) / 32 : 0) + 3) / 4);
-    const double wide = (keep_padded(L->keep) + D) / 192.0, two = p.nrb16 == 2 ? (f32 ? 1.9 : q8 ? 1.7 : 3.0) : 1.0;
-    const double tv = wide * (p.nrb16 == 8 ? 0.72 : p.nrb16 == 4 ? 1.2 : two * (q8 ? (f32 ? 0.9 : 0.67) : f32 ? 1.8 : 0.37));
+    const double wide = (keep_padded(L->keep) + D) / 192.0;
+    const double tv = wide * (p.per == 128 ? 0.72 : p.per == 64 ? 1.2 : q8 ? (f32 ? 0.9 : 0.67) : f32 ? 1.8 : 0.37);
     const double tr = block ? 3.0 : f32 ? 4.0 : 2.0;
     const double token = q8 ? keep_padded(L->keep) + D + 4 : (double)elem_size(L->dtype) * (keep_padded(L->keep) + D);
     const double stream = block ? 0.0 : (double)units * L->max_seq_len * token / 6.2e6;
-    auto folds = [&](int S) {
-        return !block && ctx && ctx->fuse_merge && ctx->xcd_deal_ok && S > 1 && units % 8 == 0 && groups <= DEC_COUNTERS && in_block * S <= 64;
-    };
     auto cost = [&](int sv, int sr) {
         const int S = sv + sr;
         const int64_t W = groups * S;
-        const double v = (nv + sv - 1) / sv * tv, r = sr ? (nr + sr - 1) / sr * tr : 0.0;
-        double loop = v > r ? v : r;
-        if (block && W > n_cu) loop *= 1.5;
-        loop = loop > stream ? loop + 0.35 * stream : stream + 0.35 * loop;
-        const double rounds = (double)((groups * sv + n_wg - 1) / n_wg) + (W > n_wg ? 0.3 : 0.0);
-        const double merge = S == 1 ? 0.0 : folds(S) ? 1.5 : 2.5 + S / 32.0 + (double)rows * units * S * 1040 / 5e6;
-        return (6.0 + loop) * (W > n_wg ? rounds : 1.0) + merge;
+        const double shared = block && W > n_cu ? 1.5 : 1.0;
+        double v = (nv + sv - 1) / sv * tv * shared, r = sr ? (nr + sr - 1) / sr * tr * shared : 0.0, behind = 0.0;
+        v = v > stream ? v + 0.35 * stream : stream + 0.35 * v;
+        const int64_t rounds = (groups * sv + n_wg - 1) / n_wg;
+        if (W > rounds * n_wg) behind = !block && W <= 2 * n_cu ? 0.2 * r : 6.0 + r;
+        else if (rounds == 1 && r > v) v = r;
+        const double merge = S == 1 ? 0.0 : 2.5 + S / 32.0 + (double)rows * units * S * 1040 / 5e6;
+        return (6.0 + v) * rounds + behind + merge;
     };
     const int most_v = nv < 1 ? 1 : nv < 48 ? nv : 48, r0 = nr ? 1 : 0, r1 = nr < slots / 2 ? nr : slots / 2;
     static const int tries[] = {1, 2, 3, 4, 5, 6, 7, 8, 10, 12, 14, 16, 20, 24, 28, 32, 40, 48};
@@ -363,19 +366,16 @@ RowsPlan rows_plan(const rk_ctx* ctx, const rk_layout* L, int T, int text_rows, 
     p.Sv = 1;
     p.Sr = r0;
     for (int r = r0; r <= r1 && r <= 8; r += r < 4 ? 1 : 2) {
-        const int64_t full = n_wg / groups - r;        // what fills the device
         auto look = [&](int64_t v) {
             if (v < 1 || v > most_v || v > slots - r) return;
             const double c = cost((int)v, r);
             if (c < best - 0.01) { best = c; p.Sv = (int)v; p.Sr = r; }
         };
         for (int v : tries) look(v);
-        look(full);
+        look(n_wg / groups - r);            // what fills the device
+        look(n_wg / groups);                // without the full-width rows
     }
     if (ctx && ctx->decode_splits > 0) p.Sv = ctx->decode_splits < slots - p.Sr ? ctx->decode_splits : slots - p.Sr;
-    // The partials of a row block folded by its last work-group: where the units fill the XCDs evenly, and what one work-group then reads is
-    // little (the merge launch spreads it over the device).
-    p.fold = folds(p.Sv + p.Sr);
     return p;
 }
 
@@ -1057,12 +1057,11 @@ static rk_status rows_common(rk_ctx* ctx, const rk_layout* L, const void* q, con
     const size_t slots = (size_t)a.B * T * a.Hq * (p.Sv + p.Sr);
     a.ws_acc = (float*)align_up((uintptr_t)workspace, 256); a.ws_m = a.ws_acc + slots * D; a.ws_l = a.ws_m + slots;
     a.max_len = L->max_seq_len;
-    a.done = p.fold ? ctx->tickets + APP_TICKETS : nullptr;
     hipStream_t st = as_stream(stream);
-    e = L->dtype == RK_F32 ? (q8 ? launch_rows_q8_f32(a, p.nrb16, st) : launch_rows_f32(a, p.nrb16, st))
-                           : (q8 ? launch_rows_q8_bf16(a, p.nrb16, st) : launch_rows_bf16(a, p.nrb16, st));
+    e = L->dtype == RK_F32 ? (q8 ? launch_rows_q8_f32(a, p.per, st) : launch_rows_f32(a, p.per, st))
+                           : (q8 ? launch_rows_q8_bf16(a, p.per, st) : launch_rows_bf16(a, p.per, st));
     if (e != hipSuccess) return hip_fail(ctx, e, "attention launch");
-    if (p.Sv + p.Sr > 1 && !p.fold) {
+    if (p.Sv + p.Sr > 1) {
         e = launch_rows_merge(L->dtype, a, st);
         if (e != hipSuccess) return hip_fail(ctx, e, "attention merge launch");
     }

@@ -128,46 +128,47 @@ struct BlockState {
 };
 
 // TG tiles of the cache on their way into LDS: [tile][octet][token] and, BLOCK_V behind, [tile][channel block][step][lane].  A wave's pieces lie in
-// one tile each, so that an address is a uniform base and an offset that never changes.
+// one tile each, so that an address is a uniform base and an offset that never changes.  (`last`: the sequence's last tile, taken instead of one
+// behind it.)
 template <int TG>
 __device__ __forceinline__ int tile_of(int s, int t, int last) { return TG == 1 ? s : min(TG * s + t, last); }
 template <int FMT, int R, int TG> struct CacheStage;
-template <int R, int TG>
-struct CacheStage<ROWS_BF16, R, TG> {
-    static constexpr int KP = TG * 4 * R, NK = (KP + BLOCK_NT - 1) / BLOCK_NT, DEPTH = TG == 2 || R > 96 ? 2 : 3;
-    uint4 k[NK], v[2 * TG];
-    // tiles TG s ..+TG-1 of the sequence (`last`: its last tile, taken instead of one behind it)
-    __device__ __forceinline__ void load(const char* Ku, const char* Vu, int s, int last, int rp, int tid, int wave)
+template <int R>
+struct CacheStage<ROWS_BF16, R, 1> {
+    static constexpr int KP = 4 * R, NK = (KP + BLOCK_NT - 1) / BLOCK_NT, DEPTH = R > 96 ? 2 : 3;
+    uint4 k[NK], v[2];
+    // tile s of the sequence
+    __device__ __forceinline__ void load(const char* Ku, const char* Vu, int s, int, int rp, int tid, int)
     {
 #pragma unroll
-        for (int j = 0; j < NK; ++j) {           // piece: [tile][octet][token]
-            const int tile = min((BLOCK_NT * j + 64 * wave) / (4 * R), TG - 1), p = (BLOCK_NT * j + tid) % (4 * R), m = p & 31, o = p >> 5;
-            k[j] = *(const uint4*)(Ku + (size_t)tile_of<TG>(s, tile, last) * (64 * rp) + (uint32_t)((m >> 4) * (32 * rp) + (8 * o < rp ? o : 0) * 256 + (m & 15) * 16));
+        for (int j = 0; j < NK; ++j) {           // piece: [octet][token]
+            const int p = (BLOCK_NT * j + tid) % KP, m = p & 31, o = p >> 5;
+            k[j] = *(const uint4*)(Ku + (size_t)s * (64 * rp) + (uint32_t)((m >> 4) * (32 * rp) + (8 * o < rp ? o : 0) * 256 + (m & 15) * 16));
         }
 #pragma unroll
-        for (int j = 0; j < 2 * TG; ++j) v[j] = *(const uint4*)(Vu + (size_t)tile_of<TG>(s, j >> 1, last) * 8192 + (uint32_t)((j & 1) * 4096 + tid * 16));
+        for (int j = 0; j < 2; ++j) v[j] = *(const uint4*)(Vu + (size_t)s * 8192 + (uint32_t)(j * 4096 + tid * 16));
     }
-    // `left`: tokens of the stage that exist; Values behind them may be anything
+    // `left`: tokens of the tile that exist; Values behind them may be anything
     __device__ __forceinline__ void store(char* buf, float*, int left, int tid)
     {
 #pragma unroll
         for (int j = 0; j < NK; ++j)
             if (BLOCK_NT * (j + 1) <= KP || BLOCK_NT * j + tid < KP) *(uint4*)(buf + (BLOCK_NT * j + tid) * 16) = k[j];
         const int n = tid & 15, g = (tid >> 4) & 3;
-        if (left < 32 * TG) {
+        if (left < 32) {
 #pragma unroll
-            for (int j = 0; j < 2 * TG; ++j) {
+            for (int j = 0; j < 2; ++j) {
                 uint32_t x[4] = {v[j].x, v[j].y, v[j].z, v[j].w};
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const int t = 32 * (j >> 1) + 16 * (i >> 1) + 4 * g + 2 * (i & 1);
+                    const int t = 16 * (i >> 1) + 4 * g + 2 * (i & 1);
                     x[i] &= t + 1 < left ? ~0u : t < left ? 0xffffu : 0u;
                 }
                 v[j] = make_uint4(x[0], x[1], x[2], x[3]);
             }
         }
 #pragma unroll
-        for (int j = 0; j < 2 * TG; ++j) *(uint4*)(buf + BLOCK_V + (j >> 1) * 8192 + value_place(4 * (j & 1) + (tid >> 6), g, n)) = v[j];
+        for (int j = 0; j < 2; ++j) *(uint4*)(buf + BLOCK_V + value_place(4 * j + (tid >> 6), g, n)) = v[j];
     }
 };
 template <int R, int TG>
@@ -586,21 +587,24 @@ static hipError_t launch_block_rw(dim3 grid, const RowsArgs& a, hipStream_t st)
     attn_block<FMT, R, RW><<<grid, BLOCK_NT, BLOCK_LDS, st>>>(a);
     return hipGetLastError();
 }
+// rows: of a work-group, 128, or over the 8-bit cache 64
 template <int FMT, int R>
-static hipError_t launch_block_r(int nrb16, dim3 grid, const RowsArgs& a, hipStream_t st)
+static hipError_t launch_block_r(int rows, dim3 grid, const RowsArgs& a, hipStream_t st)
 {
-    return nrb16 == 4 ? launch_block_rw<FMT, R, 2>(grid, a, st) : launch_block_rw<FMT, R, 4>(grid, a, st);
+    if constexpr (FMT == ROWS_Q8_BF16)
+        if (rows == 64) return launch_block_rw<FMT, R, 2>(grid, a, st);
+    return launch_block_rw<FMT, R, 4>(grid, a, st);
 }
 template <int FMT>
-static hipError_t launch_block_fmt(const RowsArgs& a, int nrb16, hipStream_t st)
+static hipError_t launch_block_fmt(const RowsArgs& a, int rows, hipStream_t st)
 {
     const dim3 grid = rows_grid(a);
     if (!grid.x) return hipErrorInvalidValue;
     switch ((a.r + 31) / 32) {
-        case 1: return launch_block_r<FMT, 32>(nrb16, grid, a, st);
-        case 2: return launch_block_r<FMT, 64>(nrb16, grid, a, st);
-        case 3: return launch_block_r<FMT, 96>(nrb16, grid, a, st);
-        default: return launch_block_r<FMT, 128>(nrb16, grid, a, st);
+        case 1: return launch_block_r<FMT, 32>(rows, grid, a, st);
+        case 2: return launch_block_r<FMT, 64>(rows, grid, a, st);
+        case 3: return launch_block_r<FMT, 96>(rows, grid, a, st);
+        default: return launch_block_r<FMT, 128>(rows, grid, a, st);
     }
 }
 

@@ -4,7 +4,7 @@
 //   row (t, h) of KV head hk: x_c = q R_r . k~_c + q . delta_mu, x_m = q . k_m (text rows, and drafts that mask[t] names),
 //   out = softmax(scale x) . (V_c, V_m)       one softmax; a row that sees nothing: zeros.
 //
-// A KV head's T G rows share its Keys and Values, so a work-group takes 16 NRB rows (NRB matrix-core columns of 16) over one stretch of
+// A KV head's T G rows share its Keys and Values, so a work-group takes 16 rows (a matrix-core column each) over one stretch of
 // tokens, a wave 32 tokens at a time: every Key and Value is requested once for all the rows, straight into the registers that feed the matrix
 // cores, and nothing passes through LDS in the loop.  Both products are turned so that a lane keeps one row: S^T = K q^T leaves lane (g, n)
 // with row n's scores of tokens 4 g ..+3, which is how O^T = V^T P^T wants them as its B operand, and every accumulator of the lane belongs to row
@@ -60,56 +60,40 @@ __device__ __forceinline__ bf16x8 codes_bf16(uint32_t lo, uint32_t hi)
     return __builtin_bit_cast(bf16x8, make_uint4(d[0], d[1], d[2], d[3]));
 }
 
-// The softmax state of a wave: NRB blocks of 16 rows, row n of each in the lanes (., n).
-template <int NRB>
+// The softmax state of a wave: row n in the lanes (., n).
 struct RowState {
-    float m[NRB], l[NRB];        // log2 domain; l: this lane's tokens only, until the end
-    f32x4 O[NRB][8];
+    float m, l;                  // log2 domain; l: this lane's tokens only, until the end
+    f32x4 O[8];
     __device__ __forceinline__ void clear()
     {
+        m = ROWS_NEG_INF;
+        l = 0.f;
 #pragma unroll
-        for (int rb = 0; rb < NRB; ++rb) {
-            m[rb] = ROWS_NEG_INF;
-            l[rb] = 0.f;
-#pragma unroll
-            for (int cb = 0; cb < 8; ++cb) O[rb][cb] = (f32x4){0.f, 0.f, 0.f, 0.f};
-        }
+        for (int cb = 0; cb < 8; ++cb) O[cb] = (f32x4){0.f, 0.f, 0.f, 0.f};
     }
     // scores of 32 tokens -> weights
-    __device__ __forceinline__ void weigh(f32x4 (&s)[NRB][2])
+    __device__ __forceinline__ void weigh(f32x4 (&s)[2])
     {
-        float mt[NRB];
-        bool behind = false;
+        const float mt = groups_max(fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])),
+                                          fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3]))));
+        if (__any(mt > m + 8.f)) {
+            const float m_new = fmaxf(m, mt);
+            const float alpha = m > ROWS_NEG_INF ? rows_exp2(m - m_new) : 0.f;      // (0 . 0 before the first score)
+            l *= alpha;
 #pragma unroll
-        for (int rb = 0; rb < NRB; ++rb) {
-            mt[rb] = groups_max(fmaxf(fmaxf(fmaxf(s[rb][0][0], s[rb][0][1]), fmaxf(s[rb][0][2], s[rb][0][3])),
-                                      fmaxf(fmaxf(s[rb][1][0], s[rb][1][1]), fmaxf(s[rb][1][2], s[rb][1][3]))));
-            behind |= mt[rb] > m[rb] + 8.f;
+            for (int cb = 0; cb < 8; ++cb) O[cb] *= alpha;
+            m = m_new;
         }
-        if (__any(behind)) {
+        const float ref = m > ROWS_NEG_INF ? m : 0.f;         // every score so far may be minus infinity: no weight, not NaN
+        float sum = 0.f;
 #pragma unroll
-            for (int rb = 0; rb < NRB; ++rb) {
-                const float m_new = fmaxf(m[rb], mt[rb]);
-                const float alpha = m[rb] > ROWS_NEG_INF ? rows_exp2(m[rb] - m_new) : 0.f;      // (0 . 0 before the first score)
-                l[rb] *= alpha;
+        for (int tb = 0; tb < 2; ++tb)
 #pragma unroll
-                for (int cb = 0; cb < 8; ++cb) O[rb][cb] *= alpha;
-                m[rb] = m_new;
+            for (int ii = 0; ii < 4; ++ii) {
+                s[tb][ii] = rows_exp2(s[tb][ii] - ref);
+                sum += s[tb][ii];
             }
-        }
-#pragma unroll
-        for (int rb = 0; rb < NRB; ++rb) {
-            const float ref = m[rb] > ROWS_NEG_INF ? m[rb] : 0.f;         // every score so far may be minus infinity: no weight, not NaN
-            float sum = 0.f;
-#pragma unroll
-            for (int tb = 0; tb < 2; ++tb)
-#pragma unroll
-                for (int ii = 0; ii < 4; ++ii) {
-                    s[rb][tb][ii] = rows_exp2(s[rb][tb][ii] - ref);
-                    sum += s[rb][tb][ii];
-                }
-            l[rb] += sum;
-        }
+        l += sum;
     }
 };
 
@@ -179,52 +163,46 @@ struct TileF32 {
 };
 
 // The rotated queries as B operands, and what a tile does with them.
-template <int FMT, int R, int NRB>
+template <int FMT, int R>
 struct CacheRows {
     static constexpr bool Q8 = FMT >= ROWS_Q8_BF16, F32 = FMT == ROWS_F32;
     static constexpr int NP = FMT == ROWS_Q8_F32 ? 3 : 2, KS = R / 32;
-    bf16x8 qf[F32 ? 1 : NRB][F32 ? 1 : KS][NP];
-    f32x4 q4[F32 ? NRB : 1][F32 ? R / 16 : 1];
+    bf16x8 qf[F32 ? 1 : KS][NP];
+    f32x4 q4[F32 ? R / 16 : 1];
 
-    // qt: [16 NRB][R + 4] of LDS
+    // qt: [16][R + 4] of LDS
     __device__ __forceinline__ void take(const float* qt, float scale_log2, int g, int n)
     {
+        const float* row = qt + n * (R + 4);
+        if constexpr (F32) {
 #pragma unroll
-        for (int rb = 0; rb < NRB; ++rb) {
-            const float* row = qt + (16 * rb + n) * (R + 4);
-            if constexpr (F32) {
+            for (int i = 0; i < R / 16; ++i) q4[i] = *(const f32x4*)(row + 16 * i + 4 * g) * scale_log2;
+        } else {
 #pragma unroll
-                for (int i = 0; i < R / 16; ++i) q4[rb][i] = *(const f32x4*)(row + 16 * i + 4 * g) * scale_log2;
-            } else {
-#pragma unroll
-                for (int i = 0; i < KS; ++i) {
-                    const f32x4 a = *(const f32x4*)(row + 32 * i + 8 * g) * scale_log2, b = *(const f32x4*)(row + 32 * i + 8 * g + 4) * scale_log2;
-                    const float x[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-                    parts_of<NP>(x, qf[rb][i]);
-                }
+            for (int i = 0; i < KS; ++i) {
+                const f32x4 a = *(const f32x4*)(row + 32 * i + 8 * g) * scale_log2, b = *(const f32x4*)(row + 32 * i + 8 * g + 4) * scale_log2;
+                const float x[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+                parts_of<NP>(x, qf[i]);
             }
         }
     }
 
     // `left`: tokens of the tile that exist
-    __device__ __forceinline__ void step(TileF32<R>& T, RowState<NRB>& st, int left, int rp, int g)
+    __device__ __forceinline__ void step(TileF32<R>& T, RowState& st, int left, int rp, int g)
     {
-        f32x4 s[NRB][2];
+        f32x4 s[2];
         if (rp < R) {
 #pragma unroll
             for (int tb = 0; tb < 2; ++tb) T.k[tb][R / 16 - 1] = (f32x4){0.f, 0.f, 0.f, 0.f};
         }
 #pragma unroll
         for (int tb = 0; tb < 2; ++tb) {
-#pragma unroll
-            for (int rb = 0; rb < NRB; ++rb) s[rb][tb] = (f32x4){0.f, 0.f, 0.f, 0.f};
+            s[tb] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < R / 16; ++i)
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-#pragma unroll
-                    for (int rb = 0; rb < NRB; ++rb)
-                        s[rb][tb] = __builtin_amdgcn_mfma_f32_16x16x4f32(T.k[tb][i][e], q4[rb][i][e], s[rb][tb], 0, 0, 0);
+                    s[tb] = __builtin_amdgcn_mfma_f32_16x16x4f32(T.k[tb][i][e], q4[i][e], s[tb], 0, 0, 0);
         }
         if (left < 32) {
 #pragma unroll
@@ -232,8 +210,7 @@ struct CacheRows {
 #pragma unroll
                 for (int ii = 0; ii < 4; ++ii) {
                     const bool in = 16 * tb + 4 * g + ii < left;
-#pragma unroll
-                    for (int rb = 0; rb < NRB; ++rb) s[rb][tb][ii] = in ? s[rb][tb][ii] : ROWS_NEG_INF;
+                    s[tb][ii] = in ? s[tb][ii] : ROWS_NEG_INF;
 #pragma unroll
                     for (int cb = 0; cb < 8; ++cb) T.v[cb][tb][ii] = in ? T.v[cb][tb][ii] : 0.f;
                 }
@@ -245,29 +222,24 @@ struct CacheRows {
             for (int tb = 0; tb < 2; ++tb)
 #pragma unroll
                 for (int ii = 0; ii < 4; ++ii)
-#pragma unroll
-                    for (int rb = 0; rb < NRB; ++rb)
-                        st.O[rb][cb] = __builtin_amdgcn_mfma_f32_16x16x4f32(T.v[cb][tb][ii], s[rb][tb][ii], st.O[rb][cb], 0, 0, 0);
+                    st.O[cb] = __builtin_amdgcn_mfma_f32_16x16x4f32(T.v[cb][tb][ii], s[tb][ii], st.O[cb], 0, 0, 0);
     }
 
-    __device__ __forceinline__ void step(TileBf16<R>& T, RowState<NRB>& st, int left, int rp, int g)
+    __device__ __forceinline__ void step(TileBf16<R>& T, RowState& st, int left, int rp, int g)
     {
-        f32x4 s[NRB][2];
+        f32x4 s[2];
         if (rp < R && g >= 2) {
 #pragma unroll
             for (int tb = 0; tb < 2; ++tb) T.k[tb][KS - 1] = make_uint4(0, 0, 0, 0);
         }
 #pragma unroll
         for (int tb = 0; tb < 2; ++tb) {
-#pragma unroll
-            for (int rb = 0; rb < NRB; ++rb) s[rb][tb] = (f32x4){0.f, 0.f, 0.f, 0.f};
+            s[tb] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < KS; ++i)
 #pragma unroll
                 for (int p = NP - 1; p >= 0; --p)
-#pragma unroll
-                    for (int rb = 0; rb < NRB; ++rb)
-                        s[rb][tb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, T.k[tb][i]), qf[rb][i][p], s[rb][tb], 0, 0, 0);
+                    s[tb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, T.k[tb][i]), qf[i][p], s[tb], 0, 0, 0);
         }
         if (left < 32) {
 #pragma unroll
@@ -275,8 +247,7 @@ struct CacheRows {
 #pragma unroll
                 for (int ii = 0; ii < 4; ++ii) {
                     const bool in = 16 * tb + 4 * g + ii < left;
-#pragma unroll
-                    for (int rb = 0; rb < NRB; ++rb) s[rb][tb][ii] = in ? s[rb][tb][ii] : ROWS_NEG_INF;
+                    s[tb][ii] = in ? s[tb][ii] : ROWS_NEG_INF;
                     const uint32_t keep = in ? ~0u : (ii & 1 ? 0x0000ffffu : 0xffff0000u);
 #pragma unroll
                     for (int cb = 0; cb < 8; ++cb) {
@@ -286,35 +257,28 @@ struct CacheRows {
                 }
         }
         st.weigh(s);
-        bf16x8 p[NRB][2];
-#pragma unroll
-        for (int rb = 0; rb < NRB; ++rb) {
-            const float x[8] = {s[rb][0][0], s[rb][0][1], s[rb][0][2], s[rb][0][3], s[rb][1][0], s[rb][1][1], s[rb][1][2], s[rb][1][3]};
-            parts_of<2>(x, p[rb]);
-        }
+        bf16x8 p[2];
+        const float x[8] = {s[0][0], s[0][1], s[0][2], s[0][3], s[1][0], s[1][1], s[1][2], s[1][3]};
+        parts_of<2>(x, p);
 #pragma unroll
         for (int cb = 0; cb < 8; ++cb)
 #pragma unroll
             for (int k = 1; k >= 0; --k)
-#pragma unroll
-                for (int rb = 0; rb < NRB; ++rb)
-                    st.O[rb][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, T.v[cb]), p[rb][k], st.O[rb][cb], 0, 0, 0);
+                st.O[cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, T.v[cb]), p[k], st.O[cb], 0, 0, 0);
     }
 
-    __device__ __forceinline__ void step(TileQ8<R>& T, RowState<NRB>& st, int left, int rp, int g)
+    __device__ __forceinline__ void step(TileQ8<R>& T, RowState& st, int left, int rp, int g)
     {
-        f32x4 s[NRB][2];
+        f32x4 s[2];
 #pragma unroll
         for (int tb = 0; tb < 2; ++tb) {
-#pragma unroll
-            for (int rb = 0; rb < NRB; ++rb) s[rb][tb] = (f32x4){0.f, 0.f, 0.f, 0.f};
+            s[tb] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < KS; ++i) {
                 const bf16x8 kf = tb ? codes_bf16(T.k[i].z, T.k[i].w) : codes_bf16(T.k[i].x, T.k[i].y);
 #pragma unroll
                 for (int p = NP - 1; p >= 0; --p)
-#pragma unroll
-                    for (int rb = 0; rb < NRB; ++rb) s[rb][tb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[rb][i][p], s[rb][tb], 0, 0, 0);
+                    s[tb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[i][p], s[tb], 0, 0, 0);
             }
         }
         // a token's step is a factor of its score, the Value's one of its weight
@@ -326,8 +290,7 @@ struct CacheRows {
                 const uint32_t w = ii == 0 ? T.st[tb].x : ii == 1 ? T.st[tb].y : ii == 2 ? T.st[tb].z : T.st[tb].w;
                 const float ks = __uint_as_float(w << 16);
                 vs[tb][ii] = __uint_as_float(w & 0xffff0000u);
-#pragma unroll
-                for (int rb = 0; rb < NRB; ++rb) s[rb][tb][ii] *= ks;
+                s[tb][ii] *= ks;
             }
         if (left < 32) {
 #pragma unroll
@@ -336,27 +299,22 @@ struct CacheRows {
                 for (int ii = 0; ii < 4; ++ii) {
                     const bool in = 16 * tb + 4 * g + ii < left;
                     vs[tb][ii] = in ? vs[tb][ii] : 0.f;
-#pragma unroll
-                    for (int rb = 0; rb < NRB; ++rb) s[rb][tb][ii] = in ? s[rb][tb][ii] : ROWS_NEG_INF;
+                    s[tb][ii] = in ? s[tb][ii] : ROWS_NEG_INF;
                 }
         }
         st.weigh(s);
-        bf16x8 p[NRB][NP];
+        bf16x8 p[NP];
+        float x[8];
 #pragma unroll
-        for (int rb = 0; rb < NRB; ++rb) {
-            float x[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = s[rb][e >> 2][e & 3] * vs[e >> 2][e & 3];
-            parts_of<NP>(x, p[rb]);
-        }
+        for (int e = 0; e < 8; ++e) x[e] = s[e >> 2][e & 3] * vs[e >> 2][e & 3];
+        parts_of<NP>(x, p);
 #pragma unroll
         for (int cb = 0; cb < 8; ++cb) {
             const uint4 w = T.v[cb >> 1];
             const bf16x8 vf = cb & 1 ? codes_bf16(w.z, w.w) : codes_bf16(w.x, w.y);
 #pragma unroll
             for (int k = NP - 1; k >= 0; --k)
-#pragma unroll
-                for (int rb = 0; rb < NRB; ++rb) st.O[rb][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, p[rb][k], st.O[rb][cb], 0, 0, 0);
+                st.O[cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, p[k], st.O[cb], 0, 0, 0);
         }
     }
 };
@@ -384,16 +342,13 @@ __device__ __forceinline__ uint32_t tokens_of(uint32_t slots, int g)
     return __builtin_amdgcn_readfirstlane(t);
 }
 
-template <int NRB>
 struct PlainRowsBf16 {
-    bf16x8 qf[NRB][4];
+    bf16x8 qf[4];
     uint4 k[2][4], v[8];
-    __device__ __forceinline__ void take(const bf16_t* const (&qrow)[NRB], int g)
+    __device__ __forceinline__ void take(const bf16_t* qrow, int g)
     {
 #pragma unroll
-        for (int rb = 0; rb < NRB; ++rb)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) qf[rb][i] = *(const bf16x8*)(qrow[rb] + 32 * i + 8 * g);
+        for (int i = 0; i < 4; ++i) qf[i] = *(const bf16x8*)(qrow + 32 * i + 8 * g);
     }
     // rows r0 ..+31 of kp, vp; those from `rows` on repeat the last
     __device__ __forceinline__ void load(const bf16_t* kp, const bf16_t* vp, int64_t stride, int r0, int rows, int g, int n)
@@ -407,19 +362,15 @@ struct PlainRowsBf16 {
 #pragma unroll
         for (int jj = 0; jj < 8; ++jj) v[jj] = *(const uint4*)(vp + (int64_t)min(r0 + (jj < 4 ? 4 * g + jj : 12 + 4 * g + jj), rows - 1) * stride + 8 * n);
     }
-    __device__ __forceinline__ void scores(f32x4 (&s)[NRB][2], float scale_log2)
+    __device__ __forceinline__ void scores(f32x4 (&s)[2], float scale_log2)
     {
 #pragma unroll
         for (int tb = 0; tb < 2; ++tb) {
-#pragma unroll
-            for (int rb = 0; rb < NRB; ++rb) s[rb][tb] = (f32x4){0.f, 0.f, 0.f, 0.f};
+            s[tb] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int rb = 0; rb < NRB; ++rb)
-                    s[rb][tb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k[tb][i]), qf[rb][i], s[rb][tb], 0, 0, 0);
-#pragma unroll
-            for (int rb = 0; rb < NRB; ++rb) s[rb][tb] *= scale_log2;
+                s[tb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k[tb][i]), qf[i], s[tb], 0, 0, 0);
+            s[tb] *= scale_log2;
         }
     }
     __device__ __forceinline__ void drop(int jj)
@@ -472,34 +423,27 @@ struct PlainRowsBf16 {
         d.w = __builtin_amdgcn_perm(dword_of(v[7], cb >> 1), dword_of(v[6], cb >> 1), sel);
         return d;
     }
-    __device__ __forceinline__ void accumulate(const f32x4 (&s)[NRB][2], f32x4 (&O)[NRB][8]) const
+    __device__ __forceinline__ void accumulate(const f32x4 (&s)[2], f32x4 (&O)[8]) const
     {
-        bf16x8 p[NRB][2];
-#pragma unroll
-        for (int rb = 0; rb < NRB; ++rb) {
-            const float x[8] = {s[rb][0][0], s[rb][0][1], s[rb][0][2], s[rb][0][3], s[rb][1][0], s[rb][1][1], s[rb][1][2], s[rb][1][3]};
-            parts_of<2>(x, p[rb]);
-        }
+        bf16x8 p[2];
+        const float x[8] = {s[0][0], s[0][1], s[0][2], s[0][3], s[1][0], s[1][1], s[1][2], s[1][3]};
+        parts_of<2>(x, p);
 #pragma unroll
         for (int cb = 0; cb < 8; ++cb) {
             const bf16x8 vf = __builtin_bit_cast(bf16x8, column(cb));
 #pragma unroll
             for (int k2 = 1; k2 >= 0; --k2)
-#pragma unroll
-                for (int rb = 0; rb < NRB; ++rb) O[rb][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, p[rb][k2], O[rb][cb], 0, 0, 0);
+                O[cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, p[k2], O[cb], 0, 0, 0);
         }
     }
 };
 
-template <int NRB>
 struct PlainRowsF32 {
-    f32x4 qf[NRB][8], k[2][8], v[8][2];
-    __device__ __forceinline__ void take(const float* const (&qrow)[NRB], int g)
+    f32x4 qf[8], k[2][8], v[8][2];
+    __device__ __forceinline__ void take(const float* qrow, int g)
     {
 #pragma unroll
-        for (int rb = 0; rb < NRB; ++rb)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) qf[rb][i] = *(const f32x4*)(qrow[rb] + 16 * i + 4 * g);
+        for (int i = 0; i < 8; ++i) qf[i] = *(const f32x4*)(qrow + 16 * i + 4 * g);
     }
     __device__ __forceinline__ void load(const float* kp, const float* vp, int64_t stride, int r0, int rows, int g, int n)
     {
@@ -516,20 +460,17 @@ struct PlainRowsF32 {
             v[jj][1] = *(const f32x4*)(row + 4);
         }
     }
-    __device__ __forceinline__ void scores(f32x4 (&s)[NRB][2], float scale_log2)
+    __device__ __forceinline__ void scores(f32x4 (&s)[2], float scale_log2)
     {
 #pragma unroll
         for (int tb = 0; tb < 2; ++tb) {
-#pragma unroll
-            for (int rb = 0; rb < NRB; ++rb) s[rb][tb] = (f32x4){0.f, 0.f, 0.f, 0.f};
+            s[tb] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < 8; ++i)
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-#pragma unroll
-                    for (int rb = 0; rb < NRB; ++rb) s[rb][tb] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[tb][i][e], qf[rb][i][e], s[rb][tb], 0, 0, 0);
-#pragma unroll
-            for (int rb = 0; rb < NRB; ++rb) s[rb][tb] *= scale_log2;
+                    s[tb] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[tb][i][e], qf[i][e], s[tb], 0, 0, 0);
+            s[tb] *= scale_log2;
         }
     }
     __device__ __forceinline__ void drop(int jj)
@@ -567,34 +508,30 @@ struct PlainRowsF32 {
             return no_number(__float_as_uint(x)) ? x : 0.f;
         }
     };
-    __device__ __forceinline__ void accumulate(const f32x4 (&s)[NRB][2], f32x4 (&O)[NRB][8]) const
+    __device__ __forceinline__ void accumulate(const f32x4 (&s)[2], f32x4 (&O)[8]) const
     {
 #pragma unroll
         for (int cb = 0; cb < 8; ++cb)
 #pragma unroll
             for (int jj = 0; jj < 8; ++jj)
-#pragma unroll
-                for (int rb = 0; rb < NRB; ++rb)
-                    O[rb][cb] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[jj][cb >> 2][cb & 3], s[rb][jj >> 2][jj & 3], O[rb][cb], 0, 0, 0);
+                O[cb] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[jj][cb >> 2][cb & 3], s[jj >> 2][jj & 3], O[cb], 0, 0, 0);
     }
 };
 
-// q R_r of this work-group's rows into qt [16 NRB][R + 4], and q . delta_mu of row n of each block: D^T[j][row] = R_r^T . q^T, column blocks
+// q R_r of this work-group's rows into qt [16][R + 4], and q . delta_mu of row n of each block: D^T[j][row] = R_r^T . q^T, column blocks
 // of R_r shared by the waves.  q in bf16 is exact and R_r goes as head and remainder; in fp32 all of it is fp32.  load() asks for
 // everything, make() waits for it.
-template <typename T, int R, int NRB> struct Rotation;
-template <int R, int NRB>
-struct Rotation<bf16_t, R, NRB> {
+template <typename T, int R> struct Rotation;
+template <int R>
+struct Rotation<bf16_t, R> {
     static constexpr int NW = (R + 63) / 64;
-    bf16x8 qf[NRB][4];
+    bf16x8 qf[4];
     float x[NW][4][8];
     f32x4 dm[8];
-    __device__ __forceinline__ void load(const bf16_t* const (&qrow)[NRB], const float* Ru, const float* dp, int r, int wave, int g, int n)
+    __device__ __forceinline__ void load(const bf16_t* qrow, const float* Ru, const float* dp, int r, int wave, int g, int n)
     {
 #pragma unroll
-        for (int rb = 0; rb < NRB; ++rb)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) qf[rb][i] = *(const bf16x8*)(qrow[rb] + 32 * i + 8 * g);
+        for (int i = 0; i < 4; ++i) qf[i] = *(const bf16x8*)(qrow + 32 * i + 8 * g);
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
             const int j = min(16 * (wave + 4 * w) + n, r - 1);
@@ -606,53 +543,42 @@ struct Rotation<bf16_t, R, NRB> {
 #pragma unroll
         for (int i = 0; i < 8; ++i) dm[i] = *(const f32x4_any*)(dp + 32 * (i >> 1) + 8 * g + 4 * (i & 1));
     }
-    __device__ __forceinline__ void make(float* qt, float (&bias)[NRB], bool biased, int r, int wave, int g, int n)
+    __device__ __forceinline__ void make(float* qt, float& bias, bool biased, int r, int wave, int g, int n)
     {
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
             const int jb = wave + 4 * w;
             if (16 * jb >= R) break;
-            f32x4 acc[NRB];
-#pragma unroll
-            for (int rb = 0; rb < NRB; ++rb) acc[rb] = (f32x4){0.f, 0.f, 0.f, 0.f};
+            f32x4 acc = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) x[w][i][e] = 16 * jb + n < r ? x[w][i][e] : 0.f;
                 bf16x8 hi, lo;
                 split_bf16x8(x[w][i], hi, lo);
-#pragma unroll
-                for (int rb = 0; rb < NRB; ++rb) {
-                    acc[rb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lo, qf[rb][i], acc[rb], 0, 0, 0);
-                    acc[rb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(hi, qf[rb][i], acc[rb], 0, 0, 0);
-                }
+                acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lo, qf[i], acc, 0, 0, 0);
+                acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(hi, qf[i], acc, 0, 0, 0);
             }
-#pragma unroll
-            for (int rb = 0; rb < NRB; ++rb) *(f32x4*)(qt + (16 * rb + n) * (R + 4) + 16 * jb + 4 * g) = acc[rb];
+            *(f32x4*)(qt + n * (R + 4) + 16 * jb + 4 * g) = acc;
         }
+        bias = 0.f;
 #pragma unroll
-        for (int rb = 0; rb < NRB; ++rb) {
-            bias[rb] = 0.f;
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) bias[rb] = fmaf((float)qf[rb][i][e], dm[2 * i + (e >> 2)][e & 3], bias[rb]);
-            bias[rb] = biased ? groups_sum(bias[rb]) : 0.f;
-        }
+            for (int e = 0; e < 8; ++e) bias = fmaf((float)qf[i][e], dm[2 * i + (e >> 2)][e & 3], bias);
+        bias = biased ? groups_sum(bias) : 0.f;
     }
 };
-template <int R, int NRB>
-struct Rotation<float, R, NRB> {
+template <int R>
+struct Rotation<float, R> {
     static constexpr int NW = (R + 63) / 64;
-    f32x4 qf[NRB][8];
+    f32x4 qf[8];
     float x[NW][8][4];
     f32x4 dm[8];
-    __device__ __forceinline__ void load(const float* const (&qrow)[NRB], const float* Ru, const float* dp, int r, int wave, int g, int n)
+    __device__ __forceinline__ void load(const float* qrow, const float* Ru, const float* dp, int r, int wave, int g, int n)
     {
 #pragma unroll
-        for (int rb = 0; rb < NRB; ++rb)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) qf[rb][i] = *(const f32x4*)(qrow[rb] + 16 * i + 4 * g);
+        for (int i = 0; i < 8; ++i) qf[i] = *(const f32x4*)(qrow + 16 * i + 4 * g);
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
             const int j = min(16 * (wave + 4 * w) + n, r - 1);
@@ -664,34 +590,26 @@ struct Rotation<float, R, NRB> {
 #pragma unroll
         for (int i = 0; i < 8; ++i) dm[i] = *(const f32x4_any*)(dp + 16 * i + 4 * g);
     }
-    __device__ __forceinline__ void make(float* qt, float (&bias)[NRB], bool biased, int r, int wave, int g, int n)
+    __device__ __forceinline__ void make(float* qt, float& bias, bool biased, int r, int wave, int g, int n)
     {
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
             const int jb = wave + 4 * w;
             if (16 * jb >= R) break;
-            f32x4 acc[NRB];
-#pragma unroll
-            for (int rb = 0; rb < NRB; ++rb) acc[rb] = (f32x4){0.f, 0.f, 0.f, 0.f};
+            f32x4 acc = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < 8; ++i)
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-#pragma unroll
-                    for (int rb = 0; rb < NRB; ++rb)
-                        acc[rb] = __builtin_amdgcn_mfma_f32_16x16x4f32(16 * jb + n < r ? x[w][i][e] : 0.f, qf[rb][i][e], acc[rb], 0, 0, 0);
-#pragma unroll
-            for (int rb = 0; rb < NRB; ++rb) *(f32x4*)(qt + (16 * rb + n) * (R + 4) + 16 * jb + 4 * g) = acc[rb];
+                    acc = __builtin_amdgcn_mfma_f32_16x16x4f32(16 * jb + n < r ? x[w][i][e] : 0.f, qf[i][e], acc, 0, 0, 0);
+            *(f32x4*)(qt + n * (R + 4) + 16 * jb + 4 * g) = acc;
         }
+        bias = 0.f;
 #pragma unroll
-        for (int rb = 0; rb < NRB; ++rb) {
-            bias[rb] = 0.f;
+        for (int i = 0; i < 8; ++i)
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) bias[rb] = fmaf(qf[rb][i][e], dm[i][e], bias[rb]);
-            bias[rb] = biased ? groups_sum(bias[rb]) : 0.f;
-        }
+            for (int e = 0; e < 4; ++e) bias = fmaf(qf[i][e], dm[i][e], bias);
+        bias = biased ? groups_sum(bias) : 0.f;
     }
 };
 
@@ -701,16 +619,13 @@ __device__ __forceinline__ float partial_weight(float m, float l, float M)
     return l == 0.f ? 0.f : rows_exp2(m - (M > ROWS_NEG_INF ? M : 0.f));
 }
 
-// What another work-group of the launch wrote, past this compute unit's L1 (whose lines may be older).
-__device__ __forceinline__ float past_l1(const float* p) { return __hip_atomic_load(const_cast<float*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
-
 // Partials first, first + step, ... of the S of a row, by 32 lanes with four channels each: sum l_i w_i and sum acc_i w_i, w_i = 2^(m_i - M), M the maximum
 // of all S.  MC (up to eight) partials' loads at once.
-template <bool PAST_L1, int MC>
+template <int MC>
 __device__ __forceinline__ void merge_row(const float* m, const float* l, const float* acc, int S, int first, int step, int p, f32x4& num, float& sum)
 {
     float M = ROWS_NEG_INF;
-    for (int i = p; i < S; i += 32) M = fmaxf(M, PAST_L1 ? past_l1(m + i) : m[i]);
+    for (int i = p; i < S; i += 32) M = fmaxf(M, m[i]);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o));
     num = (f32x4){0.f, 0.f, 0.f, 0.f};
@@ -720,7 +635,7 @@ __device__ __forceinline__ void merge_row(const float* m, const float* l, const 
 #pragma unroll
         for (int k = 0; k < MC; ++k) av[k] = *(const f32x4*)(acc + (size_t)min(i0 + k * step, S - 1) * D + 4 * p);
         const int mine = i0 + (p & 7) * step, at = min(mine, S - 1);       // lane k of each eight: partial k's weight
-        const float mv = PAST_L1 ? past_l1(m + at) : m[at], lv = (p & 7) < MC && mine < S ? (PAST_L1 ? past_l1(l + at) : l[at]) : 0.f;
+        const float mv = m[at], lv = (p & 7) < MC && mine < S ? l[at] : 0.f;
         const float w = partial_weight(mv, lv, M), lw = lv * w;
 #pragma unroll
         for (int k = 0; k < MC; ++k) {
@@ -731,83 +646,29 @@ __device__ __forceinline__ void merge_row(const float* m, const float* l, const 
     }
 }
 
-// Which stretch and rows a work-group takes.  Work-groups go to the XCDs in turn by their index.  In both orders the row blocks of a
-// stretch follow each other on one XCD, and read it from its L2.  With counters (A.done) all splits of a unit are on the XCD u % 8, as the
-// fold inside the launch needs; else the stretches are dealt over all of them.
+// Which stretch and rows a work-group takes.  Work-groups go to the XCDs in turn by their index: the row blocks of a stretch follow each other on one
+// XCD, and read it from its L2; the stretches are dealt over all of them.
 __device__ __forceinline__ bool rows_place(const RowsArgs& A, int& split, int& u, int& block)
 {
-    const uint32_t units = A.B * A.Hkv, xcd = blockIdx.x & 7, turn = blockIdx.x >> 3;
-    if (A.done) {
-        block = turn % A.nrb;
-        u = turn / A.nrb * 8 + xcd;
-        split = blockIdx.y;
-        return u < (int)units;
-    }
+    const uint32_t units = A.B * A.Hkv, xcd = blockIdx.x & 7, turn = blockIdx.x >> 3, pair = turn / A.nrb * 8 + xcd;
     block = turn % A.nrb;
-    const uint32_t pair = turn / A.nrb * 8 + xcd;
     split = pair / units;
     u = pair - split * units;
     return pair < units * (A.Sv + A.Sr);
 }
 inline dim3 rows_grid(const RowsArgs& a)
 {
-    const int64_t units = (int64_t)a.B * a.Hkv, S = a.Sv + a.Sr;
-    const int64_t x = (a.done ? (units + 7) / 8 : (units * S + 7) / 8) * 8 * a.nrb;
-    return x > 0x7fffffff ? dim3(0) : dim3((uint32_t)x, a.done ? (uint32_t)S : 1);
+    const int64_t units = (int64_t)a.B * a.Hkv, x = (units * (a.Sv + a.Sr) + 7) / 8 * 8 * a.nrb;
+    return dim3(x > 0x7fffffff ? 0 : (uint32_t)x);
 }
 
-// The fold inside the launch.  Vector stores are counted until the L2 has them, so after the wait and the barrier this work-group's partial is in
-// the XCD's L2, which all splits of the unit share; the one that counts S reads them there (the few bytes of m and l past its L1, whose
-// lines other units share; a partial's accumulators are lines of their own, which this compute unit has not read before: it may have
-// written them, and stores go through the L1).
-template <typename T, int ROWS>
-__device__ __forceinline__ void fold_rows(const RowsArgs& A, int group, int b, int hk, int row0, int live, float* pool)
-{
-    const int S = A.Sv + A.Sr, tid = threadIdx.x, p = tid & 31, grp = tid >> 5;
-    int* last = (int*)pool;
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    if (tid == 0) *last = __hip_atomic_fetch_add(A.done + group, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == S - 1;
-    __syncthreads();
-    const bool mine = *last;
-    __syncthreads();
-    if (!mine) return;
-    if (tid == 0) A.done[group] = 0;                       // ready for the next launch on this context
-    const int rows = min(ROWS, live * A.G - row0), share = rows <= 1 ? 8 : rows <= 2 ? 4 : rows <= 4 ? 2 : 1;      // groups of 32 lanes a row
-    f32x4* part = (f32x4*)pool;                            // [group][32], and the sums behind
-    float* den = pool + 8 * 32 * 4;
-    for (int r0 = 0; r0 < rows; r0 += 8 / share) {
-        const int row = r0 + grp / share, r = row0 + min(row, rows - 1), tok = r / A.G;
-        const size_t to = (size_t)(b * A.T + tok) * A.Hq + hk * A.G + (r - tok * A.G);
-        f32x4 num;
-        float sum;
-        merge_row<true, 8>(A.ws_m + to * S, A.ws_l + to * S, A.ws_acc + to * S * D, S, grp % share, share, p, num, sum);
-        if (share > 1) {
-            part[grp * 32 + p] = num;
-            if (p == 0) den[grp] = sum;
-            __syncthreads();
-            if (grp % share == 0)
-                for (int k = 1; k < share; ++k) {
-                    num += part[(grp + k) * 32 + p];
-                    sum += den[grp + k];
-                }
-        }
-        if (grp % share == 0 && row < rows) {
-            const float inv = 1.f / sum;
-            T* o = (T*)A.out + to * D + 4 * p;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) st_elem(o + e, sum == 0.f ? 0.f : num[e] * inv);
-        }
-    }
-}
-
-template <int FMT, int R, int NRB>
-__global__ __launch_bounds__(256, NRB == 1 && FMT != ROWS_F32 ? 2 : 1) void attn_rows(RowsArgs A)
+template <int FMT, int R>
+__global__ __launch_bounds__(256, FMT == ROWS_F32 ? 1 : 2) void attn_rows(RowsArgs A)
 {
     constexpr bool F32IO = FMT == ROWS_F32 || FMT == ROWS_Q8_F32;
     typedef typename std::conditional<F32IO, float, bf16_t>::type T;
-    typedef typename std::conditional<F32IO, PlainRowsF32<NRB>, PlainRowsBf16<NRB>>::type Plain;
-    constexpr int POOL = 16 * NRB * (R + 4) > 4 * 32 * PARK * 4 ? 16 * NRB * (R + 4) : 4 * 32 * PARK * 4;
+    typedef typename std::conditional<F32IO, PlainRowsF32, PlainRowsBf16>::type Plain;
+    constexpr int POOL = 16 * (R + 4) > 4 * 32 * PARK * 4 ? 16 * (R + 4) : 4 * 32 * PARK * 4;
     __shared__ __attribute__((aligned(16))) float pool[POOL];           // q R_r, and at the end the four waves' accumulators of 16 rows
     __shared__ float sm_m[4][16], sm_l[4][16];
 
@@ -816,20 +677,14 @@ __global__ __launch_bounds__(256, NRB == 1 && FMT != ROWS_F32 ? 2 : 1) void attn
     const int b = u / A.Hkv, hk = u - b * A.Hkv;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, n = lane & 15;
     const int S = A.Sv + A.Sr;
-    const int row0 = block * 16 * NRB;                     // rows of the KV head: token by token, its G heads
+    const int row0 = block * 16;                           // rows of the KV head: token by token, its G heads
     if (row0 >= A.T * A.G) return;
-    int tok[NRB];                                          // lane (., n): the token of row n of block rb
-    const T* qrow[NRB];
-#pragma unroll
-    for (int rb = 0; rb < NRB; ++rb) {
-        const int row = min(row0 + 16 * rb + n, A.T * A.G - 1);
-        tok[rb] = row / A.G;
-        qrow[rb] = (const T*)A.q + ((size_t)(b * A.T + tok[rb]) * A.Hq + hk * A.G + (row - tok[rb] * A.G)) * D;
-    }
+    const int row = min(row0 + n, A.T * A.G - 1), tok = row / A.G;      // lane (., n): its row and the row's token
+    const T* qrow = (const T*)A.q + ((size_t)(b * A.T + tok) * A.Hq + hk * A.G + (row - tok * A.G)) * D;
     auto drafts_of = [&]() { return A.draft_k ? min(max(A.n_drafts ? A.n_drafts[b] : A.T, 0), A.T) : 0; };
     int live = A.T;                                        // tokens whose rows are asked for
 
-    RowState<NRB> st;                                      // (cleared only in front of the loops: its registers are the prologue's until then)
+    RowState st;                                      // (cleared only in front of the loops: its registers are the prologue's until then)
     const bool cache = split < A.Sv;
     if (cache) {
         typedef typename TileOf<FMT, R>::type Tile;
@@ -847,7 +702,7 @@ __global__ __launch_bounds__(256, NRB == 1 && FMT != ROWS_F32 ? 2 : 1) void attn
         // sequence is as long as the host's bound (else it is asked for again).
         int e0, e1, t0, t1;
         share(min(A.max_len, A.cap), e0, e1);
-        Rotation<T, R, NRB> rot;
+        Rotation<T, R> rot;
         const float* Ru = A.Rr + (size_t)u * D * A.r;
         rot.load(qrow, Ru, A.dmu ? A.dmu + (size_t)u * D : Ru, A.r, wave, g, n);      // (any address that can be read, without a bias)
         Tile X, Y;
@@ -860,10 +715,10 @@ __global__ __launch_bounds__(256, NRB == 1 && FMT != ROWS_F32 ? 2 : 1) void attn
         if (t0 < t1) {
             int t = t0 + wave;                             // (a wave without a tile reads the last one, and leaves it)
             if (t0 != e0 || t1 != e1) X.load(Ku, Vu, 32 * min(t, t1 - 1), A.rp, lane);
-            float bias[NRB];
+            float bias;
             rot.make(pool, bias, A.dmu != nullptr, A.r, wave, g, n);
             lds_barrier();
-            CacheRows<FMT, R, NRB> rows;
+            CacheRows<FMT, R> rows;
             rows.take(pool, A.scale_log2, g, n);
             st.clear();
 #pragma unroll 1
@@ -877,8 +732,7 @@ __global__ __launch_bounds__(256, NRB == 1 && FMT != ROWS_F32 ? 2 : 1) void attn
                 rows.step(Y, st, len - 32 * (t + 4), A.rp, g);
             }
             // the bias joins only now: it is the same for all of the cache, and would cost the scores bits
-#pragma unroll
-            for (int rb = 0; rb < NRB; ++rb) st.m[rb] += bias[rb] * A.scale_log2;
+            st.m += bias * A.scale_log2;
         } else {
             st.clear();
         }
@@ -904,25 +758,20 @@ __global__ __launch_bounds__(256, NRB == 1 && FMT != ROWS_F32 ? 2 : 1) void attn
                 const bool own = t >= tt;                  // drafts
                 const int r0 = 32 * (own ? t - tt : t), rows = own ? drafts : text;
                 X.load(own ? dk : tk, own ? dv : tv, own ? A.draft_st : A.text_st, r0, rows, g, n);
-                f32x4 s[NRB][2];
+                f32x4 s[2];
                 X.scores(s, A.scale_log2);
-                uint32_t see[NRB];                         // bit e: row n sees token slot e of this lane's group
-#pragma unroll
-                for (int rb = 0; rb < NRB; ++rb) {
-                    uint64_t mask = ~0ull;
-                    if (own) {
-                        mask = A.mask ? A.mask[(size_t)b * A.T + tok[rb]] : (2ull << tok[rb]) - 1;
-                        mask >>= r0;
-                    }
-                    const int left = rows - r0;
-                    mask &= left >= 32 ? 0xffffffffull : (1ull << left) - 1;
-                    const uint32_t lo = (uint32_t)mask >> (4 * g);
-                    see[rb] = (lo & 15) | ((lo >> 12) & 0xf0);
+                uint64_t mask = ~0ull;
+                if (own) {
+                    mask = A.mask ? A.mask[(size_t)b * A.T + tok] : (2ull << tok) - 1;
+                    mask >>= r0;
                 }
+                const int left = rows - r0;
+                mask &= left >= 32 ? 0xffffffffull : (1ull << left) - 1;
+                const uint32_t lo = (uint32_t)mask >> (4 * g);
+                const uint32_t see = (lo & 15) | ((lo >> 12) & 0xf0);      // bit e: row n sees token slot e of this lane's group
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-#pragma unroll
-                    for (int rb = 0; rb < NRB; ++rb) s[rb][e >> 2][e & 3] = (see[rb] >> e) & 1 ? s[rb][e >> 2][e & 3] : ROWS_NEG_INF;
+                    s[e >> 2][e & 3] = (see >> e) & 1 ? s[e >> 2][e & 3] : ROWS_NEG_INF;
                     if (r0 + (e < 4 ? 4 * g + e : 12 + 4 * g + e) >= rows) X.drop(e);
                 }
                 st.weigh(s);
@@ -935,81 +784,67 @@ __global__ __launch_bounds__(256, NRB == 1 && FMT != ROWS_F32 ? 2 : 1) void attn
 #pragma unroll
                 for (int ii = 0; ii < 4; ++ii) {
                     const typename Plain::Eight x(dv + (int64_t)j * A.draft_st + 32 * g + 8 * ii);
+                    const uint64_t mask = A.mask ? A.mask[(size_t)b * A.T + tok] : (2ull << tok) - 1;
 #pragma unroll
-                    for (int rb = 0; rb < NRB; ++rb) {
-                        const uint64_t mask = A.mask ? A.mask[(size_t)b * A.T + tok[rb]] : (2ull << tok[rb]) - 1;
-#pragma unroll
-                        for (int cb = 0; cb < 8; ++cb) st.O[rb][cb][ii] += (mask >> j) & 1 ? x.odd(cb) : 0.f;
-                    }
+                    for (int cb = 0; cb < 8; ++cb) st.O[cb][ii] += (mask >> j) & 1 ? x.odd(cb) : 0.f;
                 }
             }
         }
     }
 
-    // The four waves' states become one partial (or, of a single split, the result), 16 rows at a time.  Parked as quads of channels:
+    // The four waves' states become one partial (or, of a single split, the result).  Parked as quads of channels:
     // [wave][channels 4 p ..+3][row].
+    f32x4* park = (f32x4*)pool + wave * 32 * PARK;
+    __syncthreads();
 #pragma unroll
-    for (int rb = 0; rb < NRB; ++rb) {
-        if (row0 + 16 * rb >= live * A.G) break;
-        f32x4* park = (f32x4*)pool + wave * 32 * PARK;
-        __syncthreads();
-#pragma unroll
-        for (int cb = 0; cb < 8; ++cb) {
-            if (cache) park[(4 * cb + g) * PARK + n] = st.O[rb][cb];
-            else {                                         // accumulator (cb, ii) is channel 32 g + 8 ii + cb there
-                const int ii = cb >> 1, h = cb & 1;
-                park[(8 * g + cb) * PARK + n] = (f32x4){st.O[rb][4 * h][ii], st.O[rb][4 * h + 1][ii], st.O[rb][4 * h + 2][ii], st.O[rb][4 * h + 3][ii]};
-            }
-        }
-        const float l = groups_sum(st.l[rb]);
-        if (g == 0) { sm_m[wave][n] = st.m[rb]; sm_l[wave][n] = l; }
-        __syncthreads();
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const int i = tid + 256 * half, row = i >> 5, p = i & 31, mine = row0 + 16 * rb + row;
-            if (mine >= live * A.G) continue;
-            const float M = fmaxf(fmaxf(sm_m[0][row], sm_m[1][row]), fmaxf(sm_m[2][row], sm_m[3][row]));
-            f32x4 acc = (f32x4){0.f, 0.f, 0.f, 0.f};
-            float sum = 0.f;
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                const float x = partial_weight(sm_m[w][row], sm_l[w][row], M);
-                acc += ((const f32x4*)pool)[(w * 32 + p) * PARK + row] * x;
-                sum = fmaf(sm_l[w][row], x, sum);
-            }
-            const int tm = mine / A.G;
-            const size_t to = (size_t)(b * A.T + tm) * A.Hq + hk * A.G + (mine - tm * A.G);
-            if (S == 1) {
-                const float inv = 1.f / sum;
-                T* o = (T*)A.out + to * D + 4 * p;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) st_elem(o + e, sum == 0.f ? 0.f : acc[e] * inv);
-            } else {
-                const size_t slot = to * S + split;
-                *(f32x4*)(A.ws_acc + slot * D + 4 * p) = acc;
-                if (p == 0) { A.ws_m[slot] = M; A.ws_l[slot] = sum; }
-            }
+    for (int cb = 0; cb < 8; ++cb) {
+        if (cache) park[(4 * cb + g) * PARK + n] = st.O[cb];
+        else {                                         // accumulator (cb, ii) is channel 32 g + 8 ii + cb there
+            const int ii = cb >> 1, h = cb & 1;
+            park[(8 * g + cb) * PARK + n] = (f32x4){st.O[4 * h][ii], st.O[4 * h + 1][ii], st.O[4 * h + 2][ii], st.O[4 * h + 3][ii]};
         }
     }
-    if (A.done) fold_rows<T, 16 * NRB>(A, u * A.nrb + block, b, hk, row0, live, pool);
+    const float l = groups_sum(st.l);
+    if (g == 0) { sm_m[wave][n] = st.m; sm_l[wave][n] = l; }
+    __syncthreads();
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        const int i = tid + 256 * half, row = i >> 5, p = i & 31, mine = row0 + row;
+        if (mine >= live * A.G) continue;
+        const float M = fmaxf(fmaxf(sm_m[0][row], sm_m[1][row]), fmaxf(sm_m[2][row], sm_m[3][row]));
+        f32x4 acc = (f32x4){0.f, 0.f, 0.f, 0.f};
+        float sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float x = partial_weight(sm_m[w][row], sm_l[w][row], M);
+            acc += ((const f32x4*)pool)[(w * 32 + p) * PARK + row] * x;
+            sum = fmaf(sm_l[w][row], x, sum);
+        }
+        const int tm = mine / A.G;
+        const size_t to = (size_t)(b * A.T + tm) * A.Hq + hk * A.G + (mine - tm * A.G);
+        if (S == 1) {
+            const float inv = 1.f / sum;
+            T* o = (T*)A.out + to * D + 4 * p;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) st_elem(o + e, sum == 0.f ? 0.f : acc[e] * inv);
+        } else {
+            const size_t slot = to * S + split;
+            *(f32x4*)(A.ws_acc + slot * D + 4 * p) = acc;
+            if (p == 0) { A.ws_m[slot] = M; A.ws_l[slot] = sum; }
+        }
+    }
 }
 
-template <int FMT, int R>
-static void launch_rows_r(int nrb16, dim3 grid, const RowsArgs& a, hipStream_t st)
-{
-    if (nrb16 == 1) attn_rows<FMT, R, 1><<<grid, 256, 0, st>>>(a);
-    else attn_rows<FMT, R, 2><<<grid, 256, 0, st>>>(a);
-}
 template <int FMT>
-static hipError_t launch_rows_fmt(const RowsArgs& a, int nrb16, hipStream_t st)
+static hipError_t launch_rows_fmt(const RowsArgs& a, hipStream_t st)
 {
     const dim3 grid = rows_grid(a);
     if (!grid.x) return hipErrorInvalidValue;
     switch ((a.r + 31) / 32) {
-        case 1: launch_rows_r<FMT, 32>(nrb16, grid, a, st); break;
-        case 2: launch_rows_r<FMT, 64>(nrb16, grid, a, st); break;
-        case 3: launch_rows_r<FMT, 96>(nrb16, grid, a, st); break;
-        default: launch_rows_r<FMT, 128>(nrb16, grid, a, st); break;
+        case 1: attn_rows<FMT, 32><<<grid, 256, 0, st>>>(a); break;
+        case 2: attn_rows<FMT, 64><<<grid, 256, 0, st>>>(a); break;
+        case 3: attn_rows<FMT, 96><<<grid, 256, 0, st>>>(a); break;
+        default: attn_rows<FMT, 128><<<grid, 256, 0, st>>>(a); break;
     }
     return hipGetLastError();
 }

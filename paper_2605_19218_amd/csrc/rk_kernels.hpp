@@ -51,7 +51,7 @@ hipError_t launch_unpack(int dtype, int U, int cap, int r, const void* Kp, const
                          void* v_rows, hipStream_t st);
 
 // A context's counters, one a sequence: from one to the next, so that the atomics of different sequences meet on lines of their own while there is
-// room (64 x 32 work-groups of a few rows each, four counters' atomics on a line: 51 us, APART_US).
+// room (64 x 32 work-groups of a few rows each, four counters' atomics on a line: 51 us, 7.2 apart).
 constexpr int CONTEXT_TICKETS = 1 << 16;
 inline int tickets_apart(int B) { return B <= CONTEXT_TICKETS / 32 ? 32 : 1; }
 
@@ -85,13 +85,12 @@ struct RowsArgs {
     void* out;
     float *ws_m, *ws_l, *ws_acc; // [B, T, Hq, S] and [B, T, Hq, S, d]
     int32_t max_len;             // the host's bound of the lengths
-    int32_t* done;               // a counter a row block that is zero between launches: the partials are folded inside the launch; or null
 };
-// fmt: ROWS_BF16, ROWS_F32, ROWS_Q8_BF16, ROWS_Q8_F32; nrb16: blocks of 16 rows a work-group takes (1, 2; with bf16 rows 4, 8 too)
-hipError_t launch_rows_bf16(const RowsArgs& a, int nrb16, hipStream_t st);
-hipError_t launch_rows_f32(const RowsArgs& a, int nrb16, hipStream_t st);
-hipError_t launch_rows_q8_bf16(const RowsArgs& a, int nrb16, hipStream_t st);
-hipError_t launch_rows_q8_f32(const RowsArgs& a, int nrb16, hipStream_t st);
+// rows: of a work-group, 16; with bf16 rows 128 too, over the 8-bit cache also 64
+hipError_t launch_rows_bf16(const RowsArgs& a, int rows, hipStream_t st);
+hipError_t launch_rows_f32(const RowsArgs& a, int rows, hipStream_t st);
+hipError_t launch_rows_q8_bf16(const RowsArgs& a, int rows, hipStream_t st);
+hipError_t launch_rows_q8_f32(const RowsArgs& a, int rows, hipStream_t st);
 hipError_t launch_rows_merge(int dtype, const RowsArgs& a, hipStream_t st);
 // row text_len[b] + i of the text segment receives draft path[b][i], i < n_path[b]; len_out[b] counts them
 struct PathArgs {

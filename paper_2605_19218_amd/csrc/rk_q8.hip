@@ -405,11 +405,16 @@ static hipError_t compress_q8_r(const RowsDev& keys, const RowsDev& vals, int B,
 hipError_t launch_compress_q8(int dtype, const RowsDev& keys, const RowsDev& vals, int B, int Hkv, int cap, int r, const float* Rr, void* Kq,
                               void* Vq, int32_t* seq_len_out, int n_cu, hipStream_t st)
 {
-    // 128 tokens a work-group, a block a wave, while that gives no more than eight work-groups a compute unit; then longer pieces, so that R_r
-    // is made ready less often
-    const int64_t total = (int64_t)B * Hkv * keys.n_tokens;
+    // Tokens of a work-group: the count whose rounds of work-groups (as many of them on a compute unit as their LDS lets) come out shortest, each counted with
+    // 16 tokens more for making R_r ready.  With 128 / 256 / 512 (us, with the rows read back, r = 64): 32768 tokens x heads 18.0 / 23.3 / 34.6, 65536 22.4
+    // / 25.5 / 36.3, 131072 42.0 / 39.7 / 52.6, 256000 73.8 / 77.2 / 75.2, 524288 138.5 / 132.6 / 158.4, 2097152 540 / 518 / 528.
+    const int64_t lds = (int64_t)((r + 31) / 32) * (32 * D * 4) + 4 * 4096, side = (int64_t)n_cu * (163840 / lds);
     int each = 128;
-    while (each < 1024 && total > (int64_t)each * 8 * n_cu) each *= 2;
+    int64_t best = INT64_MAX;
+    for (int e = 128; e <= 512; e *= 2) {
+        const int64_t groups = ((int64_t)keys.n_tokens + e - 1) / e * B * Hkv, cost = (groups + side - 1) / side * (e + 16);
+        if (cost < best) { best = cost; each = e; }
+    }
     auto go = [&](auto t) {
         typedef decltype(t) T;
         uint8_t *kq = (uint8_t*)Kq, *vq = (uint8_t*)Vq;

@@ -20,7 +20,7 @@ __global__ __launch_bounds__(256) void rows_merge(const float* __restrict__ ws_m
     if (n_drafts && bt - b * n_tok >= n_drafts[b]) return;       // (rows behind the last draft stay as they were)
     f32x4 num;
     float sum;
-    merge_row<false, WIDE ? 2 : 4>(ws_m + (size_t)row * S, ws_l + (size_t)row * S, ws_acc + (size_t)row * S * D, S, WIDE ? grp : 0, WIDE ? 8 : 1, p, num, sum);
+    merge_row<WIDE ? 2 : 4>(ws_m + (size_t)row * S, ws_l + (size_t)row * S, ws_acc + (size_t)row * S * D, S, WIDE ? grp : 0, WIDE ? 8 : 1, p, num, sum);
     if constexpr (WIDE) {
         part[grp][p] = num;
         if (p == 0) den[grp] = sum;
@@ -43,7 +43,7 @@ hipError_t launch_rows_merge(int dtype, const RowsArgs& a, hipStream_t st)
     const int rows = a.B * a.T * a.Hq, S = a.Sv + a.Sr;
     auto go = [&](auto t) {
         typedef decltype(t) E;
-        if (S > 4 && rows <= 4096)
+        if (S > 4 && rows <= 2048)
             rows_merge<E, true><<<rows, 256, 0, st>>>(a.ws_m, a.ws_l, a.ws_acc, (E*)a.out, rows, S, a.Hq, a.T, a.draft_k ? a.n_drafts : nullptr);
         else
             rows_merge<E, false><<<(rows + 7) / 8, 256, 0, st>>>(a.ws_m, a.ws_l, a.ws_acc, (E*)a.out, rows, S, a.Hq, a.T,

@@ -3,8 +3,8 @@
 #include "rk_attn_block.hpp"
 
 namespace rk {
-hipError_t launch_rows_bf16(const RowsArgs& a, int nrb16, hipStream_t st) 
+hipError_t launch_rows_bf16(const RowsArgs& a, int rows, hipStream_t st)
 {
-    return nrb16 <= 2 ? launch_rows_fmt<ROWS_BF16>(a, nrb16, st) : launch_block_fmt<ROWS_BF16>(a, nrb16, st);
+    return rows == 16 ? launch_rows_fmt<ROWS_BF16>(a, st) : launch_block_fmt<ROWS_BF16>(a, rows, st);
 }
 }  // namespace rk

@@ -3,5 +3,5 @@
 #include "rk_attn_rows.hpp"
 
 namespace rk {
-hipError_t launch_rows_f32(const RowsArgs& a, int nrb16, hipStream_t st) { return launch_rows_fmt<ROWS_F32>(a, nrb16, st); }
+hipError_t launch_rows_f32(const RowsArgs& a, int, hipStream_t st) { return launch_rows_fmt<ROWS_F32>(a, st); }
 }  // namespace rk
