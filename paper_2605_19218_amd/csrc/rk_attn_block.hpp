@@ -1,16 +1,21 @@
 // Attention of many query rows a KV head (more than 32: trees of drafts on grouped-query layers), bf16 rows, over the packed bf16 or the 8-bit
 // cache.  The mathematics, the splits and the partials are those of attn_rows (rk_attn_rows.hpp); what differs is who holds what:
 //
-// attn_rows gives every wave other tokens and the same rows, which is right while memory is the bound.  From 64 rows on the matrix cores are, and a
+// attn_rows gives every wave other tokens and the same rows, which is right while memory is the bound.  With many rows the matrix cores are, and a
 // wave that keeps 64 rows' accumulators beside its tiles needs more registers than there are.  Here a work-group stages the tokens in LDS, once for
 // all its rows, as operands of v_mfma_f32_32x32x16_bf16, and a wave owns 32 rows: 64 registers of accumulators, so that two waves
 // share a SIMD and one's softmax runs under the other's products.  A tile of 32 tokens read from LDS (12 KB at r = 64) feeds 24 instructions of 32
 // cycles.  8-bit codes become bf16 on their way into LDS, once for the work-group.  What is requested of memory is DEPTH stages ahead, in registers: a
-// round trip to HBM takes as long as two or three stages' arithmetic.
+// round trip to HBM takes as long as two or three stages' arithmetic (three stages do not fit beside 128 channels).
+// What bounds it: issue.  Of a SIMD's cycles the products take 35 %, the vector instructions between them (weights, their two parts, codes) 30 to 39 %, and
+// what waits at a barrier the rest.  112 rows x 32 units x 16384 tokens, r = 64, 1024 text rows: 65 us, 57 GFLOP issued, 870 TFLOP/s; 448 rows over 8 bits:
+// 214 us, 187 GFLOP, 873.  (Eight waves behind one barrier took 221 us for what two work-groups of four took 209; one bf16 part of the weights would save a third of the
+// products, and the error would be that of the result's own rounding.)
 //   S^T[token][row] = K . q~^T, O^T[channel][row] = V^T . P^T: lane (h, n) = (lane / 32, lane % 32) holds row n's scores of tokens 8 j + 4 h ..+3,
 //   j < 4.  Step s of the second product takes j = s and j = s + 2 of them as they are: tokens 4 g ..+3 and 16 + 4 g ..+3, g = 2 s + h, which is a
 //   16-byte piece of the Value cache; a Key operand is one of the Key cache.  So the stages are copied piece by piece.
-// RW: row groups of a work-group, 32 rows each; the 4 / RW waves of a group take a tile of a stage each.
+// RW: row groups of a work-group, 32 rows each; the 4 / RW waves of a group take a tile of a stage each.  128 rows; over 8 bits also 64, whose codes take
+// as long to convert for fewer rows but leave no wave idle.
 #pragma once
 #include "rk_attn_rows.hpp"
 

@@ -13,7 +13,12 @@
 // rescaled a few times instead of at every new maximum.  Maxima, sums and accumulators are fp32.  Over 16-bit products the weights go as two
 // bf16 parts (17 bits), as q R_r does; with fp32 rows three (all 24); a code is exact in one.
 // Stretches: the cache's 32-token tiles are shared by the first Sv splits, the text's and the drafts' by the others, by the sequence's own lengths;
-// rows_merge folds the partials.  What bounds it: memory with few rows, the matrix cores from about 64 rows a KV head on.
+// rows_merge folds the partials (inside the launch, by the work-group that ends last, it took up to 3 us more: one work-group reads all of a unit).  More than 16
+// rows are blocks of 16 that read the same tokens, on one XCD, out of its L2, up to where attn_block is faster.  (Two blocks of 16 in one wave
+// shared each read, but their accumulators wandered between the two halves of the register file at every tile: 32 rows, 32 units x 16000 tokens 45.8 us, as
+// two work-groups 44.1; 8 x 16000 20.2 and 16.4.)
+// What bounds it: memory and its latency.  One token over 8 bits, 28 rows of 4 KV heads x 8 x 16384 tokens, r = 64: 20.2 us for 103 MB, 5.1 TB/s; 32 heads x 2880
+// tokens with fp32 rows 10.3 us; 8 heads x 1024 tokens 6.1 us, of which launch, length, rotation and the first tiles' round trips are all but 1.
 #pragma once
 #include "rk_kernels.hpp"
 
