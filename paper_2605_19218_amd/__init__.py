@@ -140,9 +140,10 @@ def lib():
             _rkbind.bind(Layout, Text, *[C.cast(f, C.c_void_p).value for f in
                                          (L.rk_decode_attn, L.rk_append_decode_attn, L.rk_decode_attn_dual,
                                           L.rk_append_text_decode_attn_dual)])
-            _rkbind.bind_drafts(Drafts, *[C.cast(f, C.c_void_p).value for f in
+            _rkbind.bind_drafts(Drafts, Rows, *[C.cast(f, C.c_void_p).value for f in
                                           (L.rk_append_quant, L.rk_decode_attn_quant, L.rk_decode_attn_tree,
-                                           L.rk_decode_attn_tree_quant, L.rk_append_text_path)])
+                                           L.rk_decode_attn_tree_quant, L.rk_append_text_path, L.rk_compress_quant,
+                                           L.rk_unpack_cache_quant)])
             _bind = _rkbind
         _lib = L
     return _lib
@@ -433,6 +434,8 @@ def rk_cache_bytes_quant(layout: Layout):
 
 def rk_compress_quant(ctx, layout: Layout, keys: Rows, R_r, k_q8, values: Rows, v_cache, seq_len_out=None, stream=None) -> None:
     """rk_compress into 8-bit caches (`v_cache` is the 8-bit Value cache)."""
+    if _bind is not None and _done(ctx, _bind.compress_quant(ctx, layout, keys, R_r, k_q8, values, v_cache, seq_len_out, stream)):
+        return
     kref = C.byref(keys.c()) if keys is not None else None
     vref = C.byref(values.c()) if values is not None else None
     _check(ctx, lib().rk_compress_quant(ctx, C.byref(layout.c()), kref, _ptr(R_r), _ptr(k_q8), vref, _ptr(v_cache),
@@ -448,6 +451,8 @@ def rk_append_quant(ctx, layout: Layout, k_new, v_new, R_r, k_q8, v_q8, seq_len_
 
 
 def rk_unpack_cache_quant(ctx, layout: Layout, k_q8, v_q8, k_rows, v_rows, stream=None) -> None:
+    if _bind is not None and _done(ctx, _bind.unpack_quant(ctx, layout, k_q8, v_q8, k_rows, v_rows, stream)):
+        return
     _check(ctx, lib().rk_unpack_cache_quant(ctx, C.byref(layout.c()), _ptr(k_q8), _ptr(v_q8), _ptr(k_rows), _ptr(v_rows),
                                          _stream(stream)))
 

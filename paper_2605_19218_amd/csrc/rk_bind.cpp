@@ -1,6 +1,7 @@
 // CPython side of the calls that a program makes once per generated token and layer: the arguments of rk_decode_attn,
 // rk_append_decode_attn, rk_decode_attn_dual and rk_append_text_decode_attn_dual, of rk_append_quant and rk_decode_attn_quant, and, once per
-// round of drafts and layer, of rk_decode_attn_tree, rk_decode_attn_tree_quant and rk_append_text_path, marshalled in C.  The same through ctypes costs some 5 us a
+// round of drafts and layer, of rk_decode_attn_tree, rk_decode_attn_tree_quant and rk_append_text_path, marshalled in C; with them the prompt's
+// rk_compress_quant and rk_unpack_cache_quant, which short prompts wait for as well.  The same through ctypes costs some 5 us a
 // call (structures built field by field, a converter per argument), which is as long as a short decode runs on the device: 8 KV heads x
 // 1024 tokens were called every 8.7 us, of which the device needed 5.8.
 //
@@ -30,6 +31,9 @@ typedef rk_status (*tree_fn)(rk_ctx*, const rk_layout*, const void*, const void*
 typedef rk_status (*path_fn)(rk_ctx*, const rk_layout*, const rk_text*, const rk_drafts*, const int32_t*, int32_t, const int32_t*,
                              int32_t*, void*);
 
+typedef rk_status (*compress_fn)(rk_ctx*, const rk_layout*, const rk_rows*, const float*, void*, const rk_rows*, void*, int32_t*, void*);
+typedef rk_status (*unpack_fn)(rk_ctx*, const rk_layout*, const void*, const void*, void*, void*, void*);
+
 decode_fn fn_decode;
 append_decode_fn fn_append_decode;
 dual_fn fn_dual;
@@ -38,10 +42,12 @@ append_quant_fn fn_append_quant;
 dual_fn fn_decode_quant;
 tree_fn fn_tree, fn_tree_quant;
 path_fn fn_path;
-PyTypeObject *layout_type, *text_type, *drafts_type;      // the binding's classes (kept alive)
+compress_fn fn_compress;
+unpack_fn fn_unpack;
+PyTypeObject *layout_type, *text_type, *drafts_type, *rows_type;      // the binding's classes (kept alive)
 
 PyObject *s_batch, *s_nq, *s_nkv, *s_hd, *s_keep, *s_dtype, *s_cap, *s_max_seq, *s_seq, *s_data_ptr, *s_numel, *s_esize, *s_cuda_stream,
-    *s_k, *s_v, *s_max_len, *s_len, *s_strides, *s_stride, *s_shape, *s_n_tokens, *s_n_tokens_dev, *s_mask;
+    *s_k, *s_v, *s_max_len, *s_len, *s_strides, *s_stride, *s_shape, *s_n_tokens, *s_n_tokens_dev, *s_mask, *s_data, *s_tok_idx, *s_tok_off;
 
 // All of these return false where the argument is not of the plain kind; an exception may then be set, and the caller clears it.
 bool integer(PyObject* o, long long* out)
@@ -172,6 +178,29 @@ bool drafts(PyObject* o, rk_drafts* d)
     d->stride_b = st[0];
     d->stride_h = st[1];
     d->stride_t = st[2];
+    return true;
+}
+bool rows(PyObject* o, rk_rows* r)
+{
+    if (!rows_type || Py_TYPE(o) != rows_type) return false;
+    void *data = nullptr, *n = nullptr, *idx = nullptr, *off = nullptr;
+    int64_t st[3];
+    if (!address_of(o, s_data, &data) || !address_of(o, s_n_tokens_dev, &n) || !address_of(o, s_tok_idx, &idx) || !address_of(o, s_tok_off, &off) ||
+        !int32_of(o, s_n_tokens, &r->n_tokens))
+        return false;
+    PyObject* key = PyObject_GetAttr(o, s_data);
+    PyObject* given = key ? PyObject_GetAttr(o, s_strides) : nullptr;
+    const bool ok = given && strides_of(given, key, st);
+    Py_XDECREF(given);
+    Py_XDECREF(key);
+    if (!ok) return false;
+    r->data = (decltype(r->data))data;
+    r->n_tokens_dev = (decltype(r->n_tokens_dev))n;
+    r->tok_idx = (decltype(r->tok_idx))idx;
+    r->tok_off = (decltype(r->tok_off))off;
+    r->stride_b = st[0];
+    r->stride_h = st[1];
+    r->stride_t = st[2];
     return true;
 }
 bool stream_of(PyObject* o, void** out)
@@ -342,6 +371,34 @@ PyObject* py_append_path(PyObject*, PyObject* const* a, Py_ssize_t n)
     return answer(s);
 }
 
+// (ctx, layout, keys, R_r, k_q8, values, v_q8, seq_len_out, stream)
+PyObject* py_compress_quant(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    void *ctx, *p[2], *q[2], *stream;
+    rk_layout L;
+    rk_rows k, v;
+    if (n != 9 || !fn_compress || !address(a[0], &ctx) || !layout(a[1], &L) || !rows(a[2], &k) || !addresses(a + 3, 2, p) || !rows(a[5], &v) ||
+        !addresses(a + 6, 2, q) || !stream_of(a[8], &stream))
+        return other_path();
+    rk_status s;
+    Py_BEGIN_ALLOW_THREADS
+    s = fn_compress((rk_ctx*)ctx, &L, &k, (const float*)p[0], p[1], &v, q[0], (int32_t*)q[1], stream);
+    Py_END_ALLOW_THREADS
+    return answer(s);
+}
+// (ctx, layout, k_q8, v_q8, k_rows, v_rows, stream)
+PyObject* py_unpack_quant(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    void *ctx, *p[4], *stream;
+    rk_layout L;
+    if (n != 7 || !fn_unpack || !address(a[0], &ctx) || !layout(a[1], &L) || !addresses(a + 2, 4, p) || !stream_of(a[6], &stream)) return other_path();
+    rk_status s;
+    Py_BEGIN_ALLOW_THREADS
+    s = fn_unpack((rk_ctx*)ctx, &L, p[0], p[1], p[2], p[3], stream);
+    Py_END_ALLOW_THREADS
+    return answer(s);
+}
+
 // bind(Layout, Text, addresses of the four entry points)
 PyObject* py_bind(PyObject*, PyObject* args)
 {
@@ -361,29 +418,36 @@ PyObject* py_bind(PyObject*, PyObject* args)
     Py_RETURN_NONE;
 }
 
-// bind_drafts(Drafts, addresses of the five entry points)
+// bind_drafts(Drafts, Rows, addresses of the seven entry points)
 PyObject* py_bind_drafts(PyObject*, PyObject* args)
 {
-    PyObject* dt;
-    unsigned long long f[5];
-    if (!PyArg_ParseTuple(args, "O!KKKKK", &PyType_Type, &dt, f, f + 1, f + 2, f + 3, f + 4)) return nullptr;
+    PyObject *dt, *rt;
+    unsigned long long f[7];
+    if (!PyArg_ParseTuple(args, "O!O!KKKKKKK", &PyType_Type, &dt, &PyType_Type, &rt, f, f + 1, f + 2, f + 3, f + 4, f + 5, f + 6)) return nullptr;
     Py_INCREF(dt);
+    Py_INCREF(rt);
     Py_XDECREF((PyObject*)drafts_type);
+    Py_XDECREF((PyObject*)rows_type);
     drafts_type = (PyTypeObject*)dt;
+    rows_type = (PyTypeObject*)rt;
     fn_append_quant = (append_quant_fn)(uintptr_t)f[0];
     fn_decode_quant = (dual_fn)(uintptr_t)f[1];
     fn_tree = (tree_fn)(uintptr_t)f[2];
     fn_tree_quant = (tree_fn)(uintptr_t)f[3];
     fn_path = (path_fn)(uintptr_t)f[4];
+    fn_compress = (compress_fn)(uintptr_t)f[5];
+    fn_unpack = (unpack_fn)(uintptr_t)f[6];
     Py_RETURN_NONE;
 }
 
 PyMethodDef methods[] = {
-    {"bind_drafts", py_bind_drafts, METH_VARARGS, "bind_drafts(Drafts, five entry point addresses)"},
+    {"bind_drafts", py_bind_drafts, METH_VARARGS, "bind_drafts(Drafts, Rows, seven entry point addresses)"},
     {"append_quant", (PyCFunction)(void (*)(void))py_append_quant, METH_FASTCALL, "rk_append_quant; its status, or None for arguments not taken here"},
     {"decode_quant", (PyCFunction)(void (*)(void))py_decode_quant, METH_FASTCALL, "rk_decode_attn_quant, likewise"},
     {"tree", (PyCFunction)(void (*)(void))py_tree, METH_FASTCALL, "rk_decode_attn_tree, likewise"},
     {"tree_quant", (PyCFunction)(void (*)(void))py_tree_quant, METH_FASTCALL, "rk_decode_attn_tree_quant, likewise"},
+    {"compress_quant", (PyCFunction)(void (*)(void))py_compress_quant, METH_FASTCALL, "rk_compress_quant, likewise"},
+    {"unpack_quant", (PyCFunction)(void (*)(void))py_unpack_quant, METH_FASTCALL, "rk_unpack_cache_quant, likewise"},
     {"append_path", (PyCFunction)(void (*)(void))py_append_path, METH_FASTCALL, "rk_append_text_path, likewise"},
     {"bind", py_bind, METH_VARARGS, "bind(Layout, Text, four entry point addresses)"},
     {"decode", (PyCFunction)(void (*)(void))py_decode, METH_FASTCALL, "rk_decode_attn; its status, or None for arguments not taken here"},
@@ -404,7 +468,8 @@ PyMODINIT_FUNC PyInit__rkbind(void)
         {&s_cap, "capacity"}, {&s_max_seq, "max_seq_len"}, {&s_seq, "seq_len"}, {&s_data_ptr, "data_ptr"}, {&s_numel, "numel"},
         {&s_esize, "element_size"}, {&s_cuda_stream, "cuda_stream"}, {&s_k, "k"}, {&s_v, "v"}, {&s_max_len, "max_len"}, {&s_len, "len"},
         {&s_strides, "strides"}, {&s_stride, "stride"}, {&s_shape, "shape"},
-        {&s_n_tokens, "n_tokens"}, {&s_n_tokens_dev, "n_tokens_dev"}, {&s_mask, "mask"}};
+        {&s_n_tokens, "n_tokens"}, {&s_n_tokens_dev, "n_tokens_dev"}, {&s_mask, "mask"}, {&s_data, "data"},
+        {&s_tok_idx, "tok_idx"}, {&s_tok_off, "tok_off"}};
     for (auto& x : names)
         if (!(*x.at = PyUnicode_InternFromString(x.text))) return nullptr;
     return PyModule_Create(&module);

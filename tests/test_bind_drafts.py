@@ -10,16 +10,19 @@ import paper_2605_19218_amd as rk
 
 B, HQ, HKV, T = 2, 8, 2, 6
 vp, f32, sz, i32 = C.c_void_p, C.c_float, C.c_size_t, C.c_int
-PL, PT, PD = C.POINTER(rk.rk_layout), C.POINTER(rk.rk_text), C.POINTER(rk.rk_drafts)
+PL, PT, PD, PR = C.POINTER(rk.rk_layout), C.POINTER(rk.rk_text), C.POINTER(rk.rk_drafts), C.POINTER(rk.rk_rows)
 SIGNATURES = {
     "rk_append_quant": [vp, PL, vp, vp, vp, vp, vp, vp, vp],
     "rk_decode_attn_quant": [vp, PL, vp, vp, vp, vp, vp, PT, f32, vp, vp, sz, vp],
     "rk_decode_attn_tree": [vp, PL, vp, vp, vp, vp, vp, PT, PD, f32, vp, vp, sz, vp],
     "rk_decode_attn_tree_quant": [vp, PL, vp, vp, vp, vp, vp, PT, PD, f32, vp, vp, sz, vp],
     "rk_append_text_path": [vp, PL, PT, PD, vp, i32, vp, vp, vp],
+    "rk_compress_quant": [vp, PL, PR, vp, vp, PR, vp, vp, vp],
+    "rk_unpack_cache_quant": [vp, PL, vp, vp, vp, vp, vp],
 }
 FAST = {"rk_append_quant": "append_quant", "rk_decode_attn_quant": "decode_quant", "rk_decode_attn_tree": "tree",
-        "rk_decode_attn_tree_quant": "tree_quant", "rk_append_text_path": "append_path"}
+        "rk_decode_attn_tree_quant": "tree_quant", "rk_append_text_path": "append_path", "rk_compress_quant": "compress_quant",
+        "rk_unpack_cache_quant": "unpack_quant"}
 
 
 class OtherDrafts(rk.Drafts):
@@ -44,7 +47,11 @@ def drafts(cls=rk.Drafts, **more):
     return cls(**{**a, **more})
 
 
-def call(name, lay=None, txt=None, d=None, ws=None, scale=0.0, kv=None, ctx=77, n=None):
+def rows(cls=rk.Rows, **more):
+    return cls(**{"data": tensor(B, HKV, 50, 128), "n_tokens": 50, **more})
+
+
+def call(name, lay=None, txt=None, d=None, ws=None, scale=0.0, kv=None, ctx=77, n=None, rw=None):
     """positional arguments of an entry point; kv: in the place of a tensor"""
     lay = lay or layout()
     t = [tensor(4, 16) for _ in range(6)]
@@ -52,6 +59,10 @@ def call(name, lay=None, txt=None, d=None, ws=None, scale=0.0, kv=None, ctx=77, 
         t[1] = kv
     if name == "rk_append_quant":
         return [ctx, lay, *t]
+    if name == "rk_unpack_cache_quant":
+        return [ctx, lay, *t[:4]]
+    if name == "rk_compress_quant":
+        return [ctx, lay, rw or rows(), t[0], t[1], rows(n_tokens=49), *t[2:4]]
     if name == "rk_append_text_path":
         return [ctx, lay, txt, d, kv if kv is not None else tensor(B, 5, dtype=torch.int32), t[2], t[3], n]
     return [ctx, lay, *t[:5], txt, *([d] if "tree" in name else []), scale, tensor(4, 16), ws]
@@ -67,7 +78,7 @@ def paths(monkeypatch):
 
     def entry(kinds):
         def f(*a):
-            seen.append([[getattr(x.contents, n) for n, _ in x.contents._fields_] if kind in (PL, PT, PD) and x else None if kind in (PL, PT, PD)
+            seen.append([[getattr(x.contents, n) for n, _ in x.contents._fields_] if kind in (PL, PT, PD, PR) and x else None if kind in (PL, PT, PD, PR)
                          else x for x, kind in zip(a, kinds)])
             return 0
         return C.CFUNCTYPE(i32, *kinds)(f)
@@ -78,7 +89,7 @@ def paths(monkeypatch):
         keep[-1].argtypes, keep[-1].restype = kinds, i32
         setattr(stub, name, keep[-1])
     real, bind = rk.lib(), rk._bind
-    bind.bind_drafts(rk.Drafts, *[C.cast(getattr(stub, n), vp).value for n in SIGNATURES])
+    bind.bind_drafts(rk.Drafts, rk.Rows, *[C.cast(getattr(stub, n), vp).value for n in SIGNATURES])
 
     def record(name, args, kw, fast):
         seen.clear()
@@ -92,7 +103,7 @@ def paths(monkeypatch):
         return list(seen[0])
 
     yield record, bind
-    bind.bind_drafts(rk.Drafts, *[C.cast(getattr(real, n), vp).value for n in SIGNATURES])
+    bind.bind_drafts(rk.Drafts, rk.Rows, *[C.cast(getattr(real, n), vp).value for n in SIGNATURES])
 
 
 @pytest.mark.parametrize("name", list(SIGNATURES))
@@ -109,6 +120,9 @@ def test_same_arguments(paths, name):
         forms.append((dict(txt=None, d=drafts(), ws=ws), {"workspace_bytes": 0}))
     if name == "rk_append_text_path":
         forms.append((dict(txt=text(), d=drafts(), kv=1 << 40, n=3), {}))
+    if name == "rk_compress_quant":
+        forms += [(dict(rw=rows(n_tokens_dev=tensor(B, dtype=torch.int32), strides=(7, 6, 5))), {}),
+                  (dict(rw=rows(tok_idx=tensor(9, dtype=torch.int32), tok_off=1 << 33, n_tokens=9)), {"stream": 5})]
     for form, kw in forms:
         args = call(name, **form)
         assert record(name, args, kw, True) == record(name, args, kw, False)
@@ -127,6 +141,8 @@ def test_other_forms_go_to_ctypes(paths, name):
                   dict(txt=text(), d=drafts(n_tokens=1 << 40), ws=ws), dict(txt=text(), d=drafts(mask="m"), ws=ws)]
     if "path" in name:
         forms += [dict(txt=None, d=drafts()), dict(txt=text(), d=drafts(), n=1 << 40), dict(txt=text(), d=drafts(), n="3")]
+    if "compress" in name:
+        forms += [dict(rw="rows"), dict(rw=rows(strides=[1, 2, 3])), dict(rw=rows(n_tokens=1 << 31)), dict(rw=rows(tok_off="x"))]
     for form in forms:
         args = call(name, **{"n": 5, **form})
         assert fast(*args, None, *([None] if "attn" in name else [])) is None
