@@ -937,21 +937,21 @@ rk_status rk_compress_quant(rk_ctx* ctx, const rk_layout* L, const rk_rows* keys
     if (s != RK_OK) return s;
     s = check_rows(ctx, L, values, "values");
     if (s != RK_OK) return s;
-    if (!R_r || !k_q8 || !v_q8) return fail(ctx, RK_ERR_INVALID_ARG, "compress_q8: R_r, k_q8 or v_q8 is NULL");
+    if (!R_r || !k_q8 || !v_q8) return fail(ctx, RK_ERR_INVALID_ARG, "compress_quant: R_r, k_q8 or v_q8 is NULL");
     if (((uintptr_t)k_q8 & 15) || ((uintptr_t)v_q8 & 15))
-        return fail(ctx, RK_ERR_INVALID_ARG, "compress_q8: the caches must be 16-byte aligned");
+        return fail(ctx, RK_ERR_INVALID_ARG, "compress_quant: the caches must be 16-byte aligned");
     if (values->n_tokens != keys->n_tokens || values->tok_idx != keys->tok_idx || values->tok_off != keys->tok_off ||
         values->n_tokens_dev != keys->n_tokens_dev)
-        return fail(ctx, RK_ERR_INVALID_ARG, "compress_q8: values must use the same row selection as keys");
+        return fail(ctx, RK_ERR_INVALID_ARG, "compress_quant: values must use the same row selection as keys");
     if (keys->n_tokens > L->capacity)
-        return fail(ctx, RK_ERR_CAPACITY, "compress_q8: %d rows exceed capacity %d", keys->n_tokens, L->capacity);
+        return fail(ctx, RK_ERR_CAPACITY, "compress_quant: %d rows exceed capacity %d", keys->n_tokens, L->capacity);
     if (ctx->device == RK_DEVICE_NONE) return fail(ctx, RK_ERR_NO_DEVICE, "valid arguments, but the context has no device");
     DeviceGuard dev(ctx->device);
     hipError_t e = dev.status;
     if (e != hipSuccess) return hip_fail(ctx, e, "hipSetDevice");
     e = launch_compress_q8(L->dtype, to_dev(keys), to_dev(values), L->batch, L->n_kv_heads, L->capacity, L->keep, R_r, k_q8, v_q8,
                            seq_len_out, ctx->n_cu, as_stream(stream));
-    return e == hipSuccess ? RK_OK : hip_fail(ctx, e, "compress_q8 launch");
+    return e == hipSuccess ? RK_OK : hip_fail(ctx, e, "compress_quant launch");
 }
 
 rk_status rk_append_quant(rk_ctx* ctx, const rk_layout* L, const void* k_new, const void* v_new, const float* R_r, void* k_q8,
@@ -961,18 +961,18 @@ rk_status rk_append_quant(rk_ctx* ctx, const rk_layout* L, const void* k_new, co
     rk_status s = check_layout(ctx, L);
     if (s != RK_OK) return s;
     if (!k_new || !v_new || !R_r || !k_q8 || !v_q8 || !L->seq_len || !seq_len_out)
-        return fail(ctx, RK_ERR_INVALID_ARG, "append_q8: NULL pointer");
+        return fail(ctx, RK_ERR_INVALID_ARG, "append_quant: NULL pointer");
     if (((uintptr_t)k_q8 & 15) || ((uintptr_t)v_q8 & 15))
-        return fail(ctx, RK_ERR_INVALID_ARG, "append_q8: the caches must be 16-byte aligned");
+        return fail(ctx, RK_ERR_INVALID_ARG, "append_quant: the caches must be 16-byte aligned");
     if (L->max_seq_len + 1 > L->capacity)
-        return fail(ctx, RK_ERR_CAPACITY, "append_q8: %d + 1 rows exceed capacity %d", L->max_seq_len, L->capacity);
+        return fail(ctx, RK_ERR_CAPACITY, "append_quant: %d + 1 rows exceed capacity %d", L->max_seq_len, L->capacity);
     if (ctx->device == RK_DEVICE_NONE) return fail(ctx, RK_ERR_NO_DEVICE, "valid arguments, but the context has no device");
     DeviceGuard dev(ctx->device);
     hipError_t e = dev.status;
     if (e != hipSuccess) return hip_fail(ctx, e, "hipSetDevice");
     e = launch_append_q8(L->dtype, L->batch, L->n_kv_heads, L->capacity, L->keep, k_new, v_new, R_r, k_q8, v_q8, L->seq_len,
                          seq_len_out, ctx->tickets, as_stream(stream));
-    return e == hipSuccess ? RK_OK : hip_fail(ctx, e, "append_q8 launch");
+    return e == hipSuccess ? RK_OK : hip_fail(ctx, e, "append_quant launch");
 }
 
 rk_status rk_unpack_cache_quant(rk_ctx* ctx, const rk_layout* L, const void* k_q8, const void* v_q8, void* k_rows, void* v_rows,
@@ -982,16 +982,16 @@ rk_status rk_unpack_cache_quant(rk_ctx* ctx, const rk_layout* L, const void* k_q
     rk_status s = check_layout(ctx, L);
     if (s != RK_OK) return s;
     if (!k_q8 || (v_rows && !v_q8) || (!k_rows && !v_rows))       // (the steps of the Values lie beside the Keys')
-        return fail(ctx, RK_ERR_INVALID_ARG, "unpack_q8: nothing to do or source missing");
+        return fail(ctx, RK_ERR_INVALID_ARG, "unpack_quant: nothing to do or source missing");
     if (((uintptr_t)k_q8 & 15) || ((uintptr_t)v_q8 & 15))
-        return fail(ctx, RK_ERR_INVALID_ARG, "unpack_q8: the caches must be 16-byte aligned");
+        return fail(ctx, RK_ERR_INVALID_ARG, "unpack_quant: the caches must be 16-byte aligned");
     if (ctx->device == RK_DEVICE_NONE) return fail(ctx, RK_ERR_NO_DEVICE, "valid arguments, but the context has no device");
     DeviceGuard dev(ctx->device);
     hipError_t e = dev.status;
     if (e != hipSuccess) return hip_fail(ctx, e, "hipSetDevice");
     e = launch_unpack_q8(L->dtype, L->batch, L->n_kv_heads, L->capacity, L->keep, k_q8, v_q8, L->seq_len, k_rows, v_rows,
                          as_stream(stream));
-    return e == hipSuccess ? RK_OK : hip_fail(ctx, e, "unpack_q8 launch");
+    return e == hipSuccess ? RK_OK : hip_fail(ctx, e, "unpack_quant launch");
 }
 
 size_t rk_tree_workspace_size(const rk_ctx* ctx, const rk_layout* L, int32_t n_tokens)
