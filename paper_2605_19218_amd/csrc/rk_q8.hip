@@ -5,7 +5,7 @@
 // the codes are made with the rounded one (it costs at most 2^-7 of the step itself, and halves what the steps take).  A row with an infinity or
 // a NaN has s = NaN: all of it reads back as NaN.  A row whose largest element is below 2^-100 has s = 0 (1 / s stays finite).
 // What bounds these kernels is memory; the layout (rk_device.hpp) is made for the attention that reads it.  Measured at r = 64 in bf16: 32 heads x 16384 prompt
-// tokens written in 86 us (380 MB, 4.4 TB/s), read back in 45 (304 MB, 6.7 TB/s); a token of 64 x 32 heads appended in 16.6 us (67 MB of R_r, 4.1
+// tokens written in 86 us (380 MB, 4.4 TB/s), read back in 44 (304 MB, 6.9 TB/s); a token of 64 x 32 heads appended in 13.6 us (67 MB of R_r, 4.9
 // TB/s), of 8 heads, r = 32, in 4.
 #include "rk_kernels.hpp"
 
@@ -315,7 +315,9 @@ __global__ __launch_bounds__(256) void append_q8(int Hkv, int cap, int r, const 
 
 // ---------------------------------------------------------------------------
 // Both caches back to rows, a wave a block of 32 tokens: what was read 16 bytes a lane is written as whole rows, the Values by the same
-// transpose of bytes as above.  Bound by memory (5 of 7 bytes are written at r = 64 in bf16).
+// transpose of bytes as above.  Bound by memory (two of three bytes are written at r = 64 in bf16), for short heads by the round trips to the length and
+// to the codes: PIECES, of a lane's Keys (R / 32), are counted at compile time so that all loads of a block are in flight at once (64 x 32 heads of up to 150
+// tokens, appended to and read back: 45.7 us with three round trips a block, 44.6).
 __device__ __forceinline__ float code_at(uint32_t w, int i) { return (float)((int32_t)(w << (24 - 8 * i)) >> 24); }
 __device__ __forceinline__ void store8(bf16_t* p, const float (&x)[8])
 {
@@ -330,7 +332,7 @@ __device__ __forceinline__ void store8(float* p, const float (&x)[8])
     nt_store16(p + 4, make_uint4(__float_as_uint(x[4]), __float_as_uint(x[5]), __float_as_uint(x[6]), __float_as_uint(x[7])));
 }
 
-template <typename T>
+template <typename T, int PIECES>
 __global__ __launch_bounds__(256) void unpack_q8(int Hkv, int cap, int r, const uint8_t* __restrict__ Kq, const uint8_t* __restrict__ Vq,
                                                  const int32_t* __restrict__ seq_len, T* __restrict__ k_rows, T* __restrict__ v_rows)
 {
@@ -340,28 +342,46 @@ __global__ __launch_bounds__(256) void unpack_q8(int Hkv, int cap, int r, const 
     const int t0 = (blockIdx.x * 4 + (threadIdx.x >> 6)) * 32;
     const int len = seq_len ? min(max(seq_len[b], 0), cap) : cap;
     if (t0 >= len) return;
-    const int rp = keep_padded(r);
+    const int rp = keep_padded(r), octs = (r + 7) / 8;
     const size_t blocks = slab_tokens(cap) / 32;
     const uint8_t* kb = Kq + (u * blocks + (t0 >> 5)) * q8_kblock(rp);
-    const uint16_t* steps = (const uint16_t*)(kb + 32 * rp);
-    auto step = [&](int tl, int which) { return __uint_as_float((uint32_t)steps[2 * tl + which] << 16); };
+    const uint32_t* steps = (const uint32_t*)(kb + 32 * rp);       // (Key, Value) of a token
+    // everything is asked for first: the Values' codes and steps, the Keys' pieces (consecutive lanes take consecutive octets of a token: whole rows are
+    // written; the last pieces may be read twice)
+    uint2 raw[8];
+    uint4 vst[2];
+    if (v_rows) {
+        const uint8_t* from = Vq + (u * blocks + (t0 >> 5)) * (size_t)(32 * D) + (n >> 2) * 1024 + g * 256 + (n & 1) * 128 + (n & 2) * 4;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) raw[k] = *(const uint2*)(from + 16 * k);
+#pragma unroll
+        for (int tb = 0; tb < 2; ++tb) vst[tb] = *(const uint4*)(steps + 16 * tb + 4 * g);
+    }
     if (k_rows) {
-        // consecutive lanes take consecutive octets of a token: whole rows are written
-        const int octs = (r + 7) / 8;
+        uint4 piece[PIECES];
+        uint32_t kst[PIECES][2];
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            const int p = min(lane + 64 * i, 16 * octs - 1), tn = p / octs, oct = p - tn * octs;
+            piece[i] = *(const uint4*)(kb + oct * 256 + tn * 16);
+            kst[i][0] = steps[tn];
+            kst[i][1] = steps[16 + tn];
+        }
         const bool wide = r % 8 == 0 && ((uintptr_t)k_rows & 15) == 0;
         T* to = k_rows + (u * cap + t0) * (size_t)r;
-        for (int p = lane; p < 16 * octs; p += 64) {
-            const int tn = p / octs, oct = p - tn * octs;
-            const uint4 raw = *(const uint4*)(kb + oct * 256 + tn * 16);
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            const int p = lane + 64 * i, tn = p / octs, oct = p - tn * octs;
+            if (p >= 16 * octs) break;
 #pragma unroll
             for (int tb = 0; tb < 2; ++tb) {
                 const int tl = 16 * tb + tn;
                 if (t0 + tl >= len) continue;
-                const float s = step(tl, 0);
+                const float s = __uint_as_float(kst[i][tb] << 16);
                 float x[8];
 #pragma unroll
                 for (int c = 0; c < 8; ++c) {
-                    const uint32_t w = tb ? (c < 4 ? raw.z : raw.w) : (c < 4 ? raw.x : raw.y);
+                    const uint32_t w = tb ? (c < 4 ? piece[i].z : piece[i].w) : (c < 4 ? piece[i].x : piece[i].y);
                     x[c] = code_at(w, c & 3) * s;
                 }
                 T* at = to + (size_t)tl * r + 8 * oct;
@@ -375,16 +395,13 @@ __global__ __launch_bounds__(256) void unpack_q8(int Hkv, int cap, int r, const 
     }
     if (v_rows) {
         const bool wide = ((uintptr_t)v_rows & 15) == 0;
-        const uint8_t* from = Vq + (u * blocks + (t0 >> 5)) * (size_t)(32 * D) + (n >> 2) * 1024 + g * 256 + (n & 1) * 128 + (n & 2) * 4;
         T* to = v_rows + (u * cap + t0) * (size_t)D;
-        uint2 raw[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) raw[k] = *(const uint2*)(from + 16 * k);
 #pragma unroll
         for (int jj = 0; jj < 8; ++jj) {
             const int tl = jj < 4 ? 4 * g + jj : 12 + 4 * g + jj;
             if (t0 + tl >= len) continue;
-            const float s = step(tl, 1);
+            const uint4 w = vst[jj >> 2];
+            const float s = __uint_as_float(((jj & 3) == 0 ? w.x : (jj & 3) == 1 ? w.y : (jj & 3) == 2 ? w.z : w.w) & 0xffff0000u);
             float x[8];
 #pragma unroll
             for (int k = 0; k < 8; ++k) x[k] = code_at(jj < 4 ? raw[k].x : raw[k].y, jj & 3) * s;
@@ -452,11 +469,19 @@ hipError_t launch_unpack_q8(int dtype, int B, int Hkv, int cap, int r, const voi
                             void* v_rows, hipStream_t st)
 {
     const dim3 grid((cap + 127) / 128, Hkv, B);
-    if (dtype == 0)
-        unpack_q8<float><<<grid, 256, 0, st>>>(Hkv, cap, r, (const uint8_t*)Kq, (const uint8_t*)Vq, seq_len, (float*)k_rows, (float*)v_rows);
-    else
-        unpack_q8<bf16_t><<<grid, 256, 0, st>>>(Hkv, cap, r, (const uint8_t*)Kq, (const uint8_t*)Vq, seq_len, (bf16_t*)k_rows, (bf16_t*)v_rows);
-    return hipGetLastError();
+    auto go = [&](auto t) {
+        typedef decltype(t) T;
+        const uint8_t *kq = (const uint8_t*)Kq, *vq = (const uint8_t*)Vq;
+        T *k = (T*)k_rows, *v = (T*)v_rows;
+        switch ((r + 31) / 32) {
+            case 1: unpack_q8<T, 1><<<grid, 256, 0, st>>>(Hkv, cap, r, kq, vq, seq_len, k, v); break;
+            case 2: unpack_q8<T, 2><<<grid, 256, 0, st>>>(Hkv, cap, r, kq, vq, seq_len, k, v); break;
+            case 3: unpack_q8<T, 3><<<grid, 256, 0, st>>>(Hkv, cap, r, kq, vq, seq_len, k, v); break;
+            default: unpack_q8<T, 4><<<grid, 256, 0, st>>>(Hkv, cap, r, kq, vq, seq_len, k, v); break;
+        }
+        return hipGetLastError();
+    };
+    return dtype == 0 ? go(0.f) : go(bf16_t{});
 }
 
 }  // namespace rk
