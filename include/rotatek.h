@@ -16,7 +16,7 @@
  *     rk_destroy (512 KB of counters) and the fixed scratch array behind
  *     rk_decode_attn_static; no other call allocates or frees.
  *   - A context holds small device counters that rk_append and every decode entry
- *     point use and leave at zero.  Calls on ONE context must
+ *     point use and leave at zero (where a call does not, its comment says so).  Calls on ONE context must
  *     therefore not overlap in time on the GPU (use one stream per context, or
  *     one context per stream); calls on different contexts are independent.
  *   - All kernels are enqueued on the caller's stream (`stream` is a
@@ -437,7 +437,8 @@ rk_status rk_unpack_cache_quant(rk_ctx* ctx, const rk_layout* L, const void* k_q
 size_t rk_tree_workspace_size(const rk_ctx* ctx, const rk_layout* L, int32_t n_tokens);
 
 /* rk_decode_attn_dual over 8-bit caches; text may be NULL (rk_decode_attn over them).  q and out: [B,H_q,d].
- * 16-byte aligned: q, both caches, workspace.  Calls on one context must not overlap.  A sequence with nothing to attend yields zeros.
+ * 16-byte aligned: q, both caches, workspace.  Calls with workspaces of their own may overlap, on one context too.
+ * A sequence with nothing to attend yields zeros.
  * Errors: INVALID_ARG, UNSUPPORTED, CAPACITY (max_seq_len > capacity), WORKSPACE, HIP.                         */
 rk_status rk_decode_attn_quant(rk_ctx* ctx, const rk_layout* L, const void* q, const void* k_q8, const void* v_q8,
                             const float* R_r, const float* delta_mu, const rk_text* text, float scale, void* out,
@@ -449,8 +450,8 @@ rk_status rk_decode_attn_quant(rk_ctx* ctx, const rk_layout* L, const void* q, c
  * text rows of rk_decode_attn_dual), under ONE softmax; a row that sees nothing is zeros.  What a row does not
  * see does not touch it, also where it is an infinity or a NaN.  Rows of out from the sequence's count of drafts on
  * stay as they were.  Nothing is appended: rk_append_text_path takes the accepted drafts into the text segment.
- * B T H_q at most 2^31 - 1.  Workspace: rk_tree_workspace_size(ctx, L, T), 16-byte aligned, as q and the caches are; calls on one
- * context must not overlap.  The cache is the one of rk_compress, or of rk_compress_quant for the second.
+ * B T H_q at most 2^31 - 1.  Workspace: rk_tree_workspace_size(ctx, L, T), 16-byte aligned, as q and the caches are; calls with
+ * workspaces of their own may overlap.  The cache is the one of rk_compress, or of rk_compress_quant for the second.
  * Errors: INVALID_ARG (a malformed text or drafts too), UNSUPPORTED, CAPACITY (max_seq_len > capacity), WORKSPACE, HIP. */
 rk_status rk_decode_attn_tree(rk_ctx* ctx, const rk_layout* L, const void* q, const void* k_packed, const void* v_cache,
                               const float* R_r, const float* delta_mu, const rk_text* text, const rk_drafts* drafts,

@@ -523,7 +523,7 @@ struct PlainRowsF32 {
     }
 };
 
-// q R_r of this work-group's rows into qt [16][R + 4], and q . delta_mu of row n of each block: D^T[j][row] = R_r^T . q^T, column blocks
+// q R_r of this work-group's rows into qt [16][R + 4], and q . delta_mu of row n: D^T[j][row] = R_r^T . q^T, column blocks
 // of R_r shared by the waves.  q in bf16 is exact and R_r goes as head and remainder; in fp32 all of it is fp32.  load() asks for
 // everything, make() waits for it.
 template <typename T, int R> struct Rotation;

@@ -109,6 +109,20 @@ def test_captured_round(ctx, q8, T):  # noqa: F811
         assert torch.equal(a.k, b.k) and torch.equal(a.v, b.v) and torch.equal(a.tk, b.tk) and torch.equal(a.tv, b.tv)
 
 
+@pytest.mark.parametrize("T", [1, 3, 16, 40])
+def test_calls_on_one_context_at_once(ctx, blocks, T):  # noqa: F811
+    """Attention keeps nothing in the context: calls with workspaces of their own may overlap."""
+    xs = [Layer(ctx, np.random.default_rng(31 + i), BF, bool(i & 1), 2, 16, 4, 64, [3000, 2000], [40, 3], T, [T, (T + 1) // 2]) for i in range(3)]
+    streams = [torch.cuda.Stream() for _ in xs]
+    torch.cuda.synchronize()
+    for _ in range(6):
+        for x, s in zip(xs, streams):
+            x.call(stream=s)
+    torch.cuda.synchronize()
+    for x in xs:
+        x.check()
+
+
 @pytest.mark.parametrize("bound", [0, 220000])
 @pytest.mark.parametrize("M", [0, 70])
 @pytest.mark.parametrize("Hq", [33, 48, 130])
