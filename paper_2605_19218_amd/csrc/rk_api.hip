@@ -326,8 +326,8 @@ size_t rows_ws(const rk_ctx* ctx, const rk_layout* L, int T)
 // tokens each; of the kernels of many rows 32 tokens with 128 rows, 64 with 64) takes, at r = 64, with 16 rows bf16 0.37, fp32 1.8, 8 bits 0.67 (fp32
 // rows 0.9), with many 0.72 and 1.2; a step of full-width rows 2 to 3, which is their latency.  All work-groups of few rows cannot be faster than the
 // device streams; of many rows two share a compute unit and each takes half as long again.  A split more is a partial a row, written and read.  The
-// splits of full-width rows come last: they run beside the others while there is room for two work-groups a compute unit (of few rows), and behind them
-// otherwise.  Measured with each count (us): one token over 8 bits, 8 units x 30000 / 8 tokens, r = 64: 8 splits 31.0, 16 20.0, 32 15.1, 48 13.9; 16 x 8 units x
+// splits of full-width rows come last: they run beside the others while there is room for two work-groups a compute unit (of few rows; over an fp32 cache, whose
+// registers leave room for one, some 5 behind: 20 rows, 32 x 2000 tokens 29.3 with 4 splits, 26.3 with 3; 32 x 8000 57.5 and 61.1), and behind them otherwise.  Measured with each count (us): one token over 8 bits, 8 units x 30000 / 8 tokens, r = 64: 8 splits 31.0, 16 20.0, 32 15.1, 48 13.9; 16 x 8 units x
 // 600, r = 128: 1 12.1, 2 13.4, 4 15.6; 32 rows, 32 x 16000: 2 64.1, 3 50.4, 4 44.1, 6 52.9, 8 46.1; 8 x 16000: 8 18.0, 12 16.4, 16 16.4, 24 18.6; 448
 // rows over 8 bits, 32 x 16384: 2 291, 4 243, 6 264, 8 259.
 RowsPlan rows_plan(const rk_ctx* ctx, const rk_layout* L, int T, int text_rows, bool drafts, bool q8)
@@ -355,7 +355,7 @@ RowsPlan rows_plan(const rk_ctx* ctx, const rk_layout* L, int T, int text_rows, 
         double v = (nv + sv - 1) / sv * tv * shared, r = sr ? (nr + sr - 1) / sr * tr * shared : 0.0, behind = 0.0;
         v = v > stream ? v + 0.35 * stream : stream + 0.35 * v;
         const int64_t rounds = (groups * sv + n_wg - 1) / n_wg;
-        if (W > rounds * n_wg) behind = !block && W <= 2 * n_cu ? 0.2 * r : 6.0 + r;
+        if (W > rounds * n_wg) behind = block || W > 2 * n_cu ? 6.0 + r : f32 && !q8 ? 3.0 + 0.5 * r : 0.2 * r;
         else if (rounds == 1 && r > v) v = r;
         const double merge = S == 1 ? 0.0 : 2.5 + S / 32.0 + (double)rows * units * S * 1040 / 5e6;
         return (6.0 + v) * rounds + behind + merge;
