@@ -11,18 +11,36 @@
 
 namespace rk {
 
-// The step of a row from the bits of its largest magnitude, as bf16 bits, and 1 / s (0 where every code is 0).  By products with 1 / 127 (which falls
-// short of it by 4e-9 of itself: a quotient that is a bfloat16 comes out as that) and the reciprocal's 1 ulp: the two divisions, ten rows a lane and
-// block, were a third of the kernel's instructions.
-__device__ __forceinline__ uint32_t row_step(uint32_t top, float& inv)
+// The step of a row from the bits of its largest magnitude, and 1 / s to 1 ulp (0 where every code is 0).  The product with 1 / 127 falls short of the quotient by
+// 4e-9 of itself, so that a quotient that is a bfloat16 comes out as that; one that lies a rounding above it comes down to it (two of 2^23 magnitudes a binade), which
+// the remainder shows: 127 s has 15 bits.  Every magnitude of a binade was compared with the quotient in 64 bits.  (The two divisions, ten rows a lane
+// and block, were a third of the kernel's instructions.)
+__device__ __forceinline__ float row_step(uint32_t top, float& inv)
 {
-    const uint32_t up = (__float_as_uint(__uint_as_float(top) * (1.f / 127.f)) + 0xffffu) & 0xffff0000u;
+    uint32_t up = (__float_as_uint(__uint_as_float(top) * (1.f / 127.f)) + 0xffffu) & 0xffff0000u;
+    up += fmaf(-127.f, __uint_as_float(up), __uint_as_float(top)) > 0.f ? 0x10000u : 0u;
     const bool finite = top < 0x7f800000u, tiny = top < 0x0d800000u;        // 2^-100
     inv = finite && !tiny ? __builtin_amdgcn_rcpf(__uint_as_float(up)) : 0.f;
-    return !finite ? 0x7fc0u : tiny ? 0u : up >> 16;
+    return __uint_as_float(!finite ? 0x7fc00000u : tiny ? 0u : up);
 }
-// the code in the low byte: 1.5 2^23 + c is c's two's complement there, and the sum is rounded once, to the nearest even
-__device__ __forceinline__ uint32_t code_of(float x, float inv) { return __float_as_uint(fmaf(x, inv, 12582912.f)); }
+// The code, in the low byte: 1.5 2^23 + c is c's two's complement there, and the sum is rounded once, to the nearest even.  x / s as a division rounds it: x times the
+// reciprocal, and the remainder, which is exact since s has 8 bits, once more by it.  A quotient half way between two codes then comes out as that, and no other one
+// does: the next lie more than half a unit of fp32's last place away.  (x / s of every step's and every fp32 x's mantissa was compared in 64 bits, with reciprocals off by a unit
+// each way.  x times the reciprocal alone takes the other code for some of the ties, which a twentieth of normal bfloat16 rows have.)  A row that is no
+// number gets any code: its step is NaN.
+__device__ __forceinline__ uint32_t code_of(float x, float s, float inv)
+{
+    const float q = x * inv;
+    return __float_as_uint(fmaf(fmaf(-q, s, x), inv, q) + 12582912.f);
+}
+// Of a bfloat16 x: what is no tie lies 2^-9 and more from one, so that the quotient rounded to 2^-11 (the last place at 1.5 2^12) tells them apart, and two
+// operations do (every x and step, as above; with four, 32 heads x 16384 tokens written and read back took 133.5 us for 132.7).
+__device__ __forceinline__ uint32_t code_of_bf16(float x, float inv) { return __float_as_uint(fmaf(x, inv, 6144.f) + (12582912.f - 6144.f)); }
+template <typename T>
+__device__ __forceinline__ uint32_t code_of_stored(float x, float s, float inv)
+{
+    return sizeof(T) == 2 ? code_of_bf16(x, inv) : code_of(x, s, inv);
+}
 __device__ __forceinline__ uint32_t low_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d)
 {
     return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0c0c0400u), __builtin_amdgcn_perm(b, a, 0x0c0c0400u), 0x05040100u);
@@ -173,8 +191,7 @@ __global__ __launch_bounds__(256) void compress_q8(RowsDev keys, RowsDev vals, i
                 }
             }
         }
-        float inv[2];
-        uint32_t ks[2];
+        float inv[2], ks[2];
 #pragma unroll
         for (int tb = 0; tb < 2; ++tb) {
             uint32_t top = 0;
@@ -193,7 +210,7 @@ __global__ __launch_bounds__(256) void compress_q8(RowsDev keys, RowsDev vals, i
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const f32x4 a = acc[tb][jb + e];
-                    w[e] = low_bytes(code_of(a[0], inv[tb]), code_of(a[1], inv[tb]), code_of(a[2], inv[tb]), code_of(a[3], inv[tb]));
+                    w[e] = low_bytes(code_of(a[0], ks[tb], inv[tb]), code_of(a[1], ks[tb], inv[tb]), code_of(a[2], ks[tb], inv[tb]), code_of(a[3], ks[tb], inv[tb]));
                 }
                 // odd lane groups give their half of jb and get the even ones' half of jb + 1
                 const auto x = __builtin_amdgcn_permlane16_swap(w[0], w[1], false, false);
@@ -209,12 +226,12 @@ __global__ __launch_bounds__(256) void compress_q8(RowsDev keys, RowsDev vals, i
         }
         {
             const int tl = 16 * (g & 1) + n;
-            if (g < 2 && t0 + tl < n_b) steps[2 * tl] = (uint16_t)(g ? ks[1] : ks[0]);
+            if (g < 2 && t0 + tl < n_b) steps[2 * tl] = (uint16_t)(__float_as_uint(g ? ks[1] : ks[0]) >> 16);
         }
 
         // ---- Values
-        uint32_t lo4[8], hi4[8], vs[8];
-        float vinv[8];
+        uint32_t lo4[8], hi4[8];
+        float vs[8], vinv[8];
 #pragma unroll
         for (int jj = 0; jj < 8; ++jj) {
             uint32_t top = 0;
@@ -222,14 +239,15 @@ __global__ __launch_bounds__(256) void compress_q8(RowsDev keys, RowsDev vals, i
             for (int k = 0; k < 8; ++k) top = max(top, mag(xv[jj][k]));
             vs[jj] = row_step(row16_umax(top), vinv[jj]);
         }
+        auto code = [&](float x, int jj) { return code_of_stored<T>(x, vs[jj], vinv[jj]); };
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            lo4[k] = low_bytes(code_of(xv[0][k], vinv[0]), code_of(xv[1][k], vinv[1]), code_of(xv[2][k], vinv[2]), code_of(xv[3][k], vinv[3]));
-            hi4[k] = low_bytes(code_of(xv[4][k], vinv[4]), code_of(xv[5][k], vinv[5]), code_of(xv[6][k], vinv[6]), code_of(xv[7][k], vinv[7]));
+            lo4[k] = low_bytes(code(xv[0][k], 0), code(xv[1][k], 1), code(xv[2][k], 2), code(xv[3][k], 3));
+            hi4[k] = low_bytes(code(xv[4][k], 4), code(xv[5][k], 5), code(xv[6][k], 6), code(xv[7][k], 7));
         }
         uint32_t mine = 0;
 #pragma unroll
-        for (int jj = 0; jj < 8; ++jj) mine = n == jj ? vs[jj] : mine;
+        for (int jj = 0; jj < 8; ++jj) mine = n == jj ? __float_as_uint(vs[jj]) >> 16 : mine;
         {
             const int tl = (n & 7) < 4 ? 4 * g + (n & 7) : 12 + 4 * g + (n & 7);
             if (n < 8 && t0 + tl < n_b) steps[2 * tl + 1] = (uint16_t)mine;
@@ -297,15 +315,15 @@ __global__ __launch_bounds__(256) void append_q8(int Hkv, int cap, int r, const 
     if ((tid & 63) == 0) tops[wave] = top;
     __syncthreads();
     float inv;
-    const uint32_t step = row_step(max(tops[2 * half], tops[2 * half + 1]), inv);
+    const float step = row_step(max(tops[2 * half], tops[2 * half + 1]), inv);
     if (room) {
         const int rp = keep_padded(r);
         const size_t blocks = slab_tokens(cap) / 32;
         uint8_t* kb = Kq + ((size_t)u * blocks + (len >> 5)) * q8_kblock(rp);
-        const uint8_t code = (uint8_t)code_of(x, inv);
+        const uint8_t code = (uint8_t)code_of(x, step, inv);
         if (half) Vq[(size_t)u * blocks * (32 * D) + q8_vidx(len, j)] = code;
         else if (j < rp) kb[q8_kplace(len, j)] = code;
-        if (j == 0) ((uint16_t*)(kb + 32 * rp))[2 * (len & 31) + half] = (uint16_t)step;
+        if (j == 0) ((uint16_t*)(kb + 32 * rp))[2 * (len & 31) + half] = (uint16_t)(__float_as_uint(step) >> 16);
     }
     if (tid == 0 && atomicAdd(tickets + (size_t)b * apart, 1) == Hkv - 1) {
         tickets[(size_t)b * apart] = 0;
