@@ -401,8 +401,8 @@ rk_status rk_append_text_decode_attn_dual(rk_ctx* ctx, const rk_layout* L, const
 /* ---- the caches in 8 bits -------------------------------------------------------
  * Half the bytes of a bf16 cache: a row x of a head (the rotated Key k R_r, in fp32, or a Value) is held as
  * whole numbers c = round(x / s), ties to even, |c| <= 127, and one step s for the row, max |x| / 127 rounded up
- * to a bfloat16; what is read back is c s.  (Quotients and k R_r are rounded as fp32 arithmetic does, k R_r with bf16
- * products to 2^-16 of |k| |R_r|, so that a value within that of the middle between two codes may take either.)
+ * to a bfloat16; what is read back is c s.  (Both are exactly that, for any Value and any k R_r in fp32.  k R_r itself is of fp32 products
+ * and sums, in an order of each entry point's own: a value within their rounding of the middle between two codes may take either.)
  * A row with an infinity or a NaN reads back as NaN; one whose largest magnitude is below 2^-100 as zeros.
  * L->dtype is the type of Keys, Values, q, out and rows read back; the caches are byte buffers of
  * rk_cache_bytes_quant() bytes, 16-byte aligned, in a layout of their own (blocks of 32 tokens; slabs spaced as in the

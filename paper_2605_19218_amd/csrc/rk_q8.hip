@@ -90,24 +90,47 @@ __device__ __forceinline__ void load8(const float* p, float (&x)[8])
 }
 
 // ---------------------------------------------------------------------------
-// Prompt rows.  A wave takes blocks of 32 tokens.  Keys: D^T[channel j][token] = R_r^T . K^T on v_mfma_f32_16x16x32_bf16, R_r as bf16 head
-// and remainder in LDS (made once a work-group), an fp32 Key likewise, without the product of the two remainders: 2^-16 of |k| |R_r|, a
-// five-hundredth of a step.  Lane (g, n) then holds channels 16 jb + 4 g ..+3 of tokens n and 16 + n: the row's maximum is two lane swaps, and
+// Prompt rows.  A wave takes blocks of 32 tokens.  Keys: D^T[channel j][token] = R_r^T . K^T on v_mfma_f32_16x16x32_bf16, R_r as three bf16 parts in LDS (made
+// once a work-group), which hold all of its 24 bits, an fp32 Key likewise, without the three smallest of the nine products (2^-24 of |k| |R_r|): k R_r is what
+// fp32 products and sums make of it, so that a token gets the same codes by a prompt and by itself but for the order of the sums (with two parts, 2^-17 of |R_r| off, one code
+// in some ten thousand was another one).  Lane (g, n) then holds channels 16 jb + 4 g ..+3 of tokens n and 16 + n: the row's maximum is two lane swaps, and
 // a swap of halves between two jb makes the 16 bytes of the layout (one octet of both tokens).
 // Values: lane (g, n) takes channels 8 n ..+7 of the eight tokens whose codes the layout puts side by side, the bytes are transposed in
 // the lane, and go through LDS into the layout.  What a unit reads is asked for before the block's arithmetic, a block a wave; three work-groups a
 // compute unit hide the rest (registers spent on fewer bank conflicts in the Values' transposition cost more than it gave: 144 us for 133,
 // written and read back).
 // Grid: (blocks of `each` tokens, h_kv, b).
-template <typename T, int R>
-__global__ __launch_bounds__(256) void compress_q8(RowsDev keys, RowsDev vals, int Hkv, int cap, int r, int each, const float* __restrict__ Rr,
-                                                   uint8_t* __restrict__ Kq, uint8_t* __restrict__ Vq, int32_t* __restrict__ seq_len_out)
+constexpr int write_waves(int R) { return R > 96 ? 8 : 4; }              // (one work-group fits into a compute unit's LDS at R = 128)
+constexpr int WRITE_V = 1024;                                            // LDS of a wave for its Value codes
+constexpr int write_lds(int R) { return R * D * 6 + write_waves(R) * WRITE_V; }
+// an fp32 Key's eight channels as three parts of 8 bits: the first cut off, so that the largest numbers have one
+__device__ __forceinline__ void key_parts(const float (&x)[8], bf16x8 (&p)[3])
 {
-    constexpr int JB = R / 16;
+    uint32_t h[4], m[4], l[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float a = x[2 * i], b = x[2 * i + 1];
+        h[i] = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+        const float ra = a - __uint_as_float(__float_as_uint(a) & 0xffff0000u), rb = b - __uint_as_float(__float_as_uint(b) & 0xffff0000u);
+        m[i] = __builtin_bit_cast(uint32_t, (bf16x2){(__bf16)ra, (__bf16)rb});
+        const float sa = ra - __uint_as_float(m[i] << 16), sb = rb - __uint_as_float(m[i] & 0xffff0000u);
+        l[i] = __builtin_bit_cast(uint32_t, (bf16x2){(__bf16)sa, (__bf16)sb});
+    }
+    p[0] = __builtin_bit_cast(bf16x8, make_uint4(h[0], h[1], h[2], h[3]));
+    p[1] = __builtin_bit_cast(bf16x8, make_uint4(m[0], m[1], m[2], m[3]));
+    p[2] = __builtin_bit_cast(bf16x8, make_uint4(l[0], l[1], l[2], l[3]));
+}
+
+template <typename T, int R>
+__global__ __launch_bounds__(64 * write_waves(R)) void compress_q8(RowsDev keys, RowsDev vals, int Hkv, int cap, int r, int each,
+                                                                   const float* __restrict__ Rr, uint8_t* __restrict__ Kq, uint8_t* __restrict__ Vq,
+                                                                   int32_t* __restrict__ seq_len_out)
+{
+    constexpr int JB = R / 16, NW = write_waves(R);
     constexpr bool F32 = sizeof(T) == 4;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-    bf16x8* frag = (bf16x8*)smem;               // [jb][i][part][lane]
-    unsigned char* vcodes = smem + R * D * 4 + (threadIdx.x >> 6) * 4096;      // this wave's block of Value codes
+    bf16x8* frag = (bf16x8*)smem;               // [i][jb][part][lane]
+    unsigned char* vcodes = smem + R * D * 6 + (threadIdx.x >> 6) * WRITE_V;
     const int h = blockIdx.y, b = blockIdx.z, u = b * Hkv + h;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, n = lane & 15;
     const int n_b = min(rows_count(keys, b), cap);
@@ -117,18 +140,20 @@ __global__ __launch_bounds__(256) void compress_q8(RowsDev keys, RowsDev vals, i
     const int blk0 = (int)first, blk1 = (int)min(first + each, (int64_t)n_b);
 
     const float* Ru = Rr + (size_t)u * D * r;
-    for (int f = wave; f < JB * 4; f += 4) {
-        const int j = 16 * (f >> 2) + n, c0 = 32 * (f & 3) + 8 * g;
-        float x[8];
+    for (int f = wave; f < JB * 4; f += NW) {
+        const int i = f / JB, j = 16 * (f - i * JB) + n, c0 = 32 * i + 8 * g;
+        bf16x8 part[3];
 #pragma unroll
         for (int jj = 0; jj < 8; ++jj) {
             const float v = Ru[(c0 + jj) * r + min(j, r - 1)];
-            x[jj] = j < r ? v : 0.f;
+            __bf16 hi, mid, lo;
+            split3_bf16(j < r ? v : 0.f, hi, mid, lo);
+            part[0][jj] = hi;
+            part[1][jj] = mid;
+            part[2][jj] = lo;
         }
-        bf16x8 hi, lo;
-        split_bf16x8(x, hi, lo);
-        frag[(2 * f) * 64 + lane] = hi;
-        frag[(2 * f + 1) * 64 + lane] = lo;
+#pragma unroll
+        for (int p = 0; p < 3; ++p) frag[(3 * f + p) * 64 + lane] = part[p];
     }
     __syncthreads();
 
@@ -145,7 +170,7 @@ __global__ __launch_bounds__(256) void compress_q8(RowsDev keys, RowsDev vals, i
     };
 
 #pragma unroll 1
-    for (int t0 = blk0 + 32 * wave; t0 < blk1; t0 += 128) {
+    for (int t0 = blk0 + 32 * wave; t0 < blk1; t0 += 32 * NW) {
         const bool full = t0 + 32 <= n_b;
         uint8_t* kb = Ku + (size_t)(t0 >> 5) * kblk;
         uint8_t* vb = Vu + (size_t)(t0 >> 5) * (32 * D);
@@ -160,34 +185,42 @@ __global__ __launch_bounds__(256) void compress_q8(RowsDev keys, RowsDev vals, i
         }
         // ---- Keys
         f32x4 acc[2][JB];
+#pragma unroll
+        for (int jb = 0; jb < JB; ++jb) acc[0][jb] = acc[1][jb] = (f32x4){0.f, 0.f, 0.f, 0.f};
         {
-            bf16x8 kh[2][4], kl[2][F32 ? 4 : 1];
+            float x[F32 ? 2 : 1][4][8];
+            bf16x8 kf[2][4];
 #pragma unroll
             for (int tb = 0; tb < 2; ++tb) {
                 const T* kr = kdata + row_of(t0 + 16 * tb + n) * keys.st + 8 * g;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    if constexpr (F32) {
-                        float x[8];
-                        load8(kr + 32 * i, x);
-                        split_bf16x8(x, kh[tb][i], kl[tb][i]);
-                    } else {
-                        kh[tb][i] = *(const bf16x8*)(kr + 32 * i);
-                    }
+                    if constexpr (F32) load8(kr + 32 * i, x[tb][i]);
+                    else kf[tb][i] = *(const bf16x8*)(kr + 32 * i);
                 }
             }
 #pragma unroll
-            for (int jb = 0; jb < JB; ++jb) {
-                acc[0][jb] = acc[1][jb] = (f32x4){0.f, 0.f, 0.f, 0.f};
+            for (int i = 0; i < 4; ++i) {
+                constexpr int NP = F32 ? 3 : 1;
+                bf16x8 k[2][NP];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const bf16x8 hi = frag[((jb * 4 + i) * 2) * 64 + lane], lo = frag[((jb * 4 + i) * 2 + 1) * 64 + lane];
+                for (int tb = 0; tb < 2; ++tb) {
+                    if constexpr (F32) key_parts(x[tb][i], k[tb]);
+                    else k[tb][0] = kf[tb][i];
+                }
 #pragma unroll
-                    for (int tb = 0; tb < 2; ++tb) {
-                        acc[tb][jb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lo, kh[tb][i], acc[tb][jb], 0, 0, 0);
-                        if constexpr (F32) acc[tb][jb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(hi, kl[tb][i], acc[tb][jb], 0, 0, 0);
-                        acc[tb][jb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(hi, kh[tb][i], acc[tb][jb], 0, 0, 0);
-                    }
+                for (int jb = 0; jb < JB; ++jb) {
+                    bf16x8 a[3];
+#pragma unroll
+                    for (int p = 0; p < 3; ++p) a[p] = frag[((i * JB + jb) * 3 + p) * 64 + lane];
+#pragma unroll
+                    for (int sum = 2; sum >= 0; --sum)              // (the smallest products first)
+#pragma unroll
+                        for (int p = sum; p >= 0; --p)
+                            if (sum - p < NP)
+#pragma unroll
+                                for (int tb = 0; tb < 2; ++tb)
+                                    acc[tb][jb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[p], k[tb][sum - p], acc[tb][jb], 0, 0, 0);
                 }
             }
         }
@@ -255,15 +288,19 @@ __global__ __launch_bounds__(256) void compress_q8(RowsDev keys, RowsDev vals, i
         // channel 8 n + k is place 8 (n % 2) + k of channel block n / 2; blocks lie in pairs
         uint8_t* to = vb + (n >> 2) * 1024 + g * 256 + (n & 1) * 128;
         if (full) {
-            // through LDS, so that a store is a kilobyte on end: from the lanes as they are, 64 bytes a lane in four stores, the
-            // stores of a block touched every line of it four times
-            unsigned char* at = vcodes + (to - vb) + (n & 2) * 4;
+            // through LDS, so that a store is a kilobyte on end (from the lanes as they are, 64 bytes a lane in four stores, the
+            // stores of a block touched every line of it four times), a kilobyte at a time: what LDS is left makes a third work-group on a compute unit
 #pragma unroll
-            for (int k = 0; k < 8; ++k) *(uint2*)(at + 16 * k) = make_uint2(lo4[k], hi4[k]);
-            wave_lds_fence();
+            for (int j = 0; j < 4; ++j) {
+                if (n >> 2 == j) {
+                    unsigned char* at = vcodes + g * 256 + (n & 1) * 128 + (n & 2) * 4;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) *(uint4*)(vb + 1024 * j + 16 * lane) = *(const uint4*)(vcodes + 1024 * j + 16 * lane);
-            wave_lds_fence();
+                    for (int k = 0; k < 8; ++k) *(uint2*)(at + 16 * k) = make_uint2(lo4[k], hi4[k]);
+                }
+                wave_lds_fence();
+                *(uint4*)(vb + 1024 * j + 16 * lane) = *(const uint4*)(vcodes + 16 * lane);
+                wave_lds_fence();
+            }
         } else {
             to += (n & 2) * 4;
 #pragma unroll
@@ -437,11 +474,11 @@ template <typename T, int R>
 static hipError_t compress_q8_r(const RowsDev& keys, const RowsDev& vals, int B, int Hkv, int cap, int r, int each, const float* Rr, uint8_t* Kq,
                                 uint8_t* Vq, int32_t* seq_len_out, hipStream_t st)
 {
-    const size_t lds = (size_t)R * D * 4 + 4 * 4096;
+    constexpr int lds = write_lds(R);
     const hipError_t e = allow_dynamic_lds((const void*)compress_q8<T, R>, lds);
     if (e != hipSuccess) return e;
     const int nb = keys.n_tokens > 0 ? (int)(((int64_t)keys.n_tokens + each - 1) / each) : 1;
-    compress_q8<T, R><<<dim3(nb, Hkv, B), 256, lds, st>>>(keys, vals, Hkv, cap, r, each, Rr, Kq, Vq, seq_len_out);
+    compress_q8<T, R><<<dim3(nb, Hkv, B), 64 * write_waves(R), lds, st>>>(keys, vals, Hkv, cap, r, each, Rr, Kq, Vq, seq_len_out);
     return hipGetLastError();
 }
 
@@ -449,13 +486,14 @@ hipError_t launch_compress_q8(int dtype, const RowsDev& keys, const RowsDev& val
                               void* Vq, int32_t* seq_len_out, int n_cu, hipStream_t st)
 {
     // Tokens of a work-group: the count whose rounds of work-groups (as many of them on a compute unit as their LDS lets) come out shortest, each counted with
-    // 16 tokens more for making R_r ready.  With 128 / 256 / 512 (us, with the rows read back, r = 64): 32768 tokens x heads 18.0 / 23.3 / 34.6, 65536 22.4
-    // / 25.5 / 36.3, 131072 42.0 / 39.7 / 52.6, 256000 73.8 / 77.2 / 75.2, 524288 138.5 / 132.6 / 158.4, 2097152 540 / 518 / 528.
-    const int64_t lds = (int64_t)((r + 31) / 32) * (32 * D * 4) + 4 * 4096, side = (int64_t)n_cu * (163840 / lds);
+    // 96 tokens more for making R_r ready.  With 128 / 256 / 512 (us): r = 64, bf16, 32768 tokens x heads 10.0 / 18.7 / 30.8, 65536 15.9 / 20.4 / 32.4, 131072 27.2 / 25.4
+    // / 34.0, 256000 48.9 / 46.6 / 45.1, 524288 109 / 98 / 110, 1280000 238 / 218 / 222; fp32 131072 40.2 / 37.8 / 43.8, 524288 174 / 165 / 159; r = 128, bf16
+    // 65536 28.7 / 19.7 / 27.3, 131072 53.8 / 37.0 / 33.9, 524288 242 / 161 / 149.
+    const int64_t R = (r + 31) / 32 * 32, side = (int64_t)n_cu * (163840 / write_lds((int)R));
     int each = 128;
     int64_t best = INT64_MAX;
-    for (int e = 128; e <= 512; e *= 2) {
-        const int64_t groups = ((int64_t)keys.n_tokens + e - 1) / e * B * Hkv, cost = (groups + side - 1) / side * (e + 16);
+    for (int e = 32 * write_waves((int)R); e <= 512; e *= 2) {
+        const int64_t groups = ((int64_t)keys.n_tokens + e - 1) / e * B * Hkv, cost = (groups + side - 1) / side * (e + 96);
         if (cost < best) { best = cost; each = e; }
     }
     auto go = [&](auto t) {

@@ -21,9 +21,14 @@ def ctx():
 
 def in_8_bits(x):
     """[..., n] float64 -> the step of each row and its codes, by the definition."""
-    m, e = np.frexp(np.abs(x).max(-1, keepdims=True) / 127)
-    s = np.ldexp(np.ceil(np.ldexp(m, 8)), e - 8)
-    return s, np.rint(x / s)
+    top = np.abs(x).max(-1, keepdims=True)
+    m, e = np.frexp(top / 127)
+    s = np.where(top < 2.0 ** -100, 0.0, np.ldexp(np.ceil(np.ldexp(m, 8)), e - 8))      # (smaller rows are zeros)
+    return s, np.rint(over(x, s))
+
+
+def over(x, s):
+    return np.where(s > 0, x / np.where(s > 0, s, 1), 0.0)
 
 
 def read_back(ctx, lay, k, v):
@@ -126,3 +131,41 @@ def test_steps_next_to_a_bfloat16(ctx, way):
     s, c = in_8_bits(f64(V))
     _, v = way(ctx, V, V, identity(1, 1, 16), F32)
     assert differ(v, c * s) == 0
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("way", [written, appended])
+@pytest.mark.parametrize("r", [16, 37, 64, 96, 128])
+@pytest.mark.parametrize("e", [-90, 0, 90])
+def test_codes_of_rotated_keys(ctx, dt, way, r, e):
+    """A Key with one channel is a row of R_r times a number: fp32 arithmetic has it but for a rounding or two (R_r in three bf16 parts: exact products, three
+    sums of 2^-23 at most), 2^-21 of itself with room, by a prompt as by a token. So a code is off by what that makes of 127, and the step is certain unless the largest element is as near
+    to a border."""
+    B, H, N = 2, 2, 1000
+    g = np.random.default_rng(r + e + 90)
+    Rr = torch.from_numpy(g.standard_normal((B, H, D, r)).astype(np.float32)).to(DEV)
+    v = torch.from_numpy((g.standard_normal((B, H, N)) * 2.0 ** e).astype(np.float32)).to(dt).to(DEV)
+    at = torch.from_numpy(g.integers(0, D, (B, H, N))).to(DEV)
+    K = torch.zeros(B, H, N, D, dtype=dt, device=DEV).scatter_(-1, at[..., None], v[..., None])
+    got, _ = way(ctx, K, K, Rr, dt)
+    x = f64(v)[..., None] * np.take_along_axis(f64(Rr), at.cpu().numpy()[..., None], 2)
+    off = 2.0 ** -21
+    s, _ = in_8_bits(x)
+    sure = (in_8_bits(x * (1 - off))[0] == s) & (in_8_bits(x * (1 + off))[0] == s)
+    assert sure.mean() > 0.99
+    c = over(got, s)
+    far = np.abs(over(x, s) - c) > 0.5 + 127 * off
+    sure = np.broadcast_to(sure, c.shape)
+    assert int((far & sure).sum()) == 0 and differ((np.rint(c) * s)[sure], got[sure]) == 0
+
+
+@pytest.mark.parametrize("way", [written, appended])
+def test_the_largest_keys_are_numbers(ctx, way):
+    """Finite fp32 Keys next to the largest: rows that are finite too."""
+    top = torch.finfo(F32).max
+    K = torch.zeros(1, 1, 40, D, device=DEV)
+    K[0, 0, range(40), range(40)] = torch.tensor([top, -top] * 20, device=DEV)
+    x = f64(K)[..., :64] * 0.5
+    s, c = in_8_bits(x[:, :, :40])
+    k, _ = way(ctx, K, K, 0.5 * identity(1, 1, 64), F32)
+    assert differ(k, c * s) == 0
