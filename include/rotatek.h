@@ -436,6 +436,12 @@ rk_status rk_unpack_cache_quant(rk_ctx* ctx, const rk_layout* L, const void* k_q
  * outside 1..RK_MAX_DRAFTS.  It does not depend on lengths: what serves one max_seq_len serves every other.   */
 size_t rk_tree_workspace_size(const rk_ctx* ctx, const rk_layout* L, int32_t n_tokens);
 
+/* How these calls share their work out: n_tokens drafts a sequence (0: rk_decode_attn_quant, 1..RK_MAX_DRAFTS the trees), text_rows the host's bound of the
+ * text (0: none), quant != 0: over 8-bit caches.  Query rows of a work-group (16, 64 or 128 of a KV head's n_tokens H_q / H_kv), splits of
+ * the cache and, behind them, of the text and the drafts.  INVALID_ARG and UNSUPPORTED as the calls.           */
+rk_status rk_tree_plan(const rk_ctx* ctx, const rk_layout* L, int32_t n_tokens, int32_t text_rows, int32_t quant,
+                       int32_t* rows_per_work_group, int32_t* n_splits, int32_t* n_text_splits);
+
 /* rk_decode_attn_dual over 8-bit caches; text may be NULL (rk_decode_attn over them).  q and out: [B,H_q,d].
  * 16-byte aligned: q, both caches, workspace.  Calls with workspaces of their own may overlap, on one context too.
  * A sequence with nothing to attend yields zeros.

@@ -30,7 +30,7 @@ EXPORTS = [
     "rk_gather_rotation", "rk_compress", "rk_append", "rk_decode_attn", "rk_cache_bytes", "rk_unpack_cache",
     "rk_decode_attn_dual", "rk_append_text", "rk_fit_subspace", "rk_query_sigma", "rk_append_decode_attn",
     "rk_append_text_decode_attn_dual", "rk_decode_attn_static", "rk_stream_read", "rk_cache_bytes_quant", "rk_compress_quant",
-    "rk_append_quant", "rk_unpack_cache_quant", "rk_tree_workspace_size", "rk_decode_attn_quant", "rk_decode_attn_tree",
+    "rk_append_quant", "rk_unpack_cache_quant", "rk_tree_workspace_size", "rk_tree_plan", "rk_decode_attn_quant", "rk_decode_attn_tree",
     "rk_decode_attn_tree_quant", "rk_append_text_path",
 ]
 RK_MAX_DRAFTS = 64
@@ -124,6 +124,7 @@ def lib():
         L.rk_unpack_cache_quant.argtypes = [vp, PL, vp, vp, vp, vp, vp]
         L.rk_tree_workspace_size.argtypes = [vp, PL, i32]
         L.rk_tree_workspace_size.restype = sz
+        L.rk_tree_plan.argtypes = [vp, PL, i32, i32, i32, C.POINTER(i32), C.POINTER(i32), C.POINTER(i32)]
         L.rk_decode_attn_quant.argtypes = [vp, PL, vp, vp, vp, vp, vp, PT, f32, vp, vp, sz, vp]
         L.rk_decode_attn_tree.argtypes = [vp, PL, vp, vp, vp, vp, vp, PT, PD, f32, vp, vp, sz, vp]
         L.rk_decode_attn_tree_quant.argtypes = [vp, PL, vp, vp, vp, vp, vp, PT, PD, f32, vp, vp, sz, vp]
@@ -459,6 +460,15 @@ def rk_unpack_cache_quant(ctx, layout: Layout, k_q8, v_q8, k_rows, v_rows, strea
 
 def rk_tree_workspace_size(ctx, layout: Layout, n_tokens: int) -> int:
     return int(lib().rk_tree_workspace_size(ctx, C.byref(layout.c()), int(n_tokens)))
+
+
+def rk_tree_plan(ctx, layout: Layout, n_tokens: int, text_rows: int = 0, quant: bool = False):
+    """(query rows of a work-group, splits of the cache, splits of the text and the drafts); n_tokens 0: rk_decode_attn_quant."""
+    p, s, t = C.c_int32(), C.c_int32(), C.c_int32()
+    st = lib().rk_tree_plan(ctx, C.byref(layout.c()), int(n_tokens), int(text_rows), int(quant), C.byref(p), C.byref(s), C.byref(t))
+    if st != RK_OK:
+        raise RotateKError(st, lib().rk_status_str(st).decode())
+    return p.value, s.value, t.value
 
 
 def rk_decode_attn_quant(ctx, layout: Layout, q, k_q8, v_q8, R_r, delta_mu, text: Optional[Text], scale: float, out, workspace,

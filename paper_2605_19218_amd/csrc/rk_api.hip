@@ -300,12 +300,14 @@ struct RowsPlan { int per, nrb, Sv, Sr; };
 // tokens, 128 rows 13.2 / 17.3 / 17.8; 8 x 16000, 96 26.4 / 35.3 / 29.6, 128 32.7 / 37.0 / 32.2; 32 x 2000, 128 21.0 / 32.0 / 27.0; 32 x 8000, 32
 // 27.4 / 38.8 / 32.0, 96 56.0 / 54.0 / 43.7; 256 x 600, 32 25.2 / 35.6 / 29.2, 64 45.9 / 42.7 / 36.6; over 8 bits: 8 x 16000, 40 21.5 / 24.3 / 31.1, 96
 // 36.3 / 34.8 / 34.8; 32 x 8000, 32 24.2 / 29.0 / 33.5, 64 38.9 / 36.6 / 43.0, 128 66.4 / 55.3 / 53.2; 128 x 2000, 64 42.6 / 38.1 / 47.1, 448 - / 169.6 /
-// 148.0.  (fp32 rows, 16 against 32 a work-group while there were such kernels: 8 x 16000, 32 35.6 / 41.5; 256 x 600, 32 67 / 58.5.)
-int rows_per_group(const rk_ctx* ctx, const rk_layout* L, int T, bool q8)
+// 148.0.  (fp32 rows, 16 against 32 a work-group while there were such kernels: 8 x 16000, 32 35.6 / 41.5; 256 x 600, 32 67 / 58.5.)  Tokens of the text count as the
+// cache's: 8 units, 64 rows, 1000 cached and 4000 of text 16.4 / - / 19.1, 30000 of text 46.3 / - / 40.7, over 8 bits 46.1 / 38.4 / 40.7; 32 units, 112 rows, 8000 of text
+// 83.8 / - / 59.5.
+int rows_per_group(const rk_ctx* ctx, const rk_layout* L, int T, int text_rows, bool q8)
 {
     const int64_t rows = (int64_t)T * (L->n_q_heads / L->n_kv_heads), units = (int64_t)L->batch * L->n_kv_heads, n_cu = ctx ? ctx->n_cu : 256;
     const int64_t blocks = (rows + 15) / 16 * units;
-    if (L->dtype == RK_F32 || rows <= 32 || (blocks <= 2 * n_cu && blocks * L->max_seq_len <= 2500 * n_cu)) return 16;
+    if (L->dtype == RK_F32 || rows <= 32 || (blocks <= 2 * n_cu && blocks * ((int64_t)L->max_seq_len + text_rows) <= 2500 * n_cu)) return 16;
     return q8 && rows <= 64 ? 64 : 128;
 }
 // partial slots of a row: what any length may take
@@ -329,11 +331,14 @@ size_t rows_ws(const rk_ctx* ctx, const rk_layout* L, int T)
 // splits of full-width rows come last: they run beside the others while there is room for two work-groups a compute unit (of few rows; over an fp32 cache, whose
 // registers leave room for one, some 5 behind: 20 rows, 32 x 2000 tokens 29.3 with 4 splits, 26.3 with 3; 32 x 8000 57.5 and 61.1), and behind them otherwise.  Measured with each count (us): one token over 8 bits, 8 units x 30000 / 8 tokens, r = 64: 8 splits 31.0, 16 20.0, 32 15.1, 48 13.9; 16 x 8 units x
 // 600, r = 128: 1 12.1, 2 13.4, 4 15.6; 32 rows, 32 x 16000: 2 64.1, 3 50.4, 4 44.1, 6 52.9, 8 46.1; 8 x 16000: 8 18.0, 12 16.4, 16 16.4, 24 18.6; 448
-// rows over 8 bits, 32 x 16384: 2 291, 4 243, 6 264, 8 259.
+// rows over 8 bits, 32 x 16384: 2 291, 4 243, 6 264, 8 259.  A text that is longer than the cache decides by itself, by its bytes and its steps on a full device (splits of
+// the text, the cache's at their best): one token over 8 bits, 8 units, 2880 cached, 100000 of text: 1 1378, 4 355, 8 185, 16 101, 24 74.4, 32 77.3, 60 78.4; 32 rows,
+// 8 units, none cached, 30000 of text: 8 54.4, 16 33.0, 24 32.5, 32 30.2, 60 33.2; fp32 32 units, 4000 cached, 12000 of text: 1 466, 4 136, 8 99.8, 12 105; 112 rows (128 a
+// work-group), 32 units, 1000 and 8000: 1 309, 4 90, 8 61.2, 12 59.5.
 RowsPlan rows_plan(const rk_ctx* ctx, const rk_layout* L, int T, int text_rows, bool drafts, bool q8)
 {
     RowsPlan p;
-    p.per = rows_per_group(ctx, L, T, q8);
+    p.per = rows_per_group(ctx, L, T, text_rows, q8);
     const int64_t units = (int64_t)L->batch * L->n_kv_heads, rows = (int64_t)T * (L->n_q_heads / L->n_kv_heads);
     p.nrb = (int)((rows + p.per - 1) / p.per);
     const bool block = p.per > 16, f32 = L->dtype == RK_F32;
@@ -348,24 +353,28 @@ RowsPlan rows_plan(const rk_ctx* ctx, const rk_layout* L, int T, int text_rows, 
     const double tr = block ? 3.0 : f32 ? 4.0 : 2.0;
     const double token = q8 ? keep_padded(L->keep) + D + 4 : (double)elem_size(L->dtype) * (keep_padded(L->keep) + D);
     const double stream = block ? 0.0 : (double)units * L->max_seq_len * token / 6.2e6;
+    // what all full-width rows take at least, however they are split: read once, and their steps on a full device
+    const double text_stream = (double)units * text * 2 * D * elem_size(L->dtype) / 6.2e6, text_steps = (double)groups * nr * (block ? 4.5 : f32 ? 4.0 : 1.3) / n_wg;
+    const double least = text_stream > text_steps ? text_stream : text_steps;
     auto cost = [&](int sv, int sr) {
         const int S = sv + sr;
         const int64_t W = groups * S;
         const double shared = block && W > n_cu ? 1.5 : 1.0;
         double v = (nv + sv - 1) / sv * tv * shared, r = sr ? (nr + sr - 1) / sr * tr * shared : 0.0, behind = 0.0;
         v = v > stream ? v + 0.35 * stream : stream + 0.35 * v;
+        if (sr && r < least) r = least;
         const int64_t rounds = (groups * sv + n_wg - 1) / n_wg;
         if (W > rounds * n_wg) behind = block || W > 2 * n_cu ? 6.0 + r : f32 && !q8 ? 3.0 + 0.5 * r : 0.2 * r;
-        else if (rounds == 1 && r > v) v = r;
+        if (behind < r - v) behind = r - v;                  // (beside the last round, and longer than it)
         const double merge = S == 1 ? 0.0 : 2.5 + S / 32.0 + (double)rows * units * S * 1040 / 5e6;
         return (6.0 + v) * rounds + behind + merge;
     };
-    const int most_v = nv < 1 ? 1 : nv < 48 ? nv : 48, r0 = nr ? 1 : 0, r1 = nr < slots / 2 ? nr : slots / 2;
+    const int most_v = nv < 1 ? 1 : nv < 48 ? nv : 48, r0 = nr ? 1 : 0, r1 = nr < slots - 1 ? nr : slots - 1;
     static const int tries[] = {1, 2, 3, 4, 5, 6, 7, 8, 10, 12, 14, 16, 20, 24, 28, 32, 40, 48};
     double best = 1e30;
     p.Sv = 1;
     p.Sr = r0;
-    for (int r = r0; r <= r1 && r <= 8; r += r < 4 ? 1 : 2) {
+    for (int r = r0; r <= r1; r += r < 4 ? 1 : r < 8 ? 2 : r < 16 ? 4 : r < 32 ? 8 : 14) {
         auto look = [&](int64_t v) {
             if (v < 1 || v > most_v || v > slots - r) return;
             const double c = cost((int)v, r);
@@ -375,7 +384,10 @@ RowsPlan rows_plan(const rk_ctx* ctx, const rk_layout* L, int T, int text_rows, 
         look(n_wg / groups - r);            // what fills the device
         look(n_wg / groups);                // without the full-width rows
     }
-    if (ctx && ctx->decode_splits > 0) p.Sv = ctx->decode_splits < slots - p.Sr ? ctx->decode_splits : slots - p.Sr;
+    if (ctx && ctx->decode_splits > 0) {
+        p.Sv = ctx->decode_splits;
+        if (p.Sr > slots - p.Sv) p.Sr = slots - p.Sv;         // (eight at least, see rows_slots)
+    }
     return p;
 }
 
@@ -998,6 +1010,19 @@ size_t rk_tree_workspace_size(const rk_ctx* ctx, const rk_layout* L, int32_t n_t
 {
     if (check_layout(nullptr, L) != RK_OK || n_tokens < 1 || n_tokens > RK_MAX_DRAFTS) return 0;
     return rows_ws(ctx, L, n_tokens);
+}
+
+rk_status rk_tree_plan(const rk_ctx* ctx, const rk_layout* L, int32_t n_tokens, int32_t text_rows, int32_t quant, int32_t* rows_per_work_group,
+                       int32_t* n_splits, int32_t* n_text_splits)
+{
+    const rk_status s = check_layout(nullptr, L);
+    if (s != RK_OK) return s;
+    if (n_tokens < 0 || n_tokens > RK_MAX_DRAFTS || text_rows < 0 || !rows_per_work_group || !n_splits || !n_text_splits) return RK_ERR_INVALID_ARG;
+    const RowsPlan p = rows_plan(ctx, L, n_tokens ? n_tokens : 1, text_rows, n_tokens > 0, quant != 0);
+    *rows_per_work_group = p.per;
+    *n_splits = p.Sv;
+    *n_text_splits = p.Sr;
+    return RK_OK;
 }
 
 static rk_status check_drafts(rk_ctx* ctx, const rk_drafts* d)
