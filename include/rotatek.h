@@ -433,7 +433,10 @@ rk_status rk_unpack_cache_quant(rk_ctx* ctx, const rk_layout* L, const void* k_q
 
 /* ---- attention of drafted tokens, and over 8-bit caches ------------------------------
  * Bytes of workspace for n_tokens query tokens a sequence (rk_decode_attn_quant: 1), 0 for an invalid layout or n_tokens
- * outside 1..RK_MAX_DRAFTS.  It does not depend on lengths: what serves one max_seq_len serves every other.   */
+ * outside 1..RK_MAX_DRAFTS: 520 bytes for each of the B n_tokens H_q query rows and of the 10 to 64 partials that a row may have (many with few
+ * rows a compute unit), and alignment.  It does not depend on lengths: what serves one max_seq_len or text serves every other.  It does depend on the
+ * context's device (NULL: 256 compute units) and on RK_OPT_DECODE_SPLITS, which N set makes N + 8 partials a row at least: ask
+ * with the context that makes the calls, after its options are set.                                             */
 size_t rk_tree_workspace_size(const rk_ctx* ctx, const rk_layout* L, int32_t n_tokens);
 
 /* How these calls share their work out: n_tokens drafts a sequence (0: rk_decode_attn_quant, 1..RK_MAX_DRAFTS the trees), text_rows the host's bound of the

@@ -61,6 +61,28 @@ def test_plans_fit_the_workspace():
         rk.rk_destroy(ctx)
 
 
+def test_workspace_by_rows_and_options():
+    """As the header has it: 520 bytes a row and partial, 10 to 64 partials, N + 8 at least once the splits are set to N; a workspace of before is refused then."""
+    ctx, P = rk.rk_create(rk.RK_DEVICE_NONE), 4096
+    try:
+        for B, Hq, Hkv, T in ((1, 32, 8, 1), (8, 28, 4, 16), (64, 32, 32, 64), (1, 1, 1, 1)):
+            L, rows = lay(B, Hq, Hkv, 64, rk.RK_BF16, 4000), B * T * Hq
+            size = rk.rk_tree_workspace_size(ctx, L, T)
+            assert size == rk.rk_tree_workspace_size(None, L, T) and 10 * 520 * rows <= size <= 64 * 520 * rows + 512
+            for N in (1, 60, 300):
+                rk.rk_set_option(ctx, rk.RK_OPT_DECODE_SPLITS, N)
+                assert rk.rk_tree_workspace_size(ctx, L, T) >= max(size, (N + 8) * 520 * rows)
+            L.seq_len = P
+            d = rk.Drafts(P, P, T, strides=(0, 0, 128))
+            for n, status in ((size, rk.RK_ERR_WORKSPACE), (rk.rk_tree_workspace_size(ctx, L, T), rk.RK_ERR_NO_DEVICE)):
+                with pytest.raises(rk.RotateKError) as e:
+                    rk.rk_decode_attn_tree(ctx, L, P, P, P, P, P, None, d, 0.0, P, P, workspace_bytes=n)
+                assert e.value.status == status
+            rk.rk_set_option(ctx, rk.RK_OPT_DECODE_SPLITS, 0)
+    finally:
+        rk.rk_destroy(ctx)
+
+
 def test_refusals():
     L = lay(1, 8, 8, 64, rk.RK_BF16, 100)
     for a in ((L, -1), (L, 65), (L, 4, -1), (lay(1, 8, 8, 0, rk.RK_BF16, 100), 4)):
