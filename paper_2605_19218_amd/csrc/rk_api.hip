@@ -334,7 +334,8 @@ size_t rows_ws(const rk_ctx* ctx, const rk_layout* L, int T)
 // rows over 8 bits, 32 x 16384: 2 291, 4 243, 6 264, 8 259.  A text that is longer than the cache decides by itself, by its bytes and its steps on a full device (splits of
 // the text, the cache's at their best): one token over 8 bits, 8 units, 2880 cached, 100000 of text: 1 1378, 4 355, 8 185, 16 101, 24 74.4, 32 77.3, 60 78.4; 32 rows,
 // 8 units, none cached, 30000 of text: 8 54.4, 16 33.0, 24 32.5, 32 30.2, 60 33.2; fp32 32 units, 4000 cached, 12000 of text: 1 466, 4 136, 8 99.8, 12 105; 112 rows (128 a
-// work-group), 32 units, 1000 and 8000: 1 309, 4 90, 8 61.2, 12 59.5.
+// work-group), 32 units, 1000 and 8000: 1 309, 4 90, 8 61.2, 12 59.5.  (The constants are for r = 64, by channels for others: of 33 shapes with r = 16, 32 and 128
+// the plan came within 4 % of the best rows and splits in the middle, 19 % at worst.)
 RowsPlan rows_plan(const rk_ctx* ctx, const rk_layout* L, int T, int text_rows, bool drafts, bool q8)
 {
     RowsPlan p;
@@ -365,7 +366,9 @@ RowsPlan rows_plan(const rk_ctx* ctx, const rk_layout* L, int T, int text_rows, 
         if (sr && r < least) r = least;
         const int64_t rounds = (groups * sv + n_wg - 1) / n_wg;
         if (W > rounds * n_wg) behind = block || W > 2 * n_cu ? 6.0 + r : f32 && !q8 ? 3.0 + 0.5 * r : 0.2 * r;
-        if (behind < r - v) behind = r - v;                  // (beside the last round, and longer than it)
+        // beside the last round, and longer than it: a long text keeps the memory busy, which the cache's steps wait for too (32 units, 4000 cached and 12000 of text: 1 + 8
+        // splits 53.0, 8 + 8 39.6)
+        if (r > v && behind < (r - v) * (1.0 + 0.5 * v / r)) behind = (r - v) * (1.0 + 0.5 * v / r);
         const double merge = S == 1 ? 0.0 : 2.5 + S / 32.0 + (double)rows * units * S * 1040 / 5e6;
         return (6.0 + v) * rounds + behind + merge;
     };

@@ -31,6 +31,11 @@ def test_a_long_text_is_shared_out(B, Hq, Hkv, T, cached, text, quant, dtype):
     assert groups * sr >= 0.5 * N_CU or sv + sr >= 0.75 * slots, (per, sv, sr, groups)
 
 
+def test_the_cache_beside_a_long_text_keeps_its_splits():
+    """A long text keeps the memory busy: one work-group that walks through the whole cache beside it would end last."""
+    assert plan(4, 8, 8, 4, 4000, 12000, False)[1] >= 4 and plan(1, 32, 8, 0, 2880, 20000, True, rk.RK_F32)[1] >= 4
+
+
 @pytest.mark.parametrize("quant", [False, True])
 def test_rows_a_work_group_go_by_all_tokens(quant):
     """Many rows share what is staged once the tokens that they read are many, cached or text."""
