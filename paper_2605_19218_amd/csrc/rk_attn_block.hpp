@@ -7,9 +7,9 @@
 // share a SIMD and one's softmax runs under the other's products.  A tile of 32 tokens read from LDS (12 KB at r = 64) feeds 24 instructions of 32
 // cycles.  8-bit codes become bf16 on their way into LDS, once for the work-group.  What is requested of memory is DEPTH stages ahead, in registers: a
 // round trip to HBM takes as long as two or three stages' arithmetic (three stages do not fit beside 128 channels).
-// What bounds it: issue.  Of a SIMD's cycles the products take 35 %, the vector instructions between them (weights, their two parts, codes) 30 to 39 %, and
-// what waits at a barrier the rest.  112 rows x 32 units x 16384 tokens, r = 64, 1024 text rows: 65 us, 57 GFLOP issued, 870 TFLOP/s; 448 rows over 8 bits:
-// 214 us, 187 GFLOP, 873.  (Eight waves behind one barrier took 221 us for what two work-groups of four took 209; one bf16 part of the weights would save a third of the
+// What bounds it: no one thing.  Of a SIMD's cycles the products take 34 %, the vector instructions between them (weights, their two parts, codes) 28 % over the packed and
+// 38 over the 8-bit cache, and 38 and 28 % neither: waits at a stage's barrier, and for LDS in front of it.  112 rows x 32 units x 16384 tokens, r = 64, 1024 text rows: 65 us, 57
+// GFLOP issued, 870 TFLOP/s; 448 rows over 8 bits: 214 to 219 us, 187 GFLOP, 860.  (Eight waves behind one barrier took 221 us for what two work-groups of four took 209; one bf16 part of the weights would save a third of the
 // products, and the error would be that of the result's own rounding.)
 //   S^T[token][row] = K . q~^T, O^T[channel][row] = V^T . P^T: lane (h, n) = (lane / 32, lane % 32) holds row n's scores of tokens 8 j + 4 h ..+3,
 //   j < 4.  Step s of the second product takes j = s and j = s + 2 of them as they are: tokens 4 g ..+3 and 16 + 4 g ..+3, g = 2 s + h, which is a

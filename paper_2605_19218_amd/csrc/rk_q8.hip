@@ -5,8 +5,9 @@
 // the codes are made with the rounded one (it costs at most 2^-7 of the step itself, and halves what the steps take).  A row with an infinity or
 // a NaN has s = NaN: all of it reads back as NaN.  A row whose largest element is below 2^-100 has s = 0 (1 / s stays finite).
 // What bounds these kernels is memory; the layout (rk_device.hpp) is made for the attention that reads it.  Measured at r = 64 in bf16: 32 heads x 16384 prompt
-// tokens written in 86 us (380 MB, 4.4 TB/s), read back in 44 (304 MB, 6.9 TB/s); a token of 64 x 32 heads appended in 13.6 us (67 MB of R_r, 4.9
-// TB/s), of 8 heads, r = 32, in 4.
+// tokens written in 90 us (380 MB, 4.2 TB/s; of its cycles the vector instructions take 36 %, the products 11), read back in 43.5 (304 MB, 7.0 TB/s); a token of 64 x 32 heads
+// appended in 13.6 us (67 MB of R_r, 4.9 TB/s), of 8 heads, r = 32, in 4.  In fp32: 158 us (640 MB, 4.1 TB/s), 173 (505 MB, 2.9: two 16-byte stores a lane, each of half a
+// line's pieces), 12.4.
 #include "rk_kernels.hpp"
 
 namespace rk {
@@ -97,8 +98,7 @@ __device__ __forceinline__ void load8(const float* p, float (&x)[8])
 // a swap of halves between two jb makes the 16 bytes of the layout (one octet of both tokens).
 // Values: lane (g, n) takes channels 8 n ..+7 of the eight tokens whose codes the layout puts side by side, the bytes are transposed in
 // the lane, and go through LDS into the layout.  What a unit reads is asked for before the block's arithmetic, a block a wave; three work-groups a
-// compute unit hide the rest (registers spent on fewer bank conflicts in the Values' transposition cost more than it gave: 144 us for 133,
-// written and read back).
+// compute unit hide the rest (registers spent on fewer bank conflicts in the Values' transposition cost more than it gave).
 // Grid: (blocks of `each` tokens, h_kv, b).
 constexpr int write_waves(int R) { return R > 96 ? 8 : 4; }              // (one work-group fits into a compute unit's LDS at R = 128)
 constexpr int WRITE_V = 1024;                                            // LDS of a wave for its Value codes
