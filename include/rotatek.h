@@ -150,6 +150,36 @@ typedef struct {
     const uint64_t* mask;          /* device [B, n_tokens] or NULL */
 } rk_drafts;
 
+/* Rows of a [B, H, N, d] tensor, any H that the call names: element (b, h, t, c) at data[b*stride_b + h*stride_h + t*stride_t + c], L->dtype,
+ * 16-byte aligned, strides non-negative multiples of 8 elements (of the result: no two rows may share an element). */
+typedef struct {
+    void* data;
+    int64_t stride_b, stride_h, stride_t;
+} rk_heads;
+
+/* Positions of several axes (of an image or a video: time, height, width; of text: one, or the same on all).  Token t of sequence b stands at
+ * pos[a*stride_a + b*stride_b + t] on axis a, and pair i of a row's channels turns by the angle pos[axis[i]] * inv_freq[i], in radians: (x, y) ->
+ * (x cos - y sin, x sin + y cos).  Channels from 2 n_pairs on have no position.  The angle is taken in 64 bits, so that far positions lose
+ * nothing of it; products and sums are fp32, rounded once to L->dtype.                                                                            */
+#define RK_MAX_AXES 4
+#define RK_MAX_PAIRS 64
+enum {
+    RK_ROPE_HALVES = 0,            /* pair i: channels i and n_pairs + i */
+    RK_ROPE_ADJACENT = 1           /* pair i: channels 2 i and 2 i + 1   */
+};
+enum {
+    RK_ROPE_INVERSE = 1u           /* rk_rope flag: by minus the angle. Takes positions off again; the gradient of rk_rope, too */
+};
+typedef struct {
+    const int32_t* pos;            /* device                             */
+    int64_t stride_a, stride_b;    /* in elements                        */
+    const float* inv_freq;         /* device [n_pairs]                   */
+    int32_t n_axes;                /* 1..RK_MAX_AXES                     */
+    int32_t n_pairs;               /* 1..RK_MAX_PAIRS                    */
+    int32_t pairing;               /* RK_ROPE_HALVES | RK_ROPE_ADJACENT  */
+    uint8_t axis[RK_MAX_PAIRS];    /* host: the axis of each pair, < n_axes */
+} rk_rotary;
+
 /* Outputs of rk_fit_rotation (all device, fp32 unless noted). */
 typedef struct {
     float* R;            /* [B,H_kv,d,d]  column c = eigenvector of eigvals[c] (solver order) */
@@ -478,6 +508,56 @@ rk_status rk_decode_attn_tree_quant(rk_ctx* ctx, const rk_layout* L, const void*
 rk_status rk_append_text_path(rk_ctx* ctx, const rk_layout* L, const rk_text* text, const rk_drafts* drafts,
                               const int32_t* path, int32_t path_len, const int32_t* n_path, int32_t* len_out,
                               void* stream);
+
+/* ---- positions ------------------------------------------------------------------------
+ * Puts positions on (or takes them off) the first n_tokens rows of every head: q has n_q_heads, k n_kv_heads; either pair may be NULL.  Sequence b has
+ * n_tokens_dev[b] of them (device [B], held within 0..n_tokens; NULL: all n_tokens); rows of the results from there on stay as they were.  A result may lie exactly over
+ * its source (same data, same strides); other than that results and sources may not share elements.  n_tokens may be 0.
+ * Errors: INVALID_ARG, UNSUPPORTED, HIP.                                                                        */
+rk_status rk_rope(rk_ctx* ctx, const rk_layout* L, const rk_rotary* rope, int32_t n_tokens, const int32_t* n_tokens_dev, const rk_heads* q,
+                  const rk_heads* q_out, const rk_heads* k, const rk_heads* k_out, uint32_t flags, void* stream);
+
+/* New tokens join the text segment with their positions on: row len[b] + t of text->k / text->v receives row t of k, turned, and of v as it is, for
+ * every KV head and t < n_tokens_dev[b] (as above); len_out[b] = len[b] + the rows written, which end where the segment is full.  len_out may be text->len
+ * or another array.  q and q_out as in rk_rope (all n_tokens_dev[b] rows), or both NULL.  One token a sequence is a decode's step, in
+ * front of rk_decode_attn_window or rk_decode_attn_dual; many are a prompt, in front of rk_prefill_attn_window.  The stretch of memory from the segment's first row to its
+ * last may not meet k's or v's.  RK_ERR_CAPACITY if text->max_len + n_tokens > text->capacity (max_len bounds len[b] BEFORE the call).  Calls on
+ * one context must not overlap.  Errors: INVALID_ARG, UNSUPPORTED, CAPACITY, HIP.                                */
+rk_status rk_rope_append_text(rk_ctx* ctx, const rk_layout* L, const rk_rotary* rope, int32_t n_tokens, const int32_t* n_tokens_dev,
+                              const rk_heads* q, const rk_heads* q_out, const rk_heads* k, const rk_heads* v, const rk_text* text,
+                              int32_t* len_out, void* stream);
+
+/* ---- attention with a window and sinks ---------------------------------------------------
+ * A row of the text segment stands at its own index.  A token at position p attends row j <= p if j < sinks or p - j < window: a sliding window,
+ * itself the last row of it, and the segment's first rows, which stay visible.  window 0: all rows up to itself.  What a token does not see does not touch it,
+ * also where it is an infinity or a NaN.
+ *
+ * Bytes of workspace for the calls below, for n_tokens new tokens a sequence (rk_decode_attn_window: 1); 0 for an invalid layout or n_tokens outside
+ * 1..RK_MAX_TOKENS.  What serves some n_tokens serves fewer; it does not depend on lengths.  It does depend on the context's device (NULL: 256 compute
+ * units) and on RK_OPT_DECODE_SPLITS: ask with the context that makes the calls.                                */
+size_t rk_window_workspace_size(const rk_ctx* ctx, const rk_layout* L, int32_t n_tokens);
+
+/* The attention of new tokens over the text segment that holds them already: a prompt, or a part of one.  Sequence b has n_b = n_tokens_dev[b] (device [B], held
+ * within 0..n_tokens; NULL: n_tokens) of them, the last n_b of its len[b] rows (text->len NULL: max_len): token t stands at len[b] - n_b + t.  One that stands in
+ * front of row 0 sees nothing and yields zeros.  q, out: heads of n_q_heads; rows of out from n_b on stay as they were; out may lie exactly over q.
+ * Scores q . k * scale (1/sqrt(d) when `scale` <= 0).  With 16-bit rows the softmax weights enter the product with the Values as bf16 (the sum that
+ * divides it is fp32 of fp32 weights).  Workspace: rk_window_workspace_size(ctx, L, n_tokens), 16-byte aligned; calls with workspaces of their own may overlap.
+ * B n_tokens H_q at most 2^31 - 1.  Errors: INVALID_ARG, UNSUPPORTED, CAPACITY, WORKSPACE, HIP.                  */
+rk_status rk_prefill_attn_window(rk_ctx* ctx, const rk_layout* L, const rk_heads* q, int32_t n_tokens, const int32_t* n_tokens_dev,
+                                 const rk_text* text, int32_t window, int32_t sinks, float scale, const rk_heads* out, void* workspace,
+                                 size_t workspace_bytes, void* stream);
+
+/* rk_decode_attn_dual with a window on the text: one token a sequence, at position len[b] - 1 of the text segment (its own row is appended
+ * already), attends all of the rotated cache and the text rows that it sees, under ONE softmax.  k_packed and v_cache both NULL: the text alone, as
+ * on a layer without a rotated cache (R_r, delta_mu and L->seq_len are not read then).  text is required.  q, out: [B,H_q,d], q 16-byte aligned.  The second
+ * takes the 8-bit caches.  Workspace: rk_window_workspace_size(ctx, L, 1), 16-byte aligned; calls with workspaces of their own may overlap.  A sequence with nothing
+ * to attend yields zeros.  Errors: as rk_decode_attn_dual.                                                      */
+rk_status rk_decode_attn_window(rk_ctx* ctx, const rk_layout* L, const void* q, const void* k_packed, const void* v_cache, const float* R_r,
+                                const float* delta_mu, const rk_text* text, int32_t window, int32_t sinks, float scale, void* out,
+                                void* workspace, size_t workspace_bytes, void* stream);
+rk_status rk_decode_attn_window_quant(rk_ctx* ctx, const rk_layout* L, const void* q, const void* k_q8, const void* v_q8, const float* R_r,
+                                      const float* delta_mu, const rk_text* text, int32_t window, int32_t sinks, float scale, void* out,
+                                      void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -31,9 +31,13 @@ EXPORTS = [
     "rk_decode_attn_dual", "rk_append_text", "rk_fit_subspace", "rk_query_sigma", "rk_append_decode_attn",
     "rk_append_text_decode_attn_dual", "rk_decode_attn_static", "rk_stream_read", "rk_cache_bytes_quant", "rk_compress_quant",
     "rk_append_quant", "rk_unpack_cache_quant", "rk_tree_workspace_size", "rk_tree_plan", "rk_decode_attn_quant", "rk_decode_attn_tree",
-    "rk_decode_attn_tree_quant", "rk_append_text_path",
+    "rk_decode_attn_tree_quant", "rk_append_text_path", "rk_rope", "rk_rope_append_text", "rk_window_workspace_size",
+    "rk_prefill_attn_window", "rk_decode_attn_window", "rk_decode_attn_window_quant",
 ]
 RK_MAX_DRAFTS = 64
+RK_MAX_AXES, RK_MAX_PAIRS = 4, 64
+RK_ROPE_HALVES, RK_ROPE_ADJACENT = 0, 1
+RK_ROPE_INVERSE = 1
 RK_STATIC_SCRATCH_BYTES = 8 << 20
 
 
@@ -69,6 +73,15 @@ class rk_drafts(C.Structure):
                 ("stride_t", C.c_int64), ("n_tokens", C.c_int32), ("n_tokens_dev", C.c_void_p), ("mask", C.c_void_p)]
 
 
+class rk_heads(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("stride_b", C.c_int64), ("stride_h", C.c_int64), ("stride_t", C.c_int64)]
+
+
+class rk_rotary(C.Structure):
+    _fields_ = [("pos", C.c_void_p), ("stride_a", C.c_int64), ("stride_b", C.c_int64), ("inv_freq", C.c_void_p),
+                ("n_axes", C.c_int32), ("n_pairs", C.c_int32), ("pairing", C.c_int32), ("axis", C.c_uint8 * RK_MAX_PAIRS)]
+
+
 class RotateKError(RuntimeError):
     def __init__(self, status: int, text: str):
         super().__init__(f"rotatek status {status}: {text}")
@@ -90,6 +103,7 @@ def lib():
         vp, i32, i64, u32, f32, sz = C.c_void_p, C.c_int32, C.c_int64, C.c_uint32, C.c_float, C.c_size_t
         PL, PR, PF = C.POINTER(rk_layout), C.POINTER(rk_rows), C.POINTER(rk_fit_out)
         PT, PD = C.POINTER(rk_text), C.POINTER(rk_drafts)
+        PH, PO = C.POINTER(rk_heads), C.POINTER(rk_rotary)
         L.rk_create.argtypes = [C.POINTER(vp), C.c_int]
         L.rk_destroy.argtypes = [vp]
         L.rk_status_str.argtypes = [C.c_int]
@@ -129,9 +143,16 @@ def lib():
         L.rk_decode_attn_tree.argtypes = [vp, PL, vp, vp, vp, vp, vp, PT, PD, f32, vp, vp, sz, vp]
         L.rk_decode_attn_tree_quant.argtypes = [vp, PL, vp, vp, vp, vp, vp, PT, PD, f32, vp, vp, sz, vp]
         L.rk_append_text_path.argtypes = [vp, PL, PT, PD, vp, i32, vp, vp, vp]
+        L.rk_rope.argtypes = [vp, PL, PO, i32, vp, PH, PH, PH, PH, u32, vp]
+        L.rk_rope_append_text.argtypes = [vp, PL, PO, i32, vp, PH, PH, PH, PH, PT, vp, vp]
+        L.rk_window_workspace_size.argtypes = [vp, PL, i32]
+        L.rk_window_workspace_size.restype = sz
+        L.rk_prefill_attn_window.argtypes = [vp, PL, PH, i32, vp, PT, i32, i32, f32, PH, vp, sz, vp]
+        L.rk_decode_attn_window.argtypes = [vp, PL, vp, vp, vp, vp, vp, PT, i32, i32, f32, vp, vp, sz, vp]
+        L.rk_decode_attn_window_quant.argtypes = [vp, PL, vp, vp, vp, vp, vp, PT, i32, i32, f32, vp, vp, sz, vp]
         for name in EXPORTS:
             if name not in ("rk_status_str", "rk_last_error", "rk_fit_workspace_size", "rk_decode_workspace_size",
-                            "rk_tree_workspace_size"):
+                            "rk_tree_workspace_size", "rk_window_workspace_size"):
                 getattr(L, name).restype = C.c_int
         try:
             from . import _rkbind
@@ -265,6 +286,38 @@ class Drafts:
     def c(self) -> rk_drafts:
         st = self.strides if self.strides is not None else tuple(self.k.stride()[:3])
         return rk_drafts(_ptr(self.k), _ptr(self.v), st[0], st[1], st[2], self.n_tokens, _ptr(self.n_tokens_dev), _ptr(self.mask))
+
+
+@dataclass
+class Heads:
+    """Rows of a [B, H, N, d] tensor-like (any strides, channels contiguous): queries, Keys, Values or a result."""
+    data: Any
+    strides: Optional[tuple] = None      # (stride_b, stride_h, stride_t) in elements
+
+    def c(self) -> rk_heads:
+        st = self.strides if self.strides is not None else tuple(self.data.stride()[:3])
+        return rk_heads(_ptr(self.data), st[0], st[1], st[2])
+
+
+@dataclass
+class Rope:
+    """Positions of several axes: pos int32 [n_axes, B, N] (tokens contiguous), inv_freq fp32 [n_pairs] (both device); axis: the axis of each
+    pair (default: axis 0 for all of inv_freq)."""
+    pos: Any
+    inv_freq: Any
+    axis: Optional[Any] = None           # n_pairs ints, < n_axes
+    pairing: int = RK_ROPE_HALVES
+    n_axes: Optional[int] = None         # default: pos.shape[0]
+    strides: Optional[tuple] = None      # (stride_a, stride_b) of pos in elements
+
+    def c(self) -> rk_rotary:
+        st = self.strides if self.strides is not None else tuple(self.pos.stride()[:2])
+        axes = self.n_axes if self.n_axes is not None else int(self.pos.shape[0])
+        axis = list(self.axis) if self.axis is not None else [0] * int(self.inv_freq.numel())
+        if len(axis) > RK_MAX_PAIRS or any(not 0 <= a < 256 for a in axis):
+            raise ValueError(f"axis: at most {RK_MAX_PAIRS} axes, each in 0..{RK_MAX_AXES - 1}")
+        return rk_rotary(_ptr(self.pos), st[0], st[1], _ptr(self.inv_freq), axes, len(axis), int(self.pairing),
+                         (C.c_uint8 * RK_MAX_PAIRS)(*axis))
 
 
 # ---- the ABI, same names -----------------------------------------------------
@@ -520,3 +573,50 @@ def rk_append_text_path(ctx, layout: Layout, text: Text, drafts: Drafts, path, n
     dref = C.byref(drafts.c()) if drafts is not None else None
     _check(ctx, lib().rk_append_text_path(ctx, C.byref(layout.c()), tref, dref, _ptr(path), n, _ptr(n_path), _ptr(len_out),
                                           _stream(stream)))
+
+
+def _ref(x):
+    """A reference to the structure of an argument holder, or None."""
+    return C.byref(x.c()) if x is not None else None
+
+
+def rk_rope(ctx, layout: Layout, rope: Rope, n_tokens: int, q: Optional[Heads], q_out: Optional[Heads], k: Optional[Heads],
+            k_out: Optional[Heads], flags: int = 0, n_tokens_dev=None, stream=None) -> None:
+    _check(ctx, lib().rk_rope(ctx, C.byref(layout.c()), _ref(rope), int(n_tokens), _ptr(n_tokens_dev), _ref(q), _ref(q_out), _ref(k),
+                              _ref(k_out), flags, _stream(stream)))
+
+
+def rk_rope_append_text(ctx, layout: Layout, rope: Rope, n_tokens: int, q: Optional[Heads], q_out: Optional[Heads], k: Heads, v: Heads,
+                        text: Text, len_out, n_tokens_dev=None, stream=None) -> None:
+    """len_out: device int32 [B], may be text.len."""
+    _check(ctx, lib().rk_rope_append_text(ctx, C.byref(layout.c()), _ref(rope), int(n_tokens), _ptr(n_tokens_dev), _ref(q), _ref(q_out),
+                                          _ref(k), _ref(v), _ref(text), _ptr(len_out), _stream(stream)))
+
+
+def rk_window_workspace_size(ctx, layout: Layout, n_tokens: int) -> int:
+    return int(lib().rk_window_workspace_size(ctx, C.byref(layout.c()), int(n_tokens)))
+
+
+def rk_prefill_attn_window(ctx, layout: Layout, q: Heads, n_tokens: int, text: Text, window: int, sinks: int, scale: float, out: Heads,
+                           workspace, n_tokens_dev=None, stream=None, workspace_bytes: Optional[int] = None) -> None:
+    wb = workspace_bytes if workspace_bytes is not None else (_nbytes(workspace) if workspace is not None else 0)
+    _check(ctx, lib().rk_prefill_attn_window(ctx, C.byref(layout.c()), _ref(q), int(n_tokens), _ptr(n_tokens_dev), _ref(text), int(window),
+                                             int(sinks), float(scale), _ref(out), _ptr(workspace), wb, _stream(stream)))
+
+
+def rk_decode_attn_window(ctx, layout: Layout, q, k_packed, v_cache, R_r, delta_mu, text: Text, window: int, sinks: int, scale: float, out,
+                          workspace, stream=None, workspace_bytes: Optional[int] = None) -> None:
+    """k_packed and v_cache both None: the text alone."""
+    wb = workspace_bytes if workspace_bytes is not None else (_nbytes(workspace) if workspace is not None else 0)
+    _check(ctx, lib().rk_decode_attn_window(ctx, C.byref(layout.c()), _ptr(q), _ptr(k_packed), _ptr(v_cache), _ptr(R_r), _ptr(delta_mu),
+                                            _ref(text), int(window), int(sinks), float(scale), _ptr(out), _ptr(workspace), wb,
+                                            _stream(stream)))
+
+
+def rk_decode_attn_window_quant(ctx, layout: Layout, q, k_q8, v_q8, R_r, delta_mu, text: Text, window: int, sinks: int, scale: float, out,
+                                workspace, stream=None, workspace_bytes: Optional[int] = None) -> None:
+    """rk_decode_attn_window over 8-bit caches."""
+    wb = workspace_bytes if workspace_bytes is not None else (_nbytes(workspace) if workspace is not None else 0)
+    _check(ctx, lib().rk_decode_attn_window_quant(ctx, C.byref(layout.c()), _ptr(q), _ptr(k_q8), _ptr(v_q8), _ptr(R_r), _ptr(delta_mu),
+                                                  _ref(text), int(window), int(sinks), float(scale), _ptr(out), _ptr(workspace), wb,
+                                                  _stream(stream)))

@@ -14,7 +14,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "librotatek.so")
 BIND = os.path.join(HERE, "_rkbind" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))      # (another interpreter does not find it)
 SOURCES = ["rk_api.hip", "rk_fit.hip", "rk_eig.hip", "rk_subspace.hip", "rk_compress.hip", "rk_decode.hip", "rk_q8.hip", "rk_tree.hip",
-           "rk_tree_bf16.hip", "rk_tree_f32.hip", "rk_tree_q8_bf16.hip", "rk_tree_q8_f32.hip"]
+           "rk_tree_bf16.hip", "rk_tree_f32.hip", "rk_tree_q8_bf16.hip", "rk_tree_q8_f32.hip", "rk_window.hip", "rk_rope.hip"]
 
 
 def hipcc() -> str:

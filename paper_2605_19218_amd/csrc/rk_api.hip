@@ -336,10 +336,11 @@ size_t rows_ws(const rk_ctx* ctx, const rk_layout* L, int T)
 // 8 units, none cached, 30000 of text: 8 54.4, 16 33.0, 24 32.5, 32 30.2, 60 33.2; fp32 32 units, 4000 cached, 12000 of text: 1 466, 4 136, 8 99.8, 12 105; 112 rows (128 a
 // work-group), 32 units, 1000 and 8000: 1 309, 4 90, 8 61.2, 12 59.5.  (The constants are for r = 64, by channels for others: of 33 shapes with r = 16, 32 and 128
 // the plan came within 4 % of the best rows and splits in the middle, 19 % at worst.)
-RowsPlan rows_plan(const rk_ctx* ctx, const rk_layout* L, int T, int text_rows, bool drafts, bool q8)
+// (per: rows of a work-group, 0: the cheapest)
+RowsPlan rows_plan(const rk_ctx* ctx, const rk_layout* L, int T, int text_rows, bool drafts, bool q8, int per = 0)
 {
     RowsPlan p;
-    p.per = rows_per_group(ctx, L, T, text_rows, q8);
+    p.per = per ? per : rows_per_group(ctx, L, T, text_rows, q8);
     const int64_t units = (int64_t)L->batch * L->n_kv_heads, rows = (int64_t)T * (L->n_q_heads / L->n_kv_heads);
     p.nrb = (int)((rows + p.per - 1) / p.per);
     const bool block = p.per > 16, f32 = L->dtype == RK_F32;
@@ -392,6 +393,121 @@ RowsPlan rows_plan(const rk_ctx* ctx, const rk_layout* L, int T, int text_rows, 
         if (p.Sr > slots - p.Sv) p.Sr = slots - p.Sv;         // (eight at least, see rows_slots)
     }
     return p;
+}
+
+// Text rows that one token sees at most.
+int window_rows(int max_len, int window, int sinks)
+{
+    if (window <= 0 || window >= max_len) return max_len;
+    const int64_t most = (int64_t)window + sinks;
+    return most < max_len ? (int)most : max_len;
+}
+// One token with a window on the text.  Without a cache: a split for each 128 rows it sees (a tile for each wave), one work-group a compute unit.
+RowsPlan window_plan(const rk_ctx* ctx, const rk_layout* L, bool cache, int text_rows, bool q8)
+{
+    if (cache) return rows_plan(ctx, L, 1, text_rows, false, q8, 16);
+    const int64_t units = (int64_t)L->batch * L->n_kv_heads, n_cu = ctx ? ctx->n_cu : 256;
+    RowsPlan p;
+    p.per = 16;
+    p.nrb = (L->n_q_heads / L->n_kv_heads + 15) / 16;
+    int64_t s = n_cu / (units * p.nrb), most = ((int64_t)text_rows + 127) / 128;
+    if (s > most) s = most;
+    if (s > rows_slots(ctx, L, 1)) s = rows_slots(ctx, L, 1);
+    p.Sv = 0;
+    p.Sr = s < 1 ? 1 : (int)s;
+    return p;
+}
+
+// Prompts: splits of what a row block sees, where its blocks leave compute units idle (two work-groups a compute unit), of at least 4 tiles.
+constexpr int PREFILL_SPLITS_MAX = 32;
+int prefill_splits(const rk_ctx* ctx, const rk_layout* L, int n, int rows_seen)
+{
+    const int64_t G = L->n_q_heads / L->n_kv_heads, per = prefill_block_rows(L->dtype), blocks = ((int64_t)n * G + per - 1) / per;
+    int64_t s = 2 * (int64_t)(ctx ? ctx->n_cu : 256) / (blocks * L->batch * L->n_kv_heads);
+    const int64_t most = ((int64_t)rows_seen + 127) / 128;
+    if (s > most) s = most;
+    if (s > PREFILL_SPLITS_MAX) s = PREFILL_SPLITS_MAX;
+    return s < 1 ? 1 : (int)s;
+}
+// rows * splits of n tokens or fewer: at most PREFILL_SPLITS_MAX a row, and a block's rows for two work-groups a compute unit
+size_t prefill_ws(const rk_ctx* ctx, const rk_layout* L, int n)
+{
+    const size_t rows = (size_t)L->batch * L->n_q_heads * n, most = (size_t)prefill_block_rows(L->dtype) * 2 * (ctx ? ctx->n_cu : 256);
+    const size_t slots = rows < most / PREFILL_SPLITS_MAX ? rows * PREFILL_SPLITS_MAX : most;
+    return align_up(slots * (D + 2) * sizeof(float), 256) + 256;
+}
+
+rk_status check_window(rk_ctx* ctx, int32_t window, int32_t sinks)
+{
+    if (window < 0 || sinks < 0) return fail(ctx, RK_ERR_INVALID_ARG, "window %d, sinks %d: negative", window, sinks);
+    return RK_OK;
+}
+
+rk_status check_heads(rk_ctx* ctx, const rk_heads* x, const char* name)
+{
+    if (!x || !x->data) return fail(ctx, RK_ERR_INVALID_ARG, "%s: NULL", name);
+    if ((uintptr_t)x->data & 15) return fail(ctx, RK_ERR_INVALID_ARG, "%s: must be 16-byte aligned", name);
+    if (x->stride_b < 0 || x->stride_h < 0 || x->stride_t < 0 || x->stride_b % 8 || x->stride_h % 8 || x->stride_t % 8)
+        return fail(ctx, RK_ERR_INVALID_ARG, "%s: strides must be non-negative multiples of 8 elements", name);
+    return RK_OK;
+}
+// Elements from the first to one behind the last of B x H x n rows.
+int64_t heads_span(int64_t sb, int64_t sh, int64_t st, int B, int H, int n) { return (B - 1) * sb + (H - 1) * sh + (int64_t)(n - 1) * st + D; }
+
+// Of a result: whether each row has elements of its own.  Sorted by their strides, each axis has to step over all that the axes below it cover (an
+// axis of one does not step); heads of a projection's rows lie so.
+bool rows_apart(const rk_heads* x, int B, int H, int n)
+{
+    int64_t st[3] = {x->stride_b, x->stride_h, x->stride_t}, count[3] = {B, H, n};
+    int64_t covered = D;
+    bool done[3] = {B == 1, H == 1, n == 1};
+    for (int k = 0; k < 3; ++k) {
+        int at = -1;
+        for (int i = 0; i < 3; ++i)
+            if (!done[i] && (at < 0 || st[i] < st[at])) at = i;
+        if (at < 0) return true;
+        if (st[at] < covered) return false;
+        covered += (count[at] - 1) * st[at];
+        done[at] = true;
+    }
+    return true;
+}
+
+rk_status check_result(rk_ctx* ctx, const rk_heads* x, const char* name, int B, int H, int n)
+{
+    const rk_status s = check_heads(ctx, x, name);
+    if (s != RK_OK) return s;
+    if (n > 0 && !rows_apart(x, B, H, n)) return fail(ctx, RK_ERR_INVALID_ARG, "%s: rows share elements", name);
+    return RK_OK;
+}
+
+rk_status check_tokens(rk_ctx* ctx, const rk_layout* L, int32_t n)
+{
+    if (n < 0 || n > RK_MAX_TOKENS) return fail(ctx, RK_ERR_INVALID_ARG, "n_tokens %d outside 0..%d", n, RK_MAX_TOKENS);
+    if ((int64_t)n * L->batch > INT32_MAX / L->n_q_heads) return fail(ctx, RK_ERR_UNSUPPORTED, "more than %d query rows", INT32_MAX);
+    return RK_OK;
+}
+
+rk_status check_rotary(rk_ctx* ctx, const rk_rotary* r)
+{
+    if (!r || !r->pos || !r->inv_freq) return fail(ctx, RK_ERR_INVALID_ARG, "rope: NULL, or NULL pos or inv_freq");
+    if (r->n_axes < 1 || r->n_axes > RK_MAX_AXES) return fail(ctx, RK_ERR_INVALID_ARG, "rope: n_axes %d outside 1..%d", r->n_axes, RK_MAX_AXES);
+    if (r->n_pairs < 1 || r->n_pairs > RK_MAX_PAIRS) return fail(ctx, RK_ERR_INVALID_ARG, "rope: n_pairs %d outside 1..%d", r->n_pairs, RK_MAX_PAIRS);
+    if (r->pairing != RK_ROPE_HALVES && r->pairing != RK_ROPE_ADJACENT) return fail(ctx, RK_ERR_INVALID_ARG, "rope: unknown pairing %d", r->pairing);
+    if (r->stride_a < 0 || r->stride_b < 0) return fail(ctx, RK_ERR_INVALID_ARG, "rope: negative strides of pos");
+    for (int i = 0; i < r->n_pairs; ++i)
+        if (r->axis[i] >= r->n_axes) return fail(ctx, RK_ERR_INVALID_ARG, "rope: axis %d of pair %d, of %d axes", r->axis[i], i, r->n_axes);
+    return RK_OK;
+}
+
+RopeArgs rope_args(const rk_layout* L, const rk_rotary* r, int n, const int32_t* n_dev)
+{
+    RopeArgs a{};
+    a.pos = r->pos; a.pos_sa = r->stride_a; a.pos_sb = r->stride_b; a.inv_freq = r->inv_freq;
+    for (int i = 0; i < r->n_pairs; ++i) a.axes[i >> 5] |= (uint64_t)(r->axis[i] & 3) << (2 * (i & 31));
+    a.n_axes = r->n_axes; a.n_pairs = r->n_pairs; a.pairing = r->pairing;
+    a.B = L->batch; a.Hq = L->n_q_heads; a.Hkv = L->n_kv_heads; a.n = n; a.n_dev = n_dev;
+    return a;
 }
 
 hipStream_t as_stream(void* s) { return (hipStream_t)s; }
@@ -1159,6 +1275,191 @@ rk_status rk_append_text_path(rk_ctx* ctx, const rk_layout* L, const rk_text* te
                      path, n_path, len_out, L->batch, L->n_kv_heads, drafts->n_tokens, path_len};
     e = launch_append_path(L->dtype, a, ctx->tickets, as_stream(stream));
     return e == hipSuccess ? RK_OK : hip_fail(ctx, e, "append_text_path launch");
+}
+
+// q and q_out together, or neither
+static rk_status check_turned(rk_ctx* ctx, const rk_heads* x, const rk_heads* out, const char* name, int B, int H, int n)
+{
+    if (!x && !out) return RK_OK;
+    const rk_status s = check_heads(ctx, x, name);
+    return s != RK_OK ? s : check_result(ctx, out, name, B, H, n);
+}
+
+rk_status rk_rope(rk_ctx* ctx, const rk_layout* L, const rk_rotary* rope, int32_t n_tokens, const int32_t* n_tokens_dev, const rk_heads* q,
+                  const rk_heads* q_out, const rk_heads* k, const rk_heads* k_out, uint32_t flags, void* stream)
+{
+    if (!ctx) return RK_ERR_INVALID_ARG;
+    rk_status s = check_layout(ctx, L);
+    if (s != RK_OK || (s = check_tokens(ctx, L, n_tokens)) != RK_OK || (s = check_rotary(ctx, rope)) != RK_OK) return s;
+    if (!q && !q_out && !k && !k_out) return fail(ctx, RK_ERR_INVALID_ARG, "rope: neither q nor k");
+    if ((s = check_turned(ctx, q, q_out, "rope: q or q_out", L->batch, L->n_q_heads, n_tokens)) != RK_OK) return s;
+    if ((s = check_turned(ctx, k, k_out, "rope: k or k_out", L->batch, L->n_kv_heads, n_tokens)) != RK_OK) return s;
+    if (flags & ~RK_ROPE_INVERSE) return fail(ctx, RK_ERR_INVALID_ARG, "rope: unknown flags %x", flags);
+    if (ctx->device == RK_DEVICE_NONE) return fail(ctx, RK_ERR_NO_DEVICE, "valid arguments, but the context has no device");
+    if (n_tokens == 0) return RK_OK;
+    DeviceGuard dev(ctx->device);
+    hipError_t e = dev.status;
+    if (e != hipSuccess) return hip_fail(ctx, e, "hipSetDevice");
+    RopeArgs a = rope_args(L, rope, n_tokens, n_tokens_dev);
+    a.inverse = flags & RK_ROPE_INVERSE;
+    if (q) {
+        a.q = q->data; a.q_sb = q->stride_b; a.q_sh = q->stride_h; a.q_st = q->stride_t;
+        a.qo = q_out->data; a.qo_sb = q_out->stride_b; a.qo_sh = q_out->stride_h; a.qo_st = q_out->stride_t;
+    }
+    if (k) {
+        a.k = k->data; a.k_sb = k->stride_b; a.k_sh = k->stride_h; a.k_st = k->stride_t;
+        a.ko = k_out->data; a.ko_sb = k_out->stride_b; a.ko_sh = k_out->stride_h; a.ko_st = k_out->stride_t;
+    }
+    e = launch_rope(L->dtype, a, nullptr, ctx->n_cu, as_stream(stream));
+    return e == hipSuccess ? RK_OK : hip_fail(ctx, e, "rope launch");
+}
+
+rk_status rk_rope_append_text(rk_ctx* ctx, const rk_layout* L, const rk_rotary* rope, int32_t n_tokens, const int32_t* n_tokens_dev,
+                              const rk_heads* q, const rk_heads* q_out, const rk_heads* k, const rk_heads* v, const rk_text* text,
+                              int32_t* len_out, void* stream)
+{
+    if (!ctx) return RK_ERR_INVALID_ARG;
+    rk_status s = check_layout(ctx, L);
+    if (s != RK_OK || (s = check_tokens(ctx, L, n_tokens)) != RK_OK || (s = check_rotary(ctx, rope)) != RK_OK) return s;
+    if (!text) return fail(ctx, RK_ERR_INVALID_ARG, "rope_append_text: text is NULL");
+    if ((s = check_text(ctx, text, true)) != RK_OK) return s;
+    if ((s = check_turned(ctx, q, q_out, "rope_append_text: q or q_out", L->batch, L->n_q_heads, n_tokens)) != RK_OK) return s;
+    if ((s = check_heads(ctx, k, "rope_append_text: k")) != RK_OK || (s = check_heads(ctx, v, "rope_append_text: v")) != RK_OK) return s;
+    if (!len_out) return fail(ctx, RK_ERR_INVALID_ARG, "rope_append_text: len_out is NULL");
+    if (n_tokens < 1) return fail(ctx, RK_ERR_INVALID_ARG, "rope_append_text: n_tokens %d", n_tokens);
+    if (text->max_len > text->capacity - n_tokens)
+        return fail(ctx, RK_ERR_CAPACITY, "rope_append_text: %d + %d rows exceed capacity %d", text->max_len, n_tokens, text->capacity);
+    // rows written by one work-group may be read by another: the segment's rows and the sources lie apart
+    const size_t es = elem_size(L->dtype);
+    const size_t tb = heads_span(text->stride_b, text->stride_h, text->stride_t, L->batch, L->n_kv_heads, text->capacity) * es;
+    for (const rk_heads* x : {k, v}) {
+        const size_t xb = heads_span(x->stride_b, x->stride_h, x->stride_t, L->batch, L->n_kv_heads, n_tokens) * es;
+        if (ranges_meet(text->k, tb, x->data, xb) || ranges_meet(text->v, tb, x->data, xb))
+            return fail(ctx, RK_ERR_INVALID_ARG, "rope_append_text: text segment and new rows overlap in memory");
+    }
+    if (ctx->device == RK_DEVICE_NONE) return fail(ctx, RK_ERR_NO_DEVICE, "valid arguments, but the context has no device");
+    DeviceGuard dev(ctx->device);
+    hipError_t e = dev.status;
+    if (e != hipSuccess) return hip_fail(ctx, e, "hipSetDevice");
+    RopeArgs a = rope_args(L, rope, n_tokens, n_tokens_dev);
+    if (q) {
+        a.q = q->data; a.q_sb = q->stride_b; a.q_sh = q->stride_h; a.q_st = q->stride_t;
+        a.qo = q_out->data; a.qo_sb = q_out->stride_b; a.qo_sh = q_out->stride_h; a.qo_st = q_out->stride_t;
+    }
+    a.k = k->data; a.k_sb = k->stride_b; a.k_sh = k->stride_h; a.k_st = k->stride_t;
+    a.v = v->data; a.v_sb = v->stride_b; a.v_sh = v->stride_h; a.v_st = v->stride_t;
+    a.ko = text->k; a.vo = text->v; a.ko_sb = text->stride_b; a.ko_sh = text->stride_h; a.ko_st = text->stride_t;
+    a.len = text->len; a.cap = text->capacity; a.len_out = len_out;
+    e = launch_rope(L->dtype, a, ctx->tickets, ctx->n_cu, as_stream(stream));
+    return e == hipSuccess ? RK_OK : hip_fail(ctx, e, "rope_append_text launch");
+}
+
+size_t rk_window_workspace_size(const rk_ctx* ctx, const rk_layout* L, int32_t n_tokens)
+{
+    if (check_layout(nullptr, L) != RK_OK || n_tokens < 1 || n_tokens > RK_MAX_TOKENS) return 0;
+    const size_t one = rows_ws(ctx, L, 1), many = prefill_ws(ctx, L, n_tokens);
+    return one > many ? one : many;
+}
+
+rk_status rk_prefill_attn_window(rk_ctx* ctx, const rk_layout* L, const rk_heads* q, int32_t n_tokens, const int32_t* n_tokens_dev,
+                                 const rk_text* text, int32_t window, int32_t sinks, float scale, const rk_heads* out, void* workspace,
+                                 size_t workspace_bytes, void* stream)
+{
+    if (!ctx) return RK_ERR_INVALID_ARG;
+    rk_status s = check_layout(ctx, L);
+    if (s != RK_OK || (s = check_tokens(ctx, L, n_tokens)) != RK_OK || (s = check_window(ctx, window, sinks)) != RK_OK) return s;
+    if (n_tokens < 1) return fail(ctx, RK_ERR_INVALID_ARG, "prefill_attn_window: n_tokens %d", n_tokens);
+    if ((s = check_heads(ctx, q, "prefill_attn_window: q")) != RK_OK) return s;
+    if ((s = check_result(ctx, out, "prefill_attn_window: out", L->batch, L->n_q_heads, n_tokens)) != RK_OK) return s;
+    if (!text) return fail(ctx, RK_ERR_INVALID_ARG, "prefill_attn_window: text is NULL");
+    if ((s = check_text(ctx, text, false)) != RK_OK) return s;
+    if (text->max_len > RK_MAX_TOKENS) return fail(ctx, RK_ERR_INVALID_ARG, "prefill_attn_window: max_len exceeds %d", RK_MAX_TOKENS);
+    const size_t need = prefill_ws(ctx, L, n_tokens);
+    if (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 15))
+        return fail(ctx, RK_ERR_WORKSPACE, "prefill_attn_window workspace: need %zu bytes, 16-byte aligned", need);
+    if (ctx->device == RK_DEVICE_NONE) return fail(ctx, RK_ERR_NO_DEVICE, "valid arguments, but the context has no device");
+    DeviceGuard dev(ctx->device);
+    hipError_t e = dev.status;
+    if (e != hipSuccess) return hip_fail(ctx, e, "hipSetDevice");
+    PrefillArgs a{};
+    a.q = q->data; a.q_sb = q->stride_b; a.q_sh = q->stride_h; a.q_st = q->stride_t;
+    a.out = out->data; a.o_sb = out->stride_b; a.o_sh = out->stride_h; a.o_st = out->stride_t;
+    a.k = text->k; a.v = text->v; a.sb = text->stride_b; a.sh = text->stride_h; a.st = text->stride_t;
+    a.len = text->len; a.max_len = text->max_len; a.n_dev = n_tokens_dev; a.n = n_tokens;
+    a.B = L->batch; a.Hq = L->n_q_heads; a.Hkv = L->n_kv_heads; a.G = a.Hq / a.Hkv;
+    a.window = window; a.sinks = sinks;
+    const int64_t per = prefill_block_rows(L->dtype);
+    a.blocks = (int)(((int64_t)n_tokens * a.G + per - 1) / per);
+    const int64_t seen = (int64_t)window + sinks + per / a.G + 1;       // by a block of rows
+    a.S = prefill_splits(ctx, L, n_tokens, window > 0 && seen < text->max_len ? (int)seen : text->max_len);
+    const float sc = scale > 0.f ? scale : 1.0f / sqrtf((float)L->head_dim);
+    a.scale_log2 = sc * 1.44269504088896340736f;
+    const size_t slots = (size_t)a.B * a.Hq * n_tokens * a.S;
+    a.ws_acc = (float*)align_up((uintptr_t)workspace, 256); a.ws_m = a.ws_acc + slots * D; a.ws_l = a.ws_m + slots;
+    e = launch_prefill(L->dtype, a, as_stream(stream));
+    return e == hipSuccess ? RK_OK : hip_fail(ctx, e, "prefill_attn_window launch");
+}
+
+static rk_status window_common(rk_ctx* ctx, const rk_layout* L, const void* q, const void* k_cache, const void* v_cache, const float* R_r,
+                               const float* delta_mu, const rk_text* text, int32_t window, int32_t sinks, bool q8, float scale, void* out,
+                               void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!ctx) return RK_ERR_INVALID_ARG;
+    rk_status s = check_layout(ctx, L);
+    if (s != RK_OK || (s = check_window(ctx, window, sinks)) != RK_OK) return s;
+    const bool cache = k_cache || v_cache;
+    if (!q || !out || (cache && (!k_cache || !v_cache || !R_r || !L->seq_len)))
+        return fail(ctx, RK_ERR_INVALID_ARG, "attention: NULL pointer (q, out; one of the caches, R_r, seq_len)");
+    if (((uintptr_t)k_cache & 15) || ((uintptr_t)v_cache & 15) || ((uintptr_t)q & 15))
+        return fail(ctx, RK_ERR_INVALID_ARG, "attention: q and the caches must be 16-byte aligned");
+    if (cache && L->max_seq_len > L->capacity)
+        return fail(ctx, RK_ERR_CAPACITY, "attention: max_seq_len %d exceeds capacity %d", L->max_seq_len, L->capacity);
+    if (!text) return fail(ctx, RK_ERR_INVALID_ARG, "decode_attn_window: text is NULL");
+    if ((s = check_text(ctx, text, false)) != RK_OK) return s;
+    const size_t need = rows_ws(ctx, L, 1);
+    if (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 15))
+        return fail(ctx, RK_ERR_WORKSPACE, "attention workspace: need %zu bytes, 16-byte aligned", need);
+    if (ctx->device == RK_DEVICE_NONE) return fail(ctx, RK_ERR_NO_DEVICE, "valid arguments, but the context has no device");
+    DeviceGuard dev(ctx->device);
+    hipError_t e = dev.status;
+    if (e != hipSuccess) return hip_fail(ctx, e, "hipSetDevice");
+    const RowsPlan p = window_plan(ctx, L, cache, window_rows(text->max_len, window, sinks), q8);
+    WindowRowsArgs a{};
+    a.q = q; a.Kc = k_cache; a.Vc = v_cache; a.Rr = R_r; a.dmu = delta_mu; a.seq_len = L->seq_len; a.out = out;
+    a.B = L->batch; a.T = 1; a.Hq = L->n_q_heads; a.Hkv = L->n_kv_heads; a.G = a.Hq / a.Hkv;
+    a.cap = L->capacity; a.r = L->keep; a.rp = keep_padded(L->keep);
+    a.Sv = p.Sv; a.Sr = p.Sr; a.nrb = p.nrb;
+    const float sc = scale > 0.f ? scale : 1.0f / sqrtf((float)L->head_dim);
+    a.scale_log2 = sc * 1.44269504088896340736f;
+    a.text_k = text->k; a.text_v = text->v; a.text_len = text->len; a.text_max = text->max_len;
+    a.text_sb = text->stride_b; a.text_sh = text->stride_h; a.text_st = text->stride_t;
+    const size_t slots = (size_t)a.B * a.Hq * (p.Sv + p.Sr);
+    a.ws_acc = (float*)align_up((uintptr_t)workspace, 256); a.ws_m = a.ws_acc + slots * D; a.ws_l = a.ws_m + slots;
+    a.max_len = L->max_seq_len;
+    a.window = window; a.sinks = sinks;
+    hipStream_t st = as_stream(stream);
+    e = L->dtype == RK_F32 ? (q8 ? launch_window_rows_q8_f32(a, st) : launch_window_rows_f32(a, st))
+                           : (q8 ? launch_window_rows_q8_bf16(a, st) : launch_window_rows_bf16(a, st));
+    if (e != hipSuccess) return hip_fail(ctx, e, "attention launch");
+    if (p.Sv + p.Sr > 1) {
+        e = launch_rows_merge(L->dtype, a, st);
+        if (e != hipSuccess) return hip_fail(ctx, e, "attention merge launch");
+    }
+    return RK_OK;
+}
+
+rk_status rk_decode_attn_window(rk_ctx* ctx, const rk_layout* L, const void* q, const void* k_packed, const void* v_cache, const float* R_r,
+                                const float* delta_mu, const rk_text* text, int32_t window, int32_t sinks, float scale, void* out,
+                                void* workspace, size_t workspace_bytes, void* stream)
+{
+    return window_common(ctx, L, q, k_packed, v_cache, R_r, delta_mu, text, window, sinks, false, scale, out, workspace, workspace_bytes, stream);
+}
+
+rk_status rk_decode_attn_window_quant(rk_ctx* ctx, const rk_layout* L, const void* q, const void* k_q8, const void* v_q8, const float* R_r,
+                                      const float* delta_mu, const rk_text* text, int32_t window, int32_t sinks, float scale, void* out,
+                                      void* workspace, size_t workspace_bytes, void* stream)
+{
+    return window_common(ctx, L, q, k_q8, v_q8, R_r, delta_mu, text, window, sinks, true, scale, out, workspace, workspace_bytes, stream);
 }
 
 }  // extern "C"

@@ -20,6 +20,7 @@
 // What bounds it: memory and its latency.  One token over 8 bits, 28 rows of 4 KV heads x 8 x 16384 tokens, r = 64: 20.2 us for 103 MB, 5.1 TB/s; 32 heads x 2880
 // tokens with fp32 rows 10.3 us; 8 heads x 1024 tokens 6.1 us, of which launch, length, rotation and the first tiles' round trips are all but 1.
 #pragma once
+#include <type_traits>
 #include "rk_kernels.hpp"
 
 namespace rk {
@@ -347,6 +348,9 @@ __device__ __forceinline__ uint32_t tokens_of(uint32_t slots, int g)
     return __builtin_amdgcn_readfirstlane(t);
 }
 
+// the r-th row that a window leaves: the sinks in front of s0, then the others `skip` rows further
+__device__ __forceinline__ int row_behind(int r, int s0, int skip) { return r + (r >= s0 ? skip : 0); }
+
 struct PlainRowsBf16 {
     bf16x8 qf[4];
     uint4 k[2][4], v[8];
@@ -355,17 +359,18 @@ struct PlainRowsBf16 {
 #pragma unroll
         for (int i = 0; i < 4; ++i) qf[i] = *(const bf16x8*)(qrow + 32 * i + 8 * g);
     }
-    // rows r0 ..+31 of kp, vp; those from `rows` on repeat the last
-    __device__ __forceinline__ void load(const bf16_t* kp, const bf16_t* vp, int64_t stride, int r0, int rows, int g, int n)
+    // rows r0 ..+31 of kp, vp; those from `rows` on repeat the last; from row s0 on they lie `skip` rows further
+    __device__ __forceinline__ void load(const bf16_t* kp, const bf16_t* vp, int64_t stride, int r0, int rows, int g, int n, int s0 = 0, int skip = 0)
     {
 #pragma unroll
         for (int tb = 0; tb < 2; ++tb) {
-            const bf16_t* row = kp + (int64_t)min(r0 + 16 * tb + n, rows - 1) * stride + 8 * g;
+            const bf16_t* row = kp + (int64_t)row_behind(min(r0 + 16 * tb + n, rows - 1), s0, skip) * stride + 8 * g;
 #pragma unroll
             for (int i = 0; i < 4; ++i) k[tb][i] = *(const uint4*)(row + 32 * i);
         }
 #pragma unroll
-        for (int jj = 0; jj < 8; ++jj) v[jj] = *(const uint4*)(vp + (int64_t)min(r0 + (jj < 4 ? 4 * g + jj : 12 + 4 * g + jj), rows - 1) * stride + 8 * n);
+        for (int jj = 0; jj < 8; ++jj)
+            v[jj] = *(const uint4*)(vp + (int64_t)row_behind(min(r0 + (jj < 4 ? 4 * g + jj : 12 + 4 * g + jj), rows - 1), s0, skip) * stride + 8 * n);
     }
     __device__ __forceinline__ void scores(f32x4 (&s)[2], float scale_log2)
     {
@@ -450,17 +455,17 @@ struct PlainRowsF32 {
 #pragma unroll
         for (int i = 0; i < 8; ++i) qf[i] = *(const f32x4*)(qrow + 16 * i + 4 * g);
     }
-    __device__ __forceinline__ void load(const float* kp, const float* vp, int64_t stride, int r0, int rows, int g, int n)
+    __device__ __forceinline__ void load(const float* kp, const float* vp, int64_t stride, int r0, int rows, int g, int n, int s0 = 0, int skip = 0)
     {
 #pragma unroll
         for (int tb = 0; tb < 2; ++tb) {
-            const float* row = kp + (int64_t)min(r0 + 16 * tb + n, rows - 1) * stride + 4 * g;
+            const float* row = kp + (int64_t)row_behind(min(r0 + 16 * tb + n, rows - 1), s0, skip) * stride + 4 * g;
 #pragma unroll
             for (int i = 0; i < 8; ++i) k[tb][i] = *(const f32x4*)(row + 16 * i);
         }
 #pragma unroll
         for (int jj = 0; jj < 8; ++jj) {
-            const float* row = vp + (int64_t)min(r0 + (jj < 4 ? 4 * g + jj : 12 + 4 * g + jj), rows - 1) * stride + 8 * n;
+            const float* row = vp + (int64_t)row_behind(min(r0 + (jj < 4 ? 4 * g + jj : 12 + 4 * g + jj), rows - 1), s0, skip) * stride + 8 * n;
             v[jj][0] = *(const f32x4*)row;
             v[jj][1] = *(const f32x4*)(row + 4);
         }
@@ -667,8 +672,9 @@ inline dim3 rows_grid(const RowsArgs& a)
     return dim3(x > 0x7fffffff ? 0 : (uint32_t)x);
 }
 
-template <int FMT, int R>
-__global__ __launch_bounds__(256, FMT == ROWS_F32 ? 1 : 2) void attn_rows(RowsArgs A)
+// WIN: of the text, the one token (the last row) sees the sinks and the window, which are taken as if they were all of it.
+template <int FMT, int R, bool WIN = false>
+__global__ __launch_bounds__(256, FMT == ROWS_F32 ? 1 : 2) void attn_rows(typename std::conditional<WIN, WindowRowsArgs, RowsArgs>::type A)
 {
     constexpr bool F32IO = FMT == ROWS_F32 || FMT == ROWS_Q8_F32;
     typedef typename std::conditional<F32IO, float, bf16_t>::type T;
@@ -747,7 +753,14 @@ __global__ __launch_bounds__(256, FMT == ROWS_F32 ? 1 : 2) void attn_rows(RowsAr
         if (A.draft_k) live = drafts;
         if (row0 >= live * A.G) return;
         st.clear();
-        const int text = A.text_k ? min(max(A.text_len ? A.text_len[b] : A.text_max, 0), A.text_max) : 0;
+        int text = A.text_k ? min(max(A.text_len ? A.text_len[b] : A.text_max, 0), A.text_max) : 0, s0 = 0, skip = 0;
+        if constexpr (WIN) {
+            if (A.window > 0 && text > A.window) {
+                s0 = min(A.sinks, text - A.window);
+                skip = text - A.window - s0;
+                text = s0 + A.window;
+            }
+        }
         const int tt = (text + 31) / 32, tiles = tt + (drafts + 31) / 32, k = split - A.Sv;
         const int t0 = (int)((int64_t)tiles * k / A.Sr), t1 = (int)((int64_t)tiles * (k + 1) / A.Sr);
         if (t0 < t1) {
@@ -762,7 +775,7 @@ __global__ __launch_bounds__(256, FMT == ROWS_F32 ? 1 : 2) void attn_rows(RowsAr
             for (int t = t0 + wave; t < t1; t += 4) {
                 const bool own = t >= tt;                  // drafts
                 const int r0 = 32 * (own ? t - tt : t), rows = own ? drafts : text;
-                X.load(own ? dk : tk, own ? dv : tv, own ? A.draft_st : A.text_st, r0, rows, g, n);
+                X.load(own ? dk : tk, own ? dv : tv, own ? A.draft_st : A.text_st, r0, rows, g, n, s0, skip);
                 f32x4 s[2];
                 X.scores(s, A.scale_log2);
                 uint64_t mask = ~0ull;
@@ -838,6 +851,21 @@ __global__ __launch_bounds__(256, FMT == ROWS_F32 ? 1 : 2) void attn_rows(RowsAr
             if (p == 0) { A.ws_m[slot] = M; A.ws_l[slot] = sum; }
         }
     }
+}
+
+// 16 rows a work-group; without a cache (Sv = 0) any R will do
+template <int FMT>
+static hipError_t launch_window_fmt(const WindowRowsArgs& a, hipStream_t st)
+{
+    const dim3 grid = rows_grid(a);
+    if (!grid.x) return hipErrorInvalidValue;
+    switch (a.Sv ? (a.r + 31) / 32 : 1) {
+        case 1: attn_rows<FMT, 32, true><<<grid, 256, 0, st>>>(a); break;
+        case 2: attn_rows<FMT, 64, true><<<grid, 256, 0, st>>>(a); break;
+        case 3: attn_rows<FMT, 96, true><<<grid, 256, 0, st>>>(a); break;
+        default: attn_rows<FMT, 128, true><<<grid, 256, 0, st>>>(a); break;
+    }
+    return hipGetLastError();
 }
 
 template <int FMT>

@@ -92,6 +92,52 @@ hipError_t launch_rows_f32(const RowsArgs& a, int rows, hipStream_t st);
 hipError_t launch_rows_q8_bf16(const RowsArgs& a, int rows, hipStream_t st);
 hipError_t launch_rows_q8_f32(const RowsArgs& a, int rows, hipStream_t st);
 hipError_t launch_rows_merge(int dtype, const RowsArgs& a, hipStream_t st);
+// One token a sequence with a window on the text (T = 1, no drafts); Sv = 0: no cache
+struct WindowRowsArgs : RowsArgs {
+    int32_t window, sinks;       // window 0: all of the text
+};
+hipError_t launch_window_rows_bf16(const WindowRowsArgs& a, hipStream_t st);
+hipError_t launch_window_rows_f32(const WindowRowsArgs& a, hipStream_t st);
+hipError_t launch_window_rows_q8_bf16(const WindowRowsArgs& a, hipStream_t st);
+hipError_t launch_window_rows_q8_f32(const WindowRowsArgs& a, hipStream_t st);
+
+// ---- rk_window.hip: new tokens over the text segment ------------------------------
+struct PrefillArgs {
+    const void* q;
+    void* out;
+    int64_t q_sb, q_sh, q_st, o_sb, o_sh, o_st;   // strides in elements
+    const void *k, *v;           // the text segment
+    int64_t sb, sh, st;
+    const int32_t *len, *n_dev;  // or null: max_len, n
+    int32_t max_len, n;
+    int32_t B, Hq, Hkv, G;
+    int32_t window, sinks;
+    int32_t blocks, S;           // row blocks of a KV head; splits of what a block sees
+    float scale_log2;
+    float *ws_m, *ws_l, *ws_acc; // [B, Hkv, n G, S] and [.., S, d]
+};
+int prefill_block_rows(int dtype);
+hipError_t launch_prefill(int dtype, const PrefillArgs& a, hipStream_t st);
+
+// ---- rk_rope.hip ----------------------------------------------------------------
+constexpr int RK_AXES = 4;
+struct RopeArgs {
+    const void *q, *k, *v;       // v (and q, k): or null
+    void *qo, *ko, *vo;          // ko and vo share their strides
+    int64_t q_sb, q_sh, q_st, qo_sb, qo_sh, qo_st, k_sb, k_sh, k_st, ko_sb, ko_sh, ko_st, v_sb, v_sh, v_st;
+    const int32_t* pos;
+    int64_t pos_sa, pos_sb;
+    const float* inv_freq;
+    uint64_t axes[2];            // two bits a pair
+    int32_t n_axes, n_pairs, pairing, inverse;
+    int32_t B, Hq, Hkv, n;
+    const int32_t* n_dev;        // or null: n
+    const int32_t* len;          // or null; else row t goes to row len[b] + t of ko and vo, below cap
+    int32_t cap;
+    int32_t* len_out;            // may be len
+};
+// tickets: as launch_append_path
+hipError_t launch_rope(int dtype, const RopeArgs& a, int32_t* tickets, int n_cu, hipStream_t st);
 // row text_len[b] + i of the text segment receives draft path[b][i], i < n_path[b]; len_out[b] counts them
 struct PathArgs {
     void *text_k, *text_v;

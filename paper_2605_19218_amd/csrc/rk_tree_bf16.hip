@@ -7,4 +7,5 @@ hipError_t launch_rows_bf16(const RowsArgs& a, int rows, hipStream_t st)
 {
     return rows == 16 ? launch_rows_fmt<ROWS_BF16>(a, st) : launch_block_fmt<ROWS_BF16>(a, rows, st);
 }
+hipError_t launch_window_rows_bf16(const WindowRowsArgs& a, hipStream_t st) { return launch_window_fmt<ROWS_BF16>(a, st); }
 }  // namespace rk

@@ -4,4 +4,5 @@
 
 namespace rk {
 hipError_t launch_rows_f32(const RowsArgs& a, int, hipStream_t st) { return launch_rows_fmt<ROWS_F32>(a, st); }
+hipError_t launch_window_rows_f32(const WindowRowsArgs& a, hipStream_t st) { return launch_window_fmt<ROWS_F32>(a, st); }
 }  // namespace rk
