@@ -30,6 +30,16 @@ struct Sight {
     __device__ __forceinline__ bool of(int j) const { return j <= p && (j < sinks || p - j < window); }
 };
 
+// Which rows and splits a work-group takes: the last blocks of all KV heads first, which see most, so that the short ones fill the gaps at the end; a head's
+// work-groups go to the same XCDs, which read its Keys and Values from their L2.
+__device__ __forceinline__ void prompt_place(const PrefillArgs& A, int& block, int& split, int& u)
+{
+    const uint32_t units = A.B * A.Hkv, rank = blockIdx.x / units;
+    u = blockIdx.x - rank * units;
+    block = A.blocks - 1 - (int)(rank / A.S);
+    split = rank % A.S;
+}
+
 struct PromptBf16 {
     typedef bf16_t T;
     static constexpr int ROW = 256, TILE = PROMPT_TOKENS * ROW;       // bytes of a token's Key (or Value) and of a stage's
@@ -187,9 +197,8 @@ __global__ __launch_bounds__(256, 2) void attn_prompt(PrefillArgs A)
     typedef typename P::T T;
     __shared__ __attribute__((aligned(16))) char lds[4 * P::TILE];    // two stages of Keys and Values
 
-    // blocks with more to see first
-    const uint32_t u = blockIdx.x / (uint32_t)(A.blocks * A.S), rest = blockIdx.x - u * (uint32_t)(A.blocks * A.S);
-    const int block = A.blocks - 1 - (int)(rest / A.S), split = rest % A.S;
+    int block, split, u;
+    prompt_place(A, block, split, u);
     const int b = u / A.Hkv, hk = u - b * A.Hkv;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, n = lane & 31;
 
@@ -310,11 +319,11 @@ __global__ __launch_bounds__(256, 2) void attn_prompt(PrefillArgs A)
 
 
 // ---- bf16, many rows: 64 rows a wave ------------------------------------------------
-// A stage of 64 tokens, three of them in LDS: loads go there without passing through registers, two stages ahead. Rows in two groups of 32, so that a Key or Value
+// A stage of 64 tokens, four of them in LDS: loads go there without passing through registers, two stages ahead, one barrier a stage. Rows in two groups of 32, so that a Key or Value
 // read from LDS feeds two products.
 // In LDS a token's row is its 256 bytes, slots permuted as slot_of() says: what a load leaves is lane by lane, so it is the lanes' addresses that are permuted.
 constexpr int WIDE_ROWS = 256, WIDE_TOKENS = 64, WIDE_ROW = 256, WIDE_VALUES = WIDE_TOKENS * WIDE_ROW, WIDE_STAGE = 2 * WIDE_VALUES;
-constexpr int WIDE_LDS = 3 * WIDE_STAGE;      // and a flag
+constexpr int WIDE_LDS = 4 * WIDE_STAGE;      // and a flag
 
 __device__ __forceinline__ uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)p; }
 // 16 bytes a lane from `from` to LDS at `to` (of the wave) + 16 lane. (Not the builtin: behind it every read of LDS waits for all loads.) What is asked for
@@ -345,31 +354,41 @@ struct WideRows {
             for (int i = 0; i < 8; ++i) asm volatile("" : "+a"(q[g][i]));
         }
     }
-    // S^T of a tile's 32 tokens; ka: this lane's places of pieces 0..3 of the tile's first token
-    __device__ __forceinline__ void scores(const char* lds, const int (&ka)[4], int at, f32x16 (&s)[2]) const
+    // a tile's 32 Keys; ka: this lane's places of pieces 0..3 of the tile's first token
+    static __device__ __forceinline__ void keys(const char* lds, const int (&ka)[4], int at, bf16x8 (&k)[8])
+    {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) k[i] = *(const bf16x8*)(lds + ka[i & 3] + at + 128 * (i >> 2));
+    }
+    // S^T of them
+    __device__ __forceinline__ void scores(const bf16x8 (&k)[8], f32x16 (&s)[2]) const
     {
 #pragma unroll
         for (int g = 0; g < 2; ++g)
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[g][i] = 0.f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const bf16x8 a = *(const bf16x8*)(lds + ka[i & 3] + at + 128 * (i >> 2));
+        for (int i = 0; i < 8; ++i)
 #pragma unroll
-            for (int g = 0; g < 2; ++g) s[g] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, q[g][i], s[g], 0, 0, 0);
-        }
+            for (int g = 0; g < 2; ++g) s[g] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[i], q[g][i], s[g], 0, 0, 0);
     }
-    // the running maxima, after the tile's own
-    __device__ __forceinline__ void follow(const f32x16 (&s)[2])
+    // the largest score of each group's row among this lane's tokens
+    static __device__ __forceinline__ float most(const f32x16& s)
+    {
+        float a = fmaxf(s[0], s[1]), b = fmaxf(s[2], s[3]);
+#pragma unroll
+        for (int i = 4; i < 16; i += 4) {
+            a = fmaxf(fmaxf(a, s[i]), s[i + 1]);
+            b = fmaxf(fmaxf(b, s[i + 2]), s[i + 3]);
+        }
+        return fmaxf(a, b);
+    }
+    // the running maxima, after a tile's
+    __device__ __forceinline__ void follow(const float (&top)[2])
     {
         float mt[2];
 #pragma unroll
-        for (int g = 0; g < 2; ++g) {
-            mt[g] = s[g][0];
-#pragma unroll
-            for (int i = 1; i < 16; ++i) mt[g] = fmaxf(mt[g], s[g][i]);
-            mt[g] = halves_max(mt[g]) * c;
-        }
+        for (int g = 0; g < 2; ++g) mt[g] = halves_max(top[g]) * c;
         if (__any(mt[0] > m[0] + 8.f || mt[1] > m[1] + 8.f)) {
 #pragma unroll
             for (int g = 0; g < 2; ++g) {
@@ -381,68 +400,86 @@ struct WideRows {
             }
         }
     }
-    __device__ __forceinline__ void weigh(f32x16& s, int g, bf16x8 (&p)[2])
+    // half x of channels 32 b + lane % 32 of the tile's tokens 16 t + (4 h ..+3, 8 + 4 h ..+3); va: this lane's places of blocks 0 and 1
+    static __device__ __forceinline__ s16x4 values(const char* lds, const int (&va)[2], int at, int t, int b, int x)
     {
-        const float ref = m[g] > ROWS_NEG_INF ? m[g] : 0.f;
-        float sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            s[i] = rows_exp2(fmaf(s[i], c, -ref));
-            sum += s[i];
-        }
-        l[g] += sum;
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            uint32_t w[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] = __builtin_bit_cast(uint32_t, (bf16x2){(__bf16)s[8 * t + 2 * e], (__bf16)s[8 * t + 2 * e + 1]});
-            p[t] = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
-        }
-    }
-    // channels 32 b + lane % 32 of the tile's tokens 16 t + (4 h ..+3, 8 + 4 h ..+3); va: this lane's places of blocks 0 and 1
-    static __device__ __forceinline__ bf16x8 values(const char* lds, const int (&va)[2], int at, int t, int b)
-    {
-        uint2 a[2];
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-            typedef __attribute__((address_space(3))) s16x4* Lds;
-            a[x] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(lds + va[b & 1] + at + (16 * t + 8 * x) * WIDE_ROW + 128 * (b >> 1))));
-        }
-        return __builtin_bit_cast(bf16x8, make_uint4(a[0].x, a[0].y, a[1].x, a[1].y));
+        typedef __attribute__((address_space(3))) s16x4* Lds;
+        return __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(lds + va[b & 1] + at + (16 * t + 8 * x) * WIDE_ROW + 128 * (b >> 1)));
     }
     // a tile on an edge: what a row does not see has no score
-    __device__ __forceinline__ void hide(f32x16 (&s)[2], int j0, int h) const
+    __device__ __forceinline__ void hide(f32x16 (&s)[2], float (&top)[2], int j0, int h) const
     {
 #pragma unroll
-        for (int g = 0; g < 2; ++g)
+        for (int g = 0; g < 2; ++g) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[g][i] = sight[g].of(j0 + 8 * (i >> 2) + 4 * h + (i & 3)) ? s[g][i] : ROWS_NEG_INF;
+            top[g] = most(s[g]);
+        }
     }
-    // One tile (Values at vt): scores s of it into O; the scores of the next tile (Keys at kt) into `next`.
-    __device__ __forceinline__ void tile(f32x16 (&s)[2], f32x16 (&next)[2], const char* lds, const int (&ka)[4], int kt, const int (&va)[2], int vt)
+    // Scores belong into the other half of the register file, where the vector instructions are that they are for; the compiler would have them beside the accumulators and
+    // copy them (64 instructions a tile). The vector instructions that read them come 300 cycles behind, matrix instructions of the same group two behind.
+    static __device__ __forceinline__ void score(f32x16& s, const bf16x8& k, const bf16x8& q, bool begin)
     {
-        bf16x8 p[2][2];
-        follow(s);
+        if (begin) asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(s) : "v"(k), "a"(q));
+        else asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(s) : "v"(k), "a"(q));
+    }
+    // One tile (Values at vt): scores s of it, whose largest are `top`, into O; the scores of the next tile (Keys k) into `next`, its largest into `top`; the Keys of
+    // the one behind it (at kt) into k.
+    // A wave has its SIMD for itself, so what runs beside the matrix instructions is what stands between them: 32 of 32 cycles, of which the first 24 have beside them
+    // the weights, 16 pairs of 52 cycles (the exponentials 16 each), two in three instructions' time, and the last eight the maxima; LDS is read one piece a step.
+    __device__ __forceinline__ void tile(f32x16 (&s)[2], f32x16 (&next)[2], float (&top)[2], bf16x8 (&k)[8], const char* lds, const int (&ka)[4], int kt,
+                                         const int (&va)[2], int vt)
+    {
+        follow(top);
         hold();
-        scores(lds, ka, kt, next);
-        weigh(s[0], 0, p[0]);
-        weigh(s[1], 1, p[1]);
+        const float ref[2] = {m[0] > ROWS_NEG_INF ? m[0] : 0.f, m[1] > ROWS_NEG_INF ? m[1] : 0.f};
+        float sum[2][2] = {{0.f, 0.f}, {0.f, 0.f}};
+        uint32_t p[2][8];
+        s16x4 v[2][4][2];
+        __builtin_amdgcn_sched_barrier(0);
+        auto weigh = [&](int pair) {             // of rows' group pair / 8, tokens 2 (pair % 8) and the next
+            const int g = pair >> 3, e = 2 * (pair & 7);
+            s[g][e] = rows_exp2(fmaf(s[g][e], c, -ref[g]));
+            s[g][e + 1] = rows_exp2(fmaf(s[g][e + 1], c, -ref[g]));
+        };
+        auto pack = [&](int pair) {
+            const int g = pair >> 3, e = 2 * (pair & 7);
+            sum[g][0] += s[g][e];
+            sum[g][1] += s[g][e + 1];
+            p[g][pair & 7] = __builtin_bit_cast(uint32_t, (bf16x2){(__bf16)s[g][e], (__bf16)s[g][e + 1]});
+        };
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int b = 0; b < 4; ++b) {
-                const bf16x8 a = values(lds, va, vt, t, b);
-#pragma unroll
-                for (int g = 0; g < 2; ++g) O[g][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, p[g][t], O[g][b], 0, 0, 0);
+        for (int x = 0; x < 32; ++x) {
+            if (x < 16) {
+                const int g = x & 1, i = x >> 1;
+                score(next[g], k[i], q[g][i], i == 0);
+                v[x >> 3][(x >> 1) & 3][x & 1] = values(lds, va, vt, x >> 3, (x >> 1) & 3, x & 1);
+            } else {
+                const int g = (x >> 3) & 1, t = (x >> 2) & 1, b = x & 3;
+                const uint2 v0 = __builtin_bit_cast(uint2, v[t][b][0]), v1 = __builtin_bit_cast(uint2, v[t][b][1]);
+                O[g][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, make_uint4(v0.x, v0.y, v1.x, v1.y)),
+                                                                  __builtin_bit_cast(bf16x8, make_uint4(p[g][4 * t], p[g][4 * t + 1], p[g][4 * t + 2], p[g][4 * t + 3])),
+                                                                  O[g][b], 0, 0, 0);
+                if (x >= 24) k[x - 24] = *(const bf16x8*)(lds + ka[x & 3] + kt + 128 * ((x - 24) >> 2));
             }
+            // pairs 2 y and 2 y + 1 in steps 3 y ..+2, each one's sums and rounding a step behind
+            if (x < 24 && x % 3 < 2) weigh(2 * (x / 3) + x % 3);
+            if (x < 25 && x % 3 == 1) pack(2 * (x / 3));
+            if (x < 25 && x % 3 == 2) pack(2 * (x / 3) + 1);
+            if (x == 26) top[0] = most(next[0]);
+            if (x == 28) top[1] = most(next[1]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int g = 0; g < 2; ++g) l[g] += sum[g][0] + sum[g][1];
     }
 };
 
 __global__ __launch_bounds__(256, 1) void attn_prompt_wide(PrefillArgs A)
 {
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    const uint32_t u = blockIdx.x / (uint32_t)(A.blocks * A.S), rest = blockIdx.x - u * (uint32_t)(A.blocks * A.S);
-    const int block = A.blocks - 1 - (int)(rest / A.S), split = rest % A.S;
+    int block, split, u;
+    prompt_place(A, block, split, u);
     const int b = u / A.Hkv, hk = u - b * A.Hkv;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, n = lane & 31;
 
@@ -522,10 +559,10 @@ __global__ __launch_bounds__(256, 1) void attn_prompt_wide(PrefillArgs A)
                 }
             }
         };
-        fetch(i0, 0);
-        fetch(min(i0 + 1, i1 - 1), WIDE_STAGE);
+#pragma unroll
+        for (int i = 0; i < 3; ++i) fetch(min(i0 + i, i1 - 1), i * WIDE_STAGE);
         if (tid == 0) *odd = 0;
-        stage_wait<8>();
+        stage_wait<16>();
         lds_barrier();
         if (edge(start(i0))) {
             clean(lds);
@@ -540,30 +577,35 @@ __global__ __launch_bounds__(256, 1) void attn_prompt_wide(PrefillArgs A)
             va[i] = r * WIDE_ROW + 16 * slot_of(r, 4 * i + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) + 8 * (lane & 1);
         }
         f32x16 s0[2], s1[2];
-        W.scores(lds, ka, 0, s0);
-        int now = 0, next = WIDE_STAGE, behind = 2 * WIDE_STAGE;
+        bf16x8 k[8];
+        float top[2];
+        WideRows::keys(lds, ka, 0, k);
+        W.scores(k, s0);
+        WideRows::keys(lds, ka, 32 * WIDE_ROW, k);
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+            asm volatile("" : "+v"(s0[g]));
+            top[g] = WideRows::most(s0[g]);
+        }
+        int now = 0;
 #pragma unroll 1
         for (int i = i0; i < i1; ++i) {
             W.hold();
-            const int j0 = start(i);
-            fetch(min(i + 2, i1 - 1), behind);
-            auto inside = [&](int j) { return j + 31 <= w_lo && (j + 31 < A.sinks || w_hi - j < window); };
-            if (!inside(j0)) W.hide(s0, j0, h);
-            W.tile(s0, s1, lds, ka, now + 32 * WIDE_ROW, va, now + WIDE_VALUES);
-            // the next stage's loads are all but the last eight, which are the ones behind it
+            const int j0 = start(i), next = (now + WIDE_STAGE) & (4 * WIDE_STAGE - 1);
+            // The next stage's loads are all but the last eight.  Behind the barrier it is there for all waves, and nobody reads the one before this any more.
             stage_wait<8>();
             lds_barrier();
+            fetch(min(i + 3, i1 - 1), (now + 3 * WIDE_STAGE) & (4 * WIDE_STAGE - 1));
             if (i + 1 < i1 && edge(start(i + 1))) {
                 clean(lds + next);
                 lds_barrier();
             }
-            if (!inside(j0 + 32)) W.hide(s1, j0 + 32, h);
-            W.tile(s1, s0, lds, ka, next, va, now + WIDE_VALUES + 32 * WIDE_ROW);
-            lds_barrier();
-            const int t = now;
+            auto inside = [&](int j) { return j + 31 <= w_lo && (j + 31 < A.sinks || w_hi - j < window); };
+            if (!inside(j0)) W.hide(s0, top, j0, h);
+            W.tile(s0, s1, top, k, lds, ka, next, va, now + WIDE_VALUES);
+            if (!inside(j0 + 32)) W.hide(s1, top, j0 + 32, h);
+            W.tile(s1, s0, top, k, lds, ka, next + 32 * WIDE_ROW, va, now + WIDE_VALUES + 32 * WIDE_ROW);
             now = next;
-            next = behind;
-            behind = t;
         }
         stage_wait<0>();             // (what was asked for twice, at the end)
         // The Values that were left out join the rows that see them: a sum of one is it, or NaN.
