@@ -166,6 +166,9 @@ def lib():
                                           (L.rk_append_quant, L.rk_decode_attn_quant, L.rk_decode_attn_tree,
                                            L.rk_decode_attn_tree_quant, L.rk_append_text_path, L.rk_compress_quant,
                                            L.rk_unpack_cache_quant)])
+            _rkbind.bind_window(Heads, Rope, *[C.cast(f, C.c_void_p).value for f in
+                                               (L.rk_rope, L.rk_rope_append_text, L.rk_prefill_attn_window, L.rk_decode_attn_window,
+                                                L.rk_decode_attn_window_quant)])
             _bind = _rkbind
         _lib = L
     return _lib
@@ -305,17 +308,21 @@ class Rope:
     pair (default: axis 0 for all of inv_freq)."""
     pos: Any
     inv_freq: Any
-    axis: Optional[Any] = None           # n_pairs ints, < n_axes
+    axis: Optional[Any] = None           # n_pairs ints, < n_axes (kept as bytes)
     pairing: int = RK_ROPE_HALVES
     n_axes: Optional[int] = None         # default: pos.shape[0]
     strides: Optional[tuple] = None      # (stride_a, stride_b) of pos in elements
 
+    def __post_init__(self):
+        axis = [int(a) for a in self.axis] if self.axis is not None else [0] * int(self.inv_freq.numel())
+        if len(axis) > RK_MAX_PAIRS or any(not 0 <= a < 256 for a in axis):
+            raise ValueError(f"axis: of at most {RK_MAX_PAIRS} pairs, each in 0..{RK_MAX_AXES - 1}")
+        self.axis = bytes(axis)
+
     def c(self) -> rk_rotary:
         st = self.strides if self.strides is not None else tuple(self.pos.stride()[:2])
         axes = self.n_axes if self.n_axes is not None else int(self.pos.shape[0])
-        axis = list(self.axis) if self.axis is not None else [0] * int(self.inv_freq.numel())
-        if len(axis) > RK_MAX_PAIRS or any(not 0 <= a < 256 for a in axis):
-            raise ValueError(f"axis: at most {RK_MAX_PAIRS} axes, each in 0..{RK_MAX_AXES - 1}")
+        axis = list(self.axis)
         return rk_rotary(_ptr(self.pos), st[0], st[1], _ptr(self.inv_freq), axes, len(axis), int(self.pairing),
                          (C.c_uint8 * RK_MAX_PAIRS)(*axis))
 
@@ -582,6 +589,8 @@ def _ref(x):
 
 def rk_rope(ctx, layout: Layout, rope: Rope, n_tokens: int, q: Optional[Heads], q_out: Optional[Heads], k: Optional[Heads],
             k_out: Optional[Heads], flags: int = 0, n_tokens_dev=None, stream=None) -> None:
+    if _bind is not None and _done(ctx, _bind.rope(ctx, layout, rope, n_tokens, q, q_out, k, k_out, flags, n_tokens_dev, stream)):
+        return
     _check(ctx, lib().rk_rope(ctx, C.byref(layout.c()), _ref(rope), int(n_tokens), _ptr(n_tokens_dev), _ref(q), _ref(q_out), _ref(k),
                               _ref(k_out), flags, _stream(stream)))
 
@@ -589,6 +598,8 @@ def rk_rope(ctx, layout: Layout, rope: Rope, n_tokens: int, q: Optional[Heads], 
 def rk_rope_append_text(ctx, layout: Layout, rope: Rope, n_tokens: int, q: Optional[Heads], q_out: Optional[Heads], k: Heads, v: Heads,
                         text: Text, len_out, n_tokens_dev=None, stream=None) -> None:
     """len_out: device int32 [B], may be text.len."""
+    if _bind is not None and _done(ctx, _bind.rope_append(ctx, layout, rope, n_tokens, q, q_out, k, v, text, len_out, n_tokens_dev, stream)):
+        return
     _check(ctx, lib().rk_rope_append_text(ctx, C.byref(layout.c()), _ref(rope), int(n_tokens), _ptr(n_tokens_dev), _ref(q), _ref(q_out),
                                           _ref(k), _ref(v), _ref(text), _ptr(len_out), _stream(stream)))
 
@@ -599,6 +610,9 @@ def rk_window_workspace_size(ctx, layout: Layout, n_tokens: int) -> int:
 
 def rk_prefill_attn_window(ctx, layout: Layout, q: Heads, n_tokens: int, text: Text, window: int, sinks: int, scale: float, out: Heads,
                            workspace, n_tokens_dev=None, stream=None, workspace_bytes: Optional[int] = None) -> None:
+    if _bind is not None and _done(ctx, _bind.prefill(ctx, layout, q, n_tokens, text, window, sinks, out, n_tokens_dev, scale, None, workspace,
+                                                      stream, workspace_bytes)):
+        return
     wb = workspace_bytes if workspace_bytes is not None else (_nbytes(workspace) if workspace is not None else 0)
     _check(ctx, lib().rk_prefill_attn_window(ctx, C.byref(layout.c()), _ref(q), int(n_tokens), _ptr(n_tokens_dev), _ref(text), int(window),
                                              int(sinks), float(scale), _ref(out), _ptr(workspace), wb, _stream(stream)))
@@ -607,6 +621,9 @@ def rk_prefill_attn_window(ctx, layout: Layout, q: Heads, n_tokens: int, text: T
 def rk_decode_attn_window(ctx, layout: Layout, q, k_packed, v_cache, R_r, delta_mu, text: Text, window: int, sinks: int, scale: float, out,
                           workspace, stream=None, workspace_bytes: Optional[int] = None) -> None:
     """k_packed and v_cache both None: the text alone."""
+    if _bind is not None and _done(ctx, _bind.window(ctx, layout, q, k_packed, v_cache, R_r, delta_mu, text, window, sinks, scale, out,
+                                                     workspace, stream, workspace_bytes)):
+        return
     wb = workspace_bytes if workspace_bytes is not None else (_nbytes(workspace) if workspace is not None else 0)
     _check(ctx, lib().rk_decode_attn_window(ctx, C.byref(layout.c()), _ptr(q), _ptr(k_packed), _ptr(v_cache), _ptr(R_r), _ptr(delta_mu),
                                             _ref(text), int(window), int(sinks), float(scale), _ptr(out), _ptr(workspace), wb,
@@ -616,6 +633,9 @@ def rk_decode_attn_window(ctx, layout: Layout, q, k_packed, v_cache, R_r, delta_
 def rk_decode_attn_window_quant(ctx, layout: Layout, q, k_q8, v_q8, R_r, delta_mu, text: Text, window: int, sinks: int, scale: float, out,
                                 workspace, stream=None, workspace_bytes: Optional[int] = None) -> None:
     """rk_decode_attn_window over 8-bit caches."""
+    if _bind is not None and _done(ctx, _bind.window_quant(ctx, layout, q, k_q8, v_q8, R_r, delta_mu, text, window, sinks, scale, out,
+                                                           workspace, stream, workspace_bytes)):
+        return
     wb = workspace_bytes if workspace_bytes is not None else (_nbytes(workspace) if workspace is not None else 0)
     _check(ctx, lib().rk_decode_attn_window_quant(ctx, C.byref(layout.c()), _ptr(q), _ptr(k_q8), _ptr(v_q8), _ptr(R_r), _ptr(delta_mu),
                                                   _ref(text), int(window), int(sinks), float(scale), _ptr(out), _ptr(workspace), wb,

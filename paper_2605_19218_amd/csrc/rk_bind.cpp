@@ -1,7 +1,8 @@
 // CPython side of the calls that a program makes once per generated token and layer: the arguments of rk_decode_attn,
 // rk_append_decode_attn, rk_decode_attn_dual and rk_append_text_decode_attn_dual, of rk_append_quant and rk_decode_attn_quant, and, once per
 // round of drafts and layer, of rk_decode_attn_tree, rk_decode_attn_tree_quant and rk_append_text_path, marshalled in C; with them the prompt's
-// rk_compress_quant and rk_unpack_cache_quant, which short prompts wait for as well.  The same through ctypes costs some 5 us a
+// rk_compress_quant and rk_unpack_cache_quant, which short prompts wait for as well, and positions and windows: rk_rope, rk_rope_append_text,
+// rk_prefill_attn_window and rk_decode_attn_window(_quant).  The same through ctypes costs some 5 us a
 // call (structures built field by field, a converter per argument), which is as long as a short decode runs on the device: 8 KV heads x
 // 1024 tokens were called every 8.7 us, of which the device needed 5.8.
 //
@@ -34,6 +35,19 @@ typedef rk_status (*path_fn)(rk_ctx*, const rk_layout*, const rk_text*, const rk
 typedef rk_status (*compress_fn)(rk_ctx*, const rk_layout*, const rk_rows*, const float*, void*, const rk_rows*, void*, int32_t*, void*);
 typedef rk_status (*unpack_fn)(rk_ctx*, const rk_layout*, const void*, const void*, void*, void*, void*);
 
+typedef rk_status (*rope_fn)(rk_ctx*, const rk_layout*, const rk_rotary*, int32_t, const int32_t*, const rk_heads*, const rk_heads*,
+                             const rk_heads*, const rk_heads*, uint32_t, void*);
+typedef rk_status (*rope_append_fn)(rk_ctx*, const rk_layout*, const rk_rotary*, int32_t, const int32_t*, const rk_heads*, const rk_heads*,
+                                    const rk_heads*, const rk_heads*, const rk_text*, int32_t*, void*);
+typedef rk_status (*prefill_fn)(rk_ctx*, const rk_layout*, const rk_heads*, int32_t, const int32_t*, const rk_text*, int32_t, int32_t, float,
+                                const rk_heads*, void*, size_t, void*);
+typedef rk_status (*window_fn)(rk_ctx*, const rk_layout*, const void*, const void*, const void*, const float*, const float*, const rk_text*,
+                               int32_t, int32_t, float, void*, void*, size_t, void*);
+
+rope_fn fn_rope;
+rope_append_fn fn_rope_append;
+prefill_fn fn_prefill;
+window_fn fn_window, fn_window_quant;
 decode_fn fn_decode;
 append_decode_fn fn_append_decode;
 dual_fn fn_dual;
@@ -44,10 +58,10 @@ tree_fn fn_tree, fn_tree_quant;
 path_fn fn_path;
 compress_fn fn_compress;
 unpack_fn fn_unpack;
-PyTypeObject *layout_type, *text_type, *drafts_type, *rows_type;      // the binding's classes (kept alive)
+PyTypeObject *layout_type, *text_type, *drafts_type, *rows_type, *heads_type, *rope_type;      // the binding's classes (kept alive)
 
 PyObject *s_batch, *s_nq, *s_nkv, *s_hd, *s_keep, *s_dtype, *s_cap, *s_max_seq, *s_seq, *s_data_ptr, *s_numel, *s_esize, *s_cuda_stream,
-    *s_k, *s_v, *s_max_len, *s_len, *s_strides, *s_stride, *s_shape, *s_n_tokens, *s_n_tokens_dev, *s_mask, *s_data, *s_tok_idx, *s_tok_off;
+    *s_k, *s_v, *s_max_len, *s_len, *s_strides, *s_stride, *s_shape, *s_n_tokens, *s_n_tokens_dev, *s_mask, *s_data, *s_tok_idx, *s_tok_off, *s_pos, *s_inv_freq, *s_axis, *s_pairing, *s_n_axes;
 
 // All of these return false where the argument is not of the plain kind; an exception may then be set, and the caller clears it.
 bool integer(PyObject* o, long long* out)
@@ -202,6 +216,68 @@ bool rows(PyObject* o, rk_rows* r)
     r->stride_h = st[1];
     r->stride_t = st[2];
     return true;
+}
+// *at: out, or null for None
+bool heads(PyObject* o, rk_heads* out, const rk_heads** at)
+{
+    *at = nullptr;
+    if (o == Py_None) return true;
+    if (!heads_type || Py_TYPE(o) != heads_type) return false;
+    void* data = nullptr;
+    int64_t st[3];
+    if (!address_of(o, s_data, &data)) return false;
+    PyObject* key = PyObject_GetAttr(o, s_data);
+    PyObject* given = key ? PyObject_GetAttr(o, s_strides) : nullptr;
+    const bool ok = given && strides_of(given, key, st);
+    Py_XDECREF(given);
+    Py_XDECREF(key);
+    if (!ok) return false;
+    out->data = data;
+    out->stride_b = st[0];
+    out->stride_h = st[1];
+    out->stride_t = st[2];
+    *at = out;
+    return true;
+}
+// axes as bytes (what Rope makes of them), and neither strides nor a count of axes given
+bool rotary(PyObject* o, rk_rotary* r)
+{
+    if (!rope_type || Py_TYPE(o) != rope_type) return false;
+    void *pos = nullptr, *freq = nullptr;
+    if (!address_of(o, s_pos, &pos) || !address_of(o, s_inv_freq, &freq) || !int32_of(o, s_pairing, &r->pairing)) return false;
+    PyObject* axis = PyObject_GetAttr(o, s_axis);
+    PyObject* given = axis ? PyObject_GetAttr(o, s_strides) : nullptr;
+    PyObject* count = given ? PyObject_GetAttr(o, s_n_axes) : nullptr;
+    PyObject* key = count ? PyObject_GetAttr(o, s_pos) : nullptr;
+    bool ok = key && PyBytes_CheckExact(axis) && PyBytes_GET_SIZE(axis) <= RK_MAX_PAIRS && given == Py_None && count == Py_None;
+    long long st[2] = {0, 0}, axes = 0;
+    if (ok) {
+        r->n_pairs = (int32_t)PyBytes_GET_SIZE(axis);
+        for (int i = 0; i < RK_MAX_PAIRS; ++i) r->axis[i] = i < r->n_pairs ? (uint8_t)PyBytes_AS_STRING(axis)[i] : 0;
+        PyObject* t = PyObject_CallMethodNoArgs(key, s_stride);
+        PyObject* shape = t ? PyObject_GetAttr(key, s_shape) : nullptr;
+        ok = shape && PyTuple_Check(t) && PyTuple_GET_SIZE(t) >= 2 && integer(PyTuple_GET_ITEM(t, 0), st) && integer(PyTuple_GET_ITEM(t, 1), st + 1) &&
+             PyTuple_Check(shape) && PyTuple_GET_SIZE(shape) >= 1 && integer(PyTuple_GET_ITEM(shape, 0), &axes) && axes >= 0 && axes <= INT32_MAX;
+        Py_XDECREF(shape);
+        Py_XDECREF(t);
+    }
+    Py_XDECREF(key);
+    Py_XDECREF(count);
+    Py_XDECREF(given);
+    Py_XDECREF(axis);
+    r->pos = (const int32_t*)pos;
+    r->inv_freq = (const float*)freq;
+    r->stride_a = st[0];
+    r->stride_b = st[1];
+    r->n_axes = (int32_t)axes;
+    return ok;
+}
+bool int32_arg(PyObject* o, int32_t* out)
+{
+    long long x = 0;
+    const bool ok = integer(o, &x) && x >= INT32_MIN && x <= INT32_MAX;
+    *out = (int32_t)x;
+    return ok;
 }
 bool stream_of(PyObject* o, void** out)
 {
@@ -399,6 +475,84 @@ PyObject* py_unpack_quant(PyObject*, PyObject* const* a, Py_ssize_t n)
     return answer(s);
 }
 
+// (ctx, layout, rope, n_tokens, q, q_out, k, k_out, flags, n_tokens_dev, stream)
+PyObject* py_rope(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    void *ctx, *count, *stream;
+    rk_layout L;
+    rk_rotary r;
+    rk_heads h[4];
+    const rk_heads* at[4];
+    int32_t tokens, flags;
+    if (n != 11 || !fn_rope || !address(a[0], &ctx) || !layout(a[1], &L) || !rotary(a[2], &r) || !int32_arg(a[3], &tokens) ||
+        !heads(a[4], h, at) || !heads(a[5], h + 1, at + 1) || !heads(a[6], h + 2, at + 2) || !heads(a[7], h + 3, at + 3) || !int32_arg(a[8], &flags) ||
+        flags < 0 || !address(a[9], &count) || !stream_of(a[10], &stream))
+        return other_path();
+    rk_status s;
+    Py_BEGIN_ALLOW_THREADS
+    s = fn_rope((rk_ctx*)ctx, &L, &r, tokens, (const int32_t*)count, at[0], at[1], at[2], at[3], (uint32_t)flags, stream);
+    Py_END_ALLOW_THREADS
+    return answer(s);
+}
+// (ctx, layout, rope, n_tokens, q, q_out, k, v, text, len_out, n_tokens_dev, stream)
+PyObject* py_rope_append(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    void *ctx, *len, *count, *stream;
+    rk_layout L;
+    rk_rotary r;
+    rk_heads h[4];
+    const rk_heads* at[4];
+    rk_text T;
+    int32_t tokens;
+    if (n != 12 || !fn_rope_append || !address(a[0], &ctx) || !layout(a[1], &L) || !rotary(a[2], &r) || !int32_arg(a[3], &tokens) ||
+        !heads(a[4], h, at) || !heads(a[5], h + 1, at + 1) || !heads(a[6], h + 2, at + 2) || !heads(a[7], h + 3, at + 3) || !text(a[8], &T) ||
+        !address(a[9], &len) || !address(a[10], &count) || !stream_of(a[11], &stream))
+        return other_path();
+    rk_status s;
+    Py_BEGIN_ALLOW_THREADS
+    s = fn_rope_append((rk_ctx*)ctx, &L, &r, tokens, (const int32_t*)count, at[0], at[1], at[2], at[3], &T, (int32_t*)len, stream);
+    Py_END_ALLOW_THREADS
+    return answer(s);
+}
+// (ctx, layout, q, n_tokens, text, window, sinks, out, n_tokens_dev, then as the others, without an address for out)
+PyObject* py_prefill(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    void *ctx, *count;
+    rk_layout L;
+    rk_heads h[2];
+    const rk_heads* at[2];
+    rk_text T;
+    Tail t;
+    int32_t tokens, window, sinks;
+    if (n != 14 || !fn_prefill || !address(a[0], &ctx) || !layout(a[1], &L) || !heads(a[2], h, at) || !int32_arg(a[3], &tokens) || !text(a[4], &T) ||
+        !int32_arg(a[5], &window) || !int32_arg(a[6], &sinks) || !heads(a[7], h + 1, at + 1) || !address(a[8], &count) || !tail(a + 9, &t))
+        return other_path();
+    rk_status s;
+    Py_BEGIN_ALLOW_THREADS
+    s = fn_prefill((rk_ctx*)ctx, &L, at[0], tokens, (const int32_t*)count, &T, window, sinks, t.scale, at[1], t.ws, t.bytes, t.stream);
+    Py_END_ALLOW_THREADS
+    return answer(s);
+}
+// (ctx, layout, q, k_cache, v_cache, R_r, delta_mu, text, window, sinks, scale, out, workspace, stream, workspace_bytes)
+PyObject* window(window_fn f, PyObject* const* a, Py_ssize_t n)
+{
+    void *ctx, *p[5];
+    rk_layout L;
+    rk_text T;
+    Tail t;
+    int32_t size, sinks;
+    if (n != 15 || !f || !address(a[0], &ctx) || !layout(a[1], &L) || !addresses(a + 2, 5, p) || !text(a[7], &T) || !int32_arg(a[8], &size) ||
+        !int32_arg(a[9], &sinks) || !tail(a + 10, &t))
+        return other_path();
+    rk_status s;
+    Py_BEGIN_ALLOW_THREADS
+    s = f((rk_ctx*)ctx, &L, p[0], p[1], p[2], (const float*)p[3], (const float*)p[4], &T, size, sinks, t.scale, t.out, t.ws, t.bytes, t.stream);
+    Py_END_ALLOW_THREADS
+    return answer(s);
+}
+PyObject* py_window(PyObject*, PyObject* const* a, Py_ssize_t n) { return window(fn_window, a, n); }
+PyObject* py_window_quant(PyObject*, PyObject* const* a, Py_ssize_t n) { return window(fn_window_quant, a, n); }
+
 // bind(Layout, Text, addresses of the four entry points)
 PyObject* py_bind(PyObject*, PyObject* args)
 {
@@ -440,7 +594,33 @@ PyObject* py_bind_drafts(PyObject*, PyObject* args)
     Py_RETURN_NONE;
 }
 
+// bind_window(Heads, Rope, addresses of the five entry points)
+PyObject* py_bind_window(PyObject*, PyObject* args)
+{
+    PyObject *ht, *rt;
+    unsigned long long f[5];
+    if (!PyArg_ParseTuple(args, "O!O!KKKKK", &PyType_Type, &ht, &PyType_Type, &rt, f, f + 1, f + 2, f + 3, f + 4)) return nullptr;
+    Py_INCREF(ht);
+    Py_INCREF(rt);
+    Py_XDECREF((PyObject*)heads_type);
+    Py_XDECREF((PyObject*)rope_type);
+    heads_type = (PyTypeObject*)ht;
+    rope_type = (PyTypeObject*)rt;
+    fn_rope = (rope_fn)(uintptr_t)f[0];
+    fn_rope_append = (rope_append_fn)(uintptr_t)f[1];
+    fn_prefill = (prefill_fn)(uintptr_t)f[2];
+    fn_window = (window_fn)(uintptr_t)f[3];
+    fn_window_quant = (window_fn)(uintptr_t)f[4];
+    Py_RETURN_NONE;
+}
+
 PyMethodDef methods[] = {
+    {"bind_window", py_bind_window, METH_VARARGS, "bind_window(Heads, Rope, five entry point addresses)"},
+    {"rope", (PyCFunction)(void (*)(void))py_rope, METH_FASTCALL, "rk_rope; its status, or None for arguments not taken here"},
+    {"rope_append", (PyCFunction)(void (*)(void))py_rope_append, METH_FASTCALL, "rk_rope_append_text, likewise"},
+    {"prefill", (PyCFunction)(void (*)(void))py_prefill, METH_FASTCALL, "rk_prefill_attn_window, likewise"},
+    {"window", (PyCFunction)(void (*)(void))py_window, METH_FASTCALL, "rk_decode_attn_window, likewise"},
+    {"window_quant", (PyCFunction)(void (*)(void))py_window_quant, METH_FASTCALL, "rk_decode_attn_window_quant, likewise"},
     {"bind_drafts", py_bind_drafts, METH_VARARGS, "bind_drafts(Drafts, Rows, seven entry point addresses)"},
     {"append_quant", (PyCFunction)(void (*)(void))py_append_quant, METH_FASTCALL, "rk_append_quant; its status, or None for arguments not taken here"},
     {"decode_quant", (PyCFunction)(void (*)(void))py_decode_quant, METH_FASTCALL, "rk_decode_attn_quant, likewise"},
@@ -469,7 +649,8 @@ PyMODINIT_FUNC PyInit__rkbind(void)
         {&s_esize, "element_size"}, {&s_cuda_stream, "cuda_stream"}, {&s_k, "k"}, {&s_v, "v"}, {&s_max_len, "max_len"}, {&s_len, "len"},
         {&s_strides, "strides"}, {&s_stride, "stride"}, {&s_shape, "shape"},
         {&s_n_tokens, "n_tokens"}, {&s_n_tokens_dev, "n_tokens_dev"}, {&s_mask, "mask"}, {&s_data, "data"},
-        {&s_tok_idx, "tok_idx"}, {&s_tok_off, "tok_off"}};
+        {&s_tok_idx, "tok_idx"}, {&s_tok_off, "tok_off"}, {&s_pos, "pos"}, {&s_inv_freq, "inv_freq"}, {&s_axis, "axis"},
+        {&s_pairing, "pairing"}, {&s_n_axes, "n_axes"}};
     for (auto& x : names)
         if (!(*x.at = PyUnicode_InternFromString(x.text))) return nullptr;
     return PyModule_Create(&module);
