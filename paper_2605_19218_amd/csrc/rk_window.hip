@@ -17,8 +17,6 @@ namespace rk {
 
 namespace {
 
-constexpr int PROMPT_ROWS = 128, PROMPT_TOKENS = 32;
-
 // Slots of 16 bytes of a token's row in LDS lie permuted by the token, so that eight tokens' same slot, and four tokens' same pair of slots, are in other banks.
 __device__ __forceinline__ int slot_of(int token, int slot) { return slot ^ (2 * (token & 3) | ((token >> 2) & 1)); }
 
@@ -40,291 +38,6 @@ __device__ __forceinline__ void prompt_place(const PrefillArgs& A, int& block, i
     split = rank % A.S;
 }
 
-struct PromptBf16 {
-    typedef bf16_t T;
-    static constexpr int ROW = 256, TILE = PROMPT_TOKENS * ROW;       // bytes of a token's Key (or Value) and of a stage's
-    bf16x8 q[8];
-    uint4 k[2], v[2];
-    __device__ __forceinline__ void take(const T* row, int h)
-    {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) q[i] = *(const bf16x8*)(row + 16 * i + 8 * h);
-    }
-    __device__ __forceinline__ void load(const T* kp, const T* vp, int64_t st, int j0, int last, int tid)
-    {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int64_t at = (int64_t)min(j0 + 16 * i + (tid >> 4), last) * st + 8 * (tid & 15);
-            k[i] = *(const uint4*)(kp + at);
-            v[i] = *(const uint4*)(vp + at);
-        }
-    }
-    __device__ __forceinline__ void store(char* kb, char* vb, int tid) const
-    {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int m = 16 * i + (tid >> 4), at = m * ROW + 16 * slot_of(m, tid & 15);
-            *(uint4*)(kb + at) = k[i];
-            *(uint4*)(vb + at) = v[i];
-        }
-    }
-    __device__ __forceinline__ void scores(const char* kb, f32x16& s, int h, int n) const
-    {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[i] = 0.f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const bf16x8 a = *(const bf16x8*)(kb + n * ROW + 16 * slot_of(n, 2 * i + h));
-            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, q[i], s, 0, 0, 0);
-        }
-    }
-    // CLEAN: Values that are no numbers count as 0; the answer: whether there are any
-    template <bool CLEAN>
-    __device__ __forceinline__ bool product(const char* vb, const f32x16& w, f32x16 (&O)[4], int lane) const
-    {
-        const int h = lane >> 5, nh = (lane >> 4) & 1, i = lane & 15;
-        bool odd = false;
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            uint32_t p[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) p[e] = __builtin_bit_cast(uint32_t, (bf16x2){(__bf16)w[8 * t + 2 * e], (__bf16)w[8 * t + 2 * e + 1]});
-            const bf16x8 b = __builtin_bit_cast(bf16x8, make_uint4(p[0], p[1], p[2], p[3]));
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                uint32_t a[4];
-#pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    const int m = 16 * t + 8 * x + 4 * h + (i >> 2);
-                    typedef __attribute__((address_space(3))) s16x4* Lds;
-                    const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(vb + m * ROW + 16 * slot_of(m, 4 * c + 2 * nh + ((i & 3) >> 1)) + 8 * (i & 1)));
-                    const uint2 z = __builtin_bit_cast(uint2, y);
-                    a[2 * x] = z.x;
-                    a[2 * x + 1] = z.y;
-                }
-                if constexpr (CLEAN) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const uint32_t keep = (odd_value(a[e]) ? 0u : 0xffff0000u) | (odd_value(a[e] << 16) ? 0u : 0xffffu);
-                        odd |= keep != ~0u;
-                        a[e] &= keep;
-                    }
-                }
-                O[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, make_uint4(a[0], a[1], a[2], a[3])), b, O[c], 0, 0, 0);
-            }
-        }
-        return odd;
-    }
-    // channel of accumulator i of block c
-    static __device__ __forceinline__ int channel(int c, int i, int h) { return 32 * c + 8 * (i >> 2) + 4 * h + (i & 3); }
-    static __device__ __forceinline__ float value(const char* vb, int m, int ch)
-    {
-        return bf16_to_f32(*(const bf16_t*)(vb + m * ROW + 16 * slot_of(m, ch >> 3) + 2 * (ch & 7)));
-    }
-};
-
-struct PromptF32 {
-    typedef float T;
-    static constexpr int ROW = 512, TILE = PROMPT_TOKENS * ROW;
-    f32x4 q[16];
-    uint4 k[4], v[4];
-    __device__ __forceinline__ void take(const T* row, int h)
-    {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) q[i] = *(const f32x4*)(row + 8 * i + 4 * h);
-    }
-    __device__ __forceinline__ void load(const T* kp, const T* vp, int64_t st, int j0, int last, int tid)
-    {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int64_t at = (int64_t)min(j0 + 8 * i + (tid >> 5), last) * st + 4 * (tid & 31);
-            k[i] = *(const uint4*)(kp + at);
-            v[i] = *(const uint4*)(vp + at);
-        }
-    }
-    __device__ __forceinline__ void store(char* kb, char* vb, int tid) const
-    {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int m = 8 * i + (tid >> 5), at = m * ROW + 16 * slot_of(m, tid & 31);
-            *(uint4*)(kb + at) = k[i];
-            *(uint4*)(vb + at) = v[i];
-        }
-    }
-    __device__ __forceinline__ void scores(const char* kb, f32x16& s, int h, int n) const
-    {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[i] = 0.f;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const f32x4 a = *(const f32x4*)(kb + n * ROW + 16 * slot_of(n, 2 * i + h));
-#pragma unroll
-            for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], q[i][e], s, 0, 0, 0);
-        }
-    }
-    template <bool CLEAN>
-    __device__ __forceinline__ bool product(const char* vb, const f32x16& w, f32x16 (&O)[4], int lane) const
-    {
-        const int h = lane >> 5, n = lane & 31;
-        bool odd = false;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int m = 8 * (i >> 2) + 4 * h + (i & 3);
-            f32x4 a = *(const f32x4*)(vb + m * ROW + 16 * slot_of(m, n));
-            if constexpr (CLEAN) {
-#pragma unroll
-                for (int c = 0; c < 4; ++c)
-                    if (odd_value(__float_as_uint(a[c]))) {
-                        odd = true;
-                        a[c] = 0.f;
-                    }
-            }
-#pragma unroll
-            for (int c = 0; c < 4; ++c) O[c] = __builtin_amdgcn_mfma_f32_32x32x2f32(a[c], w[i], O[c], 0, 0, 0);
-        }
-        return odd;
-    }
-    static __device__ __forceinline__ int channel(int c, int i, int h) { return 4 * (8 * (i >> 2) + 4 * h + (i & 3)) + c; }
-    static __device__ __forceinline__ float value(const char* vb, int m, int ch)
-    {
-        return *(const float*)(vb + m * ROW + 16 * slot_of(m, ch >> 2) + 4 * (ch & 3));
-    }
-};
-
-template <typename P>
-__global__ __launch_bounds__(256, 2) void attn_prompt(PrefillArgs A)
-{
-    typedef typename P::T T;
-    __shared__ __attribute__((aligned(16))) char lds[4 * P::TILE];    // two stages of Keys and Values
-
-    int block, split, u;
-    prompt_place(A, block, split, u);
-    const int b = u / A.Hkv, hk = u - b * A.Hkv;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, n = lane & 31;
-
-    const int len = min(max(A.len ? A.len[b] : A.max_len, 0), A.max_len), fresh = min(max(A.n_dev ? A.n_dev[b] : A.n, 0), A.n);
-    const int first = len - fresh;                         // the first new token's position
-    const int64_t rows = (int64_t)fresh * A.G, row0 = (int64_t)block * PROMPT_ROWS;
-    if (row0 >= rows) return;
-    auto token = [&](int64_t r) { return (int)((r < rows ? r : rows - 1) / A.G); };
-    const int64_t row = row0 + 32 * wave + n, mine = row < rows ? row : rows - 1;
-    const int tok = token(row), head = hk * A.G + (int)(mine - (int64_t)tok * A.G);
-    const int window = A.window > 0 ? A.window : 0x7fffffff;
-    const Sight sight{first + tok, window, A.sinks};
-
-    P tile;
-    tile.take((const T*)A.q + (int64_t)b * A.q_sb + (int64_t)head * A.q_sh + (int64_t)tok * A.q_st, h);
-
-    // tiles that any row of the block sees: `few` of the sinks, and from `from` on
-    const int p_hi = first + token(row0 + PROMPT_ROWS - 1), p_lo = max(first + token(row0), 0);
-    int few = 0, from = 0, tiles = 0;
-    if (p_hi >= 0) {
-        const int lo = A.window > 0 ? max(p_lo - A.window + 1, 0) : 0;
-        from = lo / PROMPT_TOKENS;
-        few = min((min(A.sinks, lo) + PROMPT_TOKENS - 1) / PROMPT_TOKENS, from);
-        tiles = few + p_hi / PROMPT_TOKENS - from + 1;
-    }
-    const int i0 = (int)((int64_t)tiles * split / A.S), i1 = (int)((int64_t)tiles * (split + 1) / A.S);
-    auto start = [&](int i) { return PROMPT_TOKENS * (i < few ? i : i - few + from); };
-    const int w_lo = first + token(row0 + 32 * wave), w_hi = first + token(row0 + 32 * wave + 31);     // positions of the wave's rows
-
-    const T* kp = (const T*)A.k + (int64_t)b * A.sb + (int64_t)hk * A.sh;
-    const T* vp = (const T*)A.v + (int64_t)b * A.sb + (int64_t)hk * A.sh;
-    float m = ROWS_NEG_INF, l = 0.f;                       // log2 domain; l: this lane's tokens only, until the end
-    f32x16 O[4];
-#pragma unroll
-    for (int c = 0; c < 4; ++c)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) O[c][i] = 0.f;
-
-    if (i0 < i1) {
-        tile.load(kp, vp, A.st, start(i0), len - 1, tid);
-        tile.store(lds, lds + P::TILE, tid);
-    }
-    __syncthreads();
-    for (int i = i0; i < i1; ++i) {
-        const char* kb = lds + ((i - i0) & 1) * 2 * P::TILE;
-        char* next = lds + ((i - i0 + 1) & 1) * 2 * P::TILE;
-        if (i + 1 < i1) tile.load(kp, vp, A.st, start(i + 1), len - 1, tid);
-        const int j0 = start(i), j1 = j0 + PROMPT_TOKENS - 1;
-        const bool none = j0 > w_hi || (j0 >= A.sinks && w_lo - j1 >= window);
-        if (!none) {
-            const bool all = j1 <= w_lo && (j1 < A.sinks || w_hi - j0 < window);
-            f32x16 s;
-            tile.scores(kb, s, h, n);
-            float mt = ROWS_NEG_INF;
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                s[e] *= A.scale_log2;
-                if (!all) s[e] = sight.of(j0 + 8 * (e >> 2) + 4 * h + (e & 3)) ? s[e] : ROWS_NEG_INF;
-                mt = fmaxf(mt, s[e]);
-            }
-            mt = halves_max(mt);
-            // (the maximum moves when it is behind by 2^8, as in attn_rows; a sum that holds an infinity may not meet a factor of 0)
-            if (__any(mt > m + 8.f)) {
-                const float m_new = fmaxf(m, mt), alpha = m > ROWS_NEG_INF ? fmaxf(rows_exp2(m - m_new), 0x1p-126f) : 0.f;
-                l *= alpha;
-                if (m > ROWS_NEG_INF) {
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) O[c] *= alpha;
-                }
-                m = m_new;
-            }
-            const float ref = m > ROWS_NEG_INF ? m : 0.f;
-            float sum = 0.f;
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                s[e] = rows_exp2(s[e] - ref);
-                sum += s[e];
-            }
-            l += sum;
-            if (all) {
-                tile.template product<false>(kb + P::TILE, s, O, lane);
-            } else if (__any(tile.template product<true>(kb + P::TILE, s, O, lane))) {
-#pragma unroll 1
-                for (int j = 0; j < PROMPT_TOKENS; ++j) {
-                    const bool seen = sight.of(j0 + j);
-#pragma unroll
-                    for (int c = 0; c < 4; ++c)
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            const float x = P::value(kb + P::TILE, j, P::channel(c, e, h));
-                            O[c][e] += seen && odd_value(__float_as_uint(x)) ? x : 0.f;
-                        }
-                }
-            }
-        }
-        if (i + 1 < i1) tile.store(next, next + P::TILE, tid);
-        __syncthreads();
-    }
-
-    l = halves_sum(l);
-    if (row >= rows) return;
-    if (A.S == 1) {
-        const float inv = l == 0.f ? 0.f : 1.f / l;
-        T* o = (T*)A.out + (int64_t)b * A.o_sb + (int64_t)head * A.o_sh + (int64_t)tok * A.o_st;
-#pragma unroll
-        for (int c = 0; c < 4; ++c)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) st_elem(o + P::channel(c, e, h), l == 0.f ? 0.f : O[c][e] * inv);
-    } else {
-        const size_t slot = ((size_t)u * A.n * A.G + row) * A.S + split;
-#pragma unroll
-        for (int c = 0; c < 4; ++c)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) A.ws_acc[slot * D + P::channel(c, e, h)] = O[c][e];
-        if (h == 0) { A.ws_m[slot] = m; A.ws_l[slot] = l; }
-    }
-}
-
-
-// ---- bf16, many rows: 64 rows a wave ------------------------------------------------
-// A stage of 64 tokens, four of them in LDS: loads go there without passing through registers, two stages ahead, one barrier a stage. Rows in two groups of 32, so that a Key or Value
-// read from LDS feeds two products.
-// In LDS a token's row is its 256 bytes, slots permuted as slot_of() says: what a load leaves is lane by lane, so it is the lanes' addresses that are permuted.
-constexpr int WIDE_ROWS = 256, WIDE_TOKENS = 64, WIDE_ROW = 256, WIDE_VALUES = WIDE_TOKENS * WIDE_ROW, WIDE_STAGE = 2 * WIDE_VALUES;
-constexpr int WIDE_LDS = 4 * WIDE_STAGE;      // and a flag
-
 __device__ __forceinline__ uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)p; }
 // 16 bytes a lane from `from` to LDS at `to` (of the wave) + 16 lane. (Not the builtin: behind it every read of LDS waits for all loads.) What is asked for
 // is there after stage_wait().
@@ -335,6 +48,210 @@ __device__ __forceinline__ void load_to_lds(const void* from, uint32_t to)
 // this wave's loads but the last N are there
 template <int N>
 __device__ __forceinline__ void stage_wait() { asm volatile("s_waitcnt vmcnt(%0)" : : "i"(N) : "memory"); }
+
+
+// What a block of `size` rows sees, in stages of TOKENS rows of the segment: `few` of the sinks, and from `from` on.
+template <int TOKENS>
+struct Prompt {
+    int b, hk, len, first, rows, row0, window, sinks, p_lo, p_hi, few, from, i0, i1;
+    bool before;                 // some of the rows stand in front of row 0
+    __device__ __forceinline__ Prompt(const PrefillArgs& A, int u, int block, int split, int size)
+    {
+        b = u / A.Hkv;
+        hk = u - b * A.Hkv;
+        len = min(max(A.len ? A.len[b] : A.max_len, 0), A.max_len);
+        const int fresh = min(max(A.n_dev ? A.n_dev[b] : A.n, 0), A.n);
+        first = len - fresh;
+        rows = fresh * A.G;
+        row0 = block * size;
+        window = A.window > 0 ? A.window : 0x7fffffff;
+        sinks = A.sinks;
+        if (row0 >= rows) return;
+        p_lo = first + token(A, row0);
+        p_hi = first + token(A, row0 + size - 1);
+        before = p_lo < 0;
+        p_lo = max(p_lo, 0);
+        int stages = 0;
+        few = from = 0;
+        if (p_hi >= 0) {
+            const int lo = A.window > 0 ? max(p_lo - A.window + 1, 0) : 0;
+            from = lo / TOKENS;
+            few = min((min(sinks, lo) + TOKENS - 1) / TOKENS, from);
+            stages = few + p_hi / TOKENS - from + 1;
+        }
+        // (stages and splits stay below 2^25 and 2^6)
+        i0 = (int)((uint32_t)stages * (uint32_t)split / (uint32_t)A.S);
+        i1 = (int)((uint32_t)stages * (uint32_t)(split + 1) / (uint32_t)A.S);
+    }
+    __device__ __forceinline__ int token(const PrefillArgs& A, int r) const { return (int)((uint32_t)min(r, rows - 1) / (uint32_t)A.G); }
+    __device__ __forceinline__ int start(int i) const { return TOKENS * (i < few ? i : i - few + from); }
+    // whether all rows from position lo to hi see rows j ..+n-1
+    __device__ __forceinline__ bool inside(int j, int n, int lo, int hi) const { return j + n - 1 <= lo && (j + n - 1 < sinks || hi - j < window); }
+    // whether a stage is masked for some row of the block
+    __device__ __forceinline__ bool edge(int j) const { return before || !inside(j, TOKENS, p_lo, p_hi); }
+};
+
+// Values of a stage in LDS that are no numbers become 0 (what a masked one holds may not meet a weight of 0), and the flag says that there were any
+template <typename T>
+__device__ __forceinline__ void clean_values(char* values, int bytes, int* odd, int tid)
+{
+#pragma unroll 1
+    for (int x = 16 * tid; x < bytes; x += 4096) {
+        const uint4 d = *(const uint4*)(values + x);
+        uint32_t w[4] = {d.x, d.y, d.z, d.w};
+        bool any = false;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t keep = sizeof(T) == 4 ? (odd_value(w[e]) ? 0u : ~0u) : (odd_value(w[e]) ? 0u : 0xffff0000u) | (odd_value(w[e] << 16) ? 0u : 0xffffu);
+            any |= keep != ~0u;
+            w[e] &= keep;
+        }
+        if (any) {
+            *(uint4*)(values + x) = make_uint4(w[0], w[1], w[2], w[3]);
+            *odd = 1;
+        }
+    }
+}
+
+// ---- fp32 --------------------------------------------------------------------------
+// 32 rows a wave, 128 a work-group, two work-groups a compute unit; stages of 32 tokens in LDS, two of them. Bound by the fp32 matrix instructions: 128 of 64 cycles
+// for a tile, to some 500 cycles of vector instructions.
+constexpr int F32_ROWS = 128, F32_TOKENS = 32, F32_ROW = 512, F32_VALUES = F32_TOKENS * F32_ROW, F32_STAGE = 2 * F32_VALUES;
+
+__global__ __launch_bounds__(256, 2) void attn_prompt_f32(PrefillArgs A)
+{
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    int block, split, u;
+    prompt_place(A, block, split, u);
+    const Prompt<F32_TOKENS> P(A, u, block, split, F32_ROWS);
+    if (P.row0 >= P.rows) return;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, n = lane & 31;
+    const int row = P.row0 + 32 * wave + n, mine = min(row, P.rows - 1), tok = P.token(A, mine), head = P.hk * A.G + mine - tok * A.G;
+    const Sight sight{P.first + tok, P.window, P.sinks};
+    const int w_lo = P.first + P.token(A, P.row0 + 32 * wave), w_hi = P.first + P.token(A, P.row0 + 32 * wave + 31);
+
+    f32x4 q[16];
+    const float* qp = (const float*)A.q + (int64_t)P.b * A.q_sb + (int64_t)head * A.q_sh + (int64_t)tok * A.q_st;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) q[i] = *(const f32x4*)(qp + 8 * i + 4 * h);
+    const float* kp = (const float*)A.k + (int64_t)P.b * A.sb + (int64_t)P.hk * A.sh;
+    const float* vp = (const float*)A.v + (int64_t)P.b * A.sb + (int64_t)P.hk * A.sh;
+    float m = ROWS_NEG_INF, l = 0.f;
+    f32x16 O[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) O[c][i] = 0.f;
+
+    int* odd = (int*)(lds + 2 * F32_STAGE);
+    if (P.i0 < P.i1) {
+        // rows 8 wave + 2 x + lane / 32 of a stage, x < 4
+        const uint32_t base = __builtin_amdgcn_readfirstlane(lds_address(lds)) + 8 * F32_ROW * wave;
+        auto fetch = [&](int i, int buf) {
+            const int j = P.start(i) + 8 * wave + h;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                const int64_t at = (int64_t)min(j + 2 * x, P.len - 1) * A.st + 4 * slot_of(2 * x + h, n);
+                load_to_lds(kp + at, base + buf + 2 * F32_ROW * x);
+                load_to_lds(vp + at, base + buf + F32_VALUES + 2 * F32_ROW * x);
+            }
+        };
+        fetch(P.i0, 0);
+        if (tid == 0) *odd = 0;
+        int ka[4], va[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            ka[i] = n * F32_ROW + 16 * slot_of(n, 2 * i + h);
+            va[i] = F32_VALUES + (4 * h + i) * F32_ROW + 16 * slot_of(4 * h + i, n);
+        }
+        int now = 0;
+#pragma unroll 1
+        for (int i = P.i0; i < P.i1; ++i) {
+            const int j0 = P.start(i);
+            stage_wait<0>();
+            lds_barrier();               // (this stage is there for all waves, and nobody reads the one before it any more)
+            fetch(min(i + 1, P.i1 - 1), now ^ F32_STAGE);
+            if (P.edge(j0)) {
+                clean_values<float>(lds + now + F32_VALUES, F32_VALUES, odd, tid);
+                lds_barrier();
+            }
+            f32x16 s;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[e] = 0.f;
+#pragma unroll
+            for (int x = 0; x < 16; ++x) {
+                const f32x4 a = *(const f32x4*)(lds + now + ka[x & 3] + 128 * (x >> 2));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], q[x][e], s, 0, 0, 0);
+            }
+            if (!P.inside(j0, F32_TOKENS, w_lo, w_hi)) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[e] = sight.of(j0 + 8 * (e >> 2) + 4 * h + (e & 3)) ? s[e] : ROWS_NEG_INF;
+            }
+            float mt = s[0];
+#pragma unroll
+            for (int e = 1; e < 16; ++e) mt = fmaxf(mt, s[e]);
+            mt = halves_max(mt) * A.scale_log2;
+            if (__any(mt > m + 8.f)) {
+                const float m_new = fmaxf(m, mt), alpha = m > ROWS_NEG_INF ? rows_exp2(m - m_new) : 1.f;
+                l *= alpha;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) O[c] *= alpha;
+                m = m_new;
+            }
+            const float ref = m > ROWS_NEG_INF ? m : 0.f;
+            float sum = 0.f;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                s[e] = rows_exp2(fmaf(s[e], A.scale_log2, -ref));
+                sum += s[e];
+            }
+            l += sum;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const f32x4 a = *(const f32x4*)(lds + now + va[e & 3] + 8 * F32_ROW * (e >> 2));
+#pragma unroll
+                for (int c = 0; c < 4; ++c) O[c] = __builtin_amdgcn_mfma_f32_32x32x2f32(a[c], s[e], O[c], 0, 0, 0);
+            }
+            now ^= F32_STAGE;
+        }
+        stage_wait<0>();
+        // The Values that were left out join the rows that see them: a sum of one is it, or NaN.  (O[c][i] is channel 4 (8 (i / 4) + 4 h + i % 4) + c)
+        if (*odd) {
+#pragma unroll 1
+            for (int i = P.i0; i < P.i1; ++i) {
+                const int j0 = P.start(i);
+                if (!P.edge(j0)) continue;
+#pragma unroll 1
+                for (int j = j0; j < min(j0 + F32_TOKENS, P.len); ++j)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const f32x4 v = *(const f32x4*)(vp + (int64_t)j * A.st + 4 * (8 * (e >> 2) + 4 * h + (e & 3)));
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) O[c][e] += odd_value(__float_as_uint(v[c])) && sight.of(j) ? v[c] : 0.f;
+                    }
+            }
+        }
+    }
+
+    l = halves_sum(l);
+    if (row >= P.rows) return;
+    const float inv = A.S > 1 ? 1.f : l == 0.f ? 0.f : 1.f / l;
+    const size_t slot = ((size_t)u * A.n * A.G + row) * A.S + split;
+    float* o = A.S > 1 ? A.ws_acc + slot * D : (float*)A.out + (int64_t)P.b * A.o_sb + (int64_t)head * A.o_sh + (int64_t)tok * A.o_st;
+    const bool none = A.S == 1 && l == 0.f;
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+        *(f32x4*)(o + 4 * (8 * (e >> 2) + 4 * h + (e & 3))) = none ? (f32x4){0.f, 0.f, 0.f, 0.f} : (f32x4){O[0][e], O[1][e], O[2][e], O[3][e]} * inv;
+    if (A.S > 1 && h == 0) { A.ws_m[slot] = m; A.ws_l[slot] = l; }
+}
+
+// ---- bf16, many rows: 64 rows a wave ------------------------------------------------
+// A stage of 64 tokens, four of them in LDS: loads go there without passing through registers, two stages ahead, one barrier a stage. Rows in two groups of 32, so that a Key or Value
+// read from LDS feeds two products.
+// In LDS a token's row is its 256 bytes, slots permuted as slot_of() says: what a load leaves is lane by lane, so it is the lanes' addresses that are permuted.
+constexpr int WIDE_ROWS = 256, WIDE_TOKENS = 64, WIDE_ROW = 256, WIDE_VALUES = WIDE_TOKENS * WIDE_ROW, WIDE_STAGE = 2 * WIDE_VALUES;
+constexpr int WIDE_LDS = 4 * WIDE_STAGE;      // and a flag
 
 struct WideRows {
     bf16x8 q[2][8];
@@ -480,28 +397,22 @@ __global__ __launch_bounds__(256, 1) void attn_prompt_wide(PrefillArgs A)
     extern __shared__ __attribute__((aligned(16))) char lds[];
     int block, split, u;
     prompt_place(A, block, split, u);
-    const int b = u / A.Hkv, hk = u - b * A.Hkv;
+    const Prompt<WIDE_TOKENS> P(A, u, block, split, WIDE_ROWS);
+    if (P.row0 >= P.rows) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, n = lane & 31;
-
-    const int len = min(max(A.len ? A.len[b] : A.max_len, 0), A.max_len), fresh = min(max(A.n_dev ? A.n_dev[b] : A.n, 0), A.n);
-    const int first = len - fresh;
-    const int rows = fresh * A.G, row0 = block * WIDE_ROWS;
-    if (row0 >= rows) return;
-    auto token = [&](int r) { return (int)((uint32_t)min(r, rows - 1) / (uint32_t)A.G); };
-    const int window = A.window > 0 ? A.window : 0x7fffffff;
 
     WideRows W;
     W.c = A.scale_log2;
     int tok[2], head[2];
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
-        const int mine = min(row0 + 64 * wave + 32 * g + n, rows - 1);
-        tok[g] = token(mine);
-        head[g] = hk * A.G + mine - tok[g] * A.G;
-        W.sight[g] = Sight{first + tok[g], window, A.sinks};
+        const int mine = min(P.row0 + 64 * wave + 32 * g + n, P.rows - 1);
+        tok[g] = P.token(A, mine);
+        head[g] = P.hk * A.G + mine - tok[g] * A.G;
+        W.sight[g] = Sight{P.first + tok[g], P.window, P.sinks};
         W.m[g] = ROWS_NEG_INF;
         W.l[g] = 0.f;
-        const bf16_t* q = (const bf16_t*)A.q + (int64_t)b * A.q_sb + (int64_t)head[g] * A.q_sh + (int64_t)tok[g] * A.q_st;
+        const bf16_t* q = (const bf16_t*)A.q + (int64_t)P.b * A.q_sb + (int64_t)head[g] * A.q_sh + (int64_t)tok[g] * A.q_st;
 #pragma unroll
         for (int i = 0; i < 8; ++i) W.q[g][i] = *(const bf16x8*)(q + 16 * i + 8 * h);
 #pragma unroll
@@ -510,62 +421,29 @@ __global__ __launch_bounds__(256, 1) void attn_prompt_wide(PrefillArgs A)
             for (int i = 0; i < 16; ++i) W.O[g][c][i] = 0.f;
     }
 
-    // stages that any row of the block sees: `few` of the sinks, and from `from` on
-    const int p_hi = first + token(row0 + WIDE_ROWS - 1), p_lo = max(first + token(row0), 0);
-    int few = 0, from = 0, stages = 0;
-    if (p_hi >= 0) {
-        const int lo = A.window > 0 ? max(p_lo - A.window + 1, 0) : 0;
-        from = lo / WIDE_TOKENS;
-        few = min((min(A.sinks, lo) + WIDE_TOKENS - 1) / WIDE_TOKENS, from);
-        stages = few + p_hi / WIDE_TOKENS - from + 1;
-    }
-    const int i0 = (int)((int64_t)stages * split / A.S), i1 = (int)((int64_t)stages * (split + 1) / A.S);
-    auto start = [&](int i) { return WIDE_TOKENS * (i < few ? i : i - few + from); };
-    const int w_lo = first + token(row0 + 64 * wave), w_hi = first + token(row0 + 64 * wave + 63);      // positions of the wave's rows
-
-    const bf16_t* kp = (const bf16_t*)A.k + (int64_t)b * A.sb + (int64_t)hk * A.sh;
-    const bf16_t* vp = (const bf16_t*)A.v + (int64_t)b * A.sb + (int64_t)hk * A.sh;
+    const int w_lo = P.first + P.token(A, P.row0 + 64 * wave), w_hi = P.first + P.token(A, P.row0 + 64 * wave + 63);      // positions of the wave's rows
+    const bf16_t* kp = (const bf16_t*)A.k + (int64_t)P.b * A.sb + (int64_t)P.hk * A.sh;
+    const bf16_t* vp = (const bf16_t*)A.v + (int64_t)P.b * A.sb + (int64_t)P.hk * A.sh;
     int* odd = (int*)(lds + WIDE_LDS);
-    if (i0 < i1) {
+    if (P.i0 < P.i1) {
         // rows 16 wave + 4 i + lane / 16 of a stage, i < 4: their 16-byte pieces, in the order that slot_of() undoes
         const uint32_t base = __builtin_amdgcn_readfirstlane(lds_address(lds)) + 16 * WIDE_ROW * wave;
         auto fetch = [&](int i, int buf) {
-            const int j = start(i) + 16 * wave + (lane >> 4);
+            const int j = P.start(i) + 16 * wave + (lane >> 4);
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
-                const int64_t at = (int64_t)min(j + 4 * x, len - 1) * A.st + 8 * slot_of(4 * x + (lane >> 4), lane & 15);
+                const int64_t at = (int64_t)min(j + 4 * x, P.len - 1) * A.st + 8 * slot_of(4 * x + (lane >> 4), lane & 15);
                 load_to_lds(kp + at, base + buf + 4 * WIDE_ROW * x);
                 load_to_lds(vp + at, base + buf + WIDE_VALUES + 4 * WIDE_ROW * x);
             }
         };
-        // Stages that not all of the block's rows see whole: what a masked Value holds may not meet a weight of 0, so what is no number becomes 0 there.
-        auto edge = [&](int j) { return !(j + WIDE_TOKENS - 1 <= p_lo && (j + WIDE_TOKENS - 1 < A.sinks || p_hi - j < window)) || first + token(row0) < 0; };
-        auto clean = [&](char* buf) {
-#pragma unroll 1
-            for (int x = 0; x < 4; ++x) {
-                uint4* at = (uint4*)(buf + WIDE_VALUES + 4096 * x + 16 * tid);
-                const uint4 d = *at;
-                uint32_t w[4] = {d.x, d.y, d.z, d.w};
-                bool any = false;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const uint32_t keep = (odd_value(w[e]) ? 0u : 0xffff0000u) | (odd_value(w[e] << 16) ? 0u : 0xffffu);
-                    any |= keep != ~0u;
-                    w[e] &= keep;
-                }
-                if (any) {
-                    *at = make_uint4(w[0], w[1], w[2], w[3]);
-                    *odd = 1;
-                }
-            }
-        };
-#pragma unroll
-        for (int i = 0; i < 3; ++i) fetch(min(i0 + i, i1 - 1), i * WIDE_STAGE);
+        for (int i = 0; i < 3; ++i) fetch(min(P.i0 + i, P.i1 - 1), i * WIDE_STAGE);
         if (tid == 0) *odd = 0;
         stage_wait<16>();
         lds_barrier();
-        if (edge(start(i0))) {
-            clean(lds);
+        if (P.edge(P.start(P.i0))) {
+            clean_values<bf16_t>(lds + WIDE_VALUES, WIDE_VALUES, odd, tid);
             lds_barrier();
         }
         int ka[4], va[2];
@@ -589,21 +467,20 @@ __global__ __launch_bounds__(256, 1) void attn_prompt_wide(PrefillArgs A)
         }
         int now = 0;
 #pragma unroll 1
-        for (int i = i0; i < i1; ++i) {
+        for (int i = P.i0; i < P.i1; ++i) {
             W.hold();
-            const int j0 = start(i), next = (now + WIDE_STAGE) & (4 * WIDE_STAGE - 1);
+            const int j0 = P.start(i), next = (now + WIDE_STAGE) & (4 * WIDE_STAGE - 1);
             // The next stage's loads are all but the last eight.  Behind the barrier it is there for all waves, and nobody reads the one before this any more.
             stage_wait<8>();
             lds_barrier();
-            fetch(min(i + 3, i1 - 1), (now + 3 * WIDE_STAGE) & (4 * WIDE_STAGE - 1));
-            if (i + 1 < i1 && edge(start(i + 1))) {
-                clean(lds + next);
+            fetch(min(i + 3, P.i1 - 1), (now + 3 * WIDE_STAGE) & (4 * WIDE_STAGE - 1));
+            if (i + 1 < P.i1 && P.edge(P.start(i + 1))) {
+                clean_values<bf16_t>(lds + next + WIDE_VALUES, WIDE_VALUES, odd, tid);
                 lds_barrier();
             }
-            auto inside = [&](int j) { return j + 31 <= w_lo && (j + 31 < A.sinks || w_hi - j < window); };
-            if (!inside(j0)) W.hide(s0, top, j0, h);
+            if (!P.inside(j0, 32, w_lo, w_hi)) W.hide(s0, top, j0, h);
             W.tile(s0, s1, top, k, lds, ka, next, va, now + WIDE_VALUES);
-            if (!inside(j0 + 32)) W.hide(s1, top, j0 + 32, h);
+            if (!P.inside(j0 + 32, 32, w_lo, w_hi)) W.hide(s1, top, j0 + 32, h);
             W.tile(s1, s0, top, k, lds, ka, next + 32 * WIDE_ROW, va, now + WIDE_VALUES + 32 * WIDE_ROW);
             now = next;
         }
@@ -611,11 +488,11 @@ __global__ __launch_bounds__(256, 1) void attn_prompt_wide(PrefillArgs A)
         // The Values that were left out join the rows that see them: a sum of one is it, or NaN.
         if (*odd) {
 #pragma unroll 1
-            for (int i = i0; i < i1; ++i) {
-                const int j0 = start(i);
-                if (!edge(j0)) continue;
+            for (int i = P.i0; i < P.i1; ++i) {
+                const int j0 = P.start(i);
+                if (!P.edge(j0)) continue;
 #pragma unroll 1
-                for (int j = j0; j < min(j0 + WIDE_TOKENS, len); ++j)
+                for (int j = j0; j < min(j0 + WIDE_TOKENS, P.len); ++j)
 #pragma unroll
                     for (int b = 0; b < 4; ++b)
 #pragma unroll
@@ -635,11 +512,11 @@ __global__ __launch_bounds__(256, 1) void attn_prompt_wide(PrefillArgs A)
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
         const float l = halves_sum(W.l[g]);
-        const int row = row0 + 64 * wave + 32 * g + n;
-        if (row >= rows) continue;
+        const int row = P.row0 + 64 * wave + 32 * g + n;
+        if (row >= P.rows) continue;
         if (A.S == 1) {
             const float inv = l == 0.f ? 0.f : 1.f / l;
-            bf16_t* o = (bf16_t*)A.out + (int64_t)b * A.o_sb + (int64_t)head[g] * A.o_sh + (int64_t)tok[g] * A.o_st;
+            bf16_t* o = (bf16_t*)A.out + (int64_t)P.b * A.o_sb + (int64_t)head[g] * A.o_sh + (int64_t)tok[g] * A.o_st;
 #pragma unroll
             for (int c = 0; c < 4; ++c)
 #pragma unroll
@@ -684,18 +561,18 @@ __global__ __launch_bounds__(256) void prompt_merge(PrefillArgs A)
 
 }  // namespace
 
-int prefill_block_rows(int dtype) { return dtype == 0 ? PROMPT_ROWS : WIDE_ROWS; }
+int prefill_block_rows(int dtype) { return dtype == 0 ? F32_ROWS : WIDE_ROWS; }
 
 hipError_t launch_prefill(int dtype, const PrefillArgs& a, hipStream_t st)
 {
     const int64_t units = (int64_t)a.B * a.Hkv, groups = units * a.blocks * a.S;
     if (groups > 0x7fffffff || (units * a.n * a.G + 7) / 8 > 0x7fffffff) return hipErrorInvalidValue;
-    if (dtype == 0) attn_prompt<PromptF32><<<(uint32_t)groups, 256, 0, st>>>(a);
-    else {
-        const hipError_t e = allow_dynamic_lds((const void*)attn_prompt_wide, WIDE_LDS + 16);
-        if (e != hipSuccess) return e;
-        attn_prompt_wide<<<(uint32_t)groups, 256, WIDE_LDS + 16, st>>>(a);
-    }
+    const void* kernel = dtype == 0 ? (const void*)attn_prompt_f32 : (const void*)attn_prompt_wide;
+    const int lds = (dtype == 0 ? 2 * F32_STAGE : WIDE_LDS) + 16;
+    const hipError_t e = allow_dynamic_lds(kernel, lds);
+    if (e != hipSuccess) return e;
+    if (dtype == 0) attn_prompt_f32<<<(uint32_t)groups, 256, lds, st>>>(a);
+    else attn_prompt_wide<<<(uint32_t)groups, 256, lds, st>>>(a);
     if (a.S > 1) {
         const uint32_t g = (uint32_t)((units * a.n * a.G + 7) / 8);
         if (dtype == 0) prompt_merge<float><<<g, 256, 0, st>>>(a);
