@@ -300,21 +300,19 @@ struct WideRows {
         }
         return fmaxf(a, b);
     }
-    // the running maxima, after a tile's
+    // (log2 domain, of the whole row)
+    __device__ __forceinline__ float row_most(float mine) const { return halves_max(mine) * c; }
+    __device__ __forceinline__ bool behind(const float (&top)[2]) const { return __any(top[0] > m[0] + 8.f || top[1] > m[1] + 8.f); }
+    // the running maxima move to a tile's
     __device__ __forceinline__ void follow(const float (&top)[2])
     {
-        float mt[2];
 #pragma unroll
-        for (int g = 0; g < 2; ++g) mt[g] = halves_max(top[g]) * c;
-        if (__any(mt[0] > m[0] + 8.f || mt[1] > m[1] + 8.f)) {
+        for (int g = 0; g < 2; ++g) {
+            const float m_new = fmaxf(m[g], top[g]), alpha = m[g] > ROWS_NEG_INF ? rows_exp2(m[g] - m_new) : 1.f;
+            l[g] *= alpha;
 #pragma unroll
-            for (int g = 0; g < 2; ++g) {
-                const float m_new = fmaxf(m[g], mt[g]), alpha = m[g] > ROWS_NEG_INF ? rows_exp2(m[g] - m_new) : 1.f;
-                l[g] *= alpha;
-#pragma unroll
-                for (int b = 0; b < 4; ++b) O[g][b] *= alpha;
-                m[g] = m_new;
-            }
+            for (int b = 0; b < 4; ++b) O[g][b] *= alpha;
+            m[g] = m_new;
         }
     }
     // half x of channels 32 b + lane % 32 of the tile's tokens 16 t + (4 h ..+3, 8 + 4 h ..+3); va: this lane's places of blocks 0 and 1
@@ -330,7 +328,7 @@ struct WideRows {
         for (int g = 0; g < 2; ++g) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[g][i] = sight[g].of(j0 + 8 * (i >> 2) + 4 * h + (i & 3)) ? s[g][i] : ROWS_NEG_INF;
-            top[g] = most(s[g]);
+            top[g] = row_most(most(s[g]));
         }
     }
     // Scores belong into the other half of the register file, where the vector instructions are that they are for; the compiler would have them beside the accumulators and
@@ -343,11 +341,13 @@ struct WideRows {
     // One tile (Values at vt): scores s of it, whose largest are `top`, into O; the scores of the next tile (Keys k) into `next`, its largest into `top`; the Keys of
     // the one behind it (at kt) into k.
     // A wave has its SIMD for itself, so what runs beside the matrix instructions is what stands between them: 32 of 32 cycles, of which the first 24 have beside them
-    // the weights, 16 pairs of 52 cycles (the exponentials 16 each), two in three instructions' time, and the last eight the maxima; LDS is read one piece a step.
+    // the weights, 16 pairs of 52 cycles (the exponentials 16 each), two in three instructions' time, and the last eight the maxima and beside(0..7), a load of
+    // a later stage each; LDS is read one piece a step.
+    template <typename F>
     __device__ __forceinline__ void tile(f32x16 (&s)[2], f32x16 (&next)[2], float (&top)[2], bf16x8 (&k)[8], const char* lds, const int (&ka)[4], int kt,
-                                         const int (&va)[2], int vt)
+                                         const int (&va)[2], int vt, F beside)
     {
-        follow(top);
+        if (behind(top)) follow(top);
         hold();
         const float ref[2] = {m[0] > ROWS_NEG_INF ? m[0] : 0.f, m[1] > ROWS_NEG_INF ? m[1] : 0.f};
         float sum[2][2] = {{0.f, 0.f}, {0.f, 0.f}};
@@ -383,8 +383,9 @@ struct WideRows {
             if (x < 24 && x % 3 < 2) weigh(2 * (x / 3) + x % 3);
             if (x < 25 && x % 3 == 1) pack(2 * (x / 3));
             if (x < 25 && x % 3 == 2) pack(2 * (x / 3) + 1);
-            if (x == 26) top[0] = most(next[0]);
-            if (x == 28) top[1] = most(next[1]);
+            if (x == 26 || x == 28) top[x / 2 - 13] = most(next[x / 2 - 13]);
+            if (x == 29 || x == 30) top[x - 29] = row_most(top[x - 29]);
+            if (x >= 24) beside(x - 24);
             __builtin_amdgcn_sched_barrier(0);
         }
 #pragma unroll
@@ -426,16 +427,30 @@ __global__ __launch_bounds__(256, 1) void attn_prompt_wide(PrefillArgs A)
     const bf16_t* vp = (const bf16_t*)A.v + (int64_t)P.b * A.sb + (int64_t)P.hk * A.sh;
     int* odd = (int*)(lds + WIDE_LDS);
     if (P.i0 < P.i1) {
-        // rows 16 wave + 4 i + lane / 16 of a stage, i < 4: their 16-byte pieces, in the order that slot_of() undoes
+        // Rows 16 wave + 4 x + lane / 16 of a stage, x < 4: their 16-byte pieces, in the order that slot_of() undoes.  A lane's places in a stage are the same in all of
+        // them; in one that reaches behind the last row they repeat it.
         const uint32_t base = __builtin_amdgcn_readfirstlane(lds_address(lds)) + 16 * WIDE_ROW * wave;
-        auto fetch = [&](int i, int buf) {
-            const int j = P.start(i) + 16 * wave + (lane >> 4);
+        const int64_t apart = vp - kp;
+        int64_t place[4];
+        auto places = [&](int last) {
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                const int64_t at = (int64_t)min(j + 4 * x, P.len - 1) * A.st + 8 * slot_of(4 * x + (lane >> 4), lane & 15);
-                load_to_lds(kp + at, base + buf + 4 * WIDE_ROW * x);
-                load_to_lds(vp + at, base + buf + WIDE_VALUES + 4 * WIDE_ROW * x);
-            }
+            for (int x = 0; x < 4; ++x) place[x] = (int64_t)min(16 * wave + 4 * x + (lane >> 4), last) * A.st + 8 * slot_of(4 * x + (lane >> 4), lane & 15);
+        };
+        places(WIDE_TOKENS);
+        const bf16_t* from = kp;         // the stage that is asked for
+        auto aim = [&](int i) {
+            const int j = P.start(i);
+            from = kp + (int64_t)j * A.st;
+            if (j + WIDE_TOKENS > P.len) places(P.len - 1 - j);
+        };
+        auto load = [&](int piece, int buf) {
+            const int x = piece >> 1, v = piece & 1;
+            load_to_lds((v ? from + apart : from) + place[x], base + buf + v * WIDE_VALUES + 4 * WIDE_ROW * x);
+        };
+        auto fetch = [&](int i, int buf) {
+            aim(i);
+#pragma unroll
+            for (int x = 0; x < 8; ++x) load(x, buf);
         };
 #pragma unroll
         for (int i = 0; i < 3; ++i) fetch(min(P.i0 + i, P.i1 - 1), i * WIDE_STAGE);
@@ -463,7 +478,7 @@ __global__ __launch_bounds__(256, 1) void attn_prompt_wide(PrefillArgs A)
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
             asm volatile("" : "+v"(s0[g]));
-            top[g] = WideRows::most(s0[g]);
+            top[g] = W.row_most(WideRows::most(s0[g]));
         }
         int now = 0;
 #pragma unroll 1
@@ -473,15 +488,16 @@ __global__ __launch_bounds__(256, 1) void attn_prompt_wide(PrefillArgs A)
             // The next stage's loads are all but the last eight.  Behind the barrier it is there for all waves, and nobody reads the one before this any more.
             stage_wait<8>();
             lds_barrier();
-            fetch(min(i + 3, P.i1 - 1), (now + 3 * WIDE_STAGE) & (4 * WIDE_STAGE - 1));
+            aim(min(i + 3, P.i1 - 1));
+            const int later = (now + 3 * WIDE_STAGE) & (4 * WIDE_STAGE - 1);
             if (i + 1 < P.i1 && P.edge(P.start(i + 1))) {
                 clean_values<bf16_t>(lds + next + WIDE_VALUES, WIDE_VALUES, odd, tid);
                 lds_barrier();
             }
             if (!P.inside(j0, 32, w_lo, w_hi)) W.hide(s0, top, j0, h);
-            W.tile(s0, s1, top, k, lds, ka, next, va, now + WIDE_VALUES);
+            W.tile(s0, s1, top, k, lds, ka, next, va, now + WIDE_VALUES, [&](int x) { load(x, later); });
             if (!P.inside(j0 + 32, 32, w_lo, w_hi)) W.hide(s1, top, j0 + 32, h);
-            W.tile(s1, s0, top, k, lds, ka, next + 32 * WIDE_ROW, va, now + WIDE_VALUES + 32 * WIDE_ROW);
+            W.tile(s1, s0, top, k, lds, ka, next + 32 * WIDE_ROW, va, now + WIDE_VALUES + 32 * WIDE_ROW, [](int) {});
             now = next;
         }
         stage_wait<0>();             // (what was asked for twice, at the end)
