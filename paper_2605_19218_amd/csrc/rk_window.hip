@@ -24,8 +24,21 @@ __device__ __forceinline__ bool odd_value(uint32_t bits) { return (bits & 0x7f80
 
 // What a row sees.
 struct Sight {
-    int p, window, sinks;        // window: 2^30 or more when there is none
+    int p, window, sinks;        // window: 2^30 when there is none
     __device__ __forceinline__ bool of(int j) const { return j <= p && (j < sinks || p - j < window); }
+    static __device__ __forceinline__ uint32_t below(int x) { return x >= 32 ? ~0u : (1u << max(x, 0)) - 1; }
+    // a bit for each of rows j ..+31 (a p in front of row 0 sees none, whatever the second difference wraps to)
+    __device__ __forceinline__ uint32_t bits(int j) const { return below(p - j + 1) & (~below((int)((uint32_t)p - (uint32_t)window - (uint32_t)j + 1u)) | below(sinks - j)); }
+    // scores of a lane's tokens j + 8 (i / 4) + i % 4: minus infinity where they are not seen
+    __device__ __forceinline__ void hide(f32x16& s, int j) const
+    {
+        const uint32_t seen = bits(j);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const uint32_t all = (uint32_t)((int32_t)(seen << (31 - 8 * (i >> 2) - (i & 3))) >> 31);
+            s[i] = __uint_as_float((__float_as_uint(s[i]) & all) | (0xff800000u & ~all));
+        }
+    }
 };
 
 // Which rows and splits a work-group takes: the last blocks of all KV heads first, which see most, so that the short ones fill the gaps at the end; a head's
@@ -64,7 +77,7 @@ struct Prompt {
         first = len - fresh;
         rows = fresh * A.G;
         row0 = block * size;
-        window = A.window > 0 ? A.window : 0x7fffffff;
+        window = A.window > 0 ? min(A.window, 1 << 30) : 1 << 30;
         sinks = A.sinks;
         if (row0 >= rows) return;
         p_lo = first + token(A, row0);
@@ -184,10 +197,7 @@ __global__ __launch_bounds__(256, 2) void attn_prompt_f32(PrefillArgs A)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], q[x][e], s, 0, 0, 0);
             }
-            if (!P.inside(j0, F32_TOKENS, w_lo, w_hi)) {
-#pragma unroll
-                for (int e = 0; e < 16; ++e) s[e] = sight.of(j0 + 8 * (e >> 2) + 4 * h + (e & 3)) ? s[e] : ROWS_NEG_INF;
-            }
+            if (!P.inside(j0, F32_TOKENS, w_lo, w_hi)) sight.hide(s, j0 + 4 * h);
             float mt = s[0];
 #pragma unroll
             for (int e = 1; e < 16; ++e) mt = fmaxf(mt, s[e]);
@@ -306,6 +316,7 @@ struct WideRows {
     // the running maxima move to a tile's
     __device__ __forceinline__ void follow(const float (&top)[2])
     {
+        hold();                  // (or they would be copied in front of the branch, for every tile)
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
             const float m_new = fmaxf(m[g], top[g]), alpha = m[g] > ROWS_NEG_INF ? rows_exp2(m[g] - m_new) : 1.f;
@@ -326,8 +337,7 @@ struct WideRows {
     {
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) s[g][i] = sight[g].of(j0 + 8 * (i >> 2) + 4 * h + (i & 3)) ? s[g][i] : ROWS_NEG_INF;
+            sight[g].hide(s[g], j0 + 4 * h);
             top[g] = row_most(most(s[g]));
         }
     }
@@ -480,6 +490,10 @@ __global__ __launch_bounds__(256, 1) void attn_prompt_wide(PrefillArgs A)
             asm volatile("" : "+v"(s0[g]));
             top[g] = W.row_most(WideRows::most(s0[g]));
         }
+        // the first tile's maxima are the running ones, with nothing to scale
+        if (!P.inside(P.start(P.i0), 32, w_lo, w_hi)) W.hide(s0, top, P.start(P.i0), h);
+#pragma unroll
+        for (int g = 0; g < 2; ++g) W.m[g] = top[g];
         int now = 0;
 #pragma unroll 1
         for (int i = P.i0; i < P.i1; ++i) {
