@@ -418,21 +418,51 @@ RowsPlan window_plan(const rk_ctx* ctx, const rk_layout* L, bool cache, int text
     return p;
 }
 
-// Prompts: splits of what a row block sees, where its blocks leave compute units idle (two work-groups a compute unit), of at least 4 tiles.
+// Prompts: rows of a block, blocks of a KV head, splits of what a block sees, whichever come out cheapest, in microseconds as measured: a work-group takes `each` for
+// its beginning and end and `step` for four tiles of few rows, for a stage of 64 tokens of many, or for an fp32 tile; work-groups run one a compute unit (fp32: two, half as
+// fast each); partials are written and read.  bf16, us with 32 / 256 rows a block: 8 units of 4 heads, 1 token on 1000 9.4 / 13.1, 40 on 4000 19.1 / 25.8, the same with a
+// window of 512 12.3 / 20.3, 300 12.4 / 25.0, 700 27.7 / 34.0, 1000 41.8 / 38.8, 500 on 8000 176 / 85, 1500 on 2000 with a window of 512 70 / 35; 32 units of 7
+// heads, 20 on 500 12.0 / 23.1, 100 17.7 / 15.7, 40 on 4000 with a window of 512 23.6 / 29.5, 1000 280 / 96; 512 units of 4 heads, 4 on 500 28.8 / 45.2, 20 on 500
+// 84.7 / 54.5.
 constexpr int PREFILL_SPLITS_MAX = 32;
-int prefill_splits(const rk_ctx* ctx, const rk_layout* L, int n, int rows_seen)
+struct PrefillPlan { int rows, blocks, S; };
+PrefillPlan prefill_plan(const rk_ctx* ctx, const rk_layout* L, int n, int max_len, int window, int sinks)
 {
-    const int64_t G = L->n_q_heads / L->n_kv_heads, per = prefill_block_rows(L->dtype), blocks = ((int64_t)n * G + per - 1) / per;
-    int64_t s = 2 * (int64_t)(ctx ? ctx->n_cu : 256) / (blocks * L->batch * L->n_kv_heads);
-    const int64_t most = ((int64_t)rows_seen + 127) / 128;
-    if (s > most) s = most;
-    if (s > PREFILL_SPLITS_MAX) s = PREFILL_SPLITS_MAX;
-    return s < 1 ? 1 : (int)s;
+    const int64_t units = (int64_t)L->batch * L->n_kv_heads, G = L->n_q_heads / L->n_kv_heads, n_cu = ctx ? ctx->n_cu : 256;
+    PrefillPlan best{};
+    double least = 1e300;
+    auto look = [&](int rows, int tokens, double each, double step) {
+        const int64_t blocks = ((int64_t)n * G + rows - 1) / rows;
+        // tokens that a block sees: with a window all blocks about as many, else half of the new ones on average
+        int64_t seen = (int64_t)max_len - n / 2;
+        if (window > 0 && (int64_t)window + sinks + rows / G + 1 < seen) seen = (int64_t)window + sinks + rows / G + 1;
+        const int64_t steps = seen > tokens ? (seen + tokens - 1) / tokens : 1;
+        for (int S = 1; S <= PREFILL_SPLITS_MAX && S <= steps; ++S) {
+            const int64_t groups = units * blocks * S;
+            // (the workspace holds 256 rows for each compute unit)
+            if (S > 1 && groups * rows > 256 * n_cu) break;
+            const double merge = S == 1 ? 0.0 : 2.5 + (double)units * n * G * S * 1040 / 4e6;
+            // (a last round that is not full costs as much as a full one, unless its work-groups are the short ones, which run last)
+            const double full = (double)((groups + n_cu - 1) / n_cu), rounds = groups <= n_cu || rows == 256 ? full : 0.5 * (full + (double)groups / n_cu);
+            const double cost = rounds * (each + step * ((steps + S - 1) / S)) + merge;
+            if (cost < least - 0.01) {
+                least = cost;
+                best = PrefillPlan{rows, (int)blocks, S};
+            }
+        }
+    };
+    if (L->dtype == RK_F32) {
+        look(128, 32, 6.0, 3.6);
+    } else {
+        look(256, 64, 13.0, 2.2);
+        look(32, 128, 9.0, 1.35);
+    }
+    return best;
 }
-// rows * splits of n tokens or fewer: at most PREFILL_SPLITS_MAX a row, and a block's rows for two work-groups a compute unit
+// rows * splits of n tokens or fewer: at most PREFILL_SPLITS_MAX a row, and a block's rows for each work-group of a full device
 size_t prefill_ws(const rk_ctx* ctx, const rk_layout* L, int n)
 {
-    const size_t rows = (size_t)L->batch * L->n_q_heads * n, most = (size_t)prefill_block_rows(L->dtype) * 2 * (ctx ? ctx->n_cu : 256);
+    const size_t rows = (size_t)L->batch * L->n_q_heads * n, most = (size_t)256 * (ctx ? ctx->n_cu : 256);
     const size_t slots = rows < most / PREFILL_SPLITS_MAX ? rows * PREFILL_SPLITS_MAX : most;
     return align_up(slots * (D + 2) * sizeof(float), 256) + 256;
 }
@@ -1388,10 +1418,8 @@ rk_status rk_prefill_attn_window(rk_ctx* ctx, const rk_layout* L, const rk_heads
     a.len = text->len; a.max_len = text->max_len; a.n_dev = n_tokens_dev; a.n = n_tokens;
     a.B = L->batch; a.Hq = L->n_q_heads; a.Hkv = L->n_kv_heads; a.G = a.Hq / a.Hkv;
     a.window = window; a.sinks = sinks;
-    const int64_t per = prefill_block_rows(L->dtype);
-    a.blocks = (int)(((int64_t)n_tokens * a.G + per - 1) / per);
-    const int64_t seen = (int64_t)window + sinks + per / a.G + 1;       // by a block of rows
-    a.S = prefill_splits(ctx, L, n_tokens, window > 0 && seen < text->max_len ? (int)seen : text->max_len);
+    const PrefillPlan p = prefill_plan(ctx, L, n_tokens, text->max_len, window, sinks);
+    a.rows = p.rows; a.blocks = p.blocks; a.S = p.S;
     const float sc = scale > 0.f ? scale : 1.0f / sqrtf((float)L->head_dim);
     a.scale_log2 = sc * 1.44269504088896340736f;
     const size_t slots = (size_t)a.B * a.Hq * n_tokens * a.S;

@@ -188,16 +188,20 @@ __global__ __launch_bounds__(256, 2) void attn_prompt_f32(PrefillArgs A)
                 clean_values<float>(lds + now + F32_VALUES, F32_VALUES, odd, tid);
                 lds_barrier();
             }
+            now ^= F32_STAGE;
+            if (j0 > w_hi) continue;     // (behind all of this wave's rows)
+            const char* at = lds + (now ^ F32_STAGE);
             f32x16 s;
 #pragma unroll
             for (int e = 0; e < 16; ++e) s[e] = 0.f;
 #pragma unroll
             for (int x = 0; x < 16; ++x) {
-                const f32x4 a = *(const f32x4*)(lds + now + ka[x & 3] + 128 * (x >> 2));
+                const f32x4 a = *(const f32x4*)(at + ka[x & 3] + 128 * (x >> 2));
 #pragma unroll
                 for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], q[x][e], s, 0, 0, 0);
             }
             if (!P.inside(j0, F32_TOKENS, w_lo, w_hi)) sight.hide(s, j0 + 4 * h);
+            __builtin_amdgcn_s_setprio(1);       // (the other wave of the SIMD has its products; 601 us without, 593 with)
             float mt = s[0];
 #pragma unroll
             for (int e = 1; e < 16; ++e) mt = fmaxf(mt, s[e]);
@@ -217,13 +221,13 @@ __global__ __launch_bounds__(256, 2) void attn_prompt_f32(PrefillArgs A)
                 sum += s[e];
             }
             l += sum;
+            __builtin_amdgcn_s_setprio(0);
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-                const f32x4 a = *(const f32x4*)(lds + now + va[e & 3] + 8 * F32_ROW * (e >> 2));
+                const f32x4 a = *(const f32x4*)(at + va[e & 3] + 8 * F32_ROW * (e >> 2));
 #pragma unroll
                 for (int c = 0; c < 4; ++c) O[c] = __builtin_amdgcn_mfma_f32_32x32x2f32(a[c], s[e], O[c], 0, 0, 0);
             }
-            now ^= F32_STAGE;
         }
         stage_wait<0>();
         // The Values that were left out join the rows that see them: a sum of one is it, or NaN.  (O[c][i] is channel 4 (8 (i / 4) + 4 h + i % 4) + c)
@@ -569,6 +573,191 @@ __global__ __launch_bounds__(256, 1) void attn_prompt_wide(PrefillArgs A)
     }
 }
 
+// ---- bf16, few rows ------------------------------------------------------------------
+// 32 rows a work-group, whose four waves take a tile of 32 tokens each in turn: what a short prompt waits for is its chain of round trips, so nothing in it is
+// waited for by four waves, every wave has its next tile on the way into its own part of LDS, and the waves meet once, to join their sums.
+constexpr int FEW_ROWS = 32, FEW_TOKENS = 32, FEW_TILE = 2 * FEW_TOKENS * 256, FEW_WAVE = 2 * FEW_TILE, FEW_LDS = 4 * FEW_WAVE;
+constexpr int FEW_PARK = 33;     // 32 rows' quads, and one: lanes that write quads side by side meet other banks
+
+__global__ __launch_bounds__(256, 1) void attn_prompt_few(PrefillArgs A)
+{
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    __shared__ float sm_m[4][32], sm_l[4][32];
+    int block, split, u;
+    prompt_place(A, block, split, u);
+    const Prompt<FEW_TOKENS> P(A, u, block, split, FEW_ROWS);
+    if (P.row0 >= P.rows) return;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, n = lane & 31;
+    const int mine = min(P.row0 + n, P.rows - 1), tok = P.token(A, mine), head = P.hk * A.G + mine - tok * A.G;
+    const Sight sight{P.first + tok, P.window, P.sinks};
+    const bf16_t* kp = (const bf16_t*)A.k + (int64_t)P.b * A.sb + (int64_t)P.hk * A.sh;
+    const bf16_t* vp = (const bf16_t*)A.v + (int64_t)P.b * A.sb + (int64_t)P.hk * A.sh;
+
+    bf16x8 q[8];
+    const bf16_t* qp = (const bf16_t*)A.q + (int64_t)P.b * A.q_sb + (int64_t)head * A.q_sh + (int64_t)tok * A.q_st;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) q[i] = *(const bf16x8*)(qp + 16 * i + 8 * h);
+
+    char* own = lds + wave * FEW_WAVE;
+    const uint32_t base = __builtin_amdgcn_readfirstlane(lds_address(own));
+    // rows 4 x + lane / 16 of a tile, x < 8
+    auto fetch = [&](int i, int buf) {
+        const int j = P.start(i);
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+            const int64_t at = (int64_t)min(j + 4 * x + (lane >> 4), P.len - 1) * A.st + 8 * slot_of(4 * x + (lane >> 4), lane & 15);
+            load_to_lds(kp + at, base + buf + 1024 * x);
+            load_to_lds(vp + at, base + buf + FEW_TILE / 2 + 1024 * x);
+        }
+    };
+    int ka[4], va[2];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) ka[i] = n * 256 + 16 * slot_of(n, 2 * i + h);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int r = 4 * h + ((lane & 15) >> 2);
+        va[i] = FEW_TILE / 2 + r * 256 + 16 * slot_of(r, 4 * i + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) + 8 * (lane & 1);
+    }
+    float m = ROWS_NEG_INF, l = 0.f;
+    f32x16 O[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) O[c][i] = 0.f;
+    bool odd = false;
+    int now = 0;
+    if (P.i0 + wave < P.i1) fetch(P.i0 + wave, 0);
+#pragma unroll 1
+    for (int i = P.i0 + wave; i < P.i1; i += 4) {
+        asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");     // (nothing reads the other tile's place any more)
+        if (i + 4 < P.i1) {
+            fetch(i + 4, now ^ FEW_TILE);
+            stage_wait<16>();
+        } else {
+            stage_wait<0>();
+        }
+        const int j0 = P.start(i);
+        const char* at = own + now;
+        f32x16 s;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[e] = 0.f;
+#pragma unroll
+        for (int x = 0; x < 8; ++x) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8*)(at + ka[x & 3] + 128 * (x >> 2)), q[x], s, 0, 0, 0);
+        const bool edge = P.edge(j0);
+        if (edge) sight.hide(s, j0 + 4 * h);
+        float mt = s[0];
+#pragma unroll
+        for (int e = 1; e < 16; ++e) mt = fmaxf(mt, s[e]);
+        mt = halves_max(mt) * A.scale_log2;
+        if (__any(mt > m + 8.f)) {
+            const float m_new = fmaxf(m, mt), alpha = m > ROWS_NEG_INF ? rows_exp2(m - m_new) : 1.f;
+            l *= alpha;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) O[c] *= alpha;
+            m = m_new;
+        }
+        const float ref = m > ROWS_NEG_INF ? m : 0.f;
+        float sum = 0.f;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            s[e] = rows_exp2(fmaf(s[e], A.scale_log2, -ref));
+            sum += s[e];
+        }
+        l += sum;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            uint32_t w[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] = __builtin_bit_cast(uint32_t, (bf16x2){(__bf16)s[8 * t + 2 * e], (__bf16)s[8 * t + 2 * e + 1]});
+            const bf16x8 p = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                uint32_t a[4];
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    typedef __attribute__((address_space(3))) s16x4* Lds;
+                    const uint2 d = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(at + va[c & 1] + (16 * t + 8 * x) * 256 + 128 * (c >> 1))));
+                    a[2 * x] = d.x;
+                    a[2 * x + 1] = d.y;
+                }
+                if (edge) {                  // Values that are no numbers count as 0 where they may be masked
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const uint32_t keep = (odd_value(a[e]) ? 0u : 0xffff0000u) | (odd_value(a[e] << 16) ? 0u : 0xffffu);
+                        odd |= keep != ~0u;
+                        a[e] &= keep;
+                    }
+                }
+                O[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, make_uint4(a[0], a[1], a[2], a[3])), p, O[c], 0, 0, 0);
+            }
+        }
+        now ^= FEW_TILE;
+    }
+    // ... and join the rows that see them behind the loop: a sum of one is it, or NaN.
+    if (__any(odd)) {
+#pragma unroll 1
+        for (int i = P.i0 + wave; i < P.i1; i += 4) {
+            const int j0 = P.start(i);
+            if (!P.edge(j0)) continue;
+#pragma unroll 1
+            for (int j = j0; j < min(j0 + FEW_TOKENS, P.len); ++j)
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const uint2 d = *(const uint2*)(vp + (int64_t)j * A.st + 32 * c + 8 * e + 4 * h);
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) {
+                            const uint32_t w = x < 2 ? d.x : d.y, v = x & 1 ? w & 0xffff0000u : w << 16;
+                            O[c][4 * e + x] += odd_value(v) && sight.of(j) ? __uint_as_float(v) : 0.f;
+                        }
+                    }
+        }
+    }
+
+    // the four waves' sums: quads of channels, [wave][channels 4 p ..+3][row]
+    l = halves_sum(l);
+    __syncthreads();
+    f32x4* park = (f32x4*)lds;
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            park[(wave * 32 + 8 * c + 2 * e + h) * FEW_PARK + n] = (f32x4){O[c][4 * e], O[c][4 * e + 1], O[c][4 * e + 2], O[c][4 * e + 3]};
+    if (h == 0) {
+        sm_m[wave][n] = m;
+        sm_l[wave][n] = l;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int r = 8 * k + (tid >> 5), p = tid & 31, row = P.row0 + r;
+        if (row >= P.rows) continue;
+        const float M = fmaxf(fmaxf(sm_m[0][r], sm_m[1][r]), fmaxf(sm_m[2][r], sm_m[3][r]));
+        f32x4 acc = (f32x4){0.f, 0.f, 0.f, 0.f};
+        float sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float x = partial_weight(sm_m[w][r], sm_l[w][r], M);
+            acc += park[(w * 32 + p) * FEW_PARK + r] * x;
+            sum = fmaf(sm_l[w][r], x, sum);
+        }
+        if (A.S == 1) {
+            const int t = P.token(A, row), hd = P.hk * A.G + row - t * A.G;
+            const float inv = sum == 0.f ? 0.f : 1.f / sum;
+            float x[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = sum == 0.f ? 0.f : acc[e] * inv;
+            *(uint2*)((bf16_t*)A.out + (int64_t)P.b * A.o_sb + (int64_t)hd * A.o_sh + (int64_t)t * A.o_st + 4 * p) =
+                make_uint2(__builtin_bit_cast(uint32_t, (bf16x2){(__bf16)x[0], (__bf16)x[1]}), __builtin_bit_cast(uint32_t, (bf16x2){(__bf16)x[2], (__bf16)x[3]}));
+        } else {
+            const size_t slot = ((size_t)u * A.n * A.G + row) * A.S + split;
+            *(f32x4*)(A.ws_acc + slot * D + 4 * p) = acc;
+            if (p == 0) { A.ws_m[slot] = M; A.ws_l[slot] = sum; }
+        }
+    }
+}
+
 // The fold of the splits' partials: 32 lanes a row, four channels each (see rows_merge).
 template <typename T>
 __global__ __launch_bounds__(256) void prompt_merge(PrefillArgs A)
@@ -591,23 +780,24 @@ __global__ __launch_bounds__(256) void prompt_merge(PrefillArgs A)
 
 }  // namespace
 
-int prefill_block_rows(int dtype) { return dtype == 0 ? F32_ROWS : WIDE_ROWS; }
-
 hipError_t launch_prefill(int dtype, const PrefillArgs& a, hipStream_t st)
 {
     const int64_t units = (int64_t)a.B * a.Hkv, groups = units * a.blocks * a.S;
     if (groups > 0x7fffffff || (units * a.n * a.G + 7) / 8 > 0x7fffffff) return hipErrorInvalidValue;
-    const void* kernel = dtype == 0 ? (const void*)attn_prompt_f32 : (const void*)attn_prompt_wide;
-    const int lds = (dtype == 0 ? 2 * F32_STAGE : WIDE_LDS) + 16;
-    const hipError_t e = allow_dynamic_lds(kernel, lds);
-    if (e != hipSuccess) return e;
-    if (dtype == 0) attn_prompt_f32<<<(uint32_t)groups, 256, lds, st>>>(a);
-    else attn_prompt_wide<<<(uint32_t)groups, 256, lds, st>>>(a);
-    if (a.S > 1) {
-        const uint32_t g = (uint32_t)((units * a.n * a.G + 7) / 8);
-        if (dtype == 0) prompt_merge<float><<<g, 256, 0, st>>>(a);
-        else prompt_merge<bf16_t><<<g, 256, 0, st>>>(a);
-    }
+    auto go = [&](void (*kernel)(PrefillArgs), int lds) {
+        const hipError_t e = allow_dynamic_lds((const void*)kernel, lds);
+        if (e != hipSuccess) return e;
+        kernel<<<(uint32_t)groups, 256, lds, st>>>(a);
+        return hipGetLastError();
+    };
+    hipError_t e;
+    if (dtype == 0) e = go(attn_prompt_f32, 2 * F32_STAGE + 16);
+    else if (a.rows == FEW_ROWS) e = go(attn_prompt_few, FEW_LDS);
+    else e = go(attn_prompt_wide, WIDE_LDS + 16);
+    if (e != hipSuccess || a.S == 1) return e;
+    const uint32_t g = (uint32_t)((units * a.n * a.G + 7) / 8);
+    if (dtype == 0) prompt_merge<float><<<g, 256, 0, st>>>(a);
+    else prompt_merge<bf16_t><<<g, 256, 0, st>>>(a);
     return hipGetLastError();
 }
 
