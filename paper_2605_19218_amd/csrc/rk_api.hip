@@ -402,19 +402,34 @@ int window_rows(int max_len, int window, int sinks)
     const int64_t most = (int64_t)window + sinks;
     return most < max_len ? (int)most : max_len;
 }
-// One token with a window on the text.  Without a cache: a split for each 128 rows it sees (a tile for each wave), one work-group a compute unit.
+// One token with a window on the text.  A split of text takes 128 rows (a tile for each wave) where that many work-groups run beside the cache's, whose splits are then
+// those it would have alone; else the plan of drafts shares the device out, and compute units that it leaves idle take splits of text more.  us: bf16, 8 units x 2000 + 500 of text 3 + 4
+// splits (the plan of drafts) 10.4, 8 + 4 8.8, 12 + 4 8.7; fp32 32 x 2880 + 272 6 + 1 25.3, 6 + 2 24.1, 6 + 4 24.0; text alone, 8 units x 1028 8 9.3, 9 8.2, 16 8.0, 24 8.6; 1 x
+// 8000 16 12.7, 32 10.1, 63 9.9; fp32 32 x 900 4 14.8, 8 12.1, 16 17.1; 256 x 4100 1 93.7, 2 96.8.
 RowsPlan window_plan(const rk_ctx* ctx, const rk_layout* L, bool cache, int text_rows, bool q8)
 {
-    if (cache) return rows_plan(ctx, L, 1, text_rows, false, q8, 16);
-    const int64_t units = (int64_t)L->batch * L->n_kv_heads, n_cu = ctx ? ctx->n_cu : 256;
+    const int64_t n_cu = ctx ? ctx->n_cu : 256, groups = (int64_t)L->batch * L->n_kv_heads * ((L->n_q_heads / L->n_kv_heads + 15) / 16);
+    const int64_t wanted = text_rows < 1 ? 1 : ((int64_t)text_rows + 127) / 128, slots = rows_slots(ctx, L, 1);
+    auto least = [](int64_t a, int64_t b) { return (int)(a < b ? a : b); };
     RowsPlan p;
-    p.per = 16;
-    p.nrb = (L->n_q_heads / L->n_kv_heads + 15) / 16;
-    int64_t s = n_cu / (units * p.nrb), most = ((int64_t)text_rows + 127) / 128;
-    if (s > most) s = most;
-    if (s > rows_slots(ctx, L, 1)) s = rows_slots(ctx, L, 1);
-    p.Sv = 0;
-    p.Sr = s < 1 ? 1 : (int)s;
+    if (!cache) {
+        p.per = 16;
+        p.nrb = (L->n_q_heads / L->n_kv_heads + 15) / 16;
+        p.Sv = 0;
+        p.Sr = least(least(n_cu / groups, wanted), slots);
+        if (p.Sr < 1) p.Sr = 1;
+        return p;
+    }
+    // (an fp32 cache leaves room for one work-group a compute unit, the others for two)
+    const bool fixed = ctx && ctx->decode_splits > 0;
+    p = rows_plan(ctx, L, 1, 0, false, q8, 16);
+    if (!fixed && text_rows > 0 && groups * (p.Sv + wanted) <= (L->dtype == RK_F32 && !q8 ? n_cu : 2 * n_cu) && p.Sv + wanted <= slots) {
+        p.Sr = (int)wanted;
+        return p;
+    }
+    p = rows_plan(ctx, L, 1, text_rows, false, q8, 16);
+    const int more = least(least(n_cu / groups, slots) - p.Sv, wanted);
+    if (!fixed && text_rows > 0 && p.Sr < more) p.Sr = more;
     return p;
 }
 

@@ -5,7 +5,7 @@
 // The angle is needed modulo a turn, and a far position times a frequency in fp32 has lost those bits (a position of 10^6 would be off by 0.06 radians): the
 // product and its division by 2 pi are fp64, and what is left of a turn, within half of one, is fp32 again, where sincospi takes it.  Pairs, products and
 // sums are fp32, rounded once.
-// Eight lanes take a row, eight pairs each, in 16-byte pieces: channels 8 o ..+7 and n_pairs + 8 o ..+7 (or 16 o ..+15 for neighbours), so that a pair's two channels
+// Eight lanes take a row, eight pairs each, in pieces of eight channels: 8 o ..+7 and n_pairs + 8 o ..+7 (or 16 o ..+15 for neighbours), so that a pair's two channels
 // are in one lane.  Its sines and cosines are the same in all heads of a token, so a wave takes eight tokens through several heads with them in registers; with fewer than eight
 // tokens it takes one through eight heads.
 #include <type_traits>
@@ -14,6 +14,8 @@
 namespace rk {
 
 namespace {
+
+constexpr int ROPE_TOKENS = 8;       // of a work-group
 
 // Eight channels of a row, in memory and as fp32.
 template <typename T> struct Piece;
@@ -54,16 +56,16 @@ template <> struct Piece<float> {
     }
 };
 
-// VEC: n_pairs is a multiple of 8, so that pieces are aligned and a lane's pairs are all there or none; else element by element.
-// ONE: a wave's eight rows are heads of one token, else eight tokens of a head, and `heads_per` heads follow each other.
-template <typename T, bool VEC, bool ONE>
-__global__ __launch_bounds__(ONE ? 1024 : 256) void rope_rows(RopeArgs A, int heads_per, int32_t* __restrict__ tickets, int apart)
+// VEC: n_pairs is a multiple of 8, so that a lane's pairs are all there or none, in two aligned pieces; else a lane has one piece (sixteen lanes a row) and reads the
+// other channels of its pairs one by one, where they are in other pieces.
+// A work-group takes TOKENS tokens (one, where there are fewer) through 1 << log_heads heads, a token's heads one after another, which is how a projection leaves them.
+template <typename T, bool VEC, int TOKENS>
+__global__ __launch_bounds__(TOKENS == 1 ? 1024 : 256) void rope_rows(RopeArgs A, int log_heads, int32_t* __restrict__ tickets, int apart)
 {
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, o = lane & 7, slot = lane >> 3, b = blockIdx.z;
+    constexpr int LANES = VEC ? 8 : 16;
+    __shared__ __attribute__((aligned(16))) float cosines[TOKENS][64], sines[TOKENS][64];
+    const int tid = threadIdx.x, o = tid % LANES, b = blockIdx.z, t0 = blockIdx.x * TOKENS, h0 = blockIdx.y << log_heads;
     const int nq = A.q ? A.Hq : 0, nk = A.k ? A.Hkv : 0, heads = nq + nk + (A.v ? A.Hkv : 0);
-    const int t = ONE ? blockIdx.x : (blockIdx.x * 4 + wave) * 8 + slot;
-    const int h0 = ONE ? (blockIdx.y * (blockDim.x >> 6) + wave) * 8 + slot : blockIdx.y * heads_per;
-    const int h1 = min(heads, ONE ? h0 + 1 : h0 + heads_per);
     const bool adj = A.pairing != 0;
     const int np = A.n_pairs;
 
@@ -71,48 +73,43 @@ __global__ __launch_bounds__(ONE ? 1024 : 256) void rope_rows(RopeArgs A, int he
     const int len = A.len ? A.len[b] : 0;
     const int fit = A.len ? (len < 0 ? 0 : min(n, max(A.cap - len, 0))) : n;      // rows of Keys and Values that are written
 
-    if (t < n && h0 < h1) {
-        float c[8], s[8];
-        int p[RK_AXES];
-#pragma unroll
-        for (int a = 0; a < RK_AXES; ++a) p[a] = a < A.n_axes ? A.pos[a * A.pos_sa + (int64_t)b * A.pos_sb + t] : 0;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int i = 8 * o + e;
-            const uint64_t word = o < 4 ? A.axes[0] : A.axes[1];
-            const int a = (int)(word >> (2 * (i & 31))) & 3;
-            const int at = a < 2 ? (a == 0 ? p[0] : p[1]) : (a == 2 ? p[2] : p[3]);
-            const double turns = (double)at * (double)(i < np ? A.inv_freq[i] : 0.f) * 0.15915494309189533577;
-            sincospif(2.f * (float)(turns - rint(turns)), &s[e], &c[e]);
-            s[e] = A.inverse ? -s[e] : s[e];
+    if (t0 < n) {
+        for (int x = tid; x < TOKENS * 64; x += blockDim.x) {
+            const int t = t0 + (x >> 6), i = x & 63;
+            if (t >= n || i >= np) continue;
+            const int a = (int)((i < 32 ? A.axes[0] : A.axes[1]) >> (2 * (i & 31))) & 3;
+            const double turns = (double)A.pos[a * A.pos_sa + (int64_t)b * A.pos_sb + t] * (double)A.inv_freq[i] * 0.15915494309189533577;
+            float s, c;
+            sincospif(2.f * (float)(turns - rint(turns)), &s, &c);
+            cosines[x >> 6][i] = c;
+            sines[x >> 6][i] = A.inverse ? -s : s;
         }
-        // where row t of head h is read and written; false: it is not written
-        auto place = [&](int h, const T*& from, T*& to, bool& turned) {
-            turned = h < nq + nk;
+        __syncthreads();
+        for (int r = tid / LANES; r < TOKENS << log_heads; r += blockDim.x / LANES) {
+            const int tl = r >> log_heads, t = t0 + tl, h = h0 + (r & ((1 << log_heads) - 1));
+            if (t >= n || h >= heads) continue;
+            const bool turned = h < nq + nk;
+            const T* from;
+            T* to;
             if (h < nq) {
                 from = (const T*)A.q + (int64_t)b * A.q_sb + (int64_t)h * A.q_sh + (int64_t)t * A.q_st;
                 to = (T*)A.qo + (int64_t)b * A.qo_sb + (int64_t)h * A.qo_sh + (int64_t)t * A.qo_st;
-                return true;
+            } else {
+                if (t >= fit) continue;
+                const int hk = turned ? h - nq : h - nq - nk;
+                from = turned ? (const T*)A.k + (int64_t)b * A.k_sb + (int64_t)hk * A.k_sh + (int64_t)t * A.k_st
+                              : (const T*)A.v + (int64_t)b * A.v_sb + (int64_t)hk * A.v_sh + (int64_t)t * A.v_st;
+                to = (turned ? (T*)A.ko : (T*)A.vo) + (int64_t)b * A.ko_sb + (int64_t)hk * A.ko_sh + (int64_t)(len + t) * A.ko_st;
             }
-            const int hk = turned ? h - nq : h - nq - nk;
-            from = turned ? (const T*)A.k + (int64_t)b * A.k_sb + (int64_t)hk * A.k_sh + (int64_t)t * A.k_st
-                          : (const T*)A.v + (int64_t)b * A.v_sb + (int64_t)hk * A.v_sh + (int64_t)t * A.v_st;
-            to = (turned ? (T*)A.ko : (T*)A.vo) + (int64_t)b * A.ko_sb + (int64_t)hk * A.ko_sh + (int64_t)(len + t) * A.ko_st;
-            return t < fit;
-        };
-        for (int h = h0; h < h1; ++h) {
-            const T* from;
-            T* to;
-            bool turned;
-            if (!place(h, from, to, turned)) continue;
+            Piece<T> u, v;
+            float x[8], y[8], c[8], s[8];
             if constexpr (VEC) {
-                const bool mine = turned && 8 * o < np;
-                const int c0 = mine && !adj ? 8 * o : 16 * o, c1 = mine && !adj ? np + 8 * o : 16 * o + 8;
-                Piece<T> u, v;
-                u.load(from + c0);
-                v.load(from + c1);
+                const bool mine = turned && 8 * o < np, halves = mine && !adj;
+                u.load(from + (halves ? 8 * o : 16 * o));
+                v.load(from + (halves ? np + 8 * o : 16 * o + 8));
                 if (mine) {
-                    float x[8], y[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) { c[e] = cosines[tl][8 * o + e]; s[e] = sines[tl][8 * o + e]; }
                     u.get(x);
                     v.get(y);
                     if (adj) {
@@ -135,24 +132,29 @@ __global__ __launch_bounds__(ONE ? 1024 : 256) void rope_rows(RopeArgs A, int he
                     u.set(x);
                     v.set(y);
                 }
-                u.store(to + c0);
-                v.store(to + c1);
+                u.store(to + (halves ? 8 * o : 16 * o));
+                v.store(to + (halves ? np + 8 * o : 16 * o + 8));
             } else {
+                u.load(from + 8 * o);
+                if (turned && 8 * o < 2 * np) {
+                    u.get(x);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int i = 8 * o + e;
-                    const bool mine = i < np;
-                    const int c0 = mine && !adj ? i : 2 * i, c1 = mine && !adj ? np + i : 2 * i + 1;
-                    if (turned && mine) {
-                        const float a0 = ld_elem(from + c0), a1 = ld_elem(from + c1);
-                        st_elem(to + c0, fmaf(a0, c[e], -a1 * s[e]));
-                        st_elem(to + c1, fmaf(a0, s[e], a1 * c[e]));
-                    } else {
-                        const T a0 = from[c0], a1 = from[c1];
-                        to[c0] = a0;
-                        to[c1] = a1;
+                    for (int e = 0; e < 8; ++e) {
+                        const int at = 8 * o + e, i = min(adj ? at >> 1 : at < np ? at : at - np, np - 1);
+                        c[e] = cosines[tl][i];
+                        s[e] = sines[tl][i];
+                        y[e] = adj ? x[e ^ 1] : ld_elem(from + (at < np ? at + np : at < 2 * np ? at - np : at));
                     }
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const int at = 8 * o + e;
+                        const bool first = adj ? !(e & 1) : at < np;
+                        // the first of a pair: x cos - y sin; the second: y sin + x cos
+                        if (at < 2 * np) x[e] = first ? fmaf(x[e], c[e], -y[e] * s[e]) : fmaf(y[e], s[e], x[e] * c[e]);
+                    }
+                    u.set(x);
                 }
+                u.store(to + 8 * o);
             }
         }
     }
@@ -179,14 +181,20 @@ hipError_t launch_rope(int dtype, const RopeArgs& a, int32_t* tickets, int n_cu,
     auto go = [&](auto e, auto vec) {
         typedef decltype(e) T;
         constexpr bool VEC = decltype(vec)::value;
-        if (a.n < 8) {
-            const int waves = (heads + 7) / 8, each = waves < 16 ? waves : 16;
-            rope_rows<T, VEC, true><<<dim3(a.n, (waves + each - 1) / each, a.B), 64 * each, 0, st>>>(a, 1, tickets, tickets_apart(a.B));
+        constexpr int lanes = VEC ? 8 : 16, rows = 256 / lanes;       // of a row; of a work-group's step
+        int log_heads = 0;
+        if (a.n < ROPE_TOKENS) {
+            // a token's heads in one work-group, up to 1024 lanes
+            while ((1 << log_heads) < heads && (lanes << log_heads) < 1024) ++log_heads;
+            const int threads = lanes << log_heads < 64 ? 64 : lanes << log_heads;
+            rope_rows<T, VEC, 1><<<dim3(a.n, (heads + (1 << log_heads) - 1) >> log_heads, a.B), threads, 0, st>>>(a, log_heads, tickets, tickets_apart(a.B));
         } else {
-            const int64_t groups = (int64_t)a.B * ((a.n + 31) / 32);
-            int per = 8;
-            while (per > 1 && groups * ((heads + per - 1) / per) < 2 * n_cu) per /= 2;
-            rope_rows<T, VEC, false><<<dim3((a.n + 31) / 32, (heads + per - 1) / per, a.B), 256, 0, st>>>(a, per, tickets, tickets_apart(a.B));
+            const int blocks = (a.n + ROPE_TOKENS - 1) / ROPE_TOKENS;
+            // eight heads, or fewer that leave four work-groups a compute unit, but a step of a work-group at least (fp32, 32 + 32 heads x 2944 tokens with 8, 16, 32 heads
+            // 43.4, 46.1, 46.2 us; 28 + 4 heads x 71000 tokens 270, 272, 277; 28 + 4 + 4 x 4400 tokens, appended 26.2, 28.8, 33.8)
+            while ((1 << log_heads) < heads && log_heads < 3) ++log_heads;
+            while (ROPE_TOKENS << log_heads > rows && (int64_t)a.B * blocks * ((heads + (1 << log_heads) - 1) >> log_heads) < 4 * n_cu) --log_heads;
+            rope_rows<T, VEC, ROPE_TOKENS><<<dim3(blocks, (heads + (1 << log_heads) - 1) >> log_heads, a.B), 256, 0, st>>>(a, log_heads, tickets, tickets_apart(a.B));
         }
         return hipGetLastError();
     };
