@@ -532,6 +532,8 @@ rk_status rk_rope_append_text(rk_ctx* ctx, const rk_layout* L, const rk_rotary* 
  * itself the last row of it, and the segment's first rows, which stay visible.  window 0: all rows up to itself.  What a token does not see does not touch it,
  * also where it is an infinity or a NaN.
  *
+ * (RK_OPT_FORCE_GENERIC changes nothing for these calls and rk_rope's.)
+ *
  * Bytes of workspace for the calls below, for n_tokens new tokens a sequence (rk_decode_attn_window: 1); 0 for an invalid layout or n_tokens outside
  * 1..RK_MAX_TOKENS.  What serves some n_tokens serves fewer; it does not depend on lengths.  It does depend on the context's device (NULL: 256 compute
  * units) and on RK_OPT_DECODE_SPLITS: ask with the context that makes the calls.                                */
@@ -546,6 +548,11 @@ size_t rk_window_workspace_size(const rk_ctx* ctx, const rk_layout* L, int32_t n
 rk_status rk_prefill_attn_window(rk_ctx* ctx, const rk_layout* L, const rk_heads* q, int32_t n_tokens, const int32_t* n_tokens_dev,
                                  const rk_text* text, int32_t window, int32_t sinks, float scale, const rk_heads* out, void* workspace,
                                  size_t workspace_bytes, void* stream);
+
+/* How it shares its work out: the rows of a work-group (a KV head's n_tokens H_q / H_kv; 32 or 256, with fp32 128) and the splits of what they see, for a
+ * segment of at most max_len rows.  INVALID_ARG and UNSUPPORTED as the call.                                    */
+rk_status rk_prefill_plan(const rk_ctx* ctx, const rk_layout* L, int32_t n_tokens, int32_t max_len, int32_t window, int32_t sinks,
+                          int32_t* rows_per_work_group, int32_t* n_splits);
 
 /* rk_decode_attn_dual with a window on the text: one token a sequence, at position len[b] - 1 of the text segment (its own row is appended
  * already), attends all of the rotated cache and the text rows that it sees, under ONE softmax.  k_packed and v_cache both NULL: the text alone, as

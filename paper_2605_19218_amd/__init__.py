@@ -31,7 +31,7 @@ EXPORTS = [
     "rk_decode_attn_dual", "rk_append_text", "rk_fit_subspace", "rk_query_sigma", "rk_append_decode_attn",
     "rk_append_text_decode_attn_dual", "rk_decode_attn_static", "rk_stream_read", "rk_cache_bytes_quant", "rk_compress_quant",
     "rk_append_quant", "rk_unpack_cache_quant", "rk_tree_workspace_size", "rk_tree_plan", "rk_decode_attn_quant", "rk_decode_attn_tree",
-    "rk_decode_attn_tree_quant", "rk_append_text_path", "rk_rope", "rk_rope_append_text", "rk_window_workspace_size",
+    "rk_decode_attn_tree_quant", "rk_append_text_path", "rk_rope", "rk_rope_append_text", "rk_window_workspace_size", "rk_prefill_plan",
     "rk_prefill_attn_window", "rk_decode_attn_window", "rk_decode_attn_window_quant",
 ]
 RK_MAX_DRAFTS = 64
@@ -147,6 +147,7 @@ def lib():
         L.rk_rope_append_text.argtypes = [vp, PL, PO, i32, vp, PH, PH, PH, PH, PT, vp, vp]
         L.rk_window_workspace_size.argtypes = [vp, PL, i32]
         L.rk_window_workspace_size.restype = sz
+        L.rk_prefill_plan.argtypes = [vp, PL, i32, i32, i32, i32, C.POINTER(i32), C.POINTER(i32)]
         L.rk_prefill_attn_window.argtypes = [vp, PL, PH, i32, vp, PT, i32, i32, f32, PH, vp, sz, vp]
         L.rk_decode_attn_window.argtypes = [vp, PL, vp, vp, vp, vp, vp, PT, i32, i32, f32, vp, vp, sz, vp]
         L.rk_decode_attn_window_quant.argtypes = [vp, PL, vp, vp, vp, vp, vp, PT, i32, i32, f32, vp, vp, sz, vp]
@@ -606,6 +607,15 @@ def rk_rope_append_text(ctx, layout: Layout, rope: Rope, n_tokens: int, q: Optio
 
 def rk_window_workspace_size(ctx, layout: Layout, n_tokens: int) -> int:
     return int(lib().rk_window_workspace_size(ctx, C.byref(layout.c()), int(n_tokens)))
+
+
+def rk_prefill_plan(ctx, layout: Layout, n_tokens: int, max_len: int, window: int, sinks: int):
+    """(query rows of a work-group, splits of what they see)."""
+    r, s = C.c_int32(), C.c_int32()
+    st = lib().rk_prefill_plan(ctx, C.byref(layout.c()), int(n_tokens), int(max_len), int(window), int(sinks), C.byref(r), C.byref(s))
+    if st != RK_OK:
+        raise RotateKError(st, lib().rk_status_str(st).decode())
+    return r.value, s.value
 
 
 def rk_prefill_attn_window(ctx, layout: Layout, q: Heads, n_tokens: int, text: Text, window: int, sinks: int, scale: float, out: Heads,

@@ -1406,6 +1406,18 @@ size_t rk_window_workspace_size(const rk_ctx* ctx, const rk_layout* L, int32_t n
     return one > many ? one : many;
 }
 
+rk_status rk_prefill_plan(const rk_ctx* ctx, const rk_layout* L, int32_t n_tokens, int32_t max_len, int32_t window, int32_t sinks,
+                          int32_t* rows_per_work_group, int32_t* n_splits)
+{
+    rk_status s = check_layout(nullptr, L);
+    if (s != RK_OK || (s = check_tokens(nullptr, L, n_tokens)) != RK_OK || (s = check_window(nullptr, window, sinks)) != RK_OK) return s;
+    if (n_tokens < 1 || max_len < 0 || max_len > RK_MAX_TOKENS || !rows_per_work_group || !n_splits) return RK_ERR_INVALID_ARG;
+    const PrefillPlan p = prefill_plan(ctx, L, n_tokens, max_len, window, sinks);
+    *rows_per_work_group = p.rows;
+    *n_splits = p.S;
+    return RK_OK;
+}
+
 rk_status rk_prefill_attn_window(rk_ctx* ctx, const rk_layout* L, const rk_heads* q, int32_t n_tokens, const int32_t* n_tokens_dev,
                                  const rk_text* text, int32_t window, int32_t sinks, float scale, const rk_heads* out, void* workspace,
                                  size_t workspace_bytes, void* stream)

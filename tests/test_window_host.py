@@ -123,3 +123,22 @@ def test_workspace():
         assert size >= last and size >= rk.rk_tree_workspace_size(None, lay(), 1)
         last = size
     assert last < 80 << 20
+
+
+def test_prefill_plan():
+    """Which kernel a prompt goes to, for 256 compute units: few rows on short prompts, many from where the device is full."""
+    plan = lambda n, most, w=0, s=0, **m: rk.rk_prefill_plan(None, lay(**{**dict(batch=1, n_q_heads=32, n_kv_heads=8), **m}), n, most, w, s)
+    assert plan(1, 1)[0] == 32 and plan(40, 1040, 512, 4)[0] == 32 and plan(300, 300)[0] == 32
+    assert plan(500, 8500)[0] == 256 and plan(16384, 16384, 4096, 4) == (256, 1) and plan(100, 100, batch=64)[0] == 256
+    assert plan(40, 1040, dtype=rk.RK_F32)[0] == 128
+    assert plan(1 << 20, 1 << 30)[1] == 1                      # (a full device takes no splits)
+    for dtype in (rk.RK_F32, rk.RK_BF16):
+        for batch, hq, hkv in ((1, 1, 1), (1, 32, 8), (8, 28, 4), (3, 64, 64)):
+            for n in (1, 7, 64, 1000, 30000):
+                for w in (0, 1, 100, 1 << 30, 2 ** 31 - 1):
+                    L = lay(batch=batch, n_q_heads=hq, n_kv_heads=hkv, dtype=dtype)
+                    rows, splits = rk.rk_prefill_plan(None, L, n, n + 5000, w, 2 ** 31 - 1)
+                    assert splits >= 1 and (splits == 1 or 520 * batch * hq * n * splits + 256 <= rk.rk_window_workspace_size(None, L, n))
+    for bad in (dict(n=0), dict(most=-1), dict(most=(1 << 30) + 1), dict(w=-1), dict(s=-1), dict(head_dim=64)):
+        with pytest.raises(rk.RotateKError):
+            plan(**{**dict(n=5, most=5), **bad})
