@@ -433,33 +433,44 @@ RowsPlan window_plan(const rk_ctx* ctx, const rk_layout* L, bool cache, int text
     return p;
 }
 
-// Prompts: rows of a block, blocks of a KV head, splits of what a block sees, whichever come out cheapest, in microseconds as measured: a work-group takes `each` for
-// its beginning and end and `step` for four tiles of few rows, for a stage of 64 tokens of many, or for an fp32 tile; work-groups run one a compute unit (fp32: two, half as
-// fast each); partials are written and read.  bf16, us with 32 / 256 rows a block: 8 units of 4 heads, 1 token on 1000 9.4 / 13.1, 40 on 4000 19.1 / 25.8, the same with a
-// window of 512 12.3 / 20.3, 300 12.4 / 25.0, 700 27.7 / 34.0, 1000 41.8 / 38.8, 500 on 8000 176 / 85, 1500 on 2000 with a window of 512 70 / 35; 32 units of 7
-// heads, 20 on 500 12.0 / 23.1, 100 17.7 / 15.7, 40 on 4000 with a window of 512 23.6 / 29.5, 1000 280 / 96; 512 units of 4 heads, 4 on 500 28.8 / 45.2, 20 on 500
-// 84.7 / 54.5.
-constexpr int PREFILL_SPLITS_MAX = 32;
+// Prompts: rows of a block, blocks of a KV head, splits of what a block sees, whichever come out cheapest, in microseconds as measured. A work-group takes `each` for its
+// beginning and end and `step` for `tokens` of what it sees; no launch is shorter than its longest work-group (`alone` of a step while compute units are to spare), nor than all of them one
+// after another on the compute units, where the last round is not full: that costs as much as a full one if they are equally long, and nothing if the short ones of a
+// causal prompt fill it. Partials are written and read.
+// us, bf16 with 32 / 256 rows a block: 8 units of 4 heads, 1 token on 1000 9.4 / 13.1, 40 on 4000 19.1 / 25.8, the same with a window of 512 12.3 / 20.3, 300 12.4 / 17.2, 700 27.7 /
+// 28.0, 1000 41.8 / 34.6, 500 on 8000 176 / 80, 1500 on 2000 with a window of 512 70 / 35; 32 units of 7 heads, 20 on 500 12.0 / 23.1, 100 17.7 / 15.7, 40 on 4000 with
+// a window of 512 23.6 / 29.5, 1000 280 / 96; 512 units of 4 heads, 4 on 500 28.8 / 45.2, 20 on 500 84.7 / 54.5.  fp32 with 128 / 256 rows: 8 units of 4 heads, 40 on 1000 with a
+// window of 512 22.6 / 25.2, 300 32.1 / 48.6, 700 70 (3 splits) / 55 (4), 1000 131 / 89, 500 on 8000 540 / 343; 32 units of 1 head, 1500 in 1, 2, 3, 4 splits 251, 193, 194, 199 /
+// 199, 132, 144, 149, 2944 591, 599, 601, 613 / 431, 431, 447, 465.  (Of 120 shapes drawn the plan's time was 2 % above the best of all rows and splits on average, 19 % at worst.)
+constexpr int PREFILL_SPLITS_MAX = 32, PREFILL_ROWS = 1024;
 struct PrefillPlan { int rows, blocks, S; };
 PrefillPlan prefill_plan(const rk_ctx* ctx, const rk_layout* L, int n, int max_len, int window, int sinks)
 {
     const int64_t units = (int64_t)L->batch * L->n_kv_heads, G = L->n_q_heads / L->n_kv_heads, n_cu = ctx ? ctx->n_cu : 256;
     PrefillPlan best{};
     double least = 1e300;
-    auto look = [&](int rows, int tokens, double each, double step) {
+    auto look = [&](int rows, int tokens, double each, double step, double alone) {
         const int64_t blocks = ((int64_t)n * G + rows - 1) / rows;
-        // tokens that a block sees: with a window all blocks about as many, else half of the new ones on average
-        int64_t seen = (int64_t)max_len - n / 2;
-        if (window > 0 && (int64_t)window + sinks + rows / G + 1 < seen) seen = (int64_t)window + sinks + rows / G + 1;
-        const int64_t steps = seen > tokens ? (seen + tokens - 1) / tokens : 1;
+        // rows of the segment that a block sees: at most, and on average over the new tokens
+        const double first = max_len > n ? (double)max_len - n + 1 : 1.0, last = max_len > 1 ? (double)max_len : 1.0;
+        double most = last, seen = 0.5 * (first + last);
+        const double bound = (double)window + sinks + rows / G + 1;
+        if (window > 0 && bound < last) {
+            most = bound;
+            seen = bound <= first ? bound : (0.5 * (first + bound) * (bound - first) + bound * (last - bound)) / (last - first);
+        }
+        const int64_t steps = (int64_t)((most + tokens - 1) / tokens);
+        const double even = 2.0 * seen / most - 1.0;           // 1: all as long, 0: from nothing up
         for (int S = 1; S <= PREFILL_SPLITS_MAX && S <= steps; ++S) {
             const int64_t groups = units * blocks * S;
-            // (the workspace holds 256 rows for each compute unit)
-            if (S > 1 && groups * rows > 256 * n_cu) break;
+            // (what the workspace holds)
+            if (S > 1 && groups * rows > PREFILL_ROWS * n_cu) break;
+            const double share = (double)groups / n_cu, full = (double)((groups + n_cu - 1) / n_cu);
+            double rounds = share + (full - share) * (even > 0.0 ? even : 0.0);
+            if (rounds < 1.0) rounds = 1.0;
+            const double mean = seen / tokens / S, longest = each + alone * ((steps + S - 1) / S), all = rounds * (each + step * (mean > 1.0 ? mean : 1.0));
             const double merge = S == 1 ? 0.0 : 2.5 + (double)units * n * G * S * 1040 / 4e6;
-            // (a last round that is not full costs as much as a full one, unless its work-groups are the short ones, which run last)
-            const double full = (double)((groups + n_cu - 1) / n_cu), rounds = groups <= n_cu || rows == 256 ? full : 0.5 * (full + (double)groups / n_cu);
-            const double cost = rounds * (each + step * ((steps + S - 1) / S)) + merge;
+            const double cost = (longest > all ? longest : all) + merge;
             if (cost < least - 0.01) {
                 least = cost;
                 best = PrefillPlan{rows, (int)blocks, S};
@@ -467,17 +478,18 @@ PrefillPlan prefill_plan(const rk_ctx* ctx, const rk_layout* L, int n, int max_l
         }
     };
     if (L->dtype == RK_F32) {
-        look(128, 32, 6.0, 3.6);
+        look(128, 32, 6.0, 4.5, 4.0);
+        look(256, 32, 10.0, 4.5, 4.0);
     } else {
-        look(256, 64, 13.0, 2.2);
-        look(32, 128, 9.0, 1.35);
+        look(256, 64, 13.0, 1.65, 1.65);
+        look(32, 128, 9.0, 1.35, 1.35);
     }
     return best;
 }
-// rows * splits of n tokens or fewer: at most PREFILL_SPLITS_MAX a row, and a block's rows for each work-group of a full device
+// rows * splits of n tokens or fewer: at most PREFILL_SPLITS_MAX a row, and PREFILL_ROWS for each compute unit
 size_t prefill_ws(const rk_ctx* ctx, const rk_layout* L, int n)
 {
-    const size_t rows = (size_t)L->batch * L->n_q_heads * n, most = (size_t)256 * (ctx ? ctx->n_cu : 256);
+    const size_t rows = (size_t)L->batch * L->n_q_heads * n, most = (size_t)PREFILL_ROWS * (ctx ? ctx->n_cu : 256);
     const size_t slots = rows < most / PREFILL_SPLITS_MAX ? rows * PREFILL_SPLITS_MAX : most;
     return align_up(slots * (D + 2) * sizeof(float), 256) + 256;
 }

@@ -112,7 +112,7 @@ struct PrefillArgs {
     int32_t max_len, n;
     int32_t B, Hq, Hkv, G;
     int32_t window, sinks;
-    int32_t rows, blocks, S;     // rows of a block: 128 (fp32), 256 or 32 (bf16); blocks of a KV head; splits of what a block sees
+    int32_t rows, blocks, S;     // rows of a block: 128 or 256 (fp32), 256 or 32 (bf16); blocks of a KV head; splits of what a block sees
     float scale_log2;
     float *ws_m, *ws_l, *ws_acc; // [B, Hkv, n G, S] and [.., S, d]
 };

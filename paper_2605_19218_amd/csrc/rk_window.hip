@@ -260,6 +260,232 @@ __global__ __launch_bounds__(256, 2) void attn_prompt_f32(PrefillArgs A)
     if (A.S > 1 && h == 0) { A.ws_m[slot] = m; A.ws_l[slot] = l; }
 }
 
+// ---- fp32, many rows: products of bf16 parts ---------------------------------------
+// The bf16 matrix instructions are 16 times as fast as the fp32 ones. A number is exactly the sum of three bf16 parts, and of the nine products of two numbers' parts the six
+// large ones leave out less than 2^-24 of the product: 96 instructions of 32 cycles for a tile in place of 128 of 64. Queries are in parts once, weights in registers, Keys and
+// Values on their way into LDS, once for the 256 rows of the eight waves: each thread asks for eight channels of a Key and of a Value a stage ahead (into a place of its own in LDS), and
+// writes their parts for all. Of the two waves of a SIMD one does that in front of its products, the other behind them.
+// (An infinity has NaN for a remainder: a row that sees one gets no number.)
+constexpr int PARTS_ROWS = 256, PARTS_TOKENS = 32, PARTS_PLANE = PARTS_TOKENS * 256, PARTS_STAGE = 6 * PARTS_PLANE, PARTS_RAW = 2 * PARTS_STAGE,
+              PARTS_LDS = PARTS_RAW + 8 * 4096;        // planes [stage][Keys 3, Values 3]; eight waves' own places; and a flag
+
+// eight numbers in parts
+__device__ __forceinline__ void parts3(const float (&x)[8], bf16x8 (&p)[3])
+{
+    float r[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r[i] = x[i];
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            w[i] = __builtin_bit_cast(uint32_t, (bf16x2){(__bf16)r[2 * i], (__bf16)r[2 * i + 1]});
+            if (k < 2) {
+                r[2 * i] -= __uint_as_float(w[i] << 16);
+                r[2 * i + 1] -= __uint_as_float(w[i] & 0xffff0000u);
+            }
+        }
+        p[k] = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
+    }
+}
+// the six products, small ones first
+__device__ __forceinline__ void product3(const bf16x8 (&a)[3], const bf16x8 (&b)[3], f32x16& s)
+{
+    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[2], b[0], s, 0, 0, 0);
+    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[0], b[2], s, 0, 0, 0);
+    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[1], b[1], s, 0, 0, 0);
+    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[1], b[0], s, 0, 0, 0);
+    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[0], b[1], s, 0, 0, 0);
+    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[0], b[0], s, 0, 0, 0);
+}
+
+__global__ __launch_bounds__(512, 2) void attn_prompt_parts(PrefillArgs A)
+{
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    int block, split, u;
+    prompt_place(A, block, split, u);
+    const Prompt<PARTS_TOKENS> P(A, u, block, split, PARTS_ROWS);
+    if (P.row0 >= P.rows) return;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, n = lane & 31;
+    const int row = P.row0 + 32 * wave + n, mine = min(row, P.rows - 1), tok = P.token(A, mine), head = P.hk * A.G + mine - tok * A.G;
+    const Sight sight{P.first + tok, P.window, P.sinks};
+    const int w_lo = P.first + P.token(A, P.row0 + 32 * wave), w_hi = P.first + P.token(A, P.row0 + 32 * wave + 31);
+
+    bf16x8 q[8][3];
+    const float* qp = (const float*)A.q + (int64_t)P.b * A.q_sb + (int64_t)head * A.q_sh + (int64_t)tok * A.q_st;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const f32x4 a = *(const f32x4*)(qp + 16 * i + 8 * h), b = *(const f32x4*)(qp + 16 * i + 8 * h + 4);
+        const float x[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+        parts3(x, q[i]);
+    }
+    const float* kp = (const float*)A.k + (int64_t)P.b * A.sb + (int64_t)P.hk * A.sh;
+    const float* vp = (const float*)A.v + (int64_t)P.b * A.sb + (int64_t)P.hk * A.sh;
+    float m = ROWS_NEG_INF, l = 0.f;
+    f32x16 O[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) O[c][i] = 0.f;
+
+    int* odd = (int*)(lds + PARTS_LDS);
+    if (tid == 0) *odd = 0;
+    __syncthreads();
+    if (P.i0 < P.i1) {
+        // this thread's token of a stage, and its eight channels
+        const int token = tid >> 4, eight = tid & 15;
+        char* own = lds + PARTS_RAW + 4096 * wave + 16 * lane;
+        const uint32_t base = __builtin_amdgcn_readfirstlane(lds_address(lds)) + PARTS_RAW + 4096 * wave;
+        auto fetch = [&](int i) {
+            const int64_t at = (int64_t)min(P.start(i) + token, P.len - 1) * A.st + 8 * eight;
+            load_to_lds(kp + at, base);
+            load_to_lds(kp + at + 4, base + 1024);
+            load_to_lds(vp + at, base + 2048);
+            load_to_lds(vp + at + 4, base + 3072);
+        };
+        // the parts of what was asked for as stage i; then stage `next` is asked for
+        auto ready = [&](int i, int next, char* to) {
+            stage_wait<0>();
+            f32x4 raw[4];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) raw[x] = *(const f32x4*)(own + 1024 * x);
+            asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
+            __builtin_amdgcn_sched_barrier(0);
+            fetch(next);
+            const int at = token * 256 + 16 * slot_of(token, eight);
+            bf16x8 p[3];
+            const float a[8] = {raw[0][0], raw[0][1], raw[0][2], raw[0][3], raw[1][0], raw[1][1], raw[1][2], raw[1][3]};
+            parts3(a, p);
+#pragma unroll
+            for (int k = 0; k < 3; ++k) *(bf16x8*)(to + k * PARTS_PLANE + at) = p[k];
+            float b[8] = {raw[2][0], raw[2][1], raw[2][2], raw[2][3], raw[3][0], raw[3][1], raw[3][2], raw[3][3]};
+            if (P.edge(P.start(i))) {            // Values that are no numbers count as 0 where they may be masked
+                bool any = false;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const bool o = odd_value(__float_as_uint(b[e]));
+                    any |= o;
+                    b[e] = o ? 0.f : b[e];
+                }
+                if (any) *odd = 1;
+            }
+            parts3(b, p);
+#pragma unroll
+            for (int k = 0; k < 3; ++k) *(bf16x8*)(to + (3 + k) * PARTS_PLANE + at) = p[k];
+        };
+        int ka[4], va[2];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) ka[i] = n * 256 + 16 * slot_of(n, 2 * i + h);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int r = 4 * h + ((lane & 15) >> 2);
+            va[i] = 3 * PARTS_PLANE + r * 256 + 16 * slot_of(r, 4 * i + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) + 8 * (lane & 1);
+        }
+        fetch(P.i0);
+        ready(P.i0, min(P.i0 + 1, P.i1 - 1), lds);
+        lds_barrier();
+        int now = 0;
+#pragma unroll 1
+        for (int i = P.i0; i < P.i1; ++i) {
+            const int j0 = P.start(i);
+            const char* at = lds + now;
+            char* other = lds + (now ^ PARTS_STAGE);
+            now ^= PARTS_STAGE;
+            const bool more = i + 1 < P.i1;
+            if (more && wave < 4) ready(i + 1, min(i + 2, P.i1 - 1), other);
+            if (j0 <= w_hi) {                    // (else behind all of this wave's rows)
+                f32x16 s;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[e] = 0.f;
+#pragma unroll
+                for (int x = 0; x < 8; ++x) {
+                    bf16x8 a[3];
+#pragma unroll
+                    for (int k = 0; k < 3; ++k) a[k] = *(const bf16x8*)(at + k * PARTS_PLANE + ka[x & 3] + 128 * (x >> 2));
+                    product3(a, q[x], s);
+                }
+                if (!P.inside(j0, PARTS_TOKENS, w_lo, w_hi)) sight.hide(s, j0 + 4 * h);
+                float mt = s[0];
+#pragma unroll
+                for (int e = 1; e < 16; ++e) mt = fmaxf(mt, s[e]);
+                mt = halves_max(mt) * A.scale_log2;
+                if (__any(mt > m + 8.f)) {
+                    const float m_new = fmaxf(m, mt), alpha = m > ROWS_NEG_INF ? rows_exp2(m - m_new) : 1.f;
+                    l *= alpha;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) O[c] *= alpha;
+                    m = m_new;
+                }
+                const float ref = m > ROWS_NEG_INF ? m : 0.f;
+                float sum = 0.f;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    s[e] = rows_exp2(fmaf(s[e], A.scale_log2, -ref));
+                    sum += s[e];
+                }
+                l += sum;
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    bf16x8 w[3];
+                    const float x[8] = {s[8 * t], s[8 * t + 1], s[8 * t + 2], s[8 * t + 3], s[8 * t + 4], s[8 * t + 5], s[8 * t + 6], s[8 * t + 7]};
+                    parts3(x, w);
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        bf16x8 a[3];
+#pragma unroll
+                        for (int k = 0; k < 3; ++k) {
+                            typedef __attribute__((address_space(3))) s16x4* Lds;
+                            uint2 d[2];
+#pragma unroll
+                            for (int y = 0; y < 2; ++y)
+                                d[y] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                                                     (Lds)(at + k * PARTS_PLANE + va[c & 1] + (16 * t + 8 * y) * 256 + 128 * (c >> 1))));
+                            a[k] = __builtin_bit_cast(bf16x8, make_uint4(d[0].x, d[0].y, d[1].x, d[1].y));
+                        }
+                        product3(a, w, O[c]);
+                    }
+                }
+            }
+            if (more && wave >= 4) ready(i + 1, min(i + 2, P.i1 - 1), other);
+            lds_barrier();
+        }
+        stage_wait<0>();
+        // The Values that were left out join the rows that see them: a sum of one is it, or NaN.
+        if (*odd) {
+#pragma unroll 1
+            for (int i = P.i0; i < P.i1; ++i) {
+                const int j0 = P.start(i);
+                if (!P.edge(j0)) continue;
+#pragma unroll 1
+                for (int j = j0; j < min(j0 + PARTS_TOKENS, P.len); ++j)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const f32x4 v = *(const f32x4*)(vp + (int64_t)j * A.st + 32 * c + 8 * e + 4 * h);
+#pragma unroll
+                            for (int x = 0; x < 4; ++x) O[c][4 * e + x] += odd_value(__float_as_uint(v[x])) && sight.of(j) ? v[x] : 0.f;
+                        }
+            }
+        }
+    }
+
+    l = halves_sum(l);
+    if (row >= P.rows) return;
+    const float inv = A.S > 1 ? 1.f : l == 0.f ? 0.f : 1.f / l;
+    const size_t slot = ((size_t)u * A.n * A.G + row) * A.S + split;
+    float* o = A.S > 1 ? A.ws_acc + slot * D : (float*)A.out + (int64_t)P.b * A.o_sb + (int64_t)head * A.o_sh + (int64_t)tok * A.o_st;
+    const bool none = A.S == 1 && l == 0.f;
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            *(f32x4*)(o + 32 * c + 8 * e + 4 * h) =
+                none ? (f32x4){0.f, 0.f, 0.f, 0.f} : (f32x4){O[c][4 * e], O[c][4 * e + 1], O[c][4 * e + 2], O[c][4 * e + 3]} * inv;
+    if (A.S > 1 && h == 0) { A.ws_m[slot] = m; A.ws_l[slot] = l; }
+}
+
 // ---- bf16, many rows: 64 rows a wave ------------------------------------------------
 // A stage of 64 tokens, four of them in LDS: loads go there without passing through registers, two stages ahead, one barrier a stage. Rows in two groups of 32, so that a Key or Value
 // read from LDS feeds two products.
@@ -784,14 +1010,15 @@ hipError_t launch_prefill(int dtype, const PrefillArgs& a, hipStream_t st)
 {
     const int64_t units = (int64_t)a.B * a.Hkv, groups = units * a.blocks * a.S;
     if (groups > 0x7fffffff || (units * a.n * a.G + 7) / 8 > 0x7fffffff) return hipErrorInvalidValue;
-    auto go = [&](void (*kernel)(PrefillArgs), int lds) {
+    auto go = [&](void (*kernel)(PrefillArgs), int lds, int threads = 256) {
         const hipError_t e = allow_dynamic_lds((const void*)kernel, lds);
         if (e != hipSuccess) return e;
-        kernel<<<(uint32_t)groups, 256, lds, st>>>(a);
+        kernel<<<(uint32_t)groups, threads, lds, st>>>(a);
         return hipGetLastError();
     };
     hipError_t e;
-    if (dtype == 0) e = go(attn_prompt_f32, 2 * F32_STAGE + 16);
+    if (dtype == 0 && a.rows == PARTS_ROWS) e = go(attn_prompt_parts, PARTS_LDS + 16, 512);
+    else if (dtype == 0) e = go(attn_prompt_f32, 2 * F32_STAGE + 16);
     else if (a.rows == FEW_ROWS) e = go(attn_prompt_few, FEW_LDS);
     else e = go(attn_prompt_wide, WIDE_LDS + 16);
     if (e != hipSuccess || a.S == 1) return e;

@@ -66,6 +66,8 @@ KERNELS = [
     (BF, 1, 32, 8, 500, 4000, 2500, 70, 256, True),
     (F32, 40, 8, 4, 90, 100, 20, 2, 128, False),
     (F32, 1, 8, 2, 45, 300, 0, 0, 128, True),
+    (F32, 16, 16, 8, 300, 400, 100, 5, 256, False),
+    (F32, 1, 32, 8, 500, 2000, 900, 30, 256, True),
 ]
 
 
