@@ -17,7 +17,10 @@ namespace rk {
 
 namespace {
 
-// Slots of 16 bytes of a token's row in LDS lie permuted by the token, so that eight tokens' same slot, and four tokens' same pair of slots, are in other banks.
+// LDS serves 256 bytes at a time, and a row of 16-bit numbers in it is 256 bytes: slots of 16 bytes lie permuted by the token, so that sixteen Keys' same slot are sixteen slots, and
+// the two pairs of slots that 32 lanes read of four Values' rows are eight pairs. (fp32 rows are twice as long: eight Keys' same slot.)
+__device__ __forceinline__ int key_slot(int token, int slot) { return slot ^ (4 * (token & 3) | ((token >> 2) & 3)); }
+__device__ __forceinline__ int value_slot(int token, int slot) { return slot ^ 4 * (token & 3); }
 __device__ __forceinline__ int slot_of(int token, int slot) { return slot ^ (2 * (token & 3) | ((token >> 2) & 1)); }
 
 __device__ __forceinline__ bool odd_value(uint32_t bits) { return (bits & 0x7f800000u) == 0x7f800000u; }
@@ -126,9 +129,9 @@ __device__ __forceinline__ void clean_values(char* values, int bytes, int* odd, 
     }
 }
 
-// ---- fp32 --------------------------------------------------------------------------
+// ---- fp32, fewer rows ----------------------------------------------------------------
 // 32 rows a wave, 128 a work-group, two work-groups a compute unit; stages of 32 tokens in LDS, two of them. Bound by the fp32 matrix instructions: 128 of 64 cycles
-// for a tile, to some 500 cycles of vector instructions.
+// for a tile, to some 500 cycles of vector instructions (8 x 28 heads, 500 tokens on 8000 3945 us, 120 TFLOP/s; the matrix cores are busy for 78 % of the cycles).
 constexpr int F32_ROWS = 128, F32_TOKENS = 32, F32_ROW = 512, F32_VALUES = F32_TOKENS * F32_ROW, F32_STAGE = 2 * F32_VALUES;
 
 __global__ __launch_bounds__(256, 2) void attn_prompt_f32(PrefillArgs A)
@@ -201,7 +204,7 @@ __global__ __launch_bounds__(256, 2) void attn_prompt_f32(PrefillArgs A)
                 for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], q[x][e], s, 0, 0, 0);
             }
             if (!P.inside(j0, F32_TOKENS, w_lo, w_hi)) sight.hide(s, j0 + 4 * h);
-            __builtin_amdgcn_s_setprio(1);       // (the other wave of the SIMD has its products; 601 us without, 593 with)
+            __builtin_amdgcn_s_setprio(1);       // (the other wave of the SIMD has its products; 32 heads x 2944 tokens 601 us without, 593 with)
             float mt = s[0];
 #pragma unroll
             for (int e = 1; e < 16; ++e) mt = fmaxf(mt, s[e]);
@@ -265,6 +268,8 @@ __global__ __launch_bounds__(256, 2) void attn_prompt_f32(PrefillArgs A)
 // large ones leave out less than 2^-24 of the product: 96 instructions of 32 cycles for a tile in place of 128 of 64. Queries are in parts once, weights in registers, Keys and
 // Values on their way into LDS, once for the 256 rows of the eight waves: each thread asks for eight channels of a Key and of a Value a stage ahead (into a place of its own in LDS), and
 // writes their parts for all. Of the two waves of a SIMD one does that in front of its products, the other behind them.
+// 8 x 28 heads, 500 tokens on 8000 2240 us, 211 TFLOP/s, 1270 of issued products: what a large bf16 matrix product reaches here. 32 heads x 2944 tokens 417 us, 170 TFLOP/s, where
+// the work-groups, one a compute unit and some three times as long as others, leave a fifth of the compute units' time unused.
 // (An infinity has NaN for a remainder: a row that sees one gets no number.)
 constexpr int PARTS_ROWS = 256, PARTS_TOKENS = 32, PARTS_PLANE = PARTS_TOKENS * 256, PARTS_STAGE = 6 * PARTS_PLANE, PARTS_RAW = 2 * PARTS_STAGE,
               PARTS_LDS = PARTS_RAW + 8 * 4096;        // planes [stage][Keys 3, Values 3]; eight waves' own places; and a flag
@@ -353,12 +358,12 @@ __global__ __launch_bounds__(512, 2) void attn_prompt_parts(PrefillArgs A)
             asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
             __builtin_amdgcn_sched_barrier(0);
             fetch(next);
-            const int at = token * 256 + 16 * slot_of(token, eight);
+            const int kat = token * 256 + 16 * key_slot(token, eight), vat = token * 256 + 16 * value_slot(token, eight);
             bf16x8 p[3];
             const float a[8] = {raw[0][0], raw[0][1], raw[0][2], raw[0][3], raw[1][0], raw[1][1], raw[1][2], raw[1][3]};
             parts3(a, p);
 #pragma unroll
-            for (int k = 0; k < 3; ++k) *(bf16x8*)(to + k * PARTS_PLANE + at) = p[k];
+            for (int k = 0; k < 3; ++k) *(bf16x8*)(to + k * PARTS_PLANE + kat) = p[k];
             float b[8] = {raw[2][0], raw[2][1], raw[2][2], raw[2][3], raw[3][0], raw[3][1], raw[3][2], raw[3][3]};
             if (P.edge(P.start(i))) {            // Values that are no numbers count as 0 where they may be masked
                 bool any = false;
@@ -372,15 +377,15 @@ __global__ __launch_bounds__(512, 2) void attn_prompt_parts(PrefillArgs A)
             }
             parts3(b, p);
 #pragma unroll
-            for (int k = 0; k < 3; ++k) *(bf16x8*)(to + (3 + k) * PARTS_PLANE + at) = p[k];
+            for (int k = 0; k < 3; ++k) *(bf16x8*)(to + (3 + k) * PARTS_PLANE + vat) = p[k];
         };
-        int ka[4], va[2];
+        int ka[8], va[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) ka[i] = n * 256 + 16 * slot_of(n, 2 * i + h);
+        for (int i = 0; i < 8; ++i) ka[i] = n * 256 + 16 * key_slot(n, 2 * i + h);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < 4; ++i) {
             const int r = 4 * h + ((lane & 15) >> 2);
-            va[i] = 3 * PARTS_PLANE + r * 256 + 16 * slot_of(r, 4 * i + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) + 8 * (lane & 1);
+            va[i] = 3 * PARTS_PLANE + r * 256 + 16 * value_slot(r, 4 * i + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) + 8 * (lane & 1);
         }
         fetch(P.i0);
         ready(P.i0, min(P.i0 + 1, P.i1 - 1), lds);
@@ -402,7 +407,7 @@ __global__ __launch_bounds__(512, 2) void attn_prompt_parts(PrefillArgs A)
                 for (int x = 0; x < 8; ++x) {
                     bf16x8 a[3];
 #pragma unroll
-                    for (int k = 0; k < 3; ++k) a[k] = *(const bf16x8*)(at + k * PARTS_PLANE + ka[x & 3] + 128 * (x >> 2));
+                    for (int k = 0; k < 3; ++k) a[k] = *(const bf16x8*)(at + k * PARTS_PLANE + ka[x]);
                     product3(a, q[x], s);
                 }
                 if (!P.inside(j0, PARTS_TOKENS, w_lo, w_hi)) sight.hide(s, j0 + 4 * h);
@@ -440,7 +445,7 @@ __global__ __launch_bounds__(512, 2) void attn_prompt_parts(PrefillArgs A)
 #pragma unroll
                             for (int y = 0; y < 2; ++y)
                                 d[y] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                                                                     (Lds)(at + k * PARTS_PLANE + va[c & 1] + (16 * t + 8 * y) * 256 + 128 * (c >> 1))));
+                                                                     (Lds)(at + k * PARTS_PLANE + va[c] + (16 * t + 8 * y) * 256)));
                             a[k] = __builtin_bit_cast(bf16x8, make_uint4(d[0].x, d[0].y, d[1].x, d[1].y));
                         }
                         product3(a, w, O[c]);
@@ -488,8 +493,11 @@ __global__ __launch_bounds__(512, 2) void attn_prompt_parts(PrefillArgs A)
 
 // ---- bf16, many rows: 64 rows a wave ------------------------------------------------
 // A stage of 64 tokens, four of them in LDS: loads go there without passing through registers, two stages ahead, one barrier a stage. Rows in two groups of 32, so that a Key or Value
-// read from LDS feeds two products.
-// In LDS a token's row is its 256 bytes, slots permuted as slot_of() says: what a load leaves is lane by lane, so it is the lanes' addresses that are permuted.
+// read from LDS feeds two products. (With 32 rows a wave and two waves a SIMD LDS would have to deliver 128 bytes a cycle, all it has.)
+// 28 heads x 16384 tokens, all visible 1692 to 1790 us, 1075 to 1137 TFLOP/s; with a window of 4096 820 to 858, 980 to 1030: a large matrix product reaches 1161 here. The matrix cores are busy for 46 % of the
+// cycles at 2.2 GHz, vector instructions for as many; without the exponentials, the reads of LDS, the barriers or the maxima each it is 2 to 10 % faster, so no one of them bounds it.
+// A work-group's beginning and end take 13 us, a stage 1.65.
+// In LDS a token's row is its 256 bytes, slots permuted as key_slot() and value_slot() say: what a load leaves is lane by lane, so it is the lanes' addresses that are permuted.
 constexpr int WIDE_ROWS = 256, WIDE_TOKENS = 64, WIDE_ROW = 256, WIDE_VALUES = WIDE_TOKENS * WIDE_ROW, WIDE_STAGE = 2 * WIDE_VALUES;
 constexpr int WIDE_LDS = 4 * WIDE_STAGE;      // and a flag
 
@@ -511,11 +519,11 @@ struct WideRows {
             for (int i = 0; i < 8; ++i) asm volatile("" : "+a"(q[g][i]));
         }
     }
-    // a tile's 32 Keys; ka: this lane's places of pieces 0..3 of the tile's first token
-    static __device__ __forceinline__ void keys(const char* lds, const int (&ka)[4], int at, bf16x8 (&k)[8])
+    // a tile's 32 Keys; ka: this lane's places of its pieces
+    static __device__ __forceinline__ void keys(const char* lds, const int (&ka)[8], int at, bf16x8 (&k)[8])
     {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) k[i] = *(const bf16x8*)(lds + ka[i & 3] + at + 128 * (i >> 2));
+        for (int i = 0; i < 8; ++i) k[i] = *(const bf16x8*)(lds + ka[i] + at);
     }
     // S^T of them
     __device__ __forceinline__ void scores(const bf16x8 (&k)[8], f32x16 (&s)[2]) const
@@ -556,11 +564,11 @@ struct WideRows {
             m[g] = m_new;
         }
     }
-    // half x of channels 32 b + lane % 32 of the tile's tokens 16 t + (4 h ..+3, 8 + 4 h ..+3); va: this lane's places of blocks 0 and 1
-    static __device__ __forceinline__ s16x4 values(const char* lds, const int (&va)[2], int at, int t, int b, int x)
+    // half x of channels 32 b + lane % 32 of the tile's tokens 16 t + (4 h ..+3, 8 + 4 h ..+3); va: this lane's places of the blocks
+    static __device__ __forceinline__ s16x4 values(const char* lds, const int (&va)[4], int at, int t, int b, int x)
     {
         typedef __attribute__((address_space(3))) s16x4* Lds;
-        return __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(lds + va[b & 1] + at + (16 * t + 8 * x) * WIDE_ROW + 128 * (b >> 1)));
+        return __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(lds + va[b] + at + (16 * t + 8 * x) * WIDE_ROW));
     }
     // a tile on an edge: what a row does not see has no score
     __device__ __forceinline__ void hide(f32x16 (&s)[2], float (&top)[2], int j0, int h) const
@@ -584,8 +592,8 @@ struct WideRows {
     // the weights, 16 pairs of 52 cycles (the exponentials 16 each), two in three instructions' time, and the last eight the maxima and beside(0..7), a load of
     // a later stage each; LDS is read one piece a step.
     template <typename F>
-    __device__ __forceinline__ void tile(f32x16 (&s)[2], f32x16 (&next)[2], float (&top)[2], bf16x8 (&k)[8], const char* lds, const int (&ka)[4], int kt,
-                                         const int (&va)[2], int vt, F beside)
+    __device__ __forceinline__ void tile(f32x16 (&s)[2], f32x16 (&next)[2], float (&top)[2], bf16x8 (&k)[8], const char* lds, const int (&ka)[8], int kt,
+                                         const int (&va)[4], int vt, F beside)
     {
         if (behind(top)) follow(top);
         hold();
@@ -617,7 +625,7 @@ struct WideRows {
                 O[g][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, make_uint4(v0.x, v0.y, v1.x, v1.y)),
                                                                   __builtin_bit_cast(bf16x8, make_uint4(p[g][4 * t], p[g][4 * t + 1], p[g][4 * t + 2], p[g][4 * t + 3])),
                                                                   O[g][b], 0, 0, 0);
-                if (x >= 24) k[x - 24] = *(const bf16x8*)(lds + ka[x & 3] + kt + 128 * ((x - 24) >> 2));
+                if (x >= 24) k[x - 24] = *(const bf16x8*)(lds + ka[x - 24] + kt);
             }
             // pairs 2 y and 2 y + 1 in steps 3 y ..+2, each one's sums and rounding a step behind
             if (x < 24 && x % 3 < 2) weigh(2 * (x / 3) + x % 3);
@@ -667,14 +675,19 @@ __global__ __launch_bounds__(256, 1) void attn_prompt_wide(PrefillArgs A)
     const bf16_t* vp = (const bf16_t*)A.v + (int64_t)P.b * A.sb + (int64_t)P.hk * A.sh;
     int* odd = (int*)(lds + WIDE_LDS);
     if (P.i0 < P.i1) {
-        // Rows 16 wave + 4 x + lane / 16 of a stage, x < 4: their 16-byte pieces, in the order that slot_of() undoes.  A lane's places in a stage are the same in all of
+        // Rows 16 wave + 4 x + lane / 16 of a stage, x < 4: their 16-byte pieces, in the order that reading them undoes.  A lane's places in a stage are the same in all of
         // them; in one that reaches behind the last row they repeat it.
         const uint32_t base = __builtin_amdgcn_readfirstlane(lds_address(lds)) + 16 * WIDE_ROW * wave;
         const int64_t apart = vp - kp;
-        int64_t place[4];
+        int64_t place[4];                // of Keys
+        int aside[4];                    // of the Values, from there
         auto places = [&](int last) {
 #pragma unroll
-            for (int x = 0; x < 4; ++x) place[x] = (int64_t)min(16 * wave + 4 * x + (lane >> 4), last) * A.st + 8 * slot_of(4 * x + (lane >> 4), lane & 15);
+            for (int x = 0; x < 4; ++x) {
+                const int token = 4 * x + (lane >> 4), slot = key_slot(token, lane & 15);
+                place[x] = (int64_t)min(16 * wave + token, last) * A.st + 8 * slot;
+                aside[x] = 8 * (value_slot(token, lane & 15) - slot);
+            }
         };
         places(WIDE_TOKENS);
         const bf16_t* from = kp;         // the stage that is asked for
@@ -685,7 +698,7 @@ __global__ __launch_bounds__(256, 1) void attn_prompt_wide(PrefillArgs A)
         };
         auto load = [&](int piece, int buf) {
             const int x = piece >> 1, v = piece & 1;
-            load_to_lds((v ? from + apart : from) + place[x], base + buf + v * WIDE_VALUES + 4 * WIDE_ROW * x);
+            load_to_lds((v ? from + apart + aside[x] : from) + place[x], base + buf + v * WIDE_VALUES + 4 * WIDE_ROW * x);
         };
         auto fetch = [&](int i, int buf) {
             aim(i);
@@ -701,13 +714,13 @@ __global__ __launch_bounds__(256, 1) void attn_prompt_wide(PrefillArgs A)
             clean_values<bf16_t>(lds + WIDE_VALUES, WIDE_VALUES, odd, tid);
             lds_barrier();
         }
-        int ka[4], va[2];
+        int ka[8], va[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) ka[i] = n * WIDE_ROW + 16 * slot_of(n, 2 * i + h);
+        for (int i = 0; i < 8; ++i) ka[i] = n * WIDE_ROW + 16 * key_slot(n, 2 * i + h);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < 4; ++i) {
             const int r = 4 * h + ((lane & 15) >> 2);
-            va[i] = r * WIDE_ROW + 16 * slot_of(r, 4 * i + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) + 8 * (lane & 1);
+            va[i] = r * WIDE_ROW + 16 * value_slot(r, 4 * i + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) + 8 * (lane & 1);
         }
         f32x16 s0[2], s1[2];
         bf16x8 k[8];
@@ -801,7 +814,8 @@ __global__ __launch_bounds__(256, 1) void attn_prompt_wide(PrefillArgs A)
 
 // ---- bf16, few rows ------------------------------------------------------------------
 // 32 rows a work-group, whose four waves take a tile of 32 tokens each in turn: what a short prompt waits for is its chain of round trips, so nothing in it is
-// waited for by four waves, every wave has its next tile on the way into its own part of LDS, and the waves meet once, to join their sums.
+// waited for by four waves, every wave has its next tile on the way into its own part of LDS, and the waves meet once, to join their sums. 40 tokens of 8 units of 4 heads behind 1000, a window
+// of 512: 7.6 us and 3.6 for the fold (256 rows a work-group: 18.8 and 3.9); a work-group takes 9 us, and 1.35 for each four tiles.
 constexpr int FEW_ROWS = 32, FEW_TOKENS = 32, FEW_TILE = 2 * FEW_TOKENS * 256, FEW_WAVE = 2 * FEW_TILE, FEW_LDS = 4 * FEW_WAVE;
 constexpr int FEW_PARK = 33;     // 32 rows' quads, and one: lanes that write quads side by side meet other banks
 
@@ -831,18 +845,19 @@ __global__ __launch_bounds__(256, 1) void attn_prompt_few(PrefillArgs A)
         const int j = P.start(i);
 #pragma unroll
         for (int x = 0; x < 8; ++x) {
-            const int64_t at = (int64_t)min(j + 4 * x + (lane >> 4), P.len - 1) * A.st + 8 * slot_of(4 * x + (lane >> 4), lane & 15);
-            load_to_lds(kp + at, base + buf + 1024 * x);
-            load_to_lds(vp + at, base + buf + FEW_TILE / 2 + 1024 * x);
+            const int token = 4 * x + (lane >> 4);
+            const int64_t at = (int64_t)min(j + token, P.len - 1) * A.st;
+            load_to_lds(kp + at + 8 * key_slot(token, lane & 15), base + buf + 1024 * x);
+            load_to_lds(vp + at + 8 * value_slot(token, lane & 15), base + buf + FEW_TILE / 2 + 1024 * x);
         }
     };
-    int ka[4], va[2];
+    int ka[8], va[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) ka[i] = n * 256 + 16 * slot_of(n, 2 * i + h);
+    for (int i = 0; i < 8; ++i) ka[i] = n * 256 + 16 * key_slot(n, 2 * i + h);
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < 4; ++i) {
         const int r = 4 * h + ((lane & 15) >> 2);
-        va[i] = FEW_TILE / 2 + r * 256 + 16 * slot_of(r, 4 * i + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) + 8 * (lane & 1);
+        va[i] = FEW_TILE / 2 + r * 256 + 16 * value_slot(r, 4 * i + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) + 8 * (lane & 1);
     }
     float m = ROWS_NEG_INF, l = 0.f;
     f32x16 O[4];
@@ -868,7 +883,7 @@ __global__ __launch_bounds__(256, 1) void attn_prompt_few(PrefillArgs A)
 #pragma unroll
         for (int e = 0; e < 16; ++e) s[e] = 0.f;
 #pragma unroll
-        for (int x = 0; x < 8; ++x) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8*)(at + ka[x & 3] + 128 * (x >> 2)), q[x], s, 0, 0, 0);
+        for (int x = 0; x < 8; ++x) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8*)(at + ka[x]), q[x], s, 0, 0, 0);
         const bool edge = P.edge(j0);
         if (edge) sight.hide(s, j0 + 4 * h);
         float mt = s[0];
@@ -902,7 +917,7 @@ __global__ __launch_bounds__(256, 1) void attn_prompt_few(PrefillArgs A)
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
                     typedef __attribute__((address_space(3))) s16x4* Lds;
-                    const uint2 d = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(at + va[c & 1] + (16 * t + 8 * x) * 256 + 128 * (c >> 1))));
+                    const uint2 d = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(at + va[c] + (16 * t + 8 * x) * 256)));
                     a[2 * x] = d.x;
                     a[2 * x + 1] = d.y;
                 }
