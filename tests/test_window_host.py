@@ -112,6 +112,7 @@ def test_decode(ctx, f):
     assert call(w=-1) == BAD and call(s=-5) == BAD and call(t=text(max_len=50)) == BAD
     assert call(L=lay(max_seq_len=129)) == CAP
     assert call(ws=None) == WS and call(wb=16) == WS and call(ws=P + 4) == WS
+    assert call(L=lay(batch=65535, n_q_heads=65534, n_kv_heads=2), wb=1 << 60) == rk.RK_ERR_UNSUPPORTED
 
 
 def test_workspace():
