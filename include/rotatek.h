@@ -519,7 +519,7 @@ rk_status rk_rope(rk_ctx* ctx, const rk_layout* L, const rk_rotary* rope, int32_
 
 /* New tokens join the text segment with their positions on: row len[b] + t of text->k / text->v receives row t of k, turned, and of v as it is, for
  * every KV head and t < n_tokens_dev[b] (as above); len_out[b] = len[b] + the rows written, which end where the segment is full.  len_out may be text->len
- * or another array.  q and q_out as in rk_rope (all n_tokens_dev[b] rows), or both NULL.  One token a sequence is a decode's step, in
+ * or an array that the call does not read.  q and q_out as in rk_rope (all n_tokens_dev[b] rows), or both NULL.  One token a sequence is a decode's step, in
  * front of rk_decode_attn_window or rk_decode_attn_dual; many are a prompt, in front of rk_prefill_attn_window.  The stretch of memory from the segment's first row to its
  * last may not meet k's or v's.  RK_ERR_CAPACITY if text->max_len + n_tokens > text->capacity (max_len bounds len[b] BEFORE the call).  Calls on
  * one context must not overlap.  Errors: INVALID_ARG, UNSUPPORTED, CAPACITY, HIP.                                */

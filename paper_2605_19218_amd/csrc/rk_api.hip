@@ -1383,6 +1383,8 @@ rk_status rk_rope_append_text(rk_ctx* ctx, const rk_layout* L, const rk_rotary* 
     if ((s = check_turned(ctx, q, q_out, "rope_append_text: q or q_out", L->batch, L->n_q_heads, n_tokens)) != RK_OK) return s;
     if ((s = check_heads(ctx, k, "rope_append_text: k")) != RK_OK || (s = check_heads(ctx, v, "rope_append_text: v")) != RK_OK) return s;
     if (!len_out) return fail(ctx, RK_ERR_INVALID_ARG, "rope_append_text: len_out is NULL");
+    // (written while other work-groups may still read it)
+    if (len_out == n_tokens_dev) return fail(ctx, RK_ERR_INVALID_ARG, "rope_append_text: len_out is n_tokens_dev");
     if (n_tokens < 1) return fail(ctx, RK_ERR_INVALID_ARG, "rope_append_text: n_tokens %d", n_tokens);
     if (text->max_len > text->capacity - n_tokens)
         return fail(ctx, RK_ERR_CAPACITY, "rope_append_text: %d + %d rows exceed capacity %d", text->max_len, n_tokens, text->capacity);
