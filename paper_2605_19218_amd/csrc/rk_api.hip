@@ -437,13 +437,22 @@ RowsPlan window_plan(const rk_ctx* ctx, const rk_layout* L, bool cache, int text
 // beginning and end and `step` for `tokens` of what it sees; no launch is shorter than its longest work-group (`alone` of a step while compute units are to spare), nor than all of them one
 // after another on the compute units, where the last round is not full: that costs as much as a full one if they are equally long, and nothing if the short ones of a
 // causal prompt fill it. Partials are written and read.
-// us, bf16 with 32 / 256 rows a block: 8 units of 4 heads, 1 token on 1000 9.4 / 13.1, 40 on 4000 19.1 / 25.8, the same with a window of 512 12.3 / 20.3, 300 12.4 / 17.2, 700 27.7 /
-// 28.0, 1000 41.8 / 34.6, 500 on 8000 176 / 80, 1500 on 2000 with a window of 512 70 / 35; 32 units of 7 heads, 20 on 500 12.0 / 23.1, 100 17.7 / 15.7, 40 on 4000 with
-// a window of 512 23.6 / 29.5, 1000 280 / 96; 512 units of 4 heads, 4 on 500 28.8 / 45.2, 20 on 500 84.7 / 54.5.  fp32 with 128 / 256 rows: 8 units of 4 heads, 40 on 1000 with a
-// window of 512 22.6 / 25.2, 300 32.1 / 48.6, 700 70 (3 splits) / 55 (4), 1000 131 / 89, 500 on 8000 540 / 343; 32 units of 1 head, 1500 in 1, 2, 3, 4 splits 251, 193, 194, 199 /
-// 199, 132, 144, 149, 2944 591, 599, 601, 613 / 431, 431, 447, 465.  (Of 120 shapes drawn the plan's time was 2 % above the best of all rows and splits on average, 19 % at worst.)
+// us, bf16 with 32 / 256 rows a block: 8 units of 4 heads, 1 token on 1000 9.7 / 13.0, 40 on 4000 18.9 / 26.5, the same with a window of 512 12.4 / 19.3, 300 12.9 / 17.7, 700 28.2 /
+// 28.9, 1000 42.8 / 34.5, 500 on 8000 176 / 83, 1500 on 2000 with a window of 512 71 / 35; 32 units of 7 heads, 20 on 500 12.0 / 21.9, 100 18.3 / 16.0, 40 on 4000 with
+// a window of 512 24.0 / 29.6, 1000 286 / 98; 512 units of 4 heads, 4 on 500 28.8 / 46.7, 20 on 500 85.1 / 54.6.  fp32 with 128 / 256 rows: 8 units of 4 heads, 40 on 1000 with a
+// window of 512 23.3 / 25.7, 300 28.1 / 31.1, 700 67 (4 splits) / 47 (5), 1000 109 / 71, 500 on 8000 525 / 339; 32 units of 1 head, 1500 in 1, 2, 3, 4 splits 251, 193, 194, 198 /
+// 190, 132, 144, 148, 2944 591, 601 / 421, 430.  (Of 100 shapes drawn the plan's time was 2 % above the best of all rows and splits on average, 17 % at worst.)
+// Where all work-groups run at once the longest is waited for, and a block takes a split for each so many tokens that it sees: less is begun, written and folded than with as many for all blocks.  us, all
+// alike / by length: fp32 8 units of 4 heads, 300 in 5 splits 34 / 28, 1000 89 / 71, 2 units of 8 heads, 1000 58 / 47; bf16 8 units of 1 head, 3000 in 4 56 / 47.  Where they do not, the
+// long ones have to come first, which they do with as many for all (fp32 4 units of 7 heads, 2944 in 2 363 / 385).
 constexpr int PREFILL_SPLITS_MAX = 32, PREFILL_ROWS = 1024;
-struct PrefillPlan { int rows, blocks, S; };
+struct PrefillPlan { int rows, blocks, S, tokens; };      // S: splits of a block; tokens not 0: one for each so many that it sees, up to S
+// The first block of which a token may see more than `most` rows.
+int prefill_cut(int rows, int64_t G, int n, int max_len, int64_t most)
+{
+    const int64_t token = most - ((int64_t)max_len - n);         // (the first to)
+    return token <= 0 ? 0 : (int)(token * G / rows);
+}
 PrefillPlan prefill_plan(const rk_ctx* ctx, const rk_layout* L, int n, int max_len, int window, int sinks)
 {
     const int64_t units = (int64_t)L->batch * L->n_kv_heads, G = L->n_q_heads / L->n_kv_heads, n_cu = ctx ? ctx->n_cu : 256;
@@ -459,21 +468,29 @@ PrefillPlan prefill_plan(const rk_ctx* ctx, const rk_layout* L, int n, int max_l
             most = bound;
             seen = bound <= first ? bound : (0.5 * (first + bound) * (bound - first) + bound * (last - bound)) / (last - first);
         }
-        const int64_t steps = (int64_t)((most + tokens - 1) / tokens);
         const double even = 2.0 * seen / most - 1.0;           // 1: all as long, 0: from nothing up
+        const int64_t steps = (int64_t)((most + tokens - 1) / tokens);
         for (int S = 1; S <= PREFILL_SPLITS_MAX && S <= steps; ++S) {
-            const int64_t groups = units * blocks * S;
             // (what the workspace holds)
-            if (S > 1 && groups * rows > PREFILL_ROWS * n_cu) break;
-            const double share = (double)groups / n_cu, full = (double)((groups + n_cu - 1) / n_cu);
+            if (S > 1 && units * blocks * S * rows > PREFILL_ROWS * n_cu) break;
+            const int64_t stretch = (steps + S - 1) / S;
+            double parts = S;
+            bool by_length = S > 1 && S <= PREFILL_CUTS + 1 && (S - 1) * stretch < steps && first <= (S - 1) * stretch * tokens;
+            if (by_length) {
+                int64_t all = blocks;
+                for (int i = 1; i < S; ++i) all += blocks - prefill_cut(rows, G, n, max_len, i * stretch * tokens);
+                by_length = units * all <= n_cu;
+                if (by_length) parts = (double)all / blocks;
+            }
+            const double groups = (double)(units * blocks) * parts, share = groups / n_cu, full = (double)(int64_t)(share + 0.999);
             double rounds = share + (full - share) * (even > 0.0 ? even : 0.0);
             if (rounds < 1.0) rounds = 1.0;
-            const double mean = seen / tokens / S, longest = each + alone * ((steps + S - 1) / S), all = rounds * (each + step * (mean > 1.0 ? mean : 1.0));
-            const double merge = S == 1 ? 0.0 : 2.5 + (double)units * n * G * S * 1040 / 4e6;
+            const double mean = seen / tokens / parts, longest = each + alone * stretch, all = rounds * (each + step * (mean > 1.0 ? mean : 1.0));
+            const double merge = S == 1 ? 0.0 : 2.5 + (double)units * n * G * parts * 1040 / 4e6;
             const double cost = (longest > all ? longest : all) + merge;
             if (cost < least - 0.01) {
                 least = cost;
-                best = PrefillPlan{rows, (int)blocks, S};
+                best = PrefillPlan{rows, (int)blocks, S, by_length ? (int)(stretch * tokens) : 0};
             }
         }
     };
@@ -1461,6 +1478,7 @@ rk_status rk_prefill_attn_window(rk_ctx* ctx, const rk_layout* L, const rk_heads
     a.window = window; a.sinks = sinks;
     const PrefillPlan p = prefill_plan(ctx, L, n_tokens, text->max_len, window, sinks);
     a.rows = p.rows; a.blocks = p.blocks; a.S = p.S;
+    for (int i = 0; i < PREFILL_CUTS; ++i) a.cut[i] = i + 1 >= p.S ? p.blocks : p.tokens ? prefill_cut(p.rows, a.G, n_tokens, text->max_len, (int64_t)(i + 1) * p.tokens) : 0;
     const float sc = scale > 0.f ? scale : 1.0f / sqrtf((float)L->head_dim);
     a.scale_log2 = sc * 1.44269504088896340736f;
     const size_t slots = (size_t)a.B * a.Hq * n_tokens * a.S;

@@ -102,6 +102,7 @@ hipError_t launch_window_rows_q8_bf16(const WindowRowsArgs& a, hipStream_t st);
 hipError_t launch_window_rows_q8_f32(const WindowRowsArgs& a, hipStream_t st);
 
 // ---- rk_window.hip: new tokens over the text segment ------------------------------
+constexpr int PREFILL_CUTS = 7;
 struct PrefillArgs {
     const void* q;
     void* out;
@@ -112,7 +113,8 @@ struct PrefillArgs {
     int32_t max_len, n;
     int32_t B, Hq, Hkv, G;
     int32_t window, sinks;
-    int32_t rows, blocks, S;     // rows of a block: 128 or 256 (fp32), 256 or 32 (bf16); blocks of a KV head; splits of what a block sees
+    int32_t rows, blocks, S;     // rows of a block: 128 or 256 (fp32), 256 or 32 (bf16); blocks of a KV head; splits of what a block sees, at most
+    int32_t cut[PREFILL_CUTS];   // blocks from cut[i] on are in i + 2 splits or more; with more than PREFILL_CUTS + 1 all blocks are in S
     float scale_log2;
     float *ws_m, *ws_l, *ws_acc; // [B, Hkv, n G, S] and [.., S, d]
 };

@@ -44,14 +44,36 @@ struct Sight {
     }
 };
 
+// The splits of a block.
+__device__ __forceinline__ int prompt_splits(const PrefillArgs& A, int block)
+{
+    int splits = 1;
+#pragma unroll
+    for (int i = 0; i < PREFILL_CUTS; ++i) splits += block >= A.cut[i] ? 1 : 0;
+    return A.S > PREFILL_CUTS + 1 ? A.S : splits;
+}
+
 // Which rows and splits a work-group takes: the last blocks of all KV heads first, which see most, so that the short ones fill the gaps at the end; a head's
-// work-groups go to the same XCDs, which read its Keys and Values from their L2.
-__device__ __forceinline__ void prompt_place(const PrefillArgs& A, int& block, int& split, int& u)
+// work-groups go to the same XCDs, which read its Keys and Values from their L2.  (No branches: with one the wide kernel spills.)
+__device__ __forceinline__ void prompt_place(const PrefillArgs& A, int& block, int& split, int& splits, int& u)
 {
     const uint32_t units = A.B * A.Hkv, rank = blockIdx.x / units;
     u = blockIdx.x - rank * units;
-    block = A.blocks - 1 - (int)(rank / A.S);
-    split = rank % A.S;
+    int at = (int)rank, end = A.blocks;          // rank among the blocks in front of `end`
+    bool found = A.S > PREFILL_CUTS + 1;
+    splits = found ? A.S : 1;
+#pragma unroll
+    for (int i = PREFILL_CUTS; i > 0; --i) {
+        const int cut = A.cut[i - 1], count = (end - cut) * (i + 1);
+        const bool here = !found && at < count;
+        splits = here ? i + 1 : splits;
+        found = found || here;
+        at -= found ? 0 : count;
+        end = found ? end : cut;
+    }
+    const int each = (int)((uint32_t)at / (uint32_t)splits);
+    block = end - 1 - each;
+    split = at - each * splits;
 }
 
 __device__ __forceinline__ uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)p; }
@@ -71,7 +93,7 @@ template <int TOKENS>
 struct Prompt {
     int b, hk, len, first, rows, row0, window, sinks, p_lo, p_hi, few, from, i0, i1;
     bool before;                 // some of the rows stand in front of row 0
-    __device__ __forceinline__ Prompt(const PrefillArgs& A, int u, int block, int split, int size)
+    __device__ __forceinline__ Prompt(const PrefillArgs& A, int u, int block, int split, int splits, int size)
     {
         b = u / A.Hkv;
         hk = u - b * A.Hkv;
@@ -96,8 +118,8 @@ struct Prompt {
             stages = few + p_hi / TOKENS - from + 1;
         }
         // (stages and splits stay below 2^25 and 2^6)
-        i0 = (int)((uint32_t)stages * (uint32_t)split / (uint32_t)A.S);
-        i1 = (int)((uint32_t)stages * (uint32_t)(split + 1) / (uint32_t)A.S);
+        i0 = (int)((uint32_t)stages * (uint32_t)split / (uint32_t)splits);
+        i1 = (int)((uint32_t)stages * (uint32_t)(split + 1) / (uint32_t)splits);
     }
     __device__ __forceinline__ int token(const PrefillArgs& A, int r) const { return (int)((uint32_t)min(r, rows - 1) / (uint32_t)A.G); }
     __device__ __forceinline__ int start(int i) const { return TOKENS * (i < few ? i : i - few + from); }
@@ -137,9 +159,9 @@ constexpr int F32_ROWS = 128, F32_TOKENS = 32, F32_ROW = 512, F32_VALUES = F32_T
 __global__ __launch_bounds__(256, 2) void attn_prompt_f32(PrefillArgs A)
 {
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    int block, split, u;
-    prompt_place(A, block, split, u);
-    const Prompt<F32_TOKENS> P(A, u, block, split, F32_ROWS);
+    int block, split, splits, u;
+    prompt_place(A, block, split, splits, u);
+    const Prompt<F32_TOKENS> P(A, u, block, split, splits, F32_ROWS);
     if (P.row0 >= P.rows) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, n = lane & 31;
     const int row = P.row0 + 32 * wave + n, mine = min(row, P.rows - 1), tok = P.token(A, mine), head = P.hk * A.G + mine - tok * A.G;
@@ -253,14 +275,14 @@ __global__ __launch_bounds__(256, 2) void attn_prompt_f32(PrefillArgs A)
 
     l = halves_sum(l);
     if (row >= P.rows) return;
-    const float inv = A.S > 1 ? 1.f : l == 0.f ? 0.f : 1.f / l;
+    const float inv = splits > 1 ? 1.f : l == 0.f ? 0.f : 1.f / l;
     const size_t slot = ((size_t)u * A.n * A.G + row) * A.S + split;
-    float* o = A.S > 1 ? A.ws_acc + slot * D : (float*)A.out + (int64_t)P.b * A.o_sb + (int64_t)head * A.o_sh + (int64_t)tok * A.o_st;
-    const bool none = A.S == 1 && l == 0.f;
+    float* o = splits > 1 ? A.ws_acc + slot * D : (float*)A.out + (int64_t)P.b * A.o_sb + (int64_t)head * A.o_sh + (int64_t)tok * A.o_st;
+    const bool none = splits == 1 && l == 0.f;
 #pragma unroll
     for (int e = 0; e < 16; ++e)
         *(f32x4*)(o + 4 * (8 * (e >> 2) + 4 * h + (e & 3))) = none ? (f32x4){0.f, 0.f, 0.f, 0.f} : (f32x4){O[0][e], O[1][e], O[2][e], O[3][e]} * inv;
-    if (A.S > 1 && h == 0) { A.ws_m[slot] = m; A.ws_l[slot] = l; }
+    if (splits > 1 && h == 0) { A.ws_m[slot] = m; A.ws_l[slot] = l; }
 }
 
 // ---- fp32, many rows: products of bf16 parts ---------------------------------------
@@ -308,9 +330,9 @@ __device__ __forceinline__ void product3(const bf16x8 (&a)[3], const bf16x8 (&b)
 __global__ __launch_bounds__(512, 2) void attn_prompt_parts(PrefillArgs A)
 {
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    int block, split, u;
-    prompt_place(A, block, split, u);
-    const Prompt<PARTS_TOKENS> P(A, u, block, split, PARTS_ROWS);
+    int block, split, splits, u;
+    prompt_place(A, block, split, splits, u);
+    const Prompt<PARTS_TOKENS> P(A, u, block, split, splits, PARTS_ROWS);
     if (P.row0 >= P.rows) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, n = lane & 31;
     const int row = P.row0 + 32 * wave + n, mine = min(row, P.rows - 1), tok = P.token(A, mine), head = P.hk * A.G + mine - tok * A.G;
@@ -478,17 +500,17 @@ __global__ __launch_bounds__(512, 2) void attn_prompt_parts(PrefillArgs A)
 
     l = halves_sum(l);
     if (row >= P.rows) return;
-    const float inv = A.S > 1 ? 1.f : l == 0.f ? 0.f : 1.f / l;
+    const float inv = splits > 1 ? 1.f : l == 0.f ? 0.f : 1.f / l;
     const size_t slot = ((size_t)u * A.n * A.G + row) * A.S + split;
-    float* o = A.S > 1 ? A.ws_acc + slot * D : (float*)A.out + (int64_t)P.b * A.o_sb + (int64_t)head * A.o_sh + (int64_t)tok * A.o_st;
-    const bool none = A.S == 1 && l == 0.f;
+    float* o = splits > 1 ? A.ws_acc + slot * D : (float*)A.out + (int64_t)P.b * A.o_sb + (int64_t)head * A.o_sh + (int64_t)tok * A.o_st;
+    const bool none = splits == 1 && l == 0.f;
 #pragma unroll
     for (int c = 0; c < 4; ++c)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
             *(f32x4*)(o + 32 * c + 8 * e + 4 * h) =
                 none ? (f32x4){0.f, 0.f, 0.f, 0.f} : (f32x4){O[c][4 * e], O[c][4 * e + 1], O[c][4 * e + 2], O[c][4 * e + 3]} * inv;
-    if (A.S > 1 && h == 0) { A.ws_m[slot] = m; A.ws_l[slot] = l; }
+    if (splits > 1 && h == 0) { A.ws_m[slot] = m; A.ws_l[slot] = l; }
 }
 
 // ---- bf16, many rows: 64 rows a wave ------------------------------------------------
@@ -644,9 +666,9 @@ struct WideRows {
 __global__ __launch_bounds__(256, 1) void attn_prompt_wide(PrefillArgs A)
 {
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    int block, split, u;
-    prompt_place(A, block, split, u);
-    const Prompt<WIDE_TOKENS> P(A, u, block, split, WIDE_ROWS);
+    int block, split, splits, u;
+    prompt_place(A, block, split, splits, u);
+    const Prompt<WIDE_TOKENS> P(A, u, block, split, splits, WIDE_ROWS);
     if (P.row0 >= P.rows) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, n = lane & 31;
 
@@ -787,7 +809,7 @@ __global__ __launch_bounds__(256, 1) void attn_prompt_wide(PrefillArgs A)
         const float l = halves_sum(W.l[g]);
         const int row = P.row0 + 64 * wave + 32 * g + n;
         if (row >= P.rows) continue;
-        if (A.S == 1) {
+        if (splits == 1) {
             const float inv = l == 0.f ? 0.f : 1.f / l;
             bf16_t* o = (bf16_t*)A.out + (int64_t)P.b * A.o_sb + (int64_t)head[g] * A.o_sh + (int64_t)tok[g] * A.o_st;
 #pragma unroll
@@ -823,9 +845,9 @@ __global__ __launch_bounds__(256, 1) void attn_prompt_few(PrefillArgs A)
 {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     __shared__ float sm_m[4][32], sm_l[4][32];
-    int block, split, u;
-    prompt_place(A, block, split, u);
-    const Prompt<FEW_TOKENS> P(A, u, block, split, FEW_ROWS);
+    int block, split, splits, u;
+    prompt_place(A, block, split, splits, u);
+    const Prompt<FEW_TOKENS> P(A, u, block, split, splits, FEW_ROWS);
     if (P.row0 >= P.rows) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, n = lane & 31;
     const int mine = min(P.row0 + n, P.rows - 1), tok = P.token(A, mine), head = P.hk * A.G + mine - tok * A.G;
@@ -983,7 +1005,7 @@ __global__ __launch_bounds__(256, 1) void attn_prompt_few(PrefillArgs A)
             acc += park[(w * 32 + p) * FEW_PARK + r] * x;
             sum = fmaf(sm_l[w][r], x, sum);
         }
-        if (A.S == 1) {
+        if (splits == 1) {
             const int t = P.token(A, row), hd = P.hk * A.G + row - t * A.G;
             const float inv = sum == 0.f ? 0.f : 1.f / sum;
             float x[4];
@@ -999,19 +1021,20 @@ __global__ __launch_bounds__(256, 1) void attn_prompt_few(PrefillArgs A)
     }
 }
 
-// The fold of the splits' partials: 32 lanes a row, four channels each (see rows_merge).
+// The fold of the splits' partials, of the blocks that are in splits: 32 lanes a row, four channels each (see rows_merge).
 template <typename T>
 __global__ __launch_bounds__(256) void prompt_merge(PrefillArgs A)
 {
     const int p = threadIdx.x & 31;
-    const int64_t per = (int64_t)A.n * A.G, at = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), u = at / per, row = at - u * per;
+    const int64_t first = (int64_t)(A.S > PREFILL_CUTS + 1 ? 0 : A.cut[0]) * A.rows, per = (int64_t)A.n * A.G - first, x = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), u = x / per, row = x - u * per + first;
     const int b = (int)(u / A.Hkv), hk = (int)(u - (int64_t)b * A.Hkv);
     if (b >= A.B) return;
     const int fresh = min(max(A.n_dev ? A.n_dev[b] : A.n, 0), A.n);
     if (row >= (int64_t)fresh * A.G) return;
     f32x4 num;
     float sum;
-    merge_row<4>(A.ws_m + at * A.S, A.ws_l + at * A.S, A.ws_acc + at * A.S * D, A.S, 0, 1, p, num, sum);
+    const int64_t at = (u * A.n * A.G + row) * A.S;
+    merge_row<4>(A.ws_m + at, A.ws_l + at, A.ws_acc + at * D, prompt_splits(A, (int)(row / A.rows)), 0, 1, p, num, sum);
     const int tok = (int)(row / A.G), head = hk * A.G + (int)(row - (int64_t)tok * A.G);
     const float inv = 1.f / sum;
     T* o = (T*)A.out + (int64_t)b * A.o_sb + (int64_t)head * A.o_sh + (int64_t)tok * A.o_st + 4 * p;
@@ -1023,8 +1046,14 @@ __global__ __launch_bounds__(256) void prompt_merge(PrefillArgs A)
 
 hipError_t launch_prefill(int dtype, const PrefillArgs& a, hipStream_t st)
 {
-    const int64_t units = (int64_t)a.B * a.Hkv, groups = units * a.blocks * a.S;
-    if (groups > 0x7fffffff || (units * a.n * a.G + 7) / 8 > 0x7fffffff) return hipErrorInvalidValue;
+    const int64_t units = (int64_t)a.B * a.Hkv;
+    int64_t groups = units * a.blocks * a.S, merged = units * a.n * a.G;
+    if (a.S <= PREFILL_CUTS + 1) {
+        groups = units * a.blocks;
+        for (int i = 0; i < PREFILL_CUTS; ++i) groups += units * (a.blocks - a.cut[i]);
+        merged -= units * a.cut[0] * a.rows;
+    }
+    if (groups > 0x7fffffff || (merged + 7) / 8 > 0x7fffffff) return hipErrorInvalidValue;
     auto go = [&](void (*kernel)(PrefillArgs), int lds, int threads = 256) {
         const hipError_t e = allow_dynamic_lds((const void*)kernel, lds);
         if (e != hipSuccess) return e;
@@ -1037,7 +1066,7 @@ hipError_t launch_prefill(int dtype, const PrefillArgs& a, hipStream_t st)
     else if (a.rows == FEW_ROWS) e = go(attn_prompt_few, FEW_LDS);
     else e = go(attn_prompt_wide, WIDE_LDS + 16);
     if (e != hipSuccess || a.S == 1) return e;
-    const uint32_t g = (uint32_t)((units * a.n * a.G + 7) / 8);
+    const uint32_t g = (uint32_t)((merged + 7) / 8);
     if (dtype == 0) prompt_merge<float><<<g, 256, 0, st>>>(a);
     else prompt_merge<bf16_t><<<g, 256, 0, st>>>(a);
     return hipGetLastError();

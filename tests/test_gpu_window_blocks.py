@@ -68,6 +68,14 @@ KERNELS = [
     (F32, 1, 8, 2, 45, 300, 0, 0, 128, True),
     (F32, 16, 16, 8, 300, 400, 100, 5, 256, False),
     (F32, 1, 32, 8, 500, 2000, 900, 30, 256, True),
+    # few work-groups: blocks that see more are in more splits, up to eight
+    (BF, 1, 1, 1, 3000, 3100, 0, 0, 32, True),
+    (BF, 1, 8, 8, 2500, 2500, 0, 0, 256, True),
+    (F32, 1, 8, 2, 300, 300, 0, 0, 128, True),
+    (F32, 1, 8, 4, 600, 1100, 700, 9, 128, True),
+    (F32, 1, 16, 2, 700, 900, 300, 40, 256, True),
+    # ... and more than eight, the same for all
+    (BF, 1, 2, 2, 30, 5000, 0, 0, 32, True),
 ]
 
 
