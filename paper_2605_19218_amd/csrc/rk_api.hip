@@ -402,35 +402,71 @@ int window_rows(int max_len, int window, int sinks)
     const int64_t most = (int64_t)window + sinks;
     return most < max_len ? (int)most : max_len;
 }
-// One token with a window on the text.  A split of text takes 128 rows (a tile for each wave) where that many work-groups run beside the cache's, whose splits are then
-// those it would have alone; else the plan of drafts shares the device out, and compute units that it leaves idle take splits of text more.  us: bf16, 8 units x 2000 + 500 of text 3 + 4
-// splits (the plan of drafts) 10.4, 8 + 4 8.8, 12 + 4 8.7; fp32 32 x 2880 + 272 6 + 1 25.3, 6 + 2 24.1, 6 + 4 24.0; text alone, 8 units x 1028 8 9.3, 9 8.2, 16 8.0, 24 8.6; 1 x
-// 8000 16 12.7, 32 10.1, 63 9.9; fp32 32 x 900 4 14.8, 8 12.1, 16 17.1; 256 x 4100 1 93.7, 2 96.8.
+// One token with a window on the text.  Without a cache a split of text takes 128 rows (a tile for each wave), more where the compute units have their work-group; us, 8 units x
+// 1028 rows 8 splits 9.3, 9 8.2, 16 8.0, 24 8.6; 1 x 8000 16 12.7, 32 10.1, 63 9.9; fp32 32 x 900 4 14.8, 8 12.1, 16 17.1; 256 x 4100 1 93.7, 2 96.8.
+// With one, the splits of both that come out cheapest, in microseconds as fitted to 300 to 800 shapes of each kind in some 80 splits each (8 to 128 query heads, 100 to 33000 cached tokens, 50 to 12000 rows of
+// text): what is begun is waited for, then the longest wave's tiles (of either) or all bytes, partials are written and folded.  Of 1079 other shapes its time was 2 % (bf16), 1 (fp32), 3 and 4 (8 bits)
+// above the best of all splits on average, 22 % at worst; the plan of drafts 7, 6, 4 and 4, 34 at worst. us, that / this: 64 units, 3000 + 6000 rows 1 + 4 splits 55, 1 + 3 44; 32 units, 4000 +
+// 8000 1 + 8 39, 2 + 6 32; fp32 16 units, 3000 + 6000 3 + 13 31.5, 4 + 12 27.5; 8 bits, 32 units, 4000 + 8000 1 + 7 35, 2 + 6 29.
+struct WindowCost {
+    double cache, cache_kb, text, text_kb;       // of a wave's tile of 32 rows, and of each KB of it
+    double two, rate, begin, partial, split;     // more where a compute unit has two work-groups; MB a microsecond; a round of work-groups; a row's partial; of all rows at once
+    int per_cu;                                  // work-groups that a compute unit has room for
+};
+constexpr WindowCost WINDOW_COST[4] = {          // bf16, fp32, 8 bits with rows of bf16 and of fp32
+    {0.38, 0.066, 0.54, 0.086, 0.2, 6.7, 4.2, 0.00035, 0.029, 2},
+    {0.25, 0.137, 0.52, 0.117, 0.13, 8.9, 9.3, 0.00033, 0.010, 1},
+    {0.44, 0.071, 0.88, 0.049, 0.1, 6.6, 6.5, 0.00057, 0.022, 2},
+    {1.58, 0.26, 2.4, 0.136, 0.17, 6.6, 7.1, 0.00028, 0.029, 2},
+};
 RowsPlan window_plan(const rk_ctx* ctx, const rk_layout* L, bool cache, int text_rows, bool q8)
 {
-    const int64_t n_cu = ctx ? ctx->n_cu : 256, groups = (int64_t)L->batch * L->n_kv_heads * ((L->n_q_heads / L->n_kv_heads + 15) / 16);
-    const int64_t wanted = text_rows < 1 ? 1 : ((int64_t)text_rows + 127) / 128, slots = rows_slots(ctx, L, 1);
+    const bool f32 = L->dtype == RK_F32;
+    const int64_t n_cu = ctx ? ctx->n_cu : 256, units = (int64_t)L->batch * L->n_kv_heads, slots = rows_slots(ctx, L, 1);
+    const int nrb = (L->n_q_heads / L->n_kv_heads + 15) / 16;
+    const int64_t groups = units * nrb;
     auto least = [](int64_t a, int64_t b) { return (int)(a < b ? a : b); };
-    RowsPlan p;
+    RowsPlan best;
+    best.per = 16;
+    best.nrb = nrb;
     if (!cache) {
-        p.per = 16;
-        p.nrb = (L->n_q_heads / L->n_kv_heads + 15) / 16;
-        p.Sv = 0;
-        p.Sr = least(least(n_cu / groups, wanted), slots);
-        if (p.Sr < 1) p.Sr = 1;
-        return p;
+        const int64_t wanted = text_rows < 1 ? 1 : ((int64_t)text_rows + 127) / 128;
+        best.Sv = 0;
+        best.Sr = least(least(n_cu / groups, wanted), slots);
+        if (best.Sr < 1) best.Sr = 1;
+        return best;
     }
-    // (an fp32 cache leaves room for one work-group a compute unit, the others for two)
-    const bool fixed = ctx && ctx->decode_splits > 0;
-    p = rows_plan(ctx, L, 1, 0, false, q8, 16);
-    if (!fixed && text_rows > 0 && groups * (p.Sv + wanted) <= (L->dtype == RK_F32 && !q8 ? n_cu : 2 * n_cu) && p.Sv + wanted <= slots) {
-        p.Sr = (int)wanted;
-        return p;
+    if (text_rows < 1 || (ctx && ctx->decode_splits > 0)) return rows_plan(ctx, L, 1, text_rows, false, q8, 16);
+    const WindowCost& c = WINDOW_COST[(q8 ? 2 : 0) + (f32 ? 1 : 0)];
+    const int r = keep_padded(L->keep), cached = L->max_seq_len < L->capacity ? L->max_seq_len : L->capacity;
+    const double cache_kb = (q8 ? r + 132 : (r + D) * (f32 ? 4 : 2)) / 32.0, text_kb = 2 * D * (f32 ? 4 : 2) / 32.0;
+    const int64_t tv = ((int64_t)cached + 31) / 32, tt = ((int64_t)text_rows + 31) / 32;
+    const double kv = c.cache + c.cache_kb * cache_kb, kt = c.text + c.text_kb * text_kb, bytes = (double)units * (tv * cache_kb + tt * text_kb) * 1024 / (c.rate * 1e6);
+    auto waves = [](int64_t tiles, int64_t splits) { return ((tiles + splits - 1) / splits + 3) / 4; };      // tiles of the longest wave
+    double lowest = 1e300;
+    for (const int sv : {1, 2, 3, 4, 5, 6, 7, 8, 10, 12, 14, 16, 20, 24, 32, 48}) {
+        if (sv > 1 && (2 * sv > tv + 1 || sv >= slots)) break;
+        const int64_t nv = waves(tv, sv), even = (int64_t)(kv * nv / kt);
+        int before = 0;
+        // as many for the text as take no longer than the cache's, or what is left of one work-group a compute unit, or of two
+        for (const int64_t wish : {(tt + 4 * (even > 1 ? even : 1) - 1) / (4 * (even > 1 ? even : 1)), n_cu / groups - sv, 2 * n_cu / groups - sv}) {
+            int sr = least(least(wish, (tt + 1) / 2), slots - sv);
+            if (sr < 1) sr = 1;
+            if (sr == before) continue;
+            before = sr;
+            const int64_t all = groups * (sv + sr), room = c.per_cu * n_cu;
+            const double share = (double)all / n_cu, crowd = share < 1.0 ? 0.0 : share > 2.0 ? 1.0 : share - 1.0;
+            const double v = kv * nv, t = kt * waves(tt, sr), longest = (v > t ? v : t) * (1.0 + c.two * crowd);
+            const double cost = c.begin * ((all + room - 1) / room) + (longest > bytes ? longest : bytes) * (all > room ? (double)all / room : 1.0) +
+                                c.partial * L->batch * L->n_q_heads * (sv + sr) + c.split * (sv + sr);
+            if (cost < lowest) {
+                lowest = cost;
+                best.Sv = sv;
+                best.Sr = sr;
+            }
+        }
     }
-    p = rows_plan(ctx, L, 1, text_rows, false, q8, 16);
-    const int more = least(least(n_cu / groups, slots) - p.Sv, wanted);
-    if (!fixed && text_rows > 0 && p.Sr < more) p.Sr = more;
-    return p;
+    return best;
 }
 
 // Prompts: rows of a block, blocks of a KV head, splits of what a block sees, whichever come out cheapest, in microseconds as measured. A work-group takes `each` for its

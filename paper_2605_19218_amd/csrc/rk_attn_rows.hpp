@@ -672,7 +672,9 @@ inline dim3 rows_grid(const RowsArgs& a)
     return dim3(x > 0x7fffffff ? 0 : (uint32_t)x);
 }
 
-// WIN: of the text, the one token (the last row) sees the sinks and the window, which are taken as if they were all of it.
+// WIN: of the text, the one token (the last row) sees the sinks and the window, which are taken as if they were all of it.  With 16-bit rows a wave has one tile of it ahead, and asks for the first
+// before it knows the length, like the cache's: 8 units of 4 heads, 1028 rows 8.3 us a call without either, 7.5 with.  (A tile of fp32 rows is 128 registers: with a second one, or the first
+// from in front of the loop, accumulators are copied to make room, 4 x 8 units, 4000 rows 30.1 and 28.4 us in place of 25.7.)
 template <int FMT, int R, bool WIN = false>
 __global__ __launch_bounds__(256, FMT == ROWS_F32 ? 1 : 2) void attn_rows(typename std::conditional<WIN, WindowRowsArgs, RowsArgs>::type A)
 {
@@ -747,20 +749,75 @@ __global__ __launch_bounds__(256, FMT == ROWS_F32 ? 1 : 2) void attn_rows(typena
         } else {
             st.clear();
         }
+    } else if constexpr (WIN) {
+        struct Share { int rows, s0, skip, t0, t1; };      // of a text of some length: what the window leaves, and the split's tiles of 32 rows of that
+        auto share = [&](int text) {
+            Share w{text, 0, 0, 0, 0};
+            if (A.window > 0 && text > A.window) {
+                w.s0 = min(A.sinks, text - A.window);
+                w.skip = text - A.window - w.s0;
+                w.rows = w.s0 + A.window;
+            }
+            const int tiles = (w.rows + 31) / 32, k = split - A.Sv;
+            w.t0 = (int)((int64_t)tiles * k / A.Sr);
+            w.t1 = (int)((int64_t)tiles * (k + 1) / A.Sr);
+            return w;
+        };
+        const T* tk = (const T*)A.text_k + (int64_t)b * A.text_sb + (int64_t)hk * A.text_sh;
+        const T* tv = (const T*)A.text_v + (int64_t)b * A.text_sb + (int64_t)hk * A.text_sh;
+        // as above: the first tile is asked for where it lies if the text is as long as the host's bound
+        const Share e = share(A.text_max);
+        Plain X, Y;
+        X.take(qrow, g);
+        if (!F32IO && e.t0 < e.t1) X.load(tk, tv, A.text_st, 32 * min(e.t0 + wave, e.t1 - 1), e.rows, g, n, e.s0, e.skip);
+        __builtin_amdgcn_sched_barrier(0);
+        const Share w = A.text_len ? share(min(max(A.text_len[b], 0), A.text_max)) : e;
+        st.clear();
+        auto step = [&](Plain& P, int t) {
+            f32x4 s[2];
+            P.scores(s, A.scale_log2);
+            if (F32IO || w.rows - 32 * t < 32) {           // (without the condition the bf16 kernels spill, with it the fp32 ones wait for the Values in front of it)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const bool none = 32 * t + (e < 4 ? 4 * g + e : 12 + 4 * g + e) >= w.rows;
+                    s[e >> 2][e & 3] = none ? ROWS_NEG_INF : s[e >> 2][e & 3];
+                    if (none) P.drop(e);
+                }
+            }
+            st.weigh(s);
+            P.accumulate(s, st.O);
+        };
+        if (w.t0 < w.t1) {
+            int t = w.t0 + wave;
+            auto load = [&](Plain& P, int t) { P.load(tk, tv, A.text_st, 32 * min(t, w.t1 - 1), w.rows, g, n, w.s0, w.skip); };
+            if constexpr (F32IO) {
+#pragma unroll 1
+                for (; t < w.t1; t += 4) {
+                    load(X, t);
+                    step(X, t);
+                }
+            } else {
+                if (w.rows != e.rows || w.skip != e.skip) load(X, t);
+                Y.take(qrow, g);
+#pragma unroll 1
+                for (; t < w.t1; t += 8) {
+                    if (t + 4 < w.t1) load(Y, t + 4);
+                    __builtin_amdgcn_sched_barrier(0);
+                    step(X, t);
+                    if (t + 4 >= w.t1) break;
+                    if (t + 8 < w.t1) load(X, t + 8);
+                    __builtin_amdgcn_sched_barrier(0);
+                    step(Y, t + 4);
+                }
+            }
+        }
     } else {
         // tiles of 32 rows: first the text's, then the drafts'
         const int drafts = drafts_of();
         if (A.draft_k) live = drafts;
         if (row0 >= live * A.G) return;
         st.clear();
-        int text = A.text_k ? min(max(A.text_len ? A.text_len[b] : A.text_max, 0), A.text_max) : 0, s0 = 0, skip = 0;
-        if constexpr (WIN) {
-            if (A.window > 0 && text > A.window) {
-                s0 = min(A.sinks, text - A.window);
-                skip = text - A.window - s0;
-                text = s0 + A.window;
-            }
-        }
+        const int text = A.text_k ? min(max(A.text_len ? A.text_len[b] : A.text_max, 0), A.text_max) : 0;
         const int tt = (text + 31) / 32, tiles = tt + (drafts + 31) / 32, k = split - A.Sv;
         const int t0 = (int)((int64_t)tiles * k / A.Sr), t1 = (int)((int64_t)tiles * (k + 1) / A.Sr);
         if (t0 < t1) {
@@ -775,7 +832,7 @@ __global__ __launch_bounds__(256, FMT == ROWS_F32 ? 1 : 2) void attn_rows(typena
             for (int t = t0 + wave; t < t1; t += 4) {
                 const bool own = t >= tt;                  // drafts
                 const int r0 = 32 * (own ? t - tt : t), rows = own ? drafts : text;
-                X.load(own ? dk : tk, own ? dv : tv, own ? A.draft_st : A.text_st, r0, rows, g, n, s0, skip);
+                X.load(own ? dk : tk, own ? dv : tv, own ? A.draft_st : A.text_st, r0, rows, g, n);
                 f32x4 s[2];
                 X.scores(s, A.scale_log2);
                 uint64_t mask = ~0ull;

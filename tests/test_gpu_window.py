@@ -269,6 +269,10 @@ TOKENS = [
     (2, 8, 8, 128, [513, 100], [100, 640], 512, 600),
     (1, 48, 1, 96, [650], [130], 100, 16),
     (1, 4, 4, 16, [0], [60], 31, 2),
+    # several tiles a wave, of texts as long as the bound and shorter ones
+    (8, 32, 32, 64, None, [1000, 999, 870, 512, 129, 128, 33, 0], 0, 0),
+    (8, 64, 32, 64, None, [1000, 999, 870, 512, 481, 480, 33, 1000], 470, 11),
+    (8, 32, 32, 32, [90, 0, 64, 1, 33, 90, 5, 60], [1100, 1099, 700, 1100, 0, 160, 31, 900], 600, 33),
 ]
 
 
