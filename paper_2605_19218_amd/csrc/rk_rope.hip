@@ -5,12 +5,12 @@
 // The angle is needed modulo a turn, and a far position times a frequency in fp32 has lost those bits (a position of 10^6 would be off by up to 0.03 radians): the
 // product and its division by 2 pi are fp64, and what is left of a turn, within half of one, is fp32 again, where sincospi takes it.  Pairs, products and
 // sums are fp32, rounded once.
-// Eight lanes take a row, eight pairs each, in pieces of eight channels: 8 o ..+7 and n_pairs + 8 o ..+7 (or 16 o ..+15 for neighbours), so that a pair's two channels
-// are in one lane.  Sines and cosines are the same in all heads of a token: a work-group makes those of its tokens once, in LDS, and takes the tokens' heads in the order in which they
-// lie in memory.  (Made by each lane for its own pairs, a wave taking eight tokens through head after head: 50 us in place of 43 below.)
+// Pairs of halves: eight lanes take a row, eight pairs each, in pieces of eight channels, 8 o ..+7 and n_pairs + 8 o ..+7, so that a pair's two channels are in one lane; neighbours, and halves
+// that are no multiple of eight, sixteen lanes.  Sines and cosines are the same in all heads of a token: a work-group makes those of its tokens once, in LDS, and takes the tokens' heads in the
+// order in which they lie in memory.  (Made by each lane for its own pairs, a wave taking eight tokens through head after head: 50 us in place of 43 below.)
 // Bound by memory: 28 + 4 heads x 71000 tokens of bf16 270 us, 1.44 GB, 5.3 TB/s; fp32, 32 + 32 heads x 2944 tokens from memory 43 us, 193 MB, 4.5 TB/s (a copy of as many bytes 37); 28 +
-// 4 + 4 heads x 4400 tokens into segments 24 us, 116 MB, 4.8 TB/s; one token of 64 sequences x 96 heads 3.5 us. With n_pairs that is no multiple of 8 the channels read one by one cost half of the
-// rate: 40 heads x 16000 tokens with 13 pairs 114 us, 328 MB.
+// 4 + 4 heads x 4400 tokens into segments 23.5 us, 116 MB, 4.9 TB/s; one token of 64 sequences x 96 heads 3.5 us. 328 MB, 40 heads: bf16 x 16000 tokens 64 pairs 73 us, neighbours 77, 13 pairs 90 (117 with
+// the pairs' other channels read one by one), 63 99; fp32 x 8000 64, 69, 69, 72.
 #include <type_traits>
 #include "rk_kernels.hpp"
 
@@ -25,6 +25,7 @@ template <typename T> struct Piece;
 template <> struct Piece<bf16_t> {
     uint4 d;
     __device__ __forceinline__ void load(const bf16_t* p) { d = *(const uint4*)p; }
+    __device__ __forceinline__ void load_anywhere(const bf16_t* p) { __builtin_memcpy(&d, p, 16); }
     __device__ __forceinline__ void store(bf16_t* p) const { *(uint4*)p = d; }
     __device__ __forceinline__ void get(float (&x)[8]) const
     {
@@ -46,6 +47,11 @@ template <> struct Piece<bf16_t> {
 template <> struct Piece<float> {
     f32x4 a, b;
     __device__ __forceinline__ void load(const float* p) { a = *(const f32x4*)p; b = *(const f32x4*)(p + 4); }
+    __device__ __forceinline__ void load_anywhere(const float* p)
+    {
+        __builtin_memcpy(&a, p, 16);
+        __builtin_memcpy(&b, p + 4, 16);
+    }
     __device__ __forceinline__ void store(float* p) const { *(f32x4*)p = a; *(f32x4*)(p + 4) = b; }
     __device__ __forceinline__ void get(float (&x)[8]) const
     {
@@ -59,14 +65,15 @@ template <> struct Piece<float> {
     }
 };
 
-// VEC: n_pairs is a multiple of 8, so that a lane's pairs are all there or none, in two aligned pieces; else a lane has one piece (sixteen lanes a row) and reads the
-// other channels of its pairs one by one, where they are in other pieces.
+// VEC: pairs of halves, a multiple of 8, so that a lane's are all there or none, in two aligned pieces; else a lane has one piece (sixteen lanes a row): neighbours are all in it (fp32, 64 pairs,
+// 40 heads x 8000 tokens 68 us, in two pieces of sixteen channels a lane 83), the other channels of pairs of halves it reads from where they are, at any alignment.
 // A work-group takes TOKENS tokens (one, where there are fewer) through 1 << log_heads heads, a token's heads one after another, which is how a projection leaves them.
 template <typename T, bool VEC, int TOKENS>
 __global__ __launch_bounds__(TOKENS == 1 ? 1024 : 256) void rope_rows(RopeArgs A, int log_heads, int32_t* __restrict__ tickets, int apart)
 {
-    constexpr int LANES = VEC ? 8 : 16;
-    __shared__ __attribute__((aligned(16))) float cosines[TOKENS][64], sines[TOKENS][64];
+    constexpr int LANES = VEC ? 8 : 16, ANGLES = VEC ? 64 : 128;
+    // by pairs; else by channels, what its own number and the pair's other one are taken times
+    __shared__ __attribute__((aligned(16))) float cosines[TOKENS][ANGLES], sines[TOKENS][ANGLES];
     const int tid = threadIdx.x, o = tid % LANES, b = blockIdx.z, t0 = blockIdx.x * TOKENS, h0 = blockIdx.y << log_heads;
     const int nq = A.q ? A.Hq : 0, nk = A.k ? A.Hkv : 0, heads = nq + nk + (A.v ? A.Hkv : 0);
     const bool adj = A.pairing != 0;
@@ -84,8 +91,14 @@ __global__ __launch_bounds__(TOKENS == 1 ? 1024 : 256) void rope_rows(RopeArgs A
             const double turns = (double)A.pos[a * A.pos_sa + (int64_t)b * A.pos_sb + t] * (double)A.inv_freq[i] * 0.15915494309189533577;
             float s, c;
             sincospif(2.f * (float)(turns - rint(turns)), &s, &c);
-            cosines[x >> 6][i] = c;
-            sines[x >> 6][i] = A.inverse ? -s : s;
+            if (A.inverse) s = -s;
+            const int one = VEC ? i : adj ? 2 * i : i, two = adj ? 2 * i + 1 : np + i;
+            cosines[x >> 6][one] = c;
+            sines[x >> 6][one] = VEC ? s : -s;
+            if (!VEC) {
+                cosines[x >> 6][two] = c;
+                sines[x >> 6][two] = s;
+            }
         }
         __syncthreads();
         for (int r = tid / LANES; r < TOKENS << log_heads; r += blockDim.x / LANES) {
@@ -107,54 +120,53 @@ __global__ __launch_bounds__(TOKENS == 1 ? 1024 : 256) void rope_rows(RopeArgs A
             Piece<T> u, v;
             float x[8], y[8], c[8], s[8];
             if constexpr (VEC) {
-                const bool mine = turned && 8 * o < np, halves = mine && !adj;
-                u.load(from + (halves ? 8 * o : 16 * o));
-                v.load(from + (halves ? np + 8 * o : 16 * o + 8));
+                const bool mine = turned && 8 * o < np;
+                u.load(from + (mine ? 8 * o : 16 * o));
+                v.load(from + (mine ? np + 8 * o : 16 * o + 8));
                 if (mine) {
 #pragma unroll
                     for (int e = 0; e < 8; ++e) { c[e] = cosines[tl][8 * o + e]; s[e] = sines[tl][8 * o + e]; }
                     u.get(x);
                     v.get(y);
-                    if (adj) {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const float a0 = x[2 * e], a1 = x[2 * e + 1], b0 = y[2 * e], b1 = y[2 * e + 1];
-                            x[2 * e] = fmaf(a0, c[e], -a1 * s[e]);
-                            x[2 * e + 1] = fmaf(a0, s[e], a1 * c[e]);
-                            y[2 * e] = fmaf(b0, c[4 + e], -b1 * s[4 + e]);
-                            y[2 * e + 1] = fmaf(b0, s[4 + e], b1 * c[4 + e]);
-                        }
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            const float a0 = x[e], a1 = y[e];
-                            x[e] = fmaf(a0, c[e], -a1 * s[e]);
-                            y[e] = fmaf(a0, s[e], a1 * c[e]);
-                        }
+                    for (int e = 0; e < 8; ++e) {
+                        const float a0 = x[e], a1 = y[e];
+                        x[e] = fmaf(a0, c[e], -a1 * s[e]);
+                        y[e] = fmaf(a0, s[e], a1 * c[e]);
                     }
                     u.set(x);
                     v.set(y);
                 }
-                u.store(to + (halves ? 8 * o : 16 * o));
-                v.store(to + (halves ? np + 8 * o : 16 * o + 8));
+                u.store(to + (mine ? 8 * o : 16 * o));
+                v.store(to + (mine ? np + 8 * o : 16 * o + 8));
             } else {
                 u.load(from + 8 * o);
                 if (turned && 8 * o < 2 * np) {
+                    // (np is 63 at most here, so that eight from 8 o + np on end inside the row; where a half ends inside a piece, the others' are the row's first)
                     u.get(x);
+                    if (adj) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const int at = 8 * o + e, i = min(adj ? at >> 1 : at < np ? at : at - np, np - 1);
-                        c[e] = cosines[tl][i];
-                        s[e] = sines[tl][i];
-                        y[e] = adj ? x[e ^ 1] : ld_elem(from + (at < np ? at + np : at < 2 * np ? at - np : at));
+                        for (int e = 0; e < 8; ++e) y[e] = x[e ^ 1];
+                    } else {
+                        const bool first_half = 8 * o < np;
+                        v.load_anywhere(from + (first_half ? 8 * o + np : 8 * o - np));
+                        v.get(y);
+                        if (first_half && 8 * o + 8 > np) {
+                            float z[8];
+                            v.load(from);
+                            v.get(z);
+#pragma unroll
+                            for (int k = 1; k < 8; ++k)
+                                if ((np & 7) == k)
+#pragma unroll
+                                    for (int e = k; e < 8; ++e) y[e] = z[e - k];
+                        }
                     }
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const int at = 8 * o + e;
-                        const bool first = adj ? !(e & 1) : at < np;
-                        // the first of a pair: x cos - y sin; the second: y sin + x cos
-                        if (at < 2 * np) x[e] = first ? fmaf(x[e], c[e], -y[e] * s[e]) : fmaf(y[e], s[e], x[e] * c[e]);
-                    }
+                    for (int e = 0; e < 8; ++e) { c[e] = cosines[tl][8 * o + e]; s[e] = sines[tl][8 * o + e]; }
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (8 * o + e < 2 * np) x[e] = fmaf(x[e], c[e], y[e] * s[e]);
                     u.set(x);
                 }
                 u.store(to + 8 * o);
@@ -202,7 +214,7 @@ hipError_t launch_rope(int dtype, const RopeArgs& a, int32_t* tickets, int n_cu,
         return hipGetLastError();
     };
     auto by_type = [&](auto vec) { return dtype == 0 ? go(0.f, vec) : go(bf16_t{}, vec); };
-    return a.n_pairs % 8 == 0 ? by_type(std::true_type{}) : by_type(std::false_type{});
+    return a.pairing == 0 && a.n_pairs % 8 == 0 ? by_type(std::true_type{}) : by_type(std::false_type{});
 }
 
 }  // namespace rk
