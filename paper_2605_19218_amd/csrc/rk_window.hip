@@ -570,6 +570,25 @@ struct WideRows {
         }
         return fmaxf(a, b);
     }
+    // The same, for scores that came out of assembly: of those the compiler makes each maximum's operands canonical first, 12 instructions more a tile. (What it reads is long done, and so is
+    // what it writes when row_most() takes it.)
+    static __device__ __forceinline__ float max3(float a, float b, float c)
+    {
+        float d;
+        asm("v_max3_f32 %0, %1, %2, %3" : "=v"(d) : "v"(a), "v"(b), "v"(c));
+        return d;
+    }
+    static __device__ __forceinline__ float most3(const f32x16& s)
+    {
+        float a = max3(s[0], s[1], s[2]), b = max3(s[3], s[4], s[5]);
+#pragma unroll
+        for (int i = 6; i < 14; i += 4) {
+            a = max3(a, s[i], s[i + 1]);
+            b = max3(b, s[i + 2], s[i + 3]);
+        }
+        a = max3(a, s[14], s[15]);
+        return max3(a, b, b);
+    }
     // (log2 domain, of the whole row)
     __device__ __forceinline__ float row_most(float mine) const { return halves_max(mine) * c; }
     __device__ __forceinline__ bool behind(const float (&top)[2]) const { return __any(top[0] > m[0] + 8.f || top[1] > m[1] + 8.f); }
@@ -610,20 +629,16 @@ struct WideRows {
     }
     // One tile (Values at vt): scores s of it, whose largest are `top`, into O; the scores of the next tile (Keys k) into `next`, its largest into `top`; the Keys of
     // the one behind it (at kt) into k.
-    // A wave has its SIMD for itself, so what runs beside the matrix instructions is what stands between them: 32 of 32 cycles, of which the first 24 have beside them
-    // the weights, 16 pairs of 52 cycles (the exponentials 16 each), two in three instructions' time, and the last eight the maxima and beside(0..7), a load of
-    // a later stage each; LDS is read one piece a step.
-    template <typename F>
+    // A wave has its SIMD for itself, so what runs beside the matrix instructions is what stands between them: 32 of 32 cycles. Behind the first two stand the branches (what is to be hidden,
+    // maxima that move): in front of them the matrix cores would wait, WAIT_A. 24 have beside them the weights, 16 pairs of 52 cycles (the exponentials 16 each), two in three instructions'
+    // time, and the last eight the maxima and beside(0..7), a load of a later stage each; LDS is read one piece a step.
+    template <typename E, typename F>
     __device__ __forceinline__ void tile(f32x16 (&s)[2], f32x16 (&next)[2], float (&top)[2], bf16x8 (&k)[8], const char* lds, const int (&ka)[8], int kt,
-                                         const int (&va)[4], int vt, F beside)
+                                         const int (&va)[4], int vt, E edge, F beside)
     {
-        if (behind(top)) follow(top);
-        hold();
-        const float ref[2] = {m[0] > ROWS_NEG_INF ? m[0] : 0.f, m[1] > ROWS_NEG_INF ? m[1] : 0.f};
-        float sum[2][2] = {{0.f, 0.f}, {0.f, 0.f}};
+        float sum[2][2] = {{0.f, 0.f}, {0.f, 0.f}}, ref[2];
         uint32_t p[2][8];
         s16x4 v[2][4][2];
-        __builtin_amdgcn_sched_barrier(0);
         auto weigh = [&](int pair) {             // of rows' group pair / 8, tokens 2 (pair % 8) and the next
             const int g = pair >> 3, e = 2 * (pair & 7);
             s[g][e] = rows_exp2(fmaf(s[g][e], c, -ref[g]));
@@ -631,10 +646,11 @@ struct WideRows {
         };
         auto pack = [&](int pair) {
             const int g = pair >> 3, e = 2 * (pair & 7);
-            sum[g][0] += s[g][e];
-            sum[g][1] += s[g][e + 1];
-            p[g][pair & 7] = __builtin_bit_cast(uint32_t, (bf16x2){(__bf16)s[g][e], (__bf16)s[g][e + 1]});
+            const bf16x2 w = {(__bf16)s[g][e], (__bf16)s[g][e + 1]};
+            p[g][pair & 7] = __builtin_bit_cast(uint32_t, w);
+            sum[g][pair & 1] = __builtin_amdgcn_fdot2_f32_bf16(w, (bf16x2){(__bf16)1.f, (__bf16)1.f}, sum[g][pair & 1], false);
         };
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int x = 0; x < 32; ++x) {
             if (x < 16) {
@@ -649,11 +665,19 @@ struct WideRows {
                                                                   O[g][b], 0, 0, 0);
                 if (x >= 24) k[x - 24] = *(const bf16x8*)(lds + ka[x - 24] + kt);
             }
-            // pairs 2 y and 2 y + 1 in steps 3 y ..+2, each one's sums and rounding a step behind
-            if (x < 24 && x % 3 < 2) weigh(2 * (x / 3) + x % 3);
-            if (x < 25 && x % 3 == 1) pack(2 * (x / 3));
-            if (x < 25 && x % 3 == 2) pack(2 * (x / 3) + 1);
-            if (x == 26 || x == 28) top[x / 2 - 13] = most(next[x / 2 - 13]);
+            if (x == 1) {
+                edge();
+                if (behind(top)) follow(top);
+                hold();
+#pragma unroll
+                for (int g = 0; g < 2; ++g) ref[g] = m[g] > ROWS_NEG_INF ? m[g] : 0.f;
+            }
+            // pairs 2 y and 2 y + 1 in steps 4 + 3 y ..+2, each one's sums and rounding a step behind
+            const int y = x - 4;
+            if (y >= 0 && y < 24 && y % 3 < 2) weigh(2 * (y / 3) + y % 3);
+            if (y >= 0 && y < 25 && y % 3 == 1) pack(2 * (y / 3));
+            if (y >= 0 && y < 25 && y % 3 == 2) pack(2 * (y / 3) + 1);
+            if (x == 26 || x == 28) top[x / 2 - 13] = most3(next[x / 2 - 13]);
             if (x == 29 || x == 30) top[x - 29] = row_most(top[x - 29]);
             if (x >= 24) beside(x - 24);
             __builtin_amdgcn_sched_barrier(0);
@@ -773,10 +797,11 @@ __global__ __launch_bounds__(256, 1) void attn_prompt_wide(PrefillArgs A)
                 clean_values<bf16_t>(lds + next + WIDE_VALUES, WIDE_VALUES, odd, tid);
                 lds_barrier();
             }
-            if (!P.inside(j0, 32, w_lo, w_hi)) W.hide(s0, top, j0, h);
-            W.tile(s0, s1, top, k, lds, ka, next, va, now + WIDE_VALUES, [&](int x) { load(x, later); });
-            if (!P.inside(j0 + 32, 32, w_lo, w_hi)) W.hide(s1, top, j0 + 32, h);
-            W.tile(s1, s0, top, k, lds, ka, next + 32 * WIDE_ROW, va, now + WIDE_VALUES + 32 * WIDE_ROW, [](int) {});
+            W.tile(
+                s0, s1, top, k, lds, ka, next, va, now + WIDE_VALUES, [&]() { if (!P.inside(j0, 32, w_lo, w_hi)) W.hide(s0, top, j0, h); }, [&](int x) { load(x, later); });
+            W.tile(
+                s1, s0, top, k, lds, ka, next + 32 * WIDE_ROW, va, now + WIDE_VALUES + 32 * WIDE_ROW, [&]() { if (!P.inside(j0 + 32, 32, w_lo, w_hi)) W.hide(s1, top, j0 + 32, h); },
+                [](int) {});
             now = next;
         }
         stage_wait<0>();             // (what was asked for twice, at the end)
@@ -804,14 +829,16 @@ __global__ __launch_bounds__(256, 1) void attn_prompt_wide(PrefillArgs A)
         }
     }
 
+    // Rows go out through LDS, sixteen lanes a row: as they lie in the accumulators each store would be 16 bytes of 32 rows.
+    if (splits == 1) {
+        lds_barrier();               // (nobody reads a stage any more)
+        char* own = lds + wave * WIDE_STAGE;
+        int64_t* places = (int64_t*)(own + 64 * WIDE_ROW);
 #pragma unroll
-    for (int g = 0; g < 2; ++g) {
-        const float l = halves_sum(W.l[g]);
-        const int row = P.row0 + 64 * wave + 32 * g + n;
-        if (row >= P.rows) continue;
-        if (splits == 1) {
-            const float inv = l == 0.f ? 0.f : 1.f / l;
-            bf16_t* o = (bf16_t*)A.out + (int64_t)P.b * A.o_sb + (int64_t)head[g] * A.o_sh + (int64_t)tok[g] * A.o_st;
+        for (int g = 0; g < 2; ++g) {
+            const float l = halves_sum(W.l[g]), inv = l == 0.f ? 0.f : 1.f / l;
+            if (h == 0)
+                places[32 * g + n] = P.row0 + 64 * wave + 32 * g + n < P.rows ? (int64_t)P.b * A.o_sb + (int64_t)head[g] * A.o_sh + (int64_t)tok[g] * A.o_st : -1;
 #pragma unroll
             for (int c = 0; c < 4; ++c)
 #pragma unroll
@@ -819,18 +846,31 @@ __global__ __launch_bounds__(256, 1) void attn_prompt_wide(PrefillArgs A)
                     float x[4];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) x[e] = l == 0.f ? 0.f : W.O[g][c][4 * q + e] * inv;
-                    *(uint2*)(o + 32 * c + 8 * q + 4 * h) =
+                    *(uint2*)(own + (32 * g + n) * WIDE_ROW + 16 * ((4 * c + q) ^ (n & 15)) + 8 * h) =
                         make_uint2(__builtin_bit_cast(uint32_t, (bf16x2){(__bf16)x[0], (__bf16)x[1]}), __builtin_bit_cast(uint32_t, (bf16x2){(__bf16)x[2], (__bf16)x[3]}));
                 }
-        } else {
-            const size_t slot = ((size_t)u * A.n * A.G + row) * A.S + split;
-#pragma unroll
-            for (int c = 0; c < 4; ++c)
-#pragma unroll
-                for (int q = 0; q < 4; ++q)
-                    *(f32x4*)(A.ws_acc + slot * D + 32 * c + 8 * q + 4 * h) = (f32x4){W.O[g][c][4 * q], W.O[g][c][4 * q + 1], W.O[g][c][4 * q + 2], W.O[g][c][4 * q + 3]};
-            if (h == 0) { A.ws_m[slot] = W.m[g]; A.ws_l[slot] = l; }
         }
+#pragma unroll 4
+        for (int x = 0; x < 16; ++x) {
+            const int r = 4 * x + (lane >> 4);
+            const int64_t place = places[r];
+            const uint4 d = *(const uint4*)(own + r * WIDE_ROW + 16 * ((lane & 15) ^ (r & 15)));
+            if (place >= 0) *(uint4*)((bf16_t*)A.out + place + 8 * (lane & 15)) = d;
+        }
+        return;
+    }
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+        const float l = halves_sum(W.l[g]);
+        const int row = P.row0 + 64 * wave + 32 * g + n;
+        if (row >= P.rows) continue;
+        const size_t slot = ((size_t)u * A.n * A.G + row) * A.S + split;
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                *(f32x4*)(A.ws_acc + slot * D + 32 * c + 8 * q + 4 * h) = (f32x4){W.O[g][c][4 * q], W.O[g][c][4 * q + 1], W.O[g][c][4 * q + 2], W.O[g][c][4 * q + 3]};
+        if (h == 0) { A.ws_m[slot] = W.m[g]; A.ws_l[slot] = l; }
     }
 }
 
