@@ -482,6 +482,7 @@ RowsPlan window_plan(const rk_ctx* ctx, const rk_layout* L, bool cache, int text
 // alike / by length: fp32 8 units of 4 heads, 300 in 5 splits 34 / 28, 1000 89 / 71, 2 units of 8 heads, 1000 58 / 47; bf16 8 units of 1 head, 3000 in 4 56 / 47.  Where they do not, the
 // long ones have to come first, which they do with as many for all (fp32 4 units of 7 heads, 2944 in 2 363 / 385).
 constexpr int PREFILL_SPLITS_MAX = 32, PREFILL_ROWS = 1024;
+constexpr int64_t PREFILL_FAR = 1 << 24;         // elements between rows
 struct PrefillPlan { int rows, blocks, S, tokens; };      // S: splits of a block; tokens not 0: one for each so many that it sees, up to S
 // The first block of which a token may see more than `most` rows.
 int prefill_cut(int rows, int64_t G, int n, int max_len, int64_t most)
@@ -489,7 +490,7 @@ int prefill_cut(int rows, int64_t G, int n, int max_len, int64_t most)
     const int64_t token = most - ((int64_t)max_len - n);         // (the first to)
     return token <= 0 ? 0 : (int)(token * G / rows);
 }
-PrefillPlan prefill_plan(const rk_ctx* ctx, const rk_layout* L, int n, int max_len, int window, int sinks)
+PrefillPlan prefill_plan(const rk_ctx* ctx, const rk_layout* L, int n, int max_len, int window, int sinks, int64_t stride_t = D)
 {
     const int64_t units = (int64_t)L->batch * L->n_kv_heads, G = L->n_q_heads / L->n_kv_heads, n_cu = ctx ? ctx->n_cu : 256;
     PrefillPlan best{};
@@ -534,7 +535,7 @@ PrefillPlan prefill_plan(const rk_ctx* ctx, const rk_layout* L, int n, int max_l
         look(128, 32, 6.0, 4.5, 4.0);
         look(256, 32, 10.0, 4.5, 4.0);
     } else {
-        look(256, 64, 13.0, 1.65, 1.65);
+        if (stride_t < PREFILL_FAR) look(256, 64, 13.0, 1.65, 1.65);       // (its lanes' addresses are 32 bits)
         look(32, 128, 9.0, 1.35, 1.35);
     }
     return best;
@@ -1512,7 +1513,7 @@ rk_status rk_prefill_attn_window(rk_ctx* ctx, const rk_layout* L, const rk_heads
     a.len = text->len; a.max_len = text->max_len; a.n_dev = n_tokens_dev; a.n = n_tokens;
     a.B = L->batch; a.Hq = L->n_q_heads; a.Hkv = L->n_kv_heads; a.G = a.Hq / a.Hkv;
     a.window = window; a.sinks = sinks;
-    const PrefillPlan p = prefill_plan(ctx, L, n_tokens, text->max_len, window, sinks);
+    const PrefillPlan p = prefill_plan(ctx, L, n_tokens, text->max_len, window, sinks, text->stride_t);
     a.rows = p.rows; a.blocks = p.blocks; a.S = p.S;
     for (int i = 0; i < PREFILL_CUTS; ++i) a.cut[i] = i + 1 >= p.S ? p.blocks : p.tokens ? prefill_cut(p.rows, a.G, n_tokens, text->max_len, (int64_t)(i + 1) * p.tokens) : 0;
     const float sc = scale > 0.f ? scale : 1.0f / sqrtf((float)L->head_dim);

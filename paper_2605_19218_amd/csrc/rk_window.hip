@@ -83,6 +83,12 @@ __device__ __forceinline__ void load_to_lds(const void* from, uint32_t to)
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(to), "v"(from) : "m0", "memory");
 }
+// The same with the address as a sum: of the wave (from, to + step) and of the lane, 32 bits.
+template <int STEP>
+__device__ __forceinline__ void load_to_lds(const char* from, uint32_t lane_bytes, uint32_t to)
+{
+    asm volatile("s_add_u32 m0, %0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3" : : "s"(to), "i"(STEP), "v"(lane_bytes), "s"(from) : "m0", "scc", "memory");
+}
 // this wave's loads but the last N are there
 template <int N>
 __device__ __forceinline__ void stage_wait() { asm volatile("s_waitcnt vmcnt(%0)" : : "i"(N) : "memory"); }
@@ -125,6 +131,24 @@ struct Prompt {
     __device__ __forceinline__ int start(int i) const { return TOKENS * (i < few ? i : i - few + from); }
     // whether all rows from position lo to hi see rows j ..+n-1
     __device__ __forceinline__ bool inside(int j, int n, int lo, int hi) const { return j + n - 1 <= lo && (j + n - 1 < sinks || hi - j < window); }
+    // Which of the block's tiles of SIZE rows, counted through its stages, inside() says yes for, for positions lo to hi: those in front of `a`, and `n` from `b` on.
+    struct Inside {
+        int a, b, n;
+        __device__ __forceinline__ bool of(int tile) const { return tile < a || (uint32_t)(tile - b) < (uint32_t)n; }
+    };
+    template <int SIZE>
+    __device__ __forceinline__ Inside tiles_inside(int lo, int hi) const
+    {
+        constexpr int PER = TOKENS / SIZE;
+        const int whole = (lo + 1) / SIZE;       // tiles that end in front of lo's next row (none for a lo in front of row 0)
+        const int moved = PER * (from - few), first = max(hi - window + SIZE, 0) / SIZE;
+        Inside t;
+        t.a = max(min(sinks / SIZE, whole), 0);
+        if (few < from) t.a = min(t.a, PER * few);
+        t.b = max(first - moved, few < from ? PER * few : 0);
+        t.n = max(whole - moved - t.b, 0);
+        return t;
+    }
     // whether a stage is masked for some row of the block
     __device__ __forceinline__ bool edge(int j) const { return before || !inside(j, TOKENS, p_lo, p_hi); }
 };
@@ -679,7 +703,14 @@ struct WideRows {
             if (y >= 0 && y < 25 && y % 3 == 2) pack(2 * (y / 3) + 1);
             if (x == 26 || x == 28) top[x / 2 - 13] = most3(next[x / 2 - 13]);
             if (x == 29 || x == 30) top[x - 29] = row_most(top[x - 29]);
-            if (x >= 24) beside(x - 24);
+            if (x == 24) beside(std::integral_constant<int, 0>{});
+            if (x == 25) beside(std::integral_constant<int, 1>{});
+            if (x == 26) beside(std::integral_constant<int, 2>{});
+            if (x == 27) beside(std::integral_constant<int, 3>{});
+            if (x == 28) beside(std::integral_constant<int, 4>{});
+            if (x == 29) beside(std::integral_constant<int, 5>{});
+            if (x == 30) beside(std::integral_constant<int, 6>{});
+            if (x == 31) beside(std::integral_constant<int, 7>{});
             __builtin_amdgcn_sched_barrier(0);
         }
 #pragma unroll
@@ -722,41 +753,50 @@ __global__ __launch_bounds__(256, 1) void attn_prompt_wide(PrefillArgs A)
     int* odd = (int*)(lds + WIDE_LDS);
     if (P.i0 < P.i1) {
         // Rows 16 wave + 4 x + lane / 16 of a stage, x < 4: their 16-byte pieces, in the order that reading them undoes.  A lane's places in a stage are the same in all of
-        // them; in one that reaches behind the last row they repeat it.
+        // them; in one that reaches behind the last row they repeat it.  (Bytes in 32 bits: rows are less than 2^24 elements apart.)
         const uint32_t base = __builtin_amdgcn_readfirstlane(lds_address(lds)) + 16 * WIDE_ROW * wave;
-        const int64_t apart = vp - kp;
-        int64_t place[4];                // of Keys
-        int aside[4];                    // of the Values, from there
+        const int64_t step = 2 * WIDE_TOKENS * A.st, apart = (const char*)vp - (const char*)kp;
+        uint32_t place[2][4];            // of Keys, of Values
         auto places = [&](int last) {
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
-                const int token = 4 * x + (lane >> 4), slot = key_slot(token, lane & 15);
-                place[x] = (int64_t)min(16 * wave + token, last) * A.st + 8 * slot;
-                aside[x] = 8 * (value_slot(token, lane & 15) - slot);
+                const int token = 4 * x + (lane >> 4);
+                const uint32_t row = 2 * (uint32_t)min(16 * wave + token, last) * (uint32_t)A.st;
+                place[0][x] = row + 16 * key_slot(token, lane & 15);
+                place[1][x] = row + 16 * value_slot(token, lane & 15);
             }
         };
         places(WIDE_TOKENS);
-        const bf16_t* from = kp;         // the stage that is asked for
-        auto aim = [&](int i) {
-            const int j = P.start(i);
-            from = kp + (int64_t)j * A.st;
-            if (j + WIDE_TOKENS > P.len) places(P.len - 1 - j);
+        const int tail = P.len % WIDE_TOKENS ? P.few + P.len / WIDE_TOKENS - P.from : -1;        // the stage that reaches behind the last row
+        const char* from = (const char*)kp + P.start(P.i0) * (step / WIDE_TOKENS);               // the stage that is asked for: i
+        if (P.i0 == tail) places((P.len - 1) % WIDE_TOKENS);
+        auto aim = [&](int i) {          // from the one in front of it (there is none behind the last: that is asked for again)
+            if (i < P.i1) {
+                from += i == P.few ? step * (P.from - P.few + 1) : step;
+                if (i == tail) places((P.len - 1) % WIDE_TOKENS);
+            }
         };
-        auto load = [&](int piece, int buf) {
-            const int x = piece >> 1, v = piece & 1;
-            load_to_lds((v ? from + apart + aside[x] : from) + place[x], base + buf + v * WIDE_VALUES + 4 * WIDE_ROW * x);
+        auto load = [&](auto piece, int buf) {
+            constexpr int x = decltype(piece)::value >> 1, v = decltype(piece)::value & 1;
+            load_to_lds<v * WIDE_VALUES + 4 * WIDE_ROW * x>(v ? from + apart : from, place[v][x], base + buf);
         };
-        auto fetch = [&](int i, int buf) {
-            aim(i);
-#pragma unroll
-            for (int x = 0; x < 8; ++x) load(x, buf);
+        auto fetch = [&](int buf) {
+            load(std::integral_constant<int, 0>{}, buf); load(std::integral_constant<int, 1>{}, buf);
+            load(std::integral_constant<int, 2>{}, buf); load(std::integral_constant<int, 3>{}, buf);
+            load(std::integral_constant<int, 4>{}, buf); load(std::integral_constant<int, 5>{}, buf);
+            load(std::integral_constant<int, 6>{}, buf); load(std::integral_constant<int, 7>{}, buf);
         };
-#pragma unroll
-        for (int i = 0; i < 3; ++i) fetch(min(P.i0 + i, P.i1 - 1), i * WIDE_STAGE);
+        fetch(0);
+        aim(P.i0 + 1);
+        fetch(WIDE_STAGE);
+        aim(P.i0 + 2);
+        fetch(2 * WIDE_STAGE);
+        const auto whole = P.before ? typename Prompt<WIDE_TOKENS>::Inside{0, 0, 0} : P.template tiles_inside<WIDE_TOKENS>(P.p_lo, P.p_hi);      // stages that no row's edge is in
+        const auto inside = P.template tiles_inside<32>(w_lo, w_hi);
         if (tid == 0) *odd = 0;
         stage_wait<16>();
         lds_barrier();
-        if (P.edge(P.start(P.i0))) {
+        if (!whole.of(P.i0)) {
             clean_values<bf16_t>(lds + WIDE_VALUES, WIDE_VALUES, odd, tid);
             lds_barrier();
         }
@@ -780,28 +820,28 @@ __global__ __launch_bounds__(256, 1) void attn_prompt_wide(PrefillArgs A)
             top[g] = W.row_most(WideRows::most(s0[g]));
         }
         // the first tile's maxima are the running ones, with nothing to scale
-        if (!P.inside(P.start(P.i0), 32, w_lo, w_hi)) W.hide(s0, top, P.start(P.i0), h);
+        if (!inside.of(2 * P.i0)) W.hide(s0, top, P.start(P.i0), h);
 #pragma unroll
         for (int g = 0; g < 2; ++g) W.m[g] = top[g];
         int now = 0;
 #pragma unroll 1
         for (int i = P.i0; i < P.i1; ++i) {
             W.hold();
-            const int j0 = P.start(i), next = (now + WIDE_STAGE) & (4 * WIDE_STAGE - 1);
+            const int next = (now + WIDE_STAGE) & (4 * WIDE_STAGE - 1);
             // The next stage's loads are all but the last eight.  Behind the barrier it is there for all waves, and nobody reads the one before this any more.
             stage_wait<8>();
             lds_barrier();
-            aim(min(i + 3, P.i1 - 1));
+            aim(i + 3);
             const int later = (now + 3 * WIDE_STAGE) & (4 * WIDE_STAGE - 1);
-            if (i + 1 < P.i1 && P.edge(P.start(i + 1))) {
+            if (i + 1 < P.i1 && !whole.of(i + 1)) {
                 clean_values<bf16_t>(lds + next + WIDE_VALUES, WIDE_VALUES, odd, tid);
                 lds_barrier();
             }
             W.tile(
-                s0, s1, top, k, lds, ka, next, va, now + WIDE_VALUES, [&]() { if (!P.inside(j0, 32, w_lo, w_hi)) W.hide(s0, top, j0, h); }, [&](int x) { load(x, later); });
+                s0, s1, top, k, lds, ka, next, va, now + WIDE_VALUES, [&]() { if (!inside.of(2 * i)) W.hide(s0, top, P.start(i), h); }, [&](auto x) { load(x, later); });
             W.tile(
-                s1, s0, top, k, lds, ka, next + 32 * WIDE_ROW, va, now + WIDE_VALUES + 32 * WIDE_ROW, [&]() { if (!P.inside(j0 + 32, 32, w_lo, w_hi)) W.hide(s1, top, j0 + 32, h); },
-                [](int) {});
+                s1, s0, top, k, lds, ka, next + 32 * WIDE_ROW, va, now + WIDE_VALUES + 32 * WIDE_ROW, [&]() { if (!inside.of(2 * i + 1)) W.hide(s1, top, P.start(i) + 32, h); },
+                [](auto) {});
             now = next;
         }
         stage_wait<0>();             // (what was asked for twice, at the end)
