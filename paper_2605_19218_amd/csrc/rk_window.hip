@@ -565,11 +565,11 @@ struct WideRows {
             for (int i = 0; i < 8; ++i) asm volatile("" : "+a"(q[g][i]));
         }
     }
-    // a tile's 32 Keys; ka: this lane's places of its pieces
-    static __device__ __forceinline__ void keys(const char* lds, const int (&ka)[8], int at, bf16x8 (&k)[8])
+    // Piece i of a tile's 32 Keys (slots 2 i + h, permuted: key_slot); ka: where this lane's piece 0 of the stage is in LDS, `more`: the tile in it.
+    static __device__ __forceinline__ bf16x8 key(uint32_t ka, int more, int i)
     {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) k[i] = *(const bf16x8*)(lds + ka[i] + at);
+        typedef const __attribute__((address_space(3))) char* Lds;
+        return *(const __attribute__((address_space(3))) bf16x8*)((Lds)(uintptr_t)(ka ^ 32 * i) + more);
     }
     // S^T of them
     __device__ __forceinline__ void scores(const bf16x8 (&k)[8], f32x16 (&s)[2]) const
@@ -596,22 +596,15 @@ struct WideRows {
     }
     // The same, for scores that came out of assembly: of those the compiler makes each maximum's operands canonical first, 12 instructions more a tile. (What it reads is long done, and so is
     // what it writes when row_most() takes it.)
-    static __device__ __forceinline__ float max3(float a, float b, float c)
-    {
-        float d;
-        asm("v_max3_f32 %0, %1, %2, %3" : "=v"(d) : "v"(a), "v"(b), "v"(c));
-        return d;
-    }
     static __device__ __forceinline__ float most3(const f32x16& s)
     {
-        float a = max3(s[0], s[1], s[2]), b = max3(s[3], s[4], s[5]);
-#pragma unroll
-        for (int i = 6; i < 14; i += 4) {
-            a = max3(a, s[i], s[i + 1]);
-            b = max3(b, s[i + 2], s[i + 3]);
-        }
-        a = max3(a, s[14], s[15]);
-        return max3(a, b, b);
+        float a, b;
+        asm("v_max3_f32 %0, %2, %3, %4\n\tv_max3_f32 %1, %5, %6, %7\n\tv_max3_f32 %0, %0, %8, %9\n\tv_max3_f32 %1, %1, %10, %11\n\t"
+            "v_max3_f32 %0, %0, %12, %13\n\tv_max3_f32 %1, %1, %14, %15\n\tv_max3_f32 %0, %0, %16, %17\n\tv_max_f32 %0, %0, %1"
+            : "=&v"(a), "=&v"(b)
+            : "v"(s[0]), "v"(s[1]), "v"(s[2]), "v"(s[3]), "v"(s[4]), "v"(s[5]), "v"(s[6]), "v"(s[7]), "v"(s[8]), "v"(s[9]), "v"(s[10]), "v"(s[11]), "v"(s[12]), "v"(s[13]),
+              "v"(s[14]), "v"(s[15]));
+        return a;
     }
     // (log2 domain, of the whole row)
     __device__ __forceinline__ float row_most(float mine) const { return halves_max(mine) * c; }
@@ -629,11 +622,11 @@ struct WideRows {
             m[g] = m_new;
         }
     }
-    // half x of channels 32 b + lane % 32 of the tile's tokens 16 t + (4 h ..+3, 8 + 4 h ..+3); va: this lane's places of the blocks
-    static __device__ __forceinline__ s16x4 values(const char* lds, const int (&va)[4], int at, int t, int b, int x)
+    // half x of channels 32 b + lane % 32 of the tile's tokens 16 t + (4 h ..+3, 8 + 4 h ..+3); va: where this lane's place of block 0 of the stage is in LDS (see value_slot), `more`: the tile in it
+    static __device__ __forceinline__ s16x4 values(uint32_t va, int more, int t, int b, int x)
     {
-        typedef __attribute__((address_space(3))) s16x4* Lds;
-        return __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(lds + va[b] + at + (16 * t + 8 * x) * WIDE_ROW));
+        typedef __attribute__((address_space(3))) char* Lds;
+        return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)((Lds)(uintptr_t)(va ^ 64 * b) + more + (16 * t + 8 * x) * WIDE_ROW));
     }
     // a tile on an edge: what a row does not see has no score
     __device__ __forceinline__ void hide(f32x16 (&s)[2], float (&top)[2], int j0, int h) const
@@ -651,14 +644,14 @@ struct WideRows {
         if (begin) asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(s) : "v"(k), "a"(q));
         else asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(s) : "v"(k), "a"(q));
     }
-    // One tile (Values at vt): scores s of it, whose largest are `top`, into O; the scores of the next tile (Keys k) into `next`, its largest into `top`; the Keys of
-    // the one behind it (at kt) into k.
+    // One tile (vt of a stage's Values at va): scores s of it, whose largest are `top`, into O; the scores of the next tile (Keys k) into `next`, its largest into `top`; the Keys of
+    // the one behind it (kt of a stage's at ka) into k.
     // A wave has its SIMD for itself, so what runs beside the matrix instructions is what stands between them: 32 of 32 cycles. Behind the first two stand the branches (what is to be hidden,
     // maxima that move): in front of them the matrix cores would wait, WAIT_A. 24 have beside them the weights, 16 pairs of 52 cycles (the exponentials 16 each), two in three instructions'
     // time, and the last eight the maxima and beside(0..7), a load of a later stage each; LDS is read one piece a step.
     template <typename E, typename F>
-    __device__ __forceinline__ void tile(f32x16 (&s)[2], f32x16 (&next)[2], float (&top)[2], bf16x8 (&k)[8], const char* lds, const int (&ka)[8], int kt,
-                                         const int (&va)[4], int vt, E edge, F beside)
+    __device__ __forceinline__ void tile(f32x16 (&s)[2], f32x16 (&next)[2], float (&top)[2], bf16x8 (&k)[8], uint32_t ka, int kt, uint32_t va, int vt,
+                                         E edge, F beside)
     {
         float sum[2][2] = {{0.f, 0.f}, {0.f, 0.f}}, ref[2];
         uint32_t p[2][8];
@@ -680,14 +673,14 @@ struct WideRows {
             if (x < 16) {
                 const int g = x & 1, i = x >> 1;
                 score(next[g], k[i], q[g][i], i == 0);
-                v[x >> 3][(x >> 1) & 3][x & 1] = values(lds, va, vt, x >> 3, (x >> 1) & 3, x & 1);
+                v[x >> 3][(x >> 1) & 3][x & 1] = values(va, vt, x >> 3, (x >> 1) & 3, x & 1);
             } else {
                 const int g = (x >> 3) & 1, t = (x >> 2) & 1, b = x & 3;
                 const uint2 v0 = __builtin_bit_cast(uint2, v[t][b][0]), v1 = __builtin_bit_cast(uint2, v[t][b][1]);
                 O[g][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, make_uint4(v0.x, v0.y, v1.x, v1.y)),
                                                                   __builtin_bit_cast(bf16x8, make_uint4(p[g][4 * t], p[g][4 * t + 1], p[g][4 * t + 2], p[g][4 * t + 3])),
                                                                   O[g][b], 0, 0, 0);
-                if (x >= 24) k[x - 24] = *(const bf16x8*)(lds + ka[x - 24] + kt);
+                if (x >= 24) k[x - 24] = key(ka, kt, x - 24);
             }
             if (x == 1) {
                 edge();
@@ -720,7 +713,7 @@ struct WideRows {
 
 __global__ __launch_bounds__(256, 1) void attn_prompt_wide(PrefillArgs A)
 {
-    extern __shared__ __attribute__((aligned(16))) char lds[];
+    extern __shared__ __attribute__((aligned(256))) char lds[];
     int block, split, splits, u;
     prompt_place(A, block, split, splits, u);
     const Prompt<WIDE_TOKENS> P(A, u, block, split, splits, WIDE_ROWS);
@@ -800,20 +793,16 @@ __global__ __launch_bounds__(256, 1) void attn_prompt_wide(PrefillArgs A)
             clean_values<bf16_t>(lds + WIDE_VALUES, WIDE_VALUES, odd, tid);
             lds_barrier();
         }
-        int ka[8], va[4];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) ka[i] = n * WIDE_ROW + 16 * key_slot(n, 2 * i + h);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int r = 4 * h + ((lane & 15) >> 2);
-            va[i] = r * WIDE_ROW + 16 * value_slot(r, 4 * i + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) + 8 * (lane & 1);
-        }
+        const uint32_t at = lds_address(lds), vr = 4 * h + ((lane & 15) >> 2), ka = at + n * WIDE_ROW + 16 * key_slot(n, h);
+        const uint32_t va = at + WIDE_VALUES + vr * WIDE_ROW + 16 * value_slot(vr, 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) + 8 * (lane & 1);
         f32x16 s0[2], s1[2];
         bf16x8 k[8];
         float top[2];
-        WideRows::keys(lds, ka, 0, k);
+#pragma unroll
+        for (int x = 0; x < 8; ++x) k[x] = WideRows::key(ka, 0, x);
         W.scores(k, s0);
-        WideRows::keys(lds, ka, 32 * WIDE_ROW, k);
+#pragma unroll
+        for (int x = 0; x < 8; ++x) k[x] = WideRows::key(ka, 32 * WIDE_ROW, x);
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
             asm volatile("" : "+v"(s0[g]));
@@ -838,9 +827,9 @@ __global__ __launch_bounds__(256, 1) void attn_prompt_wide(PrefillArgs A)
                 lds_barrier();
             }
             W.tile(
-                s0, s1, top, k, lds, ka, next, va, now + WIDE_VALUES, [&]() { if (!inside.of(2 * i)) W.hide(s0, top, P.start(i), h); }, [&](auto x) { load(x, later); });
+                s0, s1, top, k, ka + next, 0, va + now, 0, [&]() { if (!inside.of(2 * i)) W.hide(s0, top, P.start(i), h); }, [&](auto x) { load(x, later); });
             W.tile(
-                s1, s0, top, k, lds, ka, next + 32 * WIDE_ROW, va, now + WIDE_VALUES + 32 * WIDE_ROW, [&]() { if (!inside.of(2 * i + 1)) W.hide(s1, top, P.start(i) + 32, h); },
+                s1, s0, top, k, ka + next, 32 * WIDE_ROW, va + now, 32 * WIDE_ROW, [&]() { if (!inside.of(2 * i + 1)) W.hide(s1, top, P.start(i) + 32, h); },
                 [](auto) {});
             now = next;
         }
