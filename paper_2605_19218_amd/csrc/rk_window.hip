@@ -550,9 +550,10 @@ constexpr int WIDE_LDS = 4 * WIDE_STAGE;      // and a flag
 struct WideRows {
     bf16x8 q[2][8];
     f32x16 O[2][4];
-    float m[2], l[2];
+    float m[2], l[2][2];         // running maximum, and sum in two halves
+    float ref[2], limit[2];      // by m: what weights are taken relative to, and the score (not scaled) that the maximum moves for
     Sight sight[2];
-    float c;                     // scale, log2 domain
+    float c, inv_c;              // scale, log2 domain
 
     // Accumulators and queries stay in the half of the register file that only matrix instructions read and write.
     __device__ __forceinline__ void hold()
@@ -606,20 +607,33 @@ struct WideRows {
               "v"(s[14]), "v"(s[15]));
         return a;
     }
-    // (log2 domain, of the whole row)
-    __device__ __forceinline__ float row_most(float mine) const { return halves_max(mine) * c; }
-    __device__ __forceinline__ bool behind(const float (&top)[2]) const { return __any(top[0] > m[0] + 8.f || top[1] > m[1] + 8.f); }
+    // (of the whole row)
+    static __device__ __forceinline__ float row_most(float mine)
+    {
+        const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(mine), __float_as_uint(mine), false, false);
+        float d;
+        asm("v_max_f32 %0, %1, %2" : "=v"(d) : "v"(b[0]), "v"(b[1]));      // (as halves_max(), no canonical operands)
+        return d;
+    }
+    __device__ __forceinline__ void settle(int g)
+    {
+        ref[g] = m[g] > ROWS_NEG_INF ? m[g] : 0.f;
+        limit[g] = (m[g] + 8.f) * inv_c;
+    }
+    __device__ __forceinline__ bool behind(const float (&top)[2]) const { return __any(top[0] > limit[0] || top[1] > limit[1]); }
     // the running maxima move to a tile's
     __device__ __forceinline__ void follow(const float (&top)[2])
     {
         hold();                  // (or they would be copied in front of the branch, for every tile)
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
-            const float m_new = fmaxf(m[g], top[g]), alpha = m[g] > ROWS_NEG_INF ? rows_exp2(m[g] - m_new) : 1.f;
-            l[g] *= alpha;
+            const float m_new = fmaxf(m[g], top[g] * c), alpha = m[g] > ROWS_NEG_INF ? rows_exp2(m[g] - m_new) : 1.f;
+            l[g][0] *= alpha;
+            l[g][1] *= alpha;
 #pragma unroll
             for (int b = 0; b < 4; ++b) O[g][b] *= alpha;
             m[g] = m_new;
+            settle(g);
         }
     }
     // half x of channels 32 b + lane % 32 of the tile's tokens 16 t + (4 h ..+3, 8 + 4 h ..+3); va: where this lane's place of block 0 of the stage is in LDS (see value_slot), `more`: the tile in it
@@ -653,7 +667,6 @@ struct WideRows {
     __device__ __forceinline__ void tile(f32x16 (&s)[2], f32x16 (&next)[2], float (&top)[2], bf16x8 (&k)[8], uint32_t ka, int kt, uint32_t va, int vt,
                                          E edge, F beside)
     {
-        float sum[2][2] = {{0.f, 0.f}, {0.f, 0.f}}, ref[2];
         uint32_t p[2][8];
         s16x4 v[2][4][2];
         auto weigh = [&](int pair) {             // of rows' group pair / 8, tokens 2 (pair % 8) and the next
@@ -665,7 +678,7 @@ struct WideRows {
             const int g = pair >> 3, e = 2 * (pair & 7);
             const bf16x2 w = {(__bf16)s[g][e], (__bf16)s[g][e + 1]};
             p[g][pair & 7] = __builtin_bit_cast(uint32_t, w);
-            sum[g][pair & 1] = __builtin_amdgcn_fdot2_f32_bf16(w, (bf16x2){(__bf16)1.f, (__bf16)1.f}, sum[g][pair & 1], false);
+            l[g][pair & 1] = __builtin_amdgcn_fdot2_f32_bf16(w, (bf16x2){(__bf16)1.f, (__bf16)1.f}, l[g][pair & 1], false);
         };
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -686,8 +699,6 @@ struct WideRows {
                 edge();
                 if (behind(top)) follow(top);
                 hold();
-#pragma unroll
-                for (int g = 0; g < 2; ++g) ref[g] = m[g] > ROWS_NEG_INF ? m[g] : 0.f;
             }
             // pairs 2 y and 2 y + 1 in steps 4 + 3 y ..+2, each one's sums and rounding a step behind
             const int y = x - 4;
@@ -706,8 +717,6 @@ struct WideRows {
             if (x == 31) beside(std::integral_constant<int, 7>{});
             __builtin_amdgcn_sched_barrier(0);
         }
-#pragma unroll
-        for (int g = 0; g < 2; ++g) l[g] += sum[g][0] + sum[g][1];
     }
 };
 
@@ -722,6 +731,7 @@ __global__ __launch_bounds__(256, 1) void attn_prompt_wide(PrefillArgs A)
 
     WideRows W;
     W.c = A.scale_log2;
+    W.inv_c = 1.f / W.c;
     int tok[2], head[2];
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
@@ -730,7 +740,7 @@ __global__ __launch_bounds__(256, 1) void attn_prompt_wide(PrefillArgs A)
         head[g] = P.hk * A.G + mine - tok[g] * A.G;
         W.sight[g] = Sight{P.first + tok[g], P.window, P.sinks};
         W.m[g] = ROWS_NEG_INF;
-        W.l[g] = 0.f;
+        W.l[g][0] = W.l[g][1] = 0.f;
         const bf16_t* q = (const bf16_t*)A.q + (int64_t)P.b * A.q_sb + (int64_t)head[g] * A.q_sh + (int64_t)tok[g] * A.q_st;
 #pragma unroll
         for (int i = 0; i < 8; ++i) W.q[g][i] = *(const bf16x8*)(q + 16 * i + 8 * h);
@@ -811,7 +821,10 @@ __global__ __launch_bounds__(256, 1) void attn_prompt_wide(PrefillArgs A)
         // the first tile's maxima are the running ones, with nothing to scale
         if (!inside.of(2 * P.i0)) W.hide(s0, top, P.start(P.i0), h);
 #pragma unroll
-        for (int g = 0; g < 2; ++g) W.m[g] = top[g];
+        for (int g = 0; g < 2; ++g) {
+            W.m[g] = top[g] * W.c;
+            W.settle(g);
+        }
         int now = 0;
 #pragma unroll 1
         for (int i = P.i0; i < P.i1; ++i) {
@@ -865,7 +878,7 @@ __global__ __launch_bounds__(256, 1) void attn_prompt_wide(PrefillArgs A)
         int64_t* places = (int64_t*)(own + 64 * WIDE_ROW);
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
-            const float l = halves_sum(W.l[g]), inv = l == 0.f ? 0.f : 1.f / l;
+            const float l = halves_sum(W.l[g][0] + W.l[g][1]), inv = l == 0.f ? 0.f : 1.f / l;
             if (h == 0)
                 places[32 * g + n] = P.row0 + 64 * wave + 32 * g + n < P.rows ? (int64_t)P.b * A.o_sb + (int64_t)head[g] * A.o_sh + (int64_t)tok[g] * A.o_st : -1;
 #pragma unroll
@@ -890,7 +903,7 @@ __global__ __launch_bounds__(256, 1) void attn_prompt_wide(PrefillArgs A)
     }
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
-        const float l = halves_sum(W.l[g]);
+        const float l = halves_sum(W.l[g][0] + W.l[g][1]);
         const int row = P.row0 + 64 * wave + 32 * g + n;
         if (row >= P.rows) continue;
         const size_t slot = ((size_t)u * A.n * A.G + row) * A.S + split;
