@@ -660,7 +660,7 @@ struct WideRows {
     }
     // One tile (vt of a stage's Values at va): scores s of it, whose largest are `top`, into O; the scores of the next tile (Keys k) into `next`, its largest into `top`; the Keys of
     // the one behind it (kt of a stage's at ka) into k.
-    // A wave has its SIMD for itself, so what runs beside the matrix instructions is what stands between them: 32 of 32 cycles. Behind the first two stand the branches (what is to be hidden,
+    // A wave has its SIMD for itself, so what runs beside the matrix instructions is what stands between them: 32 of 32 cycles. Behind the first stand the branches (what is to be hidden,
     // maxima that move): in front of them the matrix cores would wait, WAIT_A. 24 have beside them the weights, 16 pairs of 52 cycles (the exponentials 16 each), two in three instructions'
     // time, and the last eight the maxima and beside(0..7), a load of a later stage each; LDS is read one piece a step.
     template <typename E, typename F>
@@ -695,13 +695,13 @@ struct WideRows {
                                                                   O[g][b], 0, 0, 0);
                 if (x >= 24) k[x - 24] = key(ka, kt, x - 24);
             }
-            if (x == 1) {
+            if (x == 0) {
                 edge();
                 if (behind(top)) follow(top);
                 hold();
             }
-            // pairs 2 y and 2 y + 1 in steps 4 + 3 y ..+2, each one's sums and rounding a step behind
-            const int y = x - 4;
+            // pairs 2 y and 2 y + 1 in steps 1 + 3 y ..+2, each one's sums and rounding a step behind
+            const int y = x - 1;
             if (y >= 0 && y < 24 && y % 3 < 2) weigh(2 * (y / 3) + y % 3);
             if (y >= 0 && y < 25 && y % 3 == 1) pack(2 * (y / 3));
             if (y >= 0 && y < 25 && y % 3 == 2) pack(2 * (y / 3) + 1);
