@@ -473,11 +473,11 @@ RowsPlan window_plan(const rk_ctx* ctx, const rk_layout* L, bool cache, int text
 // beginning and end and `step` for `tokens` of what it sees; no launch is shorter than its longest work-group (`alone` of a step while compute units are to spare), nor than all of them one
 // after another on the compute units, where the last round is not full: that costs as much as a full one if they are equally long, and nothing if the short ones of a
 // causal prompt fill it. Partials are written and read.
-// us, bf16 with 32 / 256 rows a block: 8 units of 4 heads, 1 token on 1000 9.7 / 13.0, 40 on 4000 18.9 / 26.5, the same with a window of 512 12.4 / 19.3, 300 12.9 / 17.7, 700 28.2 /
-// 28.9, 1000 42.8 / 34.5, 500 on 8000 176 / 83, 1500 on 2000 with a window of 512 71 / 35; 32 units of 7 heads, 20 on 500 12.0 / 21.9, 100 18.3 / 16.0, 40 on 4000 with
-// a window of 512 24.0 / 29.6, 1000 286 / 98; 512 units of 4 heads, 4 on 500 28.8 / 46.7, 20 on 500 85.1 / 54.6.  fp32 with 128 / 256 rows: 8 units of 4 heads, 40 on 1000 with a
-// window of 512 23.3 / 25.7, 300 28.1 / 31.1, 700 67 (4 splits) / 47 (5), 1000 109 / 71, 500 on 8000 525 / 339; 32 units of 1 head, 1500 in 1, 2, 3, 4 splits 251, 193, 194, 198 /
-// 190, 132, 144, 148, 2944 591, 601 / 421, 430.  (Of 100 shapes drawn the plan's time was 2 % above the best of all rows and splits on average, 17 % at worst.)
+// us, bf16 with 32 / 256 rows a block: 8 units of 4 heads, 1 token on 1000 9.7 / 12.6, 40 on 4000 19.1 / 25.7, the same with a window of 512 12.3 / 18.8, 300 12.9 / 16.7, 700 28.3 /
+// 25.9, 1000 42.6 / 33.0, 500 on 8000 175 / 77, 1500 on 2000 with a window of 512 70 / 32; 32 units of 7 heads, 20 on 500 11.9 / 20.8, 100 18.2 / 14.4, 40 on 4000 with
+// a window of 512 24.1 / 28.6, 1000 286 / 90; 512 units of 4 heads, 4 on 500 28.9 / 46.0, 20 on 500 85.0 / 52.3.  fp32 with 128 / 256 rows: 8 units of 4 heads, 40 on 1000 with a
+// window of 512 23.2 / 25.7, 300 28.0 / 30.9, 700 67 (4 splits) / 46 (5), 1000 109 / 69, 500 on 8000 525 / 327; 32 units of 1 head, 1500 in 1, 2, 3, 4 splits 251, 193, 194, 198 /
+// 190, 128, 140, 145, 2944 587, 600 / 406, 416.  (Of 100 shapes drawn the plan's time was 2 % above the best of all rows and splits on average, 17 % at worst.)
 // Where all work-groups run at once the longest is waited for, and a block takes a split for each so many tokens that it sees: less is begun, written and folded than with as many for all blocks.  us, all
 // alike / by length: fp32 8 units of 4 heads, 300 in 5 splits 34 / 28, 1000 89 / 71, 2 units of 8 heads, 1000 58 / 47; bf16 8 units of 1 head, 3000 in 4 56 / 47.  Where they do not, the
 // long ones have to come first, which they do with as many for all (fp32 4 units of 7 heads, 2944 in 2 363 / 385).
@@ -535,7 +535,7 @@ PrefillPlan prefill_plan(const rk_ctx* ctx, const rk_layout* L, int n, int max_l
         look(128, 32, 6.0, 4.5, 4.0);
         look(256, 32, 10.0, 4.5, 4.0);
     } else {
-        if (stride_t < PREFILL_FAR) look(256, 64, 13.0, 1.65, 1.65);       // (its lanes' addresses are 32 bits)
+        if (stride_t < PREFILL_FAR) look(256, 64, 12.0, 1.55, 1.55);       // (its lanes' addresses are 32 bits)
         look(32, 128, 9.0, 1.35, 1.35);
     }
     return best;

@@ -540,9 +540,11 @@ __global__ __launch_bounds__(512, 2) void attn_prompt_parts(PrefillArgs A)
 // ---- bf16, many rows: 64 rows a wave ------------------------------------------------
 // A stage of 64 tokens, four of them in LDS: loads go there without passing through registers, two stages ahead, one barrier a stage. Rows in two groups of 32, so that a Key or Value
 // read from LDS feeds two products. (With 32 rows a wave and two waves a SIMD LDS would have to deliver 128 bytes a cycle, all it has.)
-// 28 heads x 16384 tokens, all visible 1692 to 1790 us, 1075 to 1137 TFLOP/s; with a window of 4096 820 to 858, 980 to 1030: a large matrix product reaches 1161 here. The matrix cores are busy for 46 % of the
-// cycles at 2.2 GHz, vector instructions for as many; without the exponentials, the reads of LDS, the barriers or the maxima each it is 2 to 10 % faster, so no one of them bounds it.
-// A work-group's beginning and end take 13 us, a stage 1.65.
+// 28 heads x 16384 tokens, all visible 1613 us, 1193 TFLOP/s; with a window of 4096 771 to 780, 1080 to 1090; 32 x 2944 85, 835 (a large library product reaches 1161 here). A wave has its
+// SIMD for itself and issues an instruction in 4 to 5 cycles, so their number bounds it: of some 210 a tile 32 are products of 32 cycles, 32 exponentials of 16. What took instructions away took time
+// away: loads' addresses as a wave's and a lane's part 814 -> 800, one exclusive or for each LDS address 800 -> 787, sums by pairs of rounded weights (they divide what those weights made), kept
+// over tiles like the maxima's limits, 787 -> 780; and branches beside products in place of between them 837 -> 826.
+// A work-group's beginning and end take 12 us, a stage 1.55.
 // In LDS a token's row is its 256 bytes, slots permuted as key_slot() and value_slot() say: what a load leaves is lane by lane, so it is the lanes' addresses that are permuted.
 constexpr int WIDE_ROWS = 256, WIDE_TOKENS = 64, WIDE_ROW = 256, WIDE_VALUES = WIDE_TOKENS * WIDE_ROW, WIDE_STAGE = 2 * WIDE_VALUES;
 constexpr int WIDE_LDS = 4 * WIDE_STAGE;      // and a flag
@@ -661,7 +663,7 @@ struct WideRows {
     // One tile (vt of a stage's Values at va): scores s of it, whose largest are `top`, into O; the scores of the next tile (Keys k) into `next`, its largest into `top`; the Keys of
     // the one behind it (kt of a stage's at ka) into k.
     // A wave has its SIMD for itself, so what runs beside the matrix instructions is what stands between them: 32 of 32 cycles. Behind the first stand the branches (what is to be hidden,
-    // maxima that move): in front of them the matrix cores would wait, WAIT_A. 24 have beside them the weights, 16 pairs of 52 cycles (the exponentials 16 each), two in three instructions'
+    // maxima that move): in front of them the matrix cores would wait. 24 have beside them the weights, 16 pairs of 52 cycles (the exponentials 16 each), two in three instructions'
     // time, and the last eight the maxima and beside(0..7), a load of a later stage each; LDS is read one piece a step.
     template <typename E, typename F>
     __device__ __forceinline__ void tile(f32x16 (&s)[2], f32x16 (&next)[2], float (&top)[2], bf16x8 (&k)[8], uint32_t ka, int kt, uint32_t va, int vt,
