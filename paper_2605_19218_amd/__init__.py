@@ -292,21 +292,27 @@ class Drafts:
         return rk_drafts(_ptr(self.k), _ptr(self.v), st[0], st[1], st[2], self.n_tokens, _ptr(self.n_tokens_dev), _ptr(self.mask))
 
 
-@dataclass
+@dataclass(frozen=True)
 class Heads:
-    """Rows of a [B, H, N, d] tensor-like (any strides, channels contiguous): queries, Keys, Values or a result."""
+    """Rows of a [B, H, N, d] tensor-like (any strides, channels contiguous): queries, Keys, Values or a result.  The strides are the data's when this
+    is made; it can serve many calls."""
     data: Any
     strides: Optional[tuple] = None      # (stride_b, stride_h, stride_t) in elements
+
+    def __post_init__(self):
+        if self.strides is None and hasattr(self.data, "stride"):
+            object.__setattr__(self, "strides", tuple(self.data.stride()[:3]))
 
     def c(self) -> rk_heads:
         st = self.strides if self.strides is not None else tuple(self.data.stride()[:3])
         return rk_heads(_ptr(self.data), st[0], st[1], st[2])
 
 
-@dataclass
+@dataclass(frozen=True)
 class Rope:
     """Positions of several axes: pos int32 [n_axes, B, N] (tokens contiguous), inv_freq fp32 [n_pairs] (both device); axis: the axis of each
-    pair (default: axis 0 for all of inv_freq)."""
+    pair (default: axis 0 for all of inv_freq).  As Heads: made once, it can serve many calls, also where what pos holds changes; for another pos,
+    dataclasses.replace(rope, pos=other, strides=None, n_axes=None)."""
     pos: Any
     inv_freq: Any
     axis: Optional[Any] = None           # n_pairs ints, < n_axes (kept as bytes)
@@ -315,17 +321,24 @@ class Rope:
     strides: Optional[tuple] = None      # (stride_a, stride_b) of pos in elements
 
     def __post_init__(self):
-        axis = [int(a) for a in self.axis] if self.axis is not None else [0] * int(self.inv_freq.numel())
-        if len(axis) > RK_MAX_PAIRS or any(not 0 <= a < 256 for a in axis):
-            raise ValueError(f"axis: of at most {RK_MAX_PAIRS} pairs, each in 0..{RK_MAX_AXES - 1}")
-        self.axis = bytes(axis)
+        axis = self.axis
+        if not isinstance(axis, bytes):
+            axis = [int(a) for a in axis] if axis is not None else [0] * int(self.inv_freq.numel())
+            if any(not 0 <= a < 256 for a in axis):
+                raise ValueError(f"axis: each in 0..{RK_MAX_AXES - 1}")
+        if len(axis) > RK_MAX_PAIRS:
+            raise ValueError(f"axis: of at most {RK_MAX_PAIRS} pairs")
+        object.__setattr__(self, "axis", bytes(axis))
+        if self.strides is None and hasattr(self.pos, "stride"):
+            object.__setattr__(self, "strides", tuple(self.pos.stride()[:2]))
+        if self.n_axes is None and hasattr(self.pos, "shape"):
+            object.__setattr__(self, "n_axes", int(self.pos.shape[0]))
 
     def c(self) -> rk_rotary:
         st = self.strides if self.strides is not None else tuple(self.pos.stride()[:2])
         axes = self.n_axes if self.n_axes is not None else int(self.pos.shape[0])
-        axis = list(self.axis)
-        return rk_rotary(_ptr(self.pos), st[0], st[1], _ptr(self.inv_freq), axes, len(axis), int(self.pairing),
-                         (C.c_uint8 * RK_MAX_PAIRS)(*axis))
+        return rk_rotary(_ptr(self.pos), st[0], st[1], _ptr(self.inv_freq), axes, len(self.axis), int(self.pairing),
+                         (C.c_uint8 * RK_MAX_PAIRS)(*self.axis))
 
 
 # ---- the ABI, same names -----------------------------------------------------

@@ -217,6 +217,19 @@ bool rows(PyObject* o, rk_rows* r)
     r->stride_t = st[2];
     return true;
 }
+// the n elements of the tuple that attribute `name` is
+bool tuple_of(PyObject* o, PyObject* name, int n, int64_t* out)
+{
+    PyObject* t = PyObject_GetAttr(o, name);
+    bool ok = t && PyTuple_Check(t) && PyTuple_GET_SIZE(t) == n;
+    for (int i = 0; ok && i < n; ++i) {
+        long long x;
+        ok = integer(PyTuple_GET_ITEM(t, i), &x);
+        out[i] = x;
+    }
+    Py_XDECREF(t);
+    return ok;
+}
 // *at: out, or null for None
 bool heads(PyObject* o, rk_heads* out, const rk_heads** at)
 {
@@ -225,13 +238,7 @@ bool heads(PyObject* o, rk_heads* out, const rk_heads** at)
     if (!heads_type || Py_TYPE(o) != heads_type) return false;
     void* data = nullptr;
     int64_t st[3];
-    if (!address_of(o, s_data, &data)) return false;
-    PyObject* key = PyObject_GetAttr(o, s_data);
-    PyObject* given = key ? PyObject_GetAttr(o, s_strides) : nullptr;
-    const bool ok = given && strides_of(given, key, st);
-    Py_XDECREF(given);
-    Py_XDECREF(key);
-    if (!ok) return false;
+    if (!address_of(o, s_data, &data) || !tuple_of(o, s_strides, 3, st)) return false;
     out->data = data;
     out->stride_b = st[0];
     out->stride_h = st[1];
@@ -239,37 +246,26 @@ bool heads(PyObject* o, rk_heads* out, const rk_heads** at)
     *at = out;
     return true;
 }
-// axes as bytes (what Rope makes of them), and neither strides nor a count of axes given
+// axes, strides and their number as Rope makes them
 bool rotary(PyObject* o, rk_rotary* r)
 {
     if (!rope_type || Py_TYPE(o) != rope_type) return false;
     void *pos = nullptr, *freq = nullptr;
-    if (!address_of(o, s_pos, &pos) || !address_of(o, s_inv_freq, &freq) || !int32_of(o, s_pairing, &r->pairing)) return false;
+    int64_t st[2];
+    if (!address_of(o, s_pos, &pos) || !address_of(o, s_inv_freq, &freq) || !int32_of(o, s_pairing, &r->pairing) || !int32_of(o, s_n_axes, &r->n_axes) ||
+        !tuple_of(o, s_strides, 2, st))
+        return false;
     PyObject* axis = PyObject_GetAttr(o, s_axis);
-    PyObject* given = axis ? PyObject_GetAttr(o, s_strides) : nullptr;
-    PyObject* count = given ? PyObject_GetAttr(o, s_n_axes) : nullptr;
-    PyObject* key = count ? PyObject_GetAttr(o, s_pos) : nullptr;
-    bool ok = key && PyBytes_CheckExact(axis) && PyBytes_GET_SIZE(axis) <= RK_MAX_PAIRS && given == Py_None && count == Py_None;
-    long long st[2] = {0, 0}, axes = 0;
+    const bool ok = axis && PyBytes_CheckExact(axis) && PyBytes_GET_SIZE(axis) <= RK_MAX_PAIRS;
     if (ok) {
         r->n_pairs = (int32_t)PyBytes_GET_SIZE(axis);
         for (int i = 0; i < RK_MAX_PAIRS; ++i) r->axis[i] = i < r->n_pairs ? (uint8_t)PyBytes_AS_STRING(axis)[i] : 0;
-        PyObject* t = PyObject_CallMethodNoArgs(key, s_stride);
-        PyObject* shape = t ? PyObject_GetAttr(key, s_shape) : nullptr;
-        ok = shape && PyTuple_Check(t) && PyTuple_GET_SIZE(t) >= 2 && integer(PyTuple_GET_ITEM(t, 0), st) && integer(PyTuple_GET_ITEM(t, 1), st + 1) &&
-             PyTuple_Check(shape) && PyTuple_GET_SIZE(shape) >= 1 && integer(PyTuple_GET_ITEM(shape, 0), &axes) && axes >= 0 && axes <= INT32_MAX;
-        Py_XDECREF(shape);
-        Py_XDECREF(t);
     }
-    Py_XDECREF(key);
-    Py_XDECREF(count);
-    Py_XDECREF(given);
     Py_XDECREF(axis);
     r->pos = (const int32_t*)pos;
     r->inv_freq = (const float*)freq;
     r->stride_a = st[0];
     r->stride_b = st[1];
-    r->n_axes = (int32_t)axes;
     return ok;
 }
 bool int32_arg(PyObject* o, int32_t* out)

@@ -1,5 +1,6 @@
 """The calls of positions and windows marshalled in C hand the library what the ctypes path hands it, or leave the call to it."""
 import ctypes as C
+import dataclasses
 import types
 
 import pytest
@@ -106,6 +107,7 @@ def test_same_arguments(paths, name):
              (dict(h=heads(data=1 << 40, strides=(16, 8, 8)), txt=text(strides=(9, 8, 7), capacity=40), count=1 << 41, kv=1 << 42, ints=(0, 0)),
               {"stream": types.SimpleNamespace(cuda_stream=321)}),
              (dict(rp=rope(pos=tensor(2, B, 9, dtype=torch.int32)[:, :, :N], axis=[1] * 64), ctx=None, ws=DROP), {"workspace_bytes": 0} if attn else {}),
+             (dict(rp=rope(strides=(6, 3), n_axes=3)), {}),
              (dict(ws=1 << 40), {"workspace_bytes": 99} if attn else {})]
     for form, kw in forms:
         args, more = call(name, **form)
@@ -123,7 +125,7 @@ def test_other_forms_go_to_ctypes(paths, name):
     if "decode" not in name:
         forms += [dict(h=heads(cls=OtherHeads)), dict(h=heads(strides=[1, 2, 3])), dict(n=True)]
     if "rope" in name:
-        forms += [dict(rp=rope(strides=(6, 3))), dict(rp=rope(n_axes=3))]
+        forms += [dict(rp=rope(strides=[6, 3])), dict(rp=rope(n_axes=True))]
     if "append" in name or "attn" in name:
         forms += [dict(txt=text(strides=[1, 2, 3]))]
     if "attn" in name:
@@ -134,10 +136,23 @@ def test_other_forms_go_to_ctypes(paths, name):
 
 
 def test_axes_are_bytes():
-    assert rope().axis == bytes([0, 1, 2, 2, 0]) and rope(axis=None).axis == bytes(5)
-    r = rope()
-    r.axis = [2, 1]                              # later assignments are served by ctypes
+    assert rope().axis == bytes([0, 1, 2, 2, 0]) and rope(axis=None).axis == bytes(5) and rope(axis=bytes([2, 1])).axis == bytes([2, 1])
+    r = dataclasses.replace(rope(), axis=[2, 1])
     assert list(r.c().axis)[:3] == [2, 1, 0] and r.c().n_pairs == 2
+    for axis in ([256], [-1], [0] * 65, bytes(65)):
+        with pytest.raises(ValueError):
+            rope(axis=axis)
+
+
+def test_what_is_made_stays():
+    """Strides belong to the data they were taken from: both are given once."""
+    h, r = heads(), rope()
+    assert h.strides == tuple(h.data.stride()[:3]) and r.strides == tuple(r.pos.stride()[:2]) and r.n_axes == 3
+    for x, name in ((h, "data"), (h, "strides"), (r, "pos"), (r, "axis")):
+        with pytest.raises(dataclasses.FrozenInstanceError):
+            setattr(x, name, None)
+    other = dataclasses.replace(r, pos=tensor(4, B, 2 * N, dtype=torch.int32), strides=None, n_axes=None)
+    assert other.strides == (2 * N * B, 2 * N) and other.n_axes == 4 and other.axis == r.axis
 
 
 @pytest.mark.parametrize("name", list(SIGNATURES))
