@@ -630,22 +630,28 @@ __device__ __forceinline__ float partial_weight(float m, float l, float M)
 }
 
 // Partials first, first + step, ... of the S of a row, by 32 lanes with four channels each: sum l_i w_i and sum acc_i w_i, w_i = 2^(m_i - M), M the maximum
-// of all S.  MC (up to eight) partials' loads at once.
+// of all S.  MC (up to eight) partials' loads at once, the first of them beside those of the maxima, which are a round trip of their own.
 template <int MC>
 __device__ __forceinline__ void merge_row(const float* m, const float* l, const float* acc, int S, int first, int step, int p, f32x4& num, float& sum)
 {
+    f32x4 av[MC];
+    float mv, lv;
+    auto load = [&](int i0) {
+#pragma unroll
+        for (int k = 0; k < MC; ++k) av[k] = *(const f32x4*)(acc + (size_t)min(i0 + k * step, S - 1) * D + 4 * p);
+        const int mine = i0 + (p & 7) * step, at = min(mine, S - 1);       // lane k of each eight: partial k's weight
+        mv = m[at];
+        lv = l[at];
+        if ((p & 7) >= MC || mine >= S) lv = 0.f;
+    };
+    load(first);
     float M = ROWS_NEG_INF;
     for (int i = p; i < S; i += 32) M = fmaxf(M, m[i]);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o));
     num = (f32x4){0.f, 0.f, 0.f, 0.f};
     sum = 0.f;
-    for (int i0 = first; i0 < S; i0 += MC * step) {
-        f32x4 av[MC];
-#pragma unroll
-        for (int k = 0; k < MC; ++k) av[k] = *(const f32x4*)(acc + (size_t)min(i0 + k * step, S - 1) * D + 4 * p);
-        const int mine = i0 + (p & 7) * step, at = min(mine, S - 1);       // lane k of each eight: partial k's weight
-        const float mv = m[at], lv = (p & 7) < MC && mine < S ? l[at] : 0.f;
+    for (int i0 = first; i0 < S;) {
         const float w = partial_weight(mv, lv, M), lw = lv * w;
 #pragma unroll
         for (int k = 0; k < MC; ++k) {
@@ -653,6 +659,8 @@ __device__ __forceinline__ void merge_row(const float* m, const float* l, const 
             const float wk = __shfl(w, k, 8);
             if (i0 + k * step < S) num += av[k] * wk;
         }
+        i0 += MC * step;
+        if (i0 < S) load(i0);
     }
 }
 
