@@ -78,16 +78,20 @@ __device__ __forceinline__ void prompt_place(const PrefillArgs& A, int& block, i
 
 __device__ __forceinline__ uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)p; }
 // 16 bytes a lane from `from` to LDS at `to` (of the wave) + 16 lane. (Not the builtin: behind it every read of LDS waits for all loads.) What is asked for
-// is there after stage_wait().
+// is there after stage_wait(). (What is the wave's has to be said where code is not optimised.)
 __device__ __forceinline__ void load_to_lds(const void* from, uint32_t to)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(to), "v"(from) : "m0", "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(from) : "m0", "memory");
 }
 // The same with the address as a sum: of the wave (from, to + step) and of the lane, 32 bits.
 template <int STEP>
 __device__ __forceinline__ void load_to_lds(const char* from, uint32_t lane_bytes, uint32_t to)
 {
+#ifdef __OPTIMIZE__
     asm volatile("s_add_u32 m0, %0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3" : : "s"(to), "i"(STEP), "v"(lane_bytes), "s"(from) : "m0", "scc", "memory");
+#else                            // (a wave's address is in no scalar register then)
+    load_to_lds(from + lane_bytes, to + STEP);
+#endif
 }
 // this wave's loads but the last N are there
 template <int N>
