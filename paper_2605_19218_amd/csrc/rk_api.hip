@@ -562,15 +562,19 @@ rk_status check_heads(rk_ctx* ctx, const rk_heads* x, const char* name)
         return fail(ctx, RK_ERR_INVALID_ARG, "%s: strides must be non-negative multiples of 8 elements", name);
     return RK_OK;
 }
-// Elements from the first to one behind the last of B x H x n rows.
-int64_t heads_span(int64_t sb, int64_t sh, int64_t st, int B, int H, int n) { return (B - 1) * sb + (H - 1) * sh + (int64_t)(n - 1) * st + D; }
+// Bytes from the first to the end of the last of B x H x n rows (strides are the caller's: more than 2^62 bytes are 2^62).
+size_t heads_bytes(int64_t sb, int64_t sh, int64_t st, int B, int H, int n, size_t es)
+{
+    const __int128 bytes = ((__int128)(B - 1) * sb + (__int128)(H - 1) * sh + (__int128)(n - 1) * st + D) * es;
+    return bytes < (__int128)1 << 62 ? (size_t)bytes : (size_t)1 << 62;
+}
 
 // Of a result: whether each row has elements of its own.  Sorted by their strides, each axis has to step over all that the axes below it cover (an
 // axis of one does not step); heads of a projection's rows lie so.
 bool rows_apart(const rk_heads* x, int B, int H, int n)
 {
-    int64_t st[3] = {x->stride_b, x->stride_h, x->stride_t}, count[3] = {B, H, n};
-    int64_t covered = D;
+    const int64_t st[3] = {x->stride_b, x->stride_h, x->stride_t}, count[3] = {B, H, n};
+    __int128 covered = D;
     bool done[3] = {B == 1, H == 1, n == 1};
     for (int k = 0; k < 3; ++k) {
         int at = -1;
@@ -578,7 +582,7 @@ bool rows_apart(const rk_heads* x, int B, int H, int n)
             if (!done[i] && (at < 0 || st[i] < st[at])) at = i;
         if (at < 0) return true;
         if (st[at] < covered) return false;
-        covered += (count[at] - 1) * st[at];
+        covered += (__int128)(count[at] - 1) * st[at];
         done[at] = true;
     }
     return true;
@@ -1444,9 +1448,9 @@ rk_status rk_rope_append_text(rk_ctx* ctx, const rk_layout* L, const rk_rotary* 
         return fail(ctx, RK_ERR_CAPACITY, "rope_append_text: %d + %d rows exceed capacity %d", text->max_len, n_tokens, text->capacity);
     // rows written by one work-group may be read by another: the segment's rows and the sources lie apart
     const size_t es = elem_size(L->dtype);
-    const size_t tb = heads_span(text->stride_b, text->stride_h, text->stride_t, L->batch, L->n_kv_heads, text->capacity) * es;
+    const size_t tb = heads_bytes(text->stride_b, text->stride_h, text->stride_t, L->batch, L->n_kv_heads, text->capacity, es);
     for (const rk_heads* x : {k, v}) {
-        const size_t xb = heads_span(x->stride_b, x->stride_h, x->stride_t, L->batch, L->n_kv_heads, n_tokens) * es;
+        const size_t xb = heads_bytes(x->stride_b, x->stride_h, x->stride_t, L->batch, L->n_kv_heads, n_tokens, es);
         if (ranges_meet(text->k, tb, x->data, xb) || ranges_meet(text->v, tb, x->data, xb))
             return fail(ctx, RK_ERR_INVALID_ARG, "rope_append_text: text segment and new rows overlap in memory");
     }

@@ -84,6 +84,9 @@ def test_rope_append_text(ctx):
     assert call(t=text(max_len=2 ** 31 - 1, capacity=2 ** 31 - 1)) == CAP
     assert call(k=heads(2, data=P + 128)) == BAD and call(v=heads(2, data=P + 128)) == BAD      # over the segment
     assert call(qo=heads(8, strides=(0, 0, 128))) == BAD and call(r=rope(n_axes=9)) == BAD
+    # strides whose products pass 64 bits: the stretch still meets the segment, and rows do not lie apart for it
+    assert call(n=5, k=heads(2, data=P - 4096, strides=(0, 0, 1 << 62))) == BAD and call(n=5, k=heads(2, strides=(0, 0, 1 << 62))) == NONE
+    assert call(qo=heads(8, strides=(1 << 62, 1 << 61, 128))) == BAD and call(qo=heads(8, strides=((1 << 63) - 8, 1 << 59, 128))) == NONE
     # the lengths that come out may lie over those that go in, not over the counts that every work-group reads
     assert call(n_tokens_dev=FAR) == NONE and call(n_tokens_dev=FAR, out=FAR) == BAD
 
