@@ -103,6 +103,15 @@ hipError_t launch_window_rows_q8_f32(const WindowRowsArgs& a, hipStream_t st);
 
 // ---- rk_window.hip: new tokens over the text segment ------------------------------
 constexpr int PREFILL_CUTS = 7;
+// Divides numbers below 2^31 by a number that the host knows: x / d = x m >> (31 + s), m = floor(2^(31 + s) / d) + 1, 2^s >= d (the product is too large by x / 2^31 of a d at
+// most).  A division proper is some 20 instructions, each waiting for the one before.
+struct Divisor { uint32_t m, s; };
+inline Divisor divisor(uint32_t d)
+{
+    uint32_t s = 0;
+    while ((1ull << s) < d) ++s;
+    return Divisor{(uint32_t)((1ull << (31 + s)) / d + 1), s};
+}
 struct PrefillArgs {
     const void* q;
     void* out;
@@ -115,6 +124,7 @@ struct PrefillArgs {
     int32_t window, sinks;
     int32_t rows, blocks, S;     // rows of a block: 128 or 256 (fp32), 256 or 32 (bf16); blocks of a KV head; splits of what a block sees, at most
     int32_t cut[PREFILL_CUTS];   // blocks from cut[i] on are in i + 2 splits or more; with more than PREFILL_CUTS + 1 all blocks are in S
+    Divisor by_units, by_hkv, by_g, by_merged;    // B Hkv; Hkv; G; rows of a KV head that are in splits
     float scale_log2;
     float *ws_m, *ws_l, *ws_acc; // [B, Hkv, n G, S] and [.., S, d]
 };

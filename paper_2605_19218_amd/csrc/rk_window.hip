@@ -44,6 +44,8 @@ struct Sight {
     }
 };
 
+__device__ __forceinline__ uint32_t over(uint32_t x, const Divisor& d) { return (uint32_t)((uint64_t)x * d.m >> (31 + d.s)); }
+
 // The splits of a block.
 __device__ __forceinline__ int prompt_splits(const PrefillArgs& A, int block)
 {
@@ -57,7 +59,7 @@ __device__ __forceinline__ int prompt_splits(const PrefillArgs& A, int block)
 // work-groups go to the same XCDs, which read its Keys and Values from their L2.  (No branches: with one the wide kernel spills.)
 __device__ __forceinline__ void prompt_place(const PrefillArgs& A, int& block, int& split, int& splits, int& u)
 {
-    const uint32_t units = A.B * A.Hkv, rank = blockIdx.x / units;
+    const uint32_t units = A.B * A.Hkv, rank = over(blockIdx.x, A.by_units);
     u = blockIdx.x - rank * units;
     int at = (int)rank, end = A.blocks;          // rank among the blocks in front of `end`
     bool found = A.S > PREFILL_CUTS + 1;
@@ -105,7 +107,7 @@ struct Prompt {
     bool before;                 // some of the rows stand in front of row 0
     __device__ __forceinline__ Prompt(const PrefillArgs& A, int u, int block, int split, int splits, int size)
     {
-        b = u / A.Hkv;
+        b = over(u, A.by_hkv);
         hk = u - b * A.Hkv;
         len = min(max(A.len ? A.len[b] : A.max_len, 0), A.max_len);
         const int fresh = min(max(A.n_dev ? A.n_dev[b] : A.n, 0), A.n);
@@ -131,7 +133,7 @@ struct Prompt {
         i0 = (int)((uint32_t)stages * (uint32_t)split / (uint32_t)splits);
         i1 = (int)((uint32_t)stages * (uint32_t)(split + 1) / (uint32_t)splits);
     }
-    __device__ __forceinline__ int token(const PrefillArgs& A, int r) const { return (int)((uint32_t)min(r, rows - 1) / (uint32_t)A.G); }
+    __device__ __forceinline__ int token(const PrefillArgs& A, int r) const { return (int)over(min(r, rows - 1), A.by_g); }
     __device__ __forceinline__ int start(int i) const { return TOKENS * (i < few ? i : i - few + from); }
     // whether all rows from position lo to hi see rows j ..+n-1
     __device__ __forceinline__ bool inside(int j, int n, int lo, int hi) const { return j + n - 1 <= lo && (j + n - 1 < sinks || hi - j < window); }
@@ -1114,16 +1116,18 @@ template <typename T>
 __global__ __launch_bounds__(256) void prompt_merge(PrefillArgs A)
 {
     const int p = threadIdx.x & 31;
-    const int64_t first = (int64_t)(A.S > PREFILL_CUTS + 1 ? 0 : A.cut[0]) * A.rows, per = (int64_t)A.n * A.G - first, x = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), u = x / per, row = x - u * per + first;
-    const int b = (int)(u / A.Hkv), hk = (int)(u - (int64_t)b * A.Hkv);
+    // (all of these are below 2^31)
+    const uint32_t first = (A.S > PREFILL_CUTS + 1 ? 0 : A.cut[0]) * A.rows, all = (uint32_t)A.n * A.G, x = blockIdx.x * 8 + (threadIdx.x >> 5), u = over(x, A.by_merged),
+                   row = x - u * (all - first) + first;
+    const int b = (int)over(u, A.by_hkv), hk = (int)u - b * A.Hkv;
     if (b >= A.B) return;
     const int fresh = min(max(A.n_dev ? A.n_dev[b] : A.n, 0), A.n);
-    if (row >= (int64_t)fresh * A.G) return;
+    if (row >= (uint32_t)fresh * A.G) return;
     f32x4 num;
     float sum;
-    const int64_t at = (u * A.n * A.G + row) * A.S;
-    merge_row<4>(A.ws_m + at, A.ws_l + at, A.ws_acc + at * D, prompt_splits(A, (int)(row / A.rows)), 0, 1, p, num, sum);
-    const int tok = (int)(row / A.G), head = hk * A.G + (int)(row - (int64_t)tok * A.G);
+    const int64_t at = ((int64_t)u * all + row) * A.S;
+    merge_row<4>(A.ws_m + at, A.ws_l + at, A.ws_acc + at * D, prompt_splits(A, (int)(row >> __builtin_ctz(A.rows))), 0, 1, p, num, sum);
+    const int tok = (int)over(row, A.by_g), head = hk * A.G + (int)row - tok * A.G;
     const float inv = 1.f / sum;
     T* o = (T*)A.out + (int64_t)b * A.o_sb + (int64_t)head * A.o_sh + (int64_t)tok * A.o_st + 4 * p;
 #pragma unroll
@@ -1132,8 +1136,9 @@ __global__ __launch_bounds__(256) void prompt_merge(PrefillArgs A)
 
 }  // namespace
 
-hipError_t launch_prefill(int dtype, const PrefillArgs& a, hipStream_t st)
+hipError_t launch_prefill(int dtype, const PrefillArgs& args, hipStream_t st)
 {
+    PrefillArgs a = args;
     const int64_t units = (int64_t)a.B * a.Hkv;
     int64_t groups = units * a.blocks * a.S, merged = units * a.n * a.G;
     if (a.S <= PREFILL_CUTS + 1) {
@@ -1141,6 +1146,10 @@ hipError_t launch_prefill(int dtype, const PrefillArgs& a, hipStream_t st)
         for (int i = 0; i < PREFILL_CUTS; ++i) groups += units * (a.blocks - a.cut[i]);
         merged -= units * a.cut[0] * a.rows;
     }
+    a.by_units = divisor((uint32_t)units);
+    a.by_hkv = divisor((uint32_t)a.Hkv);
+    a.by_g = divisor((uint32_t)a.G);
+    a.by_merged = divisor(a.S > 1 ? (uint32_t)(merged / units) : 1);
     if (groups > 0x7fffffff || (merged + 7) / 8 > 0x7fffffff) return hipErrorInvalidValue;
     auto go = [&](void (*kernel)(PrefillArgs), int lds, int threads = 256) {
         const hipError_t e = allow_dynamic_lds((const void*)kernel, lds);
