@@ -138,3 +138,30 @@ def test_broadcast_sources(ctx):
     for b in range(2):
         ref, err = turned(np.repeat(f64(x[0]), 4, 0), pos[:, b], inv_freq(), [0] * 64, False)
         assert (np.abs(f64(out[b]) - ref) <= 2.0 ** -24 * np.abs(ref) + err * 1.01).all()
+
+
+@pytest.mark.parametrize("apart", [(1 << 24) - 8, 1 << 24])
+def test_rows_far_apart(ctx, apart):
+    """Rows of the segment as far apart as the kernel of many rows takes them, and farther: 23 GB of which 700 rows are read."""
+    g = np.random.default_rng(23)
+    n, Hq, H = 700, 32, 8
+    lay = rk.Layout(1, Hq, H, 64, rk.RK_BF16, 32, 0)
+    assert rk.rk_prefill_plan(ctx, lay, n, n, 0, 0)[0] == 256
+    q, k, v = (normal(g, (1, n, h, D), BF).transpose(1, 2) for h in (Hq, H, H))
+    room = torch.empty((n - 1) * apart + 2 * H * D, dtype=BF, device=DEV)
+    far = [torch.as_strided(room, (1, H, n, D), (0, D, apart, 1), i * H * D) for i in range(2)]
+    for x, y in zip(far, (k, v)):
+        x.copy_(y)
+    out = torch.zeros(2, 1, n, Hq, D, dtype=BF, device=DEV)
+    ws = torch.empty(rk.rk_window_workspace_size(ctx, lay, n), dtype=torch.uint8, device=DEV)
+    for o, (a, b) in zip(out, (far, (k, v))):
+        rk.rk_prefill_attn_window(ctx, lay, rk.Heads(q), n, rk.Text(a, b, n, strides=tuple(a.stride()[:3])), 0, 0, 0.0, rk.Heads(o.transpose(1, 2)), ws)
+    if apart < 1 << 24:
+        assert torch.equal(out[0], out[1])
+    t = np.array([0, 1, 31, 32, 63, 64, 65, 300, 511, 640, 698, 699])
+    for h in (0, 13, 31):
+        see = np.arange(n)[None] <= t[:, None]
+        x = f64(q[0, h, t])
+        ref, size, mean = attend(x, [(f64(k[0, h // 4]), x, np.zeros(len(t)), f64(v[0, h // 4]), see)])
+        for o in out:
+            assert (np.abs(f64(o[0, t, h]) - ref) <= tolerance(ref, size, mean, n, BF, True)).all()
