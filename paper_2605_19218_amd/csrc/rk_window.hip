@@ -398,8 +398,8 @@ __global__ __launch_bounds__(512, 2) void attn_prompt_parts(PrefillArgs A)
             const int64_t at = (int64_t)min(P.start(i) + token, P.len - 1) * A.st + 8 * eight;
             load_to_lds(kp + at, base);
             load_to_lds(kp + at + 4, base + 1024);
-            load_to_lds(vp + at, base + 2048);
-            load_to_lds(vp + at + 4, base + 3072);
+            load_to_lds(vp + at, base + 2 * 1024);
+            load_to_lds(vp + at + 4, base + 3 * 1024);
         };
         // the parts of what was asked for as stage i; then stage `next` is asked for
         auto ready = [&](int i, int next, char* to) {
