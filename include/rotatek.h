@@ -550,7 +550,7 @@ rk_status rk_prefill_attn_window(rk_ctx* ctx, const rk_layout* L, const rk_heads
                                  const rk_text* text, int32_t window, int32_t sinks, float scale, const rk_heads* out, void* workspace,
                                  size_t workspace_bytes, void* stream);
 
-/* How it shares its work out: the rows of a work-group (a KV head's n_tokens H_q / H_kv; 32 or 256, with fp32 128 or 256) and the splits of what they see, for a
+/* How it shares its work out: the rows of a work-group (a KV head's n_tokens H_q / H_kv; 32 or 256, with fp32 also 128) and the splits of what they see, for a
  * segment of at most max_len rows, which lie less than 2^24 elements apart (others are taken by 32 with 16-bit rows).  n_splits is the most that any work-group's rows are in.
  * INVALID_ARG and UNSUPPORTED as the call.                                                                       */
 rk_status rk_prefill_plan(const rk_ctx* ctx, const rk_layout* L, int32_t n_tokens, int32_t max_len, int32_t window, int32_t sinks,

@@ -470,14 +470,15 @@ RowsPlan window_plan(const rk_ctx* ctx, const rk_layout* L, bool cache, int text
 }
 
 // Prompts: rows of a block, blocks of a KV head, splits of what a block sees, whichever come out cheapest, in microseconds as measured. A work-group takes `each` for its
-// beginning and end and `step` for `tokens` of what it sees; no launch is shorter than its longest work-group (`alone` of a step while compute units are to spare), nor than all of them one
+// beginning and end (`again` where others follow it), `edge` for a tile that is masked for some of its rows, and `step` for `tokens` of what it sees; no launch is shorter than its longest work-group (`alone` of a step while compute units are to spare), nor than all of them one
 // after another on the compute units, where the last round is not full: that costs as much as a full one if they are equally long, and nothing if the short ones of a
 // causal prompt fill it. Partials are written and read.
-// us, bf16 with 32 / 256 rows a block: 8 units of 4 heads, 1 token on 1000 9.7 / 12.6, 40 on 4000 19.1 / 25.7, the same with a window of 512 12.3 / 18.8, 300 12.9 / 16.7, 700 28.3 /
-// 25.9, 1000 42.6 / 33.0, 500 on 8000 175 / 77, 1500 on 2000 with a window of 512 70 / 32; 32 units of 7 heads, 20 on 500 11.9 / 20.8, 100 18.2 / 14.4, 40 on 4000 with
-// a window of 512 24.1 / 28.6, 1000 286 / 90; 512 units of 4 heads, 4 on 500 28.9 / 46.0, 20 on 500 85.0 / 52.3.  fp32 with 128 / 256 rows: 8 units of 4 heads, 40 on 1000 with a
-// window of 512 23.2 / 25.7, 300 28.0 / 30.9, 700 67 (4 splits) / 46 (5), 1000 109 / 69, 500 on 8000 525 / 327; 32 units of 1 head, 1500 in 1, 2, 3, 4 splits 251, 193, 194, 198 /
-// 190, 128, 140, 145, 2944 587, 600 / 406, 416.  (Of 100 shapes drawn the plan's time was 2 % above the best of all rows and splits on average, 17 % at worst.)
+// us, bf16 with 32 / 256 rows a block: 8 units of 4 heads, 1 token on 1000 9.0 / 11.8, 40 on 4000 18.6 / 24.8, the same with a window of 512 11.7 / 17.9, 300 12.7 / 16.5, 700 28.1 /
+// 25.9, 1000 42.6 / 32.1, 500 on 8000 175 / 77, 1500 on 2000 with a window of 512 71 / 32; 32 units of 7 heads, 20 on 500 11.9 / 20.3, 100 17.8 / 14.1, 40 on 4000 with
+// a window of 512 24.1 / 27.8, 1000 283 / 90; 32 units of 1 head, 674 with a window of 55 18.4 / 27.5; 512 units of 4 heads, 4 on 500 28.6 / 45.4, 20 on 500 85 / 52.
+// fp32 with 32 / 128 / 256 rows: 8 units of 4 heads, 8 on 4000 20.4 / 28.3 / 30.4, 40 on 1000 with a window of 512 16.6 / 21.9 / 24.2, 100 11.2 / 15.0 / 20.3, 300 23.6 / 27.0 / 29.8, 700
+// 68 / 66 / 46, 500 on 8000 - / 525 / 339; 32 units of 7 heads, 100 29.8 / 22.4 / 25.6; 512 of 4, 4 on 500 62 / 131 / 153, 20 on 500 201 / 146 / 174; 32 units of 1 head, 1500 in 1, 2, 3, 4
+// splits of 256 rows 190, 128, 140, 145, 2944 406, 416.  (Of 240 shapes drawn the plan's time was 1 % above the best of all rows and splits on average, 24 % at worst.)
 // Where all work-groups run at once the longest is waited for, and a block takes a split for each so many tokens that it sees: less is begun, written and folded than with as many for all blocks.  us, all
 // alike / by length: fp32 8 units of 4 heads, 300 in 5 splits 34 / 28, 1000 89 / 71, 2 units of 8 heads, 1000 58 / 47; bf16 8 units of 1 head, 3000 in 4 56 / 47.  Where they do not, the
 // long ones have to come first, which they do with as many for all (fp32 4 units of 7 heads, 2944 in 2 363 / 385).
@@ -495,18 +496,21 @@ PrefillPlan prefill_plan(const rk_ctx* ctx, const rk_layout* L, int n, int max_l
     const int64_t units = (int64_t)L->batch * L->n_kv_heads, G = L->n_q_heads / L->n_kv_heads, n_cu = ctx ? ctx->n_cu : 256;
     PrefillPlan best{};
     double least = 1e300;
-    auto look = [&](int rows, int tokens, double each, double step, double alone) {
+    auto look = [&](int rows, int tokens, int tile, double each, double again, double step, double alone, double edge) {
         const int64_t blocks = ((int64_t)n * G + rows - 1) / rows;
         // rows of the segment that a block sees: at most, and on average over the new tokens
         const double first = max_len > n ? (double)max_len - n + 1 : 1.0, last = max_len > 1 ? (double)max_len : 1.0;
         double most = last, seen = 0.5 * (first + last);
-        const double bound = (double)window + sinks + rows / G + 1;
+        const double bound = (double)window + sinks + rows / G + 1 + tile / 2;       // (a window begins inside a tile)
         if (window > 0 && bound < last) {
             most = bound;
             seen = bound <= first ? bound : (0.5 * (first + bound) * (bound - first) + bound * (last - bound)) / (last - first);
         }
         const double even = 2.0 * seen / most - 1.0;           // 1: all as long, 0: from nothing up
-        const int64_t steps = (int64_t)((most + tokens - 1) / tokens);
+        const int64_t steps = (int64_t)((most + tokens - 1) / tokens), edges = (rows / G / tile + 1) * (window > 0 && bound < last ? 2 : 1);
+        const double masked = edge * (edges < steps ? edges : steps);
+        each += masked;
+        again += masked;
         for (int S = 1; S <= PREFILL_SPLITS_MAX && S <= steps; ++S) {
             // (what the workspace holds)
             if (S > 1 && units * blocks * S * rows > PREFILL_ROWS * n_cu) break;
@@ -522,8 +526,8 @@ PrefillPlan prefill_plan(const rk_ctx* ctx, const rk_layout* L, int n, int max_l
             const double groups = (double)(units * blocks) * parts, share = groups / n_cu, full = (double)(int64_t)(share + 0.999);
             double rounds = share + (full - share) * (even > 0.0 ? even : 0.0);
             if (rounds < 1.0) rounds = 1.0;
-            const double mean = seen / tokens / parts, longest = each + alone * stretch, all = rounds * (each + step * (mean > 1.0 ? mean : 1.0));
-            const double merge = S == 1 ? 0.0 : 2.5 + (double)units * n * G * parts * 1040 / 4e6;
+            const double mean = seen / tokens / parts, longest = each + alone * stretch, all = (rounds > 1.0 ? again : each) * rounds + rounds * step * (mean > 1.0 ? mean : 1.0);
+            const double merge = S == 1 ? 0.0 : 2.5 + 0.1 * S + (double)units * n * G * parts * 1040 / 4e6;
             const double cost = (longest > all ? longest : all) + merge;
             if (cost < least - 0.01) {
                 least = cost;
@@ -532,11 +536,12 @@ PrefillPlan prefill_plan(const rk_ctx* ctx, const rk_layout* L, int n, int max_l
         }
     };
     if (L->dtype == RK_F32) {
-        look(128, 32, 6.0, 4.5, 4.0);
-        look(256, 32, 10.0, 4.5, 4.0);
+        look(32, 128, 32, 6.5, 12.0, 4.5, 4.5, 0.0);
+        look(128, 32, 32, 5.0, 7.0, 4.5, 4.3, 0.0);
+        look(256, 32, 32, 8.0, 11.0, 4.5, 4.2, 0.0);
     } else {
-        if (stride_t < PREFILL_FAR) look(256, 64, 12.0, 1.55, 1.55);       // (its lanes' addresses are 32 bits)
-        look(32, 128, 9.0, 1.35, 1.35);
+        if (stride_t < PREFILL_FAR) look(256, 64, 64, 7.0, 8.0, 1.55, 1.5, 2.0);       // (its lanes' addresses are 32 bits)
+        look(32, 128, 32, 6.0, 6.5, 1.35, 1.35, 0.0);
     }
     return best;
 }

@@ -122,7 +122,7 @@ struct PrefillArgs {
     int32_t max_len, n;
     int32_t B, Hq, Hkv, G;
     int32_t window, sinks;
-    int32_t rows, blocks, S;     // rows of a block: 128 or 256 (fp32), 256 or 32 (bf16); blocks of a KV head; splits of what a block sees, at most
+    int32_t rows, blocks, S;     // rows of a block: 32 or 256, fp32 also 128; blocks of a KV head; splits of what a block sees, at most
     int32_t cut[PREFILL_CUTS];   // blocks from cut[i] on are in i + 2 splits or more; with more than PREFILL_CUTS + 1 all blocks are in S
     Divisor by_units, by_hkv, by_g, by_merged;    // B Hkv; Hkv; G; rows of a KV head that are in splits
     float scale_log2;

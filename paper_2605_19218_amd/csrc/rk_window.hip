@@ -181,7 +181,7 @@ __device__ __forceinline__ void clean_values(char* values, int bytes, int* odd, 
     }
 }
 
-// ---- fp32, fewer rows ----------------------------------------------------------------
+// ---- fp32, 128 rows ----------------------------------------------------------------
 // 32 rows a wave, 128 a work-group, two work-groups a compute unit; stages of 32 tokens in LDS, two of them. Bound by the fp32 matrix instructions: 128 of 64 cycles
 // for a tile, to some 500 cycles of vector instructions (8 x 28 heads, 500 tokens on 8000 3945 us, 120 TFLOP/s; the matrix cores are busy for 78 % of the cycles).
 constexpr int F32_ROWS = 128, F32_TOKENS = 32, F32_ROW = 512, F32_VALUES = F32_TOKENS * F32_ROW, F32_STAGE = 2 * F32_VALUES;
@@ -931,6 +931,46 @@ __global__ __launch_bounds__(256, 1) void attn_prompt_wide(PrefillArgs A)
 constexpr int FEW_ROWS = 32, FEW_TOKENS = 32, FEW_TILE = 2 * FEW_TOKENS * 256, FEW_WAVE = 2 * FEW_TILE, FEW_LDS = 4 * FEW_WAVE;
 constexpr int FEW_PARK = 33;     // 32 rows' quads, and one: lanes that write quads side by side meet other banks
 
+// The fold of the four waves' sums of 32 rows, parked: 32 lanes a row, four channels each.
+template <typename T>
+__device__ __forceinline__ void few_fold(const PrefillArgs& A, const Prompt<FEW_TOKENS>& P, int u, int split, int splits, const f32x4* park, float (&sm_m)[4][32], float (&sm_l)[4][32],
+                                         float m, float l, int tid)
+{
+    if ((tid & 32) == 0) {
+        sm_m[tid >> 6][tid & 31] = m;
+        sm_l[tid >> 6][tid & 31] = l;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int r = 8 * k + (tid >> 5), p = tid & 31, row = P.row0 + r;
+        if (row >= P.rows) continue;
+        const float M = fmaxf(fmaxf(sm_m[0][r], sm_m[1][r]), fmaxf(sm_m[2][r], sm_m[3][r]));
+        f32x4 acc = (f32x4){0.f, 0.f, 0.f, 0.f};
+        float sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float x = partial_weight(sm_m[w][r], sm_l[w][r], M);
+            acc += park[(w * 32 + p) * FEW_PARK + r] * x;
+            sum = fmaf(sm_l[w][r], x, sum);
+        }
+        if (splits == 1) {
+            const int t = P.token(A, row), hd = P.hk * A.G + row - t * A.G;
+            const float inv = sum == 0.f ? 0.f : 1.f / sum;
+            float x[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = sum == 0.f ? 0.f : acc[e] * inv;
+            T* o = (T*)A.out + (int64_t)P.b * A.o_sb + (int64_t)hd * A.o_sh + (int64_t)t * A.o_st + 4 * p;
+            if constexpr (sizeof(T) == 4) *(f32x4*)o = (f32x4){x[0], x[1], x[2], x[3]};
+            else *(uint2*)o = make_uint2(__builtin_bit_cast(uint32_t, (bf16x2){(__bf16)x[0], (__bf16)x[1]}), __builtin_bit_cast(uint32_t, (bf16x2){(__bf16)x[2], (__bf16)x[3]}));
+        } else {
+            const size_t slot = ((size_t)u * A.n * A.G + row) * A.S + split;
+            *(f32x4*)(A.ws_acc + slot * D + 4 * p) = acc;
+            if (p == 0) { A.ws_m[slot] = M; A.ws_l[slot] = sum; }
+        }
+    }
+}
+
 __global__ __launch_bounds__(256, 1) void attn_prompt_few(PrefillArgs A)
 {
     extern __shared__ __attribute__((aligned(16))) char lds[];
@@ -1077,38 +1117,138 @@ __global__ __launch_bounds__(256, 1) void attn_prompt_few(PrefillArgs A)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
             park[(wave * 32 + 8 * c + 2 * e + h) * FEW_PARK + n] = (f32x4){O[c][4 * e], O[c][4 * e + 1], O[c][4 * e + 2], O[c][4 * e + 3]};
-    if (h == 0) {
-        sm_m[wave][n] = m;
-        sm_l[wave][n] = l;
-    }
-    __syncthreads();
+    few_fold<bf16_t>(A, P, u, split, splits, park, sm_m, sm_l, m, l, tid);
+}
+
+// ---- fp32, few rows ------------------------------------------------------------------
+// The same with fp32 products: a wave's tile is 32 KB of LDS, so it has one, whose Keys' half is asked for again as soon as the scores are there, and whose Values' half behind the products.
+// 40 tokens of 8 units of 4 heads behind 1000, a window of 512: 16.6 us with the fold (128 rows a work-group: 21.9), 100 tokens 11.2 (15.0), 512 units of 4 heads, 4 tokens on 500 62 (131).
+// Bound by round trips, and by the fp32 products, 8200 cycles a tile.
+constexpr int FEW32_VALUES = FEW_TOKENS * F32_ROW, FEW32_WAVE = 2 * FEW32_VALUES, FEW32_LDS = 4 * FEW32_WAVE;
+
+__global__ __launch_bounds__(256, 1) void attn_prompt_few_f32(PrefillArgs A)
+{
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    __shared__ float sm_m[4][32], sm_l[4][32];
+    int block, split, splits, u;
+    prompt_place(A, block, split, splits, u);
+    const Prompt<FEW_TOKENS> P(A, u, block, split, splits, FEW_ROWS);
+    if (P.row0 >= P.rows) return;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, n = lane & 31;
+    const int mine = min(P.row0 + n, P.rows - 1), tok = P.token(A, mine), head = P.hk * A.G + mine - tok * A.G;
+    const Sight sight{P.first + tok, P.window, P.sinks};
+    const float* kp = (const float*)A.k + (int64_t)P.b * A.sb + (int64_t)P.hk * A.sh;
+    const float* vp = (const float*)A.v + (int64_t)P.b * A.sb + (int64_t)P.hk * A.sh;
+
+    f32x4 q[16];
+    const float* qp = (const float*)A.q + (int64_t)P.b * A.q_sb + (int64_t)head * A.q_sh + (int64_t)tok * A.q_st;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const int r = 8 * k + (tid >> 5), p = tid & 31, row = P.row0 + r;
-        if (row >= P.rows) continue;
-        const float M = fmaxf(fmaxf(sm_m[0][r], sm_m[1][r]), fmaxf(sm_m[2][r], sm_m[3][r]));
-        f32x4 acc = (f32x4){0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < 16; ++i) q[i] = *(const f32x4*)(qp + 8 * i + 4 * h);
+
+    char* own = lds + wave * FEW32_WAVE;
+    const uint32_t base = __builtin_amdgcn_readfirstlane(lds_address(own));
+    // rows 2 x + lane / 32 of a tile, x < 16
+    auto fetch = [&](const float* from, int i, int half) {
+        const int j = P.start(i);
+#pragma unroll
+        for (int x = 0; x < 16; ++x) load_to_lds(from + (int64_t)min(j + 2 * x + h, P.len - 1) * A.st + 4 * slot_of(2 * x + h, n), base + half + 2 * F32_ROW * x);
+    };
+    int ka[4], va[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        ka[i] = n * F32_ROW + 16 * slot_of(n, 2 * i + h);
+        va[i] = FEW32_VALUES + (4 * h + i) * F32_ROW + 16 * slot_of(4 * h + i, n);
+    }
+    float m = ROWS_NEG_INF, l = 0.f;
+    f32x16 O[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) O[c][i] = 0.f;
+    bool odd = false;
+    if (P.i0 + wave < P.i1) {
+        fetch(kp, P.i0 + wave, 0);
+        fetch(vp, P.i0 + wave, FEW32_VALUES);
+    }
+#pragma unroll 1
+    for (int i = P.i0 + wave; i < P.i1; i += 4) {
+        const int j0 = P.start(i);
+        const bool edge = P.edge(j0), more = i + 4 < P.i1;
+        stage_wait<16>();                // (all but the Values)
+        f32x16 s;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[e] = 0.f;
+#pragma unroll
+        for (int x = 0; x < 16; ++x) {
+            const f32x4 a = *(const f32x4*)(own + ka[x & 3] + 128 * (x >> 2));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], q[x][e], s, 0, 0, 0);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");     // (nothing reads the Keys any more)
+        if (more) fetch(kp, i + 4, 0);
+        if (edge) sight.hide(s, j0 + 4 * h);
+        float mt = s[0];
+#pragma unroll
+        for (int e = 1; e < 16; ++e) mt = fmaxf(mt, s[e]);
+        mt = halves_max(mt) * A.scale_log2;
+        if (__any(mt > m + 8.f)) {
+            const float m_new = fmaxf(m, mt), alpha = m > ROWS_NEG_INF ? rows_exp2(m - m_new) : 1.f;
+            l *= alpha;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) O[c] *= alpha;
+            m = m_new;
+        }
+        const float ref = m > ROWS_NEG_INF ? m : 0.f;
         float sum = 0.f;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            const float x = partial_weight(sm_m[w][r], sm_l[w][r], M);
-            acc += park[(w * 32 + p) * FEW_PARK + r] * x;
-            sum = fmaf(sm_l[w][r], x, sum);
+        for (int e = 0; e < 16; ++e) {
+            s[e] = rows_exp2(fmaf(s[e], A.scale_log2, -ref));
+            sum += s[e];
         }
-        if (splits == 1) {
-            const int t = P.token(A, row), hd = P.hk * A.G + row - t * A.G;
-            const float inv = sum == 0.f ? 0.f : 1.f / sum;
-            float x[4];
+        l += sum;
+        if (more) stage_wait<16>();      // (all but the next Keys)
+        else stage_wait<0>();
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[e] = sum == 0.f ? 0.f : acc[e] * inv;
-            *(uint2*)((bf16_t*)A.out + (int64_t)P.b * A.o_sb + (int64_t)hd * A.o_sh + (int64_t)t * A.o_st + 4 * p) =
-                make_uint2(__builtin_bit_cast(uint32_t, (bf16x2){(__bf16)x[0], (__bf16)x[1]}), __builtin_bit_cast(uint32_t, (bf16x2){(__bf16)x[2], (__bf16)x[3]}));
-        } else {
-            const size_t slot = ((size_t)u * A.n * A.G + row) * A.S + split;
-            *(f32x4*)(A.ws_acc + slot * D + 4 * p) = acc;
-            if (p == 0) { A.ws_m[slot] = M; A.ws_l[slot] = sum; }
+        for (int e = 0; e < 16; ++e) {
+            f32x4 a = *(const f32x4*)(own + va[e & 3] + 8 * F32_ROW * (e >> 2));
+            if (edge) {                  // Values that are no numbers count as 0 where they may be masked
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const bool no = odd_value(__float_as_uint(a[c]));
+                    odd |= no;
+                    a[c] = no ? 0.f : a[c];
+                }
+            }
+#pragma unroll
+            for (int c = 0; c < 4; ++c) O[c] = __builtin_amdgcn_mfma_f32_32x32x2f32(a[c], s[e], O[c], 0, 0, 0);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");     // (nor the Values)
+        if (more) fetch(vp, i + 4, FEW32_VALUES);
+    }
+    // ... and join the rows that see them behind the loop: a sum of one is it, or NaN.  (O[c][e] is channel 4 (8 (e / 4) + 4 h + e % 4) + c)
+    if (__any(odd)) {
+#pragma unroll 1
+        for (int i = P.i0 + wave; i < P.i1; i += 4) {
+            const int j0 = P.start(i);
+            if (!P.edge(j0)) continue;
+#pragma unroll 1
+            for (int j = j0; j < min(j0 + FEW_TOKENS, P.len); ++j)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const f32x4 v = *(const f32x4*)(vp + (int64_t)j * A.st + 4 * (8 * (e >> 2) + 4 * h + (e & 3)));
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) O[c][e] += odd_value(__float_as_uint(v[c])) && sight.of(j) ? v[c] : 0.f;
+                }
         }
     }
+
+    // the four waves' sums: quads of channels, [wave][channels 4 p ..+3][row]
+    l = halves_sum(l);
+    __syncthreads();
+    f32x4* park = (f32x4*)lds;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) park[(wave * 32 + 8 * (e >> 2) + 4 * h + (e & 3)) * FEW_PARK + n] = (f32x4){O[0][e], O[1][e], O[2][e], O[3][e]};
+    few_fold<float>(A, P, u, split, splits, park, sm_m, sm_l, m, l, tid);
 }
 
 // The fold of the splits' partials, of the blocks that are in splits: 32 lanes a row, four channels each (see rows_merge).
@@ -1159,6 +1299,7 @@ hipError_t launch_prefill(int dtype, const PrefillArgs& args, hipStream_t st)
     };
     hipError_t e;
     if (dtype == 0 && a.rows == PARTS_ROWS) e = go(attn_prompt_parts, PARTS_LDS + 16, 512);
+    else if (dtype == 0 && a.rows == FEW_ROWS) e = go(attn_prompt_few_f32, FEW32_LDS);
     else if (dtype == 0) e = go(attn_prompt_f32, 2 * F32_STAGE + 16);
     else if (a.rows == FEW_ROWS) e = go(attn_prompt_few, FEW_LDS);
     else e = go(attn_prompt_wide, WIDE_LDS + 16);

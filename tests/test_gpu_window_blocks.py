@@ -64,6 +64,10 @@ KERNELS = [
     (BF, 40, 8, 4, 130, 200, 33, 70, 256, False),
     (BF, 2, 28, 4, 300, 3000, 0, 0, 256, True),
     (BF, 1, 32, 8, 500, 4000, 2500, 70, 256, True),
+    (F32, 40, 8, 4, 9, 40, 7, 2, 32, False),
+    (F32, 2, 16, 2, 230, 400, 0, 0, 32, False),
+    (F32, 2, 8, 2, 40, 300, 0, 0, 32, True),
+    (F32, 1, 16, 2, 150, 1500, 900, 40, 32, True),
     (F32, 40, 8, 4, 90, 100, 20, 2, 128, False),
     (F32, 1, 8, 2, 45, 300, 0, 0, 128, True),
     (F32, 16, 16, 8, 300, 400, 100, 5, 256, False),
@@ -71,7 +75,7 @@ KERNELS = [
     # few work-groups: blocks that see more are in more splits, up to eight
     (BF, 1, 1, 1, 3000, 3100, 0, 0, 32, True),
     (BF, 1, 8, 8, 2500, 2500, 0, 0, 256, True),
-    (F32, 1, 8, 2, 300, 300, 0, 0, 128, True),
+    (F32, 1, 8, 2, 300, 300, 0, 0, 32, True),
     (F32, 1, 8, 4, 600, 1100, 700, 9, 128, True),
     (F32, 1, 16, 2, 700, 900, 300, 40, 256, True),
     # ... and more than eight, the same for all

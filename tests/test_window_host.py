@@ -136,7 +136,7 @@ def test_prefill_plan():
     plan = lambda n, most, w=0, s=0, **m: rk.rk_prefill_plan(None, lay(**{**dict(batch=1, n_q_heads=32, n_kv_heads=8), **m}), n, most, w, s)
     assert plan(1, 1)[0] == 32 and plan(40, 1040, 512, 4)[0] == 32 and plan(300, 300)[0] == 32
     assert plan(500, 8500)[0] == 256 and plan(16384, 16384, 4096, 4) == (256, 1) and plan(100, 100, batch=64)[0] == 256
-    assert plan(40, 1040, dtype=rk.RK_F32)[0] == 128 and plan(500, 8500, dtype=rk.RK_F32)[0] == 256
+    assert plan(40, 1040, 512, 4, dtype=rk.RK_F32)[0] == 32 and plan(100, 100, batch=4, n_q_heads=56, dtype=rk.RK_F32)[0] == 128 and plan(500, 8500, dtype=rk.RK_F32)[0] == 256
     assert plan(1 << 20, 1 << 30)[1] == 1                      # (a full device takes no splits)
     for dtype in (rk.RK_F32, rk.RK_BF16):
         for batch, hq, hkv in ((1, 1, 1), (1, 32, 8), (8, 28, 4), (3, 64, 64)):
