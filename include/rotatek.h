@@ -543,8 +543,9 @@ size_t rk_window_workspace_size(const rk_ctx* ctx, const rk_layout* L, int32_t n
  * within 0..n_tokens; NULL: n_tokens) of them, the last n_b of its len[b] rows (text->len NULL: max_len): token t stands at len[b] - n_b + t.  One that stands in
  * front of row 0 sees nothing and yields zeros.  q, out: heads of n_q_heads; rows of out from n_b on stay as they were; out may lie exactly over q.
  * Scores q . k * scale (1/sqrt(d) when `scale` <= 0).  With 16-bit rows the softmax weights enter the product with the Values as bf16 (the sum that
- * divides it is fp32).  With fp32 rows a product is of all 24 bits or leaves out less than 2^-24 of itself, and a token that sees a Key with an infinity
- * may get NaN even where its score would be minus infinity.  Workspace: rk_window_workspace_size(ctx, L, n_tokens), 16-byte aligned; calls with workspaces of their own may overlap.
+ * divides it is fp32).  With fp32 rows a product is of all 24 bits or leaves out less than 2^-24 of itself (of a number below 2^-100: less than 2^-125 of that number);
+ * a token that sees a Key with an infinity, or holds one in its query, may get NaN even where its score would be minus infinity.  A token that sees a Value
+ * with an infinity gets it in that channel, or NaN: where it sees one of the other sign or a NaN, and where its weight is less than fp32 holds.  Workspace: rk_window_workspace_size(ctx, L, n_tokens), 16-byte aligned; calls with workspaces of their own may overlap.
  * B n_tokens H_q at most 2^31 - 1.  Errors: INVALID_ARG, UNSUPPORTED, CAPACITY, WORKSPACE, HIP.                  */
 rk_status rk_prefill_attn_window(rk_ctx* ctx, const rk_layout* L, const rk_heads* q, int32_t n_tokens, const int32_t* n_tokens_dev,
                                  const rk_text* text, int32_t window, int32_t sinks, float scale, const rk_heads* out, void* workspace,

@@ -322,13 +322,25 @@ __global__ __launch_bounds__(256, 2) void attn_prompt_f32(PrefillArgs A)
 // writes their parts for all. Of the two waves of a SIMD one does that in front of its products, the other behind them.
 // 8 x 28 heads, 500 tokens on 8000 2240 us, 211 TFLOP/s, 1270 of issued products: what a large bf16 matrix product reaches here. 32 heads x 2944 tokens 417 us, 170 TFLOP/s, where
 // the work-groups, one a compute unit and some three times as long as others, leave a fifth of the compute units' time unused.
-// (An infinity has NaN for a remainder: a row that sees one gets no number.)
+// What that holds for: numbers from 2^-100 on (of smaller ones, parts below the smallest normal number may count as 0, less than 2^-125 of the number in all). Above the largest bf16
+// number the first part is rounded towards zero (2^-23 of a product left out there), and an infinity has no other parts, so that finite numbers have finite parts. An infinity times a part of 0 is NaN:
+// Values that are no numbers are left out in every stage and join the rows that see them behind the loop, as on edges in the other kernels; for Keys and queries the header says it.
+// (Looking for such numbers costs 1 %: 32 heads x 2944 tokens 408 -> 413 us.)
 constexpr int PARTS_ROWS = 256, PARTS_TOKENS = 32, PARTS_PLANE = PARTS_TOKENS * 256, PARTS_STAGE = 6 * PARTS_PLANE, PARTS_RAW = 2 * PARTS_STAGE,
               PARTS_LDS = PARTS_RAW + 8 * 4096;        // planes [stage][Keys 3, Values 3]; eight waves' own places; and a flag
 
-// eight numbers in parts
-__device__ __forceinline__ void parts3(const float (&x)[8], bf16x8 (&p)[3])
+// The bits of the largest of eight numbers' sizes (more than an infinity's where one is no number).
+__device__ __forceinline__ uint32_t largest(const float (&x)[8])
 {
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
+    return top;
+}
+// eight numbers in parts; top: largest() of them, or less where it is known to be no more than the largest bf16 number
+__device__ __forceinline__ void parts3(const float (&x)[8], bf16x8 (&p)[3], uint32_t top = 0)
+{
+    constexpr uint32_t MOST = 0x7f7f0000u;       // the largest bf16 number
     float r[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) r[i] = x[i];
@@ -341,6 +353,16 @@ __device__ __forceinline__ void parts3(const float (&x)[8], bf16x8 (&p)[3])
             if (k < 2) {
                 r[2 * i] -= __uint_as_float(w[i] << 16);
                 r[2 * i + 1] -= __uint_as_float(w[i] & 0xffff0000u);
+            }
+        }
+        if (k == 0 && top > MOST) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t bits = __float_as_uint(x[i]), size = bits & 0x7fffffffu, first = bits & 0xffff0000u;
+                if (size > MOST && size <= 0x7f800000u) {
+                    w[i >> 1] = i & 1 ? (w[i >> 1] & 0xffffu) | first : (w[i >> 1] & 0xffff0000u) | first >> 16;
+                    r[i] = size == 0x7f800000u ? 0.f : x[i] - __uint_as_float(first);
+                }
             }
         }
         p[k] = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
@@ -375,7 +397,7 @@ __global__ __launch_bounds__(512, 2) void attn_prompt_parts(PrefillArgs A)
     for (int i = 0; i < 8; ++i) {
         const f32x4 a = *(const f32x4*)(qp + 16 * i + 8 * h), b = *(const f32x4*)(qp + 16 * i + 8 * h + 4);
         const float x[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-        parts3(x, q[i]);
+        parts3(x, q[i], largest(x));
     }
     const float* kp = (const float*)A.k + (int64_t)P.b * A.sb + (int64_t)P.hk * A.sh;
     const float* vp = (const float*)A.v + (int64_t)P.b * A.sb + (int64_t)P.hk * A.sh;
@@ -413,21 +435,17 @@ __global__ __launch_bounds__(512, 2) void attn_prompt_parts(PrefillArgs A)
             const int kat = token * 256 + 16 * key_slot(token, eight), vat = token * 256 + 16 * value_slot(token, eight);
             bf16x8 p[3];
             const float a[8] = {raw[0][0], raw[0][1], raw[0][2], raw[0][3], raw[1][0], raw[1][1], raw[1][2], raw[1][3]};
-            parts3(a, p);
+            parts3(a, p, largest(a));
 #pragma unroll
             for (int k = 0; k < 3; ++k) *(bf16x8*)(to + k * PARTS_PLANE + kat) = p[k];
             float b[8] = {raw[2][0], raw[2][1], raw[2][2], raw[2][3], raw[3][0], raw[3][1], raw[3][2], raw[3][3]};
-            if (P.edge(P.start(i))) {            // Values that are no numbers count as 0 where they may be masked
-                bool any = false;
+            const uint32_t top = largest(b);
+            if (top >= 0x7f800000u) {            // Values that are no numbers count as 0
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const bool o = odd_value(__float_as_uint(b[e]));
-                    any |= o;
-                    b[e] = o ? 0.f : b[e];
-                }
-                if (any) *odd = 1;
+                for (int e = 0; e < 8; ++e) b[e] = odd_value(__float_as_uint(b[e])) ? 0.f : b[e];
+                atomicOr(odd, P.edge(P.start(i)) ? 1 : 2);
             }
-            parts3(b, p);
+            parts3(b, p, top);
 #pragma unroll
             for (int k = 0; k < 3; ++k) *(bf16x8*)(to + (3 + k) * PARTS_PLANE + vat) = p[k];
         };
@@ -509,11 +527,11 @@ __global__ __launch_bounds__(512, 2) void attn_prompt_parts(PrefillArgs A)
         }
         stage_wait<0>();
         // The Values that were left out join the rows that see them: a sum of one is it, or NaN.
-        if (*odd) {
+        if (const int found = *odd) {            // 1: in stages on an edge, 2: in others
 #pragma unroll 1
             for (int i = P.i0; i < P.i1; ++i) {
                 const int j0 = P.start(i);
-                if (!P.edge(j0)) continue;
+                if (!(found & (P.edge(j0) ? 1 : 2))) continue;
 #pragma unroll 1
                 for (int j = j0; j < min(j0 + PARTS_TOKENS, P.len); ++j)
 #pragma unroll
