@@ -294,14 +294,17 @@ class Drafts:
 
 @dataclass(frozen=True)
 class Heads:
-    """Rows of a [B, H, N, d] tensor-like (any strides, channels contiguous): queries, Keys, Values or a result.  The strides are the data's when this
-    is made; it can serve many calls."""
+    """Rows of a [B, H, N, d] tensor-like (any strides, channels contiguous, or ValueError): queries, Keys, Values or a result.  The strides are the
+    data's when this is made; it can serve many calls."""
     data: Any
     strides: Optional[tuple] = None      # (stride_b, stride_h, stride_t) in elements
 
     def __post_init__(self):
         if self.strides is None and hasattr(self.data, "stride"):
-            object.__setattr__(self, "strides", tuple(self.data.stride()[:3]))
+            st = tuple(self.data.stride())
+            if st and st[-1] != 1:
+                raise ValueError(f"data: channels must be contiguous, their stride is {st[-1]}")
+            object.__setattr__(self, "strides", st[:3])
 
     def c(self) -> rk_heads:
         st = self.strides if self.strides is not None else tuple(self.data.stride()[:3])
@@ -312,7 +315,7 @@ class Heads:
 class Rope:
     """Positions of several axes: pos int32 [n_axes, B, N] (tokens contiguous), inv_freq fp32 [n_pairs] (both device); axis: the axis of each
     pair (default: axis 0 for all of inv_freq).  As Heads: made once, it can serve many calls, also where what pos holds changes; for another pos,
-    dataclasses.replace(rope, pos=other, strides=None, n_axes=None)."""
+    dataclasses.replace(rope, pos=other, strides=None, n_axes=None).  ValueError for tensors of other types or orders, and for more pairs than inv_freq holds."""
     pos: Any
     inv_freq: Any
     axis: Optional[Any] = None           # n_pairs ints, < n_axes (kept as bytes)
@@ -329,7 +332,17 @@ class Rope:
         if len(axis) > RK_MAX_PAIRS:
             raise ValueError(f"axis: of at most {RK_MAX_PAIRS} pairs")
         object.__setattr__(self, "axis", bytes(axis))
+        for name, x, dtype in (("pos", self.pos, "int32"), ("inv_freq", self.inv_freq, "float32")):
+            if str(getattr(x, "dtype", dtype)).split(".")[-1] != dtype:
+                raise ValueError(f"{name}: must be {dtype}, is {x.dtype}")
+            if hasattr(x, "stride") and hasattr(x, "shape") and len(x.shape) and x.shape[-1] > 1 and x.stride()[-1] != 1:
+                raise ValueError(f"{name}: must be contiguous along its last axis, whose stride is {x.stride()[-1]}")
+        # (a kernel reads one of them for each pair; what is not on a device no kernel reads)
+        if getattr(self.inv_freq, "is_cuda", False) and self.inv_freq.numel() < len(axis):
+            raise ValueError(f"axis: {len(axis)} pairs, inv_freq holds {self.inv_freq.numel()}")
         if self.strides is None and hasattr(self.pos, "stride"):
+            if len(self.pos.stride()) != 3:
+                raise ValueError(f"pos: [n_axes, B, N], has {len(self.pos.stride())} axes")
             object.__setattr__(self, "strides", tuple(self.pos.stride()[:2]))
         if self.n_axes is None and hasattr(self.pos, "shape"):
             object.__setattr__(self, "n_axes", int(self.pos.shape[0]))
