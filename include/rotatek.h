@@ -521,7 +521,7 @@ rk_status rk_rope(rk_ctx* ctx, const rk_layout* L, const rk_rotary* rope, int32_
  * every KV head and t < n_tokens_dev[b] (as above); len_out[b] = len[b] + the rows written, which end where the segment is full.  len_out may be text->len
  * or an array that the call does not read.  q and q_out as in rk_rope (all n_tokens_dev[b] rows), or both NULL.  One token a sequence is a decode's step, in
  * front of rk_decode_attn_window or rk_decode_attn_dual; many are a prompt, in front of rk_prefill_attn_window.  The stretch of memory from the segment's first row to its
- * last may not meet k's or v's.  RK_ERR_CAPACITY if text->max_len + n_tokens > text->capacity (max_len bounds len[b] BEFORE the call).  Calls on
+ * last may not meet k's or v's.  No two of the segment's rows up to max_len + n_tokens may share an element, nor may text->k and text->v.  RK_ERR_CAPACITY if text->max_len + n_tokens > text->capacity (max_len bounds len[b] BEFORE the call).  Calls on
  * one context must not overlap.  Errors: INVALID_ARG, UNSUPPORTED, CAPACITY, HIP.                                */
 rk_status rk_rope_append_text(rk_ctx* ctx, const rk_layout* L, const rk_rotary* rope, int32_t n_tokens, const int32_t* n_tokens_dev,
                               const rk_heads* q, const rk_heads* q_out, const rk_heads* k, const rk_heads* v, const rk_text* text,

@@ -1451,6 +1451,10 @@ rk_status rk_rope_append_text(rk_ctx* ctx, const rk_layout* L, const rk_rotary* 
     if (n_tokens < 1) return fail(ctx, RK_ERR_INVALID_ARG, "rope_append_text: n_tokens %d", n_tokens);
     if (text->max_len > text->capacity - n_tokens)
         return fail(ctx, RK_ERR_CAPACITY, "rope_append_text: %d + %d rows exceed capacity %d", text->max_len, n_tokens, text->capacity);
+    // each row is written by a work-group of its own
+    const rk_heads rows{text->k, text->stride_b, text->stride_h, text->stride_t};
+    if (!rows_apart(&rows, L->batch, L->n_kv_heads, text->max_len + n_tokens))
+        return fail(ctx, RK_ERR_INVALID_ARG, "rope_append_text: rows of the text segment share elements");
     // rows written by one work-group may be read by another: the segment's rows and the sources lie apart
     const size_t es = elem_size(L->dtype);
     const size_t tb = heads_bytes(text->stride_b, text->stride_h, text->stride_t, L->batch, L->n_kv_heads, text->capacity, es);
