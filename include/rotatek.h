@@ -512,7 +512,8 @@ rk_status rk_append_text_path(rk_ctx* ctx, const rk_layout* L, const rk_text* te
 /* ---- positions ------------------------------------------------------------------------
  * Puts positions on (or takes them off) the first n_tokens rows of every head: q has n_q_heads, k n_kv_heads; either pair may be NULL.  Sequence b has
  * n_tokens_dev[b] of them (device [B], held within 0..n_tokens; NULL: all n_tokens); rows of the results from there on stay as they were.  A result may lie exactly over
- * its source (same data, same strides); other than that results and sources may not share elements.  n_tokens may be 0.
+ * its source (same data, same strides); other than that results and sources may not share elements.  n_tokens may be 0, and is less than 2^27 (B n_tokens H_q at most
+ * 2^31 - 1): UNSUPPORTED.
  * Errors: INVALID_ARG, UNSUPPORTED, HIP.                                                                        */
 rk_status rk_rope(rk_ctx* ctx, const rk_layout* L, const rk_rotary* rope, int32_t n_tokens, const int32_t* n_tokens_dev, const rk_heads* q,
                   const rk_heads* q_out, const rk_heads* k, const rk_heads* k_out, uint32_t flags, void* stream);
@@ -546,7 +547,8 @@ size_t rk_window_workspace_size(const rk_ctx* ctx, const rk_layout* L, int32_t n
  * divides it is fp32).  With fp32 rows a product is of all 24 bits or leaves out less than 2^-24 of itself (of a number below 2^-100: less than 2^-125 of that number);
  * a token that sees a Key with an infinity, or holds one in its query, may get NaN even where its score would be minus infinity.  A token that sees a Value
  * with an infinity gets it in that channel, or NaN: where it sees one of the other sign or a NaN, and where its weight is less than fp32 holds.  Workspace: rk_window_workspace_size(ctx, L, n_tokens), 16-byte aligned; calls with workspaces of their own may overlap.
- * B n_tokens H_q at most 2^31 - 1.  Errors: INVALID_ARG, UNSUPPORTED, CAPACITY, WORKSPACE, HIP.                  */
+ * B n_tokens H_q at most 2^31 - 1, and B H_kv times the row blocks of a KV head (its rows by rk_prefill_plan's, rounded up) less than 2^24 (2^23 for fp32 in blocks of 256): UNSUPPORTED, as
+ * more than a launch holds.  Errors: INVALID_ARG, UNSUPPORTED, CAPACITY, WORKSPACE, HIP.                         */
 rk_status rk_prefill_attn_window(rk_ctx* ctx, const rk_layout* L, const rk_heads* q, int32_t n_tokens, const int32_t* n_tokens_dev,
                                  const rk_text* text, int32_t window, int32_t sinks, float scale, const rk_heads* out, void* workspace,
                                  size_t workspace_bytes, void* stream);
@@ -561,7 +563,7 @@ rk_status rk_prefill_plan(const rk_ctx* ctx, const rk_layout* L, int32_t n_token
  * already), attends all of the rotated cache and the text rows that it sees, under ONE softmax.  k_packed and v_cache both NULL: the text alone, as
  * on a layer without a rotated cache (R_r, delta_mu and L->seq_len are not read then).  text is required.  q, out: [B,H_q,d], q 16-byte aligned.  The second
  * takes the 8-bit caches.  Workspace: rk_window_workspace_size(ctx, L, 1), 16-byte aligned; calls with workspaces of their own may overlap.  A sequence with nothing
- * to attend yields zeros.  Errors: as rk_decode_attn_dual.                                                      */
+ * to attend yields zeros.  B H_kv times splits less than 2^24, as above.  Errors: as rk_decode_attn_dual.         */
 rk_status rk_decode_attn_window(rk_ctx* ctx, const rk_layout* L, const void* q, const void* k_packed, const void* v_cache, const float* R_r,
                                 const float* delta_mu, const rk_text* text, int32_t window, int32_t sinks, float scale, void* out,
                                 void* workspace, size_t workspace_bytes, void* stream);

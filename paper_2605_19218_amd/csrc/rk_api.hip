@@ -553,6 +553,23 @@ size_t prefill_ws(const rk_ctx* ctx, const rk_layout* L, int n)
     return align_up(slots * (D + 2) * sizeof(float), 256) + 256;
 }
 
+// A launch has less than 2^32 threads along its first axis.
+rk_status check_groups(rk_ctx* ctx, int64_t groups, int threads)
+{
+    if (groups <= (int64_t)UINT32_MAX / threads && groups <= INT32_MAX) return RK_OK;
+    return fail(ctx, RK_ERR_UNSUPPORTED, "%lld work-groups of %d threads: more than a launch holds", (long long)groups, threads);
+}
+rk_status check_prefill_groups(rk_ctx* ctx, const rk_layout* L, const PrefillPlan& p)
+{
+    return check_groups(ctx, (int64_t)L->batch * L->n_kv_heads * p.blocks * p.S, L->dtype == RK_F32 && p.rows == 256 ? 512 : 256);
+}
+// of attn_rows, and of the fold behind it
+rk_status check_rows_groups(rk_ctx* ctx, const rk_layout* L, const RowsPlan& p)
+{
+    const rk_status s = check_groups(ctx, ((int64_t)L->batch * L->n_kv_heads * (p.Sv + p.Sr) + 7) / 8 * 8 * p.nrb, 256);
+    return s != RK_OK || p.Sv + p.Sr == 1 ? s : check_groups(ctx, ((int64_t)L->batch * L->n_q_heads + 7) / 8, 256);
+}
+
 rk_status check_window(rk_ctx* ctx, int32_t window, int32_t sinks)
 {
     if (window < 0 || sinks < 0) return fail(ctx, RK_ERR_INVALID_ARG, "window %d, sinks %d: negative", window, sinks);
@@ -606,6 +623,12 @@ rk_status check_tokens(rk_ctx* ctx, const rk_layout* L, int32_t n)
     if (n < 0 || n > RK_MAX_TOKENS) return fail(ctx, RK_ERR_INVALID_ARG, "n_tokens %d outside 0..%d", n, RK_MAX_TOKENS);
     if ((int64_t)n * L->batch > INT32_MAX / L->n_q_heads) return fail(ctx, RK_ERR_UNSUPPORTED, "more than %d query rows", INT32_MAX);
     return RK_OK;
+}
+// (fewer than ROPE_TOKENS: a work-group a token)
+rk_status check_rope_tokens(rk_ctx* ctx, const rk_layout* L, int32_t n)
+{
+    const rk_status s = check_tokens(ctx, L, n);
+    return s != RK_OK ? s : check_groups(ctx, ((int64_t)n + ROPE_TOKENS - 1) / ROPE_TOKENS, 256);
 }
 
 rk_status check_rotary(rk_ctx* ctx, const rk_rotary* r)
@@ -1410,7 +1433,7 @@ rk_status rk_rope(rk_ctx* ctx, const rk_layout* L, const rk_rotary* rope, int32_
 {
     if (!ctx) return RK_ERR_INVALID_ARG;
     rk_status s = check_layout(ctx, L);
-    if (s != RK_OK || (s = check_tokens(ctx, L, n_tokens)) != RK_OK || (s = check_rotary(ctx, rope)) != RK_OK) return s;
+    if (s != RK_OK || (s = check_rope_tokens(ctx, L, n_tokens)) != RK_OK || (s = check_rotary(ctx, rope)) != RK_OK) return s;
     if (!q && !q_out && !k && !k_out) return fail(ctx, RK_ERR_INVALID_ARG, "rope: neither q nor k");
     if ((s = check_turned(ctx, q, q_out, "rope: q or q_out", L->batch, L->n_q_heads, n_tokens)) != RK_OK) return s;
     if ((s = check_turned(ctx, k, k_out, "rope: k or k_out", L->batch, L->n_kv_heads, n_tokens)) != RK_OK) return s;
@@ -1440,7 +1463,7 @@ rk_status rk_rope_append_text(rk_ctx* ctx, const rk_layout* L, const rk_rotary* 
 {
     if (!ctx) return RK_ERR_INVALID_ARG;
     rk_status s = check_layout(ctx, L);
-    if (s != RK_OK || (s = check_tokens(ctx, L, n_tokens)) != RK_OK || (s = check_rotary(ctx, rope)) != RK_OK) return s;
+    if (s != RK_OK || (s = check_rope_tokens(ctx, L, n_tokens)) != RK_OK || (s = check_rotary(ctx, rope)) != RK_OK) return s;
     if (!text) return fail(ctx, RK_ERR_INVALID_ARG, "rope_append_text: text is NULL");
     if ((s = check_text(ctx, text, true)) != RK_OK) return s;
     if ((s = check_turned(ctx, q, q_out, "rope_append_text: q or q_out", L->batch, L->n_q_heads, n_tokens)) != RK_OK) return s;
@@ -1494,6 +1517,7 @@ rk_status rk_prefill_plan(const rk_ctx* ctx, const rk_layout* L, int32_t n_token
     if (s != RK_OK || (s = check_tokens(nullptr, L, n_tokens)) != RK_OK || (s = check_window(nullptr, window, sinks)) != RK_OK) return s;
     if (n_tokens < 1 || max_len < 0 || max_len > RK_MAX_TOKENS || !rows_per_work_group || !n_splits) return RK_ERR_INVALID_ARG;
     const PrefillPlan p = prefill_plan(ctx, L, n_tokens, max_len, window, sinks);
+    if ((s = check_prefill_groups(nullptr, L, p)) != RK_OK) return s;
     *rows_per_work_group = p.rows;
     *n_splits = p.S;
     return RK_OK;
@@ -1515,6 +1539,8 @@ rk_status rk_prefill_attn_window(rk_ctx* ctx, const rk_layout* L, const rk_heads
     const size_t need = prefill_ws(ctx, L, n_tokens);
     if (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 15))
         return fail(ctx, RK_ERR_WORKSPACE, "prefill_attn_window workspace: need %zu bytes, 16-byte aligned", need);
+    const PrefillPlan p = prefill_plan(ctx, L, n_tokens, text->max_len, window, sinks, text->stride_t);
+    if ((s = check_prefill_groups(ctx, L, p)) != RK_OK) return s;
     if (ctx->device == RK_DEVICE_NONE) return fail(ctx, RK_ERR_NO_DEVICE, "valid arguments, but the context has no device");
     DeviceGuard dev(ctx->device);
     hipError_t e = dev.status;
@@ -1526,7 +1552,6 @@ rk_status rk_prefill_attn_window(rk_ctx* ctx, const rk_layout* L, const rk_heads
     a.len = text->len; a.max_len = text->max_len; a.n_dev = n_tokens_dev; a.n = n_tokens;
     a.B = L->batch; a.Hq = L->n_q_heads; a.Hkv = L->n_kv_heads; a.G = a.Hq / a.Hkv;
     a.window = window; a.sinks = sinks;
-    const PrefillPlan p = prefill_plan(ctx, L, n_tokens, text->max_len, window, sinks, text->stride_t);
     a.rows = p.rows; a.blocks = p.blocks; a.S = p.S;
     for (int i = 0; i < PREFILL_CUTS; ++i) a.cut[i] = i + 1 >= p.S ? p.blocks : p.tokens ? prefill_cut(p.rows, a.G, n_tokens, text->max_len, (int64_t)(i + 1) * p.tokens) : 0;
     const float sc = scale > 0.f ? scale : 1.0f / sqrtf((float)L->head_dim);
@@ -1557,11 +1582,12 @@ static rk_status window_common(rk_ctx* ctx, const rk_layout* L, const void* q, c
     const size_t need = rows_ws(ctx, L, 1);
     if (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 15))
         return fail(ctx, RK_ERR_WORKSPACE, "attention workspace: need %zu bytes, 16-byte aligned", need);
+    const RowsPlan p = window_plan(ctx, L, cache, window_rows(text->max_len, window, sinks), q8);
+    if ((s = check_rows_groups(ctx, L, p)) != RK_OK) return s;
     if (ctx->device == RK_DEVICE_NONE) return fail(ctx, RK_ERR_NO_DEVICE, "valid arguments, but the context has no device");
     DeviceGuard dev(ctx->device);
     hipError_t e = dev.status;
     if (e != hipSuccess) return hip_fail(ctx, e, "hipSetDevice");
-    const RowsPlan p = window_plan(ctx, L, cache, window_rows(text->max_len, window, sinks), q8);
     WindowRowsArgs a{};
     a.q = q; a.Kc = k_cache; a.Vc = v_cache; a.Rr = R_r; a.dmu = delta_mu; a.seq_len = L->seq_len; a.out = out;
     a.B = L->batch; a.T = 1; a.Hq = L->n_q_heads; a.Hkv = L->n_kv_heads; a.G = a.Hq / a.Hkv;

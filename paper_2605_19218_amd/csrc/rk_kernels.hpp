@@ -132,6 +132,7 @@ hipError_t launch_prefill(int dtype, const PrefillArgs& a, hipStream_t st);
 
 // ---- rk_rope.hip ----------------------------------------------------------------
 constexpr int RK_AXES = 4;
+constexpr int ROPE_TOKENS = 8;   // of a work-group
 struct RopeArgs {
     const void *q, *k, *v;       // v (and q, k): or null
     void *qo, *ko, *vo;          // ko and vo share their strides

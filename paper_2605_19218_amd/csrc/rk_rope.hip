@@ -18,8 +18,6 @@ namespace rk {
 
 namespace {
 
-constexpr int ROPE_TOKENS = 8;       // of a work-group
-
 // Eight channels of a row, in memory and as fp32.
 template <typename T> struct Piece;
 template <> struct Piece<bf16_t> {
