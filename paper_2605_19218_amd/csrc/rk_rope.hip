@@ -9,8 +9,8 @@
 // that are no multiple of eight, sixteen lanes.  Sines and cosines are the same in all heads of a token: a work-group makes those of its tokens once, in LDS, and takes the tokens' heads in the
 // order in which they lie in memory.  (Made by each lane for its own pairs, a wave taking eight tokens through head after head: 50 us in place of 43 below.)
 // Bound by memory: 28 + 4 heads x 71000 tokens of bf16 270 us, 1.44 GB, 5.3 TB/s; fp32, 32 + 32 heads x 2944 tokens from memory 43 us, 193 MB, 4.5 TB/s (a copy of as many bytes 37); 28 +
-// 4 + 4 heads x 4400 tokens into segments 23.5 us, 116 MB, 4.9 TB/s; one token of 64 sequences x 96 heads 3.5 us. 328 MB, 40 heads: bf16 x 16000 tokens 64 pairs 73 us, neighbours 77, 13 pairs 90 (117 with
-// the pairs' other channels read one by one), 63 99; fp32 x 8000 64, 69, 69, 72.
+// 4 + 4 heads x 4400 tokens into segments 23.5 us, 116 MB, 4.9 TB/s; one token of 64 sequences x 96 heads 3.5 us. 328 MB, 40 heads: bf16 x 16000 tokens 64 pairs 67 us, neighbours 71, 13 pairs 75 (117 with
+// the pairs' other channels read one by one, 89 with each of a lane's pieces waited for before the next was asked for), 63 87 (99); fp32 x 8000 65, 68, 70, 74.
 #include <type_traits>
 #include "rk_kernels.hpp"
 
@@ -139,20 +139,26 @@ __global__ __launch_bounds__(TOKENS == 1 ? 1024 : 256) void rope_rows(RopeArgs A
                 v.store(to + (mine ? np + 8 * o : 16 * o + 8));
             } else {
                 u.load(from + 8 * o);
-                if (turned && 8 * o < 2 * np) {
+                const bool mine = turned && 8 * o < 2 * np, first_half = 8 * o < np, ends = first_half && 8 * o + 8 > np;
+                Piece<T> w;
+                if (!adj && mine) {
                     // (np is 63 at most here, so that eight from 8 o + np on end inside the row; where a half ends inside a piece, the others' are the row's first)
+                    v.load_anywhere(from + (first_half ? 8 * o + np : 8 * o - np));
+                    if (ends) w.load(from);
+                }
+                // A result may lie over its source, and the row's lanes read each other's channels: all of them are one wave's, and none of it stores before all have read.
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                __builtin_amdgcn_wave_barrier();
+                if (mine) {
                     u.get(x);
                     if (adj) {
 #pragma unroll
                         for (int e = 0; e < 8; ++e) y[e] = x[e ^ 1];
                     } else {
-                        const bool first_half = 8 * o < np;
-                        v.load_anywhere(from + (first_half ? 8 * o + np : 8 * o - np));
                         v.get(y);
-                        if (first_half && 8 * o + 8 > np) {
+                        if (ends) {
                             float z[8];
-                            v.load(from);
-                            v.get(z);
+                            w.get(z);
 #pragma unroll
                             for (int k = 1; k < 8; ++k)
                                 if ((np & 7) == k)
