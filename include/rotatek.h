@@ -547,7 +547,7 @@ size_t rk_window_workspace_size(const rk_ctx* ctx, const rk_layout* L, int32_t n
  * divides it is fp32).  With fp32 rows a product is of all 24 bits or leaves out less than 2^-24 of itself (of a number below 2^-100: less than 2^-125 of that number);
  * a token that sees a Key with an infinity, or holds one in its query, may get NaN even where its score would be minus infinity.  A token that sees a Value
  * with an infinity gets it in that channel, or NaN: where it sees one of the other sign or a NaN, and where its weight is less than fp32 holds.  Workspace: rk_window_workspace_size(ctx, L, n_tokens), 16-byte aligned; calls with workspaces of their own may overlap.
- * B n_tokens H_q at most 2^31 - 1, and B H_kv times the row blocks of a KV head (its rows by rk_prefill_plan's, rounded up) less than 2^24 (2^23 for fp32 in blocks of 256): UNSUPPORTED, as
+ * text->max_len at most RK_MAX_TOKENS; B n_tokens H_q at most 2^31 - 1, and B H_kv times the row blocks of a KV head (its rows by rk_prefill_plan's, rounded up) less than 2^24 (2^23 for fp32 in blocks of 256): UNSUPPORTED, as
  * more than a launch holds.  Errors: INVALID_ARG, UNSUPPORTED, CAPACITY, WORKSPACE, HIP.                         */
 rk_status rk_prefill_attn_window(rk_ctx* ctx, const rk_layout* L, const rk_heads* q, int32_t n_tokens, const int32_t* n_tokens_dev,
                                  const rk_text* text, int32_t window, int32_t sinks, float scale, const rk_heads* out, void* workspace,
@@ -563,7 +563,7 @@ rk_status rk_prefill_plan(const rk_ctx* ctx, const rk_layout* L, int32_t n_token
  * already), attends all of the rotated cache and the text rows that it sees, under ONE softmax.  k_packed and v_cache both NULL: the text alone, as
  * on a layer without a rotated cache (R_r, delta_mu and L->seq_len are not read then).  text is required.  q, out: [B,H_q,d], q 16-byte aligned.  The second
  * takes the 8-bit caches.  Workspace: rk_window_workspace_size(ctx, L, 1), 16-byte aligned; calls with workspaces of their own may overlap.  A sequence with nothing
- * to attend yields zeros.  B H_kv times splits less than 2^24, as above.  Errors: as rk_decode_attn_dual.         */
+ * to attend yields zeros.  text->max_len at most RK_MAX_TOKENS; B H_kv times splits less than 2^24, as above.  Errors: as rk_decode_attn_dual.         */
 rk_status rk_decode_attn_window(rk_ctx* ctx, const rk_layout* L, const void* q, const void* k_packed, const void* v_cache, const float* R_r,
                                 const float* delta_mu, const rk_text* text, int32_t window, int32_t sinks, float scale, void* out,
                                 void* workspace, size_t workspace_bytes, void* stream);

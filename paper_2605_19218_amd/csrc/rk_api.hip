@@ -1578,6 +1578,7 @@ static rk_status window_common(rk_ctx* ctx, const rk_layout* L, const void* q, c
         return fail(ctx, RK_ERR_CAPACITY, "attention: max_seq_len %d exceeds capacity %d", L->max_seq_len, L->capacity);
     if (!text) return fail(ctx, RK_ERR_INVALID_ARG, "decode_attn_window: text is NULL");
     if ((s = check_text(ctx, text, false)) != RK_OK) return s;
+    if (text->max_len > RK_MAX_TOKENS) return fail(ctx, RK_ERR_INVALID_ARG, "decode_attn_window: max_len exceeds %d", RK_MAX_TOKENS);
     if ((int64_t)L->batch * L->n_q_heads > INT32_MAX) return fail(ctx, RK_ERR_UNSUPPORTED, "attention: more than %d query rows", INT32_MAX);
     const size_t need = rows_ws(ctx, L, 1);
     if (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 15))

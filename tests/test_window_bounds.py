@@ -78,3 +78,10 @@ def test_more_heads_than_a_launch(ctx, f):
     assert call(65535, 256, 256, False) == NONE and call(65535, 257, 257, False) == UNS
     assert call(65535, 128, 128, True) == NONE and call(65535, 129, 129, True) == UNS          # the cache's work-group and the text's
     assert call(65535, 16 * 2047, 2047, False) == UNS and call(65535, 16 * 200, 200, False) == NONE
+
+
+@pytest.mark.parametrize("f", [rk.rk_decode_attn_window, rk.rk_decode_attn_window_quant])
+def test_longest_text(ctx, f):
+    """One token: the last rows of a text are numbered in 32 bits with a tile to spare, as a prompt's are."""
+    call = lambda n: status(f, ctx, lay(), P, None, None, None, None, text(max_len=n, capacity=2 ** 31 - 1), 4, 2, 0.0, P, P, workspace_bytes=1 << 62)
+    assert call(1 << 30) == NONE and call((1 << 30) + 1) == BAD and call(2 ** 31 - 1) == BAD
