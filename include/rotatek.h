@@ -124,7 +124,7 @@ typedef struct {
  * k and v is at data[b*stride_b + h*stride_h + t*stride_t + c], L->dtype, device
  * memory, caller-owned.  Bases 16-byte aligned and strides multiples of 8
  * elements.  Sequence b holds len[b] <= max_len rows (len device [B]; NULL =
- * max_len for every sequence, rk_decode_attn_dual only); max_len is the host's
+ * max_len for every sequence, where rows are only read); max_len is the host's
  * upper bound of them and capacity the rows allocated per (b, h).            */
 typedef struct {
     void* k;
@@ -160,7 +160,7 @@ typedef struct {
 /* Positions of several axes (of an image or a video: time, height, width; of text: one, or the same on all).  Token t of sequence b stands at
  * pos[a*stride_a + b*stride_b + t] on axis a, and pair i of a row's channels turns by the angle pos[axis[i]] * inv_freq[i], in radians: (x, y) ->
  * (x cos - y sin, x sin + y cos).  Channels from 2 n_pairs on have no position.  The angle is taken in 64 bits, so that far positions lose
- * nothing of it; products and sums are fp32, rounded once to L->dtype.                                                                            */
+ * nothing of it; what is left of a turn, sine and cosine, products and sums are fp32, rounded once to L->dtype.                                   */
 #define RK_MAX_AXES 4
 #define RK_MAX_PAIRS 64
 enum {
@@ -522,8 +522,8 @@ rk_status rk_rope(rk_ctx* ctx, const rk_layout* L, const rk_rotary* rope, int32_
  * every KV head and t < n_tokens_dev[b] (as above); len_out[b] = len[b] + the rows written, which end where the segment is full.  len_out may be text->len
  * or an array that the call does not read.  q and q_out as in rk_rope (all n_tokens_dev[b] rows), or both NULL.  One token a sequence is a decode's step, in
  * front of rk_decode_attn_window or rk_decode_attn_dual; many are a prompt, in front of rk_prefill_attn_window.  The stretch of memory from the segment's first row to its
- * last may not meet k's or v's.  No two of the segment's rows up to max_len + n_tokens may share an element, nor may text->k and text->v.  RK_ERR_CAPACITY if text->max_len + n_tokens > text->capacity (max_len bounds len[b] BEFORE the call).  Calls on
- * one context must not overlap.  Errors: INVALID_ARG, UNSUPPORTED, CAPACITY, HIP.                                */
+ * last may not meet k's or v's.  No two of the segment's rows up to max_len + n_tokens may share an element, nor may text->k and text->v (a segment that is only read may be one
+ * for all heads or sequences).  RK_ERR_CAPACITY if text->max_len + n_tokens > text->capacity (max_len bounds len[b] BEFORE the call).  Calls on one context must not overlap.  Errors: INVALID_ARG, UNSUPPORTED, CAPACITY, HIP.                                */
 rk_status rk_rope_append_text(rk_ctx* ctx, const rk_layout* L, const rk_rotary* rope, int32_t n_tokens, const int32_t* n_tokens_dev,
                               const rk_heads* q, const rk_heads* q_out, const rk_heads* k, const rk_heads* v, const rk_text* text,
                               int32_t* len_out, void* stream);
@@ -546,7 +546,9 @@ size_t rk_window_workspace_size(const rk_ctx* ctx, const rk_layout* L, int32_t n
  * Scores q . k * scale (1/sqrt(d) when `scale` <= 0).  With 16-bit rows the softmax weights enter the product with the Values as bf16 (the sum that
  * divides it is fp32).  With fp32 rows a product is of all 24 bits or leaves out less than 2^-24 of itself (of a number below 2^-100: less than 2^-125 of that number);
  * a token that sees a Key with an infinity, or holds one in its query, may get NaN even where its score would be minus infinity.  A token that sees a Value
- * with an infinity gets it in that channel, or NaN: where it sees one of the other sign or a NaN, and where its weight is less than fp32 holds.  Workspace: rk_window_workspace_size(ctx, L, n_tokens), 16-byte aligned; calls with workspaces of their own may overlap.
+ * with an infinity gets it in that channel, or NaN: where it sees one of the other sign or a NaN, and where its weight is less than fp32 holds.  Sums of Values are fp32 and of weights up to 2^8, so
+ * those of Values above 2^100 may pass its range.
+ * Workspace: rk_window_workspace_size(ctx, L, n_tokens), 16-byte aligned; calls with workspaces of their own may overlap.
  * text->max_len at most RK_MAX_TOKENS; B n_tokens H_q at most 2^31 - 1, and B H_kv times the row blocks of a KV head (its rows by rk_prefill_plan's, rounded up) less than 2^24 (2^23 for fp32 in blocks of 256): UNSUPPORTED, as
  * more than a launch holds.  Errors: INVALID_ARG, UNSUPPORTED, CAPACITY, WORKSPACE, HIP.                         */
 rk_status rk_prefill_attn_window(rk_ctx* ctx, const rk_layout* L, const rk_heads* q, int32_t n_tokens, const int32_t* n_tokens_dev,
@@ -562,7 +564,7 @@ rk_status rk_prefill_plan(const rk_ctx* ctx, const rk_layout* L, int32_t n_token
 /* rk_decode_attn_dual with a window on the text: one token a sequence, at position len[b] - 1 of the text segment (its own row is appended
  * already), attends all of the rotated cache and the text rows that it sees, under ONE softmax.  k_packed and v_cache both NULL: the text alone, as
  * on a layer without a rotated cache (R_r, delta_mu and L->seq_len are not read then).  text is required.  q, out: [B,H_q,d], q 16-byte aligned.  The second
- * takes the 8-bit caches.  Workspace: rk_window_workspace_size(ctx, L, 1), 16-byte aligned; calls with workspaces of their own may overlap.  A sequence with nothing
+ * takes the 8-bit caches.  (Over a packed bf16 cache and all of a text rk_decode_attn_dual may be faster, for one call at a time on a context.)  Workspace: rk_window_workspace_size(ctx, L, 1), 16-byte aligned; calls with workspaces of their own may overlap.  A sequence with nothing
  * to attend yields zeros.  text->max_len at most RK_MAX_TOKENS; B H_kv times splits less than 2^24, as above.  Errors: as rk_decode_attn_dual.         */
 rk_status rk_decode_attn_window(rk_ctx* ctx, const rk_layout* L, const void* q, const void* k_packed, const void* v_cache, const float* R_r,
                                 const float* delta_mu, const rk_text* text, int32_t window, int32_t sinks, float scale, void* out,

@@ -681,7 +681,7 @@ inline dim3 rows_grid(const RowsArgs& a)
 }
 
 // WIN: of the text, the one token (the last row) sees the sinks and the window, which are taken as if they were all of it.  With 16-bit rows a wave has one tile of it ahead, and asks for the first
-// before it knows the length, like the cache's: 8 units of 4 heads, 1028 rows 8.3 us a call without either, 7.5 with.  (A tile of fp32 rows is 128 registers: with a second one, or the first
+// before it knows the length, like the cache's: 8 units of 4 heads, 1028 rows 8.3 us a call without either, 7.5 with, on one box (with, on others, up to 8.7; this kernel 5.1 of them, the fold 2.3).  (A tile of fp32 rows is 128 registers: with a second one, or the first
 // from in front of the loop, accumulators are copied to make room, 4 x 8 units, 4000 rows 30.1 and 28.4 us in place of 25.7.)
 template <int FMT, int R, bool WIN = false>
 __global__ __launch_bounds__(256, FMT == ROWS_F32 ? 1 : 2) void attn_rows(typename std::conditional<WIN, WindowRowsArgs, RowsArgs>::type A)

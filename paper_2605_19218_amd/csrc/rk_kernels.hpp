@@ -131,7 +131,6 @@ struct PrefillArgs {
 hipError_t launch_prefill(int dtype, const PrefillArgs& a, hipStream_t st);
 
 // ---- rk_rope.hip ----------------------------------------------------------------
-constexpr int RK_AXES = 4;
 constexpr int ROPE_TOKENS = 8;   // of a work-group
 struct RopeArgs {
     const void *q, *k, *v;       // v (and q, k): or null

@@ -10,6 +10,8 @@
 // The tiles that a row block sees are the sinks' and those from the window's edge of its first token to its last token; only tiles on an edge are masked.
 // What a masked Value holds must not reach a sum, and a weight of 0 does not erase an infinity: in masked tiles Values that are no
 // numbers are left out of the product and added behind it, for the rows that see them.
+// With 16-bit rows a weight is rounded to one bf16 part for its product with the Values, off by 2^-8 of itself at most: a mean's error of a step of its own rounding, 0.0020 of the largest output where
+// that rounding alone makes 0.0015 to 0.0017.  Two parts, as attn_rows and attn_block have them, are half as many products again where prompts are bound by products.
 #include <type_traits>
 #include "rk_attn_block.hpp"
 
@@ -320,12 +322,12 @@ __global__ __launch_bounds__(256, 2) void attn_prompt_f32(PrefillArgs A)
 // large ones leave out less than 2^-24 of the product: 96 instructions of 32 cycles for a tile in place of 128 of 64. Queries are in parts once, weights in registers, Keys and
 // Values on their way into LDS, once for the 256 rows of the eight waves: each thread asks for eight channels of a Key and of a Value a stage ahead (into a place of its own in LDS), and
 // writes their parts for all. Of the two waves of a SIMD one does that in front of its products, the other behind them.
-// 8 x 28 heads, 500 tokens on 8000 2240 us, 211 TFLOP/s, 1270 of issued products: what a large bf16 matrix product reaches here. 32 heads x 2944 tokens 417 us, 170 TFLOP/s, where
+// 8 x 28 heads, 500 tokens on 8000 2325 us, 204 TFLOP/s, 1220 of issued products: what a large bf16 matrix product reaches here. 32 heads x 2944 tokens 417 to 424 us, 169 TFLOP/s, where
 // the work-groups, one a compute unit and some three times as long as others, leave a fifth of the compute units' time unused.
 // What that holds for: numbers from 2^-100 on (of smaller ones, parts below the smallest normal number may count as 0, less than 2^-125 of the number in all). Above the largest bf16
 // number the first part is rounded towards zero (2^-23 of a product left out there), and an infinity has no other parts, so that finite numbers have finite parts. An infinity times a part of 0 is NaN:
 // Values that are no numbers are left out in every stage and join the rows that see them behind the loop, as on edges in the other kernels; for Keys and queries the header says it.
-// (Looking for such numbers costs 1 %: 32 heads x 2944 tokens 408 -> 413 us.)
+// (Looking for such numbers costs 1.5 %: 32 heads x 2944 tokens 410 -> 417 us, 8 x 28 heads, 500 tokens on 8000 2290 -> 2325.)
 constexpr int PARTS_ROWS = 256, PARTS_TOKENS = 32, PARTS_PLANE = PARTS_TOKENS * 256, PARTS_STAGE = 6 * PARTS_PLANE, PARTS_RAW = 2 * PARTS_STAGE,
               PARTS_LDS = PARTS_RAW + 8 * 4096;        // planes [stage][Keys 3, Values 3]; eight waves' own places; and a flag
 
